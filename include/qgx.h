@@ -335,6 +335,118 @@ qgx_status qgx_state_import(qgx_ctx* ctx, const float* Y, const float* anchor, d
 qgx_status qgx_average_reset(qgx_ctx* ctx, int on, void* stream);
 qgx_status qgx_average_export(qgx_ctx* ctx, float* X_bar, uint64_t* count, void* stream);
 
+/* ---- Between a model's backward pass and the dual vectors ---------------------------------------------------
+ * The calls below are what a trainer does right before CODE o Q: its parameters are runs of the iterate X [d], their
+ * gradients runs of the workers' rows of V [K][d].  Tensors hold one of the types qgx_dtype, parameters and their
+ * gradients binary32; all arithmetic is in binary32 or more, a result in a narrower type is rounded once, at its
+ * store.  Strides count elements; pointers need the alignment of their elements only.  The calls enqueue work and
+ * allocate nothing; scratch is the caller's, so that calls on several streams do not meet in it, and its contents
+ * need not be kept from one call to the next. */
+typedef enum { QGX_F32 = 0, QGX_F16 = 1, QGX_BF16 = 2 } qgx_dtype;
+
+/* One gradient tensor of all K workers: worker k's n elements start at data + k * stride and belong at
+ * V[k][offset .. offset + n). */
+typedef struct {
+    void* data;       /* DEVICE */
+    uint64_t n;       /* elements per worker; 0: nothing */
+    uint64_t stride;  /* from one worker's elements to the next's */
+    uint64_t offset;
+    int32_t dtype;    /* qgx_dtype */
+} qgx_tensor;
+
+/* A list of them on the device, made by qgx_tensor_list_set in memory of the caller's.  It serves one stream at a time:
+ * the table holds the clipping's partial sums as well.  The fields are the library's. */
+typedef struct {
+    void* table;          /* DEVICE, 16-byte aligned */
+    uint64_t table_bytes;
+    uint64_t n_pieces;    /* runs the tensors are cut into, per worker */
+    uint32_t n_tensors;
+    uint32_t shared_rows; /* workers share elements of a tensor (stride < n): not to be written */
+} qgx_tensor_list;
+
+/* Bytes a table of these tensors needs.  Host-side only. */
+qgx_status qgx_tensor_list_size(qgx_ctx* ctx, const qgx_tensor* tensors /* HOST */, uint32_t n_tensors, uint64_t* bytes);
+/* Fills the table (enqueued on `stream`; `tensors` may go when the call returns) and *list.  The ranges
+ * offset .. offset + n must lie in [0, d) and may not overlap; a list of no tensors is one. */
+qgx_status qgx_tensor_list_set(qgx_ctx* ctx, const qgx_tensor* tensors /* HOST */, uint32_t n_tensors, void* table,
+                               uint64_t table_bytes, qgx_tensor_list* list, void* stream);
+
+/* Worker k's global gradient norm over all tensors of the list, N_k = ||(all its elements)||_2 (QGX_NORM_L2, squares
+ * summed in binary64 in a fixed order) or its largest magnitude (QGX_NORM_LINF), and clipping: every element is
+ * multiplied by max_norm / N_k (in binary64, rounded to binary32) where N_k > max_norm, and is passed on unchanged where it is
+ * not, or where N_k is no finite number (then QGX_EBIT_NONFINITE is set as well, as CODE o Q would).
+ *   V      DEVICE [K][d]: tensors are gathered into it as binary32 (coordinates that belong to no tensor stay as they
+ *          are); it may be the memory of a tensor of the list that lies there as it does in V, and overlaps no other.
+ *          NULL: the tensors are clipped in place, rounded to their own types.
+ *   norms  DEVICE [K] binary32 or NULL: the N_k
+ * max_norm >= 0; infinity only measures (and gathers). */
+qgx_status qgx_clip_gradients(qgx_ctx* ctx, const qgx_tensor_list* list, int norm, float max_norm, float* V,
+                              float* norms, void* stream);
+
+/* Layer norm of workers x rows rows of cols elements, row r of worker k at x + k * x_worker + r * x_row (the elements of a
+ * row are contiguous): y = (x - mean) * rstd * weight + bias, mean the row's mean, rstd = 1 / sqrt(variance + eps), the
+ * variance that of the cols elements about their mean (two passes over registers, not E x^2 - mean^2).
+ *   weight, bias  DEVICE [cols] binary32, each or both NULL (1 and 0)
+ *   y             DEVICE, same type, may be x; rows may not overlap
+ *   mean, rstd    DEVICE [workers][rows] binary32 for the backward pass, each or both NULL
+ * workers or rows 0: nothing is done.  1 <= cols <= 2^24; workers * rows < 2^31. */
+qgx_status qgx_layer_norm(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, const void* x,
+                          uint64_t x_worker, uint64_t x_row, const float* weight, const float* bias, float eps, void* y,
+                          uint64_t y_worker, uint64_t y_row, float* mean, float* rstd, void* stream);
+
+/* Its backward pass.  With h = (x - mean) * rstd and g = dy * weight:
+ *   dx  = rstd * (g - mean over the row of g - h * mean over the row of g h)      DEVICE, the type of x, or NULL
+ *   dweight_k = sum over worker k's rows of dy h, dbias_k = sum of dy             DEVICE binary32, each or NULL:
+ *         worker k's cols sums at dweight + k * param_stride (a run of the rows of V: param_stride = d), written, not added
+ *         to.  The order of the sums is fixed by the sizes and the device, so results repeat bit for bit.
+ * weight may be NULL (1); mean and rstd are the forward pass's.  dx may not be dy or x.  rows 0: the sums are 0.
+ * scratch: DEVICE, 16-byte aligned, of the bytes qgx_layer_norm_scratch reports (0: may be NULL). */
+qgx_status qgx_layer_norm_scratch(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, uint64_t* bytes);
+qgx_status qgx_layer_norm_backward(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols,
+                                   const void* dy, uint64_t dy_worker, uint64_t dy_row, const void* x, uint64_t x_worker,
+                                   uint64_t x_row, const float* weight, const float* mean, const float* rstd, void* dx,
+                                   uint64_t dx_worker, uint64_t dx_row, float* dweight, float* dbias, uint64_t param_stride,
+                                   void* scratch, uint64_t scratch_bytes, void* stream);
+
+/* Buckets of the relative position delta = key - query: interval b is bounds[b] <= delta < bounds[b + 1] and takes row
+ * rows[b] of the table; several intervals may share a row.  A delta below the first bound or from the last on is masked: keys after
+ * the query (last bound 1), or outside a window. */
+#define QGX_MAX_INTERVALS 128u
+typedef struct {
+    uint32_t n;            /* intervals, 1 .. QGX_MAX_INTERVALS */
+    const int32_t* bounds; /* HOST [n + 1], strictly ascending */
+    const uint32_t* rows;  /* HOST [n] */
+} qgx_buckets;
+
+/* Attention scores [workers][batch][heads][q][k], or gradients of them; the last dimension is contiguous. */
+typedef struct {
+    void* data;            /* DEVICE */
+    int32_t dtype;         /* qgx_dtype */
+    uint32_t heads;        /* 1 .. 65535 */
+    uint64_t workers, batch, q, k;                     /* q, k <= 2^29 */
+    uint64_t s_worker, s_batch, s_head, s_row;         /* strides */
+} qgx_scores;
+
+/* Learned relative position bias: out = in + table[row of (j - i - p)][head] for query i and key j, p = q_offset (the
+ * position of query 0 among the keys) + positions[worker * batch + n]; -infinity where j - i - p is masked, whatever `in` holds
+ * there (it is not read).  A query none of whose keys is seen has a row of -infinity.
+ *   table      DEVICE [table_rows][heads] binary32 (a run of X)
+ *   in         NULL: the bias alone, without scores; else of out's type and shape, and may be out
+ *   positions  DEVICE [workers * batch] or NULL (0): the form for single tokens of sequences of different lengths
+ * |q_offset| <= 2^30; a p beyond +-2^30 counts as that.  An out of no elements is nothing to do. */
+qgx_status qgx_position_bias(qgx_ctx* ctx, const qgx_buckets* buckets, const float* table, uint32_t table_rows,
+                             const qgx_scores* in, const qgx_scores* out, int64_t q_offset, const int32_t* positions,
+                             void* stream);
+
+/* Its gradient: dtable_k[r][head] = sum of grad over worker k's batch and all (i, j) whose delta takes row r, binary32 at
+ * dtable + k * param_stride ([table_rows][heads], a run of V's rows; written, not added to; 0 for a row that none takes).
+ * Masked places are not read.  (The gradient of the scores is grad itself.)  Results repeat bit for bit.
+ * scratch: DEVICE, 16-byte aligned, of the bytes qgx_position_bias_scratch reports (0: may be NULL). */
+qgx_status qgx_position_bias_scratch(qgx_ctx* ctx, const qgx_buckets* buckets, const qgx_scores* grad, uint64_t* bytes);
+qgx_status qgx_position_bias_backward(qgx_ctx* ctx, const qgx_buckets* buckets, const qgx_scores* grad, int64_t q_offset,
+                                      float* dtable, uint32_t table_rows, uint64_t param_stride, void* scratch,
+                                      uint64_t scratch_bytes, void* stream);
+
 /* Returns and clears the device error word (QGX_EBIT_*).  Synchronises `stream`. */
 uint32_t qgx_poll_error(qgx_ctx* ctx, void* stream);
 

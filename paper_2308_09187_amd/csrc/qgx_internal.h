@@ -255,4 +255,79 @@ constexpr uint32_t kMetricBlocks = 256;    // partial sums per worker and figure
 hipError_t launch_metrics(const float* V, const float* Vhat, uint64_t d, uint32_t K, double* partial /*[K][3][kMetricBlocks]*/,
                           double* result /*[K][3]*/, hipStream_t st);
 
+// ---- between a model's backward pass and the dual vectors (qgx_clip.hip, qgx_layer_norm.hip, qgx_position_bias.hip) ----
+struct TensorEntry {            // a tensor of a list, as the table on the device holds it
+    uint64_t data, n, stride, offset;
+    uint64_t first_piece;       // pieces of the tensors before it
+    uint32_t dtype, pad_;
+};
+constexpr uint32_t kTensorBatch = 64;      // entries that one launch brings to the device in its arguments
+struct TensorBatch {
+    TensorEntry entry[kTensorBatch];
+    uint32_t first, count;
+};
+constexpr int kClipThreads = 256;
+constexpr uint32_t kClipPiece = 8192;      // elements of a piece: the unit in which tensors are dealt to workgroups
+constexpr uint32_t kClipParts = 1024;      // most partial sums of a worker
+struct ClipArgs {
+    const TensorEntry* table;
+    double* partial;            // [K][kClipParts]
+    float* V;                   // [K][d] or null: in place
+    float* norms;               // [K] or null
+    uint64_t n_pieces, per_part, per_scale;
+    uint64_t d;
+    uint32_t n_tensors, parts;  // partial sums of a worker
+    float max_norm;
+};
+hipError_t launch_tensor_list(const TensorBatch& batch, TensorEntry* table, hipStream_t st);
+hipError_t launch_clip(const ClipArgs& a, uint32_t K, bool max_kind, Scalars* sc, hipStream_t st);
+
+struct NormArgs {
+    const void* x;
+    void* y;
+    const float* w;             // [cols] or null
+    const float* b;             // [cols] or null
+    float* mean;                // [workers][rows] or null
+    float* rstd;
+    uint64_t x_worker, x_row, y_worker, y_row;
+    uint32_t rows, n_rows, cols;   // rows of a worker, of all workers
+    float eps;
+};
+struct NormBackArgs {
+    const void* dy;
+    const void* x;
+    const float* w;
+    const float* mean;
+    const float* rstd;
+    void* dx;                   // or null
+    float* dw;                  // [workers] runs of cols, param_stride apart, or null
+    float* db;
+    uint64_t dy_worker, dy_row, x_worker, x_row, dx_worker, dx_row, param_stride;
+    uint32_t rows, n_rows, cols;
+    float* scratch;
+};
+hipError_t launch_layer_norm(int dtype, const NormArgs& a, hipStream_t st);
+uint64_t norm_back_scratch(int dtype, uint32_t workers, uint32_t rows, uint32_t cols);
+hipError_t launch_layer_norm_back(int dtype, const NormBackArgs& a, uint32_t workers, hipStream_t st);
+
+struct BucketArgs {
+    uint32_t n;
+    int32_t bounds[QGX_MAX_INTERVALS + 1];
+    uint16_t rows[QGX_MAX_INTERVALS];
+};
+struct BiasArgs {
+    const void* in;             // scores, or their gradient; null: none
+    void* out;
+    const float* table;         // [rows][heads]
+    const int32_t* positions;   // [planes / heads] or null
+    int64_t q_offset;
+    uint64_t i_worker, i_batch, i_head, i_row, o_worker, o_batch, o_head, o_row;
+    uint32_t batch, heads, q, k;
+    uint32_t planes;            // workers * batch * heads
+};
+hipError_t launch_position_bias(int dtype, const BiasArgs& a, const BucketArgs& b, hipStream_t st);
+uint64_t bias_back_scratch(int dtype, const BiasArgs& a, const BucketArgs& b, uint32_t workers);
+hipError_t launch_position_bias_back(int dtype, const BiasArgs& a, const BucketArgs& b, uint32_t workers, float* dtable,
+                                     uint32_t table_rows, uint64_t param_stride, void* scratch, hipStream_t st);
+
 }  // namespace qgx

@@ -1,5 +1,6 @@
 // Host side of the C ABI: context, validation, layout tables, launches.  No arithmetic of the
 // method happens here; every step runs in the gfx950 kernels.
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -898,6 +899,310 @@ qgx_status qgx_state_import(qgx_ctx* ctx, const float* Y, const float* anchor, d
         ctx->has_anchor = true;
     }
     QGX_HIP(ctx, launch_state_set(ctx->d_sc, S, t, ctx->lay.K, st));
+    return QGX_OK;
+}
+
+// ---- between a model's backward pass and the dual vectors -----------------------------------------------------------
+
+static uint32_t element_size(int dtype) { return dtype == QGX_F32 ? 4u : 2u; }
+static bool known_type(int dtype) { return dtype == QGX_F32 || dtype == QGX_F16 || dtype == QGX_BF16; }
+static bool aligned_to(const void* p, uint32_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1u)) == 0; }
+
+// (the partial sums come after the entries)
+static uint64_t list_entries_bytes(uint32_t n_tensors) { return ((uint64_t)n_tensors * sizeof(TensorEntry) + 15u) / 16u * 16u; }
+
+qgx_status qgx_tensor_list_size(qgx_ctx* ctx, const qgx_tensor* tensors, uint32_t n_tensors, uint64_t* bytes)
+{
+    if (!ctx || !bytes || (n_tensors && !tensors)) return fail(ctx, QGX_ERR_ARG, "qgx_tensor_list_size: null argument");
+    *bytes = list_entries_bytes(n_tensors) + (uint64_t)ctx->lay.K * kClipParts * sizeof(double);
+    return QGX_OK;
+}
+
+qgx_status qgx_tensor_list_set(qgx_ctx* ctx, const qgx_tensor* tensors, uint32_t n_tensors, void* table, uint64_t table_bytes,
+                               qgx_tensor_list* list, void* stream)
+{
+    uint64_t need = 0;
+    qgx_status s = qgx_tensor_list_size(ctx, tensors, n_tensors, &need);
+    if (s != QGX_OK) return s;
+    if (!table || !list || !aligned16(table)) return fail(ctx, QGX_ERR_ARG, "qgx_tensor_list_set: null or misaligned argument");
+    if (table_bytes < need) return fail(ctx, QGX_ERR_CAPACITY, "qgx_tensor_list_set: the table needs %llu bytes", (unsigned long long)need);
+    const uint64_t d = ctx->lay.d;
+    bool shared = false;
+    for (uint32_t i = 0; i < n_tensors; ++i) {
+        const qgx_tensor& t = tensors[i];
+        if (!known_type(t.dtype)) return fail(ctx, QGX_ERR_ARG, "tensor %u: unknown type", i);
+        if (t.n == 0) continue;
+        if (!t.data || !aligned_to(t.data, element_size(t.dtype))) return fail(ctx, QGX_ERR_ARG, "tensor %u: null or misaligned data", i);
+        if (t.n > d || t.offset > d - t.n) return fail(ctx, QGX_ERR_ARG, "tensor %u: elements beyond the %llu coordinates", i, (unsigned long long)d);
+        if (t.stride >= (1ull << 62) / ctx->lay.K) return fail(ctx, QGX_ERR_ARG, "tensor %u: stride out of range", i);
+        shared = shared || (t.stride < t.n && ctx->lay.K > 1u);
+    }
+    // ranges of V, in order; two that follow each other may not overlap
+    uint32_t* order = new (std::nothrow) uint32_t[n_tensors ? n_tensors : 1];
+    if (!order) return fail(ctx, QGX_ERR_ARG, "qgx_tensor_list_set: no memory for %u tensors", n_tensors);
+    uint32_t used = 0;
+    for (uint32_t i = 0; i < n_tensors; ++i)
+        if (tensors[i].n) order[used++] = i;
+    std::sort(order, order + used, [&](uint32_t a, uint32_t b) { return tensors[a].offset < tensors[b].offset; });
+    for (uint32_t i = 1; i < used && s == QGX_OK; ++i)
+        if (tensors[order[i]].offset < tensors[order[i - 1]].offset + tensors[order[i - 1]].n)
+            s = fail(ctx, QGX_ERR_ARG, "tensors %u and %u overlap in V", order[i - 1], order[i]);
+    delete[] order;
+    if (s != QGX_OK) return s;
+
+    TensorBatch batch{};
+    uint64_t pieces = 0;
+    for (uint32_t i = 0; i < n_tensors; ++i) {
+        const qgx_tensor& t = tensors[i];
+        batch.entry[batch.count++] = TensorEntry{(uint64_t)reinterpret_cast<uintptr_t>(t.data), t.n, t.stride, t.offset, pieces, (uint32_t)t.dtype, 0u};
+        pieces += (t.n + kClipPiece - 1u) / kClipPiece;
+        if (batch.count == kTensorBatch || i + 1u == n_tensors) {
+            QGX_HIP(ctx, launch_tensor_list(batch, (TensorEntry*)table, (hipStream_t)stream));
+            batch.first = i + 1u;
+            batch.count = 0;
+        }
+    }
+    *list = qgx_tensor_list{table, table_bytes, pieces, n_tensors, shared ? 1u : 0u};
+    return QGX_OK;
+}
+
+qgx_status qgx_clip_gradients(qgx_ctx* ctx, const qgx_tensor_list* list, int norm, float max_norm, float* V, float* norms,
+                              void* stream)
+{
+    if (!ctx || !list || !list->table) return fail(ctx, QGX_ERR_ARG, "qgx_clip_gradients: null argument");
+    if (norm != QGX_NORM_L2 && norm != QGX_NORM_LINF) return fail(ctx, QGX_ERR_ARG, "qgx_clip_gradients: the norm is L2 or L-infinity");
+    if (!(max_norm >= 0.0f)) return fail(ctx, QGX_ERR_ARG, "qgx_clip_gradients: max_norm must be >= 0");
+    if (!aligned16(V) || !aligned_to(norms, 4u)) return fail(ctx, QGX_ERR_ARG, "qgx_clip_gradients: V must be 16-byte aligned, norms 4-byte");
+    if (!V && list->shared_rows) return fail(ctx, QGX_ERR_ARG, "qgx_clip_gradients: the workers share elements, which in-place clipping would scale more than once");
+    const uint64_t entries = list_entries_bytes(list->n_tensors);
+    if (list->table_bytes < entries + (uint64_t)ctx->lay.K * kClipParts * sizeof(double))
+        return fail(ctx, QGX_ERR_CAPACITY, "qgx_clip_gradients: the list's table is too small for this context");
+    ClipArgs a{};
+    a.table = (const TensorEntry*)list->table;
+    a.partial = (double*)((char*)list->table + entries);
+    a.V = V; a.norms = norms; a.d = ctx->lay.d;
+    a.n_pieces = list->n_pieces; a.n_tensors = list->n_tensors; a.max_norm = max_norm;
+    QGX_HIP(ctx, launch_clip(a, ctx->lay.K, norm == QGX_NORM_LINF, ctx->d_sc, (hipStream_t)stream));
+    return QGX_OK;
+}
+
+// Rows of a tensor: null, misaligned, or with strides beyond what 64-bit addresses hold; rows that are written may not overlap.
+static qgx_status check_rows(qgx_ctx* ctx, const char* what, const void* p, int dtype, uint64_t workers, uint64_t rows, uint64_t cols,
+                             uint64_t worker, uint64_t row, bool written)
+{
+    if (!p || !aligned_to(p, element_size(dtype))) return fail(ctx, QGX_ERR_ARG, "%s: null or misaligned", what);
+    if (worker >= (1ull << 62) / workers || row >= (1ull << 62) / rows) return fail(ctx, QGX_ERR_ARG, "%s: stride out of range", what);
+    if (written) {
+        // either the rows of a worker lie within the step to the next worker's, or the workers of a row within that to the next row
+        const bool by_worker = (rows == 1 || row >= cols) && (workers == 1 || worker >= (rows - 1) * row + cols);
+        const bool by_row = (workers == 1 || worker >= cols) && (rows == 1 || row >= (workers - 1) * worker + cols);
+        if (!by_worker && !by_row) return fail(ctx, QGX_ERR_ARG, "%s: rows overlap", what);
+    }
+    return QGX_OK;
+}
+
+static qgx_status check_norm(qgx_ctx* ctx, const char* what, int dtype, uint64_t workers, uint64_t rows, uint64_t cols)
+{
+    if (!ctx) return QGX_ERR_ARG;
+    if (!known_type(dtype)) return fail(ctx, QGX_ERR_ARG, "%s: unknown type", what);
+    if (cols == 0 || cols > (1u << 24)) return fail(ctx, QGX_ERR_ARG, "%s: cols must be 1 .. 2^24", what);
+    if (workers > 65535u || rows >= (1ull << 31) || workers * rows >= (1ull << 31))
+        return fail(ctx, QGX_ERR_ARG, "%s: workers must be at most 65535, and workers * rows below 2^31", what);
+    return QGX_OK;
+}
+
+qgx_status qgx_layer_norm(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, const void* x, uint64_t x_worker,
+                          uint64_t x_row, const float* weight, const float* bias, float eps, void* y, uint64_t y_worker,
+                          uint64_t y_row, float* mean, float* rstd, void* stream)
+{
+    qgx_status s = check_norm(ctx, "qgx_layer_norm", dtype, workers, rows, cols);
+    if (s != QGX_OK) return s;
+    if (!(eps >= 0.0f)) return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm: eps must be >= 0");
+    if (workers == 0 || rows == 0) return QGX_OK;
+    s = check_rows(ctx, "qgx_layer_norm(x)", x, dtype, workers, rows, cols, x_worker, x_row, false);
+    if (s == QGX_OK) s = check_rows(ctx, "qgx_layer_norm(y)", y, dtype, workers, rows, cols, y_worker, y_row, true);
+    if (s != QGX_OK) return s;
+    if (x == y && ((workers > 1 && x_worker != y_worker) || (rows > 1 && x_row != y_row)))
+        return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm: y at x's memory must have its strides");
+    if (!aligned_to(weight, 4u) || !aligned_to(bias, 4u) || !aligned_to(mean, 4u) || !aligned_to(rstd, 4u))
+        return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm: binary32 buffers must be 4-byte aligned");
+    NormArgs a{};
+    a.x = x; a.y = y; a.w = weight; a.b = bias; a.mean = mean; a.rstd = rstd;
+    a.x_worker = x_worker; a.x_row = x_row; a.y_worker = y_worker; a.y_row = y_row;
+    a.rows = (uint32_t)rows; a.n_rows = (uint32_t)(workers * rows); a.cols = (uint32_t)cols; a.eps = eps;
+    QGX_HIP(ctx, launch_layer_norm(dtype, a, (hipStream_t)stream));
+    return QGX_OK;
+}
+
+qgx_status qgx_layer_norm_scratch(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, uint64_t* bytes)
+{
+    const qgx_status s = check_norm(ctx, "qgx_layer_norm_scratch", dtype, workers, rows, cols);
+    if (s != QGX_OK) return s;
+    if (!bytes) return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm_scratch: null argument");
+    *bytes = norm_back_scratch(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols);
+    return QGX_OK;
+}
+
+qgx_status qgx_layer_norm_backward(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, const void* dy,
+                                   uint64_t dy_worker, uint64_t dy_row, const void* x, uint64_t x_worker, uint64_t x_row,
+                                   const float* weight, const float* mean, const float* rstd, void* dx, uint64_t dx_worker,
+                                   uint64_t dx_row, float* dweight, float* dbias, uint64_t param_stride, void* scratch,
+                                   uint64_t scratch_bytes, void* stream)
+{
+    qgx_status s = check_norm(ctx, "qgx_layer_norm_backward", dtype, workers, rows, cols);
+    if (s != QGX_OK) return s;
+    if (workers == 0) return QGX_OK;
+    if (rows) {
+        s = check_rows(ctx, "qgx_layer_norm_backward(dy)", dy, dtype, workers, rows, cols, dy_worker, dy_row, false);
+        if (s == QGX_OK) s = check_rows(ctx, "qgx_layer_norm_backward(x)", x, dtype, workers, rows, cols, x_worker, x_row, false);
+        if (s == QGX_OK && dx) s = check_rows(ctx, "qgx_layer_norm_backward(dx)", dx, dtype, workers, rows, cols, dx_worker, dx_row, true);
+        if (s != QGX_OK) return s;
+        if (!mean || !rstd) return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm_backward: null mean or rstd");
+        if (dx && (dx == dy || dx == x)) return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm_backward: dx may not be dy or x");
+    }
+    if ((dweight || dbias) && workers > 1 && param_stride < cols)
+        return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm_backward: param_stride below cols");
+    if (param_stride >= (1ull << 62) / workers) return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm_backward: stride out of range");
+    if (!aligned_to(weight, 4u) || !aligned_to(mean, 4u) || !aligned_to(rstd, 4u) || !aligned_to(dweight, 4u) || !aligned_to(dbias, 4u))
+        return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm_backward: binary32 buffers must be 4-byte aligned");
+    const uint64_t need = norm_back_scratch(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols);
+    if (need && (!scratch || !aligned16(scratch))) return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm_backward: null or misaligned scratch");
+    if (scratch_bytes < need) return fail(ctx, QGX_ERR_CAPACITY, "qgx_layer_norm_backward: scratch needs %llu bytes", (unsigned long long)need);
+    NormBackArgs a{};
+    a.dy = dy; a.x = x; a.w = weight; a.mean = mean; a.rstd = rstd; a.dx = dx; a.dw = dweight; a.db = dbias;
+    a.dy_worker = dy_worker; a.dy_row = dy_row; a.x_worker = x_worker; a.x_row = x_row; a.dx_worker = dx_worker; a.dx_row = dx_row;
+    a.param_stride = param_stride;
+    a.rows = (uint32_t)rows; a.n_rows = (uint32_t)(workers * rows); a.cols = (uint32_t)cols;
+    a.scratch = (float*)scratch;
+    QGX_HIP(ctx, launch_layer_norm_back(dtype, a, (uint32_t)workers, (hipStream_t)stream));
+    return QGX_OK;
+}
+
+static qgx_status bucket_args(qgx_ctx* ctx, const char* what, const qgx_buckets* b, uint32_t table_rows, BucketArgs& out)
+{
+    if (!b || !b->bounds || !b->rows) return fail(ctx, QGX_ERR_ARG, "%s: null buckets", what);
+    if (b->n == 0 || b->n > QGX_MAX_INTERVALS) return fail(ctx, QGX_ERR_ARG, "%s: 1 .. %u intervals", what, QGX_MAX_INTERVALS);
+    out.n = b->n;
+    for (uint32_t i = 0; i <= b->n; ++i) {
+        if (i && b->bounds[i] <= b->bounds[i - 1]) return fail(ctx, QGX_ERR_ARG, "%s: bounds not strictly ascending at %u", what, i);
+        out.bounds[i] = b->bounds[i];
+        if (i == b->n) break;
+        if (b->rows[i] >= table_rows) return fail(ctx, QGX_ERR_ARG, "%s: interval %u takes row %u of a table of %u", what, i, b->rows[i], table_rows);
+        out.rows[i] = (uint16_t)b->rows[i];
+    }
+    return QGX_OK;
+}
+
+static bool no_scores(const qgx_scores* s) { return s->workers == 0 || s->batch == 0 || s->q == 0 || s->k == 0; }
+
+// The shape is one the kernels' 32-bit counts hold, and the addresses fit 64 bits.
+static qgx_status check_scores(qgx_ctx* ctx, const char* what, const qgx_scores* s, bool written)
+{
+    if (!known_type(s->dtype)) return fail(ctx, QGX_ERR_ARG, "%s: unknown type", what);
+    if (s->heads == 0 || s->heads > 65535u || s->q > (1u << 29) || s->k > (1u << 29) || s->workers > 65535u || s->batch >= (1ull << 31) ||
+        s->workers * s->batch * s->heads >= (1ull << 31))
+        return fail(ctx, QGX_ERR_ARG, "%s: size out of range", what);
+    if (no_scores(s)) return QGX_OK;
+    if (!s->data || !aligned_to(s->data, element_size(s->dtype))) return fail(ctx, QGX_ERR_ARG, "%s: null or misaligned scores", what);
+    const uint64_t n[4] = {s->workers, s->batch, s->heads, s->q}, st[4] = {s->s_worker, s->s_batch, s->s_head, s->s_row};
+    for (int i = 0; i < 4; ++i)
+        if (st[i] >= (1ull << 60) / n[i]) return fail(ctx, QGX_ERR_ARG, "%s: stride out of range", what);
+    if (written) {
+        // smallest stride first, every one has to step over what the ones before reach
+        uint64_t reach = s->k;
+        bool done[4] = {n[0] == 1, n[1] == 1, n[2] == 1, n[3] == 1};
+        for (;;) {
+            int at = -1;
+            for (int i = 0; i < 4; ++i)
+                if (!done[i] && (at < 0 || st[i] < st[at])) at = i;
+            if (at < 0) break;
+            if (st[at] < reach) return fail(ctx, QGX_ERR_ARG, "%s: rows overlap", what);
+            reach += (n[at] - 1) * st[at];
+            done[at] = true;
+        }
+    }
+    return QGX_OK;
+}
+
+static void in_args(BiasArgs& a, const qgx_scores* s)
+{
+    a.in = s->data;
+    a.i_worker = s->s_worker; a.i_batch = s->s_batch; a.i_head = s->s_head; a.i_row = s->s_row;
+}
+
+static void shape_args(BiasArgs& a, const qgx_scores* s)
+{
+    a.batch = (uint32_t)s->batch; a.heads = s->heads; a.q = (uint32_t)s->q; a.k = (uint32_t)s->k;
+    a.planes = (uint32_t)(s->workers * s->batch * s->heads);
+}
+
+static bool offset_ok(int64_t q_offset) { return q_offset >= -(1ll << 30) && q_offset <= (1ll << 30); }
+
+qgx_status qgx_position_bias(qgx_ctx* ctx, const qgx_buckets* buckets, const float* table, uint32_t table_rows, const qgx_scores* in,
+                             const qgx_scores* out, int64_t q_offset, const int32_t* positions, void* stream)
+{
+    if (!ctx || !table || !out) return fail(ctx, QGX_ERR_ARG, "qgx_position_bias: null argument");
+    BucketArgs b{};
+    qgx_status s = bucket_args(ctx, "qgx_position_bias", buckets, table_rows, b);
+    if (s == QGX_OK) s = check_scores(ctx, "qgx_position_bias(out)", out, true);
+    if (s != QGX_OK) return s;
+    if (table_rows > 65535u || !offset_ok(q_offset)) return fail(ctx, QGX_ERR_ARG, "qgx_position_bias: table_rows or q_offset out of range");
+    if (!aligned_to(table, 4u) || !aligned_to(positions, 4u)) return fail(ctx, QGX_ERR_ARG, "qgx_position_bias: table and positions must be 4-byte aligned");
+    BiasArgs a{};
+    if (in) {
+        s = check_scores(ctx, "qgx_position_bias(in)", in, false);
+        if (s != QGX_OK) return s;
+        if (in->dtype != out->dtype || in->workers != out->workers || in->batch != out->batch || in->heads != out->heads || in->q != out->q || in->k != out->k)
+            return fail(ctx, QGX_ERR_ARG, "qgx_position_bias: in and out differ in type or shape");
+        if (in->data == out->data && ((in->workers > 1 && in->s_worker != out->s_worker) || (in->batch > 1 && in->s_batch != out->s_batch) ||
+                                      (in->heads > 1 && in->s_head != out->s_head) || (in->q > 1 && in->s_row != out->s_row)))
+            return fail(ctx, QGX_ERR_ARG, "qgx_position_bias: out at in's memory must have its strides");
+        in_args(a, in);
+    }
+    if (no_scores(out)) return QGX_OK;
+    shape_args(a, out);
+    a.out = out->data;
+    a.o_worker = out->s_worker; a.o_batch = out->s_batch; a.o_head = out->s_head; a.o_row = out->s_row;
+    a.table = table; a.positions = positions; a.q_offset = q_offset;
+    QGX_HIP(ctx, launch_position_bias(out->dtype, a, b, (hipStream_t)stream));
+    return QGX_OK;
+}
+
+qgx_status qgx_position_bias_scratch(qgx_ctx* ctx, const qgx_buckets* buckets, const qgx_scores* grad, uint64_t* bytes)
+{
+    if (!ctx || !grad || !bytes) return fail(ctx, QGX_ERR_ARG, "qgx_position_bias_scratch: null argument");
+    BucketArgs b{};
+    qgx_status s = bucket_args(ctx, "qgx_position_bias_scratch", buckets, 65535u, b);
+    if (s == QGX_OK && !known_type(grad->dtype)) s = fail(ctx, QGX_ERR_ARG, "qgx_position_bias_scratch: unknown type");
+    if (s != QGX_OK) return s;
+    BiasArgs a{};
+    shape_args(a, grad);
+    *bytes = no_scores(grad) ? 0 : bias_back_scratch(grad->dtype, a, b, (uint32_t)grad->workers);
+    return QGX_OK;
+}
+
+qgx_status qgx_position_bias_backward(qgx_ctx* ctx, const qgx_buckets* buckets, const qgx_scores* grad, int64_t q_offset, float* dtable,
+                                      uint32_t table_rows, uint64_t param_stride, void* scratch, uint64_t scratch_bytes, void* stream)
+{
+    if (!ctx || !grad || !dtable) return fail(ctx, QGX_ERR_ARG, "qgx_position_bias_backward: null argument");
+    BucketArgs b{};
+    qgx_status s = bucket_args(ctx, "qgx_position_bias_backward", buckets, table_rows, b);
+    if (s == QGX_OK) s = check_scores(ctx, "qgx_position_bias_backward", grad, false);
+    if (s != QGX_OK) return s;
+    if (table_rows > 65535u || (uint64_t)table_rows * grad->heads >= (1u << 24) || !offset_ok(q_offset))
+        return fail(ctx, QGX_ERR_ARG, "qgx_position_bias_backward: table_rows * heads or q_offset out of range");
+    if (grad->workers > 1 && param_stride < (uint64_t)table_rows * grad->heads)
+        return fail(ctx, QGX_ERR_ARG, "qgx_position_bias_backward: param_stride below the table's size");
+    if (param_stride >= (1ull << 46) || !aligned_to(dtable, 4u)) return fail(ctx, QGX_ERR_ARG, "qgx_position_bias_backward: stride out of range or misaligned dtable");
+    if (grad->workers == 0) return QGX_OK;
+    BiasArgs a{};
+    in_args(a, grad);
+    shape_args(a, grad);
+    a.q_offset = q_offset;
+    const uint64_t need = no_scores(grad) ? 0 : bias_back_scratch(grad->dtype, a, b, (uint32_t)grad->workers);
+    if (need && (!scratch || !aligned16(scratch))) return fail(ctx, QGX_ERR_ARG, "qgx_position_bias_backward: null or misaligned scratch");
+    if (scratch_bytes < need) return fail(ctx, QGX_ERR_CAPACITY, "qgx_position_bias_backward: scratch needs %llu bytes", (unsigned long long)need);
+    QGX_HIP(ctx, launch_position_bias_back(grad->dtype, a, b, (uint32_t)grad->workers, dtable, table_rows, param_stride, scratch, (hipStream_t)stream));
     return QGX_OK;
 }
 

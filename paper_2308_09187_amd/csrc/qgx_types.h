@@ -1,0 +1,61 @@
+// Tensors of the three element types (qgx_dtype) in the kernels beside the exchange: 16 bytes at a time, as binary32.
+#pragma once
+
+#include "qgx_device.h"
+
+namespace qgx {
+
+// A piece: 16 bytes of elements, at any multiple of an element's size (global accesses of 16 bytes need no more on this
+// target: the type's alignment says so to the compiler, which then keeps them whole), so that rows of odd widths and tensors at odd
+// places take the same path as aligned ones.
+template <typename T> constexpr int kPiece = 16 / (int)sizeof(T);
+
+template <typename T> struct PieceOf { typedef T type __attribute__((ext_vector_type(kPiece<T>), aligned(sizeof(T)))); };
+
+template <typename T>
+__device__ __forceinline__ void load_piece(const T* p, float (&v)[kPiece<T>])
+{
+    const typename PieceOf<T>::type x = *reinterpret_cast<const typename PieceOf<T>::type*>(p);
+#pragma unroll
+    for (int i = 0; i < kPiece<T>; ++i) v[i] = (float)x[i];
+}
+
+template <typename T>
+__device__ __forceinline__ void store_piece(T* p, const float (&v)[kPiece<T>])
+{
+    typename PieceOf<T>::type x;
+#pragma unroll
+    for (int i = 0; i < kPiece<T>; ++i) x[i] = (T)v[i];
+    *reinterpret_cast<typename PieceOf<T>::type*>(p) = x;
+}
+
+// The same for the first n elements of a piece (any n; zeros beyond), where the rest may be no memory at all.
+template <typename T>
+__device__ __forceinline__ void load_piece(const T* p, int n, float (&v)[kPiece<T>])
+{
+    if (n >= kPiece<T>) return load_piece(p, v);
+#pragma unroll
+    for (int i = 0; i < kPiece<T>; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_piece(T* p, int n, const float (&v)[kPiece<T>])
+{
+    if (n >= kPiece<T>) return store_piece(p, v);
+#pragma unroll
+    for (int i = 0; i < kPiece<T>; ++i)
+        if (i < n) p[i] = (T)v[i];
+}
+
+// The sum of LANES neighbouring lanes (4, 16 or 64) in each of them, lanes i and i xor LANES / 2 .. 1 joined in turn.
+template <int LANES, int D = LANES / 2>
+__device__ __forceinline__ float lanes_sum(float x)
+{
+    static_assert(LANES == 4 || LANES == 16 || LANES == 64, "see xor_lane");
+    const LanePair p = lane_pair<D>(__float_as_uint(x));
+    x = __uint_as_float(p.a) + __uint_as_float(p.b);
+    if constexpr (D > 1) return lanes_sum<LANES, D / 2>(x);
+    else return x;
+}
+
+}  // namespace qgx

@@ -23,12 +23,16 @@ NORM_LINF, NORM_L2 = 0, 2
 CODE_ELIAS_OMEGA, CODE_TABLE = 0, 1
 CHUNK, SUB, SUBS, MAX_SYM, MAX_BINS = 4096, 32, 128, 127, 4096
 STATIC_MAX_CHUNKS = 65536
+MAX_INTERVALS = 128
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 EXPORTS = [
     "qgx_create", "qgx_destroy", "qgx_stream_sizes", "qgx_slot_words", "qgx_compact", "qgx_select_table", "qgx_set_levels", "qgx_get_levels", "qgx_set_code_table",
     "qgx_quantize", "qgx_encode", "qgx_quantize_encode", "qgx_decode", "qgx_decode_average", "qgx_fit_levels", "qgx_fit_code",
     "qgx_state_init", "qgx_eg_step", "qgx_eg_step_static", "qgx_average_reset", "qgx_average_export", "qgx_get_scalars", "qgx_stream_bits", "qgx_debug_set_waves_per_position", "qgx_state_export", "qgx_state_import",
     "qgx_poll_error", "qgx_last_error",
+    "qgx_tensor_list_size", "qgx_tensor_list_set", "qgx_clip_gradients", "qgx_layer_norm", "qgx_layer_norm_scratch", "qgx_layer_norm_backward",
+    "qgx_position_bias", "qgx_position_bias_scratch", "qgx_position_bias_backward",
     "qgx_game_operator", "qgx_game_dual_vectors", "qgx_quantize_encode_game", "qgx_norm2", "qgx_game_gap", "qgx_quantization_metrics",
 ]
 
@@ -55,6 +59,25 @@ class _Stream(C.Structure):
                 ("payload", C.c_void_p), ("payload_words_per_worker", C.c_uint64), ("slot_words", C.c_uint64)]
 
 
+class _Tensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("n", C.c_uint64), ("stride", C.c_uint64), ("offset", C.c_uint64), ("dtype", C.c_int32)]
+
+
+class _TensorList(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("table_bytes", C.c_uint64), ("n_pieces", C.c_uint64), ("n_tensors", C.c_uint32),
+                ("shared_rows", C.c_uint32)]
+
+
+class _Buckets(C.Structure):
+    _fields_ = [("n", C.c_uint32), ("bounds", C.POINTER(C.c_int32)), ("rows", C.POINTER(C.c_uint32))]
+
+
+class _Scores(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("heads", C.c_uint32), ("workers", C.c_uint64), ("batch", C.c_uint64),
+                ("q", C.c_uint64), ("k", C.c_uint64), ("s_worker", C.c_uint64), ("s_batch", C.c_uint64), ("s_head", C.c_uint64),
+                ("s_row", C.c_uint64)]
+
+
 _lib = None
 
 
@@ -71,6 +94,15 @@ def load():
         lib.qgx_destroy.restype = None
         lib.qgx_poll_error.restype = C.c_uint32
         lib.qgx_last_error.restype = C.c_char_p
+        u64, ptr, f32 = C.c_uint64, C.c_void_p, C.c_float    # (argument types given once: plain numbers then pass as they are)
+        lib.qgx_clip_gradients.argtypes = [ptr, ptr, C.c_int, f32, ptr, ptr, ptr]
+        lib.qgx_layer_norm.argtypes = [ptr, C.c_int, u64, u64, u64, ptr, u64, u64, ptr, ptr, f32, ptr, u64, u64, ptr, ptr, ptr]
+        lib.qgx_layer_norm_scratch.argtypes = [ptr, C.c_int, u64, u64, u64, ptr]
+        lib.qgx_layer_norm_backward.argtypes = [ptr, C.c_int, u64, u64, u64, ptr, u64, u64, ptr, u64, u64, ptr, ptr, ptr, ptr, u64, u64,
+                                                ptr, ptr, u64, ptr, u64, ptr]
+        lib.qgx_position_bias.argtypes = [ptr, ptr, ptr, C.c_uint32, ptr, ptr, C.c_int64, ptr, ptr]
+        lib.qgx_position_bias_scratch.argtypes = [ptr, ptr, ptr, ptr]
+        lib.qgx_position_bias_backward.argtypes = [ptr, ptr, ptr, C.c_int64, ptr, C.c_uint32, u64, ptr, u64, ptr]
         _lib = lib
     return _lib
 
@@ -83,6 +115,47 @@ def _stream_handle(stream):
     if stream is None:                       # the handle alone: a Stream object around it takes 3 us, a call with its launch 4.6
         return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     return C.c_void_p(stream.cuda_stream)
+
+
+def _need(ok, text):
+    if not ok:
+        raise QgxError(ERR_ARG, text)
+
+
+def _on(stream):
+    """Memory made for a call on `stream` comes from that stream's pool, so that its next use is in order after the call."""
+    return torch.cuda.stream(stream)             # (None: the current stream stays)
+
+
+def _parameter(t, shape, name):
+    """Address of a contiguous binary32 parameter, or of a run of one; None stays None."""
+    if t is None:
+        return None
+    _need(t.is_cuda and t.dtype == torch.float32 and tuple(t.shape) == shape and t.is_contiguous(), "%s: contiguous float32 of shape %s on the GPU" % (name, shape))
+    return t.data_ptr()
+
+
+def _dense_last(t):
+    return t.dim() == 0 or t.shape[-1] <= 1 or t.stride(-1) == 1
+
+
+class Buckets:
+    """Buckets of the relative position delta = key - query: interval b holds bounds[b] <= delta < bounds[b + 1] and takes
+    row rows[b] of the table; a delta outside [bounds[0], bounds[-1]) is masked."""
+
+    def __init__(self, bounds, rows):
+        _need(len(bounds) == len(rows) + 1, "Buckets: one bound more than rows")
+        self._bounds = (C.c_int32 * len(bounds))(*[int(x) for x in bounds])
+        self._rows = (C.c_uint32 * max(1, len(rows)))(*[int(x) for x in rows])
+        self._c = _Buckets(len(rows), self._bounds, self._rows)
+        self._ref = C.addressof(self._c)
+
+
+class TensorList:
+    """Gradient tensors of the K workers and where they belong in V; made by Context.tensor_list.  Holds the tensors."""
+
+    def __init__(self, tensors, table, struct):
+        self.tensors, self.table, self._c = tensors, table, struct
 
 
 class Stream:
@@ -245,6 +318,154 @@ class Context:
                                                       C.c_void_p(err.ctypes.data), C.c_void_p(nrm.ctypes.data),
                                                       _stream_handle(stream)))
         return nnz, err, nrm
+
+    # -- between a model's backward pass and the dual vectors -----------------------------------------
+    def tensor_list(self, tensors, offsets=None, stream=None):
+        """The K workers' gradient tensors, each [K, n] or [n] for K = 1 (rows contiguous, any step between them), for
+        clip_gradients.  offsets[i]: where tensor i's elements belong in a worker's row of V; None: one after the other."""
+        tensors = list(tensors)
+        if offsets is None:
+            offsets, at = [], 0
+            for t in tensors:
+                offsets.append(at)
+                at += t.shape[-1] if t.dim() else 1
+        _need(len(offsets) == len(tensors), "tensor_list: an offset for every tensor")
+        arr = (_Tensor * max(1, len(tensors)))()
+        for i, (t, off) in enumerate(zip(tensors, offsets)):
+            _need(t.is_cuda and t.dtype in DTYPES, "tensor %d: float32, float16 or bfloat16 on the GPU" % i)
+            _need((t.dim() == 2 and t.shape[0] == self.K) or (t.dim() == 1 and self.K == 1), "tensor %d: shape [K, n]" % i)
+            _need(_dense_last(t), "tensor %d: a worker's elements must be contiguous" % i)
+            arr[i] = _Tensor(t.data_ptr(), t.shape[-1], t.stride(0) if t.dim() == 2 and self.K > 1 else 0, int(off), DTYPES[t.dtype])
+        need, out = C.c_uint64(), _TensorList()
+        self._check(self.lib.qgx_tensor_list_size(self._h, arr, C.c_uint32(len(tensors)), C.byref(need)))
+        with _on(stream):
+            table = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+        self._check(self.lib.qgx_tensor_list_set(self._h, arr, C.c_uint32(len(tensors)), _ptr(table), need, C.byref(out), _stream_handle(stream)))
+        return TensorList(tensors, table, out)
+
+    def clip_gradients(self, tensors: TensorList, max_norm, norm=NORM_L2, out=None, stream=None):
+        """Clips every worker's gradients to the global norm max_norm, into out = V [K, d] or, without it, in place.
+        Returns the workers' norms before, [K]."""
+        if out is not None:
+            _need(out.is_cuda and out.dtype == torch.float32 and tuple(out.shape) == (self.K, self.d) and out.is_contiguous(),
+                  "clip_gradients: out is V [K, d], contiguous float32 on the GPU")
+        with _on(stream):
+            norms = torch.empty(self.K, dtype=torch.float32, device=self.device)
+        self._check(self.lib.qgx_clip_gradients(self._h, C.addressof(tensors._c), norm, max_norm, None if out is None else out.data_ptr(),
+                                                norms.data_ptr(), _stream_handle(stream)))
+        return norms
+
+    @staticmethod
+    def _rows(t, name, like=None):
+        """(workers, rows, cols, step between workers, between rows) of [workers, rows, cols], [rows, cols] or [cols]."""
+        _need(t.is_cuda and t.dtype in DTYPES, "%s: float32, float16 or bfloat16 on the GPU" % name)
+        _need(1 <= t.dim() <= 3 and _dense_last(t), "%s: [workers, rows, cols], [rows, cols] or [cols], rows contiguous" % name)
+        _need(like is None or (t.shape == like.shape and t.dtype == like.dtype), "%s: of x's shape and type" % name)
+        sh, st = t.shape, t.stride()
+        if t.dim() == 3:
+            return sh[0], sh[1], sh[2], st[0], st[1]
+        return (1, sh[0], sh[1], 0, st[0]) if t.dim() == 2 else (1, 1, sh[0], 0, 0)
+
+    def layer_norm(self, x, weight=None, bias=None, eps=1e-5, out=None, save=True, stream=None):
+        """Layer norm over the last dimension of x.  Returns (y, mean, rstd), the last two what the backward pass takes
+        (save=False: None); weight and bias float32 [cols], runs of X say, or None."""
+        wk, rows, cols, xw, xr = self._rows(x, "x")
+        w, b = _parameter(weight, (cols,), "weight"), _parameter(bias, (cols,), "bias")
+        with _on(stream):
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+            mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if save else None
+            rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if save else None
+        _, _, _, yw, yr = self._rows(y, "out", x)
+        self._check(self.lib.qgx_layer_norm(self._h, DTYPES[x.dtype], wk, rows, cols, x.data_ptr(), xw, xr, w, b, eps, y.data_ptr(), yw, yr,
+                                            mean.data_ptr() if save else None, rstd.data_ptr() if save else None, _stream_handle(stream)))
+        return y, mean, rstd
+
+    def layer_norm_backward(self, dy, x, weight, mean, rstd, dw=None, db=None, dx=None, need_dx=True, stream=None):
+        """Returns dx (None with need_dx=False) and writes the workers' weight and bias gradients, the sums over their
+        rows, to dw and db: float32 [workers, cols], runs of V's rows say (or [cols] where x has no worker dimension)."""
+        wk, rows, cols, xw, xr = self._rows(x, "x")
+        _, _, _, gw, gr = self._rows(dy, "dy", x)
+        w = _parameter(weight, (cols,), "weight")
+        m, r = _parameter(mean, tuple(x.shape[:-1]), "mean"), _parameter(rstd, tuple(x.shape[:-1]), "rstd")
+        step = None
+        for t, name in ((dw, "dw"), (db, "db")):
+            if t is None:
+                continue
+            _need(t.is_cuda and t.dtype == torch.float32 and t.shape[-1] == cols and _dense_last(t) and
+                  ((t.dim() == 2 and t.shape[0] == wk) or (t.dim() == 1 and wk == 1)), "%s: float32 [workers, cols] on the GPU" % name)
+            s = t.stride(0) if t.dim() == 2 and wk > 1 else cols
+            _need(step in (None, s), "dw and db: one step between workers")
+            step = s
+        with _on(stream):
+            if dx is None and need_dx:
+                dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            need = C.c_uint64()
+            self._check(self.lib.qgx_layer_norm_scratch(self._h, DTYPES[x.dtype], wk, rows, cols, C.addressof(need)))
+            scratch = torch.empty(need.value, dtype=torch.uint8, device=x.device) if need.value else None
+        _, _, _, dw_, dr = (0, 0, 0, 0, 0) if dx is None else self._rows(dx, "dx", x)
+        self._check(self.lib.qgx_layer_norm_backward(
+            self._h, DTYPES[x.dtype], wk, rows, cols, dy.data_ptr(), gw, gr, x.data_ptr(), xw, xr, w, m, r,
+            None if dx is None else dx.data_ptr(), dw_, dr, None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
+            cols if step is None else step, None if scratch is None else scratch.data_ptr(), need.value, _stream_handle(stream)))
+        return dx
+
+    @staticmethod
+    def _scores(t, name):
+        """[workers, batch, heads, q, k], [batch, heads, q, k] or [heads, q, k], keys contiguous."""
+        _need(t.is_cuda and t.dtype in DTYPES, "%s: float32, float16 or bfloat16 on the GPU" % name)
+        _need(3 <= t.dim() <= 5 and _dense_last(t), "%s: [workers, batch, heads, q, k], the last dimension contiguous" % name)
+        lead = 5 - t.dim()
+        sh, st = (1,) * lead + tuple(t.shape), (0,) * lead + t.stride()
+        return _Scores(t.data_ptr(), DTYPES[t.dtype], sh[2], sh[0], sh[1], sh[3], sh[4], st[0], st[1], st[2], st[3])
+
+    def _bias(self, table, buckets, src, out, q_offset, positions, stream):
+        o = self._scores(out, "out")
+        _need(table.dim() == 2 and table.shape[1] == o.heads, "table: [rows, heads]")
+        tab = _parameter(table, tuple(table.shape), "table")
+        pos = None
+        if positions is not None:
+            _need(positions.is_cuda and positions.dtype == torch.int32 and positions.is_contiguous() and
+                  positions.numel() == o.workers * o.batch, "positions: contiguous int32, one for every sequence, on the GPU")
+            pos = positions.data_ptr()
+        i = None if src is None else self._scores(src, "scores")
+        self._check(self.lib.qgx_position_bias(self._h, buckets._ref, tab, table.shape[0], None if i is None else C.addressof(i),
+                                               C.addressof(o), q_offset, pos, _stream_handle(stream)))
+        return out
+
+    def position_bias(self, table, buckets: Buckets, q, k, dtype=torch.float32, q_offset=0, out=None, stream=None):
+        """The bias alone, [heads, q, k]: table[row of (j - i - q_offset)][head], -inf where that is masked."""
+        if out is None:
+            with _on(stream):
+                out = torch.empty((table.shape[1], q, k), dtype=dtype, device=table.device)
+        return self._bias(table, buckets, None, out, q_offset, None, stream)
+
+    def add_position_bias(self, scores, table, buckets: Buckets, q_offset=0, positions=None, out=None, stream=None):
+        """scores [.., batch, heads, q, k] plus the bias, -inf where a place is masked.  positions int32 [.., batch]: added to
+        q_offset sequence by sequence (the position of its first query).  out may be scores."""
+        if out is None:
+            with _on(stream):
+                out = torch.empty(scores.shape, dtype=scores.dtype, device=scores.device)
+        return self._bias(table, buckets, scores, out, q_offset, positions, stream)
+
+    def position_bias_backward(self, grad, buckets: Buckets, dtable, q_offset=0, stream=None):
+        """Writes the table's gradient, float32 [workers, rows, heads] (a run of V's rows say; [rows, heads] where grad has
+        no worker dimension), from the gradient of the biased scores."""
+        g = self._scores(grad, "grad")
+        _need(dtable.is_cuda and dtable.dtype == torch.float32 and dtable.dim() == (3 if grad.dim() == 5 else 2) and
+              dtable.shape[-1] == g.heads, "dtable: float32 [workers, rows, heads] on the GPU")
+        rows = dtable.shape[-2]
+        _need((rows <= 1 or dtable.stride(-2) == g.heads) and _dense_last(dtable) and (dtable.dim() == 2 or dtable.shape[0] == g.workers),
+              "dtable: a worker's table must be contiguous")
+        need = C.c_uint64()
+        self._check(self.lib.qgx_position_bias_scratch(self._h, buckets._ref, C.addressof(g), C.addressof(need)))
+        scratch = None
+        if need.value:
+            with _on(stream):
+                scratch = torch.empty(need.value, dtype=torch.uint8, device=grad.device)
+        step = dtable.stride(0) if dtable.dim() == 3 and g.workers > 1 else rows * g.heads
+        self._check(self.lib.qgx_position_bias_backward(self._h, buckets._ref, C.addressof(g), q_offset, dtable.data_ptr(), rows, step,
+                                                        None if scratch is None else scratch.data_ptr(), need.value, _stream_handle(stream)))
+        return dtable
 
     # -- DEQ o CODE and the fused updates ---------------------------------------------------------
     def decode(self, st: Stream, out=None, stream=None):
