@@ -304,11 +304,16 @@ struct NormBackArgs {
     float* db;
     uint64_t dy_worker, dy_row, x_worker, x_row, dx_worker, dx_row, param_stride;
     uint32_t rows, n_rows, cols;
-    float* scratch;
+    float* scratch;             // [workers][parts][2][sum_stride]: the workgroups' sums, of dw and of db
+    uint32_t parts, sum_stride; // filled in by the launch
 };
-hipError_t launch_layer_norm(int dtype, const NormArgs& a, hipStream_t st);
-uint64_t norm_back_scratch(int dtype, uint32_t workers, uint32_t rows, uint32_t cols);
-hipError_t launch_layer_norm_back(int dtype, const NormBackArgs& a, uint32_t workers, hipStream_t st);
+struct NormBackPlan {
+    uint32_t parts, sum_stride; // workgroups that share a worker's rows; floats of a row of sums
+    uint64_t scratch;           // bytes
+};
+hipError_t launch_layer_norm(int dtype, const NormArgs& a, uint32_t n_cu, hipStream_t st);
+NormBackPlan norm_back_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t cols, uint32_t n_cu);
+hipError_t launch_layer_norm_back(int dtype, const NormBackArgs& a, uint32_t workers, const NormBackPlan& plan, hipStream_t st);
 
 struct BucketArgs {
     uint32_t n;

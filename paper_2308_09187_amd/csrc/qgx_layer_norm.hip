@@ -1,254 +1,534 @@
 // Layer norm, forward and backward.
 //   h = (x - mean) rstd,  y = h w + b;   g = dy w,  dx = rstd (g - mean(g) - h mean(g h)),  dw = sum_rows dy h,  db = sum_rows dy
-// A row stays in registers between its sums, so that it crosses memory once; LANES threads share it.
+// A row stays in registers between its sums, so that it crosses memory once; LANES threads share it, N pieces of 16 bytes each.
+// Sums are in binary32: runs of at most N pieces one by one, then the threads' in a tree.
 #include "qgx_types.h"
 
 namespace qgx {
 
-// The sum over the LANES threads of a row, in each of them; slot: LDS of this sum's own where a row has several waves.
-template <int LANES>
-__device__ __forceinline__ float row_sum(float x, float* slot)
+template <int LANES> constexpr int kNormThreads = LANES > 256 ? LANES : 256;
+template <int LANES> constexpr int kNormGroups = kNormThreads<LANES> / LANES;     // groups of LANES threads in a workgroup
+constexpr uint32_t kNormBlocksMax = 1u << 20;             // workgroups of a launch (a grid's threads stay below 2^32); they go on from there
+
+// The sums over the LANES threads of a row, of M values at once, in each of the threads.  slot: LDS of these sums' own,
+// [M][kNormSlots], where a row has several waves; one barrier for all.
+constexpr int kNormSlots = 16;
+template <int LANES, int M>
+__device__ __forceinline__ void row_sums(float (&x)[M], float (*slot)[kNormSlots])
 {
     if constexpr (LANES <= kWave) {
-        return lanes_sum<LANES>(x);
-    } else {
-        x = lanes_sum<kWave>(x);
-        if (lane_id() == 0) slot[wave_id()] = x;
-        __syncthreads();
-        x = slot[0];
 #pragma unroll
-        for (int w = 1; w < LANES / kWave; ++w) x += slot[w];
-        return x;
+        for (int m = 0; m < M; ++m) x[m] = lanes_sum<LANES>(x[m]);
+    } else {
+#pragma unroll
+        for (int m = 0; m < M; ++m) x[m] = lanes_sum<kWave>(x[m]);
+        if (lane_id() == 0)
+#pragma unroll
+            for (int m = 0; m < M; ++m) slot[m][wave_id()] = x[m];
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            x[m] = slot[m][0];
+#pragma unroll
+            for (int w = 1; w < LANES / kWave; ++w) x[m] += slot[m][w];
+        }
     }
 }
 
-template <int LANES> constexpr int kNormThreads = LANES > 256 ? LANES : 256;
+// The place of thread `lane`'s j-th piece in a row of cols >= W columns.  A piece that would pass the row's end is moved back to
+// end there (and one that starts past it lies there too), so that every access is whole and inside the row: its first `shift`
+// columns belong to another piece.  They are left out of the row's sums; what is written for them is the same bits twice.
+struct PieceAt {
+    int c, shift;
+    bool any;                                              // some of its columns are its own
+    __device__ __forceinline__ bool owns(int i) const { return i >= shift; }
+};
 
-constexpr uint32_t kNormBlocksMax = 1u << 20;             // workgroups of a launch (a grid's threads stay below 2^32); they go on from there
-
-// The rows of a group of LANES threads: f(worker, row).
-template <int LANES, typename F>
-__device__ __forceinline__ void for_rows(uint32_t rows, uint32_t n_rows, F f)
+template <int W, int LANES>
+__device__ __forceinline__ PieceAt piece_at(int lane, int j, int cols)
 {
-    constexpr uint32_t per = kNormThreads<LANES> / LANES;
-    for (uint64_t i = (uint64_t)blockIdx.x * per + threadIdx.x / LANES; i < n_rows; i += (uint64_t)gridDim.x * per)
-        f((uint32_t)i / rows, (uint32_t)i % rows);
+    const int c0 = (lane + j * LANES) * W, c = min(c0, cols - W);
+    return PieceAt{c, c0 - c, c0 < cols};
 }
 
-template <int LANES>
-static dim3 row_grid(uint32_t n_rows)
+// The parameters of a piece's columns, `none` where there is no such vector.
+template <int W>
+__device__ __forceinline__ void load_parameters(const float* p, int c0, float none, float (&v)[W])
 {
-    constexpr uint32_t per = kNormThreads<LANES> / LANES;
-    return dim3(min((n_rows - 1u) / per + 1u, kNormBlocksMax));
+#pragma unroll
+    for (int h = 0; h < W / 4; ++h) {
+        float q[4] = {none, none, none, none};
+        if (p) load_piece(p + c0 + 4 * h, q);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[4 * h + c] = q[c];
+    }
 }
 
-template <typename T, int LANES, int N>
+// The same past whose last column there may be no memory.
+template <int W>
+__device__ __forceinline__ void load_parameters(const float* p, int c0, int cols, float none, float (&v)[W])
+{
+#pragma unroll
+    for (int c = 0; c < W; ++c) v[c] = p && c0 + c < cols ? p[c0 + c] : none;
+}
+
+// R rows to a group, one after the other in memory: the parameters are read once for them (they are 32 bytes to a piece of 16),
+// their loads are under way together, and their sums share the barriers.
+template <typename T, int LANES, int N, int R>
 __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm(NormArgs a)
 {
-    constexpr int W = kPiece<T>;
-    __shared__ float s_sum[2][16];
-    for_rows<LANES>(a.rows, a.n_rows, [&](uint32_t k, uint32_t r) {
-        const int lane = (int)(threadIdx.x % LANES), cols = (int)a.cols;
-        const T* x = (const T*)a.x + k * a.x_worker + r * a.x_row;
-        float v[N][W], sum = 0.0f, sq = 0.0f;
+    constexpr int W = kPiece<T>, kGroups = kNormGroups<LANES>;
+    __shared__ float s_sum[2][R][kNormSlots];
+    const int lane = (int)(threadIdx.x % LANES), cols = (int)a.cols;
+    PieceAt at[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int c0 = (lane + j * LANES) * W;
-            load_piece(x + c0, cols - c0, v[j]);
+    for (int j = 0; j < N; ++j) at[j] = piece_at<W, LANES>(lane, j, cols);
+    for (uint64_t first = ((uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES) * R; first < a.n_rows; first += (uint64_t)gridDim.x * kGroups * R) {
+        float v[R][N][W], sum[R], sq[R];
+        uint32_t k[R], r[R];
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            const uint32_t row = (uint32_t)min(first + q, (uint64_t)a.n_rows - 1u);      // (past the last: it again, and not written)
+            k[q] = row / a.rows;
+            r[q] = row % a.rows;
+            const T* x = (const T*)a.x + k[q] * a.x_worker + r[q] * a.x_row;
+#pragma unroll
+            for (int j = 0; j < N; ++j) load_piece(x + at[j].c, v[q][j]);
         }
 #pragma unroll
-        for (int j = 0; j < N; ++j)
+        for (int q = 0; q < R; ++q) {
+            sum[q] = 0.0f;
 #pragma unroll
-            for (int c = 0; c < W; ++c) sum += v[j][c];
-        const float mean = row_sum<LANES>(sum, s_sum[0]) / (float)cols;
+            for (int j = 0; j < N; ++j)
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int n = cols - (lane + j * LANES) * W;
-#pragma unroll
-            for (int c = 0; c < W; ++c) {
-                v[j][c] -= mean;
-                sq += c < n ? v[j][c] * v[j][c] : 0.0f;
-            }
+                for (int c = 0; c < W; ++c) sum[q] += at[j].owns(c) ? v[q][j][c] : 0.0f;
         }
-        const float rstd = 1.0f / sqrtf(row_sum<LANES>(sq, s_sum[1]) / (float)cols + a.eps);
-        T* y = (T*)a.y + k * a.y_worker + r * a.y_row;
+        row_sums<LANES>(sum, s_sum[0]);
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            const float mean = sum[q] = sum[q] / (float)cols;
+            sq[q] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int c = 0; c < W; ++c) {
+                    v[q][j][c] -= mean;
+                    const float own = at[j].owns(c) ? v[q][j][c] : 0.0f;
+                    sq[q] = fmaf(own, own, sq[q]);
+                }
+        }
+        row_sums<LANES>(sq, s_sum[1]);
+#pragma unroll
+        for (int q = 0; q < R; ++q) sq[q] = 1.0f / sqrtf(sq[q] / (float)cols + a.eps);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const int c0 = (lane + j * LANES) * W;
             float w[W], b[W];
+            load_parameters<W>(a.w, at[j].c, 1.0f, w);
+            load_parameters<W>(a.b, at[j].c, 0.0f, b);
 #pragma unroll
-            for (int c = 0; c < W; ++c) {
-                w[c] = a.w && c0 + c < cols ? a.w[c0 + c] : 1.0f;
-                b[c] = a.b && c0 + c < cols ? a.b[c0 + c] : 0.0f;
+            for (int q = 0; q < R; ++q) {
+#pragma unroll
+                for (int c = 0; c < W; ++c) v[q][j][c] = fmaf(v[q][j][c] * sq[q], w[c], b[c]);
+                if (at[j].any && first + q < a.n_rows) store_piece((T*)a.y + k[q] * a.y_worker + r[q] * a.y_row + at[j].c, v[q][j]);
             }
+        }
+        if (lane == 0)
 #pragma unroll
-            for (int c = 0; c < W; ++c) v[j][c] = v[j][c] * rstd * w[c] + b[c];
-            store_piece(y + c0, cols - c0, v[j]);
-        }
-        if (lane == 0) {
-            const size_t row = (size_t)k * a.rows + r;
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
-        }
-    });
+            for (int q = 0; q < R; ++q)
+                if (first + q < a.n_rows) {
+                    if (a.mean) a.mean[first + q] = sum[q];
+                    if (a.rstd) a.rstd[first + q] = sq[q];
+                }
+    }
 }
 
-// Rows too long for registers: read three times, twice from the cache.
-template <typename T>
-__global__ __launch_bounds__(1024) void k_layer_norm_long(NormArgs a)
+
+// Rows too long for registers, or shorter than a piece, with any ends: read three times, twice from the cache.
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_layer_norm_long(NormArgs a)
 {
-    constexpr int W = kPiece<T>, LANES = 1024;
-    __shared__ float s_sum[2][16];
-    for_rows<LANES>(a.rows, a.n_rows, [&](uint32_t k, uint32_t r) {
-        const int cols = (int)a.cols;
+    constexpr int W = kPiece<T>;
+    __shared__ float s_sum[2][1][kNormSlots];
+    const int cols = (int)a.cols;
+    for (uint32_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
+        const uint32_t k = row / a.rows, r = row % a.rows;
         const T* x = (const T*)a.x + k * a.x_worker + r * a.x_row;
         T* y = (T*)a.y + k * a.y_worker + r * a.y_row;
-        float sum = 0.0f, sq = 0.0f;
-        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += LANES * W) {
+        float sum[1] = {0.0f}, sq[1] = {0.0f};
+        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += THREADS * W) {
             float v[W];
             load_piece(x + c0, cols - c0, v);
-            for (int c = 0; c < W; ++c) sum += v[c];
+#pragma unroll
+            for (int c = 0; c < W; ++c) sum[0] += v[c];
         }
-        const float mean = row_sum<LANES>(sum, s_sum[0]) / (float)cols;
-        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += LANES * W) {
+        row_sums<THREADS>(sum, s_sum[0]);
+        const float mean = sum[0] / (float)cols;
+        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += THREADS * W) {
             float v[W];
             load_piece(x + c0, cols - c0, v);
-            for (int c = 0; c < W; ++c) sq += c0 + c < cols ? (v[c] - mean) * (v[c] - mean) : 0.0f;
+#pragma unroll
+            for (int c = 0; c < W; ++c) sq[0] += c0 + c < cols ? (v[c] - mean) * (v[c] - mean) : 0.0f;
         }
-        const float rstd = 1.0f / sqrtf(row_sum<LANES>(sq, s_sum[1]) / (float)cols + a.eps);
-        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += LANES * W) {
-            float v[W];
+        row_sums<THREADS>(sq, s_sum[1]);
+        const float rstd = 1.0f / sqrtf(sq[0] / (float)cols + a.eps);
+        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += THREADS * W) {
+            float v[W], w[W], b[W];
             load_piece(x + c0, cols - c0, v);
-            for (int c = 0; c < W; ++c) {
-                const float w = a.w && c0 + c < cols ? a.w[c0 + c] : 1.0f, b = a.b && c0 + c < cols ? a.b[c0 + c] : 0.0f;
-                v[c] = (v[c] - mean) * rstd * w + b;
-            }
+            load_parameters<W>(a.w, c0, cols, 1.0f, w);
+            load_parameters<W>(a.b, c0, cols, 0.0f, b);
+#pragma unroll
+            for (int c = 0; c < W; ++c) v[c] = fmaf((v[c] - mean) * rstd, w[c], b[c]);
             store_piece(y + c0, cols - c0, v);
         }
         if (threadIdx.x == 0) {
-            const size_t row = (size_t)k * a.rows + r;
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
-    });
-}
-
-// dx, a row per workgroup, read twice (the second time from the cache).
-template <typename T, int LANES>
-__global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_dx(NormBackArgs a)
-{
-    constexpr int W = kPiece<T>;
-    __shared__ float s_sum[2][16];
-    for_rows<LANES>(a.rows, a.n_rows, [&](uint32_t k, uint32_t r) {
-        const int lane = (int)(threadIdx.x % LANES), cols = (int)a.cols;
-        const T* x = (const T*)a.x + k * a.x_worker + r * a.x_row;
-        const T* dy = (const T*)a.dy + k * a.dy_worker + r * a.dy_row;
-        T* dx = (T*)a.dx + k * a.dx_worker + r * a.dx_row;
-        const size_t row = (size_t)k * a.rows + r;
-        const float mean = a.mean[row], rstd = a.rstd[row];
-        float s1 = 0.0f, s2 = 0.0f;
-        for (int c0 = lane * W; c0 < cols; c0 += LANES * W) {
-            float u[W], v[W];
-            load_piece(x + c0, cols - c0, u);
-            load_piece(dy + c0, cols - c0, v);
-            for (int c = 0; c < W; ++c)
-                if (c0 + c < cols) {
-                    const float g = v[c] * (a.w ? a.w[c0 + c] : 1.0f);
-                    s1 += g;
-                    s2 += g * ((u[c] - mean) * rstd);
-                }
-        }
-        s1 = row_sum<LANES>(s1, s_sum[0]) / (float)cols;
-        s2 = row_sum<LANES>(s2, s_sum[1]) / (float)cols;
-        for (int c0 = lane * W; c0 < cols; c0 += LANES * W) {
-            float u[W], v[W];
-            load_piece(x + c0, cols - c0, u);
-            load_piece(dy + c0, cols - c0, v);
-            for (int c = 0; c < W; ++c) {
-                const float g = v[c] * (a.w && c0 + c < cols ? a.w[c0 + c] : 1.0f);
-                v[c] = rstd * (g - s1 - (u[c] - mean) * rstd * s2);
-            }
-            store_piece(dx + c0, cols - c0, v);
-        }
-    });
-}
-
-// dw and db of 64 columns of a worker, four runs of its rows side by side.
-template <typename T>
-__global__ __launch_bounds__(256) void k_layer_norm_columns(NormBackArgs a)
-{
-    __shared__ float s_w[4][64], s_b[4][64];
-    const uint32_t k = blockIdx.y, c = blockIdx.x * 64u + threadIdx.x % 64u, run = threadIdx.x / 64u;
-    float dw = 0.0f, db = 0.0f;
-    if (c < a.cols)
-        for (uint32_t r = run; r < a.rows; r += 4u) {
-            const size_t row = (size_t)k * a.rows + r;
-            const float dy = (float)((const T*)a.dy + k * a.dy_worker + r * a.dy_row)[c];
-            const float x = (float)((const T*)a.x + k * a.x_worker + r * a.x_row)[c];
-            dw += dy * ((x - a.mean[row]) * a.rstd[row]);
-            db += dy;
-        }
-    s_w[run][threadIdx.x % 64u] = dw;
-    s_b[run][threadIdx.x % 64u] = db;
-    __syncthreads();
-    if (run == 0 && c < a.cols) {
-        for (int i = 1; i < 4; ++i) { dw += s_w[i][threadIdx.x]; db += s_b[i][threadIdx.x]; }
-        if (a.dw) a.dw[k * a.param_stride + c] = dw;
-        if (a.db) a.db[k * a.param_stride + c] = db;
     }
 }
 
-template <typename T, int LANES, int N>
+// ---- backward ---------------------------------------------------------------------------------------------------------
+// One pass over dy and x for all three gradients: a workgroup takes every parts-th set of rows of a worker, writes their dx and
+// keeps the columns' sums in registers (a thread has the same columns in every row).  At its end it leaves them in scratch, one row
+// of sums for each of dw and db, for k_layer_norm_join, or, where a worker has one workgroup, where they belong.
+
+// Where a workgroup's sums go: dw's and db's row of it.
+struct NormSums { float* w; float* b; };
+__device__ __forceinline__ NormSums norm_sums(const NormBackArgs& a, uint32_t k, uint32_t part)
+{
+    if (a.parts == 1u) return NormSums{a.dw ? a.dw + k * a.param_stride : nullptr, a.db ? a.db + k * a.param_stride : nullptr};
+    float* s = a.scratch + ((size_t)k * a.parts + part) * 2u * a.sum_stride;
+    return NormSums{a.dw ? s : nullptr, a.db ? s + a.sum_stride : nullptr};
+}
+
+template <typename T, int LANES, int N, int R>
+__global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBackArgs a)
+{
+    constexpr int W = kPiece<T>, kGroups = kNormGroups<LANES>;
+    __shared__ float s_sum[2][2 * R][kNormSlots];
+    __shared__ float s_cols[kGroups > 1 ? kGroups : 1][kGroups > 1 ? LANES * N * W : 1];
+    const int lane = (int)(threadIdx.x % LANES), cols = (int)a.cols, group = (int)(threadIdx.x / LANES);
+    const uint32_t k = blockIdx.y;
+    float w[N][W], dw[N][W], db[N][W];
+    PieceAt at[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        at[j] = piece_at<W, LANES>(lane, j, cols);
+        load_parameters<W>(a.w, at[j].c, 1.0f, w[j]);
+#pragma unroll
+        for (int c = 0; c < W; ++c) dw[j][c] = db[j][c] = 0.0f;
+    }
+    int turn = 0;
+    for (uint32_t set = blockIdx.x; (uint64_t)set * kGroups * R < a.rows; set += a.parts, turn ^= 1) {
+        const uint32_t first = (set * kGroups + (uint32_t)group) * R;
+        Piece<T> x[R][N], dy[R][N];
+        float mean[R], rstd[R], sum[2 * R];
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            // (in place of a row past the last: zeros)
+            const bool ok = first + q < a.rows;
+            const uint32_t r = ok ? first + q : a.rows - 1u;
+            const T* px = (const T*)a.x + k * a.x_worker + r * a.x_row;
+            const T* pg = (const T*)a.dy + k * a.dy_worker + r * a.dy_row;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                x[q][j] = *reinterpret_cast<const Piece<T>*>(px + at[j].c);
+                dy[q][j] = *reinterpret_cast<const Piece<T>*>(pg + at[j].c);
+                if (!ok) x[q][j] = dy[q][j] = (T)0.0f;
+            }
+            mean[q] = ok ? a.mean[(size_t)k * a.rows + r] : 0.0f;
+            rstd[q] = ok ? a.rstd[(size_t)k * a.rows + r] : 0.0f;
+        }
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            sum[q] = sum[R + q] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int c = 0; c < W; ++c) {
+                    const float d = (float)dy[q][j][c], g = at[j].owns(c) ? d * w[j][c] : 0.0f;
+                    const float h = ((float)x[q][j][c] - mean[q]) * rstd[q];
+                    sum[q] += g;
+                    sum[R + q] = fmaf(g, h, sum[R + q]);
+                    dw[j][c] = fmaf(d, h, dw[j][c]);
+                    db[j][c] += d;
+                }
+        }
+        if (a.dx) {
+            row_sums<LANES>(sum, s_sum[turn]);             // (two sets of slots in turn: one barrier a round)
+#pragma unroll
+            for (int q = 0; q < R; ++q) {
+                const float m1 = sum[q] / (float)cols, m2 = sum[R + q] / (float)cols;
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    float v[W];
+#pragma unroll
+                    for (int c = 0; c < W; ++c) {
+                        const float g = (float)dy[q][j][c] * w[j][c], h = ((float)x[q][j][c] - mean[q]) * rstd[q];
+                        v[c] = rstd[q] * (g - m1 - h * m2);
+                    }
+                    if (at[j].any && first + q < a.rows) store_piece((T*)a.dx + k * a.dx_worker + (first + q) * a.dx_row + at[j].c, v);
+                }
+            }
+        }
+    }
+    const NormSums out = norm_sums(a, k, blockIdx.x);
+    if constexpr (kGroups == 1) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int h = 0; h < W / 4; ++h) {              // (columns that another piece has too: the same bits)
+                const float pw[4] = {dw[j][4 * h], dw[j][4 * h + 1], dw[j][4 * h + 2], dw[j][4 * h + 3]};
+                const float pb[4] = {db[j][4 * h], db[j][4 * h + 1], db[j][4 * h + 2], db[j][4 * h + 3]};
+                if (out.w && at[j].any) store_piece(out.w + at[j].c + 4 * h, pw);
+                if (out.b && at[j].any) store_piece(out.b + at[j].c + 4 * h, pb);
+            }
+    } else {
+        // the groups' sums joined, those of dw first, then db's in the same memory
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            float* to = which ? out.b : out.w;
+            if (which) __syncthreads();
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int c = 0; c < W; ++c)
+                    if (at[j].any) s_cols[group][at[j].c + c] = which ? db[j][c] : dw[j][c];
+            __syncthreads();
+            if (to)
+                for (int c = (int)threadIdx.x; c < cols; c += kNormThreads<LANES>) {
+                    float x = s_cols[0][c];
+#pragma unroll
+                    for (int g = 1; g < kGroups; ++g) x += s_cols[g][c];
+                    to[c] = x;
+                }
+        }
+    }
+}
+
+// Rows too long for registers, or shorter than a piece: dx by itself, dy and x read a second time from the cache.
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_layer_norm_dx_long(NormBackArgs a)
+{
+    constexpr int W = kPiece<T>;
+    __shared__ float s_sum[2][2][kNormSlots];
+    const int cols = (int)a.cols;
+    int turn = 0;
+    for (uint32_t row = blockIdx.x; row < a.n_rows; row += gridDim.x, turn ^= 1) {
+        const uint32_t k = row / a.rows, r = row % a.rows;
+        const T* x = (const T*)a.x + k * a.x_worker + r * a.x_row;
+        const T* dy = (const T*)a.dy + k * a.dy_worker + r * a.dy_row;
+        T* dx = (T*)a.dx + k * a.dx_worker + r * a.dx_row;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float sum[2] = {0.0f, 0.0f};
+        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += THREADS * W) {
+            float u[W], v[W], w[W];
+            load_piece(x + c0, cols - c0, u);
+            load_piece(dy + c0, cols - c0, v);
+            load_parameters<W>(a.w, c0, cols, 1.0f, w);
+#pragma unroll
+            for (int c = 0; c < W; ++c) {
+                const float g = v[c] * w[c];
+                sum[0] += g;
+                sum[1] = fmaf(g, (u[c] - mean) * rstd, sum[1]);
+            }
+        }
+        row_sums<THREADS>(sum, s_sum[turn]);
+        const float m1 = sum[0] / (float)cols, m2 = sum[1] / (float)cols;
+        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += THREADS * W) {
+            float u[W], v[W], w[W];
+            load_piece(x + c0, cols - c0, u);
+            load_piece(dy + c0, cols - c0, v);
+            load_parameters<W>(a.w, c0, cols, 1.0f, w);
+#pragma unroll
+            for (int c = 0; c < W; ++c) v[c] = rstd * (v[c] * w[c] - m1 - (u[c] - mean) * rstd * m2);
+            store_piece(dx + c0, cols - c0, v);
+        }
+    }
+}
+
+// And their columns' sums: a thread has a piece's columns in every parts-th row of a worker.
+template <typename T>
+__global__ __launch_bounds__(256) void k_layer_norm_columns(NormBackArgs a)
+{
+    constexpr int W = kPiece<T>;
+    const uint32_t k = blockIdx.z, part = blockIdx.y;
+    const int c0 = (int)(blockIdx.x * 256u + threadIdx.x) * W, n = (int)a.cols - c0;
+    float dw[W], db[W];
+#pragma unroll
+    for (int c = 0; c < W; ++c) dw[c] = db[c] = 0.0f;
+    for (uint32_t r = part; r < a.rows; r += a.parts) {
+        float u[W], v[W];
+        load_piece((const T*)a.x + k * a.x_worker + r * a.x_row + c0, n, u);
+        load_piece((const T*)a.dy + k * a.dy_worker + r * a.dy_row + c0, n, v);
+        const float mean = a.mean[(size_t)k * a.rows + r], rstd = a.rstd[(size_t)k * a.rows + r];
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+            dw[c] = fmaf(v[c], (u[c] - mean) * rstd, dw[c]);
+            db[c] += v[c];
+        }
+    }
+    const NormSums out = norm_sums(a, k, part);
+#pragma unroll
+    for (int h = 0; h < W / 4; ++h) {
+        const float pw[4] = {dw[4 * h], dw[4 * h + 1], dw[4 * h + 2], dw[4 * h + 3]}, pb[4] = {db[4 * h], db[4 * h + 1], db[4 * h + 2], db[4 * h + 3]};
+        if (out.w) store_piece(out.w + c0 + 4 * h, n - 4 * h, pw);
+        if (out.b) store_piece(out.b + c0 + 4 * h, n - 4 * h, pb);
+    }
+}
+
+// The workgroups' sums of 64 columns joined: sixteen runs of the parts side by side, then those in order.
+__global__ __launch_bounds__(256) void k_layer_norm_join(NormBackArgs a)
+{
+    __shared__ float4 s_run[16][16];
+    const uint32_t k = blockIdx.y / 2u, which = blockIdx.y % 2u, quad = threadIdx.x % 16u, run = threadIdx.x / 16u;
+    float* out = which ? a.db : a.dw;
+    if (!out) return;
+    const uint32_t c0 = (blockIdx.x * 16u + quad) * 4u;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c0 < a.cols) {                                     // (a row of sums is whole fours of columns)
+        const float* p = a.scratch + ((size_t)k * a.parts * 2u + which) * a.sum_stride + c0;
+        for (uint32_t i = run; i < a.parts; i += 16u) {
+            const float4 x = *reinterpret_cast<const float4*>(p + (size_t)i * 2u * a.sum_stride);
+            sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+        }
+    }
+    s_run[run][quad] = sum;
+    __syncthreads();
+    if (run != 0 || c0 >= a.cols) return;
+    for (int i = 1; i < 16; ++i) {
+        const float4 x = s_run[i][quad];
+        sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+    }
+    const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+    store_piece(out + k * a.param_stride + c0, (int)(a.cols - c0), v);
+}
+
+// ---- which kernel -------------------------------------------------------------------------------------------------------
+
+template <typename T, int LANES, int N, int R>
 static hipError_t launch_norm_as(const NormArgs& a, hipStream_t st)
 {
-    hipLaunchKernelGGL((k_layer_norm<T, LANES, N>), row_grid<LANES>(a.n_rows), dim3(kNormThreads<LANES>), 0, st, a);
+    constexpr uint32_t per = kNormGroups<LANES> * R;
+    hipLaunchKernelGGL((k_layer_norm<T, LANES, N, R>), dim3(min((a.n_rows - 1u) / per + 1u, kNormBlocksMax)), dim3(kNormThreads<LANES>), 0, st, a);
     return hipGetLastError();
+}
+
+template <typename T, int LANES, int N, int R>
+static hipError_t launch_norm_by_rows(const NormArgs& a, uint32_t n_cu, hipStream_t st)
+{
+    // R rows at a time once that leaves eight workgroups for every compute unit
+    if (a.n_rows / ((uint32_t)kNormGroups<LANES> * R) >= 8u * n_cu) return launch_norm_as<T, LANES, N, R>(a, st);
+    return launch_norm_as<T, LANES, N, 1>(a, st);
 }
 
 // The fewest threads that hold a row in four pieces each.
 template <typename T>
-static hipError_t launch_norm_of(const NormArgs& a, hipStream_t st)
+static hipError_t launch_norm_of(const NormArgs& a, uint32_t n_cu, hipStream_t st)
 {
     const uint32_t pieces = (a.cols + kPiece<T> - 1u) / kPiece<T>;
-    if (pieces <= 4u) return launch_norm_as<T, 4, 1>(a, st);
-    if (pieces <= 16u) return launch_norm_as<T, 4, 4>(a, st);
-    if (pieces <= 32u) return launch_norm_as<T, 16, 2>(a, st);
-    if (pieces <= 64u) return launch_norm_as<T, 16, 4>(a, st);
-    if (pieces <= 128u) return launch_norm_as<T, 64, 2>(a, st);
-    if (pieces <= 256u) return launch_norm_as<T, 64, 4>(a, st);
-    if (pieces <= 512u) return launch_norm_as<T, 256, 2>(a, st);
-    if (pieces <= 1024u) return launch_norm_as<T, 256, 4>(a, st);
-    if (pieces <= 2048u) return launch_norm_as<T, 1024, 2>(a, st);
-    if (pieces <= 4096u) return launch_norm_as<T, 1024, 4>(a, st);
-    hipLaunchKernelGGL(k_layer_norm_long<T>, row_grid<1024>(a.n_rows), dim3(1024), 0, st, a);
+    if (a.cols < (uint32_t)kPiece<T>) {
+        hipLaunchKernelGGL((k_layer_norm_long<T, 64>), dim3(min(a.n_rows, kNormBlocksMax)), dim3(64), 0, st, a);
+        return hipGetLastError();
+    }
+    if (pieces <= 4u) return launch_norm_by_rows<T, 4, 1, 4>(a, n_cu, st);
+    if (pieces <= 16u) return launch_norm_by_rows<T, 4, 4, 2>(a, n_cu, st);
+    if (pieces <= 32u) return launch_norm_by_rows<T, 16, 2, 4>(a, n_cu, st);
+    if (pieces <= 64u) return launch_norm_by_rows<T, 16, 4, 2>(a, n_cu, st);
+    if (pieces <= 128u) return launch_norm_by_rows<T, 64, 2, 4>(a, n_cu, st);
+    if (pieces <= 256u) return launch_norm_by_rows<T, 64, 4, 2>(a, n_cu, st);
+    if (pieces <= 512u) return launch_norm_by_rows<T, 256, 2, 4>(a, n_cu, st);
+    if (pieces <= 1024u) return launch_norm_by_rows<T, 256, 4, 2>(a, n_cu, st);
+    if (pieces <= 2048u) return launch_norm_as<T, 1024, 2, 1>(a, st);
+    if (pieces <= 4096u) return launch_norm_as<T, 1024, 4, 1>(a, st);
+    hipLaunchKernelGGL((k_layer_norm_long<T, 1024>), dim3(min(a.n_rows, kNormBlocksMax)), dim3(1024), 0, st, a);
     return hipGetLastError();
 }
 
-hipError_t launch_layer_norm(int dtype, const NormArgs& a, hipStream_t st)
+hipError_t launch_layer_norm(int dtype, const NormArgs& a, uint32_t n_cu, hipStream_t st)
 {
     if (a.n_rows == 0) return hipSuccess;
-    return dtype == QGX_F32 ? launch_norm_of<float>(a, st) : dtype == QGX_F16 ? launch_norm_of<_Float16>(a, st) : launch_norm_of<__bf16>(a, st);
+    return dtype == QGX_F32   ? launch_norm_of<float>(a, n_cu, st)
+           : dtype == QGX_F16 ? launch_norm_of<_Float16>(a, n_cu, st)
+                              : launch_norm_of<__bf16>(a, n_cu, st);
+}
+
+// The backward kernel's shape for a row: threads that share one, pieces and rows of each thread; no threads: rows too long or too
+// short for it.
+struct BackShape { uint32_t lanes, pieces, rows; };
+static BackShape back_shape(uint32_t cols, uint32_t W)
+{
+    const uint32_t pieces = (cols + W - 1u) / W;
+    if (cols < W || pieces > 2048u) return BackShape{0, 0, 0};
+    if (pieces <= 4u) return BackShape{4, 1, 4};
+    if (pieces <= 16u) return pieces <= 8u ? BackShape{4, 2, 2} : BackShape{16, 1, 4};
+    if (pieces <= 64u) return pieces <= 32u ? BackShape{16, 2, 2} : BackShape{64, 1, 4};
+    if (pieces <= 128u) return BackShape{64, 2, 2};
+    if (pieces <= 256u) return BackShape{256, 1, 4};
+    if (pieces <= 512u) return BackShape{256, 2, 2};
+    if (pieces <= 1024u) return BackShape{256, 4, 1};
+    return BackShape{512, 4, 1};
+}
+
+NormBackPlan norm_back_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t cols, uint32_t n_cu)
+{
+    const uint32_t W = dtype == QGX_F32 ? 4u : 8u, pieces = (cols + W - 1u) / W;
+    const BackShape shape = back_shape(cols, W);
+    NormBackPlan p{};
+    p.sum_stride = (cols + 3u) / 4u * 4u;
+    const uint32_t at_once = shape.lanes ? max(256u, shape.lanes) / shape.lanes * shape.rows : 4u;
+    const uint32_t sets = rows / at_once + (rows % at_once != 0u);
+    // four workgroups for every compute unit, over all workers (and, where rows are long, over the columns)
+    const uint32_t want = max(1u, 4u * n_cu / (workers * (shape.lanes ? 1u : (pieces + 255u) / 256u)));
+    p.parts = max(1u, min(sets, want));
+    p.scratch = p.parts == 1u ? 0 : (uint64_t)workers * p.parts * 2u * p.sum_stride * sizeof(float);
+    return p;
+}
+
+template <typename T, int LANES, int N, int R>
+static hipError_t launch_back_as(const NormBackArgs& a, uint32_t workers, hipStream_t st)
+{
+    hipLaunchKernelGGL((k_layer_norm_back<T, LANES, N, R>), dim3(a.parts, workers), dim3(kNormThreads<LANES>), 0, st, a);
+    return hipGetLastError();
 }
 
 template <typename T>
-static hipError_t launch_norm_back_of(const NormBackArgs& a, uint32_t workers, hipStream_t st)
+static hipError_t launch_back_of(const NormBackArgs& a, uint32_t workers, hipStream_t st)
 {
+    const uint32_t pieces = (a.cols + kPiece<T> - 1u) / kPiece<T>;
+    const BackShape s = back_shape(a.cols, kPiece<T>);
+    if (s.lanes == 4u) return s.pieces == 1u ? launch_back_as<T, 4, 1, 4>(a, workers, st) : launch_back_as<T, 4, 2, 2>(a, workers, st);
+    if (s.lanes == 16u) return s.pieces == 1u ? launch_back_as<T, 16, 1, 4>(a, workers, st) : launch_back_as<T, 16, 2, 2>(a, workers, st);
+    if (s.lanes == 64u) return s.pieces == 1u ? launch_back_as<T, 64, 1, 4>(a, workers, st) : launch_back_as<T, 64, 2, 2>(a, workers, st);
+    if (s.lanes == 256u)
+        return s.pieces == 1u   ? launch_back_as<T, 256, 1, 4>(a, workers, st)
+               : s.pieces == 2u ? launch_back_as<T, 256, 2, 2>(a, workers, st)
+                                : launch_back_as<T, 256, 4, 1>(a, workers, st);
+    if (s.lanes == 512u) return launch_back_as<T, 512, 4, 1>(a, workers, st);
     if (a.dx && a.n_rows) {
-        if (a.cols <= 64u * kPiece<T>) hipLaunchKernelGGL((k_layer_norm_dx<T, 64>), row_grid<64>(a.n_rows), dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((k_layer_norm_dx<T, 256>), row_grid<256>(a.n_rows), dim3(256), 0, st, a);
+        const dim3 grid(min(a.n_rows, kNormBlocksMax));
+        if (a.cols < (uint32_t)kPiece<T>) hipLaunchKernelGGL((k_layer_norm_dx_long<T, 64>), grid, dim3(64), 0, st, a);
+        else hipLaunchKernelGGL((k_layer_norm_dx_long<T, 1024>), grid, dim3(1024), 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (a.dw || a.db) hipLaunchKernelGGL(k_layer_norm_columns<T>, dim3((a.cols + 63u) / 64u, workers), dim3(256), 0, st, a);
+    if (!a.dw && !a.db) return hipSuccess;
+    hipLaunchKernelGGL(k_layer_norm_columns<T>, dim3((pieces + 255u) / 256u, a.parts, workers), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
-uint64_t norm_back_scratch(int, uint32_t, uint32_t, uint32_t) { return 0; }
-
-hipError_t launch_layer_norm_back(int dtype, const NormBackArgs& a, uint32_t workers, hipStream_t st)
+hipError_t launch_layer_norm_back(int dtype, const NormBackArgs& args, uint32_t workers, const NormBackPlan& plan, hipStream_t st)
 {
-    return dtype == QGX_F32 ? launch_norm_back_of<float>(a, workers, st) : dtype == QGX_F16 ? launch_norm_back_of<_Float16>(a, workers, st)
-                                                                                    : launch_norm_back_of<__bf16>(a, workers, st);
+    NormBackArgs a = args;
+    a.parts = plan.parts;
+    a.sum_stride = plan.sum_stride;
+    if (!a.dx && !a.dw && !a.db) return hipSuccess;
+    const hipError_t e = dtype == QGX_F32   ? launch_back_of<float>(a, workers, st)
+                         : dtype == QGX_F16 ? launch_back_of<_Float16>(a, workers, st)
+                                            : launch_back_of<__bf16>(a, workers, st);
+    if (e != hipSuccess || a.parts == 1u || (!a.dw && !a.db)) return e;
+    hipLaunchKernelGGL(k_layer_norm_join, dim3((a.cols + 63u) / 64u, 2u * workers), dim3(256), 0, st, a);
+    return hipGetLastError();
 }
 
 }  // namespace qgx

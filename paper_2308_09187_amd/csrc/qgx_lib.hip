@@ -1030,7 +1030,7 @@ qgx_status qgx_layer_norm(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t ro
     a.x = x; a.y = y; a.w = weight; a.b = bias; a.mean = mean; a.rstd = rstd;
     a.x_worker = x_worker; a.x_row = x_row; a.y_worker = y_worker; a.y_row = y_row;
     a.rows = (uint32_t)rows; a.n_rows = (uint32_t)(workers * rows); a.cols = (uint32_t)cols; a.eps = eps;
-    QGX_HIP(ctx, launch_layer_norm(dtype, a, (hipStream_t)stream));
+    QGX_HIP(ctx, launch_layer_norm(dtype, a, ctx->n_simd / 4u, (hipStream_t)stream));
     return QGX_OK;
 }
 
@@ -1039,7 +1039,7 @@ qgx_status qgx_layer_norm_scratch(qgx_ctx* ctx, int dtype, uint64_t workers, uin
     const qgx_status s = check_norm(ctx, "qgx_layer_norm_scratch", dtype, workers, rows, cols);
     if (s != QGX_OK) return s;
     if (!bytes) return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm_scratch: null argument");
-    *bytes = norm_back_scratch(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols);
+    *bytes = workers ? norm_back_plan(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols, ctx->n_simd / 4u).scratch : 0;
     return QGX_OK;
 }
 
@@ -1065,7 +1065,8 @@ qgx_status qgx_layer_norm_backward(qgx_ctx* ctx, int dtype, uint64_t workers, ui
     if (param_stride >= (1ull << 62) / workers) return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm_backward: stride out of range");
     if (!aligned_to(weight, 4u) || !aligned_to(mean, 4u) || !aligned_to(rstd, 4u) || !aligned_to(dweight, 4u) || !aligned_to(dbias, 4u))
         return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm_backward: binary32 buffers must be 4-byte aligned");
-    const uint64_t need = norm_back_scratch(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols);
+    const NormBackPlan plan = norm_back_plan(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols, ctx->n_simd / 4u);
+    const uint64_t need = plan.scratch;
     if (need && (!scratch || !aligned16(scratch))) return fail(ctx, QGX_ERR_ARG, "qgx_layer_norm_backward: null or misaligned scratch");
     if (scratch_bytes < need) return fail(ctx, QGX_ERR_CAPACITY, "qgx_layer_norm_backward: scratch needs %llu bytes", (unsigned long long)need);
     NormBackArgs a{};
@@ -1074,7 +1075,7 @@ qgx_status qgx_layer_norm_backward(qgx_ctx* ctx, int dtype, uint64_t workers, ui
     a.param_stride = param_stride;
     a.rows = (uint32_t)rows; a.n_rows = (uint32_t)(workers * rows); a.cols = (uint32_t)cols;
     a.scratch = (float*)scratch;
-    QGX_HIP(ctx, launch_layer_norm_back(dtype, a, (uint32_t)workers, (hipStream_t)stream));
+    QGX_HIP(ctx, launch_layer_norm_back(dtype, a, (uint32_t)workers, plan, (hipStream_t)stream));
     return QGX_OK;
 }
 

@@ -12,10 +12,12 @@ template <typename T> constexpr int kPiece = 16 / (int)sizeof(T);
 
 template <typename T> struct PieceOf { typedef T type __attribute__((ext_vector_type(kPiece<T>), aligned(sizeof(T)))); };
 
+template <typename T> using Piece = typename PieceOf<T>::type;
+
 template <typename T>
 __device__ __forceinline__ void load_piece(const T* p, float (&v)[kPiece<T>])
 {
-    const typename PieceOf<T>::type x = *reinterpret_cast<const typename PieceOf<T>::type*>(p);
+    const Piece<T> x = *reinterpret_cast<const Piece<T>*>(p);
 #pragma unroll
     for (int i = 0; i < kPiece<T>; ++i) v[i] = (float)x[i];
 }
@@ -23,10 +25,10 @@ __device__ __forceinline__ void load_piece(const T* p, float (&v)[kPiece<T>])
 template <typename T>
 __device__ __forceinline__ void store_piece(T* p, const float (&v)[kPiece<T>])
 {
-    typename PieceOf<T>::type x;
+    Piece<T> x;
 #pragma unroll
     for (int i = 0; i < kPiece<T>; ++i) x[i] = (T)v[i];
-    *reinterpret_cast<typename PieceOf<T>::type*>(p) = x;
+    *reinterpret_cast<Piece<T>*>(p) = x;
 }
 
 // The same for the first n elements of a piece (any n; zeros beyond), where the rest may be no memory at all.
