@@ -423,7 +423,7 @@ typedef struct {
     void* data;            /* DEVICE */
     int32_t dtype;         /* qgx_dtype */
     uint32_t heads;        /* 1 .. 65535 */
-    uint64_t workers, batch, q, k;                     /* q, k <= 2^29 */
+    uint64_t workers, batch, q, k;                     /* q, k <= 2^29, q * k <= 2^42 */
     uint64_t s_worker, s_batch, s_head, s_row;         /* strides */
 } qgx_scores;
 
@@ -440,9 +440,10 @@ qgx_status qgx_position_bias(qgx_ctx* ctx, const qgx_buckets* buckets, const flo
 
 /* Its gradient: dtable_k[r][head] = sum of grad over worker k's batch and all (i, j) whose delta takes row r, binary32 at
  * dtable + k * param_stride ([table_rows][heads], a run of V's rows; written, not added to; 0 for a row that none takes).
- * Masked places are not read.  (The gradient of the scores is grad itself.)  Results repeat bit for bit.
+ * What masked places hold does not matter.  (The gradient of the scores is grad itself.)  Results repeat bit for bit.
  * scratch: DEVICE, 16-byte aligned, of the bytes qgx_position_bias_scratch reports (0: may be NULL). */
-qgx_status qgx_position_bias_scratch(qgx_ctx* ctx, const qgx_buckets* buckets, const qgx_scores* grad, uint64_t* bytes);
+qgx_status qgx_position_bias_scratch(qgx_ctx* ctx, const qgx_buckets* buckets, const qgx_scores* grad, int64_t q_offset,
+                                     uint64_t* bytes);
 qgx_status qgx_position_bias_backward(qgx_ctx* ctx, const qgx_buckets* buckets, const qgx_scores* grad, int64_t q_offset,
                                       float* dtable, uint32_t table_rows, uint64_t param_stride, void* scratch,
                                       uint64_t scratch_bytes, void* stream);

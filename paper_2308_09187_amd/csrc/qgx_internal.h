@@ -331,8 +331,14 @@ struct BiasArgs {
     uint32_t planes;            // workers * batch * heads
 };
 hipError_t launch_position_bias(int dtype, const BiasArgs& a, const BucketArgs& b, hipStream_t st);
-uint64_t bias_back_scratch(int dtype, const BiasArgs& a, const BucketArgs& b, uint32_t workers);
-hipError_t launch_position_bias_back(int dtype, const BiasArgs& a, const BucketArgs& b, uint32_t workers, float* dtable,
+struct BiasBackPlan {
+    int64_t first, count;       // block diagonals with a place that is not masked
+    uint64_t scratch;           // bytes: [pairs][bands * splits][intervals] sums
+    uint32_t pairs;             // workers * heads
+    uint32_t bands, splits;     // runs of 64 block diagonals; workgroups that share one
+};
+BiasBackPlan bias_back_plan(int dtype, const BiasArgs& a, const BucketArgs& b, uint32_t workers, uint32_t n_cu);
+hipError_t launch_position_bias_back(int dtype, const BiasArgs& a, const BucketArgs& b, const BiasBackPlan& plan, float* dtable,
                                      uint32_t table_rows, uint64_t param_stride, void* scratch, hipStream_t st);
 
 }  // namespace qgx

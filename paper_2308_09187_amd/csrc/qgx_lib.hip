@@ -1100,7 +1100,7 @@ static bool no_scores(const qgx_scores* s) { return s->workers == 0 || s->batch 
 static qgx_status check_scores(qgx_ctx* ctx, const char* what, const qgx_scores* s, bool written)
 {
     if (!known_type(s->dtype)) return fail(ctx, QGX_ERR_ARG, "%s: unknown type", what);
-    if (s->heads == 0 || s->heads > 65535u || s->q > (1u << 29) || s->k > (1u << 29) || s->workers > 65535u || s->batch >= (1ull << 31) ||
+    if (s->heads == 0 || s->heads > 65535u || s->q > (1u << 29) || s->k > (1u << 29) || s->q * s->k > (1ull << 42) || s->workers > 65535u || s->batch >= (1ull << 31) ||
         s->workers * s->batch * s->heads >= (1ull << 31))
         return fail(ctx, QGX_ERR_ARG, "%s: size out of range", what);
     if (no_scores(s)) return QGX_OK;
@@ -1169,16 +1169,18 @@ qgx_status qgx_position_bias(qgx_ctx* ctx, const qgx_buckets* buckets, const flo
     return QGX_OK;
 }
 
-qgx_status qgx_position_bias_scratch(qgx_ctx* ctx, const qgx_buckets* buckets, const qgx_scores* grad, uint64_t* bytes)
+qgx_status qgx_position_bias_scratch(qgx_ctx* ctx, const qgx_buckets* buckets, const qgx_scores* grad, int64_t q_offset, uint64_t* bytes)
 {
     if (!ctx || !grad || !bytes) return fail(ctx, QGX_ERR_ARG, "qgx_position_bias_scratch: null argument");
     BucketArgs b{};
     qgx_status s = bucket_args(ctx, "qgx_position_bias_scratch", buckets, 65535u, b);
-    if (s == QGX_OK && !known_type(grad->dtype)) s = fail(ctx, QGX_ERR_ARG, "qgx_position_bias_scratch: unknown type");
+    if (s == QGX_OK) s = check_scores(ctx, "qgx_position_bias_scratch", grad, false);
     if (s != QGX_OK) return s;
+    if (!offset_ok(q_offset)) return fail(ctx, QGX_ERR_ARG, "qgx_position_bias_scratch: q_offset out of range");
     BiasArgs a{};
     shape_args(a, grad);
-    *bytes = no_scores(grad) ? 0 : bias_back_scratch(grad->dtype, a, b, (uint32_t)grad->workers);
+    a.q_offset = q_offset;
+    *bytes = bias_back_plan(grad->dtype, a, b, (uint32_t)grad->workers, ctx->n_simd / 4u).scratch;
     return QGX_OK;
 }
 
@@ -1200,10 +1202,11 @@ qgx_status qgx_position_bias_backward(qgx_ctx* ctx, const qgx_buckets* buckets, 
     in_args(a, grad);
     shape_args(a, grad);
     a.q_offset = q_offset;
-    const uint64_t need = no_scores(grad) ? 0 : bias_back_scratch(grad->dtype, a, b, (uint32_t)grad->workers);
+    const BiasBackPlan plan = bias_back_plan(grad->dtype, a, b, (uint32_t)grad->workers, ctx->n_simd / 4u);
+    const uint64_t need = plan.scratch;
     if (need && (!scratch || !aligned16(scratch))) return fail(ctx, QGX_ERR_ARG, "qgx_position_bias_backward: null or misaligned scratch");
     if (scratch_bytes < need) return fail(ctx, QGX_ERR_CAPACITY, "qgx_position_bias_backward: scratch needs %llu bytes", (unsigned long long)need);
-    QGX_HIP(ctx, launch_position_bias_back(grad->dtype, a, b, (uint32_t)grad->workers, dtable, table_rows, param_stride, scratch, (hipStream_t)stream));
+    QGX_HIP(ctx, launch_position_bias_back(grad->dtype, a, b, plan, dtable, table_rows, param_stride, scratch, (hipStream_t)stream));
     return QGX_OK;
 }
 

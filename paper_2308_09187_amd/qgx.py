@@ -101,7 +101,7 @@ def load():
         lib.qgx_layer_norm_backward.argtypes = [ptr, C.c_int, u64, u64, u64, ptr, u64, u64, ptr, u64, u64, ptr, ptr, ptr, ptr, u64, u64,
                                                 ptr, ptr, u64, ptr, u64, ptr]
         lib.qgx_position_bias.argtypes = [ptr, ptr, ptr, C.c_uint32, ptr, ptr, C.c_int64, ptr, ptr]
-        lib.qgx_position_bias_scratch.argtypes = [ptr, ptr, ptr, ptr]
+        lib.qgx_position_bias_scratch.argtypes = [ptr, ptr, ptr, C.c_int64, ptr]
         lib.qgx_position_bias_backward.argtypes = [ptr, ptr, ptr, C.c_int64, ptr, C.c_uint32, u64, ptr, u64, ptr]
         _lib = lib
     return _lib
@@ -457,7 +457,7 @@ class Context:
         _need((rows <= 1 or dtable.stride(-2) == g.heads) and _dense_last(dtable) and (dtable.dim() == 2 or dtable.shape[0] == g.workers),
               "dtable: a worker's table must be contiguous")
         need = C.c_uint64()
-        self._check(self.lib.qgx_position_bias_scratch(self._h, buckets._ref, C.addressof(g), C.addressof(need)))
+        self._check(self.lib.qgx_position_bias_scratch(self._h, buckets._ref, C.addressof(g), q_offset, C.addressof(need)))
         scratch = None
         if need.value:
             with _on(stream):
