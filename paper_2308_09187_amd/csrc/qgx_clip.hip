@@ -1,199 +1,250 @@
 // Each worker's global gradient norm over its many tensors, and clipping, gathered into the dual vectors or in place.
 //   N_k = (sum over tensors and elements x^2)^(1/2), or max |x|;   c_k = N_k > M ? M / N_k : 1;   V[k][offset + i] = c_k x_i
-// Two launches: the sums of every workgroup's run of pieces, then, in every workgroup that scales, the sum of the worker's partial
-// sums again (at most kClipParts doubles from the cache) in place of a launch or a wait between the two.  Squares are summed in
-// binary64: no gradient of binary32 overflows there, and the sum's rounding does not show in the norm's 24 bits.
-// Elements are scaled in binary64 too: a factor of a few denormal bits, or none, would lose gradients that are huge but finite.
+// A launch that reads everything once and leaves a sum per workgroup, one workgroup per worker that adds those up in their order and
+// leaves the factor, and a launch that scales; where a worker's sums are few the scaling waves add them up themselves, in the same order.
+// (The last workgroup to arrive could do it, counting: but an agent-wide release and acquire in every workgroup costs 28 ns, one after
+// the other: 2048 workgroups over 33 MB took 56 us.)  The scaling launch consists of tiny workgroups, a thread moves four elements: reading
+// and writing runs at 6.5 TB/s that way and at 4.5 to 5 with workgroups that go on from tile to tile, where reads wait behind
+// the writes before them; reading alone runs at 7.2 either way (1 GiB and more).  Squares are summed in binary64: no gradient of
+// binary32 overflows there, and the sum's rounding does not show in the norm's 24 bits.  Elements are scaled in binary64 too: a
+// factor of a few denormal bits, or none, would lose gradients that are huge but finite.
 #include "qgx_types.h"
 
 namespace qgx {
 
-__global__ __launch_bounds__(64) void k_tensor_list(TensorBatch batch, TensorEntry* __restrict__ table)
+// The pieces of a batch's tensors, a thread for each.
+__global__ __launch_bounds__(256) void k_tensor_list(TensorBatch batch, TensorPiece* __restrict__ table)
 {
-    if (threadIdx.x < batch.count) table[batch.first + threadIdx.x] = batch.entry[threadIdx.x];
+    for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < batch.pieces; i += (uint64_t)gridDim.x * 256u) {
+        const uint64_t p = batch.first_piece + i;
+        uint32_t lo = 0, hi = batch.count;                 // the last tensor whose first piece is at most p (one without elements has none)
+        while (hi - lo > 1u) {
+            const uint32_t mid = (lo + hi) / 2u;
+            if (batch.entry[mid].first_piece <= p) lo = mid;
+            else hi = mid;
+        }
+        const TensorBatch::Entry& e = batch.entry[lo];
+        const uint64_t at = (p - e.first_piece) * kClipPiece, size = e.dtype == QGX_F32 ? 4u : 2u;
+        const uint32_t n = (uint32_t)min((uint64_t)kClipPiece, e.n - at);
+        table[p] = TensorPiece{e.data + at * size, e.stride * size, e.offset + (uint32_t)at, n | e.dtype << 16};
+    }
 }
 
-hipError_t launch_tensor_list(const TensorBatch& batch, TensorEntry* table, hipStream_t st)
+hipError_t launch_tensor_list(const TensorBatch& batch, TensorPiece* table, hipStream_t st)
 {
-    hipLaunchKernelGGL(k_tensor_list, dim3(1), dim3(kTensorBatch), 0, st, batch, table);
+    hipLaunchKernelGGL(k_tensor_list, dim3((uint32_t)min((batch.pieces + 255u) / 256u, (uint64_t)4096u)), dim3(256), 0, st, batch, table);
     return hipGetLastError();
 }
 
-// The tensor that piece p of the list lies in: the last entry whose first piece is at most p (tensors without elements
-// have no piece, and their successor's first piece is theirs).
-__device__ __forceinline__ uint32_t tensor_of_piece(const TensorEntry* __restrict__ table, uint32_t n_tensors, uint64_t p)
-{
-    uint32_t lo = 0, hi = n_tensors;
-    while (hi - lo > 1u) {
-        const uint32_t mid = (lo + hi) / 2u;
-        if (table[mid].first_piece <= p) lo = mid;
-        else hi = mid;
-    }
-    return lo;
-}
+template <bool MAX> struct ClipSum { double x = 0.0; };
+template <> struct ClipSum<true> { float x = 0.0f; };
 
-// f(entry, i, n): 16 bytes of the entry's elements from element i on, n of them still in the tensor; for every such run of
-// pieces [p0, p1).
-template <typename F>
-__device__ __forceinline__ void for_pieces(const TensorEntry* __restrict__ table, uint32_t n_tensors, uint64_t p0, uint64_t p1, F f)
+// A NaN among two is the result.
+template <bool MAX, typename X>
+__device__ __forceinline__ X clip_join(X a, X b)
 {
-    if (p0 >= p1) return;
-    uint32_t t = tensor_of_piece(table, n_tensors, p0);
-    for (uint64_t p = p0; p < p1;) {
-        while (t + 1u < n_tensors && table[t + 1u].first_piece <= p) ++t;
-        const TensorEntry e = table[t];
-        const uint64_t next = t + 1u < n_tensors ? table[t + 1u].first_piece : p1;
-        const uint64_t stop = next < p1 ? next : p1;
-        const uint64_t i0 = (p - e.first_piece) * kClipPiece, cut = (stop - e.first_piece) * kClipPiece, i1 = cut < e.n ? cut : e.n;
-        f(e, i0, i1);
-        p = stop;
-    }
+    if constexpr (MAX) return __builtin_elementwise_maximum(a, b);
+    else return a + b;
 }
 
 template <typename T, bool MAX>
-__device__ __forceinline__ void sum_run(const TensorEntry& e, uint32_t k, uint64_t i0, uint64_t i1, double& sum, float& big)
+__device__ __forceinline__ void sum_piece(const T* x, int n, ClipSum<MAX>& s)
 {
-    constexpr int W = kPiece<T>;
-    const T* x = reinterpret_cast<const T*>(e.data) + (uint64_t)k * e.stride;
-    for (uint64_t i = i0 + threadIdx.x * W; i < i1; i += kClipThreads * W) {
-        float v[W];
-        load_piece(x + i, (int)min((uint64_t)W, i1 - i), v);
+    constexpr int W = kPiece<T>, N = (int)kClipPiece / (kClipThreads * W);
+    Piece<T> v[N];
+    const int i0 = (int)threadIdx.x * W;
+    if (n == (int)kClipPiece) {                            // (the same for the whole workgroup: all loads are under way at once)
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = __builtin_nontemporal_load(reinterpret_cast<const Piece<T>*>(x + i0 + j * kClipThreads * W));
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = load_raw(x + i0 + j * kClipThreads * W, n - i0 - j * kClipThreads * W);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
 #pragma unroll
         for (int c = 0; c < W; ++c) {
-            if constexpr (MAX) big = __builtin_elementwise_maximum(big, fabsf(v[c]));      // (a NaN among them is the result)
-            else sum = fma((double)v[c], (double)v[c], sum);
+            const float y = (float)v[j][c];
+            if constexpr (MAX) s.x = __builtin_elementwise_maximum(s.x, fabsf(y));
+            else s.x = fma((double)y, (double)y, s.x);
         }
+}
+
+// The sum over a workgroup, in its first thread.
+template <bool MAX>
+__device__ __forceinline__ double clip_group_sum(double x, double* slot)
+{
+    if constexpr (MAX) {                                   // (binary32 values)
+        x = (double)__uint_as_float(wave_join_u32<32>(__float_as_uint((float)x), [](uint32_t a, uint32_t b) {
+            return __float_as_uint(__builtin_elementwise_maximum(__uint_as_float(a), __uint_as_float(b)));
+        }));
+    } else {
+        x = wave_sum(x);
     }
+    if (lane_id() == 0) slot[wave_id()] = x;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int w = 1; w < kClipThreads / kWave; ++w) x = clip_join<MAX>(x, slot[w]);
+    return x;
 }
 
 template <bool MAX>
 __global__ __launch_bounds__(kClipThreads) void k_clip_norm(ClipArgs a)
 {
     __shared__ double s_sum[kClipThreads / kWave];
-    __shared__ float s_big[kClipThreads / kWave];
     const uint32_t k = blockIdx.y;
-    const uint64_t p0 = blockIdx.x * a.per_part, p1 = min(p0 + a.per_part, a.n_pieces);
-    double sum = 0.0;
-    float big = 0.0f;
-    for_pieces(a.table, a.n_tensors, p0, p1, [&](const TensorEntry& e, uint64_t i0, uint64_t i1) {
-        if (e.dtype == QGX_F32) sum_run<float, MAX>(e, k, i0, i1, sum, big);
-        else if (e.dtype == QGX_F16) sum_run<_Float16, MAX>(e, k, i0, i1, sum, big);
-        else sum_run<__bf16, MAX>(e, k, i0, i1, sum, big);
-    });
-    if constexpr (MAX) {
-        big = __uint_as_float(wave_join_u32<32>(__float_as_uint(big), [](uint32_t x, uint32_t y) {
-            return __float_as_uint(__builtin_elementwise_maximum(__uint_as_float(x), __uint_as_float(y)));
-        }));
-        if (lane_id() == 0) s_big[wave_id()] = big;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int w = 1; w < kClipThreads / kWave; ++w) big = __builtin_elementwise_maximum(big, s_big[w]);
-            a.partial[(size_t)k * kClipParts + blockIdx.x] = (double)big;
-        }
-    } else {
-        sum = wave_sum(sum);
-        if (lane_id() == 0) s_sum[wave_id()] = sum;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int w = 1; w < kClipThreads / kWave; ++w) sum += s_sum[w];
-            a.partial[(size_t)k * kClipParts + blockIdx.x] = sum;
-        }
+    ClipSum<MAX> sum;
+    TensorPiece next = a.table[blockIdx.x];                // (the grid has no more workgroups than pieces)
+    for (uint64_t p = blockIdx.x; p < a.n_pieces; p += a.parts) {
+        const TensorPiece e = next;
+        next = a.table[min(p + a.parts, a.n_pieces - 1u)];
+        const void* x = reinterpret_cast<const void*>(e.data + (uint64_t)k * e.stride);
+        const int n = (int)(e.n_type & 0xFFFFu);
+        const uint32_t type = e.n_type >> 16;
+        if (type == QGX_F32) sum_piece<float, MAX>((const float*)x, n, sum);
+        else if (type == QGX_F16) sum_piece<_Float16, MAX>((const _Float16*)x, n, sum);
+        else sum_piece<__bf16, MAX>((const __bf16*)x, n, sum);
     }
+    const double x = clip_group_sum<MAX>((double)sum.x, s_sum);
+    if (threadIdx.x == 0) a.partial[(size_t)k * kClipParts + blockIdx.x] = x;
 }
+
+// A worker's norm out of its sum, and its factor.  A norm that is no finite number: the sum of squares is beyond binary64 only if an
+// element is infinite or no number.
+struct ClipFactor { double norm, scale; };
+template <bool MAX>
+__device__ __forceinline__ ClipFactor clip_factor(double sum, float max_norm)
+{
+    const double norm = MAX ? sum : sqrt(sum);
+    return ClipFactor{norm, norm < __builtin_inf() && norm > (double)max_norm ? (double)max_norm / norm : 1.0};
+}
+
+__device__ __forceinline__ void report_norm(const ClipArgs& a, uint32_t k, double norm, Scalars* sc)
+{
+    if (a.norms) a.norms[k] = (float)norm;
+    if (!(norm < __builtin_inf())) raise_error(sc, QGX_EBIT_NONFINITE);
+}
+
+// Up to kWave partial sums, in every lane of a wave.
+template <bool MAX>
+__device__ __forceinline__ double join_few(const double* __restrict__ partial, uint32_t parts)
+{
+    const double x = (uint32_t)lane_id() < parts ? partial[lane_id()] : 0.0;
+    if constexpr (!MAX) return wave_sum(x);
+    else return (double)__uint_as_float(wave_join_u32<32>(__float_as_uint((float)x), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__builtin_elementwise_maximum(__uint_as_float(a), __uint_as_float(b)));
+    }));
+}
+
+template <bool MAX>
+__global__ __launch_bounds__(kClipThreads) void k_clip_join(ClipArgs a, Scalars* sc)
+{
+    __shared__ double s_sum[kClipThreads / kWave];
+    const uint32_t k = blockIdx.x;
+    double x = 0.0;
+    for (uint32_t i = threadIdx.x; i < a.parts; i += kClipThreads) x = clip_join<MAX>(x, a.partial[(size_t)k * kClipParts + i]);
+    x = clip_group_sum<MAX>(x, s_sum);
+    if (threadIdx.x != 0) return;
+    const ClipFactor f = clip_factor<MAX>(x, a.max_norm);
+    a.scale[k] = f.scale;
+    report_norm(a, k, f.norm, sc);
+}
+
+constexpr int kScaleEach = 4;                              // elements that a thread moves at once
+constexpr uint32_t kScaleTile = kClipThreads * kScaleEach;
+constexpr uint32_t kScaleTiles = kClipPiece / kScaleTile;  // tiles of a piece
 
 template <typename T, bool GATHER>
-__device__ __forceinline__ void scale_run(const TensorEntry& e, uint32_t k, uint64_t i0, uint64_t i1, double c, float* row)
+__device__ __forceinline__ void scale_four(const TensorPiece& e, uint32_t k, int i, double c, float* to)
 {
-    constexpr int W = kPiece<T>;
-    T* x = reinterpret_cast<T*>(e.data) + (uint64_t)k * e.stride;
-    for (uint64_t i = i0 + threadIdx.x * W; i < i1; i += kClipThreads * W) {
-        float v[W];
-        const int n = (int)min((uint64_t)W, i1 - i);
-        load_piece(x + i, n, v);
+    typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    typedef float four_f __attribute__((ext_vector_type(4), aligned(4)));
+    T* x = reinterpret_cast<T*>(e.data + (uint64_t)k * e.stride) + i;
+    const int n = (int)(e.n_type & 0xFFFFu) - i;
+    if (n >= 4) {
+        const four y = __builtin_nontemporal_load(reinterpret_cast<const four*>(x));
+        four_f v;
 #pragma unroll
-        for (int q = 0; q < W; ++q) v[q] = (float)((double)v[q] * c);
+        for (int q = 0; q < 4; ++q) v[q] = (float)((double)(float)y[q] * c);
         if constexpr (GATHER) {
-            float* out = row + e.offset + i;
-#pragma unroll
-            for (int h = 0; h < W / 4; ++h) {
-                const float part[4] = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-                store_piece(out + 4 * h, n - 4 * h, part);
-            }
+            __builtin_nontemporal_store(v, reinterpret_cast<four_f*>(to + i));
         } else {
-            store_piece(x + i, n, v);
+            *reinterpret_cast<four*>(x) = four{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+        }
+    } else {
+        for (int q = 0; q < n; ++q) {
+            const float v = (float)((double)(float)x[q] * c);
+            if constexpr (GATHER) to[i + q] = v;
+            else x[q] = (T)v;
         }
     }
 }
 
-// The worker's norm from its partial sums, in every thread of the workgroup.
-template <bool MAX>
-__device__ __forceinline__ double join_parts(const double* __restrict__ partial, uint32_t parts)
-{
-    __shared__ double s_part[kClipThreads];
-    double x = 0.0;
-    for (uint32_t i = threadIdx.x; i < parts; i += kClipThreads) {
-        if constexpr (MAX) x = __builtin_elementwise_maximum(x, partial[i]);
-        else x += partial[i];
-    }
-    s_part[threadIdx.x] = x;
-    __syncthreads();
-    for (int off = kClipThreads / 2; off > 0; off >>= 1) {
-        if ((int)threadIdx.x < off) {
-            const double y = s_part[threadIdx.x + off];
-            if constexpr (MAX) s_part[threadIdx.x] = __builtin_elementwise_maximum(s_part[threadIdx.x], y);
-            else s_part[threadIdx.x] += y;
-        }
-        __syncthreads();
-    }
-    return MAX ? s_part[0] : sqrt(s_part[0]);
-}
+enum class ClipJoin { Done, Sum, Max };                     // the factor is there, or comes from the few partial sums
 
-template <bool MAX, bool GATHER>
-__global__ __launch_bounds__(kClipThreads) void k_clip_scale(ClipArgs a, Scalars* sc)
+template <bool GATHER, ClipJoin JOIN>
+__global__ __launch_bounds__(kClipThreads) void k_clip_scale(ClipArgs a, uint32_t tiles, Scalars* sc)
 {
-    const uint32_t k = blockIdx.y;
-    const double norm = join_parts<MAX>(a.partial + (size_t)k * kClipParts, a.parts);
-    // A norm that is no finite number: the sum of squares is beyond binary64 only if an element is infinite or no number.
-    const bool finite = norm < __builtin_inf();
-    const double c = finite && norm > (double)a.max_norm ? (double)a.max_norm / norm : 1.0;
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        if (a.norms) a.norms[k] = (float)norm;
-        if (!finite) raise_error(sc, QGX_EBIT_NONFINITE);
+    // from the last tile of the last worker back: part of what was read last is still in the cache
+    const uint32_t k = gridDim.y - 1u - blockIdx.y, x = tiles - 1u - blockIdx.x;
+    const TensorPiece e = a.table[x / kScaleTiles];
+    double c;
+    if constexpr (JOIN == ClipJoin::Done) {
+        c = a.scale[k];
+    } else {
+        const ClipFactor f = clip_factor<JOIN == ClipJoin::Max>(join_few<JOIN == ClipJoin::Max>(a.partial + (size_t)k * kClipParts, a.parts), a.max_norm);
+        c = f.scale;
+        if (x == 0u && threadIdx.x == 0) report_norm(a, k, f.norm, sc);
     }
     if (!GATHER && c == 1.0) return;
-    const uint64_t p0 = blockIdx.x * a.per_scale, p1 = min(p0 + a.per_scale, a.n_pieces);
-    float* row = GATHER ? a.V + (uint64_t)k * a.d : nullptr;
-    for_pieces(a.table, a.n_tensors, p0, p1, [&](const TensorEntry& e, uint64_t i0, uint64_t i1) {
-        if (e.dtype == QGX_F32) scale_run<float, GATHER>(e, k, i0, i1, c, row);
-        else if (e.dtype == QGX_F16) scale_run<_Float16, GATHER>(e, k, i0, i1, c, row);
-        else scale_run<__bf16, GATHER>(e, k, i0, i1, c, row);
-    });
+    const int i = (int)(x % kScaleTiles * kScaleTile + threadIdx.x * kScaleEach);
+    if (i >= (int)(e.n_type & 0xFFFFu)) return;
+    float* to = GATHER ? a.V + (uint64_t)k * a.d + e.offset : nullptr;
+    const uint32_t type = e.n_type >> 16;
+    if (type == QGX_F32) scale_four<float, GATHER>(e, k, i, c, to);
+    else if (type == QGX_F16) scale_four<_Float16, GATHER>(e, k, i, c, to);
+    else scale_four<__bf16, GATHER>(e, k, i, c, to);
 }
 
-hipError_t launch_clip(const ClipArgs& args, uint32_t K, bool max_kind, Scalars* sc, hipStream_t st)
+template <ClipJoin JOIN>
+static hipError_t launch_scale(ClipArgs a, uint32_t K, Scalars* sc, hipStream_t st)
+{
+    // (a grid's threads stay below 2^32: more tiles than that, of more than two million tensors, take another launch)
+    constexpr uint64_t most = 1u << 21;
+    const TensorPiece* table = a.table;
+    for (uint64_t left = a.n_pieces; left;) {
+        const uint32_t now = (uint32_t)min(left, most);
+        const dim3 grid(now * kScaleTiles, K);
+        a.table = table + (left - now);
+        if (a.V) hipLaunchKernelGGL((k_clip_scale<true, JOIN>), grid, dim3(kClipThreads), 0, st, a, now * kScaleTiles, sc);
+        else hipLaunchKernelGGL((k_clip_scale<false, JOIN>), grid, dim3(kClipThreads), 0, st, a, now * kScaleTiles, sc);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        left -= now;
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_clip(const ClipArgs& args, uint32_t K, bool max_kind, uint32_t n_cu, Scalars* sc, hipStream_t st)
 {
     ClipArgs a = args;
-    // enough workgroups to fill the GPU (eight of 256 threads per compute unit)
-    const uint64_t each = max(1u, min((uint32_t)kClipParts, (2048u + K - 1u) / K));
-    const uint64_t want = min(max(a.n_pieces, (uint64_t)1), each);
-    a.per_part = (a.n_pieces + want - 1u) / want;
-    a.parts = a.per_part ? (uint32_t)((a.n_pieces + a.per_part - 1u) / a.per_part) : 0u;
-    a.per_scale = a.per_part;
-    const dim3 grid(max(a.parts, 1u), K);
+    // eight workgroups for every compute unit over all workers
+    const uint64_t each = max(1u, min(kClipParts, 8u * n_cu / K));
+    a.parts = (uint32_t)min(a.n_pieces, each);
+    const dim3 grid(a.parts, K);
     if (a.parts) {
         if (max_kind) hipLaunchKernelGGL(k_clip_norm<true>, grid, dim3(kClipThreads), 0, st, a);
         else hipLaunchKernelGGL(k_clip_norm<false>, grid, dim3(kClipThreads), 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (a.V) {
-        if (max_kind) hipLaunchKernelGGL((k_clip_scale<true, true>), grid, dim3(kClipThreads), 0, st, a, sc);
-        else hipLaunchKernelGGL((k_clip_scale<false, true>), grid, dim3(kClipThreads), 0, st, a, sc);
-    } else {
-        if (max_kind) hipLaunchKernelGGL((k_clip_scale<true, false>), grid, dim3(kClipThreads), 0, st, a, sc);
-        else hipLaunchKernelGGL((k_clip_scale<false, false>), grid, dim3(kClipThreads), 0, st, a, sc);
-    }
-    return hipGetLastError();
+    // Few sums: a launch less.  Many: the waves' additions would outweigh it.
+    if (a.n_pieces && a.parts <= (uint32_t)kWave && a.n_pieces * kScaleTiles * K <= 16u * n_cu)
+        return max_kind ? launch_scale<ClipJoin::Max>(a, K, sc, st) : launch_scale<ClipJoin::Sum>(a, K, sc, st);
+    if (max_kind) hipLaunchKernelGGL(k_clip_join<true>, dim3(K), dim3(kClipThreads), 0, st, a, sc);
+    else hipLaunchKernelGGL(k_clip_join<false>, dim3(K), dim3(kClipThreads), 0, st, a, sc);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : launch_scale<ClipJoin::Done>(a, K, sc, st);
 }
 
 }  // namespace qgx

@@ -256,31 +256,34 @@ hipError_t launch_metrics(const float* V, const float* Vhat, uint64_t d, uint32_
                           double* result /*[K][3]*/, hipStream_t st);
 
 // ---- between a model's backward pass and the dual vectors (qgx_clip.hip, qgx_layer_norm.hip, qgx_position_bias.hip) ----
-struct TensorEntry {            // a tensor of a list, as the table on the device holds it
-    uint64_t data, n, stride, offset;
-    uint64_t first_piece;       // pieces of the tensors before it
-    uint32_t dtype, pad_;
+constexpr uint32_t kClipPiece = 4096;      // most elements of a piece, the unit in which tensors are dealt to workgroups
+struct TensorPiece {            // a run of a tensor, as the table on the device holds it
+    uint64_t data;              // its first element in worker 0's tensor
+    uint64_t stride;            // bytes from one worker's to the next's
+    uint32_t offset;            // of its first element in a row of V
+    uint32_t n_type;            // elements | dtype << 16
 };
-constexpr uint32_t kTensorBatch = 64;      // entries that one launch brings to the device in its arguments
+constexpr uint32_t kTensorBatch = 64;      // tensors that one launch brings to the device in its arguments
 struct TensorBatch {
-    TensorEntry entry[kTensorBatch];
-    uint32_t first, count;
+    struct Entry { uint64_t data, stride, n, first_piece; uint32_t offset, dtype; } entry[kTensorBatch];
+    uint64_t first_piece, pieces;          // of the batch's tensors
+    uint32_t count;
 };
 constexpr int kClipThreads = 256;
-constexpr uint32_t kClipPiece = 8192;      // elements of a piece: the unit in which tensors are dealt to workgroups
 constexpr uint32_t kClipParts = 1024;      // most partial sums of a worker
 struct ClipArgs {
-    const TensorEntry* table;
+    const TensorPiece* table;
     double* partial;            // [K][kClipParts]
+    double* scale;              // [K] factors
     float* V;                   // [K][d] or null: in place
     float* norms;               // [K] or null
-    uint64_t n_pieces, per_part, per_scale;
+    uint64_t n_pieces;
     uint64_t d;
-    uint32_t n_tensors, parts;  // partial sums of a worker
+    uint32_t parts;             // workgroups that sum a worker's pieces
     float max_norm;
 };
-hipError_t launch_tensor_list(const TensorBatch& batch, TensorEntry* table, hipStream_t st);
-hipError_t launch_clip(const ClipArgs& a, uint32_t K, bool max_kind, Scalars* sc, hipStream_t st);
+hipError_t launch_tensor_list(const TensorBatch& batch, TensorPiece* table, hipStream_t st);
+hipError_t launch_clip(const ClipArgs& a, uint32_t K, bool max_kind, uint32_t n_cu, Scalars* sc, hipStream_t st);
 
 struct NormArgs {
     const void* x;

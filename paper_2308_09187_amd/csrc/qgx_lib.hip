@@ -908,35 +908,55 @@ static uint32_t element_size(int dtype) { return dtype == QGX_F32 ? 4u : 2u; }
 static bool known_type(int dtype) { return dtype == QGX_F32 || dtype == QGX_F16 || dtype == QGX_BF16; }
 static bool aligned_to(const void* p, uint32_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1u)) == 0; }
 
-// (the partial sums come after the entries)
-static uint64_t list_entries_bytes(uint32_t n_tensors) { return ((uint64_t)n_tensors * sizeof(TensorEntry) + 15u) / 16u * 16u; }
-
-qgx_status qgx_tensor_list_size(qgx_ctx* ctx, const qgx_tensor* tensors, uint32_t n_tensors, uint64_t* bytes)
+// A list's table: the pieces, then the workers' partial sums and factors.
+static uint64_t list_pieces(const qgx_tensor* tensors, uint32_t n_tensors)
 {
-    if (!ctx || !bytes || (n_tensors && !tensors)) return fail(ctx, QGX_ERR_ARG, "qgx_tensor_list_size: null argument");
-    *bytes = list_entries_bytes(n_tensors) + (uint64_t)ctx->lay.K * kClipParts * sizeof(double);
-    return QGX_OK;
+    uint64_t pieces = 0;
+    for (uint32_t i = 0; i < n_tensors; ++i) pieces += tensors[i].n / kClipPiece + (tensors[i].n % kClipPiece != 0);
+    return pieces;
+}
+static uint64_t list_pieces_bytes(uint64_t pieces) { return (pieces * sizeof(TensorPiece) + 15u) / 16u * 16u; }
+static uint64_t list_bytes(uint64_t pieces, uint32_t K)
+{
+    return list_pieces_bytes(pieces) + (uint64_t)K * (kClipParts + 1u) * sizeof(double);
 }
 
-qgx_status qgx_tensor_list_set(qgx_ctx* ctx, const qgx_tensor* tensors, uint32_t n_tensors, void* table, uint64_t table_bytes,
-                               qgx_tensor_list* list, void* stream)
+// The sizes, types and places of a list's tensors.
+static qgx_status check_tensors(qgx_ctx* ctx, const qgx_tensor* tensors, uint32_t n_tensors)
 {
-    uint64_t need = 0;
-    qgx_status s = qgx_tensor_list_size(ctx, tensors, n_tensors, &need);
-    if (s != QGX_OK) return s;
-    if (!table || !list || !aligned16(table)) return fail(ctx, QGX_ERR_ARG, "qgx_tensor_list_set: null or misaligned argument");
-    if (table_bytes < need) return fail(ctx, QGX_ERR_CAPACITY, "qgx_tensor_list_set: the table needs %llu bytes", (unsigned long long)need);
+    if (!ctx) return QGX_ERR_ARG;
+    if (n_tensors && !tensors) return fail(ctx, QGX_ERR_ARG, "tensor list: null argument");
     const uint64_t d = ctx->lay.d;
-    bool shared = false;
     for (uint32_t i = 0; i < n_tensors; ++i) {
         const qgx_tensor& t = tensors[i];
         if (!known_type(t.dtype)) return fail(ctx, QGX_ERR_ARG, "tensor %u: unknown type", i);
         if (t.n == 0) continue;
         if (!t.data || !aligned_to(t.data, element_size(t.dtype))) return fail(ctx, QGX_ERR_ARG, "tensor %u: null or misaligned data", i);
         if (t.n > d || t.offset > d - t.n) return fail(ctx, QGX_ERR_ARG, "tensor %u: elements beyond the %llu coordinates", i, (unsigned long long)d);
-        if (t.stride >= (1ull << 62) / ctx->lay.K) return fail(ctx, QGX_ERR_ARG, "tensor %u: stride out of range", i);
-        shared = shared || (t.stride < t.n && ctx->lay.K > 1u);
+        if (t.stride >= (1ull << 60) / ctx->lay.K) return fail(ctx, QGX_ERR_ARG, "tensor %u: stride out of range", i);
     }
+    return QGX_OK;
+}
+
+qgx_status qgx_tensor_list_size(qgx_ctx* ctx, const qgx_tensor* tensors, uint32_t n_tensors, uint64_t* bytes)
+{
+    const qgx_status s = check_tensors(ctx, tensors, n_tensors);
+    if (s != QGX_OK) return s;
+    if (!bytes) return fail(ctx, QGX_ERR_ARG, "qgx_tensor_list_size: null argument");
+    *bytes = list_bytes(list_pieces(tensors, n_tensors), ctx->lay.K);
+    return QGX_OK;
+}
+
+qgx_status qgx_tensor_list_set(qgx_ctx* ctx, const qgx_tensor* tensors, uint32_t n_tensors, void* table, uint64_t table_bytes,
+                               qgx_tensor_list* list, void* stream)
+{
+    qgx_status s = check_tensors(ctx, tensors, n_tensors);
+    if (s != QGX_OK) return s;
+    if (!table || !list || !aligned16(table)) return fail(ctx, QGX_ERR_ARG, "qgx_tensor_list_set: null or misaligned argument");
+    const uint64_t pieces = list_pieces(tensors, n_tensors), need = list_bytes(pieces, ctx->lay.K);
+    if (table_bytes < need) return fail(ctx, QGX_ERR_CAPACITY, "qgx_tensor_list_set: the table needs %llu bytes", (unsigned long long)need);
+    bool shared = false;
+    for (uint32_t i = 0; i < n_tensors; ++i) shared = shared || (tensors[i].stride < tensors[i].n && ctx->lay.K > 1u);
     // ranges of V, in order; two that follow each other may not overlap
     uint32_t* order = new (std::nothrow) uint32_t[n_tensors ? n_tensors : 1];
     if (!order) return fail(ctx, QGX_ERR_ARG, "qgx_tensor_list_set: no memory for %u tensors", n_tensors);
@@ -951,16 +971,16 @@ qgx_status qgx_tensor_list_set(qgx_ctx* ctx, const qgx_tensor* tensors, uint32_t
     if (s != QGX_OK) return s;
 
     TensorBatch batch{};
-    uint64_t pieces = 0;
     for (uint32_t i = 0; i < n_tensors; ++i) {
         const qgx_tensor& t = tensors[i];
-        batch.entry[batch.count++] = TensorEntry{(uint64_t)reinterpret_cast<uintptr_t>(t.data), t.n, t.stride, t.offset, pieces, (uint32_t)t.dtype, 0u};
-        pieces += (t.n + kClipPiece - 1u) / kClipPiece;
-        if (batch.count == kTensorBatch || i + 1u == n_tensors) {
-            QGX_HIP(ctx, launch_tensor_list(batch, (TensorEntry*)table, (hipStream_t)stream));
-            batch.first = i + 1u;
-            batch.count = 0;
-        }
+        batch.entry[batch.count++] = TensorBatch::Entry{(uint64_t)reinterpret_cast<uintptr_t>(t.data), t.stride, t.n, batch.first_piece + batch.pieces,
+                                                        (uint32_t)t.offset, (uint32_t)t.dtype};
+        batch.pieces += t.n / kClipPiece + (t.n % kClipPiece != 0);
+        if (batch.count < kTensorBatch && i + 1u < n_tensors) continue;
+        if (batch.pieces) QGX_HIP(ctx, launch_tensor_list(batch, (TensorPiece*)table, (hipStream_t)stream));
+        batch.first_piece += batch.pieces;
+        batch.pieces = 0;
+        batch.count = 0;
     }
     *list = qgx_tensor_list{table, table_bytes, pieces, n_tensors, shared ? 1u : 0u};
     return QGX_OK;
@@ -974,15 +994,15 @@ qgx_status qgx_clip_gradients(qgx_ctx* ctx, const qgx_tensor_list* list, int nor
     if (!(max_norm >= 0.0f)) return fail(ctx, QGX_ERR_ARG, "qgx_clip_gradients: max_norm must be >= 0");
     if (!aligned16(V) || !aligned_to(norms, 4u)) return fail(ctx, QGX_ERR_ARG, "qgx_clip_gradients: V must be 16-byte aligned, norms 4-byte");
     if (!V && list->shared_rows) return fail(ctx, QGX_ERR_ARG, "qgx_clip_gradients: the workers share elements, which in-place clipping would scale more than once");
-    const uint64_t entries = list_entries_bytes(list->n_tensors);
-    if (list->table_bytes < entries + (uint64_t)ctx->lay.K * kClipParts * sizeof(double))
+    if (list->table_bytes < list_bytes(list->n_pieces, ctx->lay.K))
         return fail(ctx, QGX_ERR_CAPACITY, "qgx_clip_gradients: the list's table is too small for this context");
     ClipArgs a{};
-    a.table = (const TensorEntry*)list->table;
-    a.partial = (double*)((char*)list->table + entries);
+    a.table = (const TensorPiece*)list->table;
+    a.partial = (double*)((char*)list->table + list_pieces_bytes(list->n_pieces));
+    a.scale = a.partial + (uint64_t)ctx->lay.K * kClipParts;
     a.V = V; a.norms = norms; a.d = ctx->lay.d;
-    a.n_pieces = list->n_pieces; a.n_tensors = list->n_tensors; a.max_norm = max_norm;
-    QGX_HIP(ctx, launch_clip(a, ctx->lay.K, norm == QGX_NORM_LINF, ctx->d_sc, (hipStream_t)stream));
+    a.n_pieces = list->n_pieces; a.max_norm = max_norm;
+    QGX_HIP(ctx, launch_clip(a, ctx->lay.K, norm == QGX_NORM_LINF, ctx->n_simd / 4u, ctx->d_sc, (hipStream_t)stream));
     return QGX_OK;
 }
 

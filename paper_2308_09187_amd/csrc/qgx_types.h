@@ -33,6 +33,16 @@ __device__ __forceinline__ void store_piece(T* p, const float (&v)[kPiece<T>])
 
 // The same for the first n elements of a piece (any n; zeros beyond), where the rest may be no memory at all.
 template <typename T>
+__device__ __forceinline__ Piece<T> load_raw(const T* p, int n)
+{
+    if (n >= kPiece<T>) return *reinterpret_cast<const Piece<T>*>(p);
+    Piece<T> x;
+#pragma unroll
+    for (int i = 0; i < kPiece<T>; ++i) x[i] = i < n ? p[i] : (T)0.0f;
+    return x;
+}
+
+template <typename T>
 __device__ __forceinline__ void load_piece(const T* p, int n, float (&v)[kPiece<T>])
 {
     if (n >= kPiece<T>) return load_piece(p, v);
