@@ -423,7 +423,7 @@ typedef struct {
     void* data;            /* DEVICE */
     int32_t dtype;         /* qgx_dtype */
     uint32_t heads;        /* 1 .. 65535 */
-    uint64_t workers, batch, q, k;                     /* q, k <= 2^29, q * k <= 2^42 */
+    uint64_t workers, batch, q, k;                     /* q, k <= 2^29, q * k <= 2^34 */
     uint64_t s_worker, s_batch, s_head, s_row;         /* strides */
 } qgx_scores;
 

@@ -334,11 +334,14 @@ struct BiasArgs {
     uint32_t planes;            // workers * batch * heads
 };
 hipError_t launch_position_bias(int dtype, const BiasArgs& a, const BucketArgs& b, hipStream_t st);
+constexpr uint32_t kMaxBands = 128;        // bands that get workgroups by their work
 struct BiasBackPlan {
     int64_t first, count;       // block diagonals with a place that is not masked
-    uint64_t scratch;           // bytes: [pairs][bands * splits][intervals] sums
+    uint64_t scratch;           // bytes: [pairs][blocks][intervals] sums
     uint32_t pairs;             // workers * heads
-    uint32_t bands, splits;     // runs of 64 block diagonals; workgroups that share one
+    uint32_t bands, blocks;     // runs of block diagonals; workgroups over them
+    uint32_t even;              // workgroups of every band, or 0:
+    uint32_t first_block[kMaxBands + 1];   // of a band
 };
 BiasBackPlan bias_back_plan(int dtype, const BiasArgs& a, const BucketArgs& b, uint32_t workers, uint32_t n_cu);
 hipError_t launch_position_bias_back(int dtype, const BiasArgs& a, const BucketArgs& b, const BiasBackPlan& plan, float* dtable,

@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
     int turn = 0;
     for (uint32_t set = blockIdx.x; (uint64_t)set * kGroups * R < a.rows; set += a.parts, turn ^= 1) {
         const uint32_t first = (set * kGroups + (uint32_t)group) * R;
-        Piece<T> x[R][N], dy[R][N];
+        nt_u32x4 x[R][N], dy[R][N];                        // as loaded: half the registers of their values in binary32
         float mean[R], rstd[R], sum[2 * R];
 #pragma unroll
         for (int q = 0; q < R; ++q) {
@@ -232,9 +232,9 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
             const T* pg = (const T*)a.dy + k * a.dy_worker + r * a.dy_row;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                x[q][j] = *reinterpret_cast<const Piece<T>*>(px + at[j].c);
-                dy[q][j] = *reinterpret_cast<const Piece<T>*>(pg + at[j].c);
-                if (!ok) x[q][j] = dy[q][j] = (T)0.0f;
+                x[q][j] = load_bits(px + at[j].c);
+                dy[q][j] = load_bits(pg + at[j].c);
+                if (!ok) x[q][j] = dy[q][j] = nt_u32x4{0u, 0u, 0u, 0u};
             }
             mean[q] = ok ? a.mean[(size_t)k * a.rows + r] : 0.0f;
             rstd[q] = ok ? a.rstd[(size_t)k * a.rows + r] : 0.0f;
@@ -243,16 +243,18 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
         for (int q = 0; q < R; ++q) {
             sum[q] = sum[R + q] = 0.0f;
 #pragma unroll
-            for (int j = 0; j < N; ++j)
+            for (int j = 0; j < N; ++j) {
+                const Piece<T> px = __builtin_bit_cast(Piece<T>, x[q][j]), pg = __builtin_bit_cast(Piece<T>, dy[q][j]);
 #pragma unroll
                 for (int c = 0; c < W; ++c) {
-                    const float d = (float)dy[q][j][c], g = at[j].owns(c) ? d * w[j][c] : 0.0f;
-                    const float h = ((float)x[q][j][c] - mean[q]) * rstd[q];
+                    const float d = (float)pg[c], g = at[j].owns(c) ? d * w[j][c] : 0.0f;
+                    const float h = ((float)px[c] - mean[q]) * rstd[q];
                     sum[q] += g;
                     sum[R + q] = fmaf(g, h, sum[R + q]);
                     dw[j][c] = fmaf(d, h, dw[j][c]);
                     db[j][c] += d;
                 }
+            }
         }
         if (a.dx) {
             row_sums<LANES>(sum, s_sum[turn]);             // (two sets of slots in turn: one barrier a round)
@@ -261,10 +263,13 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
                 const float m1 = sum[q] / (float)cols, m2 = sum[R + q] / (float)cols;
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
+                    // (worked out again from what was loaded: kept across the sums, g and h would take four times the registers)
+                    asm volatile("" : "+v"(x[q][j]), "+v"(dy[q][j]));
+                    const Piece<T> px = __builtin_bit_cast(Piece<T>, x[q][j]), pg = __builtin_bit_cast(Piece<T>, dy[q][j]);
                     float v[W];
 #pragma unroll
                     for (int c = 0; c < W; ++c) {
-                        const float g = (float)dy[q][j][c] * w[j][c], h = ((float)x[q][j][c] - mean[q]) * rstd[q];
+                        const float g = (float)pg[c] * w[j][c], h = ((float)px[c] - mean[q]) * rstd[q];
                         v[c] = rstd[q] * (g - m1 - h * m2);
                     }
                     if (at[j].any && first + q < a.rows) store_piece((T*)a.dx + k * a.dx_worker + (first + q) * a.dx_row + at[j].c, v);

@@ -1120,7 +1120,7 @@ static bool no_scores(const qgx_scores* s) { return s->workers == 0 || s->batch 
 static qgx_status check_scores(qgx_ctx* ctx, const char* what, const qgx_scores* s, bool written)
 {
     if (!known_type(s->dtype)) return fail(ctx, QGX_ERR_ARG, "%s: unknown type", what);
-    if (s->heads == 0 || s->heads > 65535u || s->q > (1u << 29) || s->k > (1u << 29) || s->q * s->k > (1ull << 42) || s->workers > 65535u || s->batch >= (1ull << 31) ||
+    if (s->heads == 0 || s->heads > 65535u || s->q > (1u << 29) || s->k > (1u << 29) || s->q * s->k > (1ull << 34) || s->workers > 65535u || s->batch >= (1ull << 31) ||
         s->workers * s->batch * s->heads >= (1ull << 31))
         return fail(ctx, QGX_ERR_ARG, "%s: size out of range", what);
     if (no_scores(s)) return QGX_OK;

@@ -8,7 +8,7 @@
 
 namespace qgx {
 
-constexpr int kBiasThreads = 256;
+constexpr int kBiasThreads = 256, kBiasWaves = kBiasThreads / kWave;
 
 // p of a sequence, kept within +-2^30 so that a delta fits 32 bits.
 __device__ __forceinline__ int position_of(const BiasArgs& a, uint32_t seq)
@@ -17,125 +17,180 @@ __device__ __forceinline__ int position_of(const BiasArgs& a, uint32_t seq)
     return (int)max((int64_t)-(1 << 30), min(p, (int64_t)(1 << 30)));
 }
 
+// The intervals in a wave's registers, i and i + 64 in lane i.
+struct Intervals {
+    int bound0, bound1, end0, end1;
+    uint32_t row0, row1;
+    bool is0, is1;
+    __device__ __forceinline__ explicit Intervals(const BucketArgs& b)
+    {
+        const uint32_t i = (uint32_t)lane_id(), i0 = min(i, b.n - 1u), i1 = min(i + kWave, b.n - 1u);
+        bound0 = b.bounds[i0]; end0 = b.bounds[i0 + 1u]; row0 = b.rows[i0]; is0 = i < b.n;
+        bound1 = b.bounds[i1]; end1 = b.bounds[i1 + 1u]; row1 = b.rows[i1]; is1 = i + kWave < b.n;
+    }
+    // f(i, j, x0, x1) for every interval that meets first .. end: i its number, j its lane's, x0 .. x1 what it has of that run
+    template <typename F>
+    __device__ __forceinline__ void meeting(int first, int end, F f) const
+    {
+        for (uint64_t which = __ballot(is0 && bound0 < end && end0 > first); which; which &= which - 1u) {
+            const int j = __ffsll((unsigned long long)which) - 1;
+            f(j, j, max(__builtin_amdgcn_readlane(bound0, j), first), min(__builtin_amdgcn_readlane(end0, j), end));
+        }
+        for (uint64_t which = __ballot(is1 && bound1 < end && end1 > first); which; which &= which - 1u) {
+            const int j = __ffsll((unsigned long long)which) - 1;
+            f(j + kWave, j, max(__builtin_amdgcn_readlane(bound1, j), first), min(__builtin_amdgcn_readlane(end1, j), end));
+        }
+    }
+};
+
 // ---- forward --------------------------------------------------------------------------------------------------------------
-// Squares have ROWS queries (W, or one where there are fewer than W queries).  A workgroup's tile: up to 256 neighbouring squares of
-// one band of ROWS queries, or, where a band has no more than 256, 256 squares of several bands that follow each other.
+// Squares have ROWS queries (W, or one where there are fewer than W), a band is ROWS queries' squares.  A wave takes up to 64
+// neighbouring squares of a band, or whole bands where they have few squares, a lane each.  It lists its diagonals' biases in LDS of its own
+// (one or two intervals in most places): no barrier, and the scores' loads are under way meanwhile.  The last squares of a band and the last
+// band are moved back to end with the keys and queries, so that every access is whole: what two squares have in common they
+// write twice, the same bits.
 struct Tiling {
-    uint32_t per_band;                                     // squares
-    uint32_t tiles, tiles_per_band, chunk;                 // tiles_per_band 0: a tile goes on in the next band; else squares of a tile
+    uint32_t per_band, bands;                              // squares of a band; bands
+    uint32_t chunks, chunk;                                // waves that share a band, squares of each; or
+    uint32_t bands_each;                                   // bands of a wave (chunks is 1)
+    uint32_t inverse;                                      // 65536 / chunk and one, for the lanes' division: lane and chunk are at most 64
+    uint32_t tasks;                                        // (below 2^26: q k is at most 2^34)
 };
 
 template <int W, int ROWS>
-__host__ __device__ inline Tiling tiling(uint32_t q, uint32_t k)
+static Tiling tiling(uint32_t q, uint32_t k)
 {
     Tiling t{};
     t.per_band = (k + W - 1u) / W;
-    const uint32_t bands = (q + ROWS - 1u) / ROWS;
-    if (t.per_band > (uint32_t)kBiasThreads) {
-        t.tiles_per_band = (t.per_band + kBiasThreads - 1u) / kBiasThreads;
-        t.chunk = (t.per_band + t.tiles_per_band - 1u) / t.tiles_per_band;
-    }
-    // (below 2^32: q k is at most 2^42)
-    t.tiles = t.tiles_per_band ? bands * t.tiles_per_band : (uint32_t)(((uint64_t)bands * t.per_band + kBiasThreads - 1u) / kBiasThreads);
+    t.bands = (q + ROWS - 1u) / ROWS;
+    t.chunks = (t.per_band + kWave - 1u) / kWave;
+    t.chunk = (t.per_band + t.chunks - 1u) / t.chunks;
+    t.bands_each = t.chunks == 1u ? kWave / t.per_band : 1u;
+    t.inverse = 65536u / t.chunk + 1u;
+    t.tasks = (t.bands + t.bands_each - 1u) / t.bands_each * t.chunks;
     return t;
 }
 
-// The most diagonals a tile can have: its squares' keys (all of a band's where it has several) and its queries.
-template <int W, int ROWS>
-static uint32_t tile_diagonals(const Tiling& t)
-{
-    if (t.tiles_per_band) return t.chunk * W + ROWS;
-    return t.per_band * W + ((kBiasThreads - 2u) / t.per_band + 2u) * ROWS;
-}
+// The most diagonals of a wave: chunk W + bands_each ROWS - 1, and chunk bands_each is at most 64.
+constexpr int wave_diagonals(int W) { return 65 * W; }
+// One word is left out after every W, so that lanes W entries apart do not meet in a bank.
+template <int W> __device__ __forceinline__ uint32_t diagonal_slot(uint32_t x) { return x + x / W; }
 
-// A list entry's place: one word is left out after every W, so that lanes W entries apart do not meet in a bank.
-template <int W>
-__device__ __forceinline__ uint32_t diagonal_slot(uint32_t x) { return x + x / W; }
-
-template <typename T, int ROWS>
-__global__ __launch_bounds__(kBiasThreads) void k_position_bias(BiasArgs a, BucketArgs b)
+// GUARDED: squares with something in common write it once.  In place a square's scores may otherwise have been overwritten by the
+// one it overlaps before they are read.
+template <typename T, int ROWS, bool GUARDED>
+__global__ __launch_bounds__(kBiasThreads) void k_position_bias(BiasArgs a, BucketArgs b, Tiling t)
 {
     constexpr int W = kPiece<T>;
-    extern __shared__ float s_value[];
-    const Tiling t = tiling<W, ROWS>(a.q, a.k);
-    const uint32_t bands = (a.q + ROWS - 1u) / ROWS;
-    const int lo = b.bounds[0], hi = b.bounds[b.n];
-    for (uint32_t plane = blockIdx.y; plane < a.planes; plane += gridDim.y) {       // (worker, sequence, head)
-        const uint32_t head = plane % a.heads, seq = plane / a.heads, worker = seq / a.batch, n = seq % a.batch;
-        const int p = position_of(a, seq);
-        const T* in = a.in ? (const T*)a.in + worker * a.i_worker + n * a.i_batch + head * a.i_head : nullptr;
-        T* out = (T*)a.out + worker * a.o_worker + n * a.o_batch + head * a.o_head;
-        for (uint32_t tile = blockIdx.x; tile < t.tiles; tile += gridDim.x) {
-            uint32_t band0, band1, square, first = 0, end = t.per_band;    // this thread's square of `band`; the tile's squares of a band
-            uint32_t band;
-            if (t.tiles_per_band) {
-                band0 = band1 = band = tile / t.tiles_per_band;
-                first = tile % t.tiles_per_band * t.chunk;
-                end = min(first + t.chunk, t.per_band);
-                square = first + threadIdx.x;
-            } else {
-                const uint64_t at = (uint64_t)tile * kBiasThreads;
-                band0 = (uint32_t)(at / t.per_band);
-                band1 = min((uint32_t)((at + kBiasThreads - 1u) / t.per_band), bands - 1u);
-                band = (uint32_t)((at + threadIdx.x) / t.per_band);
-                square = (uint32_t)((at + threadIdx.x) % t.per_band);
-            }
-            // deltas of the tile: first, and how many
-            const int d0 = (int)(first * W) - (int)((band1 + 1u) * ROWS - 1u) - p;
-            const int count = (int)(end * W) - (int)(band0 * ROWS) - p - d0;
+    __shared__ float s_list[kBiasWaves][wave_diagonals(W) / W * (W + 1)];
+    float* list = s_list[wave_id()];
+    const uint32_t task = blockIdx.x * kBiasWaves + (uint32_t)__builtin_amdgcn_readfirstlane(wave_id()), plane = blockIdx.z * gridDim.y + blockIdx.y;
+    if (task >= t.tasks || plane >= a.planes) return;
+    const int lane = lane_id(), q = (int)a.q, k = (int)a.k, lo = b.bounds[0], hi = b.bounds[b.n];
+    const uint32_t head = plane % a.heads, seq = plane / a.heads, worker = seq / a.batch, n = seq % a.batch;
+    const uint32_t group = task / t.chunks, band0 = group * t.bands_each, first = (task - group * t.chunks) * t.chunk;
+    const uint32_t end = min(first + t.chunk, t.per_band), band1 = min(band0 + t.bands_each, t.bands);
+    const uint32_t mine = ((uint32_t)lane * t.inverse) >> 16, band = band0 + mine, square = first + (uint32_t)lane - mine * t.chunk;
+    const bool any = band < band1 && square < end;
+    const int i_at = (int)band * ROWS, j_at = (int)square * W;         // before they are moved back
+    const int i0 = min(i_at, q - ROWS), j0 = min(j_at, k - W);
+    const int p = position_of(a, seq), delta0 = j0 - i0 - p;           // of the first query and key
 
-            const int j0 = (int)square * W, i0 = (int)band * ROWS, left = (int)a.k - j0;
-            const int rows = square < end && band < bands ? min(ROWS, (int)a.q - i0) : 0;
-            const int delta0 = j0 - i0 - p;                // of the first query and key
-            float v[ROWS][W];
+    float v[ROWS][W];
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
+    for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-                for (int c = 0; c < W; ++c) v[r][c] = 0.0f;
-                // (a piece that is masked as a whole is not read)
-                if (in && r < rows && delta0 - r + W > lo && delta0 - r < hi) load_piece(in + (uint32_t)(i0 + r) * a.i_row + j0, left, v[r]);
-            }
-            __syncthreads();                               // the tile before has been dealt with
-            for (uint32_t s = threadIdx.x / kWave; s < b.n; s += kBiasThreads / kWave) {
-                const int x0 = max(b.bounds[s], d0), x1 = (int)min((int64_t)b.bounds[s + 1], (int64_t)d0 + count);
-                if (x0 >= x1) continue;
-                const float value = a.table[(size_t)b.rows[s] * a.heads + head];
-                for (int x = x0 + lane_id(); x < x1; x += kWave) s_value[diagonal_slot<W>((uint32_t)(x - d0))] = value;
-            }
-            __syncthreads();
-            if (rows > 0) {
-                float bias[ROWS + W - 1];                  // of delta0 - (ROWS - 1) on
+        for (int c = 0; c < W; ++c) v[r][c] = 0.0f;
+    // (a square that is masked as a whole is not read)
+    if (a.in && any && delta0 + W > lo && delta0 - (ROWS - 1) < hi) {
+        const T* in = (const T*)a.in + worker * a.i_worker + n * a.i_batch + head * a.i_head + (uint32_t)i0 * a.i_row + j0;
 #pragma unroll
-                for (int e = 0; e < ROWS + W - 1; ++e) bias[e] = s_value[diagonal_slot<W>((uint32_t)(delta0 - (ROWS - 1) - d0 + e))];
-                const bool all = delta0 - (ROWS - 1) >= lo && delta0 + W <= hi;
+        for (int r = 0; r < ROWS; ++r) load_piece(in + (uint32_t)r * a.i_row, v[r]);
+    }
+
+    // deltas of the wave: d0 .. d1
+    const int d0 = min((int)(first * W), k - W) - (min((int)(band1 * ROWS), q) - 1) - p;
+    const int d1 = min((int)(end * W), k) - min((int)(band0 * ROWS), q - ROWS) - p;
+    const Intervals interval(b);
+    // (all intervals' biases at once: one after the other they would be the longest wait there is)
+    const float value0 = interval.is0 ? a.table[(size_t)interval.row0 * a.heads + head] : 0.0f;
+    const float value1 = interval.is1 ? a.table[(size_t)interval.row1 * a.heads + head] : 0.0f;
+    interval.meeting(d0, d1, [&](int i, int j, int x0, int x1) {
+        const float value = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(i < kWave ? value0 : value1), j));
+        for (int x = x0 + lane; x < x1; x += kWave) list[diagonal_slot<W>((uint32_t)(x - d0))] = value;
+    });
+    wave_lds_fence();
+    if (!any) return;
+    float bias[ROWS + W - 1];                              // of delta0 - (ROWS - 1) on
+    bool seen[ROWS + W - 1];
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) {
+    for (int e = 0; e < ROWS + W - 1; ++e) {
+        const int delta = delta0 - (ROWS - 1) + e;
+        bias[e] = list[diagonal_slot<W>((uint32_t)(delta - d0))];      // (what no interval has is no number; it is not used)
+        seen[e] = delta >= lo && delta < hi;
+    }
+    T* out = (T*)a.out + worker * a.o_worker + n * a.o_batch + head * a.o_head + (uint32_t)i0 * a.o_row + j0;
 #pragma unroll
-                    for (int c = 0; c < W; ++c) {
-                        v[r][c] += bias[ROWS - 1 - r + c];
-                        if (!all && (delta0 - r + c < lo || delta0 - r + c >= hi)) v[r][c] = -__builtin_inff();
-                    }
-                    if (r < rows) store_piece(out + (uint32_t)(i0 + r) * a.o_row + j0, left, v[r]);
-                }
-            }
+    for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+        for (int c = 0; c < W; ++c) v[r][c] = seen[ROWS - 1 - r + c] ? v[r][c] + bias[ROWS - 1 - r + c] : -__builtin_inff();
+        if constexpr (!GUARDED) {
+            store_piece(out + (uint32_t)r * a.o_row, v[r]);
+        } else if (i0 + r >= i_at) {
+            if (j0 == j_at) store_piece(out + (uint32_t)r * a.o_row, v[r]);
+            else
+#pragma unroll
+                for (int c = 0; c < W; ++c)
+                    if (j0 + c >= j_at) out[(uint32_t)r * a.o_row + c] = (T)v[r][c];
         }
     }
+}
+
+// Fewer keys than a piece has elements: a thread for each query.
+template <typename T>
+__global__ __launch_bounds__(kBiasThreads) void k_position_bias_narrow(BiasArgs a, BucketArgs b)
+{
+    const uint32_t i = blockIdx.x * kBiasThreads + threadIdx.x, plane = blockIdx.z * gridDim.y + blockIdx.y;
+    if (i >= a.q || plane >= a.planes) return;
+    const uint32_t head = plane % a.heads, seq = plane / a.heads, worker = seq / a.batch, n = seq % a.batch;
+    const int p = position_of(a, seq);
+    for (uint32_t j = 0; j < a.k; ++j) {
+        const int delta = (int)j - (int)i - p;
+        float x = -__builtin_inff();
+        for (uint32_t s = 0; s < b.n; ++s)
+            if (delta >= b.bounds[s] && delta < b.bounds[s + 1]) {
+                x = a.table[(size_t)b.rows[s] * a.heads + head];
+                if (a.in) x += (float)((const T*)a.in + worker * a.i_worker + n * a.i_batch + head * a.i_head + i * a.i_row)[j];
+            }
+        ((T*)a.out + worker * a.o_worker + n * a.o_batch + head * a.o_head + i * a.o_row)[j] = (T)x;
+    }
+}
+
+// Planes over two dimensions of a grid.
+static dim3 plane_grid(uint32_t blocks, uint32_t planes)
+{
+    const uint32_t y = min(planes, 65535u);
+    return dim3(blocks, y, (planes + y - 1u) / y);
 }
 
 template <typename T, int ROWS>
 static hipError_t launch_bias_rows(const BiasArgs& a, const BucketArgs& b, hipStream_t st)
 {
-    constexpr int W = kPiece<T>;
-    const Tiling t = tiling<W, ROWS>(a.q, a.k);
-    const dim3 grid(min(t.tiles, 1u << 20), min(a.planes, 65535u));
-    const uint32_t slots = tile_diagonals<W, ROWS>(t);
-    hipLaunchKernelGGL((k_position_bias<T, ROWS>), grid, dim3(kBiasThreads), (slots + slots / W + 1u) * sizeof(float), st, a, b);
+    const Tiling t = tiling<kPiece<T>, ROWS>(a.q, a.k);
+    const dim3 grid = plane_grid((t.tasks + kBiasWaves - 1u) / kBiasWaves, a.planes);
+    const bool overlap = a.q % ROWS != 0u || a.k % kPiece<T> != 0u;
+    if (a.in == a.out && overlap) hipLaunchKernelGGL((k_position_bias<T, ROWS, true>), grid, dim3(kBiasThreads), 0, st, a, b, t);
+    else hipLaunchKernelGGL((k_position_bias<T, ROWS, false>), grid, dim3(kBiasThreads), 0, st, a, b, t);
     return hipGetLastError();
 }
 
 template <typename T>
 static hipError_t launch_bias_of(const BiasArgs& a, const BucketArgs& b, hipStream_t st)
 {
+    if (a.k < (uint32_t)kPiece<T>) {
+        hipLaunchKernelGGL(k_position_bias_narrow<T>, plane_grid((a.q + kBiasThreads - 1u) / kBiasThreads, a.planes), dim3(kBiasThreads), 0, st, a, b);
+        return hipGetLastError();
+    }
     return a.q < (uint32_t)kPiece<T> ? launch_bias_rows<T, 1>(a, b, st) : launch_bias_rows<T, kPiece<T>>(a, b, st);
 }
 
@@ -145,96 +200,168 @@ hipError_t launch_position_bias(int dtype, const BiasArgs& a, const BucketArgs& 
 }
 
 // ---- gradient -------------------------------------------------------------------------------------------------------------
-// Block diagonal D holds the squares of queries s W .. and keys (s + D) W .., s = 0, 1, ..  A wave has 64 neighbouring ones, a lane
-// each; at a step it reads W queries' runs of 64 W neighbouring keys.  (sequence, step) pairs are dealt to the waves of a band's
-// workgroups in turn.
-constexpr int kBackWaves = kBiasThreads / kWave;
+// Block diagonal D holds the squares of queries s W .. and keys (s + D) W .., s = 0, 1, ..  A band is kBand neighbouring ones, a lane each;
+// at a step the lanes of a band read W queries' runs of kBand W neighbouring keys.  A band's items are its steps in all sequences,
+// dealt in turn to the kBackGroups groups of kBand lanes of each of its workgroups; bands get workgroups by their items, for
+// the corner bands of a square of queries and keys have few.
+constexpr int kBand = 16;
+constexpr int kBackGroups = kBiasThreads / kBand;
 
-// First block diagonal that holds a place that is not masked, and their number, of queries q and keys k (in squares).
-__host__ __device__ inline void visible_diagonals(const BiasArgs& a, const BucketArgs& b, int W, int64_t* first, int64_t* count)
+// The first and the number of the block diagonals that hold a place that is not masked.
+static void visible_diagonals(const BiasArgs& a, const BucketArgs& b, int W, int64_t* first, int64_t* count)
 {
-    const int64_t q = (a.q + W - 1) / W, k = (a.k + W - 1) / W;
+    const int64_t q = ((int64_t)a.q + W - 1) / W, k = ((int64_t)a.k + W - 1) / W;
     const int64_t lo = (int64_t)b.bounds[0] + a.q_offset, hi = (int64_t)b.bounds[b.n] - 1 + a.q_offset;       // visible j - i: lo .. hi
     // square D has j - i in D W - (W - 1) .. D W + W - 1
     auto floor_div = [](int64_t x, int64_t y) { return x >= 0 ? x / y : -((-x + y - 1) / y); };
-    int64_t d0 = floor_div(lo, W), d1 = floor_div(hi + W - 1, W);
-    d0 = d0 < -(q - 1) ? -(q - 1) : d0;
-    d1 = d1 > k - 1 ? k - 1 : d1;
+    const int64_t d0 = max(floor_div(lo, W), -(q - 1)), d1 = min(floor_div(hi + W - 1, W), k - 1);
     *first = d0;
     *count = d1 >= d0 ? d1 - d0 + 1 : 0;
+}
+
+// Steps at which a band has a square: s0 .. s1.
+struct BandSteps { int s0, s1; };
+__host__ __device__ inline BandSteps band_steps(int64_t D0, int64_t D1, int q_steps, int k_steps)
+{
+    const int64_t s0 = D1 < 0 ? -D1 : 0, s1 = k_steps - D0 < q_steps ? k_steps - D0 : q_steps;
+    return BandSteps{(int)s0, (int)(s1 > s0 ? s1 : s0)};
+}
+
+// n elements of a piece that ends with its row: those before the end, the rest zeros.  row: keys of it, W or more.
+template <typename T>
+__device__ __forceinline__ nt_u32x4 load_end(const T* p, int n)
+{
+    nt_u32x4 x = load_bits(p - (kPiece<T> - n));
+    uint64_t lo = x.x | (uint64_t)x.y << 32, hi = x.z | (uint64_t)x.w << 32;
+    const int bits = (kPiece<T> - n) * 8 * (int)sizeof(T);     // 16 or 32 .. 112
+    if (bits >= 64) {
+        lo = hi >> (bits - 64);
+        hi = 0;
+    } else {
+        lo = lo >> bits | hi << (64 - bits);
+        hi >>= bits;
+    }
+    return nt_u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 
 template <typename T>
 __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a, BucketArgs b, BiasBackPlan plan, float* __restrict__ partial)
 {
-    constexpr int W = kPiece<T>, E = 2 * W - 1, kSpan = kWave * W + W;
-    __shared__ float s_low[kBackWaves][kWave + 1][W + 1];  // sums of the diagonals below a square's main one, and from it on
-    __shared__ float s_high[kBackWaves][kWave + 1][W + 1];
+    constexpr int W = kPiece<T>, E = 2 * W - 1, kSpan = kBand * W + W;
+    __shared__ float s_low[kBiasWaves][kBand + 1][W + 1];  // sums of the diagonals below a square's main one, and from it on
+    __shared__ float s_high[kBiasWaves][kBand + 1][W + 1];
     __shared__ float s_diag[kSpan];
-    const uint32_t band = blockIdx.x / plan.splits, split = blockIdx.x % plan.splits;
+    __shared__ float s_out[QGX_MAX_INTERVALS];
     const int lane = lane_id(), wave = wave_id();
-    const int64_t D0 = plan.first + (int64_t)band * kWave, D1 = min(D0 + kWave, plan.first + plan.count) - 1;     // of the band
+    // this workgroup's band, its place among the band's and their number
+    uint32_t band, split, splits;
+    if (plan.even) {
+        band = blockIdx.x / plan.even;
+        split = blockIdx.x % plan.even;
+        splits = plan.even;
+    } else {
+        // first_block ascends, and every band has a workgroup
+        const uint32_t i0 = (uint32_t)lane < plan.bands ? plan.first_block[lane] : 0xFFFFFFFFu;
+        const uint32_t i1 = (uint32_t)lane + kWave < plan.bands ? plan.first_block[lane + kWave] : 0xFFFFFFFFu;
+        band = (uint32_t)(__popcll(__ballot(i0 <= blockIdx.x)) + __popcll(__ballot(i1 <= blockIdx.x))) - 1u;
+        split = blockIdx.x - plan.first_block[band];
+        splits = plan.first_block[band + 1u] - plan.first_block[band];
+    }
+    const int64_t D0 = plan.first + (int64_t)band * kBand, D1 = min(D0 + kBand, plan.first + plan.count) - 1, D = D0 + lane % kBand;
     const int q_steps = (int)((a.q + W - 1u) / W), k_steps = (int)((a.k + W - 1u) / W);
-    // steps at which any lane has a square
-    const int s0 = (int)max((int64_t)0, -D1), s1 = (int)min((int64_t)q_steps, (int64_t)k_steps - D0), steps = max(0, s1 - s0);
-    const uint64_t work = (uint64_t)steps * a.batch;
-    const int64_t D = D0 + lane;
+    const BandSteps at = band_steps(D0, D1, q_steps, k_steps);
+    const uint32_t steps = (uint32_t)(at.s1 - at.s0);
+    const uint64_t items = (uint64_t)steps * a.batch;
+    const Intervals interval(b);
     for (uint32_t kh = blockIdx.y; kh < plan.pairs; kh += gridDim.y) {
         const uint32_t worker = kh / a.heads, head = kh % a.heads;
         const T* base = (const T*)a.in + worker * a.i_worker + head * a.i_head;
         float sum[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-        for (uint64_t x = (uint64_t)split * kBackWaves + wave; x < work; x += (uint64_t)plan.splits * kBackWaves) {
-            const uint32_t n = (uint32_t)(x / (uint32_t)steps);
-            const int s = s0 + (int)(x % (uint32_t)steps);
-            const int64_t jb = s + D;                      // the square's keys
-            if (D > D1 || jb < 0 || jb >= k_steps) continue;
-            const int i0 = s * W, left = (int)((int64_t)a.k - jb * W), rows = min(W, (int)a.q - i0);
-            const T* in = base + n * a.i_batch + (uint32_t)i0 * a.i_row + jb * W;
-            float v[W][W];
+        nt_u32x4 raw[W];                                   // the item before, as loaded
+#pragma unroll
+        for (int r = 0; r < W; ++r) raw[r] = nt_u32x4{0u, 0u, 0u, 0u};
+        // this group's first item: sequence n, step s; and from one item to its next
+        const uint32_t x0 = split * kBackGroups + threadIdx.x / kBand, hop = splits * kBackGroups;
+        uint32_t n = steps ? x0 / steps : a.batch, s = steps ? x0 % steps : 0u;
+        const uint32_t hop_n = steps ? hop / steps : 0u, hop_s = steps ? hop % steps : 0u;
+        // (the groups of a wave go on as long as any of the workgroup's has an item, and one more turn adds the last)
+        for (uint64_t turn = (uint64_t)split * kBackGroups; turn < items + hop; turn += hop) {
+            nt_u32x4 next[W];
+#pragma unroll
+            for (int r = 0; r < W; ++r) next[r] = nt_u32x4{0u, 0u, 0u, 0u};
+            const int64_t jb = (int64_t)at.s0 + s + D;     // the square's keys
+            if (n < a.batch && D <= D1 && jb >= 0 && jb < k_steps) {
+                const uint32_t i0 = ((uint32_t)at.s0 + s) * W, left = a.k - (uint32_t)jb * W;
+                const T* in = base + n * a.i_batch + i0 * a.i_row + jb * W;
+                if (i0 + W <= a.q && left >= (uint32_t)W) {
+#pragma unroll
+                    for (int r = 0; r < W; ++r) next[r] = load_bits(in + (uint32_t)r * a.i_row);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < W; ++r) {
+                        if (i0 + r >= a.q) continue;
+                        const T* from = in + (uint32_t)r * a.i_row;
+                        if (left >= (uint32_t)W) next[r] = load_bits(from);
+                        else if (a.k >= (uint32_t)W) next[r] = load_end(from, (int)left);
+                        else next[r] = __builtin_bit_cast(nt_u32x4, load_raw(from, (int)left));
+                    }
+                }
+            }
 #pragma unroll
             for (int r = 0; r < W; ++r) {
+                const Piece<T> v = __builtin_bit_cast(Piece<T>, raw[r]);
 #pragma unroll
-                for (int c = 0; c < W; ++c) v[r][c] = 0.0f;
-                if (r < rows) load_piece(in + (uint32_t)r * a.i_row, left, v[r]);
+                for (int c = 0; c < W; ++c) sum[c - r + W - 1] += (float)v[c];
+                raw[r] = next[r];
             }
-#pragma unroll
-            for (int r = 0; r < W; ++r)
-#pragma unroll
-                for (int c = 0; c < W; ++c) sum[c - r + W - 1] += v[r][c];
+            n += hop_n;
+            s += hop_s;
+            if (s >= steps) { s -= steps; ++n; }
         }
-        // A diagonal of the band is that of one lane's square from its main one on and of the next lane's below it.
+        // the wave's groups joined, then a diagonal of the band is that of one lane's square from its main one on and of the next
+        // lane's below it
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            LanePair o = lane_pair<32>(__float_as_uint(sum[e]));
+            sum[e] = __uint_as_float(o.a) + __uint_as_float(o.b);
+            o = lane_pair<16>(__float_as_uint(sum[e]));
+            sum[e] = __uint_as_float(o.a) + __uint_as_float(o.b);
+        }
         __syncthreads();                                   // the pair before has been dealt with
+        if (lane <= kBand) {
+            const bool is = lane < kBand;
 #pragma unroll
-        for (int e = 0; e < W; ++e) {
-            s_high[wave][lane][e] = sum[e + W - 1];
-            s_low[wave][lane][e] = e < W - 1 ? sum[e] : 0.0f;        // diagonal D W - (W - 1) + e
-        }
-        if (lane == 0)
-#pragma unroll
-            for (int e = 0; e < W; ++e) s_high[wave][kWave][e] = s_low[wave][kWave][e] = 0.0f;
-        __syncthreads();
-        // s_diag[x]: diagonal D0 W - W + x, x = 0 .. 64 W + W - 1
-        for (int x = (int)threadIdx.x; x < kSpan; x += kBiasThreads) {
-            const int l = x / W - 1, e = x % W;            // from the main diagonal of lane l's square on, below that of lane l + 1's
-            float t = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kBackWaves; ++w) {
-                if (l >= 0) t += s_high[w][l][e];
-                if (e > 0) t += s_low[w][l + 1][e - 1];
+            for (int e = 0; e < W; ++e) {
+                s_high[wave][lane][e] = is ? sum[e + W - 1] : 0.0f;
+                s_low[wave][lane][e] = is && e < W - 1 ? sum[e] : 0.0f;        // diagonal D W - (W - 1) + e
             }
-            s_diag[x] = t;
+        }
+        if (threadIdx.x < QGX_MAX_INTERVALS) s_out[threadIdx.x] = 0.0f;
+        __syncthreads();
+        // s_diag[x]: diagonal D0 W - W + x
+        for (int y = (int)threadIdx.x; y < kSpan; y += kBiasThreads) {
+            const int l = y / W - 1, e = y % W;            // from the main diagonal of lane l's square on, below that of lane l + 1's
+            float z = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kBiasWaves; ++w) {
+                if (l >= 0) z += s_high[w][l][e];
+                if (e > 0) z += s_low[w][l + 1][e - 1];
+            }
+            s_diag[y] = z;
         }
         __syncthreads();
-        const int64_t first = D0 * W - W - a.q_offset;     // delta of s_diag[0]
-        for (uint32_t i = (uint32_t)wave; i < b.n; i += kBackWaves) {
-            const int x0 = (int)max((int64_t)0, b.bounds[i] - first), x1 = (int)min((int64_t)kSpan, b.bounds[i + 1] - first);
-            float t = 0.0f;
-            for (int x = x0 + lane; x < x1; x += kWave) t += s_diag[x];
-            t = lanes_sum<kWave>(t);
-            if (lane == 0) partial[((size_t)kh * gridDim.x + blockIdx.x) * b.n + i] = t;
-        }
+        const int first = (int)(D0 * W - W - a.q_offset);  // delta of s_diag[0]
+        interval.meeting(first, first + kSpan, [&](int i, int, int x0, int x1) {
+            if (i % kBiasWaves != wave) return;
+            float z = 0.0f;
+            for (int y = x0 + lane; y < x1; y += kWave) z += s_diag[y - first];
+            z = lanes_sum<kWave>(z);
+            if (lane == 0) s_out[i] = z;
+        });
+        __syncthreads();
+        if (threadIdx.x < b.n) partial[((size_t)kh * gridDim.x + blockIdx.x) * b.n + threadIdx.x] = s_out[threadIdx.x];
     }
 }
 
@@ -244,14 +371,16 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias_join(BucketArgs 
                                                                      uint64_t param_stride)
 {
     const uint64_t each = (uint64_t)table_rows * heads, all = plan.pairs / heads * each;
-    for (uint64_t x = (uint64_t)blockIdx.x * kBackWaves + wave_id(); x < all; x += (uint64_t)gridDim.x * kBackWaves) {
+    const Intervals interval(b);
+    for (uint64_t x = (uint64_t)blockIdx.x * kBiasWaves + wave_id(); x < all; x += (uint64_t)gridDim.x * kBiasWaves) {
         const uint32_t worker = (uint32_t)(x / each), r = (uint32_t)(x % each / heads), head = (uint32_t)(x % heads);
         const float* p = partial + ((size_t)worker * heads + head) * parts * b.n;
         double sum = 0.0;
-        for (uint32_t i = 0; i < b.n; ++i) {
-            if (b.rows[i] != r) continue;
-            for (uint32_t u = (uint32_t)lane_id(); u < parts; u += kWave) sum += (double)p[(size_t)u * b.n + i];
-        }
+        for (int half = 0; half < 2; ++half)
+            for (uint64_t which = __ballot((uint32_t)(lane_id() + half * kWave) < b.n && (half ? interval.row1 : interval.row0) == r); which; which &= which - 1u) {
+                const uint32_t i = (uint32_t)(half * kWave + __ffsll((unsigned long long)which) - 1);
+                for (uint32_t u = (uint32_t)lane_id(); u < parts; u += kWave) sum += (double)p[(size_t)u * b.n + i];
+            }
         sum = wave_sum(sum);
         if (lane_id() == 0) dtable[worker * param_stride + (size_t)r * heads + head] = (float)sum;
     }
@@ -259,27 +388,41 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias_join(BucketArgs 
 
 BiasBackPlan bias_back_plan(int dtype, const BiasArgs& a, const BucketArgs& b, uint32_t workers, uint32_t n_cu)
 {
-    const uint32_t W = dtype == QGX_F32 ? 4u : 8u;
+    const int W = dtype == QGX_F32 ? 4 : 8;
     BiasBackPlan p{};
     p.pairs = workers * a.heads;
-    int64_t first = 0, count = 0;
-    if (a.batch && a.q && a.k) visible_diagonals(a, b, (int)W, &first, &count);
-    p.first = first;
-    p.count = count;
-    p.bands = (uint32_t)((count + kWave - 1) / kWave);
+    if (a.batch && a.q && a.k) visible_diagonals(a, b, W, &p.first, &p.count);
+    p.bands = (uint32_t)((p.count + kBand - 1) / kBand);
     if (!p.bands) return p;
-    // four workgroups for every compute unit over pairs and bands, of at least one step to a wave
-    const uint64_t work = (uint64_t)((a.q + W - 1u) / W) * a.batch, most = (work + kBackWaves - 1u) / kBackWaves;
-    const uint64_t have = (uint64_t)p.pairs * p.bands, want = (4u * n_cu + have - 1u) / have;
-    p.splits = (uint32_t)max((uint64_t)1u, min(want, most));
-    p.scratch = (uint64_t)p.pairs * p.bands * p.splits * b.n * sizeof(float);
+    const int q_steps = (int)((a.q + W - 1u) / W), k_steps = (int)((a.k + W - 1u) / W);
+    // eight workgroups for every compute unit over pairs and bands, of at least one item to a group of lanes
+    const uint64_t want = max((uint64_t)1u, (8u * (uint64_t)n_cu + p.pairs - 1u) / p.pairs);      // of a pair
+    if (p.bands > kMaxBands) {
+        const uint64_t most = ((uint64_t)q_steps * a.batch + kBackGroups - 1u) / kBackGroups;
+        p.even = (uint32_t)min((want + p.bands - 1u) / p.bands, most);
+        p.blocks = p.bands * p.even;
+    } else {
+        uint64_t items[kMaxBands], all = 0;
+        for (uint32_t i = 0; i < p.bands; ++i) {
+            const int64_t D0 = p.first + (int64_t)i * kBand, D1 = min(D0 + kBand, p.first + p.count) - 1;
+            const BandSteps s = band_steps(D0, D1, q_steps, k_steps);
+            all += items[i] = (uint64_t)(s.s1 - s.s0) * a.batch;
+        }
+        const uint64_t each = max((uint64_t)kBackGroups, (all + want - 1u) / want);       // items of a workgroup
+        for (uint32_t i = 0; i < p.bands; ++i) {
+            p.first_block[i] = p.blocks;
+            p.blocks += (uint32_t)max((uint64_t)1u, (items[i] + each - 1u) / each);
+        }
+        p.first_block[p.bands] = p.blocks;
+    }
+    p.scratch = (uint64_t)p.pairs * p.blocks * b.n * sizeof(float);
     return p;
 }
 
 template <typename T>
 static hipError_t launch_bias_back_of(const BiasArgs& a, const BucketArgs& b, const BiasBackPlan& p, float* partial, hipStream_t st)
 {
-    hipLaunchKernelGGL(k_position_bias_back<T>, dim3(p.bands * p.splits, min(p.pairs, 65535u)), dim3(kBiasThreads), 0, st, a, b, p, partial);
+    hipLaunchKernelGGL(k_position_bias_back<T>, dim3(p.blocks, min(p.pairs, 65535u)), dim3(kBiasThreads), 0, st, a, b, p, partial);
     return hipGetLastError();
 }
 
@@ -294,8 +437,8 @@ hipError_t launch_position_bias_back(int dtype, const BiasArgs& a, const BucketA
         if (e != hipSuccess) return e;
     }
     const uint64_t outputs = (uint64_t)(p.pairs / a.heads) * table_rows * a.heads;
-    hipLaunchKernelGGL(k_position_bias_join, dim3((uint32_t)min((outputs + kBackWaves - 1u) / kBackWaves, (uint64_t)1u << 20)), dim3(kBiasThreads), 0, st,
-                       b, p, a.heads, table_rows, p.bands * p.splits, partial, dtable, param_stride);
+    hipLaunchKernelGGL(k_position_bias_join, dim3((uint32_t)min((outputs + kBiasWaves - 1u) / kBiasWaves, (uint64_t)1u << 20)), dim3(kBiasThreads), 0, st,
+                       b, p, a.heads, table_rows, p.blocks, partial, dtable, param_stride);
     return hipGetLastError();
 }
 

@@ -15,6 +15,12 @@ template <typename T> struct PieceOf { typedef T type __attribute__((ext_vector_
 template <typename T> using Piece = typename PieceOf<T>::type;
 
 template <typename T>
+__device__ __forceinline__ nt_u32x4 load_bits(const T* p)
+{
+    return __builtin_bit_cast(nt_u32x4, *reinterpret_cast<const Piece<T>*>(p));
+}
+
+template <typename T>
 __device__ __forceinline__ void load_piece(const T* p, float (&v)[kPiece<T>])
 {
     const Piece<T> x = *reinterpret_cast<const Piece<T>*>(p);

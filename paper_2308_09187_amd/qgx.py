@@ -117,21 +117,30 @@ def _stream_handle(stream):
     return C.c_void_p(stream.cuda_stream)
 
 
-def _need(ok, text):
+def _need(ok, text, *what):
     if not ok:
-        raise QgxError(ERR_ARG, text)
+        raise QgxError(ERR_ARG, text % what if what else text)
 
 
-def _on(stream):
-    """Memory made for a call on `stream` comes from that stream's pool, so that its next use is in order after the call."""
-    return torch.cuda.stream(stream)             # (None: the current stream stays)
+def _handle(stream):
+    """The stream's handle as a number, for the functions whose argument types are given."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
+
+
+def _empty(like, shape, dtype, stream):
+    """Memory on like's device (new_empty: 1.5 us, torch.empty 2.3).  Made for a call on `stream` it comes from that
+    stream's pool, so that its next use is in order after the call."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _parameter(t, shape, name):
     """Address of a contiguous binary32 parameter, or of a run of one; None stays None."""
     if t is None:
         return None
-    _need(t.is_cuda and t.dtype == torch.float32 and tuple(t.shape) == shape and t.is_contiguous(), "%s: contiguous float32 of shape %s on the GPU" % (name, shape))
+    _need(t.is_cuda and t.dtype == torch.float32 and t.shape == shape and t.is_contiguous(), "%s: contiguous float32 of shape %s on the GPU", name, tuple(shape))
     return t.data_ptr()
 
 
@@ -156,6 +165,7 @@ class TensorList:
 
     def __init__(self, tensors, table, struct):
         self.tensors, self.table, self._c = tensors, table, struct
+        self._ref = C.addressof(struct)
 
 
 class Stream:
@@ -193,6 +203,8 @@ class Context:
             nseg = len(segment_len)
         cfg = _Config(self.d, self.K, self.bucket, nseg, seg, norm, code, seed)
         self._h = C.c_void_p()
+        self._need_bytes = C.c_uint64()           # where the scratch functions answer
+        self._need_ref = C.addressof(self._need_bytes)
         self._table, self._n_sym = 0, {}          # the table selected; symbols of each table that was set
         with torch.cuda.device(device):
             st = self.lib.qgx_create(C.byref(self._h), C.byref(cfg))
@@ -332,14 +344,14 @@ class Context:
         _need(len(offsets) == len(tensors), "tensor_list: an offset for every tensor")
         arr = (_Tensor * max(1, len(tensors)))()
         for i, (t, off) in enumerate(zip(tensors, offsets)):
-            _need(t.is_cuda and t.dtype in DTYPES, "tensor %d: float32, float16 or bfloat16 on the GPU" % i)
-            _need((t.dim() == 2 and t.shape[0] == self.K) or (t.dim() == 1 and self.K == 1), "tensor %d: shape [K, n]" % i)
-            _need(_dense_last(t), "tensor %d: a worker's elements must be contiguous" % i)
+            _need(t.is_cuda and t.dtype in DTYPES, "tensor %d: float32, float16 or bfloat16 on the GPU", i)
+            _need((t.dim() == 2 and t.shape[0] == self.K) or (t.dim() == 1 and self.K == 1), "tensor %d: shape [K, n]", i)
+            _need(_dense_last(t), "tensor %d: a worker's elements must be contiguous", i)
+            _need(int(off) >= 0, "tensor %d: offset below 0", i)
             arr[i] = _Tensor(t.data_ptr(), t.shape[-1], t.stride(0) if t.dim() == 2 and self.K > 1 else 0, int(off), DTYPES[t.dtype])
         need, out = C.c_uint64(), _TensorList()
         self._check(self.lib.qgx_tensor_list_size(self._h, arr, C.c_uint32(len(tensors)), C.byref(need)))
-        with _on(stream):
-            table = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+        table = _empty(torch.empty(0, device=self.device), (need.value,), torch.uint8, stream)
         self._check(self.lib.qgx_tensor_list_set(self._h, arr, C.c_uint32(len(tensors)), _ptr(table), need, C.byref(out), _stream_handle(stream)))
         return TensorList(tensors, table, out)
 
@@ -347,124 +359,144 @@ class Context:
         """Clips every worker's gradients to the global norm max_norm, into out = V [K, d] or, without it, in place.
         Returns the workers' norms before, [K]."""
         if out is not None:
-            _need(out.is_cuda and out.dtype == torch.float32 and tuple(out.shape) == (self.K, self.d) and out.is_contiguous(),
+            _need(out.is_cuda and out.dtype == torch.float32 and out.shape == (self.K, self.d) and out.is_contiguous(),
                   "clip_gradients: out is V [K, d], contiguous float32 on the GPU")
-        with _on(stream):
-            norms = torch.empty(self.K, dtype=torch.float32, device=self.device)
-        self._check(self.lib.qgx_clip_gradients(self._h, C.addressof(tensors._c), norm, max_norm, None if out is None else out.data_ptr(),
-                                                norms.data_ptr(), _stream_handle(stream)))
+        norms = _empty(tensors.table, (self.K,), torch.float32, stream)
+        st = self.lib.qgx_clip_gradients(self._h, tensors._ref, norm, max_norm, None if out is None else out.data_ptr(),
+                                         norms.data_ptr(), _handle(stream))
+        if st:
+            self._check(st)
         return norms
 
     @staticmethod
-    def _rows(t, name, like=None):
-        """(workers, rows, cols, step between workers, between rows) of [workers, rows, cols], [rows, cols] or [cols]."""
-        _need(t.is_cuda and t.dtype in DTYPES, "%s: float32, float16 or bfloat16 on the GPU" % name)
-        _need(1 <= t.dim() <= 3 and _dense_last(t), "%s: [workers, rows, cols], [rows, cols] or [cols], rows contiguous" % name)
-        _need(like is None or (t.shape == like.shape and t.dtype == like.dtype), "%s: of x's shape and type" % name)
-        sh, st = t.shape, t.stride()
-        if t.dim() == 3:
-            return sh[0], sh[1], sh[2], st[0], st[1]
-        return (1, sh[0], sh[1], 0, st[0]) if t.dim() == 2 else (1, 1, sh[0], 0, 0)
+    def _rows(t, name):
+        """(type, workers, rows, cols, step between workers, between rows) of [workers, rows, cols], [rows, cols] or [cols]."""
+        code, shape, step = DTYPES.get(t.dtype), t.shape, t.stride()
+        _need(code is not None and t.is_cuda, "%s: float32, float16 or bfloat16 on the GPU", name)
+        _need(1 <= len(shape) <= 3 and (step[-1] == 1 or shape[-1] <= 1), "%s: [workers, rows, cols], [rows, cols] or [cols], rows contiguous", name)
+        if len(shape) == 3:
+            return code, shape[0], shape[1], shape[2], step[0], step[1]
+        return (code, 1, shape[0], shape[1], 0, step[0]) if len(shape) == 2 else (code, 1, 1, shape[0], 0, 0)
+
+    @staticmethod
+    def _rows_like(t, x, name):
+        """The steps of a tensor of x's shape and type."""
+        _need(t.shape == x.shape and t.dtype == x.dtype and t.is_cuda, "%s: of x's shape and type, on the GPU", name)
+        step = t.stride()
+        _need(step[-1] == 1 or t.shape[-1] <= 1, "%s: rows must be contiguous", name)
+        return (step[0], step[1]) if len(step) == 3 else (0, step[0] if len(step) == 2 else 0)
 
     def layer_norm(self, x, weight=None, bias=None, eps=1e-5, out=None, save=True, stream=None):
         """Layer norm over the last dimension of x.  Returns (y, mean, rstd), the last two what the backward pass takes
         (save=False: None); weight and bias float32 [cols], runs of X say, or None."""
-        wk, rows, cols, xw, xr = self._rows(x, "x")
+        code, wk, rows, cols, xw, xr = self._rows(x, "x")
         w, b = _parameter(weight, (cols,), "weight"), _parameter(bias, (cols,), "bias")
-        with _on(stream):
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-            mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if save else None
-            rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if save else None
-        _, _, _, yw, yr = self._rows(y, "out", x)
-        self._check(self.lib.qgx_layer_norm(self._h, DTYPES[x.dtype], wk, rows, cols, x.data_ptr(), xw, xr, w, b, eps, y.data_ptr(), yw, yr,
-                                            mean.data_ptr() if save else None, rstd.data_ptr() if save else None, _stream_handle(stream)))
-        return y, mean, rstd
+        if out is None:
+            out, yw, yr = _empty(x, x.shape, x.dtype, stream), rows * cols, cols
+        else:
+            yw, yr = self._rows_like(out, x, "out")
+        mean = rstd = None
+        if save:
+            mean, rstd = _empty(x, (2,) + x.shape[:-1], torch.float32, stream).unbind(0)
+        st = self.lib.qgx_layer_norm(self._h, code, wk, rows, cols, x.data_ptr(), xw, xr, w, b, eps, out.data_ptr(), yw, yr,
+                                     mean.data_ptr() if save else None, rstd.data_ptr() if save else None, _handle(stream))
+        if st:
+            self._check(st)
+        return out, mean, rstd
 
     def layer_norm_backward(self, dy, x, weight, mean, rstd, dw=None, db=None, dx=None, need_dx=True, stream=None):
         """Returns dx (None with need_dx=False) and writes the workers' weight and bias gradients, the sums over their
         rows, to dw and db: float32 [workers, cols], runs of V's rows say (or [cols] where x has no worker dimension)."""
-        wk, rows, cols, xw, xr = self._rows(x, "x")
-        _, _, _, gw, gr = self._rows(dy, "dy", x)
+        code, wk, rows, cols, xw, xr = self._rows(x, "x")
+        gw, gr = self._rows_like(dy, x, "dy")
         w = _parameter(weight, (cols,), "weight")
-        m, r = _parameter(mean, tuple(x.shape[:-1]), "mean"), _parameter(rstd, tuple(x.shape[:-1]), "rstd")
+        lead = x.shape[:-1]
+        m, r = _parameter(mean, lead, "mean"), _parameter(rstd, lead, "rstd")
         step = None
         for t, name in ((dw, "dw"), (db, "db")):
             if t is None:
                 continue
-            _need(t.is_cuda and t.dtype == torch.float32 and t.shape[-1] == cols and _dense_last(t) and
-                  ((t.dim() == 2 and t.shape[0] == wk) or (t.dim() == 1 and wk == 1)), "%s: float32 [workers, cols] on the GPU" % name)
-            s = t.stride(0) if t.dim() == 2 and wk > 1 else cols
-            _need(step in (None, s), "dw and db: one step between workers")
+            _need(t.is_cuda and t.dtype == torch.float32 and (t.shape == (wk, cols) or (wk == 1 and t.shape == (cols,))) and _dense_last(t),
+                  "%s: float32 [workers, cols] on the GPU", name)
+            s = t.stride(0) if wk > 1 else cols
+            _need(step is None or step == s, "dw and db: one step between workers")
             step = s
-        with _on(stream):
-            if dx is None and need_dx:
-                dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-            need = C.c_uint64()
-            self._check(self.lib.qgx_layer_norm_scratch(self._h, DTYPES[x.dtype], wk, rows, cols, C.addressof(need)))
-            scratch = torch.empty(need.value, dtype=torch.uint8, device=x.device) if need.value else None
-        _, _, _, dw_, dr = (0, 0, 0, 0, 0) if dx is None else self._rows(dx, "dx", x)
-        self._check(self.lib.qgx_layer_norm_backward(
-            self._h, DTYPES[x.dtype], wk, rows, cols, dy.data_ptr(), gw, gr, x.data_ptr(), xw, xr, w, m, r,
-            None if dx is None else dx.data_ptr(), dw_, dr, None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
-            cols if step is None else step, None if scratch is None else scratch.data_ptr(), need.value, _stream_handle(stream)))
+        ow = orow = 0
+        if dx is not None:
+            ow, orow = self._rows_like(dx, x, "dx")
+        elif need_dx:
+            dx, ow, orow = _empty(x, x.shape, x.dtype, stream), rows * cols, cols
+        need, scratch = self._need_bytes, None
+        st = self.lib.qgx_layer_norm_scratch(self._h, code, wk, rows, cols, self._need_ref)
+        if not st:
+            if need.value:
+                scratch = _empty(x, (need.value,), torch.uint8, stream)
+            st = self.lib.qgx_layer_norm_backward(
+                self._h, code, wk, rows, cols, dy.data_ptr(), gw, gr, x.data_ptr(), xw, xr, w, m, r,
+                None if dx is None else dx.data_ptr(), ow, orow, None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
+                cols if step is None else step, None if scratch is None else scratch.data_ptr(), need.value, _handle(stream))
+        if st:
+            self._check(st)
         return dx
 
     @staticmethod
     def _scores(t, name):
         """[workers, batch, heads, q, k], [batch, heads, q, k] or [heads, q, k], keys contiguous."""
-        _need(t.is_cuda and t.dtype in DTYPES, "%s: float32, float16 or bfloat16 on the GPU" % name)
-        _need(3 <= t.dim() <= 5 and _dense_last(t), "%s: [workers, batch, heads, q, k], the last dimension contiguous" % name)
-        lead = 5 - t.dim()
-        sh, st = (1,) * lead + tuple(t.shape), (0,) * lead + t.stride()
-        return _Scores(t.data_ptr(), DTYPES[t.dtype], sh[2], sh[0], sh[1], sh[3], sh[4], st[0], st[1], st[2], st[3])
+        code, sh, st = DTYPES.get(t.dtype), t.shape, t.stride()
+        _need(code is not None and t.is_cuda, "%s: float32, float16 or bfloat16 on the GPU", name)
+        n = len(sh)
+        _need(3 <= n <= 5 and (st[-1] == 1 or sh[-1] <= 1), "%s: [workers, batch, heads, q, k], the last dimension contiguous", name)
+        return _Scores(t.data_ptr(), code, sh[-3], sh[0] if n == 5 else 1, sh[-4] if n > 3 else 1, sh[-2], sh[-1],
+                       st[0] if n == 5 else 0, st[-4] if n > 3 else 0, st[-3], st[-2])
 
     def _bias(self, table, buckets, src, out, q_offset, positions, stream):
         o = self._scores(out, "out")
         _need(table.dim() == 2 and table.shape[1] == o.heads, "table: [rows, heads]")
-        tab = _parameter(table, tuple(table.shape), "table")
+        tab = _parameter(table, table.shape, "table")
         pos = None
         if positions is not None:
             _need(positions.is_cuda and positions.dtype == torch.int32 and positions.is_contiguous() and
                   positions.numel() == o.workers * o.batch, "positions: contiguous int32, one for every sequence, on the GPU")
             pos = positions.data_ptr()
         i = None if src is None else self._scores(src, "scores")
-        self._check(self.lib.qgx_position_bias(self._h, buckets._ref, tab, table.shape[0], None if i is None else C.addressof(i),
-                                               C.addressof(o), q_offset, pos, _stream_handle(stream)))
+        st = self.lib.qgx_position_bias(self._h, buckets._ref, tab, table.shape[0], None if i is None else C.addressof(i),
+                                        C.addressof(o), q_offset, pos, _handle(stream))
+        if st:
+            self._check(st)
         return out
 
     def position_bias(self, table, buckets: Buckets, q, k, dtype=torch.float32, q_offset=0, out=None, stream=None):
         """The bias alone, [heads, q, k]: table[row of (j - i - q_offset)][head], -inf where that is masked."""
         if out is None:
-            with _on(stream):
-                out = torch.empty((table.shape[1], q, k), dtype=dtype, device=table.device)
+            out = _empty(table, (table.shape[1], q, k), dtype, stream)
         return self._bias(table, buckets, None, out, q_offset, None, stream)
 
     def add_position_bias(self, scores, table, buckets: Buckets, q_offset=0, positions=None, out=None, stream=None):
         """scores [.., batch, heads, q, k] plus the bias, -inf where a place is masked.  positions int32 [.., batch]: added to
         q_offset sequence by sequence (the position of its first query).  out may be scores."""
         if out is None:
-            with _on(stream):
-                out = torch.empty(scores.shape, dtype=scores.dtype, device=scores.device)
+            out = _empty(scores, scores.shape, scores.dtype, stream)
         return self._bias(table, buckets, scores, out, q_offset, positions, stream)
 
     def position_bias_backward(self, grad, buckets: Buckets, dtable, q_offset=0, stream=None):
         """Writes the table's gradient, float32 [workers, rows, heads] (a run of V's rows say; [rows, heads] where grad has
         no worker dimension), from the gradient of the biased scores."""
         g = self._scores(grad, "grad")
-        _need(dtable.is_cuda and dtable.dtype == torch.float32 and dtable.dim() == (3 if grad.dim() == 5 else 2) and
-              dtable.shape[-1] == g.heads, "dtable: float32 [workers, rows, heads] on the GPU")
-        rows = dtable.shape[-2]
-        _need((rows <= 1 or dtable.stride(-2) == g.heads) and _dense_last(dtable) and (dtable.dim() == 2 or dtable.shape[0] == g.workers),
-              "dtable: a worker's table must be contiguous")
-        need = C.c_uint64()
-        self._check(self.lib.qgx_position_bias_scratch(self._h, buckets._ref, C.addressof(g), q_offset, C.addressof(need)))
-        scratch = None
-        if need.value:
-            with _on(stream):
-                scratch = torch.empty(need.value, dtype=torch.uint8, device=grad.device)
-        step = dtable.stride(0) if dtable.dim() == 3 and g.workers > 1 else rows * g.heads
-        self._check(self.lib.qgx_position_bias_backward(self._h, buckets._ref, C.addressof(g), q_offset, dtable.data_ptr(), rows, step,
-                                                        None if scratch is None else scratch.data_ptr(), need.value, _stream_handle(stream)))
+        sh, step = dtable.shape, dtable.stride()
+        _need(dtable.is_cuda and dtable.dtype == torch.float32 and len(sh) == (3 if grad.dim() == 5 else 2) and sh[-1] == g.heads and
+              (len(sh) == 2 or sh[0] == g.workers), "dtable: float32 [workers, rows, heads] on the GPU")
+        rows = sh[-2]
+        _need((rows <= 1 or step[-2] == g.heads) and (step[-1] == 1 or g.heads == 1), "dtable: a worker's table must be contiguous")
+        need, scratch = self._need_bytes, None
+        st = self.lib.qgx_position_bias_scratch(self._h, buckets._ref, C.addressof(g), q_offset, self._need_ref)
+        if not st:
+            if need.value:
+                scratch = _empty(grad, (need.value,), torch.uint8, stream)
+            st = self.lib.qgx_position_bias_backward(self._h, buckets._ref, C.addressof(g), q_offset, dtable.data_ptr(), rows,
+                                                     step[0] if len(sh) == 3 and g.workers > 1 else rows * g.heads,
+                                                     None if scratch is None else scratch.data_ptr(), need.value, _handle(stream))
+        if st:
+            self._check(st)
         return dtable
 
     # -- DEQ o CODE and the fused updates ---------------------------------------------------------
