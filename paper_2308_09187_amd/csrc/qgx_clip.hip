@@ -51,23 +51,25 @@ template <typename T, bool MAX>
 __device__ __forceinline__ void sum_piece(const T* x, int n, ClipSum<MAX>& s)
 {
     constexpr int W = kPiece<T>, N = (int)kClipPiece / (kClipThreads * W);
-    Piece<T> v[N];
+    nt_u32x4 x4[N];
     const int i0 = (int)threadIdx.x * W;
     if (n == (int)kClipPiece) {                            // (the same for the whole workgroup: all loads are under way at once)
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = __builtin_nontemporal_load(reinterpret_cast<const Piece<T>*>(x + i0 + j * kClipThreads * W));
+        for (int j = 0; j < N; ++j) x4[j] = __builtin_bit_cast(nt_u32x4, __builtin_nontemporal_load(reinterpret_cast<const Piece<T>*>(x + i0 + j * kClipThreads * W)));
     } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = load_raw(x + i0 + j * kClipThreads * W, n - i0 - j * kClipThreads * W);
+        for (int j = 0; j < N; ++j) x4[j] = __builtin_bit_cast(nt_u32x4, load_raw(x + i0 + j * kClipThreads * W, n - i0 - j * kClipThreads * W));
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j)
+    for (int j = 0; j < N; ++j) {
+        float v[W];
+        values_of<T>(x4[j], v);
 #pragma unroll
         for (int c = 0; c < W; ++c) {
-            const float y = (float)v[j][c];
-            if constexpr (MAX) s.x = __builtin_elementwise_maximum(s.x, fabsf(y));
-            else s.x = fma((double)y, (double)y, s.x);
+            if constexpr (MAX) s.x = __builtin_elementwise_maximum(s.x, fabsf(v[c]));
+            else s.x = fma((double)v[c], (double)v[c], s.x);
         }
+    }
 }
 
 // The sum over a workgroup, in its first thread.

@@ -8,6 +8,14 @@ namespace qgx {
 
 template <int LANES> constexpr int kNormThreads = LANES > 256 ? LANES : 256;
 template <int LANES> constexpr int kNormGroups = kNormThreads<LANES> / LANES;     // groups of LANES threads in a workgroup
+// A thread's group: the same in all lanes of a wave, and known to be, where a group has whole waves.
+template <int LANES>
+__device__ __forceinline__ uint32_t norm_group()
+{
+    if constexpr (kNormGroups<LANES> == 1) return 0u;
+    else if constexpr (LANES == kWave) return (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / LANES));
+    else return threadIdx.x / LANES;
+}
 constexpr uint32_t kNormBlocksMax = 1u << 20;             // workgroups of a launch (a grid's threads stay below 2^32); they go on from there
 
 // The sums over the LANES threads of a row, of M values at once, in each of the threads.  slot: LDS of these sums' own,
@@ -83,7 +91,7 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm(NormArgs a)
     PieceAt at[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) at[j] = piece_at<W, LANES>(lane, j, cols);
-    for (uint64_t first = ((uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES) * R; first < a.n_rows; first += (uint64_t)gridDim.x * kGroups * R) {
+    for (uint64_t first = ((uint64_t)blockIdx.x * kGroups + norm_group<LANES>()) * R; first < a.n_rows; first += (uint64_t)gridDim.x * kGroups * R) {
         float v[R][N][W], sum[R], sq[R];
         uint32_t k[R], r[R];
 #pragma unroll
@@ -129,7 +137,7 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm(NormArgs a)
             for (int q = 0; q < R; ++q) {
 #pragma unroll
                 for (int c = 0; c < W; ++c) v[q][j][c] = fmaf(v[q][j][c] * sq[q], w[c], b[c]);
-                if (at[j].any && first + q < a.n_rows) store_piece((T*)a.y + k[q] * a.y_worker + r[q] * a.y_row + at[j].c, v[q][j]);
+                if (at[j].any && first + q < a.n_rows) stream_piece((T*)a.y + k[q] * a.y_worker + r[q] * a.y_row + at[j].c, v[q][j]);
             }
         }
         if (lane == 0)
@@ -207,7 +215,8 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
     constexpr int W = kPiece<T>, kGroups = kNormGroups<LANES>;
     __shared__ float s_sum[2][2 * R][kNormSlots];
     __shared__ float s_cols[kGroups > 1 ? kGroups : 1][kGroups > 1 ? LANES * N * W : 1];
-    const int lane = (int)(threadIdx.x % LANES), cols = (int)a.cols, group = (int)(threadIdx.x / LANES);
+    const int lane = (int)(threadIdx.x % LANES), cols = (int)a.cols;
+    const uint32_t group = norm_group<LANES>();
     const uint32_t k = blockIdx.y;
     float w[N][W], dw[N][W], db[N][W];
     PieceAt at[N];
@@ -218,42 +227,65 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
 #pragma unroll
         for (int c = 0; c < W; ++c) dw[j][c] = db[j][c] = 0.0f;
     }
-    int turn = 0;
-    for (uint32_t set = blockIdx.x; (uint64_t)set * kGroups * R < a.rows; set += a.parts, turn ^= 1) {
-        const uint32_t first = (set * kGroups + (uint32_t)group) * R;
-        nt_u32x4 x[R][N], dy[R][N];                        // as loaded: half the registers of their values in binary32
-        float mean[R], rstd[R], sum[2 * R];
+    // Of a set of rows, as loaded: half the registers of the values in binary32.  The next set's loads are under way before this one's dx is
+    // stored: a wave's loads and stores are waited for in their order.
+    nt_u32x4 x[R][N], dy[R][N], next_x[R][N], next_dy[R][N];
+    float mean[R], rstd[R], next_mean[R], next_rstd[R], sum[2 * R];
+    const uint32_t sets = (a.rows + (kGroups * R - 1u)) / (kGroups * R);
+    auto load = [&](uint32_t set) {
 #pragma unroll
         for (int q = 0; q < R; ++q) {
             // (in place of a row past the last: zeros)
-            const bool ok = first + q < a.rows;
-            const uint32_t r = ok ? first + q : a.rows - 1u;
+            const uint32_t at_row = (set * kGroups + group) * R + q, r = min(at_row, a.rows - 1u);
+            const bool ok = at_row < a.rows;
             const T* px = (const T*)a.x + k * a.x_worker + r * a.x_row;
             const T* pg = (const T*)a.dy + k * a.dy_worker + r * a.dy_row;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                x[q][j] = load_bits(px + at[j].c);
-                dy[q][j] = load_bits(pg + at[j].c);
-                if (!ok) x[q][j] = dy[q][j] = nt_u32x4{0u, 0u, 0u, 0u};
+                next_x[q][j] = load_bits(px + at[j].c);
+                next_dy[q][j] = load_bits(pg + at[j].c);
+                if (!ok) next_x[q][j] = next_dy[q][j] = nt_u32x4{0u, 0u, 0u, 0u};
             }
-            mean[q] = ok ? a.mean[(size_t)k * a.rows + r] : 0.0f;
-            rstd[q] = ok ? a.rstd[(size_t)k * a.rows + r] : 0.0f;
+            next_mean[q] = a.mean[(size_t)k * a.rows + r];
+            next_rstd[q] = a.rstd[(size_t)k * a.rows + r];
+            if (!ok) next_mean[q] = next_rstd[q] = 0.0f;
         }
+    };
+    if (blockIdx.x < sets) load(blockIdx.x);
+    int turn = 0;
+    for (uint32_t set = blockIdx.x; set < sets; set += a.parts, turn ^= 1) {
+        const uint32_t first = (set * kGroups + group) * R;
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                x[q][j] = next_x[q][j];
+                dy[q][j] = next_dy[q][j];
+            }
+            mean[q] = next_mean[q];
+            rstd[q] = next_rstd[q];
+        }
+        if (set + a.parts < sets) load(set + a.parts);     // (the same for the whole workgroup)
 #pragma unroll
         for (int q = 0; q < R; ++q) {
             sum[q] = sum[R + q] = 0.0f;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const Piece<T> px = __builtin_bit_cast(Piece<T>, x[q][j]), pg = __builtin_bit_cast(Piece<T>, dy[q][j]);
+                float u[W], v[W];
+                values_of<T>(x[q][j], u);
+                values_of<T>(dy[q][j], v);
 #pragma unroll
                 for (int c = 0; c < W; ++c) {
-                    const float d = (float)pg[c], g = at[j].owns(c) ? d * w[j][c] : 0.0f;
-                    const float h = ((float)px[c] - mean[q]) * rstd[q];
+                    const float d = v[c], g = at[j].owns(c) ? d * w[j][c] : 0.0f;
+                    const float h = (u[c] - mean[q]) * rstd[q];
                     sum[q] += g;
                     sum[R + q] = fmaf(g, h, sum[R + q]);
                     dw[j][c] = fmaf(d, h, dw[j][c]);
                     db[j][c] += d;
                 }
+                // (added here and now: left to the end of the round, the terms would be kept across the sums)
+#pragma unroll
+                for (int c = 0; c < W; ++c) asm volatile("" : "+v"(dw[j][c]), "+v"(db[j][c]));
             }
         }
         if (a.dx) {
@@ -265,14 +297,15 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
                 for (int j = 0; j < N; ++j) {
                     // (worked out again from what was loaded: kept across the sums, g and h would take four times the registers)
                     asm volatile("" : "+v"(x[q][j]), "+v"(dy[q][j]));
-                    const Piece<T> px = __builtin_bit_cast(Piece<T>, x[q][j]), pg = __builtin_bit_cast(Piece<T>, dy[q][j]);
-                    float v[W];
+                    float u[W], v[W];
+                    values_of<T>(x[q][j], u);
+                    values_of<T>(dy[q][j], v);
 #pragma unroll
                     for (int c = 0; c < W; ++c) {
-                        const float g = (float)pg[c] * w[j][c], h = ((float)px[c] - mean[q]) * rstd[q];
+                        const float g = v[c] * w[j][c], h = (u[c] - mean[q]) * rstd[q];
                         v[c] = rstd[q] * (g - m1 - h * m2);
                     }
-                    if (at[j].any && first + q < a.rows) store_piece((T*)a.dx + k * a.dx_worker + (first + q) * a.dx_row + at[j].c, v);
+                    if (at[j].any && first + q < a.rows) stream_piece((T*)a.dx + k * a.dx_worker + (first + q) * a.dx_row + at[j].c, v);
                 }
             }
         }
@@ -464,15 +497,15 @@ struct BackShape { uint32_t lanes, pieces, rows; };
 static BackShape back_shape(uint32_t cols, uint32_t W)
 {
     const uint32_t pieces = (cols + W - 1u) / W;
-    if (cols < W || pieces > 2048u) return BackShape{0, 0, 0};
-    if (pieces <= 4u) return BackShape{4, 1, 4};
-    if (pieces <= 16u) return pieces <= 8u ? BackShape{4, 2, 2} : BackShape{16, 1, 4};
-    if (pieces <= 64u) return pieces <= 32u ? BackShape{16, 2, 2} : BackShape{64, 1, 4};
-    if (pieces <= 128u) return BackShape{64, 2, 2};
-    if (pieces <= 256u) return BackShape{256, 1, 4};
-    if (pieces <= 512u) return BackShape{256, 2, 2};
+    if (cols < W || cols > 16384u) return BackShape{0, 0, 0};          // (32 columns to a thread: their sums alone take 64 registers)
+    if (pieces <= 4u) return BackShape{4, 1, 2};
+    if (pieces <= 16u) return pieces <= 8u ? BackShape{4, 2, 1} : BackShape{16, 1, 2};
+    if (pieces <= 64u) return pieces <= 32u ? BackShape{16, 2, 1} : BackShape{64, 1, 2};
+    if (pieces <= 128u) return BackShape{64, 2, 1};
+    if (pieces <= 256u) return BackShape{256, 1, 2};
+    if (pieces <= 512u) return BackShape{256, 2, 1};
     if (pieces <= 1024u) return BackShape{256, 4, 1};
-    return BackShape{512, 4, 1};
+    return pieces <= 2048u ? BackShape{512, 4, 1} : BackShape{512, 8, 1};
 }
 
 NormBackPlan norm_back_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t cols, uint32_t n_cu)
@@ -483,8 +516,10 @@ NormBackPlan norm_back_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t
     p.sum_stride = (cols + 3u) / 4u * 4u;
     const uint32_t at_once = shape.lanes ? max(256u, shape.lanes) / shape.lanes * shape.rows : 4u;
     const uint32_t sets = rows / at_once + (rows % at_once != 0u);
-    // four workgroups for every compute unit, over all workers (and, where rows are long, over the columns)
-    const uint32_t want = max(1u, 4u * n_cu / (workers * (shape.lanes ? 1u : (pieces + 255u) / 256u)));
+    // a few workgroups for every compute unit, over all workers (and, where rows are long, over the columns)
+    // (the more columns, the more a workgroup's sums weigh: 8 x 1024 x 16384 bfloat16 204 us with four for each, 179 with two)
+    const uint32_t each = shape.pieces >= 4u ? 2u : shape.lanes ? 3u : 4u;
+    const uint32_t want = max(1u, each * n_cu / (workers * (shape.lanes ? 1u : (pieces + 255u) / 256u)));
     p.parts = max(1u, min(sets, want));
     p.scratch = p.parts == 1u ? 0 : (uint64_t)workers * p.parts * 2u * p.sum_stride * sizeof(float);
     return p;
@@ -502,13 +537,15 @@ static hipError_t launch_back_of(const NormBackArgs& a, uint32_t workers, hipStr
 {
     const uint32_t pieces = (a.cols + kPiece<T> - 1u) / kPiece<T>;
     const BackShape s = back_shape(a.cols, kPiece<T>);
-    if (s.lanes == 4u) return s.pieces == 1u ? launch_back_as<T, 4, 1, 4>(a, workers, st) : launch_back_as<T, 4, 2, 2>(a, workers, st);
-    if (s.lanes == 16u) return s.pieces == 1u ? launch_back_as<T, 16, 1, 4>(a, workers, st) : launch_back_as<T, 16, 2, 2>(a, workers, st);
-    if (s.lanes == 64u) return s.pieces == 1u ? launch_back_as<T, 64, 1, 4>(a, workers, st) : launch_back_as<T, 64, 2, 2>(a, workers, st);
+    if (s.lanes == 4u) return s.pieces == 1u ? launch_back_as<T, 4, 1, 2>(a, workers, st) : launch_back_as<T, 4, 2, 1>(a, workers, st);
+    if (s.lanes == 16u) return s.pieces == 1u ? launch_back_as<T, 16, 1, 2>(a, workers, st) : launch_back_as<T, 16, 2, 1>(a, workers, st);
+    if (s.lanes == 64u) return s.pieces == 1u ? launch_back_as<T, 64, 1, 2>(a, workers, st) : launch_back_as<T, 64, 2, 1>(a, workers, st);
     if (s.lanes == 256u)
-        return s.pieces == 1u   ? launch_back_as<T, 256, 1, 4>(a, workers, st)
-               : s.pieces == 2u ? launch_back_as<T, 256, 2, 2>(a, workers, st)
+        return s.pieces == 1u   ? launch_back_as<T, 256, 1, 2>(a, workers, st)
+               : s.pieces == 2u ? launch_back_as<T, 256, 2, 1>(a, workers, st)
                                 : launch_back_as<T, 256, 4, 1>(a, workers, st);
+    if constexpr (sizeof(T) == 4)
+        if (s.pieces == 8u) return launch_back_as<T, 512, 8, 1>(a, workers, st);
     if (s.lanes == 512u) return launch_back_as<T, 512, 4, 1>(a, workers, st);
     if (a.dx && a.n_rows) {
         const dim3 grid(min(a.n_rows, kNormBlocksMax));

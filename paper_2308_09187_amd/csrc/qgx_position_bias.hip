@@ -17,16 +17,42 @@ __device__ __forceinline__ int position_of(const BiasArgs& a, uint32_t seq)
     return (int)max((int64_t)-(1 << 30), min(p, (int64_t)(1 << 30)));
 }
 
-// The intervals in a wave's registers, i and i + 64 in lane i.
+// The intervals in a wave's registers, i and i + 64 in lane i (past the last: it again).
 struct Intervals {
     int bound0, bound1, end0, end1;
     uint32_t row0, row1;
-    bool is0, is1;
+    bool is0, is1, more;                                   // there is one; more than 64 in all
     __device__ __forceinline__ explicit Intervals(const BucketArgs& b)
     {
-        const uint32_t i = (uint32_t)lane_id(), i0 = min(i, b.n - 1u), i1 = min(i + kWave, b.n - 1u);
+        const uint32_t i = (uint32_t)lane_id(), i0 = min(i, b.n - 1u);
         bound0 = b.bounds[i0]; end0 = b.bounds[i0 + 1u]; row0 = b.rows[i0]; is0 = i < b.n;
-        bound1 = b.bounds[i1]; end1 = b.bounds[i1 + 1u]; row1 = b.rows[i1]; is1 = i + kWave < b.n;
+        bound1 = bound0; end1 = end0; row1 = row0; is1 = i + kWave < b.n; more = b.n > (uint32_t)kWave;
+        if (more) {
+            const uint32_t i1 = min(i + kWave, b.n - 1u);
+            bound1 = b.bounds[i1]; end1 = b.bounds[i1 + 1u]; row1 = b.rows[i1];
+        }
+    }
+    // x0 of lane i, or x1 of lane i - 64.  (Every lane has to be here, as for any exchange between lanes.)
+    template <typename X>
+    __device__ __forceinline__ X lookup(int i, X x0, X x1) const
+    {
+        const int y0 = __builtin_amdgcn_ds_bpermute(i * 4, __builtin_bit_cast(int, x0));
+        if (!more) return __builtin_bit_cast(X, y0);
+        const int y1 = __builtin_amdgcn_ds_bpermute(i * 4, __builtin_bit_cast(int, x1));      // (the lane's number counts modulo 64)
+        return __builtin_bit_cast(X, i < kWave ? y0 : y1);
+    }
+    // The last interval that starts at delta or before, 0 where none does: a binary search through the lanes.
+    __device__ __forceinline__ int at(int delta) const
+    {
+        int i = more && __builtin_amdgcn_readfirstlane(bound1) <= delta ? kWave : 0;
+#pragma unroll
+        for (int step = kWave / 2; step > 0; step /= 2)
+            if (lookup(i + step, bound0, bound1) <= delta) i += step;
+        return i;
+    }
+    __device__ __forceinline__ int number(int first, int end) const
+    {
+        return __popcll(__ballot(is0 && bound0 < end && end0 > first)) + __popcll(__ballot(is1 && bound1 < end && end1 > first));
     }
     // f(i, j, x0, x1) for every interval that meets first .. end: i its number, j its lane's, x0 .. x1 what it has of that run
     template <typename F>
@@ -76,6 +102,8 @@ constexpr int wave_diagonals(int W) { return 65 * W; }
 // One word is left out after every W, so that lanes W entries apart do not meet in a bank.
 template <int W> __device__ __forceinline__ uint32_t diagonal_slot(uint32_t x) { return x + x / W; }
 
+constexpr int kFewIntervals = 6;
+
 // GUARDED: squares with something in common write it once.  In place a square's scores may otherwise have been overwritten by the
 // one it overlaps before they are read.
 template <typename T, int ROWS, bool GUARDED>
@@ -113,12 +141,19 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias(BiasArgs a, Buck
     const int d1 = min((int)(end * W), k) - min((int)(band0 * ROWS), q - ROWS) - p;
     const Intervals interval(b);
     // (all intervals' biases at once: one after the other they would be the longest wait there is)
-    const float value0 = interval.is0 ? a.table[(size_t)interval.row0 * a.heads + head] : 0.0f;
-    const float value1 = interval.is1 ? a.table[(size_t)interval.row1 * a.heads + head] : 0.0f;
-    interval.meeting(d0, d1, [&](int i, int j, int x0, int x1) {
-        const float value = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(i < kWave ? value0 : value1), j));
-        for (int x = x0 + lane; x < x1; x += kWave) list[diagonal_slot<W>((uint32_t)(x - d0))] = value;
-    });
+    const float value0 = a.table[(size_t)interval.row0 * a.heads + head], value1 = a.table[(size_t)interval.row1 * a.heads + head];
+    // Three in four waves of long rows meet one interval or two; where there are many (they take 0.1 us each), every diagonal is searched for.
+    if (interval.number(d0, d1) <= kFewIntervals) {
+        interval.meeting(d0, d1, [&](int i, int j, int x0, int x1) {
+            const float value = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(i < kWave ? value0 : value1), j));
+            for (int x = x0 + lane; x < x1; x += kWave) list[diagonal_slot<W>((uint32_t)(x - d0))] = value;
+        });
+    } else {
+        for (int x0 = 0; x0 < d1 - d0; x0 += kWave) {
+            const float value = interval.lookup(interval.at(d0 + x0 + lane), value0, value1);
+            if (x0 + lane < d1 - d0) list[diagonal_slot<W>((uint32_t)(x0 + lane))] = value;
+        }
+    }
     wave_lds_fence();
     if (!any) return;
     float bias[ROWS + W - 1];                              // of delta0 - (ROWS - 1) on
@@ -126,7 +161,7 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias(BiasArgs a, Buck
 #pragma unroll
     for (int e = 0; e < ROWS + W - 1; ++e) {
         const int delta = delta0 - (ROWS - 1) + e;
-        bias[e] = list[diagonal_slot<W>((uint32_t)(delta - d0))];      // (what no interval has is no number; it is not used)
+        bias[e] = list[diagonal_slot<W>((uint32_t)(delta - d0))];      // (of a masked one: anything, and not used)
         seen[e] = delta >= lo && delta < hi;
     }
     T* out = (T*)a.out + worker * a.o_worker + n * a.o_batch + head * a.o_head + (uint32_t)i0 * a.o_row + j0;
@@ -135,7 +170,7 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias(BiasArgs a, Buck
 #pragma unroll
         for (int c = 0; c < W; ++c) v[r][c] = seen[ROWS - 1 - r + c] ? v[r][c] + bias[ROWS - 1 - r + c] : -__builtin_inff();
         if constexpr (!GUARDED) {
-            store_piece(out + (uint32_t)r * a.o_row, v[r]);
+            stream_piece(out + (uint32_t)r * a.o_row, v[r]);       // (8 x 16 x 1024 x 1024 bfloat16: 106 us with plain stores, 90; loads so marked lose on odd rows)
         } else if (i0 + r >= i_at) {
             if (j0 == j_at) store_piece(out + (uint32_t)r * a.o_row, v[r]);
             else
@@ -311,9 +346,10 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a,
             }
 #pragma unroll
             for (int r = 0; r < W; ++r) {
-                const Piece<T> v = __builtin_bit_cast(Piece<T>, raw[r]);
+                float v[W];
+                values_of<T>(raw[r], v);
 #pragma unroll
-                for (int c = 0; c < W; ++c) sum[c - r + W - 1] += (float)v[c];
+                for (int c = 0; c < W; ++c) sum[c - r + W - 1] += v[c];
                 raw[r] = next[r];
             }
             n += hop_n;

@@ -20,12 +20,31 @@ __device__ __forceinline__ nt_u32x4 load_bits(const T* p)
     return __builtin_bit_cast(nt_u32x4, *reinterpret_cast<const Piece<T>*>(p));
 }
 
+// The elements of a piece out of its four words.  (Word by word: taken from a vector of 16-bit elements, the compiler keeps each in a
+// register of its own from the load on.)
+template <typename T>
+__device__ __forceinline__ void values_of(nt_u32x4 x, float (&v)[kPiece<T>])
+{
+    typedef _Float16 pair __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            v[i] = __uint_as_float(x[i]);
+        } else if constexpr (__is_same(T, _Float16)) {
+            const pair h = __builtin_bit_cast(pair, (uint32_t)x[i]);
+            v[2 * i] = (float)h.x;
+            v[2 * i + 1] = (float)h.y;
+        } else {
+            v[2 * i] = __uint_as_float(x[i] << 16);
+            v[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+        }
+    }
+}
+
 template <typename T>
 __device__ __forceinline__ void load_piece(const T* p, float (&v)[kPiece<T>])
 {
-    const Piece<T> x = *reinterpret_cast<const Piece<T>*>(p);
-#pragma unroll
-    for (int i = 0; i < kPiece<T>; ++i) v[i] = (float)x[i];
+    values_of<T>(load_bits(p), v);
 }
 
 template <typename T>
@@ -35,6 +54,16 @@ __device__ __forceinline__ void store_piece(T* p, const float (&v)[kPiece<T>])
 #pragma unroll
     for (int i = 0; i < kPiece<T>; ++i) x[i] = (T)v[i];
     *reinterpret_cast<Piece<T>*>(p) = x;
+}
+
+// A store of what is not read again soon: marked non-temporal (see nt_load4).
+template <typename T>
+__device__ __forceinline__ void stream_piece(T* p, const float (&v)[kPiece<T>])
+{
+    Piece<T> x;
+#pragma unroll
+    for (int i = 0; i < kPiece<T>; ++i) x[i] = (T)v[i];
+    __builtin_nontemporal_store(x, reinterpret_cast<Piece<T>*>(p));
 }
 
 // The same for the first n elements of a piece (any n; zeros beyond), where the rest may be no memory at all.
