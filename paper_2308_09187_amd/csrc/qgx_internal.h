@@ -339,7 +339,7 @@ struct BiasBackPlan {
     int64_t first, count;       // block diagonals with a place that is not masked
     uint64_t scratch;           // bytes: [pairs][blocks][intervals] sums
     uint32_t pairs;             // workers * heads
-    uint32_t bands, blocks;     // runs of block diagonals; workgroups over them
+    uint32_t band, bands, blocks;   // block diagonals of a band; bands; workgroups over them
     uint32_t even;              // workgroups of every band, or 0:
     uint32_t first_block[kMaxBands + 1];   // of a band
 };

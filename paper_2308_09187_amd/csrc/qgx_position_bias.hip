@@ -235,12 +235,10 @@ hipError_t launch_position_bias(int dtype, const BiasArgs& a, const BucketArgs& 
 }
 
 // ---- gradient -------------------------------------------------------------------------------------------------------------
-// Block diagonal D holds the squares of queries s W .. and keys (s + D) W .., s = 0, 1, ..  A band is kBand neighbouring ones, a lane each;
-// at a step the lanes of a band read W queries' runs of kBand W neighbouring keys.  A band's items are its steps in all sequences,
-// dealt in turn to the kBackGroups groups of kBand lanes of each of its workgroups; bands get workgroups by their items, for
-// the corner bands of a square of queries and keys have few.
-constexpr int kBand = 16;
-constexpr int kBackGroups = kBiasThreads / kBand;
+// Block diagonal D holds the squares of queries s W .. and keys (s + D) W .., s = 0, 1, ..  A band is BAND neighbouring ones, a lane each;
+// at a step the lanes of a band read W queries' runs of BAND W neighbouring keys.  A band's items are its steps in all sequences,
+// dealt in turn to the groups of BAND lanes of its workgroups; bands get workgroups by their items, for the corner
+// bands of a square of queries and keys have few.
 
 // The first and the number of the block diagonals that hold a place that is not masked.
 static void visible_diagonals(const BiasArgs& a, const BucketArgs& b, int W, int64_t* first, int64_t* count)
@@ -279,12 +277,14 @@ __device__ __forceinline__ nt_u32x4 load_end(const T* p, int n)
     return nt_u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 
-template <typename T>
+constexpr int kShort = 16;                                 // diagonals of an interval that a lane adds up
+
+template <typename T, int BAND>
 __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a, BucketArgs b, BiasBackPlan plan, float* __restrict__ partial)
 {
-    constexpr int W = kPiece<T>, E = 2 * W - 1, kSpan = kBand * W + W;
-    __shared__ float s_low[kBiasWaves][kBand + 1][W + 1];  // sums of the diagonals below a square's main one, and from it on
-    __shared__ float s_high[kBiasWaves][kBand + 1][W + 1];
+    constexpr int W = kPiece<T>, E = 2 * W - 1, kSpan = BAND * W + W, kGroups = kBiasThreads / BAND;
+    __shared__ float s_low[kBiasWaves][BAND + 1][W + 1];  // sums of the diagonals below a square's main one, and from it on
+    __shared__ float s_high[kBiasWaves][BAND + 1][W + 1];
     __shared__ float s_diag[kSpan];
     __shared__ float s_out[QGX_MAX_INTERVALS];
     const int lane = lane_id(), wave = wave_id();
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a,
         split = blockIdx.x - plan.first_block[band];
         splits = plan.first_block[band + 1u] - plan.first_block[band];
     }
-    const int64_t D0 = plan.first + (int64_t)band * kBand, D1 = min(D0 + kBand, plan.first + plan.count) - 1, D = D0 + lane % kBand;
+    const int64_t D0 = plan.first + (int64_t)band * BAND, D1 = min(D0 + BAND, plan.first + plan.count) - 1, D = D0 + lane % BAND;
     const int q_steps = (int)((a.q + W - 1u) / W), k_steps = (int)((a.k + W - 1u) / W);
     const BandSteps at = band_steps(D0, D1, q_steps, k_steps);
     const uint32_t steps = (uint32_t)(at.s1 - at.s0);
@@ -318,11 +318,11 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a,
 #pragma unroll
         for (int r = 0; r < W; ++r) raw[r] = nt_u32x4{0u, 0u, 0u, 0u};
         // this group's first item: sequence n, step s; and from one item to its next
-        const uint32_t x0 = split * kBackGroups + threadIdx.x / kBand, hop = splits * kBackGroups;
+        const uint32_t x0 = split * kGroups + threadIdx.x / BAND, hop = splits * kGroups;
         uint32_t n = steps ? x0 / steps : a.batch, s = steps ? x0 % steps : 0u;
         const uint32_t hop_n = steps ? hop / steps : 0u, hop_s = steps ? hop % steps : 0u;
         // (the groups of a wave go on as long as any of the workgroup's has an item, and one more turn adds the last)
-        for (uint64_t turn = (uint64_t)split * kBackGroups; turn < items + hop; turn += hop) {
+        for (uint64_t turn = (uint64_t)split * kGroups; turn < items + hop; turn += hop) {
             nt_u32x4 next[W];
 #pragma unroll
             for (int r = 0; r < W; ++r) next[r] = nt_u32x4{0u, 0u, 0u, 0u};
@@ -360,21 +360,24 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a,
         // lane's below it
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            LanePair o = lane_pair<32>(__float_as_uint(sum[e]));
-            sum[e] = __uint_as_float(o.a) + __uint_as_float(o.b);
-            o = lane_pair<16>(__float_as_uint(sum[e]));
-            sum[e] = __uint_as_float(o.a) + __uint_as_float(o.b);
-        }
-        __syncthreads();                                   // the pair before has been dealt with
-        if (lane <= kBand) {
-            const bool is = lane < kBand;
-#pragma unroll
-            for (int e = 0; e < W; ++e) {
-                s_high[wave][lane][e] = is ? sum[e + W - 1] : 0.0f;
-                s_low[wave][lane][e] = is && e < W - 1 ? sum[e] : 0.0f;        // diagonal D W - (W - 1) + e
+            if constexpr (BAND <= 32) {
+                const LanePair o = lane_pair<32>(__float_as_uint(sum[e]));
+                sum[e] = __uint_as_float(o.a) + __uint_as_float(o.b);
+            }
+            if constexpr (BAND <= 16) {
+                const LanePair o = lane_pair<16>(__float_as_uint(sum[e]));
+                sum[e] = __uint_as_float(o.a) + __uint_as_float(o.b);
             }
         }
-        if (threadIdx.x < QGX_MAX_INTERVALS) s_out[threadIdx.x] = 0.0f;
+        __syncthreads();                                   // the pair before has been dealt with
+        if (lane < BAND) {
+#pragma unroll
+            for (int e = 0; e < W; ++e) {
+                s_high[wave][lane][e] = sum[e + W - 1];
+                s_low[wave][lane][e] = e < W - 1 ? sum[e] : 0.0f;          // diagonal D W - (W - 1) + e
+            }
+        }
+        if (lane < W) s_high[wave][BAND][lane] = s_low[wave][BAND][lane] = 0.0f;
         __syncthreads();
         // s_diag[x]: diagonal D0 W - W + x
         for (int y = (int)threadIdx.x; y < kSpan; y += kBiasThreads) {
@@ -389,31 +392,47 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a,
         }
         __syncthreads();
         const int first = (int)(D0 * W - W - a.q_offset);  // delta of s_diag[0]
-        interval.meeting(first, first + kSpan, [&](int i, int, int x0, int x1) {
-            if (i % kBiasWaves != wave) return;
-            float z = 0.0f;
-            for (int y = x0 + lane; y < x1; y += kWave) z += s_diag[y - first];
-            z = lanes_sum<kWave>(z);
-            if (lane == 0) s_out[i] = z;
-        });
+        // Short intervals, most near the diagonal, by a lane each (the first 64 in wave 0, the others in wave 1); the long ones by a
+        // wave each in turn.  (All of them by waves, one after the other, take 0.1 us each.)
+        int turn = 0;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int bound = half ? interval.bound1 : interval.bound0, stop = half ? interval.end1 : interval.end0;
+            const int y0 = max(bound, first) - first, n = (half ? interval.is1 : interval.is0) ? min(stop, first + kSpan) - first - y0 : 0;
+            if (wave == half && n <= kShort) {
+                float z = 0.0f;
+#pragma unroll
+                for (int y = 0; y < kShort; ++y)
+                    if (y < n) z += s_diag[y0 + y];
+                s_out[half * kWave + lane] = z;
+            }
+            for (uint64_t which = __ballot(n > kShort); which; which &= which - 1u, ++turn) {
+                if (turn % kBiasWaves != wave) continue;
+                const int j = __ffsll((unsigned long long)which) - 1, from = __builtin_amdgcn_readlane(y0, j), to = from + __builtin_amdgcn_readlane(n, j);
+                float z = 0.0f;
+                for (int y = from + lane; y < to; y += kWave) z += s_diag[y];
+                z = lanes_sum<kWave>(z);
+                if (lane == 0) s_out[half * kWave + j] = z;
+            }
+        }
         __syncthreads();
         if (threadIdx.x < b.n) partial[((size_t)kh * gridDim.x + blockIdx.x) * b.n + threadIdx.x] = s_out[threadIdx.x];
     }
 }
 
 // The workgroups' sums of a worker's and a head's table row joined, in binary64, a wave for each.
-__global__ __launch_bounds__(kBiasThreads) void k_position_bias_join(BucketArgs b, BiasBackPlan plan, uint32_t heads, uint32_t table_rows,
+__global__ __launch_bounds__(kBiasThreads) void k_position_bias_join(BucketArgs b, uint32_t heads, uint32_t table_rows,
                                                                      uint32_t parts, const float* __restrict__ partial, float* dtable,
                                                                      uint64_t param_stride)
 {
-    const uint64_t each = (uint64_t)table_rows * heads, all = plan.pairs / heads * each;
     const Intervals interval(b);
-    for (uint64_t x = (uint64_t)blockIdx.x * kBiasWaves + wave_id(); x < all; x += (uint64_t)gridDim.x * kBiasWaves) {
-        const uint32_t worker = (uint32_t)(x / each), r = (uint32_t)(x % each / heads), head = (uint32_t)(x % heads);
+    const uint32_t worker = blockIdx.y, outputs = table_rows * heads;
+    for (uint32_t x = blockIdx.x * kBiasWaves + (uint32_t)__builtin_amdgcn_readfirstlane(wave_id()); x < outputs; x += gridDim.x * kBiasWaves) {
+        const uint32_t r = x / heads, head = x - r * heads;
         const float* p = partial + ((size_t)worker * heads + head) * parts * b.n;
         double sum = 0.0;
         for (int half = 0; half < 2; ++half)
-            for (uint64_t which = __ballot((uint32_t)(lane_id() + half * kWave) < b.n && (half ? interval.row1 : interval.row0) == r); which; which &= which - 1u) {
+            for (uint64_t which = __ballot(half ? interval.is1 && interval.row1 == r : interval.is0 && interval.row0 == r); which; which &= which - 1u) {
                 const uint32_t i = (uint32_t)(half * kWave + __ffsll((unsigned long long)which) - 1);
                 for (uint32_t u = (uint32_t)lane_id(); u < parts; u += kWave) sum += (double)p[(size_t)u * b.n + i];
             }
@@ -422,29 +441,35 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias_join(BucketArgs 
     }
 }
 
+// The lanes of a band.
+static uint32_t back_band(uint32_t k, int W) { return (k + W - 1u) / W >= 64u ? 64u : 16u; }
+
 BiasBackPlan bias_back_plan(int dtype, const BiasArgs& a, const BucketArgs& b, uint32_t workers, uint32_t n_cu)
 {
     const int W = dtype == QGX_F32 ? 4 : 8;
     BiasBackPlan p{};
     p.pairs = workers * a.heads;
     if (a.batch && a.q && a.k) visible_diagonals(a, b, W, &p.first, &p.count);
-    p.bands = (uint32_t)((p.count + kBand - 1) / kBand);
+    p.band = back_band(a.k, W);
+    const int64_t band = p.band;
+    const uint32_t groups = kBiasThreads / p.band;
+    p.bands = (uint32_t)((p.count + band - 1) / band);
     if (!p.bands) return p;
     const int q_steps = (int)((a.q + W - 1u) / W), k_steps = (int)((a.k + W - 1u) / W);
-    // eight workgroups for every compute unit over pairs and bands, of at least one item to a group of lanes
+    // eight workgroups for every compute unit over pairs and bands, of at least two items to a group of lanes
     const uint64_t want = max((uint64_t)1u, (8u * (uint64_t)n_cu + p.pairs - 1u) / p.pairs);      // of a pair
     if (p.bands > kMaxBands) {
-        const uint64_t most = ((uint64_t)q_steps * a.batch + kBackGroups - 1u) / kBackGroups;
+        const uint64_t most = ((uint64_t)q_steps * a.batch + groups - 1u) / groups;
         p.even = (uint32_t)min((want + p.bands - 1u) / p.bands, most);
         p.blocks = p.bands * p.even;
     } else {
         uint64_t items[kMaxBands], all = 0;
         for (uint32_t i = 0; i < p.bands; ++i) {
-            const int64_t D0 = p.first + (int64_t)i * kBand, D1 = min(D0 + kBand, p.first + p.count) - 1;
+            const int64_t D0 = p.first + (int64_t)i * band, D1 = min(D0 + band, p.first + p.count) - 1;
             const BandSteps s = band_steps(D0, D1, q_steps, k_steps);
             all += items[i] = (uint64_t)(s.s1 - s.s0) * a.batch;
         }
-        const uint64_t each = max((uint64_t)kBackGroups, (all + want - 1u) / want);       // items of a workgroup
+        const uint64_t each = max((uint64_t)groups * 2u, (all + want - 1u) / want);  // items of a workgroup
         for (uint32_t i = 0; i < p.bands; ++i) {
             p.first_block[i] = p.blocks;
             p.blocks += (uint32_t)max((uint64_t)1u, (items[i] + each - 1u) / each);
@@ -458,7 +483,9 @@ BiasBackPlan bias_back_plan(int dtype, const BiasArgs& a, const BucketArgs& b, u
 template <typename T>
 static hipError_t launch_bias_back_of(const BiasArgs& a, const BucketArgs& b, const BiasBackPlan& p, float* partial, hipStream_t st)
 {
-    hipLaunchKernelGGL(k_position_bias_back<T>, dim3(p.blocks, min(p.pairs, 65535u)), dim3(kBiasThreads), 0, st, a, b, p, partial);
+    const dim3 grid(p.blocks, min(p.pairs, 65535u));
+    if (p.band == 64u) hipLaunchKernelGGL((k_position_bias_back<T, 64>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
+    else hipLaunchKernelGGL((k_position_bias_back<T, 16>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
     return hipGetLastError();
 }
 
@@ -472,9 +499,9 @@ hipError_t launch_position_bias_back(int dtype, const BiasArgs& a, const BucketA
                                                 : launch_bias_back_of<__bf16>(a, b, p, partial, st);
         if (e != hipSuccess) return e;
     }
-    const uint64_t outputs = (uint64_t)(p.pairs / a.heads) * table_rows * a.heads;
-    hipLaunchKernelGGL(k_position_bias_join, dim3((uint32_t)min((outputs + kBiasWaves - 1u) / kBiasWaves, (uint64_t)1u << 20)), dim3(kBiasThreads), 0, st,
-                       b, p, a.heads, table_rows, p.blocks, partial, dtable, param_stride);
+    const uint32_t outputs = table_rows * a.heads;         // (below 2^24)
+    hipLaunchKernelGGL(k_position_bias_join, dim3((outputs + kBiasWaves - 1u) / kBiasWaves, p.pairs / a.heads), dim3(kBiasThreads), 0, st, b, a.heads,
+                       table_rows, p.blocks, partial, dtable, param_stride);
     return hipGetLastError();
 }
 
