@@ -308,10 +308,11 @@ struct NormBackArgs {
     uint64_t dy_worker, dy_row, x_worker, x_row, dx_worker, dx_row, param_stride;
     uint32_t rows, n_rows, cols;
     float* scratch;             // [workers][parts][2][sum_stride]: the workgroups' sums, of dw and of db
-    uint32_t parts, sum_stride; // filled in by the launch
+    uint32_t parts, sum_stride, apart; // filled in by the launch
 };
 struct NormBackPlan {
     uint32_t parts, sum_stride; // workgroups that share a worker's rows; floats of a row of sums
+    uint32_t apart;             // the columns' sums are workgroups of their own
     uint64_t scratch;           // bytes
 };
 hipError_t launch_layer_norm(int dtype, const NormArgs& a, uint32_t n_cu, hipStream_t st);

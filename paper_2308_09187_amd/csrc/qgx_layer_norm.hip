@@ -6,6 +6,8 @@
 
 namespace qgx {
 
+// Shapes with a form for small tensors; larger ones have columns enough for their sums' launch.
+template <int LANES> constexpr bool kSmall = LANES <= 256;
 template <int LANES> constexpr int kNormThreads = LANES > 256 ? LANES : 256;
 template <int LANES> constexpr int kNormGroups = kNormThreads<LANES> / LANES;     // groups of LANES threads in a workgroup
 // A thread's group: the same in all lanes of a wave, and known to be, where a group has whole waves.
@@ -209,12 +211,57 @@ __device__ __forceinline__ NormSums norm_sums(const NormBackArgs& a, uint32_t k,
     return NormSums{a.dw ? s : nullptr, a.db ? s + a.sum_stride : nullptr};
 }
 
+// Small tensors: the sums of sixteen pieces' columns by a workgroup of their own, from dy and x once more (from the cache): no scratch and
+// no second launch, which would take longer.  The rows are dealt to THREADS / 16 threads for each piece.
+template <typename T, int THREADS>
+__device__ __forceinline__ void columns_apart(const NormBackArgs& a, uint32_t k, uint32_t block, float (*s_part)[16 * kPiece<T>])
+{
+    constexpr int W = kPiece<T>, kRuns = THREADS / 16;
+    const int quad = (int)threadIdx.x % 16, run = (int)threadIdx.x / 16, cols = (int)a.cols;
+    const PieceAt at = piece_at<W, 16>(quad, (int)block, cols);
+    float dw[W], db[W];
+#pragma unroll
+    for (int c = 0; c < W; ++c) dw[c] = db[c] = 0.0f;
+#pragma unroll 4
+    for (uint32_t r = (uint32_t)run; r < a.rows; r += kRuns) {
+        float u[W], v[W];
+        load_piece((const T*)a.x + k * a.x_worker + r * a.x_row + at.c, u);
+        load_piece((const T*)a.dy + k * a.dy_worker + r * a.dy_row + at.c, v);
+        const float mean = a.mean[(size_t)k * a.rows + r], rstd = a.rstd[(size_t)k * a.rows + r];
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+            dw[c] = fmaf(v[c], (u[c] - mean) * rstd, dw[c]);
+            db[c] += v[c];
+        }
+    }
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float* to = which ? a.db : a.dw;
+        if (which) __syncthreads();
+#pragma unroll
+        for (int c = 0; c < W; ++c) s_part[run][quad * W + c] = which ? db[c] : dw[c];
+        __syncthreads();
+        if (!to || run != 0 || !at.any) continue;
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+            float x = s_part[0][quad * W + c];
+#pragma unroll
+            for (int i = 1; i < kRuns; ++i) x += s_part[i][quad * W + c];
+            if (at.owns(c)) to[k * a.param_stride + at.c + c] = x;
+        }
+    }
+}
+
 template <typename T, int LANES, int N, int R>
 __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBackArgs a)
 {
     constexpr int W = kPiece<T>, kGroups = kNormGroups<LANES>;
     __shared__ float s_sum[2][2 * R][kNormSlots];
     __shared__ float s_cols[kGroups > 1 ? kGroups : 1][kGroups > 1 ? LANES * N * W : 1];
+    if constexpr (kSmall<LANES>) {
+        __shared__ float s_part[kNormThreads<LANES> / 16][16 * W];
+        if (a.apart && blockIdx.x >= a.parts) return columns_apart<T, kNormThreads<LANES>>(a, blockIdx.y, blockIdx.x - a.parts, s_part);
+    }
     const int lane = (int)(threadIdx.x % LANES), cols = (int)a.cols;
     const uint32_t group = norm_group<LANES>();
     const uint32_t k = blockIdx.y;
@@ -251,10 +298,12 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
             if (!ok) next_mean[q] = next_rstd[q] = 0.0f;
         }
     };
-    if (blockIdx.x < sets) load(blockIdx.x);
+    constexpr bool kAhead = N < 8;                         // (there the registers are taken: the ones of f32 rows of more than 8192 columns)
+    if (kAhead && blockIdx.x < sets) load(blockIdx.x);
     int turn = 0;
     for (uint32_t set = blockIdx.x; set < sets; set += a.parts, turn ^= 1) {
         const uint32_t first = (set * kGroups + group) * R;
+        if (!kAhead) load(set);
 #pragma unroll
         for (int q = 0; q < R; ++q) {
 #pragma unroll
@@ -265,7 +314,7 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
             mean[q] = next_mean[q];
             rstd[q] = next_rstd[q];
         }
-        if (set + a.parts < sets) load(set + a.parts);     // (the same for the whole workgroup)
+        if (kAhead && set + a.parts < sets) load(set + a.parts);     // (the same for the whole workgroup)
 #pragma unroll
         for (int q = 0; q < R; ++q) {
             sum[q] = sum[R + q] = 0.0f;
@@ -310,6 +359,7 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
             }
         }
     }
+    if (kSmall<LANES> && a.apart) return;
     const NormSums out = norm_sums(a, k, blockIdx.x);
     if constexpr (kGroups == 1) {
 #pragma unroll
@@ -521,14 +571,18 @@ NormBackPlan norm_back_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t
     const uint32_t each = shape.pieces >= 4u ? 2u : shape.lanes ? 3u : 4u;
     const uint32_t want = max(1u, each * n_cu / (workers * (shape.lanes ? 1u : (pieces + 255u) / 256u)));
     p.parts = max(1u, min(sets, want));
-    p.scratch = p.parts == 1u ? 0 : (uint64_t)workers * p.parts * 2u * p.sum_stride * sizeof(float);
+    // Few rows and little in all: a workgroup for every set, the columns' sums apart.
+    p.apart = p.parts > 1u && shape.lanes && shape.lanes <= 256u && rows <= 256u && (uint64_t)workers * rows * cols <= (1u << 20);
+    if (p.apart) p.parts = sets;
+    p.scratch = p.parts == 1u || p.apart ? 0 : (uint64_t)workers * p.parts * 2u * p.sum_stride * sizeof(float);
     return p;
 }
 
 template <typename T, int LANES, int N, int R>
 static hipError_t launch_back_as(const NormBackArgs& a, uint32_t workers, hipStream_t st)
 {
-    hipLaunchKernelGGL((k_layer_norm_back<T, LANES, N, R>), dim3(a.parts, workers), dim3(kNormThreads<LANES>), 0, st, a);
+    const uint32_t apart = a.apart ? (a.cols + 16u * kPiece<T> - 1u) / (16u * kPiece<T>) : 0u;
+    hipLaunchKernelGGL((k_layer_norm_back<T, LANES, N, R>), dim3(a.parts + apart, workers), dim3(kNormThreads<LANES>), 0, st, a);
     return hipGetLastError();
 }
 
@@ -564,11 +618,12 @@ hipError_t launch_layer_norm_back(int dtype, const NormBackArgs& args, uint32_t 
     NormBackArgs a = args;
     a.parts = plan.parts;
     a.sum_stride = plan.sum_stride;
+    a.apart = plan.apart && (a.dw || a.db);
     if (!a.dx && !a.dw && !a.db) return hipSuccess;
     const hipError_t e = dtype == QGX_F32   ? launch_back_of<float>(a, workers, st)
                          : dtype == QGX_F16 ? launch_back_of<_Float16>(a, workers, st)
                                             : launch_back_of<__bf16>(a, workers, st);
-    if (e != hipSuccess || a.parts == 1u || (!a.dw && !a.db)) return e;
+    if (e != hipSuccess || a.parts == 1u || a.apart || (!a.dw && !a.db)) return e;
     hipLaunchKernelGGL(k_layer_norm_join, dim3((a.cols + 63u) / 64u, 2u * workers), dim3(256), 0, st, a);
     return hipGetLastError();
 }

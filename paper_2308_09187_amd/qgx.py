@@ -122,9 +122,9 @@ def _need(ok, text, *what):
         raise QgxError(ERR_ARG, text % what if what else text)
 
 
-def _handle(stream):
-    """The stream's handle as a number, for the functions whose argument types are given."""
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
+def _handle(stream, t):
+    """The stream's handle as a number, for the functions whose argument types are given; None: the current one of t's device."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def _empty(like, shape, dtype, stream):
@@ -146,6 +146,14 @@ def _parameter(t, shape, name):
 
 def _dense_last(t):
     return t.dim() == 0 or t.shape[-1] <= 1 or t.stride(-1) == 1
+
+
+def _empty_like(t, stream):
+    """The same of t's shape and type, contiguous (1.3 us)."""
+    if stream is None:
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 class Buckets:
@@ -363,7 +371,7 @@ class Context:
                   "clip_gradients: out is V [K, d], contiguous float32 on the GPU")
         norms = _empty(tensors.table, (self.K,), torch.float32, stream)
         st = self.lib.qgx_clip_gradients(self._h, tensors._ref, norm, max_norm, None if out is None else out.data_ptr(),
-                                         norms.data_ptr(), _handle(stream))
+                                         norms.data_ptr(), _handle(stream, norms))
         if st:
             self._check(st)
         return norms
@@ -392,14 +400,14 @@ class Context:
         code, wk, rows, cols, xw, xr = self._rows(x, "x")
         w, b = _parameter(weight, (cols,), "weight"), _parameter(bias, (cols,), "bias")
         if out is None:
-            out, yw, yr = _empty(x, x.shape, x.dtype, stream), rows * cols, cols
+            out, yw, yr = _empty_like(x, stream), rows * cols, cols
         else:
             yw, yr = self._rows_like(out, x, "out")
         mean = rstd = None
         if save:
             mean, rstd = _empty(x, (2,) + x.shape[:-1], torch.float32, stream).unbind(0)
         st = self.lib.qgx_layer_norm(self._h, code, wk, rows, cols, x.data_ptr(), xw, xr, w, b, eps, out.data_ptr(), yw, yr,
-                                     mean.data_ptr() if save else None, rstd.data_ptr() if save else None, _handle(stream))
+                                     mean.data_ptr() if save else None, rstd.data_ptr() if save else None, _handle(stream, x))
         if st:
             self._check(st)
         return out, mean, rstd
@@ -425,7 +433,7 @@ class Context:
         if dx is not None:
             ow, orow = self._rows_like(dx, x, "dx")
         elif need_dx:
-            dx, ow, orow = _empty(x, x.shape, x.dtype, stream), rows * cols, cols
+            dx, ow, orow = _empty_like(x, stream), rows * cols, cols
         need, scratch = self._need_bytes, None
         st = self.lib.qgx_layer_norm_scratch(self._h, code, wk, rows, cols, self._need_ref)
         if not st:
@@ -434,7 +442,7 @@ class Context:
             st = self.lib.qgx_layer_norm_backward(
                 self._h, code, wk, rows, cols, dy.data_ptr(), gw, gr, x.data_ptr(), xw, xr, w, m, r,
                 None if dx is None else dx.data_ptr(), ow, orow, None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
-                cols if step is None else step, None if scratch is None else scratch.data_ptr(), need.value, _handle(stream))
+                cols if step is None else step, None if scratch is None else scratch.data_ptr(), need.value, _handle(stream, x))
         if st:
             self._check(st)
         return dx
@@ -460,7 +468,7 @@ class Context:
             pos = positions.data_ptr()
         i = None if src is None else self._scores(src, "scores")
         st = self.lib.qgx_position_bias(self._h, buckets._ref, tab, table.shape[0], None if i is None else C.addressof(i),
-                                        C.addressof(o), q_offset, pos, _handle(stream))
+                                        C.addressof(o), q_offset, pos, _handle(stream, out))
         if st:
             self._check(st)
         return out
@@ -475,7 +483,7 @@ class Context:
         """scores [.., batch, heads, q, k] plus the bias, -inf where a place is masked.  positions int32 [.., batch]: added to
         q_offset sequence by sequence (the position of its first query).  out may be scores."""
         if out is None:
-            out = _empty(scores, scores.shape, scores.dtype, stream)
+            out = _empty_like(scores, stream)
         return self._bias(table, buckets, scores, out, q_offset, positions, stream)
 
     def position_bias_backward(self, grad, buckets: Buckets, dtable, q_offset=0, stream=None):
@@ -494,7 +502,7 @@ class Context:
                 scratch = _empty(grad, (need.value,), torch.uint8, stream)
             st = self.lib.qgx_position_bias_backward(self._h, buckets._ref, C.addressof(g), q_offset, dtable.data_ptr(), rows,
                                                      step[0] if len(sh) == 3 and g.workers > 1 else rows * g.heads,
-                                                     None if scratch is None else scratch.data_ptr(), need.value, _handle(stream))
+                                                     None if scratch is None else scratch.data_ptr(), need.value, _handle(stream, grad))
         if st:
             self._check(st)
         return dtable
