@@ -502,15 +502,17 @@ static hipError_t launch_norm_as(const NormArgs& a, hipStream_t st)
     return hipGetLastError();
 }
 
-template <typename T, int LANES, int N, int R>
+// Two rows at a time once that leaves eight workgroups for every compute unit (8 x 4096 x 4096 bfloat16: 83 us with four rows, 88 with
+// one, 81 with two).
+template <typename T, int LANES, int N>
 static hipError_t launch_norm_by_rows(const NormArgs& a, uint32_t n_cu, hipStream_t st)
 {
-    // R rows at a time once that leaves eight workgroups for every compute unit
-    if (a.n_rows / ((uint32_t)kNormGroups<LANES> * R) >= 8u * n_cu) return launch_norm_as<T, LANES, N, R>(a, st);
+    if (a.n_rows / ((uint32_t)kNormGroups<LANES> * 2u) >= 8u * n_cu) return launch_norm_as<T, LANES, N, 2>(a, st);
     return launch_norm_as<T, LANES, N, 1>(a, st);
 }
 
-// The fewest threads that hold a row in four pieces each.
+// The fewest threads that hold a row in a piece or two each; four where a workgroup of 256 has to (four for 64 of bfloat16 took
+// 32 us for 8 x 65536 rows in four threads each, two 24).
 template <typename T>
 static hipError_t launch_norm_of(const NormArgs& a, uint32_t n_cu, hipStream_t st)
 {
@@ -519,15 +521,16 @@ static hipError_t launch_norm_of(const NormArgs& a, uint32_t n_cu, hipStream_t s
         hipLaunchKernelGGL((k_layer_norm_long<T, 64>), dim3(min(a.n_rows, kNormBlocksMax)), dim3(64), 0, st, a);
         return hipGetLastError();
     }
-    if (pieces <= 4u) return launch_norm_by_rows<T, 4, 1, 4>(a, n_cu, st);
-    if (pieces <= 16u) return launch_norm_by_rows<T, 4, 4, 2>(a, n_cu, st);
-    if (pieces <= 32u) return launch_norm_by_rows<T, 16, 2, 4>(a, n_cu, st);
-    if (pieces <= 64u) return launch_norm_by_rows<T, 16, 4, 2>(a, n_cu, st);
-    if (pieces <= 128u) return launch_norm_by_rows<T, 64, 2, 4>(a, n_cu, st);
-    if (pieces <= 256u) return launch_norm_by_rows<T, 64, 4, 2>(a, n_cu, st);
-    if (pieces <= 512u) return launch_norm_by_rows<T, 256, 2, 4>(a, n_cu, st);
-    if (pieces <= 1024u) return launch_norm_by_rows<T, 256, 4, 2>(a, n_cu, st);
-    if (pieces <= 2048u) return launch_norm_as<T, 1024, 2, 1>(a, st);
+    if (pieces <= 4u) return launch_norm_by_rows<T, 4, 1>(a, n_cu, st);
+    if (pieces <= 8u) return launch_norm_by_rows<T, 4, 2>(a, n_cu, st);
+    if (pieces <= 16u) return launch_norm_by_rows<T, 16, 1>(a, n_cu, st);
+    if (pieces <= 32u) return launch_norm_by_rows<T, 16, 2>(a, n_cu, st);
+    if (pieces <= 64u) return launch_norm_by_rows<T, 64, 1>(a, n_cu, st);
+    if (pieces <= 128u) return launch_norm_by_rows<T, 64, 2>(a, n_cu, st);
+    if (pieces <= 256u) return launch_norm_by_rows<T, 256, 1>(a, n_cu, st);
+    if (pieces <= 512u) return launch_norm_by_rows<T, 256, 2>(a, n_cu, st);
+    if (pieces <= 1024u) return launch_norm_as<T, 256, 4, 1>(a, st);
+    if (pieces <= 2048u) return launch_norm_as<T, 512, 4, 1>(a, st);
     if (pieces <= 4096u) return launch_norm_as<T, 1024, 4, 1>(a, st);
     hipLaunchKernelGGL((k_layer_norm_long<T, 1024>), dim3(min(a.n_rows, kNormBlocksMax)), dim3(1024), 0, st, a);
     return hipGetLastError();
