@@ -265,6 +265,7 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
     const int lane = (int)(threadIdx.x % LANES), cols = (int)a.cols;
     const uint32_t group = norm_group<LANES>();
     const uint32_t k = blockIdx.y;
+    constexpr bool kAhead = N < 8;                         // (no registers are left for the next rows of binary32 of more than 8192 columns)
     float w[N][W], dw[N][W], db[N][W];
     PieceAt at[N];
 #pragma unroll
@@ -298,7 +299,6 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
             if (!ok) next_mean[q] = next_rstd[q] = 0.0f;
         }
     };
-    constexpr bool kAhead = N < 8;                         // (there the registers are taken: the ones of f32 rows of more than 8192 columns)
     if (kAhead && blockIdx.x < sets) load(blockIdx.x);
     int turn = 0;
     for (uint32_t set = blockIdx.x; set < sets; set += a.parts, turn ^= 1) {
@@ -315,6 +315,7 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
             rstd[q] = next_rstd[q];
         }
         if (kAhead && set + a.parts < sets) load(set + a.parts);     // (the same for the whole workgroup)
+        // With t = x - mean: sums of g and g t, dw += dy t rstd, db += dy
 #pragma unroll
         for (int q = 0; q < R; ++q) {
             sum[q] = sum[R + q] = 0.0f;
@@ -325,11 +326,10 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
                 values_of<T>(dy[q][j], v);
 #pragma unroll
                 for (int c = 0; c < W; ++c) {
-                    const float d = v[c], g = at[j].owns(c) ? d * w[j][c] : 0.0f;
-                    const float h = (u[c] - mean[q]) * rstd[q];
+                    const float d = v[c], t = u[c] - mean[q], g = at[j].owns(c) ? d * w[j][c] : 0.0f;
                     sum[q] += g;
-                    sum[R + q] = fmaf(g, h, sum[R + q]);
-                    dw[j][c] = fmaf(d, h, dw[j][c]);
+                    sum[R + q] = fmaf(g, t, sum[R + q]);
+                    dw[j][c] = fmaf(d, t * rstd[q], dw[j][c]);
                     db[j][c] += d;
                 }
                 // (added here and now: left to the end of the round, the terms would be kept across the sums)
@@ -337,25 +337,22 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
                 for (int c = 0; c < W; ++c) asm volatile("" : "+v"(dw[j][c]), "+v"(db[j][c]));
             }
         }
-        if (a.dx) {
-            row_sums<LANES>(sum, s_sum[turn]);             // (two sets of slots in turn: one barrier a round)
+        if (!a.dx) continue;
+        row_sums<LANES>(sum, s_sum[turn]);                 // (two sets of slots in turn: one barrier a round)
+        // dx = rstd (g - mean g - h mean(g h)) = dy (rstd w) - (t rstd^2 mean(g h) + rstd mean g)
 #pragma unroll
-            for (int q = 0; q < R; ++q) {
-                const float m1 = sum[q] / (float)cols, m2 = sum[R + q] / (float)cols;
+        for (int q = 0; q < R; ++q) {
+            const float minus_m1 = -rstd[q] * (sum[q] / (float)cols), minus_m2 = -rstd[q] * rstd[q] * (rstd[q] * (sum[R + q] / (float)cols));
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    // (worked out again from what was loaded: kept across the sums, g and h would take four times the registers)
-                    asm volatile("" : "+v"(x[q][j]), "+v"(dy[q][j]));
-                    float u[W], v[W];
-                    values_of<T>(x[q][j], u);
-                    values_of<T>(dy[q][j], v);
+            for (int j = 0; j < N; ++j) {
+                // (worked out again from what was loaded: kept across the sums, the values would take twice its registers)
+                asm volatile("" : "+v"(x[q][j]), "+v"(dy[q][j]));
+                float u[W], out[W];
+                values_of<T>(x[q][j], u);
+                values_of<T>(dy[q][j], out);
 #pragma unroll
-                    for (int c = 0; c < W; ++c) {
-                        const float g = v[c] * w[j][c], h = (u[c] - mean[q]) * rstd[q];
-                        v[c] = rstd[q] * (g - m1 - h * m2);
-                    }
-                    if (at[j].any && first + q < a.rows) stream_piece((T*)a.dx + k * a.dx_worker + (first + q) * a.dx_row + at[j].c, v);
-                }
+                for (int c = 0; c < W; ++c) out[c] = fmaf(out[c], rstd[q] * w[j][c], fmaf(u[c] - mean[q], minus_m2, minus_m1));
+                if (at[j].any && first + q < a.rows) stream_piece((T*)a.dx + k * a.dx_worker + (first + q) * a.dx_row + at[j].c, out);
             }
         }
     }
@@ -465,26 +462,38 @@ __global__ __launch_bounds__(256) void k_layer_norm_columns(NormBackArgs a)
     }
 }
 
-// The workgroups' sums of 64 columns joined: sixteen runs of the parts side by side, then those in order.
+// x over the sixteen lanes that differ in all but the lowest two bits.
+__device__ __forceinline__ float join_runs(float x)
+{
+    LanePair p = lane_pair<32>(__float_as_uint(x));
+    p = lane_pair<16>(__float_as_uint(__uint_as_float(p.a) + __uint_as_float(p.b)));
+    p = lane_pair<8>(__float_as_uint(__uint_as_float(p.a) + __uint_as_float(p.b)));
+    p = lane_pair<4>(__float_as_uint(__uint_as_float(p.a) + __uint_as_float(p.b)));
+    return __uint_as_float(p.a) + __uint_as_float(p.b);
+}
+
+// The workgroups' sums of sixteen columns joined: four to a thread, 64 runs of the parts side by side.
 __global__ __launch_bounds__(256) void k_layer_norm_join(NormBackArgs a)
 {
-    __shared__ float4 s_run[16][16];
-    const uint32_t k = blockIdx.y / 2u, which = blockIdx.y % 2u, quad = threadIdx.x % 16u, run = threadIdx.x / 16u;
+    __shared__ float4 s_run[4][4];
+    const uint32_t k = blockIdx.y / 2u, which = blockIdx.y % 2u, quad = threadIdx.x % 4u, run = threadIdx.x / 4u;
     float* out = which ? a.db : a.dw;
     if (!out) return;
-    const uint32_t c0 = (blockIdx.x * 16u + quad) * 4u;
+    const uint32_t c0 = (blockIdx.x * 4u + quad) * 4u;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c0 < a.cols) {                                     // (a row of sums is whole fours of columns)
         const float* p = a.scratch + ((size_t)k * a.parts * 2u + which) * a.sum_stride + c0;
-        for (uint32_t i = run; i < a.parts; i += 16u) {
+#pragma unroll 4
+        for (uint32_t i = run; i < a.parts; i += 64u) {
             const float4 x = *reinterpret_cast<const float4*>(p + (size_t)i * 2u * a.sum_stride);
             sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
         }
     }
-    s_run[run][quad] = sum;
+    sum = make_float4(join_runs(sum.x), join_runs(sum.y), join_runs(sum.z), join_runs(sum.w));
+    if (lane_id() < 4) s_run[wave_id()][quad] = sum;
     __syncthreads();
     if (run != 0 || c0 >= a.cols) return;
-    for (int i = 1; i < 16; ++i) {
+    for (int i = 1; i < 4; ++i) {
         const float4 x = s_run[i][quad];
         sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
     }
@@ -627,7 +636,7 @@ hipError_t launch_layer_norm_back(int dtype, const NormBackArgs& args, uint32_t 
                          : dtype == QGX_F16 ? launch_back_of<_Float16>(a, workers, st)
                                             : launch_back_of<__bf16>(a, workers, st);
     if (e != hipSuccess || a.parts == 1u || a.apart || (!a.dw && !a.db)) return e;
-    hipLaunchKernelGGL(k_layer_norm_join, dim3((a.cols + 63u) / 64u, 2u * workers), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_layer_norm_join, dim3((a.cols + 15u) / 16u, 2u * workers), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
