@@ -360,6 +360,8 @@ typedef struct {
     void* table;          /* DEVICE, 16-byte aligned */
     uint64_t table_bytes;
     uint64_t n_pieces;    /* runs the tensors are cut into, per worker */
+    uint64_t d;           /* of the context it was made for, as K: it serves no other shape */
+    uint32_t K;
     uint32_t n_tensors;
     uint32_t shared_rows; /* workers share elements of a tensor (stride < n): not to be written */
 } qgx_tensor_list;
@@ -377,7 +379,7 @@ qgx_status qgx_tensor_list_set(qgx_ctx* ctx, const qgx_tensor* tensors /* HOST *
  * not, or where N_k is no finite number (then QGX_EBIT_NONFINITE is set as well, as CODE o Q would).
  *   V      DEVICE [K][d]: tensors are gathered into it as binary32 (coordinates that belong to no tensor stay as they
  *          are); it may be the memory of a tensor of the list that lies there as it does in V, and overlaps no other.
- *          NULL: the tensors are clipped in place, rounded to their own types.
+ *          NULL: the tensors are clipped in place, rounded to their own types; they may not overlap each other then.
  *   norms  DEVICE [K] binary32 or NULL: the N_k
  * max_norm >= 0; infinity only measures (and gathers). */
 qgx_status qgx_clip_gradients(qgx_ctx* ctx, const qgx_tensor_list* list, int norm, float max_norm, float* V,

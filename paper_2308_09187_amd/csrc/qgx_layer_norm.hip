@@ -520,8 +520,9 @@ static hipError_t launch_norm_by_rows(const NormArgs& a, uint32_t n_cu, hipStrea
     return launch_norm_as<T, LANES, N, 1>(a, st);
 }
 
-// The fewest threads that hold a row in a piece or two each; four where a workgroup of 256 has to (four for 64 of bfloat16 took
-// 32 us for 8 x 65536 rows in four threads each, two 24).
+// The fewest threads that hold a row in a piece or two each, where steps are wide in three (8 x 8192 x 1100 bfloat16: 62 us in three pieces of 64
+// threads, 84 in one of 256 of which half are idle), and in up to four of a workgroup's 256 or more (four pieces to each of four
+// threads took 32 us for 8 x 65536 x 64, two 24).
 template <typename T>
 static hipError_t launch_norm_of(const NormArgs& a, uint32_t n_cu, hipStream_t st)
 {
@@ -536,9 +537,12 @@ static hipError_t launch_norm_of(const NormArgs& a, uint32_t n_cu, hipStream_t s
     if (pieces <= 32u) return launch_norm_by_rows<T, 16, 2>(a, n_cu, st);
     if (pieces <= 64u) return launch_norm_by_rows<T, 64, 1>(a, n_cu, st);
     if (pieces <= 128u) return launch_norm_by_rows<T, 64, 2>(a, n_cu, st);
+    if (pieces <= 192u) return launch_norm_by_rows<T, 64, 3>(a, n_cu, st);
     if (pieces <= 256u) return launch_norm_by_rows<T, 256, 1>(a, n_cu, st);
     if (pieces <= 512u) return launch_norm_by_rows<T, 256, 2>(a, n_cu, st);
+    if (pieces <= 768u) return launch_norm_as<T, 256, 3, 1>(a, st);
     if (pieces <= 1024u) return launch_norm_as<T, 256, 4, 1>(a, st);
+    if (pieces <= 1536u) return launch_norm_as<T, 512, 3, 1>(a, st);
     if (pieces <= 2048u) return launch_norm_as<T, 512, 4, 1>(a, st);
     if (pieces <= 4096u) return launch_norm_as<T, 1024, 4, 1>(a, st);
     hipLaunchKernelGGL((k_layer_norm_long<T, 1024>), dim3(min(a.n_rows, kNormBlocksMax)), dim3(1024), 0, st, a);
@@ -631,6 +635,7 @@ hipError_t launch_layer_norm_back(int dtype, const NormBackArgs& args, uint32_t 
     a.parts = plan.parts;
     a.sum_stride = plan.sum_stride;
     a.apart = plan.apart && (a.dw || a.db);
+    if (a.apart && !a.dx) a.parts = 0u;                    // no rows' workgroups
     if (!a.dx && !a.dw && !a.db) return hipSuccess;
     const hipError_t e = dtype == QGX_F32   ? launch_back_of<float>(a, workers, st)
                          : dtype == QGX_F16 ? launch_back_of<_Float16>(a, workers, st)

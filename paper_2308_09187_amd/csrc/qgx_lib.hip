@@ -957,6 +957,7 @@ qgx_status qgx_tensor_list_set(qgx_ctx* ctx, const qgx_tensor* tensors, uint32_t
     if (table_bytes < need) return fail(ctx, QGX_ERR_CAPACITY, "qgx_tensor_list_set: the table needs %llu bytes", (unsigned long long)need);
     bool shared = false;
     for (uint32_t i = 0; i < n_tensors; ++i) shared = shared || (tensors[i].stride < tensors[i].n && ctx->lay.K > 1u);
+    const uint64_t d = ctx->lay.d;
     // ranges of V, in order; two that follow each other may not overlap
     uint32_t* order = new (std::nothrow) uint32_t[n_tensors ? n_tensors : 1];
     if (!order) return fail(ctx, QGX_ERR_ARG, "qgx_tensor_list_set: no memory for %u tensors", n_tensors);
@@ -982,7 +983,7 @@ qgx_status qgx_tensor_list_set(qgx_ctx* ctx, const qgx_tensor* tensors, uint32_t
         batch.pieces = 0;
         batch.count = 0;
     }
-    *list = qgx_tensor_list{table, table_bytes, pieces, n_tensors, shared ? 1u : 0u};
+    *list = qgx_tensor_list{table, table_bytes, pieces, d, ctx->lay.K, n_tensors, shared ? 1u : 0u};
     return QGX_OK;
 }
 
@@ -994,6 +995,8 @@ qgx_status qgx_clip_gradients(qgx_ctx* ctx, const qgx_tensor_list* list, int nor
     if (!(max_norm >= 0.0f)) return fail(ctx, QGX_ERR_ARG, "qgx_clip_gradients: max_norm must be >= 0");
     if (!aligned16(V) || !aligned_to(norms, 4u)) return fail(ctx, QGX_ERR_ARG, "qgx_clip_gradients: V must be 16-byte aligned, norms 4-byte");
     if (!V && list->shared_rows) return fail(ctx, QGX_ERR_ARG, "qgx_clip_gradients: the workers share elements, which in-place clipping would scale more than once");
+    if (list->d != ctx->lay.d || list->K != ctx->lay.K)
+        return fail(ctx, QGX_ERR_ARG, "qgx_clip_gradients: the list was made for %u workers of %llu coordinates", list->K, (unsigned long long)list->d);
     if (list->table_bytes < list_bytes(list->n_pieces, ctx->lay.K))
         return fail(ctx, QGX_ERR_CAPACITY, "qgx_clip_gradients: the list's table is too small for this context");
     ClipArgs a{};

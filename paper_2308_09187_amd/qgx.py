@@ -64,8 +64,8 @@ class _Tensor(C.Structure):
 
 
 class _TensorList(C.Structure):
-    _fields_ = [("table", C.c_void_p), ("table_bytes", C.c_uint64), ("n_pieces", C.c_uint64), ("n_tensors", C.c_uint32),
-                ("shared_rows", C.c_uint32)]
+    _fields_ = [("table", C.c_void_p), ("table_bytes", C.c_uint64), ("n_pieces", C.c_uint64), ("d", C.c_uint64), ("K", C.c_uint32),
+                ("n_tensors", C.c_uint32), ("shared_rows", C.c_uint32)]
 
 
 class _Buckets(C.Structure):
@@ -166,6 +166,37 @@ class Buckets:
         self._rows = (C.c_uint32 * max(1, len(rows)))(*[int(x) for x in rows])
         self._c = _Buckets(len(rows), self._bounds, self._rows)
         self._ref = C.addressof(self._c)
+
+    @classmethod
+    def logarithmic(cls, rows, far, both=False, window=None):
+        """Buckets of a table of `rows` rows: of m rows for keys at and before the query, the first m // 2 have a distance
+        each (0, 1, ..), the others start at m // 2 times equal powers of far / (m // 2), the last of them holding all that is
+        further.  both=False: m = rows, keys after the query are masked; both=True: m = rows // 2, and as many rows again,
+        m .., for the keys after it, by the same distances.  window: keys that far before (and after) or further are masked.
+        The starts are worked out in whole numbers: exact, whatever the machine's logarithm."""
+        m = rows // 2 if both else rows
+        exact = m // 2
+        _need(m >= 2 and far > exact, "Buckets.logarithmic: two rows a side at least, and far beyond those of one distance each")
+        start = list(range(exact))
+        for t in range(m - exact):                       # the smallest n with (n / exact)^(m - exact) >= (far / exact)^t
+            n = start[-1] + 1
+            while n ** (m - exact) < exact ** (m - exact - t) * far ** t:
+                n += 1
+            start.append(n)
+        end = (1 << 30) if window is None else int(window)
+        _need(end >= 1, "Buckets.logarithmic: a window of one key at least")
+        start = [n for n in start if n < end]
+        bounds, ids = [1 - end], []
+        for b in range(len(start) - 1, -1, -1):          # keys before the query, the furthest first
+            ids.append(b)
+            bounds.append(1 - start[b])
+        if both:
+            for b, n in enumerate(start):
+                stop = start[b + 1] if b + 1 < len(start) else end
+                if stop > 1:                             # (distance 0 is with the keys before)
+                    ids.append(m + b)
+                    bounds.append(stop)
+        return cls(bounds, ids)
 
 
 class TensorList:

@@ -255,6 +255,9 @@ def test_refusals(qgx):
     refused(lambda: ctx.clip_gradients(lst, 1.0, norm=1, out=V))
     refused(lambda: ctx.clip_gradients(lst, 1.0, out=V[:, :99]))
     refused(lambda: ctx.clip_gradients(lst, 1.0, out=V.double()))
+    other = qgx.Context(60, 2, 256)
+    refused(lambda: other.clip_gradients(lst, 1.0))                       # made for 100 coordinates
+    other.close()
     lst._c.table_bytes -= 8
     refused(lambda: ctx.clip_gradients(lst, 1.0, out=V), qgx.ERR_CAPACITY)
     ctx.close()
