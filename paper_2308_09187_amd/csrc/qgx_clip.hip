@@ -8,6 +8,8 @@
 // the writes before them; reading alone runs at 7.2 either way (1 GiB and more).  Squares are summed in binary64: no gradient of
 // binary32 overflows there, and the sum's rounding does not show in the norm's 24 bits.  Elements are scaled in binary64 too: a
 // factor of a few denormal bits, or none, would lose gradients that are huge but finite.
+#include <type_traits>
+
 #include "qgx_types.h"
 
 namespace qgx {
@@ -34,6 +36,16 @@ hipError_t launch_tensor_list(const TensorBatch& batch, TensorPiece* table, hipS
 {
     hipLaunchKernelGGL(k_tensor_list, dim3((uint32_t)min((batch.pieces + 255u) / 256u, (uint64_t)4096u)), dim3(256), 0, st, batch, table);
     return hipGetLastError();
+}
+
+// f with a value of the piece's type (the same in the whole workgroup).
+template <typename F>
+__device__ __forceinline__ void with_type(const TensorPiece& e, F f)
+{
+    const uint32_t type = e.n_type >> 16;
+    if (type == QGX_F32) f(float());
+    else if (type == QGX_F16) f(_Float16());
+    else f(__bf16());
 }
 
 template <bool MAX> struct ClipSum { double x = 0.0; };
@@ -72,17 +84,20 @@ __device__ __forceinline__ void sum_piece(const T* x, int n, ClipSum<MAX>& s)
     }
 }
 
+// The largest of a wave's binary32 values, a NaN among them the result.
+__device__ __forceinline__ double wave_largest(double x)
+{
+    return (double)__uint_as_float(wave_join_u32<32>(__float_as_uint((float)x), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__builtin_elementwise_maximum(__uint_as_float(a), __uint_as_float(b)));
+    }));
+}
+
 // The sum over a workgroup, in its first thread.
 template <bool MAX>
 __device__ __forceinline__ double clip_group_sum(double x, double* slot)
 {
-    if constexpr (MAX) {                                   // (binary32 values)
-        x = (double)__uint_as_float(wave_join_u32<32>(__float_as_uint((float)x), [](uint32_t a, uint32_t b) {
-            return __float_as_uint(__builtin_elementwise_maximum(__uint_as_float(a), __uint_as_float(b)));
-        }));
-    } else {
-        x = wave_sum(x);
-    }
+    if constexpr (MAX) x = wave_largest(x);
+    else x = wave_sum(x);
     if (lane_id() == 0) slot[wave_id()] = x;
     __syncthreads();
     if (threadIdx.x == 0)
@@ -102,10 +117,7 @@ __global__ __launch_bounds__(kClipThreads) void k_clip_norm(ClipArgs a)
         next = a.table[min(p + a.parts, a.n_pieces - 1u)];
         const void* x = reinterpret_cast<const void*>(e.data + (uint64_t)k * e.stride);
         const int n = (int)(e.n_type & 0xFFFFu);
-        const uint32_t type = e.n_type >> 16;
-        if (type == QGX_F32) sum_piece<float, MAX>((const float*)x, n, sum);
-        else if (type == QGX_F16) sum_piece<_Float16, MAX>((const _Float16*)x, n, sum);
-        else sum_piece<__bf16, MAX>((const __bf16*)x, n, sum);
+        with_type(e, [&](auto t) { sum_piece<decltype(t), MAX>((const decltype(t)*)x, n, sum); });
     }
     const double x = clip_group_sum<MAX>((double)sum.x, s_sum);
     if (threadIdx.x == 0) a.partial[(size_t)k * kClipParts + blockIdx.x] = x;
@@ -132,10 +144,8 @@ template <bool MAX>
 __device__ __forceinline__ double join_few(const double* __restrict__ partial, uint32_t parts)
 {
     const double x = (uint32_t)lane_id() < parts ? partial[lane_id()] : 0.0;
-    if constexpr (!MAX) return wave_sum(x);
-    else return (double)__uint_as_float(wave_join_u32<32>(__float_as_uint((float)x), [](uint32_t a, uint32_t b) {
-        return __float_as_uint(__builtin_elementwise_maximum(__uint_as_float(a), __uint_as_float(b)));
-    }));
+    if constexpr (MAX) return wave_largest(x);
+    else return wave_sum(x);
 }
 
 template <bool MAX>
@@ -156,29 +166,61 @@ constexpr int kScaleEach = 4;                              // elements that a th
 constexpr uint32_t kScaleTile = kClipThreads * kScaleEach;
 constexpr uint32_t kScaleTiles = kClipPiece / kScaleTile;  // tiles of a piece
 
-template <typename T, bool GATHER>
-__device__ __forceinline__ void scale_four(const TensorPiece& e, uint32_t k, int i, double c, float* to)
+// Four elements of a piece from element i on as they lie there (two words of 16-bit ones), zeros past its end.
+template <typename T>
+__device__ __forceinline__ nt_u32x4 load_four(const TensorPiece& e, uint32_t k, int i)
 {
     typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    typedef float four_f __attribute__((ext_vector_type(4), aligned(4)));
-    T* x = reinterpret_cast<T*>(e.data + (uint64_t)k * e.stride) + i;
+    const T* x = reinterpret_cast<const T*>(e.data + (uint64_t)k * e.stride) + i;
     const int n = (int)(e.n_type & 0xFFFFu) - i;
+    four y;
     if (n >= 4) {
-        const four y = __builtin_nontemporal_load(reinterpret_cast<const four*>(x));
-        four_f v;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = (float)((double)(float)y[q] * c);
-        if constexpr (GATHER) {
-            __builtin_nontemporal_store(v, reinterpret_cast<four_f*>(to + i));
-        } else {
-            *reinterpret_cast<four*>(x) = four{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
-        }
+        y = __builtin_nontemporal_load(reinterpret_cast<const four*>(x));
     } else {
-        for (int q = 0; q < n; ++q) {
-            const float v = (float)((double)(float)x[q] * c);
-            if constexpr (GATHER) to[i + q] = v;
-            else x[q] = (T)v;
-        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] = q < n ? x[q] : (T)0.0f;
+    }
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(nt_u32x4, y);
+    } else {
+        const uint64_t z = __builtin_bit_cast(uint64_t, y);
+        return nt_u32x4{(uint32_t)z, (uint32_t)(z >> 32), 0u, 0u};
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void values_of_four(nt_u32x4 x, float (&v)[4])
+{
+    if constexpr (sizeof(T) == 4) {
+        values_of<T>(x, v);
+    } else {
+        float w[kPiece<T>];
+        values_of<T>(x, w);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = w[q];
+    }
+}
+
+// They scaled, to V (row: the piece's first coordinate there) or to where they were.
+template <typename T, bool GATHER>
+__device__ __forceinline__ void store_four(const TensorPiece& e, uint32_t k, int i, double c, const float (&v)[4], float* row)
+{
+    using To = std::conditional_t<GATHER, float, T>;
+    typedef To four __attribute__((ext_vector_type(4), aligned(sizeof(To))));
+    To* to;
+    if constexpr (GATHER) to = row + i;
+    else to = reinterpret_cast<T*>(e.data + (uint64_t)k * e.stride) + i;
+    const int n = (int)(e.n_type & 0xFFFFu) - i;
+    four y;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] = (To)(float)((double)v[q] * c);
+    if (n >= 4) {
+        if constexpr (GATHER) __builtin_nontemporal_store(y, reinterpret_cast<four*>(to));
+        else *reinterpret_cast<four*>(to) = y;
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (q < n) to[q] = y[q];
     }
 }
 
@@ -202,10 +244,73 @@ __global__ __launch_bounds__(kClipThreads) void k_clip_scale(ClipArgs a, uint32_
     const int i = (int)(x % kScaleTiles * kScaleTile + threadIdx.x * kScaleEach);
     if (i >= (int)(e.n_type & 0xFFFFu)) return;
     float* to = GATHER ? a.V + (uint64_t)k * a.d + e.offset : nullptr;
-    const uint32_t type = e.n_type >> 16;
-    if (type == QGX_F32) scale_four<float, GATHER>(e, k, i, c, to);
-    else if (type == QGX_F16) scale_four<_Float16, GATHER>(e, k, i, c, to);
-    else scale_four<__bf16, GATHER>(e, k, i, c, to);
+    with_type(e, [&](auto t) {
+        using T = decltype(t);
+        float v[4];
+        values_of_four<T>(load_four<T>(e, k, i), v);
+        store_four<T, GATHER>(e, k, i, c, v, to);
+    });
+}
+
+// A few pieces: a workgroup for each worker holds them in registers between its sum and its stores, in one launch (4 x 16384 binary32
+// 5.8 us a call, in two launches 8.5; sixteen pieces take one compute unit 16 us, two launches over the GPU 5.5).
+constexpr int kSmallThreads = 1024, kSmallPieces = 4;
+static_assert(kSmallThreads * kScaleEach == (int)kClipPiece, "a thread has four elements of a piece");
+
+template <bool MAX, bool GATHER>
+__global__ __launch_bounds__(kSmallThreads) void k_clip_small(ClipArgs a, Scalars* sc)
+{
+    __shared__ double s_sum[kSmallThreads / kWave];
+    const uint32_t k = blockIdx.x, n_pieces = (uint32_t)a.n_pieces;
+    const int i = (int)threadIdx.x * kScaleEach;
+    // (no way out of the loops: the pieces' places, then all elements, are under way at once)
+    TensorPiece e[kSmallPieces];
+#pragma unroll
+    for (int p = 0; p < kSmallPieces; ++p) {
+        e[p] = a.table[min((uint32_t)p, n_pieces - 1u)];
+        if (p >= (int)n_pieces) e[p].n_type &= ~0xFFFFu;   // no elements
+    }
+    nt_u32x4 raw[kSmallPieces];
+#pragma unroll
+    for (int p = 0; p < kSmallPieces; ++p) with_type(e[p], [&](auto t) { raw[p] = load_four<decltype(t)>(e[p], k, i); });
+    ClipSum<MAX> sum;
+#pragma unroll
+    for (int p = 0; p < kSmallPieces; ++p) {
+        float v[4];
+        with_type(e[p], [&](auto t) { values_of_four<decltype(t)>(raw[p], v); });
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (MAX) sum.x = __builtin_elementwise_maximum(sum.x, fabsf(v[q]));
+            else sum.x = fma((double)v[q], (double)v[q], sum.x);
+        }
+    }
+    double x = (double)sum.x;
+    if constexpr (MAX) x = wave_largest(x);
+    else x = wave_sum(x);
+    if (lane_id() == 0) s_sum[wave_id()] = x;
+    __syncthreads();
+    x = s_sum[0];
+#pragma unroll
+    for (int w = 1; w < kSmallThreads / kWave; ++w) x = clip_join<MAX>(x, s_sum[w]);
+    const ClipFactor f = clip_factor<MAX>(x, a.max_norm);
+    if (threadIdx.x == 0) report_norm(a, k, f.norm, sc);
+    if (!GATHER && f.scale == 1.0) return;
+#pragma unroll
+    for (int p = 0; p < kSmallPieces; ++p)
+        with_type(e[p], [&](auto t) {
+            float v[4];
+            values_of_four<decltype(t)>(raw[p], v);
+            store_four<decltype(t), GATHER>(e[p], k, i, f.scale, v, GATHER ? a.V + (uint64_t)k * a.d + e[p].offset : nullptr);
+        });
+}
+
+static hipError_t launch_small(const ClipArgs& a, uint32_t K, bool max_kind, Scalars* sc, hipStream_t st)
+{
+    if (max_kind && a.V) hipLaunchKernelGGL((k_clip_small<true, true>), dim3(K), dim3(kSmallThreads), 0, st, a, sc);
+    else if (max_kind) hipLaunchKernelGGL((k_clip_small<true, false>), dim3(K), dim3(kSmallThreads), 0, st, a, sc);
+    else if (a.V) hipLaunchKernelGGL((k_clip_small<false, true>), dim3(K), dim3(kSmallThreads), 0, st, a, sc);
+    else hipLaunchKernelGGL((k_clip_small<false, false>), dim3(K), dim3(kSmallThreads), 0, st, a, sc);
+    return hipGetLastError();
 }
 
 template <ClipJoin JOIN>
@@ -230,6 +335,7 @@ static hipError_t launch_scale(ClipArgs a, uint32_t K, Scalars* sc, hipStream_t 
 hipError_t launch_clip(const ClipArgs& args, uint32_t K, bool max_kind, uint32_t n_cu, Scalars* sc, hipStream_t st)
 {
     ClipArgs a = args;
+    if (a.n_pieces && a.n_pieces <= (uint32_t)kSmallPieces) return launch_small(a, K, max_kind, sc, st);
     // eight workgroups for every compute unit over all workers
     const uint64_t each = max(1u, min(kClipParts, 8u * n_cu / K));
     a.parts = (uint32_t)min(a.n_pieces, each);
