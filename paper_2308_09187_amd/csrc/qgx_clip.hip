@@ -1,7 +1,8 @@
 // Each worker's global gradient norm over its many tensors, and clipping, gathered into the dual vectors or in place.
 //   N_k = (sum over tensors and elements x^2)^(1/2), or max |x|;   c_k = N_k > M ? M / N_k : 1;   V[k][offset + i] = c_k x_i
-// A launch that reads everything once and leaves a sum per workgroup, one workgroup per worker that adds those up in their order and
-// leaves the factor, and a launch that scales; where a worker's sums are few the scaling waves add them up themselves, in the same order.
+// A launch that reads everything once and leaves a sum per workgroup, one workgroup per worker that adds those up and leaves the
+// factor, and a launch that scales; where a worker's sums are few every scaling wave adds them up itself, and where its pieces are few one
+// launch does it all.  Which it is, and the order of all sums, follows from the sizes and the device.
 // (The last workgroup to arrive could do it, counting: but an agent-wide release and acquire in every workgroup costs 28 ns, one after
 // the other: 2048 workgroups over 33 MB took 56 us.)  The scaling launch consists of tiny workgroups, a thread moves four elements: reading
 // and writing runs at 6.5 TB/s that way and at 4.5 to 5 with workgroups that go on from tile to tile, where reads wait behind

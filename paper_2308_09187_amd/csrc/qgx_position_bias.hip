@@ -116,6 +116,9 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias(BiasArgs a, Buck
     if (task >= t.tasks || plane >= a.planes) return;
     const int lane = lane_id(), q = (int)a.q, k = (int)a.k, lo = b.bounds[0], hi = b.bounds[b.n];
     const uint32_t head = plane % a.heads, seq = plane / a.heads, worker = seq / a.batch, n = seq % a.batch;
+    // All intervals' biases at once and first: one after the other, or after the scores, they would be the longest wait there is.
+    const Intervals interval(b);
+    const float value0 = a.table[(size_t)interval.row0 * a.heads + head], value1 = a.table[(size_t)interval.row1 * a.heads + head];
     const uint32_t group = task / t.chunks, band0 = group * t.bands_each, first = (task - group * t.chunks) * t.chunk;
     const uint32_t end = min(first + t.chunk, t.per_band), band1 = min(band0 + t.bands_each, t.bands);
     const uint32_t mine = ((uint32_t)lane * t.inverse) >> 16, band = band0 + mine, square = first + (uint32_t)lane - mine * t.chunk;
@@ -139,9 +142,6 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias(BiasArgs a, Buck
     // deltas of the wave: d0 .. d1
     const int d0 = min((int)(first * W), k - W) - (min((int)(band1 * ROWS), q) - 1) - p;
     const int d1 = min((int)(end * W), k) - min((int)(band0 * ROWS), q - ROWS) - p;
-    const Intervals interval(b);
-    // (all intervals' biases at once: one after the other they would be the longest wait there is)
-    const float value0 = a.table[(size_t)interval.row0 * a.heads + head], value1 = a.table[(size_t)interval.row1 * a.heads + head];
     // Three in four waves of long rows meet one interval or two; where there are many (they take 0.1 us each), every diagonal is searched for.
     if (interval.number(d0, d1) <= kFewIntervals) {
         interval.meeting(d0, d1, [&](int i, int j, int x0, int x1) {
