@@ -334,7 +334,7 @@ struct BiasArgs {
     uint32_t batch, heads, q, k;
     uint32_t planes;            // workers * batch * heads
 };
-hipError_t launch_position_bias(int dtype, const BiasArgs& a, const BucketArgs& b, hipStream_t st);
+hipError_t launch_position_bias(int dtype, const BiasArgs& a, const BucketArgs& b, uint32_t n_cu, hipStream_t st);
 constexpr uint32_t kMaxBands = 128;        // bands that get workgroups by their work
 struct BiasBackPlan {
     int64_t first, count;       // block diagonals with a place that is not masked

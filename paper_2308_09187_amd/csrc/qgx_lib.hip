@@ -1188,7 +1188,7 @@ qgx_status qgx_position_bias(qgx_ctx* ctx, const qgx_buckets* buckets, const flo
     a.out = out->data;
     a.o_worker = out->s_worker; a.o_batch = out->s_batch; a.o_head = out->s_head; a.o_row = out->s_row;
     a.table = table; a.positions = positions; a.q_offset = q_offset;
-    QGX_HIP(ctx, launch_position_bias(out->dtype, a, b, (hipStream_t)stream));
+    QGX_HIP(ctx, launch_position_bias(out->dtype, a, b, ctx->n_simd / 4u, (hipStream_t)stream));
     return QGX_OK;
 }
 

@@ -115,6 +115,22 @@ def test_tokens_of_sequences_of_different_lengths(ctx, qgx, q, k, name, typ):
 
 
 @pytest.mark.parametrize("typ", list(TYPES))
+@pytest.mark.parametrize("name", ["causal", "both", "every"])
+@pytest.mark.parametrize("q,k", [(1, 1100), (3, 1100), (1, 2600), (1, 1024)])
+def test_tokens_of_many_sequences(ctx, qgx, q, k, name, typ):
+    N, heads = 350, 8                                         # enough that a wave takes several pieces
+    bounds, rows, R = BUCKETS[name]
+    b = qgx.Buckets(bounds, rows)
+    table, scores = put(rnd(1, R, heads), "f32"), put(rnd(2, N, heads, q, k), typ)
+    pos = np.random.default_rng(3).integers(-5, k + 70, N)
+    p = torch.from_numpy(pos.astype(np.int32)).cuda()
+    out = ctx.add_position_bias(scores, table, b, positions=p)
+    check_out(host(out), host(scores), host(table), np.stack([rows_of(name, q, k, x) for x in pos]), typ)
+    ctx.add_position_bias(scores, table, b, positions=p, out=scores)
+    assert torch.equal(scores, out)
+
+
+@pytest.mark.parametrize("typ", list(TYPES))
 def test_masked_and_special_scores(ctx, qgx, typ):
     heads, n = 2, 40
     low = float(torch.finfo(TYPES[typ]).min)
