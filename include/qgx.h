@@ -431,7 +431,7 @@ typedef struct {
 
 /* Learned relative position bias: out = in + table[row of (j - i - p)][head] for query i and key j, p = q_offset (the
  * position of query 0 among the keys) + positions[worker * batch + n]; -infinity where j - i - p is masked, whatever `in` holds
- * there (it is not read).  A query none of whose keys is seen has a row of -infinity.
+ * there.  A query none of whose keys is seen has a row of -infinity.
  *   table      DEVICE [table_rows][heads] binary32 (a run of X)
  *   in         NULL: the bias alone, without scores; else of out's type and shape, and may be out
  *   positions  DEVICE [workers * batch] or NULL (0): the form for single tokens of sequences of different lengths

