@@ -5,7 +5,7 @@
 //   gradient: a thread walks down a block diagonal, its sums of 2 W - 1 diagonals in registers over all queries and sequences, and only at its
 //     end are they sorted into the buckets, which are runs of diagonals.  No element meets a bucket, an atomic or a search.
 // Both are bound by memory.  8 x 16 x 1024 x 1024 bfloat16: forward, 537 MB, 82 us, 6.5 TB/s (95 with its memory out of the cache);
-// gradient, 268 MB, 51 us, 5.2 TB/s.
+// gradient, 268 MB, 53 us, 5.1 TB/s; 64 x 16 x 197 x 197 28 us, 2.8 TB/s.
 #include "qgx_types.h"
 
 namespace qgx {
@@ -351,26 +351,32 @@ __host__ __device__ inline BandSteps band_steps(int64_t D0, int64_t D1, int q_st
     return BandSteps{(int)s0, (int)(s1 > s0 ? s1 : s0)};
 }
 
-// n elements of a piece that ends with its row: those before the end, the rest zeros.  row: keys of it, W or more.
+// The last n elements of a piece, moved to its front, and zeros after them.
 template <typename T>
-__device__ __forceinline__ nt_u32x4 load_end(const T* p, int n)
+__device__ __forceinline__ nt_u32x4 last_elements(nt_u32x4 x, int n)
 {
-    nt_u32x4 x = load_bits(p - (kPiece<T> - n));
     uint64_t lo = x.x | (uint64_t)x.y << 32, hi = x.z | (uint64_t)x.w << 32;
-    const int bits = (kPiece<T> - n) * 8 * (int)sizeof(T);     // 16 or 32 .. 112
+    const int bits = (kPiece<T> - n) * 8 * (int)sizeof(T);     // 0, 16 or 32 .. 112
     if (bits >= 64) {
         lo = hi >> (bits - 64);
         hi = 0;
-    } else {
+    } else if (bits) {
         lo = lo >> bits | hi << (64 - bits);
         hi >>= bits;
     }
     return nt_u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 
+// A square as loaded: the rows that it has (none where there is no square), and its keys' number.
+template <typename T> struct Square {
+    nt_u32x4 row[kPiece<T>];
+    int rows, keys;
+};
+
 constexpr int kShort = 16;                                 // diagonals of an interval that a lane adds up
 
-template <typename T, int BAND>
+// NARROW: fewer keys than a piece has elements.
+template <typename T, int BAND, bool NARROW>
 __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a, BucketArgs b, BiasBackPlan plan, float* __restrict__ partial)
 {
     constexpr int W = kPiece<T>, E = 2 * W - 1, kSpan = BAND * W + W, kGroups = kBiasThreads / BAND;
@@ -405,47 +411,67 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a,
         float sum[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-        nt_u32x4 raw[W];                                   // the item before, as loaded
-#pragma unroll
-        for (int r = 0; r < W; ++r) raw[r] = nt_u32x4{0u, 0u, 0u, 0u};
         // this group's first item: sequence n, step s; and from one item to its next
         const uint32_t x0 = split * kGroups + threadIdx.x / BAND, hop = splits * kGroups;
         uint32_t n = steps ? x0 / steps : a.batch, s = steps ? x0 % steps : 0u;
         const uint32_t hop_n = steps ? hop / steps : 0u, hop_s = steps ? hop % steps : 0u;
-        // (the groups of a wave go on as long as any of the workgroup's has an item, and one more turn adds the last)
-        for (uint64_t turn = (uint64_t)split * kGroups; turn < items + hop; turn += hop) {
-            nt_u32x4 next[W];
-#pragma unroll
-            for (int r = 0; r < W; ++r) next[r] = nt_u32x4{0u, 0u, 0u, 0u};
+        // Two squares' loads are under way at a time (64 x 16 x 197 x 197 bfloat16 39 us with one, 28; 8 x 16 x 1024 x 1024 53 either way).
+        // Every lane loads W pieces whether it has a square or not (a neighbour's then), for a wait for the square before has to know how
+        // many loads came after it.
+        auto load = [&](Square<T>& x) {
             const int64_t jb = (int64_t)at.s0 + s + D;     // the square's keys
-            if (n < a.batch && D <= D1 && jb >= 0 && jb < k_steps) {
-                const uint32_t i0 = ((uint32_t)at.s0 + s) * W, left = a.k - (uint32_t)jb * W;
-                const T* in = base + n * a.i_batch + i0 * a.i_row + jb * W;
-                if (i0 + W <= a.q && left >= (uint32_t)W) {
+            const bool any = n < a.batch && D <= D1 && jb >= 0 && jb < k_steps;
+            const uint32_t i0 = ((uint32_t)at.s0 + s) * W, j0 = (uint32_t)max((int64_t)0, min(jb - max(D - D1, (int64_t)0), (int64_t)k_steps - 1)) * W;
+            const T* in = base + min(n, a.batch - 1u) * a.i_batch + i0 * a.i_row;
+            x.rows = any ? (int)min((uint32_t)W, a.q - i0) : 0;
+            x.keys = (int)min((uint32_t)W, a.k - j0);
+            if constexpr (NARROW) {
 #pragma unroll
-                    for (int r = 0; r < W; ++r) next[r] = load_bits(in + (uint32_t)r * a.i_row);
+                for (int r = 0; r < W; ++r)
+                    x.row[r] = __builtin_bit_cast(nt_u32x4, load_raw(in + min((uint32_t)r, a.q - 1u - i0) * a.i_row, x.keys));
+            } else {
+                in += j0 - (uint32_t)(W - x.keys);         // (moved back to end with its row)
+                if (__ballot(i0 + W > a.q) == 0) {
+#pragma unroll
+                    for (int r = 0; r < W; ++r) x.row[r] = load_bits(in + (uint32_t)r * a.i_row);
                 } else {
 #pragma unroll
-                    for (int r = 0; r < W; ++r) {
-                        if (i0 + r >= a.q) continue;
-                        const T* from = in + (uint32_t)r * a.i_row;
-                        if (left >= (uint32_t)W) next[r] = load_bits(from);
-                        else if (a.k >= (uint32_t)W) next[r] = load_end(from, (int)left);
-                        else next[r] = __builtin_bit_cast(nt_u32x4, load_raw(from, (int)left));
-                    }
+                    for (int r = 0; r < W; ++r) x.row[r] = load_bits(in + min((uint32_t)r, a.q - 1u - i0) * a.i_row);
                 }
-            }
-#pragma unroll
-            for (int r = 0; r < W; ++r) {
-                float v[W];
-                values_of<T>(raw[r], v);
-#pragma unroll
-                for (int c = 0; c < W; ++c) sum[c - r + W - 1] += v[c];
-                raw[r] = next[r];
             }
             n += hop_n;
             s += hop_s;
             if (s >= steps) { s -= steps; ++n; }
+        };
+        auto add = [&](Square<T>& x) {
+            if (__ballot(x.rows < W || x.keys < W) != 0)
+#pragma unroll
+                for (int r = 0; r < W; ++r) {
+                    if (!NARROW) x.row[r] = last_elements<T>(x.row[r], x.keys);
+                    if (r >= x.rows) x.row[r] = nt_u32x4{0u, 0u, 0u, 0u};
+                }
+#pragma unroll
+            for (int r = 0; r < W; ++r) {
+                float v[W];
+                values_of<T>(x.row[r], v);
+#pragma unroll
+                for (int c = 0; c < W; ++c) sum[c - r + W - 1] += v[c];
+            }
+        };
+        // (the same number of turns for the whole workgroup: a group without an item any more has squares of no rows)
+        const uint64_t before = (uint64_t)split * kGroups;
+        uint64_t turns = items > before ? (items - before + hop - 1u) / hop : 0u;
+        if (turns) {
+            Square<T> even, odd;
+            load(even);
+            for (;; turns -= 2u) {
+                if (turns == 1u) { add(even); break; }
+                load(odd);
+                add(even);
+                if (turns == 2u) { add(odd); break; }
+                load(even);
+                add(odd);
+            }
         }
         // the wave's groups joined, then a diagonal of the band is that of one lane's square from its main one on and of the next
         // lane's below it
@@ -547,8 +573,9 @@ BiasBackPlan bias_back_plan(int dtype, const BiasArgs& a, const BucketArgs& b, u
     p.bands = (uint32_t)((p.count + band - 1) / band);
     if (!p.bands) return p;
     const int q_steps = (int)((a.q + W - 1u) / W), k_steps = (int)((a.k + W - 1u) / W);
-    // eight workgroups for every compute unit over pairs and bands
-    const uint64_t want = max((uint64_t)1u, (8u * (uint64_t)n_cu + p.pairs - 1u) / p.pairs);      // of a pair
+    // Workgroups of a pair: six for every compute unit over all pairs and bands while a group of lanes has four items then, and not below three,
+    // which is what a compute unit holds at once (4 x 3 x 4 x 1019 x 1019 bfloat16 27 us with six, 25 with three; 8 x 16 x 1024 x 1024 53 and 55).
+    const uint64_t want = max((uint64_t)1u, (6u * (uint64_t)n_cu + p.pairs - 1u) / p.pairs), least = max((uint64_t)1u, (3u * (uint64_t)n_cu + p.pairs - 1u) / p.pairs);
     if (p.bands > kMaxBands) {
         const uint64_t most = ((uint64_t)q_steps * a.batch + groups - 1u) / groups;
         p.even = (uint32_t)min((want + p.bands - 1u) / p.bands, most);
@@ -560,9 +587,8 @@ BiasBackPlan bias_back_plan(int dtype, const BiasArgs& a, const BucketArgs& b, u
             const BandSteps s = band_steps(D0, D1, q_steps, k_steps);
             all += items[i] = (uint64_t)(s.s1 - s.s0) * a.batch;
         }
-        // items of a workgroup: one for a group of lanes while that leaves four workgroups for every compute unit, else two or more (9 x 7 x 47 x 47
-        // bfloat16 14.0 us a call with two, 11.6 with one; 6 x 18 x 370 x 370 18.7 and 21.5)
-        const uint64_t each = max((uint64_t)groups * (all / groups * p.pairs <= 4u * n_cu ? 1u : 2u), (all + want - 1u) / want);
+        // items of a workgroup
+        const uint64_t each = max((uint64_t)groups, max((all + want - 1u) / want, min((uint64_t)groups * 4u, (all + least - 1u) / least)));
         for (uint32_t i = 0; i < p.bands; ++i) {
             p.first_block[i] = p.blocks;
             p.blocks += (uint32_t)max((uint64_t)1u, (items[i] + each - 1u) / each);
@@ -577,8 +603,9 @@ template <typename T>
 static hipError_t launch_bias_back_of(const BiasArgs& a, const BucketArgs& b, const BiasBackPlan& p, float* partial, hipStream_t st)
 {
     const dim3 grid(p.blocks, min(p.pairs, 65535u));
-    if (p.band == 64u) hipLaunchKernelGGL((k_position_bias_back<T, 64>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
-    else hipLaunchKernelGGL((k_position_bias_back<T, 16>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
+    if (a.k < (uint32_t)kPiece<T>) hipLaunchKernelGGL((k_position_bias_back<T, 16, true>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
+    else if (p.band == 64u) hipLaunchKernelGGL((k_position_bias_back<T, 64, false>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
+    else hipLaunchKernelGGL((k_position_bias_back<T, 16, false>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
     return hipGetLastError();
 }
 
