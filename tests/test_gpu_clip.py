@@ -195,6 +195,25 @@ def test_workers_that_share_a_gradient(qgx):
     ctx.close()
 
 
+def test_offsets_beyond_32_bits(qgx):
+    K, n, far = 2, 50001, (1 << 32) + 24                     # workers' tensors four thousand million elements apart
+    memory = torch.empty(far + (1 << 20), device="cuda", dtype=torch.bfloat16)
+    tensors = [memory.as_strided((K, n), (far, 1), at) for at in (1, 300001)]
+    for i, t in enumerate(tensors):
+        t.copy_(torch.from_numpy(np.random.default_rng(i).standard_normal((K, n))))
+    offsets, d = [0, up4(n)], 2 * up4(n)
+    c = qgx.Context(d, K, 256)
+    norms, scale, V = want(tensors, offsets, d, 3.0, "l2", np.full((K, d), 7.0))
+    lst, got = c.tensor_list(tensors, offsets), torch.full((K, d), 7.0, device="cuda")
+    close(c.clip_gradients(lst, 3.0, out=got).cpu(), norms, 2 * 2.0 ** -24)
+    close(got.cpu(), V, 2 * 2.0 ** -24)
+    before = [t.clone() for t in tensors]
+    c.clip_gradients(lst, 3.0)
+    for t, x in zip(tensors, before):
+        close(t.double().cpu().numpy(), x.double().cpu().numpy() * scale[:, None], (2.0 ** -8 + 2.0 ** -24) * 1.001)
+    c.close()
+
+
 def test_repeats_bit_for_bit_and_on_another_stream(qgx):
     K = 4
     tensors, offsets, d = make([300001, 40, 70000], K, [torch.float32, torch.bfloat16])

@@ -257,6 +257,23 @@ def test_gradients_against_differences(ctx):
         assert np.abs(num - got).max() <= 2e-5 * max(1.0, np.abs(num).max())
 
 
+def test_offsets_beyond_32_bits(ctx):
+    K, rows, cols, far = 2, 3, 1001, (1 << 32) + 24
+    memory = torch.empty(far + (1 << 20), device="cuda", dtype=torch.bfloat16)
+    view = lambda at: memory.as_strided((K, rows, cols), (far, 1024, 1), at)
+    x, dy, w, mean, rstd = back_inputs(K, rows, cols, "bf16", seed=9)
+    xs, gs, ys = view(0), view(100001), view(200002)
+    xs.copy_(x)
+    gs.copy_(dy)
+    y, m, r = ctx.layer_norm(xs, w, w, out=ys)
+    y2, m2, r2 = ctx.layer_norm(x, w, w)
+    assert torch.equal(ys, y2) and torch.equal(m, m2) and torch.equal(r, r2)
+    check_forward(host(x), host(w), host(w), 1e-5, "bf16", host(ys), host(m), host(r))
+    dw, db = torch.empty(K, cols, device="cuda"), torch.empty(K, cols, device="cuda")
+    dx = ctx.layer_norm_backward(gs, xs, w, mean, rstd, dw=dw, db=db, dx=view(300003))
+    check_backward(host(dy), host(x), host(w), host(mean), host(rstd), "bf16", host(dx), host(dw), host(db))
+
+
 def test_nothing_to_do(ctx):
     x = torch.empty(2, 0, 64, device="cuda")
     w = torch.ones(64, device="cuda")

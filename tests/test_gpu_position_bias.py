@@ -257,6 +257,23 @@ def test_gradient_against_differences(ctx, qgx):
     assert np.abs(num - host(dt)).max() <= 1e-5 * max(1.0, np.abs(num).max())
 
 
+@pytest.mark.parametrize("q,k", [(1, 1500), (40, 45), (9, 5)])
+def test_offsets_beyond_32_bits(ctx, qgx, q, k):
+    N, heads, far = 2, 3, (1 << 32) + 24
+    bounds, rows, R = BUCKETS["causal"]
+    b = qgx.Buckets(bounds, rows)
+    memory = torch.empty(far + (1 << 20), device="cuda", dtype=torch.bfloat16)
+    view = lambda at: memory.as_strided((N, heads, q, k), (far, q * k + 11, k, 1), at)
+    x, table = put(rnd(1, N, heads, q, k), "bf16"), put(rnd(2, R, heads), "f32")
+    xs = view(0).copy_(x)
+    out = ctx.add_position_bias(xs, table, b, q_offset=k - q, out=view(300001))
+    check_out(host(out), host(x), host(table), rows_of("causal", q, k, k - q), "bf16")
+    dt = torch.empty(R, heads, device="cuda")
+    ctx.position_bias_backward(xs, b, dt, q_offset=k - q)
+    exact, mag, count = expect_grad(host(x)[None], "causal", heads, k - q)
+    assert (np.abs(host(dt) - exact[0]) <= (count[:, None] + 2) * U * mag[0] + TINY["f32"]).all()
+
+
 def test_nothing_to_do(ctx, qgx):
     b = qgx.Buckets(*BUCKETS["causal"][:2])
     table = torch.zeros(12, 3, device="cuda")
