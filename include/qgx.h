@@ -364,6 +364,8 @@ typedef struct {
     uint32_t K;
     uint32_t n_tensors;
     uint32_t shared_rows; /* workers share elements of a tensor (stride < n): not to be written */
+    int32_t dtype;        /* the tensors' type, -1: several */
+    uint64_t first, end;  /* addresses between which all elements lie */
 } qgx_tensor_list;
 
 /* Bytes a table of these tensors needs.  Host-side only. */

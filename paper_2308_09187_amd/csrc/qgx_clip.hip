@@ -2,7 +2,7 @@
 //   N_k = (sum over tensors and elements x^2)^(1/2), or max |x|;   c_k = N_k > M ? M / N_k : 1;   V[k][offset + i] = c_k x_i
 // A launch that reads everything once and leaves a sum per workgroup, one workgroup per worker that adds those up and leaves the
 // factor, and a launch that scales; where a worker's sums are few every scaling wave adds them up itself, and where its pieces are few one
-// launch does it all.  Which it is, and the order of all sums, follows from the sizes and the device.
+// launch does it all, each workgroup for itself.  Which it is, and the order of all sums, follows from the sizes and the device.
 // (The last workgroup to arrive could do it, counting: but an agent-wide release and acquire in every workgroup costs 28 ns, one after
 // the other: 2048 workgroups over 33 MB took 56 us.)  The scaling launch consists of tiny workgroups, a thread moves four elements: reading
 // and writing runs at 6.5 TB/s that way and at 4.5 to 5 with workgroups that go on from tile to tile, where reads wait behind
@@ -169,7 +169,7 @@ constexpr uint32_t kScaleTile = kClipThreads * kScaleEach;
 constexpr uint32_t kScaleTiles = kClipPiece / kScaleTile;  // tiles of a piece
 
 // Four elements of a piece from element i on as they lie there (two words of 16-bit ones), zeros past its end.
-template <typename T>
+template <typename T, bool AGAIN = false>
 __device__ __forceinline__ nt_u32x4 load_four(const TensorPiece& e, uint32_t k, int i)
 {
     typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
@@ -177,7 +177,9 @@ __device__ __forceinline__ nt_u32x4 load_four(const TensorPiece& e, uint32_t k, 
     const int n = (int)(e.n_type & 0xFFFFu) - i;
     four y;
     if (n >= 4) {
-        y = __builtin_nontemporal_load(reinterpret_cast<const four*>(x));
+        // (AGAIN: others read it as well)
+        if constexpr (AGAIN) y = *reinterpret_cast<const four*>(x);
+        else y = __builtin_nontemporal_load(reinterpret_cast<const four*>(x));
     } else {
 #pragma unroll
         for (int q = 0; q < 4; ++q) y[q] = q < n ? x[q] : (T)0.0f;
@@ -316,6 +318,69 @@ __global__ __launch_bounds__(kSmallThreads) void k_clip_small(ClipArgs a, Scalar
         });
 }
 
+// Some pieces more, all of one type, into V: a workgroup for each piece of each worker, which sums up all of the worker's pieces, as every other
+// one of that worker's does, and scales its own: no second launch has to wait for the sums.  (Not in place, where a piece might have been
+// scaled before another workgroup has read it.)  4 x 65536 binary32 6.3 us a call, 8.0 in two launches; 4 x 32768 5.7 and 8.1; 32 pieces
+// take 13 us.
+constexpr int kAgainPieces = 16;
+
+template <typename T, bool MAX, int PIECES>
+__global__ __launch_bounds__(kSmallThreads) void k_clip_again(ClipArgs a, Scalars* sc)
+{
+    __shared__ double s_sum[kSmallThreads / kWave];
+    const uint32_t k = blockIdx.x, mine = blockIdx.y, n_pieces = (uint32_t)a.n_pieces;      // (a worker's workgroups on as few XCDs as can be)
+    const int i = (int)threadIdx.x * kScaleEach;
+    nt_u32x4 raw[PIECES], own = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        TensorPiece e = a.table[min((uint32_t)p, n_pieces - 1u)];
+        if (p >= (int)n_pieces) e.n_type &= ~0xFFFFu;      // no elements
+        raw[p] = load_four<T, true>(e, k, i);
+    }
+    ClipSum<MAX> sum;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        float v[4];
+        values_of_four<T>(raw[p], v);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (MAX) sum.x = __builtin_elementwise_maximum(sum.x, fabsf(v[q]));
+            else sum.x = fma((double)v[q], (double)v[q], sum.x);
+        }
+        if (p == (int)mine) own = raw[p];
+    }
+    double x = (double)sum.x;
+    if constexpr (MAX) x = wave_largest(x);
+    else x = wave_sum(x);
+    if (lane_id() == 0) s_sum[wave_id()] = x;
+    __syncthreads();
+    x = s_sum[0];
+#pragma unroll
+    for (int w = 1; w < kSmallThreads / kWave; ++w) x = clip_join<MAX>(x, s_sum[w]);
+    const ClipFactor f = clip_factor<MAX>(x, a.max_norm);
+    if (mine == 0u && threadIdx.x == 0) report_norm(a, k, f.norm, sc);
+    const TensorPiece e = a.table[mine];
+    float v[4];
+    values_of_four<T>(own, v);
+    store_four<T, true>(e, k, i, f.scale, v, a.V + (uint64_t)k * a.d + e.offset);
+}
+
+template <typename T, int PIECES>
+static hipError_t launch_again(const ClipArgs& a, uint32_t K, bool max_kind, Scalars* sc, hipStream_t st)
+{
+    const dim3 grid(K, (uint32_t)a.n_pieces);
+    if (max_kind) hipLaunchKernelGGL((k_clip_again<T, true, PIECES>), grid, dim3(kSmallThreads), 0, st, a, sc);
+    else hipLaunchKernelGGL((k_clip_again<T, false, PIECES>), grid, dim3(kSmallThreads), 0, st, a, sc);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_again_of(const ClipArgs& a, uint32_t K, bool max_kind, Scalars* sc, hipStream_t st)
+{
+    return a.n_pieces <= (uint64_t)kAgainPieces / 2u ? launch_again<T, kAgainPieces / 2>(a, K, max_kind, sc, st)
+                                                     : launch_again<T, kAgainPieces>(a, K, max_kind, sc, st);
+}
+
 static hipError_t launch_small(const ClipArgs& a, uint32_t K, bool max_kind, Scalars* sc, hipStream_t st)
 {
     if (max_kind && a.V) hipLaunchKernelGGL((k_clip_small<true, true>), dim3(K), dim3(kSmallThreads), 0, st, a, sc);
@@ -349,6 +414,11 @@ hipError_t launch_clip(const ClipArgs& args, uint32_t K, bool max_kind, uint32_t
 {
     ClipArgs a = args;
     if (a.n_pieces && a.n_pieces <= (uint32_t)kSmallPieces) return launch_small(a, K, max_kind, sc, st);
+    if (a.apart && a.n_pieces && a.n_pieces <= (uint64_t)kAgainPieces && K * a.n_pieces <= n_cu) {
+        if (a.dtype == QGX_F32) return launch_again_of<float>(a, K, max_kind, sc, st);
+        if (a.dtype == QGX_F16) return launch_again_of<_Float16>(a, K, max_kind, sc, st);
+        if (a.dtype == QGX_BF16) return launch_again_of<__bf16>(a, K, max_kind, sc, st);
+    }
     // eight workgroups for every compute unit over all workers
     const uint64_t each = max(1u, min(kClipParts, 8u * n_cu / K));
     a.parts = (uint32_t)min(a.n_pieces, each);

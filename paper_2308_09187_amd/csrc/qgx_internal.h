@@ -281,6 +281,8 @@ struct ClipArgs {
     uint64_t d;
     uint32_t parts;             // workgroups that sum a worker's pieces
     float max_norm;
+    bool apart;                 // V shares no memory with the tensors
+    int32_t dtype;              // of all tensors, -1: not of all
 };
 hipError_t launch_tensor_list(const TensorBatch& batch, TensorPiece* table, hipStream_t st);
 hipError_t launch_clip(const ClipArgs& a, uint32_t K, bool max_kind, uint32_t n_cu, Scalars* sc, hipStream_t st);

@@ -983,7 +983,16 @@ qgx_status qgx_tensor_list_set(qgx_ctx* ctx, const qgx_tensor* tensors, uint32_t
         batch.pieces = 0;
         batch.count = 0;
     }
-    *list = qgx_tensor_list{table, table_bytes, pieces, d, ctx->lay.K, n_tensors, shared ? 1u : 0u};
+    uint64_t first = ~0ull, end = 0;
+    int32_t dtype = -2;                                    // (none yet)
+    for (uint32_t i = 0; i < n_tensors; ++i) {
+        if (!tensors[i].n) continue;
+        const uint64_t at = (uint64_t)reinterpret_cast<uintptr_t>(tensors[i].data);
+        dtype = dtype == -2 || dtype == tensors[i].dtype ? tensors[i].dtype : -1;
+        first = std::min(first, at);
+        end = std::max(end, at + ((ctx->lay.K - 1u) * tensors[i].stride + tensors[i].n) * element_size(tensors[i].dtype));
+    }
+    *list = qgx_tensor_list{table, table_bytes, pieces, d, ctx->lay.K, n_tensors, shared ? 1u : 0u, dtype, first, end};
     return QGX_OK;
 }
 
@@ -1005,6 +1014,9 @@ qgx_status qgx_clip_gradients(qgx_ctx* ctx, const qgx_tensor_list* list, int nor
     a.scale = a.partial + (uint64_t)ctx->lay.K * kClipParts;
     a.V = V; a.norms = norms; a.d = ctx->lay.d;
     a.n_pieces = list->n_pieces; a.max_norm = max_norm;
+    a.dtype = list->dtype;
+    const uint64_t v = (uint64_t)reinterpret_cast<uintptr_t>(V);
+    a.apart = V && (v >= list->end || v + (uint64_t)ctx->lay.K * ctx->lay.d * sizeof(float) <= list->first);
     QGX_HIP(ctx, launch_clip(a, ctx->lay.K, norm == QGX_NORM_LINF, ctx->n_simd / 4u, ctx->d_sc, (hipStream_t)stream));
     return QGX_OK;
 }

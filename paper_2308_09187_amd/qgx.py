@@ -65,7 +65,7 @@ class _Tensor(C.Structure):
 
 class _TensorList(C.Structure):
     _fields_ = [("table", C.c_void_p), ("table_bytes", C.c_uint64), ("n_pieces", C.c_uint64), ("d", C.c_uint64), ("K", C.c_uint32),
-                ("n_tensors", C.c_uint32), ("shared_rows", C.c_uint32)]
+                ("n_tensors", C.c_uint32), ("shared_rows", C.c_uint32), ("dtype", C.c_int32), ("first", C.c_uint64), ("end", C.c_uint64)]
 
 
 class _Buckets(C.Structure):

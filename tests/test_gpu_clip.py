@@ -195,6 +195,38 @@ def test_workers_that_share_a_gradient(qgx):
     ctx.close()
 
 
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("kind", ["l2", "linf"])
+@pytest.mark.parametrize("sizes", [[5 * 4096], [20000, 3], [30, 7, 4096, 1, 9, 4097, 2], [8 * 4096 + 1], [65536], [4096] * 16, [5] * 17])
+def test_some_pieces(qgx, sizes, kind, typ):
+    K = 3
+    tensors, offsets, d = make(sizes, K, [TYPES[typ]])
+    c = qgx.Context(d, K, 256)
+    lst, fill = c.tensor_list(tensors, offsets), np.full((K, d), 7.0)
+    norms, _, _ = want(tensors, offsets, d, np.inf, kind, fill)
+    limit = float(np.float32(np.median(norms) * 0.9))
+    norms, _, exact = want(tensors, offsets, d, limit, kind, fill)
+    V = torch.full((K, d), 7.0, device="cuda")
+    close(c.clip_gradients(lst, limit, norm=qgx.NORM_L2 if kind == "l2" else qgx.NORM_LINF, out=V).cpu().numpy(), norms, 2.0 ** -23)
+    close(V.cpu().numpy(), exact, 2.0 ** -22)
+    c.close()
+
+
+@pytest.mark.parametrize("shift", [0, 40960])
+def test_v_in_the_memory_of_its_tensors(qgx, shift):
+    """A tensor that lies where V has it, of as many pieces as a workgroup reads for itself elsewhere."""
+    K, n = 2, 40960
+    d = n + shift
+    c = qgx.Context(d, K, 256)
+    V = torch.from_numpy(np.random.default_rng(1).standard_normal((K, d)).astype(np.float32)).cuda()
+    tensors, offsets = [V[:, shift:]], [shift]
+    norms, _, exact = want(tensors, offsets, d, 2.0, "l2", V.double().cpu().numpy())
+    lst = c.tensor_list(tensors, offsets)
+    close(c.clip_gradients(lst, 2.0, out=V).cpu().numpy(), norms, 2.0 ** -23)
+    close(V.cpu().numpy(), exact, 2.0 ** -22)
+    c.close()
+
+
 def test_offsets_beyond_32_bits(qgx):
     K, n, far = 2, 50001, (1 << 32) + 24                     # workers' tensors four thousand million elements apart
     memory = torch.empty(far + (1 << 20), device="cuda", dtype=torch.bfloat16)
