@@ -368,15 +368,15 @@ __device__ __forceinline__ nt_u32x4 last_elements(nt_u32x4 x, int n)
 }
 
 // A square as loaded: the rows that it has (none where there is no square), and its keys' number.
-template <typename T> struct Square {
-    nt_u32x4 row[kPiece<T>];
+template <int ROWS> struct Square {
+    nt_u32x4 row[ROWS];
     int rows, keys;
 };
 
 constexpr int kShort = 16;                                 // diagonals of an interval that a lane adds up
 
-// NARROW: fewer keys than a piece has elements.
-template <typename T, int BAND, bool NARROW>
+// ROWS: W, or 1 where there is one query (64 x 16 x 1 x 32768 bfloat16 51 us with W, 23).  NARROW: fewer keys than a piece has elements.
+template <typename T, int BAND, int ROWS, bool NARROW>
 __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a, BucketArgs b, BiasBackPlan plan, float* __restrict__ partial)
 {
     constexpr int W = kPiece<T>, E = 2 * W - 1, kSpan = BAND * W + W, kGroups = kBiasThreads / BAND;
@@ -418,40 +418,40 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a,
         // Two squares' loads are under way at a time (64 x 16 x 197 x 197 bfloat16 39 us with one, 28; 8 x 16 x 1024 x 1024 53 either way).
         // Every lane loads W pieces whether it has a square or not (a neighbour's then), for a wait for the square before has to know how
         // many loads came after it.
-        auto load = [&](Square<T>& x) {
+        auto load = [&](Square<ROWS>& x) {
             const int64_t jb = (int64_t)at.s0 + s + D;     // the square's keys
             const bool any = n < a.batch && D <= D1 && jb >= 0 && jb < k_steps;
             const uint32_t i0 = ((uint32_t)at.s0 + s) * W, j0 = (uint32_t)max((int64_t)0, min(jb - max(D - D1, (int64_t)0), (int64_t)k_steps - 1)) * W;
             const T* in = base + min(n, a.batch - 1u) * a.i_batch + i0 * a.i_row;
-            x.rows = any ? (int)min((uint32_t)W, a.q - i0) : 0;
+            x.rows = any ? (int)min((uint32_t)ROWS, a.q - i0) : 0;
             x.keys = (int)min((uint32_t)W, a.k - j0);
             if constexpr (NARROW) {
 #pragma unroll
-                for (int r = 0; r < W; ++r)
+                for (int r = 0; r < ROWS; ++r)
                     x.row[r] = __builtin_bit_cast(nt_u32x4, load_raw(in + min((uint32_t)r, a.q - 1u - i0) * a.i_row, x.keys));
             } else {
                 in += j0 - (uint32_t)(W - x.keys);         // (moved back to end with its row)
-                if (__ballot(i0 + W > a.q) == 0) {
+                if (__ballot(i0 + ROWS > a.q) == 0) {
 #pragma unroll
-                    for (int r = 0; r < W; ++r) x.row[r] = load_bits(in + (uint32_t)r * a.i_row);
+                    for (int r = 0; r < ROWS; ++r) x.row[r] = load_bits(in + (uint32_t)r * a.i_row);
                 } else {
 #pragma unroll
-                    for (int r = 0; r < W; ++r) x.row[r] = load_bits(in + min((uint32_t)r, a.q - 1u - i0) * a.i_row);
+                    for (int r = 0; r < ROWS; ++r) x.row[r] = load_bits(in + min((uint32_t)r, a.q - 1u - i0) * a.i_row);
                 }
             }
             n += hop_n;
             s += hop_s;
             if (s >= steps) { s -= steps; ++n; }
         };
-        auto add = [&](Square<T>& x) {
-            if (__ballot(x.rows < W || x.keys < W) != 0)
+        auto add = [&](Square<ROWS>& x) {
+            if (__ballot(x.rows < ROWS || x.keys < W) != 0)
 #pragma unroll
-                for (int r = 0; r < W; ++r) {
+                for (int r = 0; r < ROWS; ++r) {
                     if (!NARROW) x.row[r] = last_elements<T>(x.row[r], x.keys);
                     if (r >= x.rows) x.row[r] = nt_u32x4{0u, 0u, 0u, 0u};
                 }
 #pragma unroll
-            for (int r = 0; r < W; ++r) {
+            for (int r = 0; r < ROWS; ++r) {
                 float v[W];
                 values_of<T>(x.row[r], v);
 #pragma unroll
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a,
         const uint64_t before = (uint64_t)split * kGroups;
         uint64_t turns = items > before ? (items - before + hop - 1u) / hop : 0u;
         if (turns) {
-            Square<T> even, odd;
+            Square<ROWS> even, odd;
             load(even);
             for (;; turns -= 2u) {
                 if (turns == 1u) { add(even); break; }
@@ -603,9 +603,12 @@ template <typename T>
 static hipError_t launch_bias_back_of(const BiasArgs& a, const BucketArgs& b, const BiasBackPlan& p, float* partial, hipStream_t st)
 {
     const dim3 grid(p.blocks, min(p.pairs, 65535u));
-    if (a.k < (uint32_t)kPiece<T>) hipLaunchKernelGGL((k_position_bias_back<T, 16, true>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
-    else if (p.band == 64u) hipLaunchKernelGGL((k_position_bias_back<T, 64, false>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
-    else hipLaunchKernelGGL((k_position_bias_back<T, 16, false>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
+    constexpr int W = kPiece<T>;
+    if (a.k < (uint32_t)W) hipLaunchKernelGGL((k_position_bias_back<T, 16, W, true>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
+    else if (a.q == 1u && p.band == 64u) hipLaunchKernelGGL((k_position_bias_back<T, 64, 1, false>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
+    else if (a.q == 1u) hipLaunchKernelGGL((k_position_bias_back<T, 16, 1, false>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
+    else if (p.band == 64u) hipLaunchKernelGGL((k_position_bias_back<T, 64, W, false>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
+    else hipLaunchKernelGGL((k_position_bias_back<T, 16, W, false>), grid, dim3(kBiasThreads), 0, st, a, b, p, partial);
     return hipGetLastError();
 }
 
