@@ -154,43 +154,90 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm(NormArgs a)
     }
 }
 
+// Rows too long for registers, or (SHORT) shorter than a piece: read three times, twice from the cache.  All threads take as many turns, four
+// turns' loads under way at once (300 x 50001 bfloat16 106 us where every turn asked for its columns first, 36; 2 x 3000 x 33000 binary32
+// 579 and 404).
+template <typename T, int THREADS, bool SHORT>
+__device__ __forceinline__ void long_piece(const T* row, PieceAt at, int cols, float (&v)[kPiece<T>])
+{
+    if constexpr (SHORT) load_piece(row + at.c, at.any ? cols - at.c : 0, v);
+    else load_piece(row + at.c, v);
+}
 
-// Rows too long for registers, or shorter than a piece, with any ends: read three times, twice from the cache.
-template <typename T, int THREADS>
+template <int W, int THREADS, bool SHORT>
+__device__ __forceinline__ PieceAt long_piece_at(int turn, int cols)
+{
+    if constexpr (SHORT) return PieceAt{(int)threadIdx.x * W, 0, (int)threadIdx.x * W < cols};
+    else return piece_at<W, THREADS>((int)threadIdx.x, turn, cols);
+}
+
+// A thread's own columns of a piece; where it has been moved back the others may have been written already, from what was there.
+template <typename T, bool SHORT>
+__device__ __forceinline__ void store_own(T* row, PieceAt at, int cols, const float (&v)[kPiece<T>])
+{
+    if (!at.any) return;
+    if constexpr (SHORT) {
+        store_piece(row + at.c, cols - at.c, v);
+    } else if (at.shift == 0) {
+        store_piece(row + at.c, v);
+    } else {
+#pragma unroll
+        for (int c = 0; c < kPiece<T>; ++c)
+            if (at.owns(c)) row[at.c + c] = (T)v[c];
+    }
+}
+
+template <int W, bool SHORT>
+__device__ __forceinline__ void long_parameters(const float* p, PieceAt at, int cols, float none, float (&v)[W])
+{
+    if constexpr (SHORT) load_parameters<W>(p, at.c, cols, none, v);
+    else load_parameters<W>(p, at.c, none, v);
+}
+
+template <typename T, int THREADS, bool SHORT>
 __global__ __launch_bounds__(THREADS) void k_layer_norm_long(NormArgs a)
 {
     constexpr int W = kPiece<T>;
     __shared__ float s_sum[2][1][kNormSlots];
-    const int cols = (int)a.cols;
+    const int cols = (int)a.cols, turns = (cols + THREADS * W - 1) / (THREADS * W);
     for (uint32_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
         const uint32_t k = row / a.rows, r = row % a.rows;
         const T* x = (const T*)a.x + k * a.x_worker + r * a.x_row;
         T* y = (T*)a.y + k * a.y_worker + r * a.y_row;
         float sum[1] = {0.0f}, sq[1] = {0.0f};
-        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += THREADS * W) {
+#pragma unroll 4
+        for (int j = 0; j < turns; ++j) {
+            const PieceAt at = long_piece_at<W, THREADS, SHORT>(j, cols);
             float v[W];
-            load_piece(x + c0, cols - c0, v);
+            long_piece<T, THREADS, SHORT>(x, at, cols, v);
 #pragma unroll
-            for (int c = 0; c < W; ++c) sum[0] += v[c];
+            for (int c = 0; c < W; ++c) sum[0] += at.owns(c) ? v[c] : 0.0f;
         }
         row_sums<THREADS>(sum, s_sum[0]);
         const float mean = sum[0] / (float)cols;
-        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += THREADS * W) {
+#pragma unroll 4
+        for (int j = 0; j < turns; ++j) {
+            const PieceAt at = long_piece_at<W, THREADS, SHORT>(j, cols);
             float v[W];
-            load_piece(x + c0, cols - c0, v);
+            long_piece<T, THREADS, SHORT>(x, at, cols, v);
 #pragma unroll
-            for (int c = 0; c < W; ++c) sq[0] += c0 + c < cols ? (v[c] - mean) * (v[c] - mean) : 0.0f;
+            for (int c = 0; c < W; ++c) {
+                const float t = at.owns(c) && (!SHORT || at.c + c < cols) ? v[c] - mean : 0.0f;
+                sq[0] = fmaf(t, t, sq[0]);
+            }
         }
         row_sums<THREADS>(sq, s_sum[1]);
         const float rstd = 1.0f / sqrtf(sq[0] / (float)cols + a.eps);
-        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += THREADS * W) {
+#pragma unroll 4
+        for (int j = 0; j < turns; ++j) {
+            const PieceAt at = long_piece_at<W, THREADS, SHORT>(j, cols);
             float v[W], w[W], b[W];
-            load_piece(x + c0, cols - c0, v);
-            load_parameters<W>(a.w, c0, cols, 1.0f, w);
-            load_parameters<W>(a.b, c0, cols, 0.0f, b);
+            long_piece<T, THREADS, SHORT>(x, at, cols, v);
+            long_parameters<W, SHORT>(a.w, at, cols, 1.0f, w);
+            long_parameters<W, SHORT>(a.b, at, cols, 0.0f, b);
 #pragma unroll
             for (int c = 0; c < W; ++c) v[c] = fmaf((v[c] - mean) * rstd, w[c], b[c]);
-            store_piece(y + c0, cols - c0, v);
+            store_own<T, SHORT>(y, at, cols, v);
         }
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -393,13 +440,14 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
     }
 }
 
-// Rows too long for registers, or shorter than a piece: dx by itself, dy and x read a second time from the cache.
-template <typename T, int THREADS>
+// Rows too long for registers, or (SHORT) shorter than a piece: dx by itself, dy and x read a second time from the cache (all three
+// gradients of 2 x 1024 x 32768 bfloat16, 402 MB: 310 us where every turn asked for its columns first, 159).
+template <typename T, int THREADS, bool SHORT>
 __global__ __launch_bounds__(THREADS) void k_layer_norm_dx_long(NormBackArgs a)
 {
     constexpr int W = kPiece<T>;
     __shared__ float s_sum[2][2][kNormSlots];
-    const int cols = (int)a.cols;
+    const int cols = (int)a.cols, turns = (cols + THREADS * W - 1) / (THREADS * W);
     int turn = 0;
     for (uint32_t row = blockIdx.x; row < a.n_rows; row += gridDim.x, turn ^= 1) {
         const uint32_t k = row / a.rows, r = row % a.rows;
@@ -408,28 +456,32 @@ __global__ __launch_bounds__(THREADS) void k_layer_norm_dx_long(NormBackArgs a)
         T* dx = (T*)a.dx + k * a.dx_worker + r * a.dx_row;
         const float mean = a.mean[row], rstd = a.rstd[row];
         float sum[2] = {0.0f, 0.0f};
-        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += THREADS * W) {
+#pragma unroll 2
+        for (int j = 0; j < turns; ++j) {
+            const PieceAt at = long_piece_at<W, THREADS, SHORT>(j, cols);
             float u[W], v[W], w[W];
-            load_piece(x + c0, cols - c0, u);
-            load_piece(dy + c0, cols - c0, v);
-            load_parameters<W>(a.w, c0, cols, 1.0f, w);
+            long_piece<T, THREADS, SHORT>(x, at, cols, u);
+            long_piece<T, THREADS, SHORT>(dy, at, cols, v);
+            long_parameters<W, SHORT>(a.w, at, cols, 1.0f, w);
 #pragma unroll
             for (int c = 0; c < W; ++c) {
-                const float g = v[c] * w[c];
+                const float g = at.owns(c) ? v[c] * w[c] : 0.0f;       // (past the end of a short row: v is 0)
                 sum[0] += g;
                 sum[1] = fmaf(g, (u[c] - mean) * rstd, sum[1]);
             }
         }
         row_sums<THREADS>(sum, s_sum[turn]);
         const float m1 = sum[0] / (float)cols, m2 = sum[1] / (float)cols;
-        for (int c0 = (int)threadIdx.x * W; c0 < cols; c0 += THREADS * W) {
+#pragma unroll 2
+        for (int j = 0; j < turns; ++j) {
+            const PieceAt at = long_piece_at<W, THREADS, SHORT>(j, cols);
             float u[W], v[W], w[W];
-            load_piece(x + c0, cols - c0, u);
-            load_piece(dy + c0, cols - c0, v);
-            load_parameters<W>(a.w, c0, cols, 1.0f, w);
+            long_piece<T, THREADS, SHORT>(x, at, cols, u);
+            long_piece<T, THREADS, SHORT>(dy, at, cols, v);
+            long_parameters<W, SHORT>(a.w, at, cols, 1.0f, w);
 #pragma unroll
             for (int c = 0; c < W; ++c) v[c] = rstd * (v[c] * w[c] - m1 - (u[c] - mean) * rstd * m2);
-            store_piece(dx + c0, cols - c0, v);
+            store_own<T, SHORT>(dx, at, cols, v);
         }
     }
 }
@@ -530,7 +582,7 @@ static hipError_t launch_norm_of(const NormArgs& a, uint32_t n_cu, hipStream_t s
 {
     const uint32_t pieces = (a.cols + kPiece<T> - 1u) / kPiece<T>;
     if (a.cols < (uint32_t)kPiece<T>) {
-        hipLaunchKernelGGL((k_layer_norm_long<T, 64>), dim3(min(a.n_rows, kNormBlocksMax)), dim3(64), 0, st, a);
+        hipLaunchKernelGGL((k_layer_norm_long<T, 64, true>), dim3(min(a.n_rows, kNormBlocksMax)), dim3(64), 0, st, a);
         return hipGetLastError();
     }
     if (pieces <= 4u) return launch_norm_by_rows<T, 4, 1>(a, n_cu, st);
@@ -547,7 +599,7 @@ static hipError_t launch_norm_of(const NormArgs& a, uint32_t n_cu, hipStream_t s
     if (pieces <= 1536u) return launch_norm_as<T, 512, 3, 1>(a, st);
     if (pieces <= 2048u) return launch_norm_as<T, 512, 4, 1>(a, st);
     if (pieces <= 4096u) return launch_norm_as<T, 1024, 4, 1>(a, st);
-    hipLaunchKernelGGL((k_layer_norm_long<T, 1024>), dim3(min(a.n_rows, kNormBlocksMax)), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL((k_layer_norm_long<T, 1024, false>), dim3(min(a.n_rows, kNormBlocksMax)), dim3(1024), 0, st, a);
     return hipGetLastError();
 }
 
@@ -624,8 +676,8 @@ static hipError_t launch_back_of(const NormBackArgs& a, uint32_t workers, hipStr
     if (s.lanes == 1024u) return launch_back_as<T, 1024, 2, 1>(a, workers, st);
     if (a.dx && a.n_rows) {
         const dim3 grid(min(a.n_rows, kNormBlocksMax));
-        if (a.cols < (uint32_t)kPiece<T>) hipLaunchKernelGGL((k_layer_norm_dx_long<T, 64>), grid, dim3(64), 0, st, a);
-        else hipLaunchKernelGGL((k_layer_norm_dx_long<T, 1024>), grid, dim3(1024), 0, st, a);
+        if (a.cols < (uint32_t)kPiece<T>) hipLaunchKernelGGL((k_layer_norm_dx_long<T, 64, true>), grid, dim3(64), 0, st, a);
+        else hipLaunchKernelGGL((k_layer_norm_dx_long<T, 1024, false>), grid, dim3(1024), 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

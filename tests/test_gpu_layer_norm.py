@@ -100,6 +100,16 @@ def test_forward_rows_strides_and_in_place(ctx, rows, typ):
     assert torch.equal(wide[:, :, :3], keep[:, :, :3]) and torch.equal(wide[:, :, 3 + cols:], keep[:, :, 3 + cols:])
 
 
+@pytest.mark.parametrize("typ", list(TYPES))
+@pytest.mark.parametrize("cols", [3, 1001, 16390, 32769, 50001])
+def test_in_place_of_any_length(ctx, cols, typ):
+    x, w, b = put(rnd((5, cols), 2, 3, cols + 3), typ), put(rnd(6, cols), "f32"), put(rnd(7, cols), "f32")
+    view = x[..., 2:2 + cols]
+    keep, want = x.clone(), ctx.layer_norm(view, w, b)[0]
+    ctx.layer_norm(view, w, b, out=view)
+    assert torch.equal(view, want) and torch.equal(x[..., :2], keep[..., :2]) and torch.equal(x[..., 2 + cols:], keep[..., 2 + cols:])
+
+
 def test_one_token(ctx):
     x = put(rnd(1, 1000), "bf16")
     w, b = put(rnd(2, 1000), "f32"), put(rnd(3, 1000), "f32")
