@@ -364,7 +364,8 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
             rstd[q] = next_rstd[q];
         }
         if (kAhead && set + a.parts < sets) load(set + a.parts);     // (the same for the whole workgroup)
-        // With t = x - mean: sums of g and g t, dw += dy t rstd, db += dy
+        // With h = (x - mean) rstd: sums of g and g h, dw += dy h, db += dy.  (rstd stands beside x - mean wherever it is multiplied: of a row
+        // with hardly any spread rstd^2, and of others g (x - mean), lie outside binary32 where the gradients do not.)
 #pragma unroll
         for (int q = 0; q < R; ++q) {
             sum[q] = sum[R + q] = 0.0f;
@@ -375,10 +376,10 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
                 values_of<T>(dy[q][j], v);
 #pragma unroll
                 for (int c = 0; c < W; ++c) {
-                    const float d = v[c], t = u[c] - mean[q], g = at[j].owns(c) ? d * w[j][c] : 0.0f;
+                    const float d = v[c], h = (u[c] - mean[q]) * rstd[q], g = at[j].owns(c) ? d * w[j][c] : 0.0f;
                     sum[q] += g;
-                    sum[R + q] = fmaf(g, t, sum[R + q]);
-                    dw[j][c] = fmaf(d, t * rstd[q], dw[j][c]);
+                    sum[R + q] = fmaf(g, h, sum[R + q]);
+                    dw[j][c] = fmaf(d, h, dw[j][c]);
                     db[j][c] += d;
                 }
                 // (added here and now: left to the end of the round, the terms would be kept across the sums)
@@ -388,10 +389,10 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
         }
         if (!a.dx) continue;
         row_sums<LANES>(sum, s_sum[turn]);                 // (two sets of slots in turn: one barrier a round)
-        // dx = rstd (g - mean g - h mean(g h)) = dy (rstd w) - (t rstd^2 mean(g h) + rstd mean g)
+        // dx = rstd (g - mean g - h mean(g h))
 #pragma unroll
         for (int q = 0; q < R; ++q) {
-            const float minus_m1 = -rstd[q] * (sum[q] / (float)cols), minus_m2 = -rstd[q] * rstd[q] * (rstd[q] * (sum[R + q] / (float)cols));
+            const float minus_m1 = -(sum[q] / (float)cols), minus_m2 = -(sum[R + q] / (float)cols);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 // (worked out again from what was loaded: kept across the sums, the values would take twice its registers)
@@ -400,7 +401,7 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
                 values_of<T>(x[q][j], u);
                 values_of<T>(dy[q][j], out);
 #pragma unroll
-                for (int c = 0; c < W; ++c) out[c] = fmaf(out[c], rstd[q] * w[j][c], fmaf(u[c] - mean[q], minus_m2, minus_m1));
+                for (int c = 0; c < W; ++c) out[c] = rstd[q] * fmaf((u[c] - mean[q]) * rstd[q], minus_m2, fmaf(out[c], w[j][c], minus_m1));
                 if (at[j].any && first + q < a.rows) stream_piece((T*)a.dx + k * a.dx_worker + (first + q) * a.dx_row + at[j].c, out);
             }
         }
