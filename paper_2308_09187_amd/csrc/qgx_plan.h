@@ -226,4 +226,17 @@ inline bool eight_waves(uint32_t n_tasks, uint32_t workers, uint32_t n_simd, uin
     return workers >= 8u && n_tasks <= (longer ? n_simd / 8u * 3u : n_simd / 4u);
 }
 
+// ---- a bucket of relative positions within a band of diagonals -------------------------------------------------------------
+// The part of the interval bound .. stop that lies in first .. first + span: its first place there, counted from `first`, and how many
+// it has, 0 where there is none.  An interval's ends may be any 32-bit numbers, further from `first` than 32 bits hold, so both are brought
+// into the band before anything is subtracted; first and first + span are a diagonal's own (within +-(2^30 + 2^29 + 2^10)).
+struct BandPart { int at, n; };
+
+QGX_PLAN BandPart band_part(int bound, int stop, int first, int span)
+{
+    const int end = first + span;
+    const int x0 = bound < first ? first : bound < end ? bound : end, x1 = stop < first ? first : stop < end ? stop : end;
+    return BandPart{x0 - first, x1 > x0 ? x1 - x0 : 0};
+}
+
 }  // namespace qgx

@@ -7,6 +7,7 @@
 // Both are bound by memory.  8 x 16 x 1024 x 1024 bfloat16: forward, 537 MB, 82 us, 6.5 TB/s (95 with its memory out of the cache);
 // gradient, 268 MB, 53 us, 5.1 TB/s; 64 x 16 x 197 x 197 28 us, 2.8 TB/s.
 #include "qgx_types.h"
+#include "qgx_plan.h"
 
 namespace qgx {
 
@@ -515,7 +516,8 @@ __global__ __launch_bounds__(kBiasThreads) void k_position_bias_back(BiasArgs a,
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int bound = half ? interval.bound1 : interval.bound0, stop = half ? interval.end1 : interval.end0;
-            const int y0 = max(bound, first) - first, n = (half ? interval.is1 : interval.is0) ? min(stop, first + kSpan) - first - y0 : 0;
+            const BandPart part = band_part(bound, stop, first, kSpan);
+            const int y0 = part.at, n = (half ? interval.is1 : interval.is0) ? part.n : 0;
             if (wave == half && n <= kShort) {
                 float z = 0.0f;
 #pragma unroll
