@@ -1,4 +1,4 @@
-"""The position bias and its gradient where bounds and offsets lie at the ends of their ranges.  The gradient is compared exactly:
+"""The position bias and its gradient where bounds and offsets lie at the ends of their ranges, and the gradient of large squares, exactly:
 its inputs are 0, 1, 2 or 3 and no table row takes more than 2^22 of them, so that every partial sum is a whole number below 2^24 and the result
 has to be equal, in whatever order it was summed."""
 import numpy as np
@@ -6,7 +6,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from test_gpu_position_bias import TYPES, ctx, host, put, qgx  # noqa: E402, F401
+from test_gpu_position_bias import BUCKETS, TYPES, ctx, host, put, qgx  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 FAR, LOW, HIGH = 1 << 30, -(1 << 31), (1 << 31) - 1
@@ -66,3 +66,12 @@ def test_forward_of_far_ranges(ctx, qgx, q, k, name, typ):  # noqa: F811
     row = rows_of(bounds, rows, q, k, p)
     bias = np.moveaxis(np.where(row[..., None] >= 0, host(table)[np.maximum(row, 0)], -np.inf), -1, 0)
     assert np.array_equal(host(out), host(scores) + bias)      # (small whole numbers: exact in every type)
+
+
+@pytest.mark.parametrize("typ", list(TYPES))
+@pytest.mark.parametrize("name", list(BUCKETS))
+@pytest.mark.parametrize("K,N,heads,q,k", [(1, 1, 1, 2000, 2000), (2, 3, 3, 197, 197), (3, 9, 2, 130, 140), (1, 40, 5, 31, 17), (1, 2, 1, 1, 20000),
+                                           (1, 1, 2, 9000, 9), (1, 1, 1, 700, 5000), (2, 2, 2, 1019, 1019), (1, 6, 1, 5, 900), (1, 3, 2, 1000, 3)])
+def test_gradient_exactly(ctx, qgx, K, N, heads, q, k, name, typ):  # noqa: F811
+    bounds, rows, R = BUCKETS[name]
+    check_gradient(ctx, qgx, bounds, rows, R, 0, K, N, heads, q, k, typ)
