@@ -354,6 +354,8 @@ typedef struct {
     int32_t dtype;    /* qgx_dtype */
 } qgx_tensor;
 
+#define QGX_FEW_TENSORS 16
+
 /* A list of them on the device, made by qgx_tensor_list_set in memory of the caller's.  It serves one stream at a time:
  * the table holds the clipping's partial sums as well.  The fields are the library's. */
 typedef struct {
@@ -364,8 +366,9 @@ typedef struct {
     uint32_t K;
     uint32_t n_tensors;
     uint32_t shared_rows; /* workers share elements of a tensor (stride < n): not to be written */
-    int32_t dtype;        /* the tensors' type, -1: several */
-    uint64_t first, end;  /* addresses between which all elements lie */
+    int32_t dtype;        /* the tensors' type; -1: several, -2: none has elements */
+    uint32_t n_few;       /* tensors with elements, where all are cut into at most QGX_FEW_TENSORS runs; else 0 */
+    struct { uint64_t at, step, bytes; } few[QGX_FEW_TENSORS];   /* where each lies: worker 0's address, bytes from worker to worker, of one */
 } qgx_tensor_list;
 
 /* Bytes a table of these tensors needs.  Host-side only. */
@@ -376,7 +379,7 @@ qgx_status qgx_tensor_list_set(qgx_ctx* ctx, const qgx_tensor* tensors /* HOST *
                                uint64_t table_bytes, qgx_tensor_list* list, void* stream);
 
 /* Worker k's global gradient norm over all tensors of the list, N_k = ||(all its elements)||_2 (QGX_NORM_L2, squares
- * summed in binary64 in a fixed order) or its largest magnitude (QGX_NORM_LINF), and clipping: every element is
+ * summed in binary64, in an order fixed by the tensors' sizes and types, the device, and whether what is written is their memory) or its largest magnitude (QGX_NORM_LINF), and clipping: every element is
  * multiplied by max_norm / N_k (in binary64, rounded to binary32) where N_k > max_norm, and is passed on unchanged where it is
  * not, or where N_k is no finite number (then QGX_EBIT_NONFINITE is set as well, as CODE o Q would).
  *   V      DEVICE [K][d]: tensors are gathered into it as binary32 (coordinates that belong to no tensor stay as they

@@ -2,7 +2,8 @@
 //   N_k = (sum over tensors and elements x^2)^(1/2), or max |x|;   c_k = N_k > M ? M / N_k : 1;   V[k][offset + i] = c_k x_i
 // A launch that reads everything once and leaves a sum per workgroup, one workgroup per worker that adds those up and leaves the
 // factor, and a launch that scales; where a worker's sums are few every scaling wave adds them up itself, and where its pieces are few one
-// launch does it all, each workgroup for itself.  Which it is, and the order of all sums, follows from the sizes and the device.
+// launch does it all, each workgroup for itself.  Which it is, and with it the order of all sums, follows from the sizes, the types, the device
+// and whether what is written is memory of the tensors; not from where they lie otherwise.
 // (The last workgroup to arrive could do it, counting: but an agent-wide release and acquire in every workgroup costs 28 ns, one after
 // the other: 2048 workgroups over 33 MB took 56 us.)  The scaling launch consists of tiny workgroups, a thread moves four elements: reading
 // and writing runs at 6.5 TB/s that way and at 4.5 to 5 with workgroups that go on from tile to tile, where reads wait behind
@@ -323,6 +324,7 @@ __global__ __launch_bounds__(kSmallThreads) void k_clip_small(ClipArgs a, Scalar
 // scaled before another workgroup has read it.)  4 x 65536 binary32 6.3 us a call, 8.0 in two launches; 4 x 32768 5.7 and 8.1; 32 pieces
 // take 13 us.
 constexpr int kAgainPieces = 16;
+static_assert(kAgainPieces <= QGX_FEW_TENSORS, "their places are known");
 
 template <typename T, bool MAX, int PIECES>
 __global__ __launch_bounds__(kSmallThreads) void k_clip_again(ClipArgs a, Scalars* sc)

@@ -281,7 +281,7 @@ struct ClipArgs {
     uint64_t d;
     uint32_t parts;             // workgroups that sum a worker's pieces
     float max_norm;
-    bool apart;                 // V shares no memory with the tensors
+    bool apart;                 // V shares no memory with the tensors, of which there are few
     int32_t dtype;              // of all tensors, -1: not of all
 };
 hipError_t launch_tensor_list(const TensorBatch& batch, TensorPiece* table, hipStream_t st);

@@ -983,17 +983,34 @@ qgx_status qgx_tensor_list_set(qgx_ctx* ctx, const qgx_tensor* tensors, uint32_t
         batch.pieces = 0;
         batch.count = 0;
     }
-    uint64_t first = ~0ull, end = 0;
-    int32_t dtype = -2;                                    // (none yet)
+    *list = qgx_tensor_list{};
+    list->table = table; list->table_bytes = table_bytes; list->n_pieces = pieces;
+    list->d = d; list->K = ctx->lay.K; list->n_tensors = n_tensors;
+    list->shared_rows = shared ? 1u : 0u;
+    list->dtype = -2;                                      // (none yet)
     for (uint32_t i = 0; i < n_tensors; ++i) {
-        if (!tensors[i].n) continue;
-        const uint64_t at = (uint64_t)reinterpret_cast<uintptr_t>(tensors[i].data);
-        dtype = dtype == -2 || dtype == tensors[i].dtype ? tensors[i].dtype : -1;
-        first = std::min(first, at);
-        end = std::max(end, at + ((ctx->lay.K - 1u) * tensors[i].stride + tensors[i].n) * element_size(tensors[i].dtype));
+        const qgx_tensor& t = tensors[i];
+        if (!t.n) continue;
+        list->dtype = list->dtype == -2 || list->dtype == t.dtype ? t.dtype : -1;
+        if (pieces > QGX_FEW_TENSORS) continue;            // (a tensor with elements has a piece at least)
+        const uint64_t size = element_size(t.dtype);
+        list->few[list->n_few].at = (uint64_t)reinterpret_cast<uintptr_t>(t.data);
+        list->few[list->n_few].step = t.stride * size;
+        list->few[list->n_few++].bytes = t.n * size;
     }
-    *list = qgx_tensor_list{table, table_bytes, pieces, d, ctx->lay.K, n_tensors, shared ? 1u : 0u, dtype, first, end};
     return QGX_OK;
+}
+
+// Do some of the bytes from v on belong to one of the few tensors?
+static bool shares_memory(const qgx_tensor_list* list, uint64_t v, uint64_t bytes)
+{
+    for (uint32_t i = 0; i < list->n_few; ++i) {
+        const uint64_t at = list->few[i].at, step = list->few[i].step, n = list->few[i].bytes;
+        // the first worker whose elements end past v, if any
+        const uint64_t k = at + n > v ? 0 : step ? (v - at - n) / step + 1u : list->K;
+        if (k < list->K && at + k * step < v + bytes) return true;
+    }
+    return false;
 }
 
 qgx_status qgx_clip_gradients(qgx_ctx* ctx, const qgx_tensor_list* list, int norm, float max_norm, float* V, float* norms,
@@ -1015,8 +1032,7 @@ qgx_status qgx_clip_gradients(qgx_ctx* ctx, const qgx_tensor_list* list, int nor
     a.V = V; a.norms = norms; a.d = ctx->lay.d;
     a.n_pieces = list->n_pieces; a.max_norm = max_norm;
     a.dtype = list->dtype;
-    const uint64_t v = (uint64_t)reinterpret_cast<uintptr_t>(V);
-    a.apart = V && (v >= list->end || v + (uint64_t)ctx->lay.K * ctx->lay.d * sizeof(float) <= list->first);
+    a.apart = V && list->n_few && !shares_memory(list, (uint64_t)reinterpret_cast<uintptr_t>(V), (uint64_t)ctx->lay.K * ctx->lay.d * sizeof(float));
     QGX_HIP(ctx, launch_clip(a, ctx->lay.K, norm == QGX_NORM_LINF, ctx->n_simd / 4u, ctx->d_sc, (hipStream_t)stream));
     return QGX_OK;
 }

@@ -24,6 +24,7 @@ CODE_ELIAS_OMEGA, CODE_TABLE = 0, 1
 CHUNK, SUB, SUBS, MAX_SYM, MAX_BINS = 4096, 32, 128, 127, 4096
 STATIC_MAX_CHUNKS = 65536
 MAX_INTERVALS = 128
+FEW_TENSORS = 16
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 EXPORTS = [
@@ -65,7 +66,8 @@ class _Tensor(C.Structure):
 
 class _TensorList(C.Structure):
     _fields_ = [("table", C.c_void_p), ("table_bytes", C.c_uint64), ("n_pieces", C.c_uint64), ("d", C.c_uint64), ("K", C.c_uint32),
-                ("n_tensors", C.c_uint32), ("shared_rows", C.c_uint32), ("dtype", C.c_int32), ("first", C.c_uint64), ("end", C.c_uint64)]
+                ("n_tensors", C.c_uint32), ("shared_rows", C.c_uint32), ("dtype", C.c_int32), ("n_few", C.c_uint32),
+                ("few", C.c_uint64 * 3 * FEW_TENSORS)]
 
 
 class _Buckets(C.Structure):
