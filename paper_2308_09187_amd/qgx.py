@@ -164,8 +164,10 @@ class Buckets:
 
     def __init__(self, bounds, rows):
         _need(len(bounds) == len(rows) + 1, "Buckets: one bound more than rows")
-        self._bounds = (C.c_int32 * len(bounds))(*[int(x) for x in bounds])
-        self._rows = (C.c_uint32 * max(1, len(rows)))(*[int(x) for x in rows])
+        bounds, rows = [int(x) for x in bounds], [int(x) for x in rows]
+        _need(all(-(1 << 31) <= x < 1 << 31 for x in bounds) and all(0 <= x < 1 << 32 for x in rows), "Buckets: bounds and rows of 32 bits")
+        self._bounds = (C.c_int32 * len(bounds))(*bounds)
+        self._rows = (C.c_uint32 * max(1, len(rows)))(*rows)
         self._c = _Buckets(len(rows), self._bounds, self._rows)
         self._ref = C.addressof(self._c)
 
@@ -185,7 +187,7 @@ class Buckets:
             while n ** (m - exact) < exact ** (m - exact - t) * far ** t:
                 n += 1
             start.append(n)
-        end = (1 << 30) if window is None else int(window)
+        end = (1 << 30) if window is None else min(int(window), (1 << 31) - 1)       # (no delta is further)
         _need(end >= 1, "Buckets.logarithmic: a window of one key at least")
         start = [n for n in start if n < end]
         bounds, ids = [1 - end], []
@@ -388,7 +390,7 @@ class Context:
             _need(t.is_cuda and t.dtype in DTYPES, "tensor %d: float32, float16 or bfloat16 on the GPU", i)
             _need((t.dim() == 2 and t.shape[0] == self.K) or (t.dim() == 1 and self.K == 1), "tensor %d: shape [K, n]", i)
             _need(_dense_last(t), "tensor %d: a worker's elements must be contiguous", i)
-            _need(int(off) >= 0, "tensor %d: offset below 0", i)
+            _need(0 <= int(off) < 1 << 64, "tensor %d: offset outside the coordinates", i)
             arr[i] = _Tensor(t.data_ptr(), t.shape[-1], t.stride(0) if t.dim() == 2 and self.K > 1 else 0, int(off), DTYPES[t.dtype])
         need, out = C.c_uint64(), _TensorList()
         self._check(self.lib.qgx_tensor_list_size(self._h, arr, C.c_uint32(len(tensors)), C.byref(need)))
@@ -492,6 +494,7 @@ class Context:
 
     def _bias(self, table, buckets, src, out, q_offset, positions, stream):
         o = self._scores(out, "out")
+        _need(abs(q_offset) <= 1 << 30, "q_offset: beyond +-2^30")
         _need(table.dim() == 2 and table.shape[1] == o.heads, "table: [rows, heads]")
         tab = _parameter(table, table.shape, "table")
         pos = None
@@ -523,6 +526,7 @@ class Context:
         """Writes the table's gradient, float32 [workers, rows, heads] (a run of V's rows say; [rows, heads] where grad has
         no worker dimension), from the gradient of the biased scores."""
         g = self._scores(grad, "grad")
+        _need(abs(q_offset) <= 1 << 30, "q_offset: beyond +-2^30")
         sh, step = dtable.shape, dtable.stride()
         _need(dtable.is_cuda and dtable.dtype == torch.float32 and len(sh) == (3 if grad.dim() == 5 else 2) and sh[-1] == g.heads and
               (len(sh) == 2 or sh[0] == g.workers), "dtable: float32 [workers, rows, heads] on the GPU")
