@@ -338,8 +338,8 @@ qgx_status qgx_average_export(qgx_ctx* ctx, float* X_bar, uint64_t* count, void*
 /* ---- Between a model's backward pass and the dual vectors ---------------------------------------------------
  * The calls below are what a trainer does right before CODE o Q: its parameters are runs of the iterate X [d], their
  * gradients runs of the workers' rows of V [K][d].  Tensors hold one of the types qgx_dtype, parameters and their
- * gradients binary32; all arithmetic is in binary32 or more, a result in a narrower type is rounded once, at its
- * store.  Strides count elements; pointers need the alignment of their elements only.  The calls enqueue work and
+ * gradients binary32; all arithmetic is in binary32 or more, a result in a narrower type is rounded at its store (from
+ * binary32, as which the clipping's products in binary64 arrive there too).  Strides count elements; pointers need the alignment of their elements only.  The calls enqueue work and
  * allocate nothing; scratch is the caller's, so that calls on several streams do not meet in it, and its contents
  * need not be kept from one call to the next. */
 typedef enum { QGX_F32 = 0, QGX_F16 = 1, QGX_BF16 = 2 } qgx_dtype;
@@ -384,8 +384,9 @@ qgx_status qgx_tensor_list_set(qgx_ctx* ctx, const qgx_tensor* tensors /* HOST *
  * not, or where N_k is no finite number (then QGX_EBIT_NONFINITE is set as well, as CODE o Q would).
  *   V      DEVICE [K][d]: tensors are gathered into it as binary32 (coordinates that belong to no tensor stay as they
  *          are); it may be the memory of a tensor of the list that lies there as it does in V, and overlaps no other.
- *          NULL: the tensors are clipped in place, rounded to their own types; they may not overlap each other then.
- *   norms  DEVICE [K] binary32 or NULL: the N_k
+ *          NULL: the tensors are clipped in place, from binary32 rounded to their own types; they may not overlap each other then.
+ *   norms  DEVICE [K] binary32 or NULL: the N_k, rounded: infinity, without QGX_EBIT_NONFINITE, where a finite N_k is beyond
+ *          binary32 (the clipping goes by its binary64)
  * max_norm >= 0; infinity only measures (and gathers). */
 qgx_status qgx_clip_gradients(qgx_ctx* ctx, const qgx_tensor_list* list, int norm, float max_norm, float* V,
                               float* norms, void* stream);
