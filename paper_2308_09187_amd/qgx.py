@@ -177,29 +177,31 @@ class Buckets:
         each (0, 1, ..), the others start at m // 2 times equal powers of far / (m // 2), the last of them holding all that is
         further.  both=False: m = rows, keys after the query are masked; both=True: m = rows // 2, and as many rows again,
         m .., for the keys after it, by the same distances.  window: keys that far before (and after) or further are masked.
-        The starts are worked out in whole numbers: exact, whatever the machine's logarithm."""
+        The starts are worked out in whole numbers: exact, whatever the machine's logarithm.  Where several rows start within one
+        distance, the last of them has it and the others have none."""
         m = rows // 2 if both else rows
         exact = m // 2
         _need(m >= 2 and far > exact, "Buckets.logarithmic: two rows a side at least, and far beyond those of one distance each")
         start = list(range(exact))
         for t in range(m - exact):                       # the smallest n with (n / exact)^(m - exact) >= (far / exact)^t
-            n = start[-1] + 1
+            n = start[-1]
             while n ** (m - exact) < exact ** (m - exact - t) * far ** t:
                 n += 1
             start.append(n)
         end = (1 << 30) if window is None else min(int(window), (1 << 31) - 1)       # (no delta is further)
         _need(end >= 1, "Buckets.logarithmic: a window of one key at least")
         start = [n for n in start if n < end]
+        stop = start[1:] + [end]                         # (where powers are less than one apart, rows have no distance)
         bounds, ids = [1 - end], []
         for b in range(len(start) - 1, -1, -1):          # keys before the query, the furthest first
-            ids.append(b)
-            bounds.append(1 - start[b])
+            if start[b] < stop[b]:
+                ids.append(b)
+                bounds.append(1 - start[b])
         if both:
-            for b, n in enumerate(start):
-                stop = start[b + 1] if b + 1 < len(start) else end
-                if stop > 1:                             # (distance 0 is with the keys before)
+            for b in range(len(start)):
+                if max(1, start[b]) < stop[b]:           # (distance 0 is with the keys before)
                     ids.append(m + b)
-                    bounds.append(stop)
+                    bounds.append(stop[b])
         return cls(bounds, ids)
 
 
