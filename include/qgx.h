@@ -339,9 +339,10 @@ qgx_status qgx_average_export(qgx_ctx* ctx, float* X_bar, uint64_t* count, void*
  * The calls below are what a trainer does right before CODE o Q: its parameters are runs of the iterate X [d], their
  * gradients runs of the workers' rows of V [K][d].  Tensors hold one of the types qgx_dtype, parameters and their
  * gradients binary32; all arithmetic is in binary32 or more, a result in a narrower type is rounded at its store (from
- * binary32, as which the clipping's products in binary64 arrive there too).  Strides count elements; pointers need the alignment of their elements only.  The calls enqueue work and
- * allocate nothing; scratch is the caller's, so that calls on several streams do not meet in it, and its contents
- * need not be kept from one call to the next. */
+ * binary32, as which the clipping's products in binary64 arrive there too).  Strides count elements; pointers need the
+ * alignment of their elements only, but for V, tables and scratch: 16 bytes.  The calls enqueue work and allocate
+ * nothing; scratch is the caller's, so that calls on several streams do not meet in it, and its contents need not be
+ * kept from one call to the next. */
 typedef enum { QGX_F32 = 0, QGX_F16 = 1, QGX_BF16 = 2 } qgx_dtype;
 
 /* One gradient tensor of all K workers: worker k's n elements start at data + k * stride and belong at
@@ -448,7 +449,8 @@ qgx_status qgx_position_bias(qgx_ctx* ctx, const qgx_buckets* buckets, const flo
 
 /* Its gradient: dtable_k[r][head] = sum of grad over worker k's batch and all (i, j) whose delta takes row r, binary32 at
  * dtable + k * param_stride ([table_rows][heads], a run of V's rows; written, not added to; 0 for a row that none takes).
- * What masked places hold does not matter.  (The gradient of the scores is grad itself.)  Results repeat bit for bit.
+ * What masked places hold does not matter.  (The gradient of the scores is grad itself.)  All sequences have the same
+ * p = q_offset here: there is no form with positions of their own.  Results repeat bit for bit.
  * scratch: DEVICE, 16-byte aligned, of the bytes qgx_position_bias_scratch reports (0: may be NULL). */
 qgx_status qgx_position_bias_scratch(qgx_ctx* ctx, const qgx_buckets* buckets, const qgx_scores* grad, int64_t q_offset,
                                      uint64_t* bytes);

@@ -1,9 +1,12 @@
 // Layer norm, forward and backward.
 //   h = (x - mean) rstd,  y = h w + b;   g = dy w,  dx = rstd (g - mean(g) - h mean(g h)),  dw = sum_rows dy h,  db = sum_rows dy
 // A row stays in registers between its sums, so that it crosses memory once; LANES threads share it, N pieces of 16 bytes each.
-// Sums are in binary32: runs of at most N pieces one by one, then the threads' in a tree.
-// Both passes are bound by memory.  8 x 4096 x 4096 bfloat16 forward, 537 MB: 84 us, 6.4 TB/s, 97 with its memory out of the cache;
-// backward, 805 MB and the workgroups' sums: 159 us.  8 x 4096 x 2048 backward, 403 MB: 75 us, 5.4 TB/s.
+// Sums are in binary32.  A row's: a thread's columns one by one, at most 32 of them (of rows too long for registers cols / 1024), then the
+// threads' in a tree.  A column's: the rows of a workgroup's group one by one (a worker's rows over its workgroups and their groups), then the
+// groups', and the workgroups' by 64 runs and a tree.
+// Both passes are bound by memory.  8 x 4096 x 4096 bfloat16 forward, 537 MB: 91 us, 5.9 TB/s, with its memory out of the cache, 79 where the last
+// pass's is used again; backward, 805 MB and the workgroups' sums: 158 us, 5.1 TB/s, either way.  8 x 4096 x 2048 backward, 403 MB: 86 to 90 us,
+// 4.5 to 4.7 TB/s, and 75.
 #include "qgx_types.h"
 
 namespace qgx {
@@ -314,7 +317,9 @@ __global__ __launch_bounds__(kNormThreads<LANES>) void k_layer_norm_back(NormBac
     const int lane = (int)(threadIdx.x % LANES), cols = (int)a.cols;
     const uint32_t group = norm_group<LANES>();
     const uint32_t k = blockIdx.y;
-    constexpr bool kAhead = LANES * N < 4096;              // (no registers are left for the next rows of binary32 of more than 8192 columns)
+    // (No registers are left for the next rows of binary32 of more than 8192 columns: the 128 that 1024 threads leave each are 6 too few even so,
+    // which lie in scratch memory.  2 x 1024 x 16384: 97 us, 4.2 TB/s.)
+    constexpr bool kAhead = LANES * N < 4096;
     float w[N][W], dw[N][W], db[N][W];
     PieceAt at[N];
 #pragma unroll
