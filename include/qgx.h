@@ -458,6 +458,109 @@ qgx_status qgx_position_bias_backward(qgx_ctx* ctx, const qgx_buckets* buckets, 
                                       float* dtable, uint32_t table_rows, uint64_t param_stride, void* scratch,
                                       uint64_t scratch_bytes, void* stream);
 
+/* ---- An image or video model's block -------------------------------------------------------------------------------
+ * Group norm, activations kept in 8 bits for the backward pass, the weight gradient from them, rotary positions.  What stands above the
+ * clipping's calls holds for these too: types, strides, alignment, scratch, nothing allocated. */
+
+/* Rows kept in 8 bits.  A row is ceil(cols / QGX_KEPT_BLOCK) blocks of 32 elements (the last one filled up with zeros), row r's codes at
+ * codes + r * 32 * blocks, its powers at powers + r * blocks.  An element is (code - 128) * 2^(power - 127), |code - 128| <= 127: exact in
+ * bfloat16.  power 0: a block of zeros; 255: a block that held an infinity or a NaN, all of whose elements are NaN. */
+#define QGX_KEPT_BLOCK 32u
+typedef struct {
+    uint8_t* codes;        /* DEVICE, 16-byte aligned */
+    uint8_t* powers;       /* DEVICE */
+    uint64_t rows, cols;   /* rows of all workers, < 2^31; 1 <= cols <= 2^24 */
+} qgx_kept;
+
+/* Keeps workers x rows rows of cols elements (row r of worker k at x + k * x_worker + r * x_row, kept as row k * rows + r of `out`).
+ * A block's power of two 2^e is the smallest with every magnitude at most 127 * 2^e (e >= -126; e <= 121, of binary16 9, so that what is
+ * restored to x's type is finite: magnitudes beyond 127 of those are 127 of them).  Rounding of x 2^-e:
+ *   unbiased = 0  to the nearest whole number, ties to even
+ *   unbiased = 1  away from zero with the probability of the remainder, by a draw of 16 bits: element c of row r of the whole takes 16 bits of
+ *                 Philox4x32-10(key = the context's seed, counter = (c / 8, 2, r, call_id)), the low or high half (c odd) of word (c mod 8) / 2,
+ *                 and rounds away iff the draw < remainder * 2^16.  So a product with what was kept has the expectation of the product
+ *                 with x to 2^-16 of a step, as the method asks of its vectors.  call_id as in qgx_quantize (the two special values too).
+ * A block with an infinity or a NaN sets QGX_EBIT_NONFINITE. */
+qgx_status qgx_checkpoint(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, const void* x, uint64_t x_worker,
+                          uint64_t x_row, int unbiased, uint32_t call_id, const qgx_kept* out, void* stream);
+/* The elements, rounded once to dtype: row r at y + r * y_row. */
+qgx_status qgx_restore(qgx_ctx* ctx, const qgx_kept* in, int dtype, void* y, uint64_t y_row, void* stream);
+
+/* The weight gradient of y = x W + b, x [rows][cols] of each worker as it was kept, dy [rows][out]:
+ *   dweight_k[i][o] = sum over worker k's rows of x[r][i] dy[r][o]     binary32 [cols][out] at dweight + k * dw_worker
+ *   dbias_k[o]      = sum of dy[r][o]                                   binary32 [out] at dbias + k * db_worker, or NULL
+ * (runs of the rows of V: both strides d), written, not added to; rows 0: zeros.  Matrix cores: x's elements are exact in bfloat16, dy's the
+ * exact sum of one (bfloat16), two (binary16) or three (binary32) bfloat16 numbers, so that every product is exact (of magnitudes
+ * below 2^-110 a part may be lost); sums are in binary32, in an order the sizes and the device fix.  An infinity or a NaN in dy spoils the
+ * column it stands in, as in the formula.  x->rows = workers * rows.
+ * scratch: DEVICE, 16-byte aligned, of the bytes qgx_weight_gradient_scratch reports (0: may be NULL). */
+qgx_status qgx_weight_gradient_scratch(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, uint64_t out, uint64_t* bytes);
+qgx_status qgx_weight_gradient(qgx_ctx* ctx, const qgx_kept* x, int dtype, uint64_t workers, uint64_t rows, uint64_t out, const void* dy,
+                               uint64_t dy_worker, uint64_t dy_row, float* dweight, uint64_t dw_worker, float* dbias, uint64_t db_worker,
+                               void* scratch, uint64_t scratch_bytes, void* stream);
+
+/* Group norm with an activation, channels last: x [workers][batch][places][channels] (a place's channels are contiguous), in `groups` runs of
+ * channels / groups channels; a group of a sample is all places' channels of a run.
+ *   h = (x - mean) * rstd,  z = h * weight[c] + bias[c],  y = act(z),   rstd = 1 / sqrt(variance + eps)
+ * mean and variance of the group's elements, the variance about the mean (not E x^2 - mean^2). */
+typedef enum { QGX_ACT_NONE = 0, QGX_ACT_SILU = 1, QGX_ACT_LEAKY = 2 } qgx_activation;   /* z; z / (1 + e^-z); z, slope * z where z <= 0 */
+typedef struct {
+    int32_t dtype;         /* qgx_dtype of x, y, dy and dx */
+    int32_t activation;    /* qgx_activation */
+    float slope;           /* of QGX_ACT_LEAKY: finite */
+    uint32_t groups;       /* divides channels */
+    uint64_t workers, batch, places, channels;   /* workers * batch <= 65535, workers * batch * places < 2^31, channels 1 .. 2^20, places * channels < 2^36 */
+} qgx_group_shape;
+typedef struct {
+    void* data;            /* DEVICE */
+    uint64_t s_worker, s_batch, s_place;
+} qgx_places;
+
+/* Bytes of scratch for the calls below (backward: 0 or 1); 0: scratch may be NULL. */
+qgx_status qgx_group_norm_scratch(qgx_ctx* ctx, const qgx_group_shape* shape, int backward, uint64_t* bytes);
+/*   weight, bias  DEVICE [channels] binary32, each or both NULL (1 and 0)
+ *   y             may be x (with its strides)
+ *   mean, rstd    DEVICE [workers][batch][groups] binary32, each or both NULL
+ *   keep          NULL, or where x's rows are kept as well, as qgx_checkpoint does with `unbiased` and `call_id`: row (worker, batch, place) */
+qgx_status qgx_group_norm(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_places* x, const float* weight, const float* bias, float eps,
+                          const qgx_places* y, float* mean, float* rstd, const qgx_kept* keep, int unbiased, uint32_t call_id,
+                          void* scratch, uint64_t scratch_bytes, void* stream);
+/* Its backward pass, from x or, x NULL, from what was kept of it.  dz = dy act'(z), z in binary32 by one subtraction, two products and one
+ * addition as above, each rounded (so that a leaky unit's side is reproducible);  g = dz * weight,
+ *   dx = rstd * (g - mean over the group of g - h * mean over the group of g h)          DEVICE, or NULL; may not be dy or x
+ *   dweight_k[c] = sum over worker k's batch and places of dz h,  dbias_k[c] = sum of dz     DEVICE binary32, each or NULL, worker k's at
+ *                  + k * param_stride (runs of V's rows), written, not added to; zeros where batch or places is 0
+ * The order of the sums is fixed by the sizes and the device.  mean and rstd are the forward pass's. */
+qgx_status qgx_group_norm_backward(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_places* dy, const qgx_places* x, const qgx_kept* kept,
+                                   const float* weight, const float* bias, const float* mean, const float* rstd, const qgx_places* dx,
+                                   float* dweight, float* dbias, uint64_t param_stride, void* scratch, uint64_t scratch_bytes, void* stream);
+
+/* Rotary positions with several axes.  The first 2 * P of a head's dim elements are P pairs, pair p of the first pairs[0] belongs to axis 0, of the
+ * next pairs[1] to axis 1, and so on: (a, b) becomes (a cos t - b sin t, a sin t + b cos t), t = (the token's position along the pair's
+ * axis) * frequencies[p]; the elements after them stay as they are. */
+#define QGX_MAX_AXES 4u
+#define QGX_MAX_PAIRS 256u
+typedef struct {
+    uint32_t axes;                /* 1 .. QGX_MAX_AXES */
+    uint32_t pairs[QGX_MAX_AXES]; /* of each axis; P = their sum, 1 .. QGX_MAX_PAIRS */
+    int32_t neighbours;           /* 1: pair p is elements 2 p, 2 p + 1; 0: p, p + P */
+    const double* frequencies;    /* HOST [P], radians a position, finite */
+} qgx_rotary;
+typedef struct {
+    void* data;                   /* DEVICE; a head's dim elements are contiguous */
+    int32_t dtype;                /* qgx_dtype */
+    uint32_t heads, dim;          /* 1 .. 65535; 2 P .. 4096 */
+    uint64_t workers, batch, tokens;   /* workers * batch * tokens < 2^31 */
+    uint64_t s_worker, s_batch, s_token, s_head;
+} qgx_heads;
+
+/* positions DEVICE int32: of axis a, worker k, sequence n, token t at positions[a * p_axis + k * p_worker + n * p_batch + t] (a stride of 0: the same
+ * for all).  The angle is reduced in binary64 (good to 1e-9 of a turn at any position), sine and cosine are good to 2^-23, products and
+ * sums in binary32, one rounding.  back = 1: by -t, the backward pass (the transposed map, which is its inverse).  out may be in (with its
+ * strides); out's shape is in's. */
+qgx_status qgx_rotate(qgx_ctx* ctx, const qgx_rotary* rotary, const int32_t* positions, uint64_t p_axis, uint64_t p_worker, uint64_t p_batch,
+                      const qgx_heads* in, const qgx_heads* out, int back, void* stream);
+
 /* Returns and clears the device error word (QGX_EBIT_*).  Synchronises `stream`. */
 uint32_t qgx_poll_error(qgx_ctx* ctx, void* stream);
 

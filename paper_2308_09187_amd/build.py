@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqgx.so")
 SOURCES = ["qgx_lib.hip", "qgx_tables.hip", "qgx_encode.hip", "qgx_decode.hip", "qgx_fit.hip", "qgx_game.hip", "qgx_metrics.hip",
-           "qgx_clip.hip", "qgx_layer_norm.hip", "qgx_position_bias.hip"]
+           "qgx_clip.hip", "qgx_layer_norm.hip", "qgx_position_bias.hip", "qgx_checkpoint.hip", "qgx_group_norm.hip",
+           "qgx_weight_gradient.hip", "qgx_rotary.hip"]
 
 # -ffp-contract=off: the rounding decisions are specified as separately rounded binary32 operations.
 # packed-fp32 ops are switched off for the device pass (the host pass warns that it ignores the flag).

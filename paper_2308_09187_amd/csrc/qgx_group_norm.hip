@@ -1,0 +1,893 @@
+// Group norm with an activation, channels last, forward and backward.
+//   h = (x - mean) rstd,  z = h w + b,  y = act(z);   dz = dy act'(z),  g = dz w,  dx = rstd (g - mean(g) - h mean(g h)),
+//   dw = sum dz h,  db = sum dz over a worker's samples and places
+// Bound by memory.  A thread has W neighbouring channels (16 bytes) of every so manieth place, so that whatever belongs to a channel stays in
+// its registers; sums are made channel by channel (a thread's places one by one, then the threads' of a channel) and only then
+// joined to groups, whose borders may lie anywhere in a piece.  Where all places of some groups fit a workgroup's registers it has them whole: one
+// launch, x (and dy) cross memory once.  Else the places are dealt to workgroups that leave their channels' sums in scratch, a launch joins
+// them, and a second pass over x makes y or dx.
+#include "qgx_kept.h"
+#include "qgx_plan.h"
+
+namespace qgx {
+
+// ---- pieces ---------------------------------------------------------------------------------------------------------------
+
+// Where a thread's piece lies: channels c .. c + W - 1 of the sample, of which those before `shift` belong to the piece before (the last piece
+// of a span is moved back to end there).  SHORT: fewer than W channels in all, `n` of them there.
+struct ChannelsAt {
+    int c, shift, n;
+    __device__ __forceinline__ bool owns(int i) const { return i >= shift && i < n; }
+};
+
+template <int W, bool SHORT>
+__device__ __forceinline__ ChannelsAt channels_at(uint32_t j, uint32_t first, uint32_t span)
+{
+    if constexpr (SHORT) return ChannelsAt{(int)first, 0, (int)span};
+    const int c0 = (int)j * W, c = min(c0, (int)span - W);  // (of a last span shorter than a piece: before its first channel)
+    return ChannelsAt{(int)first + c, c0 - c, W};
+}
+
+// A piece as loaded: sixteen bytes, or W codes and the powers of the one or two blocks they lie in.
+template <typename T, bool KEPT> struct RawPiece { nt_u32x4 bits; };
+template <typename T> struct RawPiece<T, true> { uint32_t code[kPiece<T> / 4]; uint32_t powers; };
+
+// A sample's places: base addresses of worker k's sample n.
+template <typename T, bool KEPT>
+struct Places {
+    const T* x;
+    const uint8_t* codes;
+    const uint8_t* powers;
+    uint64_t place, power_place;
+    int cut;                                               // of a kept piece: its first channel in the second block
+};
+
+template <typename T, bool KEPT>
+__device__ __forceinline__ Places<T, KEPT> places_of(const GroupArgs& a, uint32_t sample, uint32_t batch, ChannelsAt at)
+{
+    Places<T, KEPT> p{};
+    const uint32_t k = sample / batch, n = sample % batch;
+    if constexpr (KEPT) {
+        const uint64_t row = (uint64_t)sample * a.places;
+        const int block = at.c / (int)QGX_KEPT_BLOCK;
+        p.codes = a.codes + row * a.code_place + at.c;
+        p.powers = a.powers + row * a.power_place + block;
+        p.place = a.code_place;
+        p.power_place = a.power_place;
+        p.cut = (block + 1) * (int)QGX_KEPT_BLOCK - at.c;
+    } else {
+        p.x = (const T*)a.x + k * a.x_worker + n * a.x_batch + at.c;
+        p.place = a.x_place;
+    }
+    return p;
+}
+
+template <typename T>
+__device__ __forceinline__ Places<T, false> gradients_of(const GroupArgs& a, uint32_t sample, uint32_t batch, ChannelsAt at)
+{
+    Places<T, false> p{};
+    p.x = (const T*)a.dy + sample / batch * a.dy_worker + sample % batch * a.dy_batch + at.c;
+    p.place = a.dy_place;
+    return p;
+}
+
+template <typename T, bool KEPT, bool SHORT>
+__device__ __forceinline__ RawPiece<T, KEPT> load_place(const Places<T, KEPT>& p, uint32_t place, int n)
+{
+    constexpr int W = kPiece<T>;
+    RawPiece<T, KEPT> raw;
+    if constexpr (KEPT) {
+        typedef uint32_t Words __attribute__((ext_vector_type(W / 4), aligned(1)));
+        const Words w = *reinterpret_cast<const Words*>(p.codes + place * p.place);      // (a row is filled up to 32 codes)
+#pragma unroll
+        for (int i = 0; i < W / 4; ++i) raw.code[i] = w[i];
+        const uint8_t* q = p.powers + place * p.power_place;
+        raw.powers = q[0];
+        if (p.cut < W && p.cut < n) raw.powers |= (uint32_t)q[1] << 8;
+    } else if constexpr (SHORT) {
+        raw.bits = __builtin_bit_cast(nt_u32x4, load_raw(p.x + place * p.place, n));
+    } else {
+        raw.bits = load_bits(p.x + place * p.place);
+    }
+    return raw;
+}
+
+template <typename T, bool KEPT>
+__device__ __forceinline__ RawPiece<T, KEPT> no_place()
+{
+    RawPiece<T, KEPT> raw;
+    if constexpr (KEPT) {
+#pragma unroll
+        for (int i = 0; i < kPiece<T> / 4; ++i) raw.code[i] = 0u;
+        raw.powers = 0u;
+    } else {
+        raw.bits = nt_u32x4{0u, 0u, 0u, 0u};
+    }
+    return raw;
+}
+
+template <typename T, bool KEPT>
+__device__ __forceinline__ void values_at(const RawPiece<T, KEPT>& raw, const Places<T, KEPT>& p, float (&v)[kPiece<T>])
+{
+    if constexpr (KEPT) {
+        const float lo = kept_scale(raw.powers & 0xFFu), hi = kept_scale(raw.powers >> 8);
+#pragma unroll
+        for (int c = 0; c < kPiece<T>; ++c) v[c] = kept_value((raw.code[c / 4] >> (8 * (c & 3))) & 0xFFu, c < p.cut ? lo : hi);
+    } else {
+        values_of<T>(raw.bits, v);
+    }
+}
+
+// Keeps the compiler from holding what it has made of a piece across a barrier: it is made again from what was loaded.
+template <typename T, bool KEPT>
+__device__ __forceinline__ void forget(RawPiece<T, KEPT>& raw)
+{
+    if constexpr (KEPT) {
+#pragma unroll
+        for (int i = 0; i < kPiece<T> / 4; ++i) asm volatile("" : "+v"(raw.code[i]));
+        asm volatile("" : "+v"(raw.powers));
+    } else {
+        asm volatile("" : "+v"(raw.bits));
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_place(T* p, ChannelsAt at, const float (&v)[kPiece<T>])
+{
+    if (at.shift == 0 && at.n >= kPiece<T>) return stream_piece(p, v);
+#pragma unroll
+    for (int c = 0; c < kPiece<T>; ++c)
+        if (at.owns(c)) p[c] = (T)v[c];
+}
+
+// A channel's parameter, `none` where there is no such vector.
+template <int W>
+__device__ __forceinline__ void channel_parameters(const float* p, ChannelsAt at, float none, float (&v)[W])
+{
+#pragma unroll
+    for (int c = 0; c < W; ++c) v[c] = p && c < at.n ? p[at.c + c] : none;
+}
+
+// ---- activations ----------------------------------------------------------------------------------------------------------
+
+// 1 / (1 + e^-z).  Binary32 results take the library's exponential, those rounded to 16 bits the hardware's, whose argument z log2 e is
+// off by up to 2^-24 of itself (5e-7 of the result at |z| = 5) and whose reciprocal is off by one step.
+template <typename T>
+__device__ __forceinline__ float sigmoid(float z)
+{
+    if constexpr (sizeof(T) == 4) return 1.0f / (1.0f + expf(-z));
+    else return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+}
+
+template <typename T, int W>
+__device__ __forceinline__ void activate(float (&z)[W], int activation, float slope)
+{
+    if (activation == QGX_ACT_SILU) {
+#pragma unroll
+        for (int c = 0; c < W; ++c) z[c] = z[c] * sigmoid<T>(z[c]);
+    } else if (activation == QGX_ACT_LEAKY) {
+#pragma unroll
+        for (int c = 0; c < W; ++c) z[c] = z[c] > 0.0f ? z[c] : slope * z[c];
+    }
+}
+
+// dy -> dz = dy act'(z)
+template <typename T, int W>
+__device__ __forceinline__ void activate_back(float (&dy)[W], const float (&h)[W], const float (&w)[W], const float (&b)[W], int activation, float slope)
+{
+    if (activation == QGX_ACT_SILU) {
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+            const float z = h[c] * w[c] + b[c], s = sigmoid<T>(z);
+            dy[c] *= s * (1.0f + z * (1.0f - s));
+        }
+    } else if (activation == QGX_ACT_LEAKY) {
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+            const float z = h[c] * w[c] + b[c];
+            if (!(z > 0.0f)) dy[c] *= slope;
+        }
+    }
+}
+
+// ---- sums over a workgroup ------------------------------------------------------------------------------------------------
+
+// The threads' sums of their channels in LDS, joined over the places: afterwards [runs][slots], slot j W + c the piece j's channel c.
+struct Runs { uint32_t runs, slots; };
+template <int THREADS, int W>
+__device__ __forceinline__ Runs column_sums(const float (&x)[W], uint32_t pieces, float* s)
+{
+    const uint32_t slots = pieces * W, steps = THREADS / pieces;
+    __syncthreads();                                       // (the memory may have been read for the sums before)
+#pragma unroll
+    for (int h = 0; h < W / 4; ++h)
+        *reinterpret_cast<float4*>(s + threadIdx.x * W + 4 * h) = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
+    __syncthreads();
+    if (slots > THREADS) return Runs{steps, slots};
+    const uint32_t runs = THREADS / slots, run = threadIdx.x / slots, col = threadIdx.x % slots;
+    float sum = 0.0f;
+    if (run < runs)
+        for (uint32_t i = run; i < steps; i += runs) sum += s[i * slots + col];
+    __syncthreads();
+    if (run < runs) s[threadIdx.x] = sum;                  // run * slots + col
+    __syncthreads();
+    return Runs{runs, slots};
+}
+
+template <int W, bool SHORT>
+__device__ __forceinline__ uint32_t slot_of(uint32_t channel, uint32_t pieces, uint32_t span)
+{
+    return SHORT || channel < (pieces - 1u) * W ? channel : channel + pieces * W - span;
+}
+
+// Every group's sum of what column_sums left, each times its channel's weight: out[group].  A wave takes a group.
+template <int THREADS, int W, bool SHORT>
+__device__ __forceinline__ void group_sums(Runs r, uint32_t pieces, uint32_t span, uint32_t per, const float* weight, const float* s, float* out)
+{
+    const uint32_t groups = span / per, n = r.runs * per;
+    for (uint32_t g = wave_id(); g < groups; g += THREADS / kWave) {
+        float sum = 0.0f;
+        for (uint32_t i = lane_id(); i < n; i += kWave) {
+            const uint32_t c = g * per + i % per;
+            sum = fmaf(s[i / per * r.slots + slot_of<W, SHORT>(c, pieces, span)], weight ? weight[c] : 1.0f, sum);
+        }
+        sum = lanes_sum<kWave>(sum);
+        if (lane_id() == 0) out[g] = sum;
+    }
+    __syncthreads();
+}
+
+// ---- forward, whole groups ------------------------------------------------------------------------------------------------
+
+constexpr int kGroupsMost = 256;                           // groups of a workgroup
+
+// Neighbouring spans of a sample on one XCD, one after the other: they share the cache's lines.
+__device__ __forceinline__ uint32_t group_unit(uint32_t block, uint32_t blocks)
+{
+    const uint32_t even = blocks / kXcds;                  // of each XCD
+    return block < even * kXcds ? block % kXcds * even + block / kXcds : block;
+}
+
+template <typename T, int THREADS, int N, bool SHORT>
+__global__ __launch_bounds__(THREADS) void k_group_norm(GroupArgs a, uint32_t batch)
+{
+    constexpr int W = kPiece<T>;
+    __shared__ __align__(16) float s_sums[THREADS * W];
+    __shared__ float s_mean[kGroupsMost], s_rstd[kGroupsMost];
+    const uint32_t unit = group_unit(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
+    const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = THREADS / pieces;
+    const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
+    const bool any = step < steps;
+    const ChannelsAt at = channels_at<W, SHORT>(j, first, span);
+    const Places<T, false> places = places_of<T, false>(a, sample, batch, at);
+    const float n = (float)a.places * (float)a.per;
+    RawPiece<T, false> raw[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t p = i * steps + step;
+        raw[i] = any && p < a.places ? load_place<T, false, SHORT>(places, p, at.n) : no_place<T, false>();
+    }
+    float sum[W];
+#pragma unroll
+    for (int c = 0; c < W; ++c) sum[c] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float v[W];
+        values_at(raw[i], places, v);
+#pragma unroll
+        for (int c = 0; c < W; ++c) sum[c] += v[c];
+    }
+#pragma unroll
+    for (int c = 0; c < W; ++c) sum[c] = at.owns(c) ? sum[c] : 0.0f;
+    Runs r = column_sums<THREADS, W>(sum, pieces, s_sums);
+    group_sums<THREADS, W, SHORT>(r, pieces, span, a.per, nullptr, s_sums, s_mean);
+    float mean[W], rstd[W];
+#pragma unroll
+    for (int c = 0; c < W; ++c) {
+        mean[c] = s_mean[min((uint32_t)(at.c + c) - first, span - 1u) / a.per] / n;
+        sum[c] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bool ok = any && i * steps + step < a.places;
+        float v[W];
+        forget(raw[i]);
+        values_at(raw[i], places, v);
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+            const float t = ok ? v[c] - mean[c] : 0.0f;
+            sum[c] = fmaf(t, t, sum[c]);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < W; ++c) sum[c] = at.owns(c) ? sum[c] : 0.0f;
+    r = column_sums<THREADS, W>(sum, pieces, s_sums);
+    group_sums<THREADS, W, SHORT>(r, pieces, span, a.per, nullptr, s_sums, s_rstd);
+    const uint32_t own_groups = span / a.per;
+    for (uint32_t g = threadIdx.x; g < own_groups; g += THREADS) {
+        const size_t to = (size_t)sample * a.groups + first / a.per + g;
+        if (a.mean) a.mean[to] = s_mean[g] / n;
+        if (a.rstd) a.rstd[to] = 1.0f / sqrtf(s_rstd[g] / n + a.eps);
+    }
+    float w[W], b[W];
+    channel_parameters<W>(a.w, at, 1.0f, w);
+    channel_parameters<W>(a.b, at, 0.0f, b);
+#pragma unroll
+    for (int c = 0; c < W; ++c) rstd[c] = 1.0f / sqrtf(s_rstd[min((uint32_t)(at.c + c) - first, span - 1u) / a.per] / n + a.eps);
+    T* y = (T*)a.y + sample / batch * a.y_worker + sample % batch * a.y_batch + at.c;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t p = i * steps + step;
+        if (!any || p >= a.places) continue;
+        float v[W];
+        forget(raw[i]);
+        values_at(raw[i], places, v);
+#pragma unroll
+        for (int c = 0; c < W; ++c) v[c] = fmaf((v[c] - mean[c]) * rstd[c], w[c], b[c]);
+        activate<T>(v, a.activation, a.slope);
+        store_place(y + p * a.y_place, at, v);
+    }
+}
+
+// ---- backward, whole groups -----------------------------------------------------------------------------------------------
+
+// h and dz of a piece.
+template <typename T, bool KEPT>
+__device__ __forceinline__ void back_values(const GroupArgs& a, const RawPiece<T, KEPT>& x, const Places<T, KEPT>& places, const RawPiece<T, false>& dy,
+                                            const Places<T, false>& grads, const float (&mean)[kPiece<T>], const float (&rstd)[kPiece<T>],
+                                            const float (&w)[kPiece<T>], const float (&b)[kPiece<T>], float (&h)[kPiece<T>], float (&dz)[kPiece<T>])
+{
+    values_at(x, places, h);
+    values_at(dy, grads, dz);
+#pragma unroll
+    for (int c = 0; c < kPiece<T>; ++c) h[c] = (h[c] - mean[c]) * rstd[c];
+    activate_back<T>(dz, h, w, b, a.activation, a.slope);
+}
+
+template <int W>
+__device__ __forceinline__ void statistics_of(const GroupArgs& a, uint32_t sample, ChannelsAt at, float (&mean)[W], float (&rstd)[W])
+{
+#pragma unroll
+    for (int c = 0; c < W; ++c) {
+        const size_t g = (size_t)sample * a.groups + min((uint32_t)(at.c + c), a.channels - 1u) / a.per;
+        mean[c] = a.mean_in[g];
+        rstd[c] = a.rstd_in[g];
+    }
+}
+
+// Where a workgroup's channels' sums go: in scratch [samples][parts][2][channels], or, where it has all of a worker's places, where they belong.
+__device__ __forceinline__ float* channel_sums_at(const GroupArgs& a, uint32_t sample, uint32_t batch, uint32_t part, int which)
+{
+    if (batch * a.parts == 1u) {
+        float* to = which ? a.db : a.dw;
+        return to ? to + sample * a.param_stride : nullptr;
+    }
+    return (which ? a.db : a.dw) ? a.scratch + (((size_t)sample * a.parts + part) * 2u + which) * a.channels : nullptr;
+}
+
+template <typename T, int THREADS, int N, bool KEPT, bool SHORT>
+__global__ __launch_bounds__(THREADS) void k_group_norm_back(GroupArgs a, uint32_t batch)
+{
+    constexpr int W = kPiece<T>;
+    __shared__ __align__(16) float s_sums[THREADS * W];
+    __shared__ float s_group[2][kGroupsMost];
+    const uint32_t unit = group_unit(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
+    const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = THREADS / pieces;
+    const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
+    const bool any = step < steps;
+    const ChannelsAt at = channels_at<W, SHORT>(j, first, span);
+    const Places<T, KEPT> places = places_of<T, KEPT>(a, sample, batch, at);
+    const Places<T, false> grads = gradients_of<T>(a, sample, batch, at);
+    RawPiece<T, KEPT> x[N];
+    RawPiece<T, false> dy[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t p = i * steps + step;
+        const bool ok = any && p < a.places;
+        x[i] = ok ? load_place<T, KEPT, SHORT>(places, p, at.n) : no_place<T, KEPT>();
+        dy[i] = ok ? load_place<T, false, SHORT>(grads, p, at.n) : no_place<T, false>();
+    }
+    float mean[W], rstd[W], w[W], b[W], dw[W], db[W];
+    statistics_of<W>(a, sample, at, mean, rstd);
+    channel_parameters<W>(a.w, at, 1.0f, w);
+    channel_parameters<W>(a.b, at, 0.0f, b);
+#pragma unroll
+    for (int c = 0; c < W; ++c) dw[c] = db[c] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float h[W], dz[W];
+        back_values<T, KEPT>(a, x[i], places, dy[i], grads, mean, rstd, w, b, h, dz);
+        const bool ok = any && i * steps + step < a.places;        // (a place that is none: dz is 0, h may be anything)
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+            dw[c] = ok ? fmaf(dz[c], h[c], dw[c]) : dw[c];
+            db[c] = ok ? db[c] + dz[c] : db[c];
+            asm volatile("" : "+v"(dw[c]), "+v"(db[c]));
+        }
+    }
+    const float* weight = a.w ? a.w + first : nullptr;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float sum[W];
+#pragma unroll
+        for (int c = 0; c < W; ++c) sum[c] = at.owns(c) ? (which ? db[c] : dw[c]) : 0.0f;
+        const Runs r = column_sums<THREADS, W>(sum, pieces, s_sums);
+        float* to = channel_sums_at(a, sample, batch, 0u, which);
+        if (to)
+            for (uint32_t c = threadIdx.x; c < span; c += THREADS) {
+                float x = 0.0f;
+                for (uint32_t i = 0; i < r.runs; ++i) x += s_sums[i * r.slots + slot_of<W, SHORT>(c, pieces, span)];
+                to[first + c] = x;
+            }
+        if (a.y) group_sums<THREADS, W, SHORT>(r, pieces, span, a.per, weight, s_sums, s_group[which]);
+    }
+    if (!a.y) return;
+    const float n = (float)a.places * (float)a.per;
+    float minus_m1[W], minus_m2[W];
+#pragma unroll
+    for (int c = 0; c < W; ++c) {
+        const uint32_t g = min((uint32_t)(at.c + c) - first, span - 1u) / a.per;
+        minus_m2[c] = -(s_group[0][g] / n);
+        minus_m1[c] = -(s_group[1][g] / n);
+    }
+    T* dx = (T*)a.y + sample / batch * a.y_worker + sample % batch * a.y_batch + at.c;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t p = i * steps + step;
+        if (!any || p >= a.places) continue;
+        float h[W], dz[W];
+        forget(x[i]);
+        forget(dy[i]);
+        back_values<T, KEPT>(a, x[i], places, dy[i], grads, mean, rstd, w, b, h, dz);
+#pragma unroll
+        for (int c = 0; c < W; ++c) dz[c] = rstd[c] * fmaf(h[c], minus_m2[c], fmaf(dz[c], w[c], minus_m1[c]));
+        store_place(dx + p * a.y_place, at, dz);
+    }
+}
+
+// ---- places dealt to workgroups -------------------------------------------------------------------------------------------
+// Workgroup (part, column, sample) has `part` places from part * a.part on of `span` channels.
+
+constexpr int kPartThreads = 256;
+constexpr int kPartTurns = 4;                              // places of a thread whose loads are under way together
+
+// Mean and sum of squares about it of every channel over the part's places, [samples][parts][2][channels].
+template <typename T, bool SHORT>
+__global__ __launch_bounds__(kPartThreads) void k_group_channels(GroupArgs a, uint32_t batch)
+{
+    constexpr int W = kPiece<T>;
+    __shared__ __align__(16) float s_sums[kPartThreads * W];
+    const uint32_t sample = blockIdx.z, part = blockIdx.x, first = blockIdx.y * a.span;
+    const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = kPartThreads / pieces;
+    const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
+    const ChannelsAt at = channels_at<W, SHORT>(j, first, span);
+    const Places<T, false> places = places_of<T, false>(a, sample, batch, at);
+    const uint32_t p0 = part * a.part, p1 = min(p0 + a.part, a.places);
+    float mean[W], m2[W], n = 0.0f;
+#pragma unroll
+    for (int c = 0; c < W; ++c) mean[c] = m2[c] = 0.0f;
+    if (step < steps)
+        for (uint32_t p = p0 + step; p < p1; p += steps * kPartTurns) {
+            // the turn's own mean and squares first, then joined with those before (Chan, Golub, LeVeque 1979)
+            RawPiece<T, false> raw[kPartTurns];
+            uint32_t here = 0;
+#pragma unroll
+            for (int i = 0; i < kPartTurns; ++i) {
+                raw[i] = p + i * steps < p1 ? load_place<T, false, SHORT>(places, p + i * steps, at.n) : no_place<T, false>();
+                here += p + i * steps < p1;
+            }
+            float v[kPartTurns][W];
+#pragma unroll
+            for (int i = 0; i < kPartTurns; ++i) values_at(raw[i], places, v[i]);
+            const float one = 1.0f / (float)here, share = (float)here / (n + (float)here);
+#pragma unroll
+            for (int c = 0; c < W; ++c) {
+                float sum = 0.0f, sq = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kPartTurns; ++i) sum += v[i][c];
+                const float mu = sum * one;
+#pragma unroll
+                for (int i = 0; i < kPartTurns; ++i) {
+                    const float t = (uint32_t)i < here ? v[i][c] - mu : 0.0f;
+                    sq = fmaf(t, t, sq);
+                }
+                const float apart = mu - mean[c];
+                mean[c] = fmaf(apart, share, mean[c]);
+                m2[c] += fmaf(apart * apart, n * share, sq);
+            }
+            n += (float)here;
+        }
+    // the threads' joined: sum of n mean, then of the squares about the whole's mean
+    float* to = a.scratch + ((size_t)sample * a.parts + part) * 2u * a.channels + first;
+    const float total = (float)(p1 - p0);
+    float x[W];
+#pragma unroll
+    for (int c = 0; c < W; ++c) x[c] = at.owns(c) ? n * mean[c] : 0.0f;
+    Runs r = column_sums<kPartThreads, W>(x, pieces, s_sums);
+    float all[W];
+#pragma unroll
+    for (int c = 0; c < W; ++c) {
+        all[c] = 0.0f;
+        if (at.owns(c))
+            for (uint32_t i = 0; i < r.runs; ++i) all[c] += s_sums[i * r.slots + j * W + c];
+        all[c] /= total;
+        if (step == 0 && at.owns(c)) to[at.c + c - (int)first] = all[c];
+    }
+#pragma unroll
+    for (int c = 0; c < W; ++c) x[c] = at.owns(c) ? fmaf((mean[c] - all[c]) * (mean[c] - all[c]), n, m2[c]) : 0.0f;
+    r = column_sums<kPartThreads, W>(x, pieces, s_sums);
+    if (step == 0)
+#pragma unroll
+        for (int c = 0; c < W; ++c)
+            if (at.owns(c)) {
+                float sum = 0.0f;
+                for (uint32_t i = 0; i < r.runs; ++i) sum += s_sums[i * r.slots + j * W + c];
+                to[a.channels + at.c + c - (int)first] = sum;
+            }
+}
+
+// The sum over a workgroup of 256 threads, in each.
+__device__ __forceinline__ float block_sum(float x, float* s)
+{
+    x = lanes_sum<kWave>(x);
+    if (lane_id() == 0) s[wave_id()] = x;
+    __syncthreads();
+    x = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    return x;
+}
+
+// A group's mean and rstd from its channels' over the parts.
+__global__ __launch_bounds__(256) void k_group_join(GroupArgs a)
+{
+    __shared__ float s[4];
+    const uint32_t sample = blockIdx.y, g = blockIdx.x;
+    const float* from = a.scratch + (size_t)sample * a.parts * 2u * a.channels + g * a.per;
+    const float all = (float)a.places * (float)a.per;
+    const uint32_t entries = a.parts * a.per;
+    float sum = 0.0f;
+    for (uint32_t i = threadIdx.x; i < entries; i += 256u) {
+        const uint32_t part = i / a.per, c = i % a.per;
+        const float n = (float)min(a.part, a.places - part * a.part);
+        sum = fmaf(n, from[(size_t)part * 2u * a.channels + c], sum);
+    }
+    const float mean = block_sum(sum, s) / all;
+    sum = 0.0f;
+    for (uint32_t i = threadIdx.x; i < entries; i += 256u) {
+        const uint32_t part = i / a.per, c = i % a.per;
+        const float* p = from + (size_t)part * 2u * a.channels + c;
+        const float n = (float)min(a.part, a.places - part * a.part), apart = p[0] - mean;
+        sum += fmaf(apart * apart, n, p[a.channels]);
+    }
+    const float rstd = 1.0f / sqrtf(block_sum(sum, s) / all + a.eps);
+    if (threadIdx.x == 0) {
+        const size_t to = (size_t)sample * a.groups + g, groups = (size_t)a.samples * a.groups;
+        a.sums[to] = mean;
+        a.sums[groups + to] = rstd;
+        if (a.mean) a.mean[to] = mean;
+        if (a.rstd) a.rstd[to] = rstd;
+    }
+}
+
+template <typename T, bool SHORT>
+__global__ __launch_bounds__(kPartThreads) void k_group_apply(GroupArgs a, uint32_t batch)
+{
+    constexpr int W = kPiece<T>;
+    // the last places first: the pass before left them in the cache
+    const uint32_t sample = gridDim.z - 1u - blockIdx.z, part = gridDim.x - 1u - blockIdx.x, first = blockIdx.y * a.span;
+    const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = kPartThreads / pieces;
+    const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
+    if (step >= steps) return;
+    const ChannelsAt at = channels_at<W, SHORT>(j, first, span);
+    const Places<T, false> places = places_of<T, false>(a, sample, batch, at);
+    const uint32_t p0 = part * a.part, p1 = min(p0 + a.part, a.places);
+    float mean[W], rstd[W], w[W], b[W];
+    statistics_of<W>(a, sample, at, mean, rstd);
+    channel_parameters<W>(a.w, at, 1.0f, w);
+    channel_parameters<W>(a.b, at, 0.0f, b);
+    T* y = (T*)a.y + sample / batch * a.y_worker + sample % batch * a.y_batch + at.c;
+    for (uint32_t p = p0 + step; p < p1; p += steps * kPartTurns) {
+        RawPiece<T, false> raw[kPartTurns];
+#pragma unroll
+        for (int i = 0; i < kPartTurns; ++i)
+            raw[i] = p + i * steps < p1 ? load_place<T, false, SHORT>(places, p + i * steps, at.n) : no_place<T, false>();
+#pragma unroll
+        for (int i = 0; i < kPartTurns; ++i) {
+            if (p + i * steps >= p1) break;
+            float v[W];
+            values_at(raw[i], places, v);
+#pragma unroll
+            for (int c = 0; c < W; ++c) v[c] = fmaf((v[c] - mean[c]) * rstd[c], w[c], b[c]);
+            activate<T>(v, a.activation, a.slope);
+            store_place(y + (p + i * steps) * a.y_place, at, v);
+        }
+    }
+}
+
+// Sums of dz h and dz of every channel over the part's places.
+template <typename T, bool KEPT, bool SHORT>
+__global__ __launch_bounds__(kPartThreads) void k_group_back_channels(GroupArgs a, uint32_t batch)
+{
+    constexpr int W = kPiece<T>;
+    __shared__ __align__(16) float s_sums[kPartThreads * W];
+    const uint32_t sample = blockIdx.z, part = blockIdx.x, first = blockIdx.y * a.span;
+    const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = kPartThreads / pieces;
+    const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
+    const ChannelsAt at = channels_at<W, SHORT>(j, first, span);
+    const Places<T, KEPT> places = places_of<T, KEPT>(a, sample, batch, at);
+    const Places<T, false> grads = gradients_of<T>(a, sample, batch, at);
+    const uint32_t p0 = part * a.part, p1 = min(p0 + a.part, a.places);
+    float mean[W], rstd[W], w[W], b[W], dw[W], db[W];
+    statistics_of<W>(a, sample, at, mean, rstd);
+    channel_parameters<W>(a.w, at, 1.0f, w);
+    channel_parameters<W>(a.b, at, 0.0f, b);
+#pragma unroll
+    for (int c = 0; c < W; ++c) dw[c] = db[c] = 0.0f;
+    if (step < steps)
+        for (uint32_t p = p0 + step; p < p1; p += steps * kPartTurns) {
+            RawPiece<T, KEPT> x[kPartTurns];
+            RawPiece<T, false> dy[kPartTurns];
+#pragma unroll
+            for (int i = 0; i < kPartTurns; ++i) {
+                const bool ok = p + i * steps < p1;
+                x[i] = ok ? load_place<T, KEPT, SHORT>(places, p + i * steps, at.n) : no_place<T, KEPT>();
+                dy[i] = ok ? load_place<T, false, SHORT>(grads, p + i * steps, at.n) : no_place<T, false>();
+            }
+#pragma unroll
+            for (int i = 0; i < kPartTurns; ++i) {
+                if (p + i * steps >= p1) break;
+                float h[W], dz[W];
+                back_values<T, KEPT>(a, x[i], places, dy[i], grads, mean, rstd, w, b, h, dz);
+#pragma unroll
+                for (int c = 0; c < W; ++c) {
+                    dw[c] = fmaf(dz[c], h[c], dw[c]);
+                    db[c] += dz[c];
+                }
+            }
+        }
+    float* to = a.scratch + ((size_t)sample * a.parts + part) * 2u * a.channels;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float sum[W];
+#pragma unroll
+        for (int c = 0; c < W; ++c) sum[c] = at.owns(c) ? (which ? db[c] : dw[c]) : 0.0f;
+        const Runs r = column_sums<kPartThreads, W>(sum, pieces, s_sums);
+        for (uint32_t c = threadIdx.x; c < span; c += kPartThreads) {
+            float x = 0.0f;
+            for (uint32_t i = 0; i < r.runs; ++i) x += s_sums[i * r.slots + slot_of<W, SHORT>(c, pieces, span)];
+            to[which * a.channels + first + c] = x;
+        }
+    }
+}
+
+// A group's means of g h and g from its channels' sums.
+__global__ __launch_bounds__(256) void k_group_back_join(GroupArgs a)
+{
+    __shared__ float s[4];
+    const uint32_t sample = blockIdx.y, g = blockIdx.x, entries = a.parts * a.per;
+    const float* from = a.scratch + (size_t)sample * a.parts * 2u * a.channels + g * a.per;
+    float gh = 0.0f, gs = 0.0f;
+    for (uint32_t i = threadIdx.x; i < entries; i += 256u) {
+        const uint32_t part = i / a.per, c = i % a.per;
+        const float* p = from + (size_t)part * 2u * a.channels + c;
+        const float w = a.w ? a.w[g * a.per + c] : 1.0f;
+        gh = fmaf(p[0], w, gh);
+        gs = fmaf(p[a.channels], w, gs);
+    }
+    const float all = (float)a.places * (float)a.per;
+    gh = block_sum(gh, s);
+    gs = block_sum(gs, s);
+    if (threadIdx.x == 0) {
+        const size_t to = (size_t)sample * a.groups + g, groups = (size_t)a.samples * a.groups;
+        a.sums[to] = gh / all;
+        a.sums[groups + to] = gs / all;
+    }
+}
+
+template <typename T, bool KEPT, bool SHORT>
+__global__ __launch_bounds__(kPartThreads) void k_group_back_apply(GroupArgs a, uint32_t batch)
+{
+    constexpr int W = kPiece<T>;
+    const uint32_t sample = gridDim.z - 1u - blockIdx.z, part = gridDim.x - 1u - blockIdx.x, first = blockIdx.y * a.span;
+    const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = kPartThreads / pieces;
+    const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
+    if (step >= steps) return;
+    const ChannelsAt at = channels_at<W, SHORT>(j, first, span);
+    const Places<T, KEPT> places = places_of<T, KEPT>(a, sample, batch, at);
+    const Places<T, false> grads = gradients_of<T>(a, sample, batch, at);
+    const uint32_t p0 = part * a.part, p1 = min(p0 + a.part, a.places);
+    float mean[W], rstd[W], w[W], b[W], minus_m1[W], minus_m2[W];
+    statistics_of<W>(a, sample, at, mean, rstd);
+    channel_parameters<W>(a.w, at, 1.0f, w);
+    channel_parameters<W>(a.b, at, 0.0f, b);
+#pragma unroll
+    for (int c = 0; c < W; ++c) {
+        const size_t g = (size_t)sample * a.groups + min((uint32_t)(at.c + c), a.channels - 1u) / a.per;
+        minus_m2[c] = -a.sums[g];
+        minus_m1[c] = -a.sums[(size_t)a.samples * a.groups + g];
+    }
+    T* dx = (T*)a.y + sample / batch * a.y_worker + sample % batch * a.y_batch + at.c;
+    for (uint32_t p = p0 + step; p < p1; p += steps * kPartTurns) {
+        RawPiece<T, KEPT> x[kPartTurns];
+        RawPiece<T, false> dy[kPartTurns];
+#pragma unroll
+        for (int i = 0; i < kPartTurns; ++i) {
+            const bool ok = p + i * steps < p1;
+            x[i] = ok ? load_place<T, KEPT, SHORT>(places, p + i * steps, at.n) : no_place<T, KEPT>();
+            dy[i] = ok ? load_place<T, false, SHORT>(grads, p + i * steps, at.n) : no_place<T, false>();
+        }
+#pragma unroll
+        for (int i = 0; i < kPartTurns; ++i) {
+            if (p + i * steps >= p1) break;
+            float h[W], dz[W];
+            back_values<T, KEPT>(a, x[i], places, dy[i], grads, mean, rstd, w, b, h, dz);
+#pragma unroll
+            for (int c = 0; c < W; ++c) dz[c] = rstd[c] * fmaf(h[c], minus_m2[c], fmaf(dz[c], w[c], minus_m1[c]));
+            store_place(dx + (p + i * steps) * a.y_place, at, dz);
+        }
+    }
+}
+
+// A worker's parameters' gradients: its samples' and parts' sums, four runs of them side by side.
+__global__ __launch_bounds__(256) void k_group_parameters(GroupArgs a, uint32_t batch)
+{
+    __shared__ float s[4][kWave];
+    const uint32_t k = blockIdx.y, which = blockIdx.z, c = blockIdx.x * kWave + lane_id(), entries = batch * a.parts;
+    float* to = which ? a.db : a.dw;
+    if (!to) return;
+    float sum = 0.0f;
+    if (c < a.channels) {
+        const float* from = a.scratch + ((size_t)k * entries * 2u + which) * a.channels + c;
+#pragma unroll 4
+        for (uint32_t i = wave_id(); i < entries; i += 4u) sum += from[(size_t)i * 2u * a.channels];
+    }
+    s[wave_id()][lane_id()] = sum;
+    __syncthreads();
+    if (wave_id() == 0 && c < a.channels) to[k * a.param_stride + c] = (s[0][lane_id()] + s[1][lane_id()]) + (s[2][lane_id()] + s[3][lane_id()]);
+}
+
+// ---- which kernel ---------------------------------------------------------------------------------------------------------
+
+static uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1u) / b); }
+
+// Whole groups where a span of at least 64 bytes (or of all channels) has its places in a workgroup's registers: 1024 threads with up to 16 pieces of
+// 16 bytes forward, 8 backward (of each of two streams).
+GroupPlan group_plan(int dtype, uint32_t samples, uint32_t places, uint32_t channels, uint32_t groups, bool backward, uint32_t n_cu)
+{
+    const uint32_t W = dtype == QGX_F32 ? 4u : 8u, per = channels / groups, most = backward ? 8u : 16u;
+    GroupPlan p{};
+    p.parts = 1;
+    p.part = places;
+    if (samples == 0 || places == 0) return p;
+    // groups of a workgroup: those of 64 bytes at least, and of more while there are workgroups enough
+    uint32_t of = min(groups, max(1u, ceil_div(4u * W, per)));
+    auto pieces_of = [&](uint32_t n) { return ceil_div((uint64_t)n * per, W); };
+    auto fits = [&](uint32_t n) {
+        const uint32_t pieces = pieces_of(n);
+        return n <= (uint32_t)kGroupsMost && pieces <= 1024u && ceil_div(places, 1024u / pieces) <= most;
+    };
+    while (of < groups && 2u * of <= groups && fits(2u * of) && (uint64_t)samples * (groups / (2u * of)) >= 4u * n_cu) of *= 2u;
+    if (channels >= W && fits(of)) {
+        p.whole = true;
+        p.span = of * per;
+        p.spans = ceil_div(groups, of);
+        const uint32_t pieces = pieces_of(of);
+        p.threads = pieces <= 256u && ceil_div(places, 256u / pieces) <= most / 2u ? 256u : 1024u;
+        p.pieces = ceil_div(places, p.threads / pieces);
+    } else {
+        p.span = min(channels, 256u * W);                  // (any channels: borders of groups do not matter here)
+        p.spans = ceil_div(channels, p.span);
+        const uint32_t pieces = ceil_div(p.span, W), steps = 256u / pieces;
+        // eight workgroups for every compute unit, but four turns for each of them
+        const uint32_t want = max(1u, ceil_div(8u * n_cu, (uint64_t)samples * p.spans));
+        p.part = max(ceil_div(places, want), 4u * steps * (uint32_t)kPartTurns);
+        p.parts = ceil_div(places, p.part);
+    }
+    const bool sums = !p.whole || backward;
+    p.at_sums = sums ? ((uint64_t)samples * p.parts * 2u * channels + 3u) / 4u * 4u : 0u;
+    const uint64_t floats = p.at_sums + (p.whole ? 0u : 2u * (uint64_t)samples * groups);
+    p.scratch = floats * sizeof(float);
+    return p;
+}
+
+static void deal(GroupArgs& a, const GroupPlan& p)
+{
+    a.span = p.span; a.spans = p.spans; a.parts = p.parts; a.part = p.part;
+    a.sums = a.scratch ? a.scratch + p.at_sums : nullptr;
+}
+
+template <typename T, int THREADS, int N, bool SHORT>
+static hipError_t launch_whole(const GroupArgs& a, uint32_t batch, hipStream_t st)
+{
+    hipLaunchKernelGGL((k_group_norm<T, THREADS, N, SHORT>), dim3(a.samples * a.spans), dim3(THREADS), 0, st, a, batch);
+    return hipGetLastError();
+}
+
+template <typename T, bool SHORT>
+static hipError_t launch_forward(GroupArgs& a, uint32_t batch, const GroupPlan& p, hipStream_t st)
+{
+    if (p.whole) {
+        if (p.threads == 256u) {
+            if (p.pieces <= 2u) return launch_whole<T, 256, 2, SHORT>(a, batch, st);
+            return p.pieces <= 4u ? launch_whole<T, 256, 4, SHORT>(a, batch, st) : launch_whole<T, 256, 8, SHORT>(a, batch, st);
+        }
+        if (p.pieces <= 4u) return launch_whole<T, 1024, 4, SHORT>(a, batch, st);
+        return p.pieces <= 8u ? launch_whole<T, 1024, 8, SHORT>(a, batch, st) : launch_whole<T, 1024, 16, SHORT>(a, batch, st);
+    }
+    const dim3 grid(a.parts, a.spans, a.samples);
+    hipLaunchKernelGGL((k_group_channels<T, SHORT>), grid, dim3(kPartThreads), 0, st, a, batch);
+    hipLaunchKernelGGL(k_group_join, dim3(a.groups, a.samples), dim3(256), 0, st, a);
+    a.mean_in = a.sums;
+    a.rstd_in = a.sums + (size_t)a.samples * a.groups;
+    hipLaunchKernelGGL((k_group_apply<T, SHORT>), grid, dim3(kPartThreads), 0, st, a, batch);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_forward_of(GroupArgs& a, uint32_t batch, const GroupPlan& p, hipStream_t st)
+{
+    return a.channels < (uint32_t)kPiece<T> ? launch_forward<T, true>(a, batch, p, st) : launch_forward<T, false>(a, batch, p, st);
+}
+
+hipError_t launch_group_norm(int dtype, const GroupArgs& args, uint32_t workers, const GroupPlan& plan, hipStream_t st)
+{
+    GroupArgs a = args;
+    if (a.samples == 0 || a.places == 0) return hipSuccess;
+    deal(a, plan);
+    const uint32_t batch = a.samples / workers;
+    return dtype == QGX_F32   ? launch_forward_of<float>(a, batch, plan, st)
+           : dtype == QGX_F16 ? launch_forward_of<_Float16>(a, batch, plan, st)
+                              : launch_forward_of<__bf16>(a, batch, plan, st);
+}
+
+template <typename T, int THREADS, int N, bool KEPT, bool SHORT>
+static hipError_t launch_back_whole(const GroupArgs& a, uint32_t batch, hipStream_t st)
+{
+    hipLaunchKernelGGL((k_group_norm_back<T, THREADS, N, KEPT, SHORT>), dim3(a.samples * a.spans), dim3(THREADS), 0, st, a, batch);
+    return hipGetLastError();
+}
+
+template <typename T, bool KEPT, bool SHORT>
+static hipError_t launch_back(const GroupArgs& a, uint32_t batch, const GroupPlan& p, hipStream_t st)
+{
+    if (p.whole) {
+        if (p.threads == 256u)
+            return p.pieces <= 2u ? launch_back_whole<T, 256, 2, KEPT, SHORT>(a, batch, st) : launch_back_whole<T, 256, 4, KEPT, SHORT>(a, batch, st);
+        return p.pieces <= 4u ? launch_back_whole<T, 1024, 4, KEPT, SHORT>(a, batch, st) : launch_back_whole<T, 1024, 8, KEPT, SHORT>(a, batch, st);
+    }
+    const dim3 grid(a.parts, a.spans, a.samples);
+    hipLaunchKernelGGL((k_group_back_channels<T, KEPT, SHORT>), grid, dim3(kPartThreads), 0, st, a, batch);
+    if (a.y) {
+        hipLaunchKernelGGL(k_group_back_join, dim3(a.groups, a.samples), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((k_group_back_apply<T, KEPT, SHORT>), grid, dim3(kPartThreads), 0, st, a, batch);
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_back_of(const GroupArgs& a, uint32_t batch, const GroupPlan& p, hipStream_t st)
+{
+    const bool few = a.channels < (uint32_t)kPiece<T>;
+    if (a.x) return few ? launch_back<T, false, true>(a, batch, p, st) : launch_back<T, false, false>(a, batch, p, st);
+    return few ? launch_back<T, true, true>(a, batch, p, st) : launch_back<T, true, false>(a, batch, p, st);
+}
+
+hipError_t launch_group_norm_back(int dtype, const GroupArgs& args, uint32_t workers, const GroupPlan& plan, hipStream_t st)
+{
+    GroupArgs a = args;
+    if (!a.y && !a.dw && !a.db) return hipSuccess;
+    deal(a, plan);
+    const uint32_t batch = a.samples / workers;
+    if (batch && a.places) {
+        const hipError_t e = dtype == QGX_F32   ? launch_back_of<float>(a, batch, plan, st)
+                             : dtype == QGX_F16 ? launch_back_of<_Float16>(a, batch, plan, st)
+                                                : launch_back_of<__bf16>(a, batch, plan, st);
+        if (e != hipSuccess) return e;
+    }
+    if ((!a.dw && !a.db) || (plan.whole && batch == 1u)) return hipSuccess;
+    // (no samples or places: sums of nothing)
+    hipLaunchKernelGGL(k_group_parameters, dim3((a.channels + kWave - 1u) / kWave, workers, 2u), dim3(256), 0, st, a, a.places ? batch : 0u);
+    return hipGetLastError();
+}
+
+}  // namespace qgx

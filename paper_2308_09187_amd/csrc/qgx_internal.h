@@ -350,4 +350,88 @@ BiasBackPlan bias_back_plan(int dtype, const BiasArgs& a, const BucketArgs& b, u
 hipError_t launch_position_bias_back(int dtype, const BiasArgs& a, const BucketArgs& b, const BiasBackPlan& plan, float* dtable,
                                      uint32_t table_rows, uint64_t param_stride, void* scratch, hipStream_t st);
 
+// ---- an image or video model's block (qgx_checkpoint.hip, qgx_group_norm.hip, qgx_weight_gradient.hip, qgx_rotary.hip) ----
+struct KeptDraws {              // what a call that rounds without bias draws from
+    uint32_t seed_lo, seed_hi, call_id, call_mode;   // call_mode: 0: call_id as given; 1, 2: 2(t-1), 2(t-1)+1 from the iteration counter on the device
+    uint32_t on;                // 0: to nearest
+};
+struct KeepArgs {
+    const void* x;              // to be kept
+    void* y;                    // restored
+    uint8_t* codes;
+    uint8_t* powers;
+    uint64_t x_worker, x_batch, x_row, y_row, tiles;
+    uint32_t rows, batch, n_rows, cols, blocks;     // rows of a sample, samples of a worker, rows of all
+    uint32_t top;               // the type's largest stored power
+};
+constexpr uint32_t kKeptTop = 248u, kKeptTopF16 = 136u;   // largest powers kept, of types of 8 and of 5 bits of exponent
+hipError_t launch_checkpoint(int dtype, const KeepArgs& a, const KeptDraws& d, Scalars* sc, hipStream_t st);
+hipError_t launch_restore(int dtype, const KeepArgs& a, hipStream_t st);
+
+struct GroupArgs {
+    const void* x;              // or null: codes and powers
+    const uint8_t* codes;
+    const uint8_t* powers;
+    const void* dy;
+    void* y;                    // or dx, or null
+    const float* w;             // [channels] or null
+    const float* b;
+    const float* mean_in;       // [samples][groups]
+    const float* rstd_in;
+    float* mean;                // [samples][groups] or null
+    float* rstd;
+    float* dw;                  // [workers] runs of channels, param_stride apart, or null
+    float* db;
+    uint64_t x_worker, x_batch, x_place, dy_worker, dy_batch, dy_place, y_worker, y_batch, y_place, param_stride;
+    uint64_t code_place, power_place;      // from a place's codes and powers to the next's
+    uint32_t samples, batch, places, channels, groups, per;    // samples = workers * batch; per = channels of a group
+    int32_t activation;
+    float slope, eps;
+    // how it is dealt out, filled in by the launch
+    uint32_t span, spans;       // whole groups' channels of a workgroup, workgroups across a sample's
+    uint32_t parts, part;       // workgroups along a sample's places, places of each
+    float* scratch;             // see GroupPlan
+    float* sums;
+};
+struct GroupPlan {
+    bool whole;                 // a workgroup has all of its groups' places in its registers
+    uint32_t threads, pieces;   // of that kernel
+    uint32_t span, spans, parts, part;
+    uint64_t at_sums;           // floats before the groups' sums, after the channels' [samples][parts][2][channels]
+    uint64_t scratch;           // bytes
+};
+GroupPlan group_plan(int dtype, uint32_t samples, uint32_t places, uint32_t channels, uint32_t groups, bool backward, uint32_t n_cu);
+hipError_t launch_group_norm(int dtype, const GroupArgs& a, uint32_t workers, const GroupPlan& plan, hipStream_t st);
+hipError_t launch_group_norm_back(int dtype, const GroupArgs& a, uint32_t workers, const GroupPlan& plan, hipStream_t st);
+
+struct WeightGradArgs {
+    const uint8_t* codes;
+    const uint8_t* powers;
+    const void* dy;
+    float* dw;                  // worker k's [cols][out] at + k * dw_worker
+    float* db;                  // or null
+    float* scratch;             // [workers][parts][cols * out + out] where parts > 1
+    uint64_t dy_worker, dy_row, dw_worker, db_worker;
+    uint32_t rows, cols, out, blocks;      // blocks: of 32 columns, of a kept row
+    uint32_t tiles_i, tiles_o, parts, part_rows;
+};
+struct WeightGradPlan {
+    uint32_t tiles_i, tiles_o, parts, part_rows;
+    uint64_t scratch;           // bytes
+};
+WeightGradPlan weight_grad_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t cols, uint32_t out, uint32_t n_cu);
+hipError_t launch_weight_grad(int dtype, const WeightGradArgs& a, uint32_t workers, const WeightGradPlan& plan, hipStream_t st);
+
+struct RotaryArgs {
+    const void* in;
+    void* out;
+    const int32_t* positions;
+    uint64_t p_axis, p_worker, p_batch, i_worker, i_batch, i_token, i_head, o_worker, o_batch, o_token, o_head;
+    uint32_t batch, tokens, heads, dim, n_tokens, pairs;      // n_tokens: of all workers and sequences
+    uint32_t axis_end[QGX_MAX_AXES];       // pairs up to an axis' last
+    int32_t neighbours, back;
+    double turns[QGX_MAX_PAIRS];           // frequencies / 2 pi
+};
+hipError_t launch_rotary(int dtype, const RotaryArgs& a, uint32_t n_cu, hipStream_t st);
+
 }  // namespace qgx

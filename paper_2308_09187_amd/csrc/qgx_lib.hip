@@ -1,6 +1,7 @@
 // Host side of the C ABI: context, validation, layout tables, launches.  No arithmetic of the
 // method happens here; every step runs in the gfx950 kernels.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -1037,6 +1038,24 @@ qgx_status qgx_clip_gradients(qgx_ctx* ctx, const qgx_tensor_list* list, int nor
     return QGX_OK;
 }
 
+// Whether the runs of `run` elements that n indices by strides st (at most 2^60 / n) give are apart: smallest stride first, every one has to
+// step over what the ones before reach.
+static bool steps_apart(const uint64_t* n, const uint64_t* st, int dims, uint64_t run)
+{
+    uint64_t reach = run;
+    bool done[4] = {true, true, true, true};
+    for (int i = 0; i < dims; ++i) done[i] = n[i] == 1;
+    for (;;) {
+        int at = -1;
+        for (int i = 0; i < dims; ++i)
+            if (!done[i] && (at < 0 || st[i] < st[at])) at = i;
+        if (at < 0) return true;
+        if (st[at] < reach) return false;
+        reach += (n[at] - 1) * st[at];
+        done[at] = true;
+    }
+}
+
 // Rows of a tensor: null, misaligned, or with strides beyond what 64-bit addresses hold; rows that are written may not overlap.
 static qgx_status check_rows(qgx_ctx* ctx, const char* what, const void* p, int dtype, uint64_t workers, uint64_t rows, uint64_t cols,
                              uint64_t worker, uint64_t row, bool written)
@@ -1159,20 +1178,7 @@ static qgx_status check_scores(qgx_ctx* ctx, const char* what, const qgx_scores*
     const uint64_t n[4] = {s->workers, s->batch, s->heads, s->q}, st[4] = {s->s_worker, s->s_batch, s->s_head, s->s_row};
     for (int i = 0; i < 4; ++i)
         if (st[i] >= (1ull << 60) / n[i]) return fail(ctx, QGX_ERR_ARG, "%s: stride out of range", what);
-    if (written) {
-        // smallest stride first, every one has to step over what the ones before reach
-        uint64_t reach = s->k;
-        bool done[4] = {n[0] == 1, n[1] == 1, n[2] == 1, n[3] == 1};
-        for (;;) {
-            int at = -1;
-            for (int i = 0; i < 4; ++i)
-                if (!done[i] && (at < 0 || st[i] < st[at])) at = i;
-            if (at < 0) break;
-            if (st[at] < reach) return fail(ctx, QGX_ERR_ARG, "%s: rows overlap", what);
-            reach += (n[at] - 1) * st[at];
-            done[at] = true;
-        }
-    }
+    if (written && !steps_apart(n, st, 4, s->k)) return fail(ctx, QGX_ERR_ARG, "%s: rows overlap", what);
     return QGX_OK;
 }
 
@@ -1258,6 +1264,299 @@ qgx_status qgx_position_bias_backward(qgx_ctx* ctx, const qgx_buckets* buckets, 
     if (need && (!scratch || !aligned16(scratch))) return fail(ctx, QGX_ERR_ARG, "qgx_position_bias_backward: null or misaligned scratch");
     if (scratch_bytes < need) return fail(ctx, QGX_ERR_CAPACITY, "qgx_position_bias_backward: scratch needs %llu bytes", (unsigned long long)need);
     QGX_HIP(ctx, launch_position_bias_back(grad->dtype, a, b, plan, dtable, table_rows, param_stride, scratch, (hipStream_t)stream));
+    return QGX_OK;
+}
+
+// ---- an image or video model's block --------------------------------------------------------------------------------
+
+// Kept rows: their number and shape, and the addresses.
+static qgx_status check_kept(qgx_ctx* ctx, const char* what, const qgx_kept* kept, uint64_t rows, uint64_t cols)
+{
+    if (kept->cols == 0 || kept->cols > (1u << 24) || kept->rows >= (1ull << 31)) return fail(ctx, QGX_ERR_ARG, "%s: kept rows or columns out of range", what);
+    if (kept->rows != rows || kept->cols != cols) return fail(ctx, QGX_ERR_ARG, "%s: kept rows of another shape", what);
+    if (rows && (!kept->codes || !kept->powers || !aligned16(kept->codes))) return fail(ctx, QGX_ERR_ARG, "%s: null or misaligned codes or powers", what);
+    return QGX_OK;
+}
+
+static uint32_t kept_blocks(uint64_t cols) { return (uint32_t)((cols + QGX_KEPT_BLOCK - 1u) / QGX_KEPT_BLOCK); }
+static uint32_t kept_top(int dtype) { return dtype == QGX_F16 ? kKeptTopF16 : kKeptTop; }
+
+static KeptDraws kept_draws(const qgx_ctx* ctx, int unbiased, uint32_t call_id)
+{
+    KeptDraws d{};
+    d.seed_lo = (uint32_t)ctx->cfg.seed; d.seed_hi = (uint32_t)(ctx->cfg.seed >> 32); d.call_id = call_id;
+    d.call_mode = call_id == QGX_CALL_FIRST_HALF ? 1u : call_id == QGX_CALL_SECOND_HALF ? 2u : 0u;
+    d.on = unbiased != 0;
+    return d;
+}
+
+qgx_status qgx_checkpoint(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, const void* x, uint64_t x_worker,
+                          uint64_t x_row, int unbiased, uint32_t call_id, const qgx_kept* out, void* stream)
+{
+    qgx_status s = check_norm(ctx, "qgx_checkpoint", dtype, workers, rows, cols);
+    if (s != QGX_OK) return s;
+    if (!out) return fail(ctx, QGX_ERR_ARG, "qgx_checkpoint: null argument");
+    s = check_kept(ctx, "qgx_checkpoint", out, workers * rows, cols);
+    if (s != QGX_OK) return s;
+    if (workers == 0 || rows == 0) return QGX_OK;
+    s = check_rows(ctx, "qgx_checkpoint(x)", x, dtype, workers, rows, cols, x_worker, x_row, false);
+    if (s != QGX_OK) return s;
+    KeepArgs a{};
+    a.x = x; a.codes = out->codes; a.powers = out->powers; a.x_worker = x_worker; a.x_row = x_row;
+    a.rows = (uint32_t)rows; a.batch = 1; a.n_rows = (uint32_t)(workers * rows); a.cols = (uint32_t)cols; a.blocks = kept_blocks(cols); a.top = kept_top(dtype);
+    QGX_HIP(ctx, launch_checkpoint(dtype, a, kept_draws(ctx, unbiased, call_id), ctx->d_sc, (hipStream_t)stream));
+    return QGX_OK;
+}
+
+qgx_status qgx_restore(qgx_ctx* ctx, const qgx_kept* in, int dtype, void* y, uint64_t y_row, void* stream)
+{
+    if (!ctx || !in) return fail(ctx, QGX_ERR_ARG, "qgx_restore: null argument");
+    qgx_status s = check_norm(ctx, "qgx_restore", dtype, 1, in->rows, in->cols);
+    if (s == QGX_OK) s = check_kept(ctx, "qgx_restore", in, in->rows, in->cols);
+    if (s != QGX_OK || in->rows == 0) return s;
+    s = check_rows(ctx, "qgx_restore(y)", y, dtype, 1, in->rows, in->cols, 0, y_row, true);
+    if (s != QGX_OK) return s;
+    KeepArgs a{};
+    a.y = y; a.codes = in->codes; a.powers = in->powers; a.y_row = y_row;
+    a.rows = a.n_rows = (uint32_t)in->rows; a.cols = (uint32_t)in->cols; a.blocks = kept_blocks(in->cols);
+    QGX_HIP(ctx, launch_restore(dtype, a, (hipStream_t)stream));
+    return QGX_OK;
+}
+
+static qgx_status check_gradient(qgx_ctx* ctx, const char* what, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, uint64_t out)
+{
+    const qgx_status s = check_norm(ctx, what, dtype, workers, rows, cols);
+    if (s != QGX_OK) return s;
+    if (out == 0 || out > (1u << 24) || cols * out >= (1ull << 31)) return fail(ctx, QGX_ERR_ARG, "%s: out must be 1 .. 2^24, and cols * out below 2^31", what);
+    return QGX_OK;
+}
+
+qgx_status qgx_weight_gradient_scratch(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, uint64_t out, uint64_t* bytes)
+{
+    const qgx_status s = check_gradient(ctx, "qgx_weight_gradient_scratch", dtype, workers, rows, cols, out);
+    if (s != QGX_OK) return s;
+    if (!bytes) return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient_scratch: null argument");
+    *bytes = weight_grad_plan(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols, (uint32_t)out, ctx->n_simd / 4u).scratch;
+    return QGX_OK;
+}
+
+qgx_status qgx_weight_gradient(qgx_ctx* ctx, const qgx_kept* x, int dtype, uint64_t workers, uint64_t rows, uint64_t out, const void* dy,
+                               uint64_t dy_worker, uint64_t dy_row, float* dweight, uint64_t dw_worker, float* dbias, uint64_t db_worker,
+                               void* scratch, uint64_t scratch_bytes, void* stream)
+{
+    if (!ctx || !x) return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient: null argument");
+    const uint64_t cols = x->cols;
+    qgx_status s = check_gradient(ctx, "qgx_weight_gradient", dtype, workers, rows, cols, out);
+    if (s == QGX_OK) s = check_kept(ctx, "qgx_weight_gradient", x, workers * rows, cols);
+    if (s != QGX_OK || workers == 0) return s;
+    if (rows) s = check_rows(ctx, "qgx_weight_gradient(dy)", dy, dtype, workers, rows, out, dy_worker, dy_row, false);
+    if (s != QGX_OK) return s;
+    if (!dweight || !aligned_to(dweight, 4u) || !aligned_to(dbias, 4u)) return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient: null or misaligned gradients");
+    if ((workers > 1 && (dw_worker < cols * out || (dbias && db_worker < out))) || dw_worker >= (1ull << 60) / workers || db_worker >= (1ull << 60) / workers)
+        return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient: the workers' gradients overlap, or a stride out of range");
+    const WeightGradPlan plan = weight_grad_plan(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols, (uint32_t)out, ctx->n_simd / 4u);
+    if (plan.scratch && (!scratch || !aligned16(scratch))) return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient: null or misaligned scratch");
+    if (scratch_bytes < plan.scratch) return fail(ctx, QGX_ERR_CAPACITY, "qgx_weight_gradient: scratch needs %llu bytes", (unsigned long long)plan.scratch);
+    WeightGradArgs a{};
+    a.codes = x->codes; a.powers = x->powers; a.dy = dy; a.dw = dweight; a.db = dbias; a.scratch = (float*)scratch;
+    a.dy_worker = dy_worker; a.dy_row = dy_row; a.dw_worker = dw_worker; a.db_worker = db_worker;
+    a.rows = (uint32_t)rows; a.cols = (uint32_t)cols; a.out = (uint32_t)out; a.blocks = kept_blocks(cols);
+    QGX_HIP(ctx, launch_weight_grad(dtype, a, (uint32_t)workers, plan, (hipStream_t)stream));
+    return QGX_OK;
+}
+
+// The shape is one the kernels' counts and grids hold.
+static qgx_status check_group(qgx_ctx* ctx, const char* what, const qgx_group_shape* g)
+{
+    if (!ctx || !g) return fail(ctx, QGX_ERR_ARG, "%s: null argument", what);
+    if (!known_type(g->dtype)) return fail(ctx, QGX_ERR_ARG, "%s: unknown type", what);
+    if (g->activation < QGX_ACT_NONE || g->activation > QGX_ACT_LEAKY) return fail(ctx, QGX_ERR_ARG, "%s: unknown activation", what);
+    if (g->activation == QGX_ACT_LEAKY && !(std::fabs(g->slope) <= FLT_MAX)) return fail(ctx, QGX_ERR_ARG, "%s: slope must be finite", what);
+    if (g->channels == 0 || g->channels > (1u << 20)) return fail(ctx, QGX_ERR_ARG, "%s: channels must be 1 .. 2^20", what);
+    if (g->groups == 0 || g->channels % g->groups) return fail(ctx, QGX_ERR_ARG, "%s: groups must divide channels", what);
+    if (g->workers > 65535u || g->batch > 65535u || g->workers * g->batch > 65535u || g->places >= (1ull << 31) || g->workers * g->batch * g->places >= (1ull << 31) ||
+        g->places * g->channels >= (1ull << 36))
+        return fail(ctx, QGX_ERR_ARG, "%s: size out of range", what);
+    return QGX_OK;
+}
+
+static GroupPlan plan_of(const qgx_ctx* ctx, const qgx_group_shape* g, bool backward)
+{
+    return group_plan(g->dtype, (uint32_t)(g->workers * g->batch), (uint32_t)g->places, (uint32_t)g->channels, g->groups, backward, ctx->n_simd / 4u);
+}
+
+static bool no_places(const qgx_group_shape* g) { return g->workers == 0 || g->batch == 0 || g->places == 0; }
+
+// A tensor of the shape: addresses, strides, and, where it is written, places that do not overlap.
+static qgx_status check_places(qgx_ctx* ctx, const char* what, const qgx_group_shape* g, const qgx_places* p, bool written)
+{
+    if (!p->data || !aligned_to(p->data, element_size(g->dtype))) return fail(ctx, QGX_ERR_ARG, "%s: null or misaligned", what);
+    const uint64_t n[3] = {g->workers, g->batch, g->places}, st[3] = {p->s_worker, p->s_batch, p->s_place};
+    for (int i = 0; i < 3; ++i)
+        if (st[i] >= (1ull << 60) / n[i]) return fail(ctx, QGX_ERR_ARG, "%s: stride out of range", what);
+    if (written && !steps_apart(n, st, 3, g->channels)) return fail(ctx, QGX_ERR_ARG, "%s: places overlap", what);
+    return QGX_OK;
+}
+
+static bool same_places(const qgx_group_shape* g, const qgx_places* a, const qgx_places* b)
+{
+    return (g->workers == 1 || a->s_worker == b->s_worker) && (g->batch == 1 || a->s_batch == b->s_batch) && (g->places == 1 || a->s_place == b->s_place);
+}
+
+static GroupArgs group_args(const qgx_group_shape* g)
+{
+    GroupArgs a{};
+    a.samples = (uint32_t)(g->workers * g->batch); a.places = (uint32_t)g->places; a.channels = (uint32_t)g->channels;
+    a.groups = g->groups; a.per = a.channels / a.groups;
+    a.activation = g->activation; a.slope = g->slope;
+    return a;
+}
+
+static qgx_status check_group_scratch(qgx_ctx* ctx, const char* what, const GroupPlan& plan, const void* scratch, uint64_t bytes)
+{
+    if (plan.whole && (uint64_t)plan.spans > (1u << 21)) return fail(ctx, QGX_ERR_ARG, "%s: size out of range", what);
+    if (plan.scratch && (!scratch || !aligned16(scratch))) return fail(ctx, QGX_ERR_ARG, "%s: null or misaligned scratch", what);
+    if (bytes < plan.scratch) return fail(ctx, QGX_ERR_CAPACITY, "%s: scratch needs %llu bytes", what, (unsigned long long)plan.scratch);
+    return QGX_OK;
+}
+
+qgx_status qgx_group_norm_scratch(qgx_ctx* ctx, const qgx_group_shape* shape, int backward, uint64_t* bytes)
+{
+    const qgx_status s = check_group(ctx, "qgx_group_norm_scratch", shape);
+    if (s != QGX_OK) return s;
+    if (!bytes) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm_scratch: null argument");
+    *bytes = no_places(shape) ? 0 : plan_of(ctx, shape, backward != 0).scratch;
+    return QGX_OK;
+}
+
+qgx_status qgx_group_norm(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_places* x, const float* weight, const float* bias, float eps,
+                          const qgx_places* y, float* mean, float* rstd, const qgx_kept* keep, int unbiased, uint32_t call_id,
+                          void* scratch, uint64_t scratch_bytes, void* stream)
+{
+    qgx_status s = check_group(ctx, "qgx_group_norm", shape);
+    if (s != QGX_OK) return s;
+    if (!x || !y) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: null argument");
+    if (!(eps >= 0.0f)) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: eps must be >= 0");
+    if (keep) s = check_kept(ctx, "qgx_group_norm(keep)", keep, shape->workers * shape->batch * shape->places, shape->channels);
+    if (s != QGX_OK || no_places(shape)) return s;
+    s = check_places(ctx, "qgx_group_norm(x)", shape, x, false);
+    if (s == QGX_OK) s = check_places(ctx, "qgx_group_norm(y)", shape, y, true);
+    if (s != QGX_OK) return s;
+    if (x->data == y->data && !same_places(shape, x, y)) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: y at x's memory must have its strides");
+    if (!aligned_to(weight, 4u) || !aligned_to(bias, 4u) || !aligned_to(mean, 4u) || !aligned_to(rstd, 4u))
+        return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: binary32 buffers must be 4-byte aligned");
+    const GroupPlan plan = plan_of(ctx, shape, false);
+    s = check_group_scratch(ctx, "qgx_group_norm", plan, scratch, scratch_bytes);
+    if (s != QGX_OK) return s;
+    GroupArgs a = group_args(shape);
+    a.x = x->data; a.x_worker = x->s_worker; a.x_batch = x->s_batch; a.x_place = x->s_place;
+    a.y = y->data; a.y_worker = y->s_worker; a.y_batch = y->s_batch; a.y_place = y->s_place;
+    a.w = weight; a.b = bias; a.mean = mean; a.rstd = rstd; a.eps = eps; a.scratch = (float*)scratch;
+    if (keep) {
+        KeepArgs k{};
+        k.x = x->data; k.codes = keep->codes; k.powers = keep->powers;
+        k.x_worker = x->s_worker; k.x_batch = x->s_batch; k.x_row = x->s_place;
+        k.batch = (uint32_t)shape->batch; k.rows = a.places; k.n_rows = a.samples * a.places; k.cols = a.channels; k.blocks = kept_blocks(a.channels); k.top = kept_top(shape->dtype);
+        QGX_HIP(ctx, launch_checkpoint(shape->dtype, k, kept_draws(ctx, unbiased, call_id), ctx->d_sc, (hipStream_t)stream));
+    }
+    QGX_HIP(ctx, launch_group_norm(shape->dtype, a, (uint32_t)shape->workers, plan, (hipStream_t)stream));
+    return QGX_OK;
+}
+
+qgx_status qgx_group_norm_backward(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_places* dy, const qgx_places* x, const qgx_kept* kept,
+                                   const float* weight, const float* bias, const float* mean, const float* rstd, const qgx_places* dx,
+                                   float* dweight, float* dbias, uint64_t param_stride, void* scratch, uint64_t scratch_bytes, void* stream)
+{
+    qgx_status s = check_group(ctx, "qgx_group_norm_backward", shape);
+    if (s != QGX_OK) return s;
+    if (!x == !kept) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm_backward: either x or what was kept of it");
+    if (kept) s = check_kept(ctx, "qgx_group_norm_backward", kept, shape->workers * shape->batch * shape->places, shape->channels);
+    if (s != QGX_OK || shape->workers == 0) return s;
+    if (!no_places(shape)) {
+        if (!dy || !mean || !rstd) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm_backward: null dy, mean or rstd");
+        s = check_places(ctx, "qgx_group_norm_backward(dy)", shape, dy, false);
+        if (s == QGX_OK && x) s = check_places(ctx, "qgx_group_norm_backward(x)", shape, x, false);
+        if (s == QGX_OK && dx) s = check_places(ctx, "qgx_group_norm_backward(dx)", shape, dx, true);
+        if (s != QGX_OK) return s;
+        if (dx && (dx->data == dy->data || (x && dx->data == x->data))) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm_backward: dx may not be dy or x");
+    }
+    if ((dweight || dbias) && shape->workers > 1 && param_stride < shape->channels)
+        return fail(ctx, QGX_ERR_ARG, "qgx_group_norm_backward: param_stride below channels");
+    if (param_stride >= (1ull << 62) / shape->workers) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm_backward: stride out of range");
+    if (!aligned_to(weight, 4u) || !aligned_to(bias, 4u) || !aligned_to(mean, 4u) || !aligned_to(rstd, 4u) || !aligned_to(dweight, 4u) || !aligned_to(dbias, 4u))
+        return fail(ctx, QGX_ERR_ARG, "qgx_group_norm_backward: binary32 buffers must be 4-byte aligned");
+    GroupPlan plan{};
+    if (!no_places(shape)) plan = plan_of(ctx, shape, true);
+    s = check_group_scratch(ctx, "qgx_group_norm_backward", plan, scratch, scratch_bytes);
+    if (s != QGX_OK) return s;
+    GroupArgs a = group_args(shape);
+    if (!no_places(shape)) {
+        a.dy = dy->data; a.dy_worker = dy->s_worker; a.dy_batch = dy->s_batch; a.dy_place = dy->s_place;
+        if (x) {
+            a.x = x->data; a.x_worker = x->s_worker; a.x_batch = x->s_batch; a.x_place = x->s_place;
+        } else {
+            a.codes = kept->codes; a.powers = kept->powers; a.power_place = kept_blocks(shape->channels); a.code_place = a.power_place * QGX_KEPT_BLOCK;
+        }
+        if (dx) { a.y = dx->data; a.y_worker = dx->s_worker; a.y_batch = dx->s_batch; a.y_place = dx->s_place; }
+    }
+    a.w = weight; a.b = bias; a.mean_in = mean; a.rstd_in = rstd; a.dw = dweight; a.db = dbias; a.param_stride = param_stride; a.scratch = (float*)scratch;
+    QGX_HIP(ctx, launch_group_norm_back(shape->dtype, a, (uint32_t)shape->workers, plan, (hipStream_t)stream));
+    return QGX_OK;
+}
+
+static qgx_status check_heads(qgx_ctx* ctx, const char* what, const qgx_heads* h, bool written)
+{
+    if (!known_type(h->dtype)) return fail(ctx, QGX_ERR_ARG, "%s: unknown type", what);
+    if (h->heads == 0 || h->heads > 65535u || h->dim == 0 || h->dim > 4096u || h->workers >= (1ull << 31) || h->batch >= (1ull << 31) || h->tokens >= (1ull << 31) ||
+        (h->workers && h->batch && h->tokens && (h->workers * h->batch >= (1ull << 31) || h->workers * h->batch * h->tokens >= (1ull << 31))))
+        return fail(ctx, QGX_ERR_ARG, "%s: size out of range", what);
+    if (h->workers == 0 || h->batch == 0 || h->tokens == 0) return QGX_OK;
+    if (!h->data || !aligned_to(h->data, element_size(h->dtype))) return fail(ctx, QGX_ERR_ARG, "%s: null or misaligned", what);
+    const uint64_t n[4] = {h->workers, h->batch, h->tokens, h->heads}, st[4] = {h->s_worker, h->s_batch, h->s_token, h->s_head};
+    for (int i = 0; i < 4; ++i)
+        if (st[i] >= (1ull << 60) / n[i]) return fail(ctx, QGX_ERR_ARG, "%s: stride out of range", what);
+    if (written && !steps_apart(n, st, 4, h->dim)) return fail(ctx, QGX_ERR_ARG, "%s: heads overlap", what);
+    return QGX_OK;
+}
+
+qgx_status qgx_rotate(qgx_ctx* ctx, const qgx_rotary* rotary, const int32_t* positions, uint64_t p_axis, uint64_t p_worker, uint64_t p_batch,
+                      const qgx_heads* in, const qgx_heads* out, int back, void* stream)
+{
+    if (!ctx || !rotary || !in || !out || !rotary->frequencies) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: null argument");
+    if (rotary->axes == 0 || rotary->axes > QGX_MAX_AXES) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: 1 .. %u axes", QGX_MAX_AXES);
+    RotaryArgs a{};
+    uint64_t pairs = 0;
+    for (uint32_t i = 0; i < rotary->axes; ++i) {
+        pairs += rotary->pairs[i];
+        if (pairs > QGX_MAX_PAIRS) break;
+        a.axis_end[i] = (uint32_t)pairs;
+    }
+    if (pairs == 0 || pairs > QGX_MAX_PAIRS) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: 1 .. %u pairs", QGX_MAX_PAIRS);
+    for (uint32_t i = rotary->axes; i < QGX_MAX_AXES; ++i) a.axis_end[i] = (uint32_t)pairs;
+    for (uint32_t p = 0; p < pairs; ++p) {
+        if (!(std::fabs(rotary->frequencies[p]) <= DBL_MAX)) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: frequency %u is not finite", p);
+        a.turns[p] = rotary->frequencies[p] * 0.15915494309189533577;                   // 1 / (2 pi)
+    }
+    qgx_status s = check_heads(ctx, "qgx_rotate(in)", in, false);
+    if (s == QGX_OK) s = check_heads(ctx, "qgx_rotate(out)", out, true);
+    if (s != QGX_OK) return s;
+    if (in->dtype != out->dtype || in->heads != out->heads || in->dim != out->dim || in->workers != out->workers || in->batch != out->batch || in->tokens != out->tokens)
+        return fail(ctx, QGX_ERR_ARG, "qgx_rotate: in and out differ in type or shape");
+    if (2u * pairs > in->dim) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: %u pairs in heads of %u elements", (uint32_t)pairs, in->dim);
+    if (in->workers == 0 || in->batch == 0 || in->tokens == 0) return QGX_OK;
+    if (in->data == out->data && ((in->workers > 1 && in->s_worker != out->s_worker) || (in->batch > 1 && in->s_batch != out->s_batch) ||
+                                  (in->tokens > 1 && in->s_token != out->s_token) || (in->heads > 1 && in->s_head != out->s_head)))
+        return fail(ctx, QGX_ERR_ARG, "qgx_rotate: out at in's memory must have its strides");
+    if (!positions || !aligned_to(positions, 4u)) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: null or misaligned positions");
+    if (p_axis >= (1ull << 58) || p_worker >= (1ull << 60) / in->workers || p_batch >= (1ull << 60) / in->batch)
+        return fail(ctx, QGX_ERR_ARG, "qgx_rotate: stride of the positions out of range");
+    a.in = in->data; a.out = out->data; a.positions = positions; a.p_axis = p_axis; a.p_worker = p_worker; a.p_batch = p_batch;
+    a.i_worker = in->s_worker; a.i_batch = in->s_batch; a.i_token = in->s_token; a.i_head = in->s_head;
+    a.o_worker = out->s_worker; a.o_batch = out->s_batch; a.o_token = out->s_token; a.o_head = out->s_head;
+    a.batch = (uint32_t)in->batch; a.tokens = (uint32_t)in->tokens; a.heads = in->heads; a.dim = in->dim; a.pairs = (uint32_t)pairs;
+    a.n_tokens = (uint32_t)(in->workers * in->batch * in->tokens);
+    a.neighbours = rotary->neighbours != 0; a.back = back != 0;
+    QGX_HIP(ctx, launch_rotary(in->dtype, a, ctx->n_simd / 4u, (hipStream_t)stream));
     return QGX_OK;
 }
 

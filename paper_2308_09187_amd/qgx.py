@@ -7,6 +7,7 @@ streams.  Loading fails loudly when the library has not been built
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 
 import numpy as np
@@ -25,6 +26,9 @@ CHUNK, SUB, SUBS, MAX_SYM, MAX_BINS = 4096, 32, 128, 127, 4096
 STATIC_MAX_CHUNKS = 65536
 MAX_INTERVALS = 128
 FEW_TENSORS = 16
+KEPT_BLOCK = 32
+ACTIVATIONS = {"none": 0, "silu": 1, "leaky": 2}
+MAX_AXES, MAX_PAIRS = 4, 256
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 EXPORTS = [
@@ -34,6 +38,8 @@ EXPORTS = [
     "qgx_poll_error", "qgx_last_error",
     "qgx_tensor_list_size", "qgx_tensor_list_set", "qgx_clip_gradients", "qgx_layer_norm", "qgx_layer_norm_scratch", "qgx_layer_norm_backward",
     "qgx_position_bias", "qgx_position_bias_scratch", "qgx_position_bias_backward",
+    "qgx_checkpoint", "qgx_restore", "qgx_weight_gradient_scratch", "qgx_weight_gradient", "qgx_group_norm_scratch", "qgx_group_norm",
+    "qgx_group_norm_backward", "qgx_rotate",
     "qgx_game_operator", "qgx_game_dual_vectors", "qgx_quantize_encode_game", "qgx_norm2", "qgx_game_gap", "qgx_quantization_metrics",
 ]
 
@@ -80,6 +86,29 @@ class _Scores(C.Structure):
                 ("s_row", C.c_uint64)]
 
 
+class _Kept(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("powers", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64)]
+
+
+class _GroupShape(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("activation", C.c_int32), ("slope", C.c_float), ("groups", C.c_uint32), ("workers", C.c_uint64),
+                ("batch", C.c_uint64), ("places", C.c_uint64), ("channels", C.c_uint64)]
+
+
+class _Places(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("s_worker", C.c_uint64), ("s_batch", C.c_uint64), ("s_place", C.c_uint64)]
+
+
+class _Rotary(C.Structure):
+    _fields_ = [("axes", C.c_uint32), ("pairs", C.c_uint32 * MAX_AXES), ("neighbours", C.c_int32), ("frequencies", C.POINTER(C.c_double))]
+
+
+class _Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("heads", C.c_uint32), ("dim", C.c_uint32), ("workers", C.c_uint64),
+                ("batch", C.c_uint64), ("tokens", C.c_uint64), ("s_worker", C.c_uint64), ("s_batch", C.c_uint64), ("s_token", C.c_uint64),
+                ("s_head", C.c_uint64)]
+
+
 _lib = None
 
 
@@ -105,6 +134,14 @@ def load():
         lib.qgx_position_bias.argtypes = [ptr, ptr, ptr, C.c_uint32, ptr, ptr, C.c_int64, ptr, ptr]
         lib.qgx_position_bias_scratch.argtypes = [ptr, ptr, ptr, C.c_int64, ptr]
         lib.qgx_position_bias_backward.argtypes = [ptr, ptr, ptr, C.c_int64, ptr, C.c_uint32, u64, ptr, u64, ptr]
+        lib.qgx_checkpoint.argtypes = [ptr, C.c_int, u64, u64, u64, ptr, u64, u64, C.c_int, C.c_uint32, ptr, ptr]
+        lib.qgx_restore.argtypes = [ptr, ptr, C.c_int, ptr, u64, ptr]
+        lib.qgx_weight_gradient_scratch.argtypes = [ptr, C.c_int, u64, u64, u64, u64, ptr]
+        lib.qgx_weight_gradient.argtypes = [ptr, ptr, C.c_int, u64, u64, u64, ptr, u64, u64, ptr, u64, ptr, u64, ptr, u64, ptr]
+        lib.qgx_group_norm_scratch.argtypes = [ptr, ptr, C.c_int, ptr]
+        lib.qgx_group_norm.argtypes = [ptr, ptr, ptr, ptr, ptr, f32, ptr, ptr, ptr, ptr, C.c_int, C.c_uint32, ptr, u64, ptr]
+        lib.qgx_group_norm_backward.argtypes = [ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr, ptr, u64, ptr, u64, ptr]
+        lib.qgx_rotate.argtypes = [ptr, ptr, ptr, u64, u64, u64, ptr, ptr, C.c_int, ptr]
         _lib = lib
     return _lib
 
@@ -203,6 +240,43 @@ class Buckets:
                     ids.append(m + b)
                     bounds.append(stop[b])
         return cls(bounds, ids)
+
+
+class Checkpoint:
+    """An activation kept in 8 bits, rows of `cols` elements in blocks of 32: codes uint8 [.., 32 * blocks] and powers uint8
+    [.., blocks], contiguous; an element is (code - 128) * 2^(power - 127).  Made by Context.new_checkpoint or
+    Context.checkpoint, or from such tensors."""
+
+    def __init__(self, codes, powers, cols):
+        cols = int(cols)
+        blocks = (cols + KEPT_BLOCK - 1) // KEPT_BLOCK
+        for t, n, name in ((codes, KEPT_BLOCK * blocks, "codes"), (powers, blocks, "powers")):
+            _need(t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous() and t.dim() >= 1 and t.shape[-1] == n, "%s: contiguous uint8 [.., %d] on the GPU", name, n)
+        _need(codes.shape[:-1] == powers.shape[:-1] and codes.get_device() == powers.get_device(), "codes and powers: of the same rows")
+        self.codes, self.powers = codes, powers
+        self.shape = codes.shape[:-1] + (cols,)
+        self._c = _Kept(codes.data_ptr(), powers.data_ptr(), math.prod(self.shape[:-1]), cols)
+        self._ref = C.addressof(self._c)
+
+
+class Rotary:
+    """Rotary positions with several axes: the first pairs[0] pairs of a head turn with the token's position along axis 0, the next
+    pairs[1] along axis 1, and so on, pair p by position * frequencies[p] radians.  neighbours: pair p is elements 2 p and
+    2 p + 1 of a head, else p and p + the number of pairs."""
+
+    def __init__(self, pairs, frequencies, neighbours=False):
+        pairs, frequencies = [int(n) for n in pairs], [float(f) for f in frequencies]
+        _need(1 <= len(pairs) <= MAX_AXES and all(n >= 0 for n in pairs) and 1 <= sum(pairs) <= MAX_PAIRS, "Rotary: 1 .. %d axes, 1 .. %d pairs", MAX_AXES, MAX_PAIRS)
+        _need(len(frequencies) == sum(pairs) and all(math.isfinite(f) for f in frequencies), "Rotary: a finite frequency for every pair")
+        self.pairs, self.neighbours = pairs, bool(neighbours)
+        self.frequencies = (C.c_double * len(frequencies))(*frequencies)
+        self._c = _Rotary(len(pairs), (C.c_uint32 * MAX_AXES)(*pairs), int(self.neighbours), self.frequencies)
+        self._ref = C.addressof(self._c)
+
+    @classmethod
+    def by_base(cls, pairs, base=10000.0, neighbours=False):
+        """Frequencies base^(-i / n), i = 0 .. n - 1, for an axis of n pairs."""
+        return cls(pairs, [base ** (-i / n) for n in pairs for i in range(n)], neighbours)
 
 
 class TensorList:
@@ -545,6 +619,198 @@ class Context:
         if st:
             self._check(st)
         return dtable
+
+    # -- an image or video model's block --------------------------------------------------------------
+    def new_checkpoint(self, shape, stream=None):
+        """Memory for an activation of this shape, the last dimension its columns (its contents are what checkpoint or group_norm put
+        there)."""
+        lead, cols = tuple(shape[:-1]), int(shape[-1])
+        blocks = (cols + KEPT_BLOCK - 1) // KEPT_BLOCK
+        _need(cols >= 1, "new_checkpoint: columns")
+        like = torch.empty(0, dtype=torch.uint8, device=self.device)
+        return Checkpoint(_empty(like, lead + (KEPT_BLOCK * blocks,), torch.uint8, stream), _empty(like, lead + (blocks,), torch.uint8, stream), cols)
+
+    @staticmethod
+    def _kept_rows(x, name):
+        """(type, workers, rows, cols, step between workers, between rows) of [.., cols] whose leading dimensions come down to two."""
+        if x.dim() > 3:
+            shape, step = x.shape, x.stride()
+            for cut in range(1, x.dim() - 1):              # [a .., b ..]: each run of dimensions one
+                if all(shape[i] == 1 or step[i - 1] == step[i] * shape[i] or shape[i - 1] == 1 for i in range(1, x.dim() - 1) if i != cut):
+                    x = x.view(math.prod(shape[:cut]), math.prod(shape[cut:-1]), shape[-1])
+                    break
+            _need(x.dim() == 3, "%s: leading dimensions that come down to two of one step each", name)
+        return Context._rows(x, name)
+
+    def checkpoint(self, x, call_id=None, out=None, stream=None):
+        """Keeps x [.., cols] in 8 bits.  call_id None: rounded to nearest; a number (or CALL_FIRST_HALF, CALL_SECOND_HALF): without bias, by
+        draws of that call."""
+        code, wk, rows, cols, xw, xr = self._kept_rows(x, "x")
+        if out is None:
+            out = self.new_checkpoint(x.shape, stream)
+        _need(out.shape == x.shape and out.codes.get_device() == x.get_device(), "out: a checkpoint of x's shape, on its device")
+        _need(call_id is None or 0 <= call_id < 1 << 32, "call_id: 32 bits")
+        st = self.lib.qgx_checkpoint(self._h, code, wk, rows, cols, x.data_ptr(), xw, xr, call_id is not None, call_id or 0, out._ref, _handle(stream, x))
+        if st:
+            self._check(st)
+        return out
+
+    def restore(self, kept: Checkpoint, dtype=torch.float32, out=None, stream=None):
+        """The kept elements, rounded once to dtype."""
+        cols = kept.shape[-1]
+        if out is None:
+            out = _empty(kept.codes, kept.shape, dtype, stream)
+        _need(out.shape == kept.shape and out.dtype in DTYPES and out.get_device() == kept.codes.get_device(), "out: of the kept shape, on its device")
+        step = cols
+        if not out.is_contiguous():
+            _need(out.dim() == 2 and out.stride(1) == 1, "out: contiguous, or [rows, cols] with contiguous rows")
+            step = out.stride(0)
+        st = self.lib.qgx_restore(self._h, kept._ref, DTYPES[out.dtype], out.data_ptr(), step, _handle(stream, out))
+        if st:
+            self._check(st)
+        return out
+
+    def weight_gradient(self, kept: Checkpoint, dy, dw, db=None, stream=None):
+        """Gradients of x W + b from the kept x [workers, rows, cols] and dy [workers, rows, out] (or both without workers): dw float32
+        [workers, cols, out] and db [workers, out], runs of V's rows say, are written.  Returns dw."""
+        code, wk, rows, out, gw, gr = self._rows(dy, "dy")
+        cols = kept.shape[-1]
+        _need(dy.dim() >= 2 and kept.shape[:-1] == dy.shape[:-1] and kept.codes.get_device() == dy.get_device(), "dy: [.., out] of the kept rows, on their device")
+        lead = dy.shape[:-2]
+        _need(dw is not None, "dw: where the gradient goes")
+        for t, shape, name in ((dw, lead + (cols, out), "dw"), (db, lead + (out,), "db")):
+            if t is None:
+                continue
+            _need(t.get_device() == dy.get_device() and t.dtype == torch.float32 and t.shape == shape and (wk == 0 or (t[0] if lead else t).is_contiguous()),
+                  "%s: float32 of shape %s, each worker's contiguous, on dy's device", name, tuple(shape))
+        need, scratch = self._need_bytes, None
+        st = self.lib.qgx_weight_gradient_scratch(self._h, code, wk, rows, cols, out, self._need_ref)
+        if not st:
+            if need.value:
+                scratch = _empty(dy, (need.value,), torch.uint8, stream)
+            st = self.lib.qgx_weight_gradient(self._h, kept._ref, code, wk, rows, out, dy.data_ptr(), gw, gr, dw.data_ptr(), dw.stride(0) if lead else 0,
+                                              None if db is None else db.data_ptr(), db.stride(0) if lead and db is not None else 0, None if scratch is None else scratch.data_ptr(), need.value, _handle(stream, dy))
+        if st:
+            self._check(st)
+        return dw
+
+    @staticmethod
+    def _places(t, like, name):
+        """Address and steps of [workers, batch, places, channels], [batch, places, channels] or [places, channels]."""
+        _need(t.shape == like.shape and t.dtype == like.dtype and t.get_device() == like.get_device(), "%s: of x's shape and type, on its device", name)
+        step = t.stride()
+        n = len(step)
+        _need(2 <= n <= 4 and (step[-1] == 1 or t.shape[-1] <= 1), "%s: [workers, batch, places, channels], channels contiguous", name)
+        return _Places(t.data_ptr(), step[0] if n == 4 else 0, step[-3] if n > 2 else 0, step[-2])
+
+    @staticmethod
+    def _group_shape(t, groups, activation, slope, name):
+        code, sh = DTYPES.get(t.dtype), t.shape
+        _need(code is not None and t.is_cuda, "%s: float32, float16 or bfloat16 on the GPU", name)
+        _need(2 <= len(sh) <= 4, "%s: [workers, batch, places, channels], [batch, places, channels] or [places, channels]", name)
+        _need(activation in ACTIVATIONS, "activation: one of %s", ", ".join(ACTIVATIONS))
+        _need(0 < groups < 1 << 32 and sh[-1] % groups == 0, "groups: a divisor of the channels")
+        return _GroupShape(code, ACTIVATIONS[activation], slope, groups, sh[0] if len(sh) == 4 else 1, sh[-3] if len(sh) > 2 else 1, sh[-2], sh[-1])
+
+    def _group_scratch(self, shape, backward, like, stream):
+        st = self.lib.qgx_group_norm_scratch(self._h, C.addressof(shape), backward, self._need_ref)
+        if st:
+            self._check(st)
+        return _empty(like, (self._need_bytes.value,), torch.uint8, stream) if self._need_bytes.value else None
+
+    def group_norm(self, x, groups, weight=None, bias=None, eps=1e-5, activation="none", slope=0.01, keep=None, call_id=None, out=None, save=True,
+                   stream=None):
+        """Group norm of x [workers, batch, places, channels] (or without workers, or without both) and an activation: "none", "silu",
+        "leaky" (slope).  Returns (y, mean, rstd), the last two [.., groups] for the backward pass (save=False: None).  keep: a
+        Checkpoint in which x is kept as well, as checkpoint(x, call_id) would."""
+        shape = self._group_shape(x, groups, activation, slope, "x")
+        channels = x.shape[-1]
+        src = self._places(x, x, "x")
+        w, b = _parameter(weight, (channels,), "weight"), _parameter(bias, (channels,), "bias")
+        if out is None:
+            out = _empty_like(x, stream)
+        dst = self._places(out, x, "out")
+        _need(keep is None or (keep.shape == x.shape and keep.codes.get_device() == x.get_device()), "keep: a checkpoint of x's shape, on its device")
+        _need(call_id is None or 0 <= call_id < 1 << 32, "call_id: 32 bits")
+        mean = rstd = None
+        if save:
+            mean, rstd = _empty(x, (2,) + x.shape[:-2] + (groups,), torch.float32, stream).unbind(0)
+        scratch = self._group_scratch(shape, 0, x, stream)
+        st = self.lib.qgx_group_norm(self._h, C.addressof(shape), C.addressof(src), w, b, eps, C.addressof(dst), mean.data_ptr() if save else None,
+                                     rstd.data_ptr() if save else None, None if keep is None else keep._ref, call_id is not None, call_id or 0,
+                                     None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel(), _handle(stream, x))
+        if st:
+            self._check(st)
+        return out, mean, rstd
+
+    def group_norm_backward(self, dy, x, groups, weight, bias, mean, rstd, activation="none", slope=0.01, dw=None, db=None, dx=None, need_dx=True,
+                            stream=None):
+        """Returns dx (None with need_dx=False) and writes the workers' weight and bias gradients to dw and db, float32 [workers, channels], runs
+        of V's rows say ([channels] where dy has no worker dimension).  x: the forward pass's input, or a Checkpoint of it."""
+        shape = self._group_shape(dy, groups, activation, slope, "dy")
+        channels, wk = dy.shape[-1], shape.workers
+        grad = self._places(dy, dy, "dy")
+        src = None
+        if isinstance(x, Checkpoint):
+            _need(x.shape == dy.shape and x.codes.get_device() == dy.get_device(), "x: a checkpoint of dy's shape, on its device")
+        else:
+            src = self._places(x, dy, "x")
+        w, b = _parameter(weight, (channels,), "weight"), _parameter(bias, (channels,), "bias")
+        lead = dy.shape[:-2] + (groups,)
+        m, r = _parameter(mean, lead, "mean"), _parameter(rstd, lead, "rstd")
+        step = None
+        for t, name in ((dw, "dw"), (db, "db")):
+            if t is None:
+                continue
+            _need(t.get_device() == dy.get_device() and t.dtype == torch.float32 and t.shape == (dy.shape[:1] if dy.dim() == 4 else ()) + (channels,) and _dense_last(t),
+                  "%s: float32 [workers, channels] on dy's device", name)
+            s = t.stride(0) if wk > 1 else channels
+            _need(step is None or step == s, "dw and db: one step between workers")
+            step = s
+        dst = None
+        if dx is not None:
+            dst = self._places(dx, dy, "dx")
+        elif need_dx:
+            dx = _empty_like(dy, stream)
+            dst = self._places(dx, dy, "dx")
+        scratch = self._group_scratch(shape, 1, dy, stream)
+        st = self.lib.qgx_group_norm_backward(
+            self._h, C.addressof(shape), C.addressof(grad), None if src is None else C.addressof(src), x._ref if src is None else None, w, b, m, r,
+            None if dst is None else C.addressof(dst), None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
+            channels if step is None else step, None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel(), _handle(stream, dy))
+        if st:
+            self._check(st)
+        return dx
+
+    @staticmethod
+    def _heads(t, name):
+        """[workers, batch, tokens, heads, dim], [batch, tokens, heads, dim] or [tokens, heads, dim], a head's elements contiguous."""
+        code, sh, st = DTYPES.get(t.dtype), t.shape, t.stride()
+        _need(code is not None and t.is_cuda, "%s: float32, float16 or bfloat16 on the GPU", name)
+        n = len(sh)
+        _need(3 <= n <= 5 and (st[-1] == 1 or sh[-1] <= 1), "%s: [workers, batch, tokens, heads, dim], the last dimension contiguous", name)
+        _need(sh[-2] < 1 << 32 and sh[-1] < 1 << 32, "%s: too many heads or elements", name)
+        return _Heads(t.data_ptr(), code, sh[-2], sh[-1], sh[0] if n == 5 else 1, sh[-4] if n > 3 else 1, sh[-3], st[0] if n == 5 else 0,
+                      st[-4] if n > 3 else 0, st[-3], st[-2])
+
+    def rotary(self, x, rotary: Rotary, positions, back=False, out=None, stream=None):
+        """x [.., batch, tokens, heads, dim] turned by its tokens' positions, int32 [axes, tokens] (the same for all sequences) or [axes, ..,
+        tokens] of x's leading dimensions.  back: by the angles' negatives, the backward pass.  out may be x."""
+        src = self._heads(x, "x")
+        _need(rotary.pairs is not None and 2 * sum(rotary.pairs) <= x.shape[-1], "rotary: more pairs than a head has")
+        if out is None:
+            out = _empty_like(x, stream)
+        _need(out.shape == x.shape and out.dtype == x.dtype and out.get_device() == x.get_device(), "out: of x's shape and type, on its device")
+        dst = self._heads(out, "out")
+        ps, pst, axes = positions.shape, positions.stride(), len(rotary.pairs)
+        _need(positions.get_device() == x.get_device() and positions.dtype == torch.int32 and (ps == (axes, x.shape[-3]) or ps == (axes,) + x.shape[:-2]) and
+              (ps[-1] <= 1 or pst[-1] == 1), "positions: int32 [axes, tokens] or [axes, .., tokens], tokens contiguous, on x's device")
+        whole = len(ps) > 2
+        st = self.lib.qgx_rotate(self._h, rotary._ref, positions.data_ptr(), pst[0], pst[1] if len(ps) == 4 else 0, pst[-2] if whole else 0,
+                                 C.addressof(src), C.addressof(dst), back, _handle(stream, x))
+        if st:
+            self._check(st)
+        return out
 
     # -- DEQ o CODE and the fused updates ---------------------------------------------------------
     def decode(self, st: Stream, out=None, stream=None):

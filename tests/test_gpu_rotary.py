@@ -1,0 +1,230 @@
+"""Rotary positions with several axes (qgx_rotate) against the formula in 64 bits.
+
+Bound: with u = 2^-24, the angle is off by the product's rounding in binary64 (2^-53 of it, 1e-9 at 2^23 radians; below 2 u up to 2^29) and sine and
+cosine by 4 u in all; a product by one more u, the sum by one u of the result: |out - exact| <= 6 u (|a| + |b|) + u |out|, then the rounding to the
+type (and half the type's smallest number)."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+ROUND = {"f32": U, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 2.0 ** -149, "f16": 2.0 ** -25, "bf16": 2.0 ** -134}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2308_09187_amd import qgx as m
+    c = m.Context(1024, 1, 256)
+    yield c
+    c.close()
+
+
+def exact(x, pairs, freq, neighbours, positions, back):
+    """x [.., tokens, heads, dim], positions [axes, .., tokens] or [axes, tokens], numpy in 64 bits: the result, and |a| + |b| of each place."""
+    P = sum(pairs)
+    axis = np.repeat(np.arange(len(pairs)), pairs)
+    angle = np.moveaxis(positions.astype(np.float64)[axis], 0, -1) * np.array(freq)
+    if back:
+        angle = -angle
+    c, s = np.cos(angle)[..., None, :], np.sin(angle)[..., None, :]
+    out, size = x.copy(), np.zeros_like(x)
+    i = (slice(0, 2 * P, 2), slice(1, 2 * P, 2)) if neighbours else (slice(0, P), slice(P, 2 * P))
+    a, b = x[..., i[0]], x[..., i[1]]
+    out[..., i[0]], out[..., i[1]] = a * c - b * s, a * s + b * c
+    size[..., i[0]] = size[..., i[1]] = np.abs(a) + np.abs(b)
+    return out, size
+
+
+def check(x, got, rotary, positions, back, typ):
+    want, size = exact(x.double().cpu().numpy(), rotary.pairs, list(rotary.frequencies), rotary.neighbours, positions.cpu().numpy(), back)
+    err = 6 * U * size + U * np.abs(want)
+    err = np.where(size == 0, 0.0, err + ROUND[typ] * (np.abs(want) + err) + TINY[typ])
+    assert (np.abs(got.double().cpu().numpy() - want) <= err).all()
+
+
+def make(seed, shape, typ):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda").to(TYPES[typ])
+
+
+def places(seed, shape, most=1000):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed + 99)
+    return torch.randint(-most, most, shape, generator=g, device="cuda", dtype=torch.int32)
+
+
+HEADS = [((1,), 2), ((3,), 6), ((3,), 9), ((4, 4), 16), ((5, 4), 19), ((2, 0, 5), 17), ((22, 21, 21), 128), ((16, 24, 24), 130), ((1, 2, 3, 4), 33),
+         ((64, 96, 96), 512), ((256,), 513), ((8,), 1000)]
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("neighbours", [False, True])
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("pairs,dim", HEADS)
+def test_heads(ctx, pairs, dim, typ, neighbours, back):
+    from paper_2308_09187_amd import qgx
+    r = qgx.Rotary.by_base(pairs, neighbours=neighbours)
+    x = make(dim, (2, 5, 3, dim), typ)
+    p = places(dim, (len(pairs), 2, 5))
+    check(x, ctx.rotary(x, r, p, back=back), r, p, back, typ)
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 1, 1), (1, 1, 700, 1), (1, 64, 1, 16), (3, 2, 17, 5), (2, 1, 4100, 2), (1, 3, 33, 70), (1, 1, 1, 3000)])
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_shapes_and_shared_positions(ctx, shape, neighbours):
+    from paper_2308_09187_amd import qgx
+    r = qgx.Rotary.by_base((6, 5, 5), 100.0, neighbours)
+    x = make(1, shape + (36,), "bf16")
+    p = places(2, (3, shape[2]))
+    check(x, ctx.rotary(x, r, p), r, p.view(3, 1, 1, -1).expand((3,) + shape[:3]), False, "bf16")
+    p = places(3, (3,) + shape[:3])
+    check(x, ctx.rotary(x, r, p), r, p, False, "bf16")
+    if shape[0] == 1:
+        check(x[0], ctx.rotary(x[0], r, p[:, 0]), r, p[:, 0], False, "bf16")
+        check(x[0, 0], ctx.rotary(x[0, 0], r, p[:, 0, 0]), r, p[:, 0, 0], False, "bf16")
+
+
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_in_place_strides_and_odd_addresses(ctx, neighbours, typ):
+    from paper_2308_09187_amd import qgx
+    r = qgx.Rotary.by_base((5, 4), neighbours=neighbours)
+    whole = make(4, (2, 3, 9, 8, 29), typ)
+    p = places(5, (2, 3, 9))
+    x = whole[0, :, :, 1:6, 3:26]                          # heads of a packed projection, 23 elements at odd places
+    want = ctx.rotary(x.contiguous(), r, p)
+    check(x, want, r, p, False, typ)
+    assert torch.equal(ctx.rotary(x, r, p), want)
+    heads_first = x.transpose(1, 2).contiguous().transpose(1, 2)
+    assert torch.equal(ctx.rotary(heads_first, r, p), want)
+    out = torch.full((3, 5, 9, 40), 3.0, device="cuda", dtype=TYPES[typ])
+    ctx.rotary(x, r, p, out=out.transpose(1, 2)[..., 7:30])
+    assert torch.equal(out.transpose(1, 2)[..., 7:30], want) and bool((out[..., :7] == 3).all()) and bool((out[..., 30:] == 3).all())
+    before = whole.clone()
+    ctx.rotary(x, r, p, out=x)
+    assert torch.equal(x, want)
+    before[0, :, :, 1:6, 3:26] = want
+    assert torch.equal(whole, before)
+    assert torch.equal(ctx.rotary(x[:1].expand(3, 9, 5, 23), r, p[:, :1].expand(2, 3, 9)), ctx.rotary(x[:1].contiguous(), r, p[:, :1].contiguous()).expand(3, 9, 5, 23))
+
+
+def test_far_positions_and_their_ends(ctx):
+    """Positions of all 31 bits: the angle in binary64, reduced there, is good to 2^31 2^-53 = 2.4e-7 radians, 4 u."""
+    from paper_2308_09187_amd import qgx
+    r = qgx.Rotary((2, 2), [1.0, 1e-4, 0.37, 0.0])
+    p = torch.tensor([[0, 1, (1 << 31) - 1, -(1 << 31), 1 << 24, 123456789], [5, -5, (1 << 31) - 1, -(1 << 31), -(1 << 24), 987654321]], dtype=torch.int32, device="cuda")
+    x = make(6, (6, 2, 8), "f32")
+    got = ctx.rotary(x, r, p).double().cpu().numpy()
+    want, size = exact(x.double().cpu().numpy(), r.pairs, list(r.frequencies), False, p.cpu().numpy(), False)
+    assert (np.abs(got - want) <= 12 * U * size).all()
+    assert np.array_equal(got[..., 3], x[..., 3].double().cpu().numpy()) and np.array_equal(got[0, :, :2], x[0, :, :2].double().cpu().numpy())
+
+
+@pytest.mark.parametrize("typ", TYPES)
+def test_back_is_the_transpose_and_the_inverse(ctx, typ):
+    """<rotary(x), dy> = <x, rotary(dy, back)>, and differences: the map is linear, so a step along dx changes the loss by <x's step, dx>."""
+    from paper_2308_09187_amd import qgx
+    r = qgx.Rotary.by_base((7, 7, 6), neighbours=True)
+    x, dy, p = make(7, (2, 11, 3, 44), typ), make(8, (2, 11, 3, 44), typ), places(9, (3, 2, 11))
+    dx = ctx.rotary(dy, r, p, back=True)
+    a = (ctx.rotary(x, r, p).double() * dy.double()).sum()
+    b = (x.double() * dx.double()).sum()
+    size = float((x.double().abs() * (dy.double().abs().sum())).mean()) + float((x.double().norm() * dy.double().norm()))
+    assert abs(float(a - b)) <= (2 * ROUND[typ] + 16 * U) * 2 * size
+    y = ctx.rotary(x, r, p)
+    back = ctx.rotary(y, r, p, back=True).double()
+    pair = torch.sqrt(x.double()[..., 0:40:2] ** 2 + x.double()[..., 1:40:2] ** 2).repeat_interleave(2, -1)
+    assert bool(((back - x.double())[..., :40].abs() <= (3 * ROUND[typ] + 24 * U) * pair + 4 * TINY[typ]).all()) and torch.equal(back[..., 40:], x.double()[..., 40:])
+
+
+def test_no_numbers_stay_in_their_pair(ctx):
+    from paper_2308_09187_amd import qgx
+    r = qgx.Rotary.by_base((4,))
+    x = make(10, (3, 2, 10), "bf16")
+    p = places(11, (1, 3))
+    clean = ctx.rotary(x, r, p)
+    x[1, 1, 2], x[2, 0, 9] = math.nan, math.inf
+    got = ctx.rotary(x, r, p)
+    bad = torch.isnan(got)
+    assert bad[1, 1, 2] and bad[1, 1, 6] and int(bad.sum()) == 2 and float(got[2, 0, 9]) == math.inf
+    keep = ~bad
+    keep[2, 0, 9] = False
+    assert torch.equal(got[keep], clean[keep])
+
+
+def test_offsets_beyond_32_bits(ctx):
+    """A cache of more than 2^32 bytes: its last tokens turned in place, all others left."""
+    from paper_2308_09187_amd import qgx
+    r = qgx.Rotary.by_base((16,))
+    cache = torch.zeros(3, (1 << 24), 2, 32, device="cuda", dtype=torch.bfloat16)      # 6 GiB
+    x = make(12, (3, 4, 2, 32), "bf16")
+    cache[:, -4:] = x
+    p = places(13, (1, 3, 4))
+    ctx.rotary(cache[:, -4:], r, p, out=cache[:, -4:])
+    assert torch.equal(cache[:, -4:], ctx.rotary(x, r, p)) and float(cache[:, -8:-4].abs().max()) == 0
+    del cache
+    torch.cuda.empty_cache()
+
+
+def test_nothing_to_do_streams_and_graphs(ctx):
+    from paper_2308_09187_amd import qgx
+    r = qgx.Rotary.by_base((4, 4))
+    assert ctx.rotary(torch.zeros(2, 0, 3, 16, device="cuda"), r, torch.zeros(2, 2, 0, device="cuda", dtype=torch.int32)).shape == (2, 0, 3, 16)
+    assert ctx.rotary(torch.zeros(0, 5, 3, 16, device="cuda"), r, torch.zeros(2, 5, device="cuda", dtype=torch.int32)).shape == (0, 5, 3, 16)
+    x, p = make(14, (4, 50, 3, 16), "f32"), places(15, (2, 4, 50))
+    want = ctx.rotary(x, r, p)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = ctx.rotary(x, r, p, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    g, y = torch.cuda.CUDAGraph(), torch.empty_like(x)
+    with torch.cuda.graph(g, stream=side):
+        ctx.rotary(x, r, p, out=y, stream=side)
+        ctx.rotary(y, r, p, back=True, out=y, stream=side)
+        ctx.rotary(y, r, p, out=y, stream=side)
+    for _ in range(3):
+        x.mul_(-1.5)
+        p.add_(7)
+        want = ctx.rotary(ctx.rotary(ctx.rotary(x, r, p), r, p, back=True), r, p)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+
+
+def test_refusals(ctx):
+    from paper_2308_09187_amd import qgx
+    r = qgx.Rotary.by_base((4, 4))
+    x, p = torch.zeros(2, 5, 3, 16, device="cuda"), torch.zeros(2, 2, 5, device="cuda", dtype=torch.int32)
+
+    def refused(f):
+        with pytest.raises(qgx.QgxError) as e:
+            f()
+        assert e.value.status == qgx.ERR_ARG and str(e.value)
+
+    refused(lambda: ctx.rotary(x.double(), r, p))
+    refused(lambda: ctx.rotary(x.cpu(), r, p))
+    refused(lambda: ctx.rotary(x[..., ::2], r, p))
+    refused(lambda: ctx.rotary(x[..., :15], r, p))
+    refused(lambda: ctx.rotary(x, r, p.long()))
+    refused(lambda: ctx.rotary(x, r, p.cpu()))
+    refused(lambda: ctx.rotary(x, r, p[:1]))
+    refused(lambda: ctx.rotary(x, r, p[:, :, :4]))
+    refused(lambda: ctx.rotary(x, r, p.transpose(1, 2).contiguous().transpose(1, 2)))
+    refused(lambda: ctx.rotary(x, r, p, out=x.bfloat16()))
+    refused(lambda: ctx.rotary(x, r, p, out=x[:1].expand(2, 5, 3, 16)))
+    refused(lambda: ctx.rotary(x, r, p, out=x[:1]))
+    y = torch.zeros(2, 3, 5, 16, device="cuda")
+    refused(lambda: ctx.rotary(y.view(2, 5, 3, 16), r, p, out=y.transpose(1, 2)))      # in place by other strides
+    refused(lambda: ctx.rotary(torch.zeros(2, 5, 3, 5000, device="cuda"), r, p))
+    refused(lambda: ctx.rotary(torch.zeros(5, 16, device="cuda"), r, p))
