@@ -416,7 +416,7 @@ struct WeightGradArgs {
     uint32_t tiles_i, tiles_o, parts, part_rows;
 };
 struct WeightGradPlan {
-    uint32_t tiles_i, tiles_o, parts, part_rows;
+    uint32_t tiles_i, tiles_o, parts, part_rows, wide;
     uint64_t scratch;           // bytes
 };
 WeightGradPlan weight_grad_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t cols, uint32_t out, uint32_t n_cu);

@@ -180,6 +180,216 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_weight_gradient(WeightGradA
     }
 }
 
+// ---- large layers ---------------------------------------------------------------------------------------------------------
+// A wave has 128 columns of X by 64 of dY, so that a byte of an operand meets many products: the matrix cores then need less of LDS and of the
+// vector units than those have.  X is decoded once for its WN waves and passes through LDS; dY goes from memory into the operand's place in
+// registers: lane c has columns 2 c and 2 c + 1, which are the columns c of two tiles, and eight rows of them, transposed in pairs.  What a
+// group of 16 rows is worked on from is loaded again for the next step as soon as it is used.
+template <typename T> struct PairAs { typedef T type __attribute__((ext_vector_type(2), aligned(sizeof(T)))); };
+template <typename T> using PairOf = typename PairAs<T>::type;
+
+template <typename T, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * kWave, 2) void k_weight_gradient_wide(WeightGradArgs a)
+{
+    constexpr int P = kGradParts<T>, kThreads = WM * WN * kWave, TM = 128 * WM, TN = 64 * WN, kOcts = kGradRows / 8;
+    constexpr int kUnits = kOcts * (TM / 4) / kThreads;    // eight rows of four columns of X, of a thread
+    constexpr int kGroups = kGradRows / 16, kAhead = sizeof(T) == 4 ? 2 : 4;     // groups of 16 rows of a step; those that are loaded ahead
+    constexpr int kPowers = TM / 32 * kGradRows / kThreads;
+    static_assert(kUnits >= 1 && kPowers >= 1, "");
+    __shared__ __align__(16) uint4 s_x[2][kOcts][TM];
+    __shared__ __align__(16) uint8_t s_power[2][TM / 32][kGradRows];
+    __shared__ float s_db[2][TN];
+    const uint32_t tiles = a.tiles_i * a.tiles_o, k = blockIdx.y;
+    const uint32_t part = blockIdx.x / tiles, tile = blockIdx.x % tiles, tile_i = tile % a.tiles_i, tile_o = tile / a.tiles_i;
+    const uint32_t row0 = part * a.part_rows, row1 = min(row0 + a.part_rows, a.rows), steps = (row1 - row0 + kGradRows - 1u) / kGradRows;
+    const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, wm = wave % WM, wn = wave / WM, c = lane % 32u, half = lane / 32u;
+    const uint64_t code_row = (uint64_t)a.blocks * 32u;
+    const uint8_t* codes0 = a.codes + (uint64_t)k * a.rows * code_row;
+    const uint8_t* powers0 = a.powers + (uint64_t)k * a.rows * a.blocks;
+    const uint32_t o = tile_o * TN + wn * 64u + 2u * c;
+    const bool edge = tile_o * TN + TN > a.out;
+    const T* dy = (const T*)a.dy + k * a.dy_worker + o;
+
+    uint32_t x[kUnits][8], next_x[kUnits][8], power[kPowers];
+    PairOf<T> d[kAhead][8];
+    auto load_codes = [&](uint32_t row) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const uint32_t unit = threadIdx.x + u * kThreads, quad = unit % (TM / 4), oct = unit / (TM / 4);
+            const uint32_t i0 = min(tile_i * TM + quad * 4u, a.blocks * 32u - 4u);
+            const uint8_t* p = codes0 + i0;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) next_x[u][r] = *reinterpret_cast<const uint32_t*>(p + min(row + oct * 8u + (uint32_t)r, row1 - 1u) * code_row);
+        }
+    };
+    auto load_powers = [&](uint32_t row) {
+#pragma unroll
+        for (int u = 0; u < kPowers; ++u) {
+            const uint32_t unit = threadIdx.x + u * kThreads, block = unit / kGradRows, at = row + unit % kGradRows;
+            power[u] = powers0[(uint64_t)min(at, row1 - 1u) * a.blocks + min(tile_i * (TM / 32) + block, a.blocks - 1u)];
+            if (at >= row1) power[u] = 0u;                 // (rows past the last: zeros)
+        }
+    };
+    auto store_powers = [&](int to) {
+#pragma unroll
+        for (int u = 0; u < kPowers; ++u) {
+            const uint32_t unit = threadIdx.x + u * kThreads;
+            s_power[to][unit / kGradRows][unit % kGradRows] = (uint8_t)power[u];
+        }
+    };
+    // rows row .. row + 15 of dY, this half's eight
+    auto load_dy = [&](uint32_t row, PairOf<T> (&v)[8]) {
+        const uint32_t first = row + half * 8u;
+        if (!edge && row + 16u <= row1) {
+            const T* p = dy + (uint64_t)first * a.dy_row;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v[r] = *reinterpret_cast<const PairOf<T>*>(p + r * a.dy_row);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const T* p = dy + (uint64_t)(first + r) * a.dy_row;
+                v[r].x = first + r < row1 && o < a.out ? p[0] : (T)0.0f;
+                v[r].y = first + r < row1 && o + 1u < a.out ? p[1] : (T)0.0f;
+            }
+        }
+    };
+    // a column of the thread's units of X, decoded, into LDS
+    auto store_column = [&](int to, int col) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const uint32_t unit = threadIdx.x + u * kThreads, quad = unit % (TM / 4), oct = unit / (TM / 4);
+            const uint2 pw = *reinterpret_cast<const uint2*>(&s_power[to][quad / 8u][oct * 8u]);
+            uint32_t v[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                v[r] = __float_as_uint(kept_value((x[u][r] >> (8 * col)) & 0xFFu, kept_scale(((r < 4 ? pw.x : pw.y) >> (8 * (r & 3))) & 0xFFu)));
+            s_x[to][oct][grad_slot(quad * 4u + col)] = make_uint4(upper_halves(v[0], v[1]), upper_halves(v[2], v[3]), upper_halves(v[4], v[5]), upper_halves(v[6], v[7]));
+        }
+    };
+    auto take_codes = [&]() {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+            for (int r = 0; r < 8; ++r) x[u][r] = next_x[u][r];
+    };
+
+    f32x16 acc[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    const bool sums = a.db && tile_i == 0 && wm == 0;
+    float db[2] = {0.0f, 0.0f};
+
+    load_powers(row0);
+    store_powers(0);
+    load_powers(row0 + kGradRows);
+    store_powers(1);
+    load_codes(row0);
+#pragma unroll
+    for (int g = 0; g < kAhead; ++g) load_dy(row0 + 16u * g, d[g]);
+    take_codes();
+    load_codes(row0 + kGradRows);
+    __syncthreads();
+#pragma unroll
+    for (int col = 0; col < 4; ++col) store_column(0, col);
+    __syncthreads();
+    for (uint32_t s = 0; s < steps; ++s) {
+        const int now = (int)(s & 1u);
+        const uint32_t row = row0 + s * kGradRows;
+        const bool more = s + 1u < steps;
+        take_codes();
+        load_codes(row + 2u * kGradRows);                  // (past the end: the last row again)
+        load_powers(row + 2u * kGradRows);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            bf16x8 v[P][2], u[4];
+            PairOf<T> (&raw)[8] = d[g % kAhead];
+            float left[2][8];
+            if constexpr (P == 1) {
+                uint32_t w[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) w[r] = __builtin_bit_cast(uint32_t, raw[r]);
+                v[0][0] = __builtin_bit_cast(bf16x8, make_uint4(__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u),
+                                                                __builtin_amdgcn_perm(w[5], w[4], 0x05040100u), __builtin_amdgcn_perm(w[7], w[6], 0x05040100u)));
+                v[0][1] = __builtin_bit_cast(bf16x8, make_uint4(upper_halves(w[0], w[1]), upper_halves(w[2], w[3]), upper_halves(w[4], w[5]), upper_halves(w[6], w[7])));
+                if (sums)
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        db[0] += __uint_as_float(w[r] << 16);
+                        db[1] += __uint_as_float(w[r] & 0xFFFF0000u);
+                    }
+            } else {
+                float most = 0.0f;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    left[0][r] = (float)raw[r].x;
+                    left[1][r] = (float)raw[r].y;
+                    most = fmaxf(fmaxf(most, fabsf(left[0][r])), fabsf(left[1][r]));
+                    if (sums) { db[0] += left[0][r]; db[1] += left[1][r]; }
+                }
+                const bool finite = most <= 3.402823466e38f;       // (a NaN may hide here, and is a NaN in every part)
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t w[8];
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) w[r] = __float_as_uint(left[j][r]);
+                        v[p][j] = __builtin_bit_cast(bf16x8, make_uint4(upper_halves(w[0], w[1]), upper_halves(w[2], w[3]), upper_halves(w[4], w[5]), upper_halves(w[6], w[7])));
+                        if (p + 1 < P)
+#pragma unroll
+                            for (int r = 0; r < 8; ++r) {
+                                left[j][r] = left[j][r] - __uint_as_float(w[r] & 0xFFFF0000u);
+                                if (!finite && (w[r] & 0x7FFFFFFFu) == 0x7F800000u) left[j][r] = 0.0f;    // (of an infinity nothing is left)
+                            }
+                    }
+            }
+            {
+                // the group's next rows
+                const uint32_t next = row + 16u * (g + kAhead);
+                if (next < row1) load_dy(next, raw);
+                else
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) raw[r] = PairOf<T>{(T)0.0f, (T)0.0f};
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = __builtin_bit_cast(bf16x8, s_x[now][2u * g + half][grad_slot(wm * 128u + 32u * i + c)]);
+            if (more) store_column(now ^ 1, g);            // (of the next step, whose powers are there since the last barrier)
+#pragma unroll
+            for (int p = P - 1; p >= 0; --p)               // (the smallest first)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u[i], v[p][j], acc[i][j], 0, 0, 0);
+        }
+        store_powers(now);                                 // (of step s + 2; this step's were read before the last barrier)
+        __syncthreads();
+    }
+    float* dw = a.parts == 1u ? a.dw + k * a.dw_worker : a.scratch + ((uint64_t)k * a.parts + part) * ((uint64_t)a.cols * a.out + a.out);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const uint32_t row = tile_i * TM + wm * 128u + 32u * i + 8u * (e / 4) + 4u * half + (e % 4);
+            if (row >= a.cols) continue;
+            float* to = dw + (uint64_t)row * a.out + o;
+            if (o + 1u < a.out) *reinterpret_cast<PairOf<float>*>(to) = PairOf<float>{acc[i][0][e], acc[i][1][e]};
+            else if (o < a.out) to[0] = acc[i][0][e];
+        }
+    if (!a.db || tile_i != 0) return;
+    if (wm == 0) {
+        s_db[half][wn * 64u + 2u * c] = db[0];
+        s_db[half][wn * 64u + 2u * c + 1u] = db[1];
+    }
+    __syncthreads();
+    float* to = a.parts == 1u ? a.db + k * a.db_worker : dw + (uint64_t)a.cols * a.out;
+    for (uint32_t i = threadIdx.x; i < TN; i += kThreads)
+        if (tile_o * TN + i < a.out) to[tile_o * TN + i] = s_db[0][i] + s_db[1][i];
+}
+
 // The parts' sums, joined in order.
 __global__ __launch_bounds__(256) void k_weight_gradient_join(WeightGradArgs a)
 {
@@ -208,14 +418,15 @@ WeightGradPlan weight_grad_plan(int dtype, uint32_t workers, uint32_t rows, uint
 {
     (void)dtype;
     WeightGradPlan p{};
-    p.tiles_i = (cols + kGradTile - 1u) / kGradTile;
-    p.tiles_o = (out + kGradTile - 1u) / kGradTile;
+    p.wide = cols > 128u && out > 128u;
+    p.tiles_i = p.wide ? (cols + 255u) / 256u : (cols + kGradTile - 1u) / kGradTile;
+    p.tiles_o = p.wide ? (out + 255u) / 256u : (out + kGradTile - 1u) / kGradTile;
     p.parts = 1;
     p.part_rows = rows;
     if (workers == 0 || rows == 0) return p;
     const uint64_t tiles = (uint64_t)workers * p.tiles_i * p.tiles_o;
     const uint32_t most = (rows + 255u) / 256u;
-    const uint32_t want = (uint32_t)min((uint64_t)most, max((uint64_t)1u, 2u * n_cu / tiles));
+    const uint32_t want = (uint32_t)min((uint64_t)most, max((uint64_t)1u, (p.wide ? 1u : 2u) * n_cu / tiles));
     p.part_rows = ((rows + want - 1u) / want + kGradRows - 1u) / kGradRows * kGradRows;
     p.parts = (rows + p.part_rows - 1u) / p.part_rows;
     if (p.parts > 1u) p.scratch = (uint64_t)workers * p.parts * ((uint64_t)cols * out + out) * sizeof(float);
@@ -234,7 +445,12 @@ hipError_t launch_weight_grad(int dtype, const WeightGradArgs& args, uint32_t wo
         return hipGetLastError();
     }
     const dim3 grid(a.tiles_i * a.tiles_o * a.parts, workers);
-    if (dtype == QGX_F32) hipLaunchKernelGGL(k_weight_gradient<float>, grid, dim3(kGradThreads), 0, st, a);
+    if (plan.wide) {
+        const dim3 threads(512);
+        if (dtype == QGX_F32) hipLaunchKernelGGL((k_weight_gradient_wide<float, 2, 4>), grid, threads, 0, st, a);
+        else if (dtype == QGX_F16) hipLaunchKernelGGL((k_weight_gradient_wide<_Float16, 2, 4>), grid, threads, 0, st, a);
+        else hipLaunchKernelGGL((k_weight_gradient_wide<__bf16, 2, 4>), grid, threads, 0, st, a);
+    } else if (dtype == QGX_F32) hipLaunchKernelGGL(k_weight_gradient<float>, grid, dim3(kGradThreads), 0, st, a);
     else if (dtype == QGX_F16) hipLaunchKernelGGL(k_weight_gradient<_Float16>, grid, dim3(kGradThreads), 0, st, a);
     else hipLaunchKernelGGL(k_weight_gradient<__bf16>, grid, dim3(kGradThreads), 0, st, a);
     if (a.parts > 1u) hipLaunchKernelGGL(k_weight_gradient_join, each, dim3(256), 0, st, a);
