@@ -184,93 +184,140 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_weight_gradient(WeightGradA
 // A wave has 128 columns of X by 64 of dY, so that a byte of an operand meets many products: the matrix cores then need less of LDS and of the
 // vector units than those have.  X is decoded once for its WN waves and passes through LDS; dY goes from memory into the operand's place in
 // registers: lane c has columns 2 c and 2 c + 1, which are the columns c of two tiles, and eight rows of them, transposed in pairs.  What a
-// group of 16 rows is worked on from is loaded again for the next step as soon as it is used.
+// group of 16 rows is worked on from is loaded again for a later one as soon as it is used.  No branch in a step: columns past the last are the
+// last ones again (and equal numbers are stored twice), rows past the last full step are a step of their own at the end.
 template <typename T> struct PairAs { typedef T type __attribute__((ext_vector_type(2), aligned(sizeof(T)))); };
 template <typename T> using PairOf = typename PairAs<T>::type;
 
-template <typename T, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * kWave, 2) void k_weight_gradient_wide(WeightGradArgs a)
+// A signed byte of a word as a number, in one instruction.
+template <int BYTE>
+__device__ __forceinline__ float byte_value(uint32_t x)
 {
-    constexpr int P = kGradParts<T>, kThreads = WM * WN * kWave, TM = 128 * WM, TN = 64 * WN, kOcts = kGradRows / 8;
-    constexpr int kUnits = kOcts * (TM / 4) / kThreads;    // eight rows of four columns of X, of a thread
-    constexpr int kGroups = kGradRows / 16, kAhead = sizeof(T) == 4 ? 2 : 4;     // groups of 16 rows of a step; those that are loaded ahead
-    constexpr int kPowers = TM / 32 * kGradRows / kThreads;
-    static_assert(kUnits >= 1 && kPowers >= 1, "");
-    __shared__ __align__(16) uint4 s_x[2][kOcts][TM];
-    __shared__ __align__(16) uint8_t s_power[2][TM / 32][kGradRows];
-    __shared__ float s_db[2][TN];
-    const uint32_t tiles = a.tiles_i * a.tiles_o, k = blockIdx.y;
-    const uint32_t part = blockIdx.x / tiles, tile = blockIdx.x % tiles, tile_i = tile % a.tiles_i, tile_o = tile / a.tiles_i;
-    const uint32_t row0 = part * a.part_rows, row1 = min(row0 + a.part_rows, a.rows), steps = (row1 - row0 + kGradRows - 1u) / kGradRows;
-    const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, wm = wave % WM, wn = wave / WM, c = lane % 32u, half = lane / 32u;
+    float v;
+    if constexpr (BYTE == 0) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(v) : "v"(x));
+    else if constexpr (BYTE == 1) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(v) : "v"(x));
+    else if constexpr (BYTE == 2) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(v) : "v"(x));
+    else asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(v) : "v"(x));
+    return v;
+}
+
+template <int C> struct Column { static constexpr int value = C; };
+
+template <typename T, int WM, int WN>
+struct WideGradient {
+    static constexpr int P = kGradParts<T>, kThreads = WM * WN * kWave, TM = 128 * WM, TN = 64 * WN, kOcts = kGradRows / 8;
+    static constexpr int kUnits = kOcts * (TM / 4) / kThreads;                   // eight rows of four columns of X, of a thread
+    static constexpr int kGroups = kGradRows / 16;                               // groups of 16 rows of a step
+    static constexpr int kAhead = P == 1 ? 4 : P == 2 ? 2 : 1;                   // groups that are loaded ahead (P products from each)
+    static constexpr int kPowers = TM / 32 * kGradRows / kThreads;
+    static_assert(kUnits >= 1 && kPowers >= 1 && kGroups % kAhead == 0, "");
+
+    struct Shared {
+        uint4 x[2][kOcts][TM];
+        float scale[2][TM / 32][kGradRows];
+        float db[2][TN];
+    };
+};
+
+template <typename T, int WM, int WN, bool SUMS>
+__device__ __forceinline__ void weight_gradient_tile(const WeightGradArgs& a, typename WideGradient<T, WM, WN>::Shared& sh, uint32_t k, uint32_t part, uint32_t tile_i, uint32_t tile_o)
+{
+    typedef WideGradient<T, WM, WN> G;
+    constexpr int P = G::P, kThreads = G::kThreads, TM = G::TM, TN = G::TN, kUnits = G::kUnits, kAhead = G::kAhead;
+    const uint32_t row0 = part * a.part_rows, row1 = min(row0 + a.part_rows, a.rows), full = (row1 - row0) / kGradRows;
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = threadIdx.x % kWave;
+    const uint32_t wm = wave % WM, wn = wave / WM, c = lane % 32u, half = lane / 32u;
     const uint64_t code_row = (uint64_t)a.blocks * 32u;
     const uint8_t* codes0 = a.codes + (uint64_t)k * a.rows * code_row;
     const uint8_t* powers0 = a.powers + (uint64_t)k * a.rows * a.blocks;
-    const uint32_t o = tile_o * TN + wn * 64u + 2u * c;
-    const bool edge = tile_o * TN + TN > a.out;
-    const T* dy = (const T*)a.dy + k * a.dy_worker + o;
+    const uint32_t o = tile_o * TN + wn * 64u + 2u * c, oc = min(o, a.out - 2u);
+    const T* dy0 = (const T*)a.dy + k * a.dy_worker;
+    const uint64_t dy_row = a.dy_row;
 
-    uint32_t x[kUnits][8], next_x[kUnits][8], power[kPowers];
+    // a thread's offsets from a step's first row (32 bits: the caller has seen to that)
+    uint32_t x_at[kUnits], p_at[G::kPowers];
+    uint32_t to_at[kUnits], scale_at[kUnits];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const uint32_t unit = threadIdx.x + u * kThreads, quad = unit % (TM / 4), oct = unit / (TM / 4);
+        x_at[u] = oct * 8u * (uint32_t)code_row + min(tile_i * TM + quad * 4u, a.blocks * 32u - 4u);
+        to_at[u] = oct * TM;
+        scale_at[u] = quad / 8u * kGradRows + oct * 8u;
+    }
+#pragma unroll
+    for (int u = 0; u < G::kPowers; ++u) {
+        const uint32_t unit = threadIdx.x + u * kThreads;
+        p_at[u] = unit % kGradRows * a.blocks + min(tile_i * (TM / 32) + unit / kGradRows, a.blocks - 1u);
+    }
+    uint32_t x[kUnits][8], next_x[kUnits][8];
+    float scale[G::kPowers];
     PairOf<T> d[kAhead][8];
-    auto load_codes = [&](uint32_t row) {
+    // of the step at `row`, all of whose rows are there: rows' addresses are the wave's, a thread's own part is 32 bits beside them
+    struct Rows { const uint8_t* p[8]; };
+    auto code_rows = [&](uint32_t row) {
+        Rows b;
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const uint32_t unit = threadIdx.x + u * kThreads, quad = unit % (TM / 4), oct = unit / (TM / 4);
-            const uint32_t i0 = min(tile_i * TM + quad * 4u, a.blocks * 32u - 4u);
-            const uint8_t* p = codes0 + i0;
+        for (int r = 0; r < 8; ++r) b.p[r] = codes0 + (uint64_t)(row + (uint32_t)r) * code_row;
+        return b;
+    };
+    auto dy_rows = [&](uint32_t row) {
+        Rows b;
 #pragma unroll
-            for (int r = 0; r < 8; ++r) next_x[u][r] = *reinterpret_cast<const uint32_t*>(p + min(row + oct * 8u + (uint32_t)r, row1 - 1u) * code_row);
-        }
+        for (int r = 0; r < 8; ++r) b.p[r] = reinterpret_cast<const uint8_t*>(dy0 + (uint64_t)(row + (uint32_t)r) * dy_row);
+        return b;
+    };
+    auto advance = [&](Rows& b, uint64_t bytes) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) b.p[r] += bytes;
+    };
+    auto load_codes = [&](const Rows& b) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) next_x[u][r] = *reinterpret_cast<const uint32_t*>(b.p[r] + x_at[u]);
     };
     auto load_powers = [&](uint32_t row) {
+        const uint8_t* p = powers0 + (uint64_t)row * a.blocks;
 #pragma unroll
-        for (int u = 0; u < kPowers; ++u) {
-            const uint32_t unit = threadIdx.x + u * kThreads, block = unit / kGradRows, at = row + unit % kGradRows;
-            power[u] = powers0[(uint64_t)min(at, row1 - 1u) * a.blocks + min(tile_i * (TM / 32) + block, a.blocks - 1u)];
-            if (at >= row1) power[u] = 0u;                 // (rows past the last: zeros)
-        }
+        for (int u = 0; u < G::kPowers; ++u) scale[u] = kept_scale(p[p_at[u]]);
     };
-    auto store_powers = [&](int to) {
+    // its rows 16 g .. 16 g + 15 of dY
+    uint32_t dy_at[G::kGroups];
 #pragma unroll
-        for (int u = 0; u < kPowers; ++u) {
+    for (int g = 0; g < G::kGroups; ++g) dy_at[g] = (uint32_t)((16u * g + half * 8u) * dy_row * sizeof(T)) + oc * (uint32_t)sizeof(T);
+    auto load_dy = [&](const Rows& b, int g, PairOf<T> (&v)[8]) {
+        uint32_t at = dy_at[g];
+        asm volatile("" : "+v"(at));                       // (else the lane's part is added to the rows' in 64 bits beforehand)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = *reinterpret_cast<const PairOf<T>*>(b.p[r] + at);
+    };
+    auto store_scales = [&](int to) {
+#pragma unroll
+        for (int u = 0; u < G::kPowers; ++u) {
             const uint32_t unit = threadIdx.x + u * kThreads;
-            s_power[to][unit / kGradRows][unit % kGradRows] = (uint8_t)power[u];
-        }
-    };
-    // rows row .. row + 15 of dY, this half's eight
-    auto load_dy = [&](uint32_t row, PairOf<T> (&v)[8]) {
-        const uint32_t first = row + half * 8u;
-        if (!edge && row + 16u <= row1) {
-            const T* p = dy + (uint64_t)first * a.dy_row;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) v[r] = *reinterpret_cast<const PairOf<T>*>(p + r * a.dy_row);
-        } else {
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const T* p = dy + (uint64_t)(first + r) * a.dy_row;
-                v[r].x = first + r < row1 && o < a.out ? p[0] : (T)0.0f;
-                v[r].y = first + r < row1 && o + 1u < a.out ? p[1] : (T)0.0f;
-            }
+            sh.scale[to][unit / kGradRows][unit % kGradRows] = scale[u];
         }
     };
     // a column of the thread's units of X, decoded, into LDS
-    auto store_column = [&](int to, int col) {
+    auto store_column = [&](int to, auto column) {
+        constexpr int col = decltype(column)::value;
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
-            const uint32_t unit = threadIdx.x + u * kThreads, quad = unit % (TM / 4), oct = unit / (TM / 4);
-            const uint2 pw = *reinterpret_cast<const uint2*>(&s_power[to][quad / 8u][oct * 8u]);
+            const float* sc = &sh.scale[to][0][0] + scale_at[u];
+            const float4 lo = *reinterpret_cast<const float4*>(sc), hi = *reinterpret_cast<const float4*>(sc + 4);
+            const float f[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
             uint32_t v[8];
 #pragma unroll
-            for (int r = 0; r < 8; ++r)
-                v[r] = __float_as_uint(kept_value((x[u][r] >> (8 * col)) & 0xFFu, kept_scale(((r < 4 ? pw.x : pw.y) >> (8 * (r & 3))) & 0xFFu)));
-            s_x[to][oct][grad_slot(quad * 4u + col)] = make_uint4(upper_halves(v[0], v[1]), upper_halves(v[2], v[3]), upper_halves(v[4], v[5]), upper_halves(v[6], v[7]));
+            for (int r = 0; r < 8; ++r) v[r] = __float_as_uint(byte_value<col>(x[u][r]) * f[r]);
+            const uint32_t quad = (threadIdx.x + u * kThreads) % (TM / 4);
+            (&sh.x[to][0][0])[to_at[u] + grad_slot(quad * 4u + col)] = make_uint4(upper_halves(v[0], v[1]), upper_halves(v[2], v[3]), upper_halves(v[4], v[5]), upper_halves(v[6], v[7]));
         }
     };
     auto take_codes = [&]() {
 #pragma unroll
         for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-            for (int r = 0; r < 8; ++r) x[u][r] = next_x[u][r];
+            for (int r = 0; r < 8; ++r) x[u][r] = next_x[u][r] ^ 0x80808080u;          // (code - 128 as signed bytes)
     };
 
     f32x16 acc[4][2];
@@ -280,93 +327,151 @@ __global__ __launch_bounds__(WM * WN * kWave, 2) void k_weight_gradient_wide(Wei
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    const bool sums = a.db && tile_i == 0 && wm == 0;
     float db[2] = {0.0f, 0.0f};
 
-    load_powers(row0);
-    store_powers(0);
-    load_powers(row0 + kGradRows);
-    store_powers(1);
-    load_codes(row0);
+    // the operands of 16 rows of dY, P parts of two tiles
+    auto operands = [&](const PairOf<T> (&raw)[8], bf16x8 (&v)[P][2]) {
+        if constexpr (P == 1) {
+            uint32_t w[8];
 #pragma unroll
-    for (int g = 0; g < kAhead; ++g) load_dy(row0 + 16u * g, d[g]);
-    take_codes();
-    load_codes(row0 + kGradRows);
-    __syncthreads();
-#pragma unroll
-    for (int col = 0; col < 4; ++col) store_column(0, col);
-    __syncthreads();
-    for (uint32_t s = 0; s < steps; ++s) {
-        const int now = (int)(s & 1u);
-        const uint32_t row = row0 + s * kGradRows;
-        const bool more = s + 1u < steps;
-        take_codes();
-        load_codes(row + 2u * kGradRows);                  // (past the end: the last row again)
-        load_powers(row + 2u * kGradRows);
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            bf16x8 v[P][2], u[4];
-            PairOf<T> (&raw)[8] = d[g % kAhead];
-            float left[2][8];
-            if constexpr (P == 1) {
-                uint32_t w[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r) w[r] = __builtin_bit_cast(uint32_t, raw[r]);
-                v[0][0] = __builtin_bit_cast(bf16x8, make_uint4(__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u),
-                                                                __builtin_amdgcn_perm(w[5], w[4], 0x05040100u), __builtin_amdgcn_perm(w[7], w[6], 0x05040100u)));
-                v[0][1] = __builtin_bit_cast(bf16x8, make_uint4(upper_halves(w[0], w[1]), upper_halves(w[2], w[3]), upper_halves(w[4], w[5]), upper_halves(w[6], w[7])));
-                if (sums)
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        db[0] += __uint_as_float(w[r] << 16);
-                        db[1] += __uint_as_float(w[r] & 0xFFFF0000u);
-                    }
-            } else {
-                float most = 0.0f;
+            for (int r = 0; r < 8; ++r) w[r] = __builtin_bit_cast(uint32_t, raw[r]);
+            v[0][0] = __builtin_bit_cast(bf16x8, make_uint4(__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u),
+                                                            __builtin_amdgcn_perm(w[5], w[4], 0x05040100u), __builtin_amdgcn_perm(w[7], w[6], 0x05040100u)));
+            v[0][1] = __builtin_bit_cast(bf16x8, make_uint4(upper_halves(w[0], w[1]), upper_halves(w[2], w[3]), upper_halves(w[4], w[5]), upper_halves(w[6], w[7])));
+            if constexpr (SUMS)
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
-                    left[0][r] = (float)raw[r].x;
-                    left[1][r] = (float)raw[r].y;
-                    most = fmaxf(fmaxf(most, fabsf(left[0][r])), fabsf(left[1][r]));
-                    if (sums) { db[0] += left[0][r]; db[1] += left[1][r]; }
+                    db[0] += __uint_as_float(w[r] << 16);
+                    db[1] += __uint_as_float(w[r] & 0xFFFF0000u);
                 }
-                const bool finite = most <= 3.402823466e38f;       // (a NaN may hide here, and is a NaN in every part)
+        } else {
+            float left[2][8], most = 0.0f;
 #pragma unroll
-                for (int p = 0; p < P; ++p)
+            for (int r = 0; r < 8; ++r) {
+                left[0][r] = (float)raw[r].x;
+                left[1][r] = (float)raw[r].y;
+                most = fmaxf(fmaxf(most, fabsf(left[0][r])), fabsf(left[1][r]));
+                if constexpr (SUMS) { db[0] += left[0][r]; db[1] += left[1][r]; }
+            }
+            // of an infinity the parts after the first are zeros (a NaN, which may hide here, is a NaN in every part)
+            const bool infinite = most > 3.402823466e38f;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) w[r] = __float_as_uint(left[j][r]);
+                    v[p][j] = __builtin_bit_cast(bf16x8, make_uint4(upper_halves(w[0], w[1]), upper_halves(w[2], w[3]), upper_halves(w[4], w[5]), upper_halves(w[6], w[7])));
+                    if (p + 1 < P)
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) left[j][r] = left[j][r] - __uint_as_float(w[r] & 0xFFFF0000u);
+                }
+            if (__builtin_expect(infinite, 0)) {
+#pragma unroll
+                for (int p = 1; p < P; ++p)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        uint32_t w[8];
 #pragma unroll
-                        for (int r = 0; r < 8; ++r) w[r] = __float_as_uint(left[j][r]);
-                        v[p][j] = __builtin_bit_cast(bf16x8, make_uint4(upper_halves(w[0], w[1]), upper_halves(w[2], w[3]), upper_halves(w[4], w[5]), upper_halves(w[6], w[7])));
-                        if (p + 1 < P)
-#pragma unroll
-                            for (int r = 0; r < 8; ++r) {
-                                left[j][r] = left[j][r] - __uint_as_float(w[r] & 0xFFFF0000u);
-                                if (!finite && (w[r] & 0x7FFFFFFFu) == 0x7F800000u) left[j][r] = 0.0f;    // (of an infinity nothing is left)
-                            }
+                        for (int r = 0; r < 8; ++r)
+                            if (fabsf((float)(j ? raw[r].y : raw[r].x)) > 3.402823466e38f) v[p][j][r] = (__bf16)0.0f;
                     }
             }
-            {
-                // the group's next rows
-                const uint32_t next = row + 16u * (g + kAhead);
-                if (next < row1) load_dy(next, raw);
-                else
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) raw[r] = PairOf<T>{(T)0.0f, (T)0.0f};
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) u[i] = __builtin_bit_cast(bf16x8, s_x[now][2u * g + half][grad_slot(wm * 128u + 32u * i + c)]);
-            if (more) store_column(now ^ 1, g);            // (of the next step, whose powers are there since the last barrier)
-#pragma unroll
-            for (int p = P - 1; p >= 0; --p)               // (the smallest first)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u[i], v[p][j], acc[i][j], 0, 0, 0);
         }
-        store_powers(now);                                 // (of step s + 2; this step's were read before the last barrier)
+    };
+    auto multiply = [&](int now, int g, const bf16x8 (&v)[P][2]) {
+        bf16x8 u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = __builtin_bit_cast(bf16x8, sh.x[now][2u * g + half][grad_slot(wm * 128u + 32u * i + c)]);
+#pragma unroll
+        for (int p = P - 1; p >= 0; --p)                   // (the smallest first)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u[i], v[p][j], acc[i][j], 0, 0, 0);
+    };
+
+    if (full) {
+        const uint32_t last = row0 + (full - 1u) * kGradRows;          // (what is loaded ahead of it is its rows again)
+        const uint32_t second = min(row0 + kGradRows, last);
+        load_powers(row0);
+        store_scales(0);
+        load_powers(second);
+        store_scales(1);
+        Rows codes = code_rows(row0), rows = dy_rows(row0);
+        load_codes(codes);
+#pragma unroll
+        for (int g = 0; g < kAhead; ++g) load_dy(rows, g, d[g]);
+        take_codes();
+        advance(codes, (second - row0) * code_row);
+        load_codes(codes);
         __syncthreads();
+        store_column(0, Column<0>{});
+        store_column(0, Column<1>{});
+        store_column(0, Column<2>{});
+        store_column(0, Column<3>{});
+        __syncthreads();
+        for (uint32_t s = 0; s < full; ++s) {
+            const int now = (int)(s & 1u);
+            const uint32_t row = row0 + s * kGradRows, next = min(row + kGradRows, last), after = min(row + 2u * kGradRows, last);
+            take_codes();
+            advance(codes, (after - next) * code_row);
+            load_codes(codes);
+            load_powers(after);
+            Rows ahead = rows;
+            advance(ahead, (next - row) * dy_row * sizeof(T));
+#pragma unroll
+            for (int g = 0; g < G::kGroups; ++g) {
+                bf16x8 v[P][2];
+                operands(d[g % kAhead], v);
+                load_dy(g + kAhead < G::kGroups ? rows : ahead, (g + kAhead) % G::kGroups, d[g % kAhead]);
+                if (g == 0) store_column(now ^ 1, Column<0>{});               // (of the next step, whose scales are there since the last barrier)
+                else if (g == 1) store_column(now ^ 1, Column<1>{});
+                else if (g == 2) store_column(now ^ 1, Column<2>{});
+                else store_column(now ^ 1, Column<3>{});
+                multiply(now, g, v);
+            }
+            rows = ahead;
+            store_scales(now);                             // (of step s + 2; this step's were read before the last barrier)
+            __syncthreads();
+        }
+    }
+    const uint32_t rest = row0 + full * kGradRows;
+    if (rest < row1) {                                     // rows past the last full step: zeros beyond the last
+#pragma unroll
+        for (int u = 0; u < G::kPowers; ++u) {
+            const uint32_t at = rest + (threadIdx.x + u * kThreads) % kGradRows, ok = min(at, row1 - 1u) - rest;
+            scale[u] = kept_scale((powers0 + (uint64_t)rest * a.blocks)[ok * a.blocks + p_at[u] - (at - rest) * a.blocks]);
+            if (at >= row1) scale[u] = 0.0f;
+        }
+        store_scales(0);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const uint32_t unit = threadIdx.x + u * kThreads, quad = unit % (TM / 4), oct = unit / (TM / 4);
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                next_x[u][r] = *reinterpret_cast<const uint32_t*>(codes0 + min(rest + oct * 8u + (uint32_t)r, row1 - 1u) * code_row + min(tile_i * TM + quad * 4u, a.blocks * 32u - 4u));
+        }
+        take_codes();
+        __syncthreads();
+        store_column(0, Column<0>{});
+        store_column(0, Column<1>{});
+        store_column(0, Column<2>{});
+        store_column(0, Column<3>{});
+        __syncthreads();
+#pragma unroll 1
+        for (uint32_t g = 0; g < (uint32_t)G::kGroups && rest + 16u * g < row1; ++g) {
+            bf16x8 v[P][2];
+            PairOf<T> raw[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const uint32_t at = rest + 16u * g + half * 8u + (uint32_t)r;
+                raw[r] = *reinterpret_cast<const PairOf<T>*>(dy0 + min(at, row1 - 1u) * dy_row + oc);
+                if (at >= row1) raw[r] = PairOf<T>{(T)0.0f, (T)0.0f};
+            }
+            operands(raw, v);
+            multiply(0, (int)g, v);
+        }
     }
     float* dw = a.parts == 1u ? a.dw + k * a.dw_worker : a.scratch + ((uint64_t)k * a.parts + part) * ((uint64_t)a.cols * a.out + a.out);
 #pragma unroll
@@ -374,20 +479,29 @@ __global__ __launch_bounds__(WM * WN * kWave, 2) void k_weight_gradient_wide(Wei
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const uint32_t row = tile_i * TM + wm * 128u + 32u * i + 8u * (e / 4) + 4u * half + (e % 4);
-            if (row >= a.cols) continue;
-            float* to = dw + (uint64_t)row * a.out + o;
-            if (o + 1u < a.out) *reinterpret_cast<PairOf<float>*>(to) = PairOf<float>{acc[i][0][e], acc[i][1][e]};
-            else if (o < a.out) to[0] = acc[i][0][e];
+            if (row < a.cols && o < a.out) *reinterpret_cast<PairOf<float>*>(dw + (uint64_t)row * a.out + oc) = PairOf<float>{acc[i][0][e], acc[i][1][e]};
         }
-    if (!a.db || tile_i != 0) return;
+    if constexpr (!SUMS) return;
     if (wm == 0) {
-        s_db[half][wn * 64u + 2u * c] = db[0];
-        s_db[half][wn * 64u + 2u * c + 1u] = db[1];
+        sh.db[half][wn * 64u + 2u * c] = db[0];
+        sh.db[half][wn * 64u + 2u * c + 1u] = db[1];
     }
     __syncthreads();
     float* to = a.parts == 1u ? a.db + k * a.db_worker : dw + (uint64_t)a.cols * a.out;
-    for (uint32_t i = threadIdx.x; i < TN; i += kThreads)
-        if (tile_o * TN + i < a.out) to[tile_o * TN + i] = s_db[0][i] + s_db[1][i];
+    for (uint32_t i = threadIdx.x; i < TN; i += kThreads) {
+        const uint32_t at = min(tile_o * TN + (i & ~1u), a.out - 2u) + (i & 1u);
+        if (tile_o * TN + (i & ~1u) < a.out) to[at] = sh.db[0][i] + sh.db[1][i];
+    }
+}
+
+template <typename T, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * kWave, 2) void k_weight_gradient_wide(WeightGradArgs a)
+{
+    __shared__ __align__(16) typename WideGradient<T, WM, WN>::Shared sh;
+    const uint32_t tiles = a.tiles_i * a.tiles_o;
+    const uint32_t part = blockIdx.x / tiles, tile = blockIdx.x % tiles, tile_i = tile % a.tiles_i, tile_o = tile / a.tiles_i;
+    if (a.db && tile_i == 0u) weight_gradient_tile<T, WM, WN, true>(a, sh, blockIdx.y, part, tile_i, tile_o);
+    else weight_gradient_tile<T, WM, WN, false>(a, sh, blockIdx.y, part, tile_i, tile_o);
 }
 
 // The parts' sums, joined in order.
@@ -446,6 +560,7 @@ hipError_t launch_weight_grad(int dtype, const WeightGradArgs& args, uint32_t wo
     }
     const dim3 grid(a.tiles_i * a.tiles_o * a.parts, workers);
     if (plan.wide) {
+        if (a.rows == 1u) a.dy_row = a.out;                // (no step is made by it)
         const dim3 threads(512);
         if (dtype == QGX_F32) hipLaunchKernelGGL((k_weight_gradient_wide<float, 2, 4>), grid, threads, 0, st, a);
         else if (dtype == QGX_F16) hipLaunchKernelGGL((k_weight_gradient_wide<_Float16, 2, 4>), grid, threads, 0, st, a);
