@@ -494,7 +494,8 @@ qgx_status qgx_restore(qgx_ctx* ctx, const qgx_kept* in, int dtype, void* y, uin
  * below 2^-110 a part may be lost); sums are in binary32, in an order the sizes and the device fix.  An infinity or a NaN in dy spoils the
  * column it stands in, as in the formula.  x->rows = workers * rows.
  * scratch: DEVICE, 16-byte aligned, of the bytes qgx_weight_gradient_scratch reports (0: may be NULL). */
-qgx_status qgx_weight_gradient_scratch(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, uint64_t out, uint64_t* bytes);
+qgx_status qgx_weight_gradient_scratch(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, uint64_t out, uint64_t dy_row,
+                                       uint64_t* bytes);
 qgx_status qgx_weight_gradient(qgx_ctx* ctx, const qgx_kept* x, int dtype, uint64_t workers, uint64_t rows, uint64_t out, const void* dy,
                                uint64_t dy_worker, uint64_t dy_row, float* dweight, uint64_t dw_worker, float* dbias, uint64_t db_worker,
                                void* scratch, uint64_t scratch_bytes, void* stream);

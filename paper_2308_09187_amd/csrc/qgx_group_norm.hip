@@ -241,20 +241,13 @@ __device__ __forceinline__ void group_sums(Runs r, uint32_t pieces, uint32_t spa
 
 constexpr int kGroupsMost = 256;                           // groups of a workgroup
 
-// Neighbouring spans of a sample on one XCD, one after the other: they share the cache's lines.
-__device__ __forceinline__ uint32_t group_unit(uint32_t block, uint32_t blocks)
-{
-    const uint32_t even = blocks / kXcds;                  // of each XCD
-    return block < even * kXcds ? block % kXcds * even + block / kXcds : block;
-}
-
 template <typename T, int THREADS, int N, bool SHORT>
 __global__ __launch_bounds__(THREADS) void k_group_norm(GroupArgs a, uint32_t batch)
 {
     constexpr int W = kPiece<T>;
     __shared__ __align__(16) float s_sums[THREADS * W];
     __shared__ float s_mean[kGroupsMost], s_rstd[kGroupsMost];
-    const uint32_t unit = group_unit(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
+    const uint32_t unit = unit_of_block(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
     const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = THREADS / pieces;
     const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
     const bool any = step < steps;
@@ -371,7 +364,7 @@ __global__ __launch_bounds__(THREADS) void k_group_norm_back(GroupArgs a, uint32
     constexpr int W = kPiece<T>;
     __shared__ __align__(16) float s_sums[THREADS * W];
     __shared__ float s_group[2][kGroupsMost];
-    const uint32_t unit = group_unit(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
+    const uint32_t unit = unit_of_block(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
     const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = THREADS / pieces;
     const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
     const bool any = step < steps;

@@ -416,10 +416,11 @@ struct WeightGradArgs {
     uint32_t tiles_i, tiles_o, parts, part_rows;
 };
 struct WeightGradPlan {
-    uint32_t tiles_i, tiles_o, parts, part_rows, wide;
+    uint32_t tiles_i, tiles_o, parts, part_rows;
+    uint32_t tile;              // columns of dY to a workgroup of the kernel for large layers; 0: the other one
     uint64_t scratch;           // bytes
 };
-WeightGradPlan weight_grad_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t cols, uint32_t out, uint32_t n_cu);
+WeightGradPlan weight_grad_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t cols, uint32_t out, uint64_t dy_row, uint32_t n_cu);
 hipError_t launch_weight_grad(int dtype, const WeightGradArgs& a, uint32_t workers, const WeightGradPlan& plan, hipStream_t st);
 
 struct RotaryArgs {

@@ -1331,12 +1331,12 @@ static qgx_status check_gradient(qgx_ctx* ctx, const char* what, int dtype, uint
     return QGX_OK;
 }
 
-qgx_status qgx_weight_gradient_scratch(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, uint64_t out, uint64_t* bytes)
+qgx_status qgx_weight_gradient_scratch(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, uint64_t out, uint64_t dy_row, uint64_t* bytes)
 {
     const qgx_status s = check_gradient(ctx, "qgx_weight_gradient_scratch", dtype, workers, rows, cols, out);
     if (s != QGX_OK) return s;
     if (!bytes) return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient_scratch: null argument");
-    *bytes = weight_grad_plan(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols, (uint32_t)out, ctx->n_simd / 4u).scratch;
+    *bytes = weight_grad_plan(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols, (uint32_t)out, dy_row, ctx->n_simd / 4u).scratch;
     return QGX_OK;
 }
 
@@ -1354,7 +1354,7 @@ qgx_status qgx_weight_gradient(qgx_ctx* ctx, const qgx_kept* x, int dtype, uint6
     if (!dweight || !aligned_to(dweight, 4u) || !aligned_to(dbias, 4u)) return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient: null or misaligned gradients");
     if ((workers > 1 && (dw_worker < cols * out || (dbias && db_worker < out))) || dw_worker >= (1ull << 60) / workers || db_worker >= (1ull << 60) / workers)
         return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient: the workers' gradients overlap, or a stride out of range");
-    const WeightGradPlan plan = weight_grad_plan(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols, (uint32_t)out, ctx->n_simd / 4u);
+    const WeightGradPlan plan = weight_grad_plan(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols, (uint32_t)out, dy_row, ctx->n_simd / 4u);
     if (plan.scratch && (!scratch || !aligned16(scratch))) return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient: null or misaligned scratch");
     if (scratch_bytes < plan.scratch) return fail(ctx, QGX_ERR_CAPACITY, "qgx_weight_gradient: scratch needs %llu bytes", (unsigned long long)plan.scratch);
     WeightGradArgs a{};

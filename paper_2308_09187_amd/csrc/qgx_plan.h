@@ -59,6 +59,13 @@ QGX_PLAN BlockWork block_by_unit(uint32_t i, uint32_t K, uint32_t units)
     return BlockWork{rest % K, even + rest / K};
 }
 
+// Neighbouring units on one XCD, one after the other: an eighth of the units to each, what is left over in order.  Grid: the units.
+QGX_PLAN uint32_t unit_of_block(uint32_t block, uint32_t units)
+{
+    const uint32_t even = units / kXcds;
+    return block < even * kXcds ? block % kXcds * even + block / kXcds : block;
+}
+
 // Where a worker's workgroups keep an order (compact placement, whole buckets) and K is a multiple of 8, the plain rows put each
 // worker on one XCD, whose workgroups then all wait for the same straggler, go on together and are in step from there on. Rows
 // turned against each other by 0, 2, 4 and 6 workers give a worker four XCDs.  What that gives grows with a worker's workgroups on an

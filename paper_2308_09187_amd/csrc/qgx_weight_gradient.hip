@@ -201,6 +201,13 @@ __device__ __forceinline__ float byte_value(uint32_t x)
     return v;
 }
 
+// sum += the eight, here and now (left to later, they would all be kept until then).
+__device__ __forceinline__ void add_eight(const float (&f)[8], float& sum)
+{
+    sum += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+    asm volatile("" : "+v"(sum));
+}
+
 template <int C> struct Column { static constexpr int value = C; };
 
 template <typename T, int WM, int WN>
@@ -208,13 +215,13 @@ struct WideGradient {
     static constexpr int P = kGradParts<T>, kThreads = WM * WN * kWave, TM = 128 * WM, TN = 64 * WN, kOcts = kGradRows / 8;
     static constexpr int kUnits = kOcts * (TM / 4) / kThreads;                   // eight rows of four columns of X, of a thread
     static constexpr int kGroups = kGradRows / 16;                               // groups of 16 rows of a step
-    static constexpr int kAhead = P == 1 ? 4 : P == 2 ? 2 : 1;                   // groups that are loaded ahead (P products from each)
+    static constexpr int kAhead = P == 1 ? 2 : 1;                   // groups that are loaded ahead (P products from each)
     static constexpr int kPowers = TM / 32 * kGradRows / kThreads;
     static_assert(kUnits >= 1 && kPowers >= 1 && kGroups % kAhead == 0, "");
 
     struct Shared {
         uint4 x[2][kOcts][TM];
-        float scale[2][TM / 32][kGradRows];
+        float scale[2][TM / 32][kGradRows + 4];            // (blocks a bank apart)
         float db[2][TN];
     };
 };
@@ -242,14 +249,18 @@ __device__ __forceinline__ void weight_gradient_tile(const WeightGradArgs& a, ty
         const uint32_t unit = threadIdx.x + u * kThreads, quad = unit % (TM / 4), oct = unit / (TM / 4);
         x_at[u] = oct * 8u * (uint32_t)code_row + min(tile_i * TM + quad * 4u, a.blocks * 32u - 4u);
         to_at[u] = oct * TM;
-        scale_at[u] = quad / 8u * kGradRows + oct * 8u;
+        scale_at[u] = quad / 8u * (kGradRows + 4u) + oct * 8u;
     }
 #pragma unroll
     for (int u = 0; u < G::kPowers; ++u) {
         const uint32_t unit = threadIdx.x + u * kThreads;
-        p_at[u] = unit % kGradRows * a.blocks + min(tile_i * (TM / 32) + unit / kGradRows, a.blocks - 1u);
+        p_at[u] = unit / (TM / 32) * a.blocks + min(tile_i * (TM / 32) + unit % (TM / 32), a.blocks - 1u);
     }
-    uint32_t x[kUnits][8], next_x[kUnits][8];
+    // codes as loaded, and as signed bytes; in the same place where registers are few (of split operands, whose steps are long, or of two
+    // units)
+    constexpr bool kApart = P == 1 && kUnits == 1;
+    uint32_t x[kUnits][8], loaded[kApart ? kUnits : 1][8];
+    uint32_t (&next_x)[kUnits][8] = [&]() -> uint32_t (&)[kUnits][8] { if constexpr (kApart) return loaded; else return x; }();
     float scale[G::kPowers];
     PairOf<T> d[kAhead][8];
     // of the step at `row`, all of whose rows are there: rows' addresses are the wave's, a thread's own part is 32 bits beside them
@@ -272,9 +283,12 @@ __device__ __forceinline__ void weight_gradient_tile(const WeightGradArgs& a, ty
     };
     auto load_codes = [&](const Rows& b) {
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
+        for (int u = 0; u < kUnits; ++u) {
+            uint32_t at = x_at[u];
+            asm volatile("" : "+v"(at));                   // (else the lane's part is added to the rows' in 64 bits beforehand)
 #pragma unroll
-            for (int u = 0; u < kUnits; ++u) next_x[u][r] = *reinterpret_cast<const uint32_t*>(b.p[r] + x_at[u]);
+            for (int r = 0; r < 8; ++r) next_x[u][r] = *reinterpret_cast<const uint32_t*>(b.p[r] + at);
+        }
     };
     auto load_powers = [&](uint32_t row) {
         const uint8_t* p = powers0 + (uint64_t)row * a.blocks;
@@ -282,12 +296,10 @@ __device__ __forceinline__ void weight_gradient_tile(const WeightGradArgs& a, ty
         for (int u = 0; u < G::kPowers; ++u) scale[u] = kept_scale(p[p_at[u]]);
     };
     // its rows 16 g .. 16 g + 15 of dY
-    uint32_t dy_at[G::kGroups];
-#pragma unroll
-    for (int g = 0; g < G::kGroups; ++g) dy_at[g] = (uint32_t)((16u * g + half * 8u) * dy_row * sizeof(T)) + oc * (uint32_t)sizeof(T);
+    const uint32_t dy_at = (uint32_t)(half * 8u * dy_row * sizeof(T)) + oc * (uint32_t)sizeof(T);
     auto load_dy = [&](const Rows& b, int g, PairOf<T> (&v)[8]) {
-        uint32_t at = dy_at[g];
-        asm volatile("" : "+v"(at));                       // (else the lane's part is added to the rows' in 64 bits beforehand)
+        uint32_t at = dy_at + (uint32_t)(16u * g * dy_row * sizeof(T));
+        asm volatile("" : "+v"(at));
 #pragma unroll
         for (int r = 0; r < 8; ++r) v[r] = *reinterpret_cast<const PairOf<T>*>(b.p[r] + at);
     };
@@ -295,7 +307,7 @@ __device__ __forceinline__ void weight_gradient_tile(const WeightGradArgs& a, ty
 #pragma unroll
         for (int u = 0; u < G::kPowers; ++u) {
             const uint32_t unit = threadIdx.x + u * kThreads;
-            sh.scale[to][unit / kGradRows][unit % kGradRows] = scale[u];
+            sh.scale[to][unit % (TM / 32)][unit / (TM / 32)] = scale[u];
         }
     };
     // a column of the thread's units of X, decoded, into LDS
@@ -329,66 +341,59 @@ __device__ __forceinline__ void weight_gradient_tile(const WeightGradArgs& a, ty
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     float db[2] = {0.0f, 0.0f};
 
-    // the operands of 16 rows of dY, P parts of two tiles
-    auto operands = [&](const PairOf<T> (&raw)[8], bf16x8 (&v)[P][2]) {
+    // the operand of 16 rows of dY for the thread's j-th column, in P parts
+    auto operand = [&](const PairOf<T> (&raw)[8], int j, bf16x8 (&v)[P]) {
         if constexpr (P == 1) {
             uint32_t w[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) w[r] = __builtin_bit_cast(uint32_t, raw[r]);
-            v[0][0] = __builtin_bit_cast(bf16x8, make_uint4(__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u),
-                                                            __builtin_amdgcn_perm(w[5], w[4], 0x05040100u), __builtin_amdgcn_perm(w[7], w[6], 0x05040100u)));
-            v[0][1] = __builtin_bit_cast(bf16x8, make_uint4(upper_halves(w[0], w[1]), upper_halves(w[2], w[3]), upper_halves(w[4], w[5]), upper_halves(w[6], w[7])));
-            if constexpr (SUMS)
+            const uint32_t pick = j ? 0x07060302u : 0x05040100u;
+            v[0] = __builtin_bit_cast(bf16x8, make_uint4(__builtin_amdgcn_perm(w[1], w[0], pick), __builtin_amdgcn_perm(w[3], w[2], pick),
+                                                         __builtin_amdgcn_perm(w[5], w[4], pick), __builtin_amdgcn_perm(w[7], w[6], pick)));
+            if constexpr (SUMS) {
+                float f[8];
 #pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    db[0] += __uint_as_float(w[r] << 16);
-                    db[1] += __uint_as_float(w[r] & 0xFFFF0000u);
-                }
+                for (int r = 0; r < 8; ++r) f[r] = __uint_as_float(j ? w[r] & 0xFFFF0000u : w[r] << 16);
+                add_eight(f, db[j]);
+            }
         } else {
-            float left[2][8], most = 0.0f;
+            float left[8], most = 0.0f;
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
-                left[0][r] = (float)raw[r].x;
-                left[1][r] = (float)raw[r].y;
-                most = fmaxf(fmaxf(most, fabsf(left[0][r])), fabsf(left[1][r]));
-                if constexpr (SUMS) { db[0] += left[0][r]; db[1] += left[1][r]; }
+                left[r] = (float)(j ? raw[r].y : raw[r].x);
+                most = fmaxf(most, fabsf(left[r]));
             }
+            if constexpr (SUMS) add_eight(left, db[j]);
             // of an infinity the parts after the first are zeros (a NaN, which may hide here, is a NaN in every part)
             const bool infinite = most > 3.402823466e38f;
 #pragma unroll
-            for (int p = 0; p < P; ++p)
+            for (int p = 0; p < P; ++p) {
+                uint32_t w[8];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    uint32_t w[8];
+                for (int r = 0; r < 8; ++r) w[r] = __float_as_uint(left[r]);
+                v[p] = __builtin_bit_cast(bf16x8, make_uint4(upper_halves(w[0], w[1]), upper_halves(w[2], w[3]), upper_halves(w[4], w[5]), upper_halves(w[6], w[7])));
+                if (p + 1 < P)
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) w[r] = __float_as_uint(left[j][r]);
-                    v[p][j] = __builtin_bit_cast(bf16x8, make_uint4(upper_halves(w[0], w[1]), upper_halves(w[2], w[3]), upper_halves(w[4], w[5]), upper_halves(w[6], w[7])));
-                    if (p + 1 < P)
-#pragma unroll
-                        for (int r = 0; r < 8; ++r) left[j][r] = left[j][r] - __uint_as_float(w[r] & 0xFFFF0000u);
-                }
+                    for (int r = 0; r < 8; ++r) left[r] = left[r] - __uint_as_float(w[r] & 0xFFFF0000u);
+            }
             if (__builtin_expect(infinite, 0)) {
 #pragma unroll
                 for (int p = 1; p < P; ++p)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                        for (int r = 0; r < 8; ++r)
-                            if (fabsf((float)(j ? raw[r].y : raw[r].x)) > 3.402823466e38f) v[p][j][r] = (__bf16)0.0f;
-                    }
+                    for (int r = 0; r < 8; ++r)
+                        if (fabsf((float)v[0][r]) > 3.402823466e38f) v[p][r] = (__bf16)0.0f;
             }
         }
     };
-    auto multiply = [&](int now, int g, const bf16x8 (&v)[P][2]) {
-        bf16x8 u[4];
+    auto columns = [&](int now, uint32_t g, bf16x8 (&u)[4]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[i] = __builtin_bit_cast(bf16x8, sh.x[now][2u * g + half][grad_slot(wm * 128u + 32u * i + c)]);
+    };
+    auto multiply = [&](const bf16x8 (&u)[4], int j, const bf16x8 (&v)[P]) {
 #pragma unroll
         for (int p = P - 1; p >= 0; --p)                   // (the smallest first)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u[i], v[p][j], acc[i][j], 0, 0, 0);
+            for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u[i], v[p], acc[i][j], 0, 0, 0);
     };
 
     if (full) {
@@ -400,47 +405,76 @@ __device__ __forceinline__ void weight_gradient_tile(const WeightGradArgs& a, ty
         store_scales(1);
         Rows codes = code_rows(row0), rows = dy_rows(row0);
         load_codes(codes);
-#pragma unroll
-        for (int g = 0; g < kAhead; ++g) load_dy(rows, g, d[g]);
         take_codes();
         advance(codes, (second - row0) * code_row);
-        load_codes(codes);
+        if (kApart) load_codes(codes);                     // (before dY's, as in the steps: what is waited for goes by the loads' order)
+#pragma unroll
+        for (int g = 0; g < kAhead; ++g) load_dy(rows, g, d[g]);
         __syncthreads();
         store_column(0, Column<0>{});
         store_column(0, Column<1>{});
         store_column(0, Column<2>{});
         store_column(0, Column<3>{});
         __syncthreads();
+        constexpr int kSets = P == 1 ? 2 : 1;              // of X's operands: the next group's beside this one's, where registers are left
+        bf16x8 u[kSets][4];
+        if (!kApart) load_codes(codes);
+        columns(0, 0, u[0]);
         for (uint32_t s = 0; s < full; ++s) {
             const int now = (int)(s & 1u);
             const uint32_t row = row0 + s * kGradRows, next = min(row + kGradRows, last), after = min(row + 2u * kGradRows, last);
             take_codes();
-            advance(codes, (after - next) * code_row);
-            load_codes(codes);
+            if (kApart) {
+                advance(codes, (after - next) * code_row);
+                load_codes(codes);
+            }
             load_powers(after);
             Rows ahead = rows;
             advance(ahead, (next - row) * dy_row * sizeof(T));
+            // The next step's X is in LDS before the last group, which has its operands by then and covers the barrier.
 #pragma unroll
             for (int g = 0; g < G::kGroups; ++g) {
-                bf16x8 v[P][2];
-                operands(d[g % kAhead], v);
+                bf16x8 v[2][P];
+                if (kSets == 1 && g) columns(now, g, u[0]);
+                if (kSets == 2 && g + 1 < G::kGroups) columns(now, g + 1, u[(g + 1) % kSets]);
+                operand(d[g % kAhead], 0, v[0]);
+                if (P > 1 && g + 1 < G::kGroups) {
+                    multiply(u[g % kSets], 0, v[0]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                operand(d[g % kAhead], 1, v[1]);
                 load_dy(g + kAhead < G::kGroups ? rows : ahead, (g + kAhead) % G::kGroups, d[g % kAhead]);
-                if (g == 0) store_column(now ^ 1, Column<0>{});               // (of the next step, whose scales are there since the last barrier)
-                else if (g == 1) store_column(now ^ 1, Column<1>{});
-                else if (g == 2) store_column(now ^ 1, Column<2>{});
-                else store_column(now ^ 1, Column<3>{});
-                multiply(now, g, v);
+                if (g == 0) {
+                    store_column(now ^ 1, Column<0>{});    // (whose scales are there since the last barrier)
+                    store_column(now ^ 1, Column<1>{});
+                } else if (g == 1) {
+                    store_column(now ^ 1, Column<2>{});
+                } else if (g == 2) {
+                    store_column(now ^ 1, Column<3>{});
+                    store_scales(now);                     // (of step s + 2; this step's were read before the last barrier)
+                    if (!kApart) {
+                        advance(codes, (after - next) * code_row);
+                        load_codes(codes);
+                    }
+                } else {
+                    __syncthreads();
+                    if (kSets == 2) columns(now ^ 1, 0, u[0]);
+                    if (P > 1) multiply(u[g % kSets], 0, v[0]);
+                }
+                if (P == 1) multiply(u[g % kSets], 0, v[0]);
+                multiply(u[g % kSets], 1, v[1]);
+                if (kSets == 1 && g + 1 == G::kGroups) columns(now ^ 1, 0, u[0]);
+                __builtin_amdgcn_sched_barrier(0);
             }
             rows = ahead;
-            store_scales(now);                             // (of step s + 2; this step's were read before the last barrier)
-            __syncthreads();
         }
+        __syncthreads();
     }
     const uint32_t rest = row0 + full * kGradRows;
     if (rest < row1) {                                     // rows past the last full step: zeros beyond the last
 #pragma unroll
         for (int u = 0; u < G::kPowers; ++u) {
-            const uint32_t at = rest + (threadIdx.x + u * kThreads) % kGradRows, ok = min(at, row1 - 1u) - rest;
+            const uint32_t at = rest + (threadIdx.x + u * kThreads) / (TM / 32), ok = min(at, row1 - 1u) - rest;
             scale[u] = kept_scale((powers0 + (uint64_t)rest * a.blocks)[ok * a.blocks + p_at[u] - (at - rest) * a.blocks]);
             if (at >= row1) scale[u] = 0.0f;
         }
@@ -461,7 +495,7 @@ __device__ __forceinline__ void weight_gradient_tile(const WeightGradArgs& a, ty
         __syncthreads();
 #pragma unroll 1
         for (uint32_t g = 0; g < (uint32_t)G::kGroups && rest + 16u * g < row1; ++g) {
-            bf16x8 v[P][2];
+            bf16x8 v[P];
             PairOf<T> raw[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
@@ -469,8 +503,13 @@ __device__ __forceinline__ void weight_gradient_tile(const WeightGradArgs& a, ty
                 raw[r] = *reinterpret_cast<const PairOf<T>*>(dy0 + min(at, row1 - 1u) * dy_row + oc);
                 if (at >= row1) raw[r] = PairOf<T>{(T)0.0f, (T)0.0f};
             }
-            operands(raw, v);
-            multiply(0, (int)g, v);
+            bf16x8 u[4];
+            columns(0, g, u);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                operand(raw, j, v);
+                multiply(u, j, v);
+            }
         }
     }
     float* dw = a.parts == 1u ? a.dw + k * a.dw_worker : a.scratch + ((uint64_t)k * a.parts + part) * ((uint64_t)a.cols * a.out + a.out);
@@ -498,23 +537,50 @@ template <typename T, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * kWave, 2) void k_weight_gradient_wide(WeightGradArgs a)
 {
     __shared__ __align__(16) typename WideGradient<T, WM, WN>::Shared sh;
-    const uint32_t tiles = a.tiles_i * a.tiles_o;
-    const uint32_t part = blockIdx.x / tiles, tile = blockIdx.x % tiles, tile_i = tile % a.tiles_i, tile_o = tile / a.tiles_i;
-    if (a.db && tile_i == 0u) weight_gradient_tile<T, WM, WN, true>(a, sh, blockIdx.y, part, tile_i, tile_o);
-    else weight_gradient_tile<T, WM, WN, false>(a, sh, blockIdx.y, part, tile_i, tile_o);
+    // the tiles of a part of a worker's rows one after the other on one XCD: they share its operands
+    const uint32_t unit = unit_of_block(blockIdx.x, gridDim.x), tiles = a.tiles_i * a.tiles_o, run = unit / tiles;
+    const uint32_t k = run / a.parts, part = run % a.parts, tile_i = unit % a.tiles_i, tile_o = unit % tiles / a.tiles_i;
+    if (a.db && tile_i == 0u) weight_gradient_tile<T, WM, WN, true>(a, sh, k, part, tile_i, tile_o);
+    else weight_gradient_tile<T, WM, WN, false>(a, sh, k, part, tile_i, tile_o);
 }
 
-// The parts' sums, joined in order.
+// The parts' sums joined: four neighbouring ones to a thread, the parts dealt to RUNS threads of a workgroup, whose sums are then added in order.
+template <int RUNS>
 __global__ __launch_bounds__(256) void k_weight_gradient_join(WeightGradArgs a)
 {
+    constexpr uint32_t kFours = 256 / RUNS;
+    __shared__ float4 s_run[RUNS][kFours];
     const uint64_t n = (uint64_t)a.cols * a.out, all = n + a.out, k = blockIdx.y;
     const float* from = a.scratch + k * a.parts * all;
-    for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < (a.db ? all : n); i += (uint64_t)gridDim.x * 256u) {
-        float x = from[i];
-#pragma unroll 4
-        for (uint32_t p = 1; p < a.parts; ++p) x += from[p * all + i];
-        if (i < n) a.dw[k * a.dw_worker + i] = x;
-        else a.db[k * a.db_worker + i - n] = x;
+    const uint32_t four = threadIdx.x % kFours, run = threadIdx.x / kFours;
+    // (first the fours of dW, then those of db)
+    const uint64_t fours = (n + 3u) / 4u, end = fours + (a.db ? (a.out + 3u) / 4u : 0u);
+    for (uint64_t first = (uint64_t)blockIdx.x * kFours; first < end; first += (uint64_t)gridDim.x * kFours) {
+        const uint64_t i = first + four;
+        const bool bias = i >= fours;
+        const uint64_t at = bias ? 4u * (i - fours) : 4u * i;
+        const int left = i < end ? (int)min((bias ? a.out : n) - at, (uint64_t)4u) : 0;
+        const float* p = from + (bias ? n : 0u) + at;
+        float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+        for (uint32_t j = run; j < a.parts; j += RUNS) {
+            float y[4];
+            load_piece(p + j * all, left, y);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[c] += y[c];
+        }
+        if constexpr (RUNS > 1) {
+            s_run[run][four] = make_float4(x[0], x[1], x[2], x[3]);
+            __syncthreads();
+            if (run == 0)
+#pragma unroll
+                for (int r = 1; r < RUNS; ++r) {
+                    const float4 y = s_run[r][four];
+                    x[0] += y.x; x[1] += y.y; x[2] += y.z; x[3] += y.w;
+                }
+            __syncthreads();
+        }
+        if (run == 0) store_piece((bias ? a.db + k * a.db_worker : a.dw + k * a.dw_worker) + at, left, x);
     }
 }
 
@@ -527,24 +593,49 @@ __global__ __launch_bounds__(256) void k_weight_gradient_zero(WeightGradArgs a)
     }
 }
 
-// Rows are split where there are fewer tiles than compute units, in parts of 256 rows at least.
-WeightGradPlan weight_grad_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t cols, uint32_t out, uint32_t n_cu)
+// Which kernel, its tile, and how the rows are split: by what a row of a tile and the join of the parts were measured to take (us, with all
+// places of the GPU taken; 4 x 8192 x 1024 x 1024: 128 columns of X by 256 of dY 77, 132, 184 us of bfloat16, binary16, binary32, by 128
+// 100, 145, 194).  A tile of 256 columns is left for one of 128 where it has more columns to spare than that costs.
+WeightGradPlan weight_grad_plan(int dtype, uint32_t workers, uint32_t rows, uint32_t cols, uint32_t out, uint64_t dy_row, uint32_t n_cu)
 {
-    (void)dtype;
     WeightGradPlan p{};
-    p.wide = cols > 128u && out > 128u;
-    p.tiles_i = p.wide ? (cols + 255u) / 256u : (cols + kGradTile - 1u) / kGradTile;
-    p.tiles_o = p.wide ? (out + 255u) / 256u : (out + kGradTile - 1u) / kGradTile;
+    const uint32_t parts_of = dtype == QGX_F32 ? 2u : dtype == QGX_F16 ? 1u : 0u;
+    const double row_256[3] = {0.038, 0.065, 0.090}, row_128[3] = {0.049, 0.071, 0.095};
+    p.tiles_i = (cols + 127u) / 128u;
     p.parts = 1;
     p.part_rows = rows;
+    // (a thread's part of an address has 32 bits, and pairs of columns are loaded)
+    const bool pairs = out >= 2u && dy_row <= (1u << 24);
+    p.tile = pairs ? 128u : 0u;
+    p.tiles_o = (out + 127u) / 128u;
     if (workers == 0 || rows == 0) return p;
-    const uint64_t tiles = (uint64_t)workers * p.tiles_i * p.tiles_o;
-    const uint32_t most = (rows + 255u) / 256u;
-    const uint32_t want = (uint32_t)min((uint64_t)most, max((uint64_t)1u, (p.wide ? 1u : 2u) * n_cu / tiles));
-    p.part_rows = ((rows + want - 1u) / want + kGradRows - 1u) / kGradRows * kGradRows;
-    p.parts = (rows + p.part_rows - 1u) / p.part_rows;
+    double best = 0.0;
+    for (uint32_t tile = pairs ? 256u : 128u; tile >= 128u; tile -= 128u) {
+        const uint32_t tiles_o = (out + tile - 1u) / tile, places = n_cu * (!pairs ? 1u : tile == 256u ? 2u : 4u);
+        const uint64_t tiles = (uint64_t)workers * p.tiles_i * tiles_o;
+        const double row = tile == 256u ? row_256[parts_of] : row_128[parts_of];
+        for (uint32_t want = 1; want <= 256u && (want == 1u || (want - 1u) * 128u < rows); ++want) {
+            const uint32_t part_rows = ((rows + want - 1u) / want + kGradRows - 1u) / kGradRows * kGradRows, parts = (rows + part_rows - 1u) / part_rows;
+            const uint64_t groups = tiles * parts, rounds = (groups + places - 1u) / places;
+            if (parts != want) continue;
+            // (with half of the places empty a row takes some two thirds of its time; a workgroup's start and end some 96 rows')
+            double us = (double)rounds * (part_rows + 96.0) * row * (2u * groups <= places ? 0.65 : 1.0);
+            if (parts > 1u) us += 4.0 + (2.0 * parts + 1.0) * workers * ((double)cols * out) * 4.0 / 5.0e6;
+            if (best == 0.0 || us < best) { best = us; p.parts = parts; p.part_rows = part_rows; p.tiles_o = tiles_o; p.tile = pairs ? tile : 0u; }
+            if (groups > 4u * places) break;
+        }
+    }
     if (p.parts > 1u) p.scratch = (uint64_t)workers * p.parts * ((uint64_t)cols * out + out) * sizeof(float);
     return p;
+}
+
+template <typename T>
+static hipError_t launch_tiles(const WeightGradArgs& a, uint32_t groups, uint32_t workers, uint32_t tile, hipStream_t st)
+{
+    if (tile == 256u) hipLaunchKernelGGL((k_weight_gradient_wide<T, 1, 4>), dim3(groups * workers), dim3(4 * kWave), 0, st, a);
+    else if (tile == 128u) hipLaunchKernelGGL((k_weight_gradient_wide<T, 1, 2>), dim3(groups * workers), dim3(2 * kWave), 0, st, a);
+    else hipLaunchKernelGGL(k_weight_gradient<T>, dim3(groups, workers), dim3(kGradThreads), 0, st, a);
+    return hipGetLastError();
 }
 
 hipError_t launch_weight_grad(int dtype, const WeightGradArgs& args, uint32_t workers, const WeightGradPlan& plan, hipStream_t st)
@@ -553,22 +644,19 @@ hipError_t launch_weight_grad(int dtype, const WeightGradArgs& args, uint32_t wo
     a.tiles_i = plan.tiles_i; a.tiles_o = plan.tiles_o; a.parts = plan.parts; a.part_rows = plan.part_rows;
     if (workers == 0) return hipSuccess;
     const uint64_t values = (uint64_t)a.cols * a.out + a.out;
-    const dim3 each((uint32_t)((values + 255u) / 256u < 4096u ? (values + 255u) / 256u : 4096u), workers);
+    const dim3 each((uint32_t)((values + 63u) / 64u < 8192u ? (values + 63u) / 64u : 8192u), workers);
     if (a.rows == 0) {
         hipLaunchKernelGGL(k_weight_gradient_zero, each, dim3(256), 0, st, a);
         return hipGetLastError();
     }
-    const dim3 grid(a.tiles_i * a.tiles_o * a.parts, workers);
-    if (plan.wide) {
-        if (a.rows == 1u) a.dy_row = a.out;                // (no step is made by it)
-        const dim3 threads(512);
-        if (dtype == QGX_F32) hipLaunchKernelGGL((k_weight_gradient_wide<float, 2, 4>), grid, threads, 0, st, a);
-        else if (dtype == QGX_F16) hipLaunchKernelGGL((k_weight_gradient_wide<_Float16, 2, 4>), grid, threads, 0, st, a);
-        else hipLaunchKernelGGL((k_weight_gradient_wide<__bf16, 2, 4>), grid, threads, 0, st, a);
-    } else if (dtype == QGX_F32) hipLaunchKernelGGL(k_weight_gradient<float>, grid, dim3(kGradThreads), 0, st, a);
-    else if (dtype == QGX_F16) hipLaunchKernelGGL(k_weight_gradient<_Float16>, grid, dim3(kGradThreads), 0, st, a);
-    else hipLaunchKernelGGL(k_weight_gradient<__bf16>, grid, dim3(kGradThreads), 0, st, a);
-    if (a.parts > 1u) hipLaunchKernelGGL(k_weight_gradient_join, each, dim3(256), 0, st, a);
+    const uint32_t groups = a.tiles_i * a.tiles_o * a.parts;
+    const hipError_t e = dtype == QGX_F32   ? launch_tiles<float>(a, groups, workers, plan.tile, st)
+                         : dtype == QGX_F16 ? launch_tiles<_Float16>(a, groups, workers, plan.tile, st)
+                                            : launch_tiles<__bf16>(a, groups, workers, plan.tile, st);
+    if (e != hipSuccess) return e;
+    // (by sixteen threads where parts are many: 256 parts of 128 x 128 sums took 65 us by one)
+    if (a.parts > 16u) hipLaunchKernelGGL(k_weight_gradient_join<16>, each, dim3(256), 0, st, a);
+    else if (a.parts > 1u) hipLaunchKernelGGL(k_weight_gradient_join<1>, each, dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

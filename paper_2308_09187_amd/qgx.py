@@ -136,7 +136,7 @@ def load():
         lib.qgx_position_bias_backward.argtypes = [ptr, ptr, ptr, C.c_int64, ptr, C.c_uint32, u64, ptr, u64, ptr]
         lib.qgx_checkpoint.argtypes = [ptr, C.c_int, u64, u64, u64, ptr, u64, u64, C.c_int, C.c_uint32, ptr, ptr]
         lib.qgx_restore.argtypes = [ptr, ptr, C.c_int, ptr, u64, ptr]
-        lib.qgx_weight_gradient_scratch.argtypes = [ptr, C.c_int, u64, u64, u64, u64, ptr]
+        lib.qgx_weight_gradient_scratch.argtypes = [ptr, C.c_int, u64, u64, u64, u64, u64, ptr]
         lib.qgx_weight_gradient.argtypes = [ptr, ptr, C.c_int, u64, u64, u64, ptr, u64, u64, ptr, u64, ptr, u64, ptr, u64, ptr]
         lib.qgx_group_norm_scratch.argtypes = [ptr, ptr, C.c_int, ptr]
         lib.qgx_group_norm.argtypes = [ptr, ptr, ptr, ptr, ptr, f32, ptr, ptr, ptr, ptr, C.c_int, C.c_uint32, ptr, u64, ptr]
@@ -684,7 +684,7 @@ class Context:
             _need(t.get_device() == dy.get_device() and t.dtype == torch.float32 and t.shape == shape and (wk == 0 or (t[0] if lead else t).is_contiguous()),
                   "%s: float32 of shape %s, each worker's contiguous, on dy's device", name, tuple(shape))
         need, scratch = self._need_bytes, None
-        st = self.lib.qgx_weight_gradient_scratch(self._h, code, wk, rows, cols, out, self._need_ref)
+        st = self.lib.qgx_weight_gradient_scratch(self._h, code, wk, rows, cols, out, gr, self._need_ref)
         if not st:
             if need.value:
                 scratch = _empty(dy, (need.value,), torch.uint8, stream)

@@ -33,7 +33,7 @@ def test_no_context():
     from ctypes import addressof
     assert lib.qgx_checkpoint(None, 0, 1, 1, 1, None, 0, 0, 0, 0, None, None) == qgx.ERR_ARG
     assert lib.qgx_restore(None, None, 0, None, 0, None) == qgx.ERR_ARG
-    assert lib.qgx_weight_gradient_scratch(None, 0, 1, 1, 1, 1, None) == qgx.ERR_ARG
+    assert lib.qgx_weight_gradient_scratch(None, 0, 1, 1, 1, 1, 1, None) == qgx.ERR_ARG
     assert lib.qgx_weight_gradient(None, None, 0, 1, 1, 1, None, 0, 0, None, 0, None, 0, None, 0, None) == qgx.ERR_ARG
     assert lib.qgx_group_norm_scratch(None, addressof(shape), 0, None) == qgx.ERR_ARG
     assert lib.qgx_group_norm(None, addressof(shape), None, None, None, 0.0, None, None, None, None, 0, 0, None, 0, None) == qgx.ERR_ARG
