@@ -438,6 +438,230 @@ __global__ __launch_bounds__(THREADS) void k_group_norm_back(GroupArgs a, uint32
     }
 }
 
+// ---- whole groups, whose pieces lie in one group each ---------------------------------------------------------------------
+// Where a group's channels are whole pieces and a span has 1, 2, 4 .. 64 of them, a thread has one group: its sum is one number, joined
+// with the lanes of its piece in registers and with the waves through LDS, one barrier a sum.
+
+template <int D, int M>
+__device__ __forceinline__ void join_lanes(float (&x)[M])
+{
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        const LanePair p = lane_pair<D>(__float_as_uint(x[m]));
+        x[m] = __uint_as_float(p.a) + __uint_as_float(p.b);
+    }
+}
+
+// The sums over the lanes of one piece (lanes that agree in their number mod pieces), in each of them.
+template <int M>
+__device__ __forceinline__ void piece_sums(float (&x)[M], uint32_t pieces)
+{
+    if (pieces <= 32u) join_lanes<32>(x);
+    if (pieces <= 16u) join_lanes<16>(x);
+    if (pieces <= 8u) join_lanes<8>(x);
+    if (pieces <= 4u) join_lanes<4>(x);
+    if (pieces <= 2u) join_lanes<2>(x);
+    if (pieces <= 1u) join_lanes<1>(x);
+}
+
+// The sums over the threads of a group, of M numbers.  s: LDS of these sums' own, [M][64][THREADS / 64].
+template <int THREADS, int M>
+__device__ __forceinline__ void one_group_sums(float (&x)[M], uint32_t pieces, uint32_t group_pieces, float* s)
+{
+    constexpr uint32_t kWaves = THREADS / kWave;
+    piece_sums(x, pieces);
+    if (lane_id() < (int)pieces)
+#pragma unroll
+        for (int m = 0; m < M; ++m) s[(m * kWave + lane_id()) * kWaves + wave_id()] = x[m];
+    __syncthreads();
+    const uint32_t first = threadIdx.x % pieces / group_pieces * group_pieces;
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        x[m] = 0.0f;
+        for (uint32_t p = 0; p < group_pieces; ++p)
+#pragma unroll
+            for (uint32_t w = 0; w < kWaves; w += 4u) {
+                const float4 y = *reinterpret_cast<const float4*>(s + (m * kWave + first + p) * kWaves + w);
+                x[m] += (y.x + y.y) + (y.z + y.w);
+            }
+    }
+}
+
+// A piece's codes and, where its first column is a block's, the power; the lanes of a block are neighbours.
+template <typename T, int W>
+__device__ __forceinline__ void keep_piece(const GroupArgs& a, const RawPiece<T, false>& raw, float (&v)[W], uint32_t channel, uint32_t row, uint32_t call,
+                                           const PhiloxKeys& keys, bool ok, Scalars* sc)
+{
+    uint32_t bits = quad_max(largest_bits<T>(raw.bits));
+    if constexpr (W == 4) bits = max(bits, (uint32_t)__builtin_amdgcn_mov_dpp((int)bits, 0x141, 0xf, 0xf, true));       // row_half_mirror: the other four lanes
+    uint32_t word[W / 4];
+    const uint32_t power = kept_codes<W>(v, bits, a.keep_top, a.draws.on != 0u, channel / 8u, channel / 4u & 1u, row, call, keys, word);
+    asm volatile("" : : "v"(word[0]));                     // (made before the next piece's is begun)
+    if (!ok) return;
+    uint8_t* to = a.keep_codes + (size_t)row * a.channels + channel;                    // (whole blocks: rows without a gap)
+    if constexpr (W == 8) *reinterpret_cast<uint2*>(to) = make_uint2(word[0], word[1]);
+    else *reinterpret_cast<uint32_t*>(to) = word[0];
+    if (channel % QGX_KEPT_BLOCK == 0u) {
+        a.keep_powers[((size_t)row * a.channels + channel) / QGX_KEPT_BLOCK] = (uint8_t)power;
+        if (power == kKeptSpoilt) raise_error(sc, QGX_EBIT_NONFINITE);
+    }
+}
+
+template <typename T, int THREADS, int N, bool KEEP>
+__global__ __launch_bounds__(THREADS, 4) void k_group_norm_one(GroupArgs a, uint32_t batch, Scalars* sc)
+{
+    constexpr int W = kPiece<T>;
+    __shared__ __align__(16) float s_sum[2][kWave * THREADS / kWave];
+    const uint32_t unit = unit_of_block(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
+    const uint32_t pieces = a.span / W, group_pieces = a.per / W, steps = THREADS / pieces;
+    const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
+    const ChannelsAt at{(int)(first + j * W), 0, W};
+    const Places<T, false> places = places_of<T, false>(a, sample, batch, at);
+    RawPiece<T, false> raw[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) raw[i] = load_place<T, false, false>(places, min(i * steps + step, a.places - 1u), W);
+    const float n = (float)a.places * (float)a.per;
+    const uint32_t call = KEEP && a.draws.on ? kept_call(a.draws, sc) : 0u;
+    const PhiloxKeys keys = philox_keys(a.draws.seed_lo, a.draws.seed_hi);
+    float sum[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        uint32_t p = i * steps + step;
+        forget(raw[i]);
+        if constexpr (KEEP) asm volatile("" : "+v"(p));    // (else the draws of all pieces are made side by side, in registers of their own)
+        float v[W], t = 0.0f;
+        values_at(raw[i], places, v);
+#pragma unroll
+        for (int c = 0; c < W; ++c) t += v[c];
+        sum[0] += p < a.places ? t : 0.0f;
+        if constexpr (KEEP) keep_piece<T, W>(a, raw[i], v, (uint32_t)at.c, sample * a.places + p, call, keys, p < a.places, sc);
+    }
+    one_group_sums<THREADS>(sum, pieces, group_pieces, s_sum[0]);
+    const float mean = sum[0] / n;
+    sum[0] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float v[W], t = 0.0f;
+        forget(raw[i]);
+        values_at(raw[i], places, v);
+#pragma unroll
+        for (int c = 0; c < W; ++c) t = fmaf(v[c] - mean, v[c] - mean, t);
+        sum[0] += i * steps + step < a.places ? t : 0.0f;
+    }
+    one_group_sums<THREADS>(sum, pieces, group_pieces, s_sum[1]);
+    const float rstd = 1.0f / sqrtf(sum[0] / n + a.eps);
+    if (threadIdx.x < pieces && j % group_pieces == 0u) {
+        const size_t to = (size_t)sample * a.groups + (first + j * W) / a.per;
+        if (a.mean) a.mean[to] = mean;
+        if (a.rstd) a.rstd[to] = rstd;
+    }
+    float w[W], b[W];
+    channel_parameters<W>(a.w, at, 1.0f, w);
+    channel_parameters<W>(a.b, at, 0.0f, b);
+    T* y = (T*)a.y + sample / batch * a.y_worker + sample % batch * a.y_batch + at.c;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t p = i * steps + step;
+        float v[W];
+        forget(raw[i]);
+        values_at(raw[i], places, v);
+#pragma unroll
+        for (int c = 0; c < W; ++c) v[c] = fmaf((v[c] - mean) * rstd, w[c], b[c]);
+        activate<T>(v, a.activation, a.slope);
+        if (p < a.places) stream_piece(y + p * a.y_place, v);
+    }
+}
+
+template <typename T, int THREADS, int N, bool KEPT>
+__global__ __launch_bounds__(THREADS, 4) void k_group_norm_back_one(GroupArgs a, uint32_t batch)
+{
+    constexpr int W = kPiece<T>, kWaves = THREADS / kWave;
+    __shared__ __align__(16) float s_sum[2 * kWave * kWaves];
+    __shared__ float s_channel[2][kWaves][kWave * W];
+    const uint32_t unit = unit_of_block(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
+    const uint32_t pieces = a.span / W, group_pieces = a.per / W, steps = THREADS / pieces;
+    const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
+    const ChannelsAt at{(int)(first + j * W), 0, W};
+    const Places<T, KEPT> places = places_of<T, KEPT>(a, sample, batch, at);
+    const Places<T, false> grads = gradients_of<T>(a, sample, batch, at);
+    RawPiece<T, KEPT> x[N];
+    RawPiece<T, false> dy[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t p = min(i * steps + step, a.places - 1u);
+        x[i] = load_place<T, KEPT, false>(places, p, W);
+        dy[i] = load_place<T, false, false>(grads, p, W);
+    }
+    const size_t g = (size_t)sample * a.groups + (first + j * W) / a.per;
+    float mean[W], rstd[W], w[W], b[W], dw[W], db[W];
+    const float one_mean = a.mean_in[g], one_rstd = a.rstd_in[g];
+#pragma unroll
+    for (int c = 0; c < W; ++c) {
+        mean[c] = one_mean;
+        rstd[c] = one_rstd;
+    }
+    channel_parameters<W>(a.w, at, 1.0f, w);
+    channel_parameters<W>(a.b, at, 0.0f, b);
+#pragma unroll
+    for (int c = 0; c < W; ++c) dw[c] = db[c] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float h[W], dz[W];
+        forget(x[i]);
+        forget(dy[i]);
+        back_values<T, KEPT>(a, x[i], places, dy[i], grads, mean, rstd, w, b, h, dz);
+        const bool ok = i * steps + step < a.places;
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+            dw[c] = ok ? fmaf(dz[c], h[c], dw[c]) : dw[c];
+            db[c] = ok ? db[c] + dz[c] : db[c];
+            asm volatile("" : "+v"(dw[c]), "+v"(db[c]));
+        }
+    }
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < W; ++c) {
+        sum[0] = fmaf(dw[c], w[c], sum[0]);
+        sum[1] = fmaf(db[c], w[c], sum[1]);
+    }
+    if (a.dw || a.db) {
+        piece_sums(dw, pieces);
+        piece_sums(db, pieces);
+        if (lane_id() < (int)pieces)
+#pragma unroll
+            for (int c = 0; c < W; ++c) {
+                s_channel[0][wave_id()][lane_id() * W + c] = dw[c];
+                s_channel[1][wave_id()][lane_id() * W + c] = db[c];
+            }
+    }
+    one_group_sums<THREADS>(sum, pieces, group_pieces, s_sum);
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float* to = channel_sums_at(a, sample, batch, 0u, which);
+        if (to)
+            for (uint32_t c = threadIdx.x; c < a.span; c += THREADS) {
+                float t = s_channel[which][0][c];
+#pragma unroll
+                for (int i = 1; i < kWaves; ++i) t += s_channel[which][i][c];
+                to[first + c] = t;
+            }
+    }
+    if (!a.y) return;
+    const float n = (float)a.places * (float)a.per, minus_m2 = -(sum[0] / n), minus_m1 = -(sum[1] / n);
+    T* dx = (T*)a.y + sample / batch * a.y_worker + sample % batch * a.y_batch + at.c;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t p = i * steps + step;
+        float h[W], dz[W];
+        forget(x[i]);
+        forget(dy[i]);
+        back_values<T, KEPT>(a, x[i], places, dy[i], grads, mean, rstd, w, b, h, dz);
+#pragma unroll
+        for (int c = 0; c < W; ++c) dz[c] = one_rstd * fmaf(h[c], minus_m2, fmaf(dz[c], w[c], minus_m1));
+        if (p < a.places) stream_piece(dx + p * a.y_place, dz);
+    }
+}
+
 // ---- places dealt to workgroups -------------------------------------------------------------------------------------------
 // Workgroup (part, column, sample) has `part` places from part * a.part on of `span` channels.
 
@@ -753,19 +977,28 @@ GroupPlan group_plan(int dtype, uint32_t samples, uint32_t places, uint32_t chan
     p.part = places;
     if (samples == 0 || places == 0) return p;
     // groups of a workgroup: those of 64 bytes at least, and of more while there are workgroups enough
-    uint32_t of = min(groups, max(1u, ceil_div(4u * W, per)));
     auto pieces_of = [&](uint32_t n) { return ceil_div((uint64_t)n * per, W); };
     auto fits = [&](uint32_t n) {
         const uint32_t pieces = pieces_of(n);
         return n <= (uint32_t)kGroupsMost && pieces <= 1024u && ceil_div(places, 1024u / pieces) <= most;
     };
-    while (of < groups && 2u * of <= groups && fits(2u * of) && (uint64_t)samples * (groups / (2u * of)) >= 4u * n_cu) of *= 2u;
+    // a piece in one group each, and 1, 2, 4 .. 64 pieces in a span (of all of which there are whole ones)
+    auto one = [&](uint32_t n) {
+        const uint32_t pieces = pieces_of(n);
+        return per % W == 0u && groups % n == 0u && pieces <= 64u && (pieces & (pieces - 1u)) == 0u && per / W <= 8u;
+    };
+    uint32_t of = min(groups, max(1u, ceil_div(4u * W, per)));
+    if (!one(of) && one(2u * of) && fits(2u * of) && 2u * of <= groups) of *= 2u;
+    while (of < groups && 2u * of <= groups && fits(2u * of) && (one(2u * of) || !one(of)) && (uint64_t)samples * (groups / (2u * of)) >= 4u * n_cu) of *= 2u;
     if (channels >= W && fits(of)) {
         p.whole = true;
+        p.one = one(of);
         p.span = of * per;
         p.spans = ceil_div(groups, of);
         const uint32_t pieces = pieces_of(of);
-        p.threads = pieces <= 256u && ceil_div(places, 256u / pieces) <= most / 2u ? 256u : 1024u;
+        p.threads = 1024u;
+        for (uint32_t t = 256u; t < 1024u; t *= 2u)
+            if (pieces <= t && ceil_div(places, t / pieces) <= most) { p.threads = t; break; }
         p.pieces = ceil_div(places, p.threads / pieces);
     } else {
         p.span = min(channels, 256u * W);                  // (any channels: borders of groups do not matter here)
@@ -789,24 +1022,31 @@ static void deal(GroupArgs& a, const GroupPlan& p)
     a.sums = a.scratch ? a.scratch + p.at_sums : nullptr;
 }
 
-template <typename T, int THREADS, int N, bool SHORT>
-static hipError_t launch_whole(const GroupArgs& a, uint32_t batch, hipStream_t st)
+template <typename T, int THREADS, int N>
+static hipError_t launch_whole_as(const GroupArgs& a, uint32_t batch, const GroupPlan& p, Scalars* sc, hipStream_t st)
 {
-    hipLaunchKernelGGL((k_group_norm<T, THREADS, N, SHORT>), dim3(a.samples * a.spans), dim3(THREADS), 0, st, a, batch);
+    const dim3 grid(a.samples * a.spans), block(THREADS);
+    if (!p.one) hipLaunchKernelGGL((k_group_norm<T, THREADS, N, false>), grid, block, 0, st, a, batch);
+    else if (a.keep_codes) hipLaunchKernelGGL((k_group_norm_one<T, THREADS, N, true>), grid, block, 0, st, a, batch, sc);
+    else hipLaunchKernelGGL((k_group_norm_one<T, THREADS, N, false>), grid, block, 0, st, a, batch, sc);
     return hipGetLastError();
 }
 
-template <typename T, bool SHORT>
-static hipError_t launch_forward(GroupArgs& a, uint32_t batch, const GroupPlan& p, hipStream_t st)
+template <typename T>
+static hipError_t launch_whole(const GroupArgs& a, uint32_t batch, const GroupPlan& p, Scalars* sc, hipStream_t st)
 {
-    if (p.whole) {
-        if (p.threads == 256u) {
-            if (p.pieces <= 2u) return launch_whole<T, 256, 2, SHORT>(a, batch, st);
-            return p.pieces <= 4u ? launch_whole<T, 256, 4, SHORT>(a, batch, st) : launch_whole<T, 256, 8, SHORT>(a, batch, st);
-        }
-        if (p.pieces <= 4u) return launch_whole<T, 1024, 4, SHORT>(a, batch, st);
-        return p.pieces <= 8u ? launch_whole<T, 1024, 8, SHORT>(a, batch, st) : launch_whole<T, 1024, 16, SHORT>(a, batch, st);
+    if (p.threads == 256u) {
+        if (p.pieces <= 4u) return launch_whole_as<T, 256, 4>(a, batch, p, sc, st);
+        return p.pieces <= 8u ? launch_whole_as<T, 256, 8>(a, batch, p, sc, st) : launch_whole_as<T, 256, 16>(a, batch, p, sc, st);
     }
+    return p.threads == 512u ? launch_whole_as<T, 512, 16>(a, batch, p, sc, st) : launch_whole_as<T, 1024, 16>(a, batch, p, sc, st);
+}
+
+template <typename T, bool SHORT>
+static hipError_t launch_forward(GroupArgs& a, uint32_t batch, const GroupPlan& p, Scalars* sc, hipStream_t st)
+{
+    if constexpr (!SHORT)
+        if (p.whole) return launch_whole<T>(a, batch, p, sc, st);
     const dim3 grid(a.parts, a.spans, a.samples);
     hipLaunchKernelGGL((k_group_channels<T, SHORT>), grid, dim3(kPartThreads), 0, st, a, batch);
     hipLaunchKernelGGL(k_group_join, dim3(a.groups, a.samples), dim3(256), 0, st, a);
@@ -817,37 +1057,45 @@ static hipError_t launch_forward(GroupArgs& a, uint32_t batch, const GroupPlan& 
 }
 
 template <typename T>
-static hipError_t launch_forward_of(GroupArgs& a, uint32_t batch, const GroupPlan& p, hipStream_t st)
+static hipError_t launch_forward_of(GroupArgs& a, uint32_t batch, const GroupPlan& p, Scalars* sc, hipStream_t st)
 {
-    return a.channels < (uint32_t)kPiece<T> ? launch_forward<T, true>(a, batch, p, st) : launch_forward<T, false>(a, batch, p, st);
+    return a.channels < (uint32_t)kPiece<T> ? launch_forward<T, true>(a, batch, p, sc, st) : launch_forward<T, false>(a, batch, p, sc, st);
 }
 
-hipError_t launch_group_norm(int dtype, const GroupArgs& args, uint32_t workers, const GroupPlan& plan, hipStream_t st)
+bool group_keeps(const GroupPlan& plan, uint32_t channels) { return plan.one && plan.span % QGX_KEPT_BLOCK == 0u && channels % QGX_KEPT_BLOCK == 0u; }
+
+hipError_t launch_group_norm(int dtype, const GroupArgs& args, uint32_t workers, const GroupPlan& plan, Scalars* sc, hipStream_t st)
 {
     GroupArgs a = args;
     if (a.samples == 0 || a.places == 0) return hipSuccess;
     deal(a, plan);
     const uint32_t batch = a.samples / workers;
-    return dtype == QGX_F32   ? launch_forward_of<float>(a, batch, plan, st)
-           : dtype == QGX_F16 ? launch_forward_of<_Float16>(a, batch, plan, st)
-                              : launch_forward_of<__bf16>(a, batch, plan, st);
+    return dtype == QGX_F32   ? launch_forward_of<float>(a, batch, plan, sc, st)
+           : dtype == QGX_F16 ? launch_forward_of<_Float16>(a, batch, plan, sc, st)
+                              : launch_forward_of<__bf16>(a, batch, plan, sc, st);
 }
 
-template <typename T, int THREADS, int N, bool KEPT, bool SHORT>
-static hipError_t launch_back_whole(const GroupArgs& a, uint32_t batch, hipStream_t st)
+template <typename T, int THREADS, int N, bool KEPT>
+static hipError_t launch_back_whole_as(const GroupArgs& a, uint32_t batch, const GroupPlan& p, hipStream_t st)
 {
-    hipLaunchKernelGGL((k_group_norm_back<T, THREADS, N, KEPT, SHORT>), dim3(a.samples * a.spans), dim3(THREADS), 0, st, a, batch);
+    const dim3 grid(a.samples * a.spans), block(THREADS);
+    if (p.one) hipLaunchKernelGGL((k_group_norm_back_one<T, THREADS, N, KEPT>), grid, block, 0, st, a, batch);
+    else hipLaunchKernelGGL((k_group_norm_back<T, THREADS, N, KEPT, false>), grid, block, 0, st, a, batch);
     return hipGetLastError();
+}
+
+template <typename T, bool KEPT>
+static hipError_t launch_back_whole(const GroupArgs& a, uint32_t batch, const GroupPlan& p, hipStream_t st)
+{
+    if (p.threads == 256u) return p.pieces <= 4u ? launch_back_whole_as<T, 256, 4, KEPT>(a, batch, p, st) : launch_back_whole_as<T, 256, 8, KEPT>(a, batch, p, st);
+    return p.threads == 512u ? launch_back_whole_as<T, 512, 8, KEPT>(a, batch, p, st) : launch_back_whole_as<T, 1024, 8, KEPT>(a, batch, p, st);
 }
 
 template <typename T, bool KEPT, bool SHORT>
 static hipError_t launch_back(const GroupArgs& a, uint32_t batch, const GroupPlan& p, hipStream_t st)
 {
-    if (p.whole) {
-        if (p.threads == 256u)
-            return p.pieces <= 2u ? launch_back_whole<T, 256, 2, KEPT, SHORT>(a, batch, st) : launch_back_whole<T, 256, 4, KEPT, SHORT>(a, batch, st);
-        return p.pieces <= 4u ? launch_back_whole<T, 1024, 4, KEPT, SHORT>(a, batch, st) : launch_back_whole<T, 1024, 8, KEPT, SHORT>(a, batch, st);
-    }
+    if constexpr (!SHORT)
+        if (p.whole) return launch_back_whole<T, KEPT>(a, batch, p, st);
     const dim3 grid(a.parts, a.spans, a.samples);
     hipLaunchKernelGGL((k_group_back_channels<T, KEPT, SHORT>), grid, dim3(kPartThreads), 0, st, a, batch);
     if (a.y) {

@@ -363,6 +363,7 @@ struct KeepArgs {
     uint64_t x_worker, x_batch, x_row, y_row, tiles;
     uint32_t rows, batch, n_rows, cols, blocks;     // rows of a sample, samples of a worker, rows of all
     uint32_t top;               // the type's largest stored power
+    uint32_t even;              // filled in by the launch: all rows of x lie one step apart
 };
 constexpr uint32_t kKeptTop = 248u, kKeptTopF16 = 136u;   // largest powers kept, of types of 8 and of 5 bits of exponent
 hipError_t launch_checkpoint(int dtype, const KeepArgs& a, const KeptDraws& d, Scalars* sc, hipStream_t st);
@@ -387,6 +388,10 @@ struct GroupArgs {
     uint32_t samples, batch, places, channels, groups, per;    // samples = workers * batch; per = channels of a group
     int32_t activation;
     float slope, eps;
+    uint8_t* keep_codes;        // where x is kept as well, or null
+    uint8_t* keep_powers;
+    uint32_t keep_top;
+    KeptDraws draws;
     // how it is dealt out, filled in by the launch
     uint32_t span, spans;       // whole groups' channels of a workgroup, workgroups across a sample's
     uint32_t parts, part;       // workgroups along a sample's places, places of each
@@ -395,13 +400,15 @@ struct GroupArgs {
 };
 struct GroupPlan {
     bool whole;                 // a workgroup has all of its groups' places in its registers
+    bool one;                   // and a thread's piece lies in one of them
     uint32_t threads, pieces;   // of that kernel
     uint32_t span, spans, parts, part;
     uint64_t at_sums;           // floats before the groups' sums, after the channels' [samples][parts][2][channels]
     uint64_t scratch;           // bytes
 };
 GroupPlan group_plan(int dtype, uint32_t samples, uint32_t places, uint32_t channels, uint32_t groups, bool backward, uint32_t n_cu);
-hipError_t launch_group_norm(int dtype, const GroupArgs& a, uint32_t workers, const GroupPlan& plan, hipStream_t st);
+bool group_keeps(const GroupPlan& plan, uint32_t channels);     // whether the kernel of this plan keeps x as well
+hipError_t launch_group_norm(int dtype, const GroupArgs& a, uint32_t workers, const GroupPlan& plan, Scalars* sc, hipStream_t st);
 hipError_t launch_group_norm_back(int dtype, const GroupArgs& a, uint32_t workers, const GroupPlan& plan, hipStream_t st);
 
 struct WeightGradArgs {

@@ -8,39 +8,20 @@
 
 namespace qgx {
 
-// A block's stored power, from the bits of its largest magnitude: the smallest 2^e with the magnitude at most 127 * 2^e (127 = 1.984375 * 2^6),
-// biased by 127; `top`: the type's largest.  0 for zeros, 255 where the magnitude is an infinity or a NaN.
-constexpr uint32_t kKeptSpoilt = 255u;
-__device__ __forceinline__ uint32_t kept_power(uint32_t bits, uint32_t top)
-{
-    const int p = (int)(bits >> 23) - 6 + (int)((bits & 0x7FFFFFu) > 0x7E0000u);
-    if (bits == 0u) return 0u;
-    return bits >= 0x7F800000u ? kKeptSpoilt : (uint32_t)min(max(p, 1), (int)top);
-}
+// A block's stored power: the smallest 2^e with the largest magnitude at most 127 * 2^e (127 = 1.984375 * 2^6), biased by 127; 0 for zeros.  From
+// the magnitude's bits: a significand beyond 1.984375 carries into the exponent.
+constexpr uint32_t kKeptSpoilt = 255u;                     // of a block with an infinity or a NaN
+__device__ __forceinline__ uint32_t kept_power(uint32_t bits) { return (uint32_t)max((int)((bits + 0x1FFFFu) >> 23) - 6, 0); }
 
-// 2^-e of a stored power (zeros and spoilt blocks: 0, so that their codes are those of zeros).
-__device__ __forceinline__ float kept_over(uint32_t power)
+// What that leaves to be put right: infinities and NaNs, magnitudes beyond the type's largest power `top` or below those whose inverse powers, times 2^16,
+// are numbers.
+__device__ __forceinline__ bool kept_is_rare(uint32_t bits, uint32_t power, uint32_t top)
 {
-    return power == 0u || power == kKeptSpoilt ? 0.0f : __uint_as_float((254u - power) << 23);
+    return power >= top || (bits != 0u && power < 16u);
 }
 
 // 2^e; 0 for zeros, infinity (and so 0 * infinity = NaN) for a spoilt block.
 __device__ __forceinline__ float kept_scale(uint32_t power) { return __uint_as_float(power << 23); }
-
-// Rounded to the nearest whole number.
-__device__ __forceinline__ uint32_t kept_code(float u)
-{
-    return (uint32_t)(int)(fminf(fmaxf(rintf(u), -127.0f), 127.0f) + 128.0f);
-}
-
-// Rounded away from zero where the draw, 16 bits, is below 2^16 times the remainder (|u| less its whole part: exact).
-__device__ __forceinline__ uint32_t kept_code(float u, uint32_t draw)
-{
-    const float m = fabsf(u), down = floorf(m);
-    const float up = (float)draw < (m - down) * 65536.0f ? down + 1.0f : down;
-    const float code = fminf(up, 127.0f);
-    return (uint32_t)(int)(128.0f + (u < 0.0f ? -code : code));
-}
 
 // An element out of its byte: both steps exact.
 __device__ __forceinline__ float kept_value(uint32_t code, float scale) { return ((float)code - 128.0f) * scale; }
@@ -50,23 +31,91 @@ __device__ __forceinline__ uint32_t kept_call(const KeptDraws& d, const Scalars*
     return d.call_mode ? 2u * (scalar_load(&sc->t) - 1u) + (d.call_mode - 1u) : d.call_id;
 }
 
-// The codes of eight columns' elements, with the bits of the block's largest magnitude known: the two words that are stored.
-// group: the column / 8.
-__device__ __forceinline__ void kept_codes(const float (&v)[8], float over, bool draws, uint32_t group, uint32_t row, uint32_t call,
-                                           const PhiloxKeys& keys, uint32_t (&word)[2])
+// A code rounded to the nearest whole number, into byte `at` of a word: u = the element over the block's power of two.
+__device__ __forceinline__ uint32_t kept_code(float u, uint32_t at, uint32_t word)
 {
-    uint32_t code[8];
+    return __builtin_amdgcn_cvt_pk_u8_f32(rintf(u) + 128.0f, at, word);
+}
+
+// Rounded away from zero where the draw d, 16 bits, is below 2^16 times the remainder of |u|, as a signed byte: with T = ceil(2^16 |u|), a whole number of 23
+// bits, the magnitude is (T + 65535 - d) >> 16.  u16 = 2^16 u: a product by a power of two; rest = 65535 - d.
+__device__ __forceinline__ uint32_t kept_code(float u16, uint32_t rest)
+{
+    const uint32_t T = (uint32_t)ceilf(fabsf(u16)), minus = (uint32_t)(__float_as_int(u16) >> 31);
+    return (((T + rest) >> 16) ^ minus) - minus;
+}
+
+// The codes of W neighbouring columns, as the words that are stored, and the block's power, from the bits of its largest magnitude.  W = 8: the columns of one
+// Philox block; W = 4: its half `half`.
+template <int W>
+__device__ __forceinline__ uint32_t kept_codes(float (&v)[W], uint32_t bits, uint32_t top, bool draws, uint32_t group, uint32_t half, uint32_t row, uint32_t call,
+                                               const PhiloxKeys& keys, uint32_t (&word)[W / 4])
+{
+    uint32_t power = kept_power(bits);
+    uint32_t over = (254u - power) << 23;                  // 2^-e (of zeros it may be anything)
+    float wide = 65536.0f;
+    if (__builtin_amdgcn_ballot_w64(kept_is_rare(bits, power, top)) != 0ull) {
+        if (bits >= 0x7F800000u) {
+            power = kKeptSpoilt;
+            over = 0u;
+#pragma unroll
+            for (int c = 0; c < W; ++c) v[c] = 0.0f;       // (0 * infinity is no zero)
+        } else if (bits) {
+            power = min(max(power, 1u), top);
+            over = (254u - power) << 23;
+            const float most = __uint_as_float(power << 23) * 127.0f;
+#pragma unroll
+            for (int c = 0; c < W; ++c) v[c] = __builtin_amdgcn_fmed3f(v[c], -most, most);
+            if (power < 16u && draws) {                    // (the elements by 2^16, which are small then)
+#pragma unroll
+                for (int c = 0; c < W; ++c) v[c] *= 65536.0f;
+                wide = 1.0f;
+            }
+        }
+    }
     if (draws) {
         uint32_t w[4];
         philox4x32_10(group, 2u, row, call, keys, w);
+        if (W == 4 && half) { w[0] = w[2]; w[1] = w[3]; }
+        const float over16 = __uint_as_float(over) * wide;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) code[c] = kept_code(v[c] * over, (c & 1) ? w[c / 2] >> 16 : w[c / 2] & 0xFFFFu);
+        for (int h = 0; h < W / 4; ++h) {
+            uint32_t code[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint32_t rest = ~w[2 * h + c / 2];
+                code[c] = kept_code(v[4 * h + c] * over16, (c & 1) ? rest >> 16 : rest & 0xFFFFu);
+            }
+            const uint32_t lo = __builtin_amdgcn_perm(code[1], code[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(code[3], code[2], 0x04000C0Cu);
+            word[h] = (lo | hi) ^ 0x80808080u;
+        }
     } else {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) code[c] = kept_code(v[c] * over);
-    }
+        for (int h = 0; h < W / 4; ++h) {
+            word[h] = 0u;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) word[h] = code[4 * h] | code[4 * h + 1] << 8 | code[4 * h + 2] << 16 | code[4 * h + 3] << 24;
+            for (int c = 0; c < 4; ++c) word[h] = kept_code(v[4 * h + c] * __uint_as_float(over), (uint32_t)c, word[h]);
+        }
+    }
+    return power;
+}
+
+// The bits of the largest magnitude of a piece's elements, as binary32's: of 16-bit elements two at a time.
+template <typename T>
+__device__ __forceinline__ uint32_t largest_bits(nt_u32x4 x)
+{
+    if constexpr (sizeof(T) == 4) {
+        const nt_u32x4 m = x & 0x7FFFFFFFu;
+        return max(max(m[0], m[1]), max(m[2], m[3]));
+    } else {
+        typedef uint16_t pair __attribute__((ext_vector_type(2)));
+        pair m = __builtin_bit_cast(pair, (uint32_t)x[0] & 0x7FFF7FFFu);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(pair, (uint32_t)x[i] & 0x7FFF7FFFu));
+        const uint16_t most = m.x > m.y ? m.x : m.y;
+        if constexpr (__is_same(T, _Float16)) return __float_as_uint((float)__builtin_bit_cast(_Float16, most));
+        else return (uint32_t)most << 16;
+    }
 }
 
 // The largest over the four lanes of a block.

@@ -1452,14 +1452,16 @@ qgx_status qgx_group_norm(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_
     a.x = x->data; a.x_worker = x->s_worker; a.x_batch = x->s_batch; a.x_place = x->s_place;
     a.y = y->data; a.y_worker = y->s_worker; a.y_batch = y->s_batch; a.y_place = y->s_place;
     a.w = weight; a.b = bias; a.mean = mean; a.rstd = rstd; a.eps = eps; a.scratch = (float*)scratch;
-    if (keep) {
+    if (keep && group_keeps(plan, a.channels)) {
+        a.keep_codes = keep->codes; a.keep_powers = keep->powers; a.keep_top = kept_top(shape->dtype); a.draws = kept_draws(ctx, unbiased, call_id);
+    } else if (keep) {
         KeepArgs k{};
-        k.x = x->data; k.codes = keep->codes; k.powers = keep->powers;
-        k.x_worker = x->s_worker; k.x_batch = x->s_batch; k.x_row = x->s_place;
-        k.batch = (uint32_t)shape->batch; k.rows = a.places; k.n_rows = a.samples * a.places; k.cols = a.channels; k.blocks = kept_blocks(a.channels); k.top = kept_top(shape->dtype);
+        k.x = x->data; k.codes = keep->codes; k.powers = keep->powers; k.x_worker = x->s_worker; k.x_batch = x->s_batch; k.x_row = x->s_place;
+        k.batch = (uint32_t)shape->batch; k.rows = a.places; k.n_rows = a.samples * a.places; k.cols = a.channels; k.blocks = kept_blocks(a.channels);
+        k.top = kept_top(shape->dtype);
         QGX_HIP(ctx, launch_checkpoint(shape->dtype, k, kept_draws(ctx, unbiased, call_id), ctx->d_sc, (hipStream_t)stream));
     }
-    QGX_HIP(ctx, launch_group_norm(shape->dtype, a, (uint32_t)shape->workers, plan, (hipStream_t)stream));
+    QGX_HIP(ctx, launch_group_norm(shape->dtype, a, (uint32_t)shape->workers, plan, ctx->d_sc, (hipStream_t)stream));
     return QGX_OK;
 }
 
