@@ -5,7 +5,8 @@ Bounds, u = 2^-24.  A group's or a channel's sum is made of a thread's places on
 with a mean's update of three roundings each) and then of the threads' in runs and trees of at most 256 terms more, or of a group wider than that its
 entries / 256: S = (320 + places * per / 65536 + parts) u of the sum of magnitudes covers all of them.  mean: S mean|x|; x - mean: that and u |x - mean|; the variance: S and twice
 the shift's square over it; rstd half of that and 3 u.  h: relative rstd's error, and the shift times rstd.  z = h w + b: three roundings.  Activations: |silu'| <= 1.1, |silu''|
-<= 0.5, the sigmoid good to (6 + 2 |z|) u.  Backward from the given mean and rstd: h by 3 u |h|; dz by its factor's error; sums as above; dx four more roundings.  Last the type's
+<= 0.5, the sigmoid good to (6 + 2 |z|) u.  Backward from the given mean and rstd: h by 3 u |h|, or from a kept element by one product and one sum of its code, 2 u (255 scale +
+|mean|) rstd; dz by its factor's error; sums as above; dx four more roundings.  Last the type's
 own rounding."""
 import math
 
@@ -183,7 +184,7 @@ def test_no_numbers_stay_in_their_group(ctx, P, C, G, bad):
 # -- backward -----------------------------------------------------------------------------------------------------------
 
 
-def check_backward(x, dy, G, w, b, mean, rstd, kind, dx, dw, db, typ):
+def check_backward(x, dy, G, w, b, mean, rstd, kind, dx, dw, db, typ, scale=None):
     """[workers, batch, places, channels] numpy, mean and rstd as the kernel sees them."""
     g = grouped(x, G)
     n = x.shape[-2] * g.shape[-1]
@@ -193,6 +194,8 @@ def check_backward(x, dy, G, w, b, mean, rstd, kind, dx, dw, db, typ):
     z = h * w + b
     _, d = act(z, kind)
     zerr = 4 * U * (np.abs(h * w) + np.abs(b))
+    if scale is not None:
+        zerr = zerr + 2 * U * np.abs(w) * ((255 * grouped(scale, G) + np.abs(mu)) * r).reshape(x.shape)
     derr = 0.5 * zerr + (10 + 3 * np.abs(z)) * U * (np.abs(d) + np.abs(z) * 0.25 + 0.25) if kind == "silu" else U * np.abs(d)
     if kind == "leaky":                                    # next to 0 binary32 decides by the header's operations
         xs, f32 = x.astype(np.float32), np.float32
@@ -202,6 +205,8 @@ def check_backward(x, dy, G, w, b, mean, rstd, kind, dx, dw, db, typ):
     dz = dy * d
     dzerr = np.abs(dy) * derr + U * np.abs(dz)
     herr = 3 * U * np.abs(h)
+    if scale is not None:
+        herr = herr + 2 * U * ((255 * grouped(scale, G) + np.abs(mu)) * r).reshape(x.shape)
     batch = x.shape[1]
     for got, terms, terr in ((dw, dz * h, dzerr * np.abs(h) + np.abs(dz) * herr), (db, dz, dzerr)):
         if got is not None:
@@ -233,7 +238,8 @@ def run_backward(ctx, x, dy, G, w, b, kind, typ, source=None, **kw):
     dw, db = torch.full((K, C), 9.0, device="cuda"), torch.full((K, C), 9.0, device="cuda")
     dx = ctx.group_norm_backward(dy, x if source is None else source, G, w, b, mean, rstd, kind, SLOPE, dw=dw, db=db, **kw)
     seen = host(x) if source is None else host(ctx.restore(source))
-    check_backward(seen, host(dy), G, np.float64(1) if w is None else host(w), np.float64(0) if b is None else host(b), host(mean), host(rstd), kind, dx, dw, db, typ)
+    scale = None if source is None else np.exp2(host(source.powers) - 127.0).repeat(32, -1)[..., :C]
+    check_backward(seen, host(dy), G, np.float64(1) if w is None else host(w), np.float64(0) if b is None else host(b), host(mean), host(rstd), kind, dx, dw, db, typ, scale)
     return dx, dw, db
 
 
