@@ -438,8 +438,7 @@ struct RotaryArgs {
     uint32_t batch, tokens, heads, dim, n_tokens, pairs;      // n_tokens: of all workers and sequences
     uint32_t axis_end[QGX_MAX_AXES];       // pairs up to an axis' last
     int32_t neighbours, back;
-    double turns[QGX_MAX_PAIRS];           // frequencies / 2 pi
 };
-hipError_t launch_rotary(int dtype, const RotaryArgs& a, uint32_t n_cu, hipStream_t st);
+hipError_t launch_rotary(int dtype, const RotaryArgs& a, const double* turns /* HOST [pairs]: frequencies / 2 pi */, uint32_t n_cu, hipStream_t st);
 
 }  // namespace qgx

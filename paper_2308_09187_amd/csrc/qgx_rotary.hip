@@ -17,8 +17,11 @@ __device__ __forceinline__ float2 cos_sin_of(double turns)
     return make_float2(c, s);
 }
 
-template <typename T, bool NEIGHBOURS>
-__global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, uint32_t tile_tokens, uint32_t turned, uint32_t items)
+// The frequencies come with the launch; PAIRS: as many as there is room for (the fewer, the sooner a launch is made).
+template <int PAIRS> struct Frequencies { double turns[PAIRS]; };
+
+template <typename T, bool NEIGHBOURS, int PAIRS>
+__global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, Frequencies<PAIRS> f, uint32_t tile_tokens, uint32_t turned, uint32_t items)
 {
     constexpr int W = kPiece<T>;
     __shared__ float s_cos[kTurnAngles], s_sin[kTurnAngles];
@@ -31,7 +34,7 @@ __global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, uint32_t 
 #pragma unroll
             for (uint32_t x = 0; x + 1 < QGX_MAX_AXES; ++x) axis += p >= a.axis_end[x];
             const int32_t at = a.positions[axis * a.p_axis + sequence / a.batch * a.p_worker + sequence % a.batch * a.p_batch + t];
-            const float2 cs = cos_sin_of((double)at * a.turns[p]);
+            const float2 cs = cos_sin_of((double)at * f.turns[p]);
             s_cos[i] = cs.x;
             s_sin[i] = a.back ? -cs.y : cs.y;
         }
@@ -81,8 +84,8 @@ __global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, uint32_t 
     }
 }
 
-template <typename T>
-static hipError_t launch_rotary_of(const RotaryArgs& a, uint32_t n_cu, hipStream_t st)
+template <typename T, int PAIRS>
+static hipError_t launch_rotary_as(const RotaryArgs& a, const double* turns, uint32_t n_cu, hipStream_t st)
 {
     constexpr uint32_t W = kPiece<T>;
     const uint32_t turned = a.neighbours ? (2u * a.pairs + W - 1u) / W : (a.pairs + W - 1u) / W;
@@ -90,17 +93,25 @@ static hipError_t launch_rotary_of(const RotaryArgs& a, uint32_t n_cu, hipStream
     const uint32_t most = max(1u, min(kTurnAngles / a.pairs, (1u << 30) / (a.heads * items)));
     const uint32_t tile = min(most, max(1u, a.n_tokens / (8u * n_cu)));
     const dim3 grid(min((a.n_tokens + tile - 1u) / tile, 1u << 20));
-    if (a.neighbours) hipLaunchKernelGGL((k_rotary<T, true>), grid, dim3(kTurnThreads), 0, st, a, tile, turned, items);
-    else hipLaunchKernelGGL((k_rotary<T, false>), grid, dim3(kTurnThreads), 0, st, a, tile, turned, items);
+    Frequencies<PAIRS> f;
+    for (uint32_t p = 0; p < (uint32_t)PAIRS; ++p) f.turns[p] = p < a.pairs ? turns[p] : 0.0;
+    if (a.neighbours) hipLaunchKernelGGL((k_rotary<T, true, PAIRS>), grid, dim3(kTurnThreads), 0, st, a, f, tile, turned, items);
+    else hipLaunchKernelGGL((k_rotary<T, false, PAIRS>), grid, dim3(kTurnThreads), 0, st, a, f, tile, turned, items);
     return hipGetLastError();
 }
 
-hipError_t launch_rotary(int dtype, const RotaryArgs& a, uint32_t n_cu, hipStream_t st)
+template <typename T>
+static hipError_t launch_rotary_of(const RotaryArgs& a, const double* turns, uint32_t n_cu, hipStream_t st)
+{
+    return a.pairs <= 64u ? launch_rotary_as<T, 64>(a, turns, n_cu, st) : launch_rotary_as<T, (int)QGX_MAX_PAIRS>(a, turns, n_cu, st);
+}
+
+hipError_t launch_rotary(int dtype, const RotaryArgs& a, const double* turns, uint32_t n_cu, hipStream_t st)
 {
     if (a.n_tokens == 0) return hipSuccess;
-    return dtype == QGX_F32   ? launch_rotary_of<float>(a, n_cu, st)
-           : dtype == QGX_F16 ? launch_rotary_of<_Float16>(a, n_cu, st)
-                              : launch_rotary_of<__bf16>(a, n_cu, st);
+    return dtype == QGX_F32   ? launch_rotary_of<float>(a, turns, n_cu, st)
+           : dtype == QGX_F16 ? launch_rotary_of<_Float16>(a, turns, n_cu, st)
+                              : launch_rotary_of<__bf16>(a, turns, n_cu, st);
 }
 
 }  // namespace qgx

@@ -253,10 +253,20 @@ class Checkpoint:
         for t, n, name in ((codes, KEPT_BLOCK * blocks, "codes"), (powers, blocks, "powers")):
             _need(t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous() and t.dim() >= 1 and t.shape[-1] == n, "%s: contiguous uint8 [.., %d] on the GPU", name, n)
         _need(codes.shape[:-1] == powers.shape[:-1] and codes.get_device() == powers.get_device(), "codes and powers: of the same rows")
-        self.codes, self.powers = codes, powers
-        self.shape = codes.shape[:-1] + (cols,)
-        self._c = _Kept(codes.data_ptr(), powers.data_ptr(), math.prod(self.shape[:-1]), cols)
+        self._set(codes, powers, codes.shape[:-1] + (cols,))
+
+    def _set(self, codes, powers, shape):
+        self.codes, self.powers, self.shape = codes, powers, shape
+        self._c = _Kept(codes.data_ptr(), powers.data_ptr(), math.prod(shape[:-1]), shape[-1])
         self._ref = C.addressof(self._c)
+        return self
+
+    @classmethod
+    def _made(cls, like, shape, stream):
+        """Memory for rows of this shape on like's device."""
+        blocks = (shape[-1] + KEPT_BLOCK - 1) // KEPT_BLOCK
+        lead = shape[:-1]
+        return cls.__new__(cls)._set(_empty(like, lead + (KEPT_BLOCK * blocks,), torch.uint8, stream), _empty(like, lead + (blocks,), torch.uint8, stream), shape)
 
 
 class Rotary:
@@ -324,6 +334,7 @@ class Context:
         self._h = C.c_void_p()
         self._need_bytes = C.c_uint64()           # where the scratch functions answer
         self._need_ref = C.addressof(self._need_bytes)
+        self._like = torch.empty(0, dtype=torch.uint8, device=device)
         self._table, self._n_sym = 0, {}          # the table selected; symbols of each table that was set
         with torch.cuda.device(device):
             st = self.lib.qgx_create(C.byref(self._h), C.byref(cfg))
@@ -624,11 +635,9 @@ class Context:
     def new_checkpoint(self, shape, stream=None):
         """Memory for an activation of this shape, the last dimension its columns (its contents are what checkpoint or group_norm put
         there)."""
-        lead, cols = tuple(shape[:-1]), int(shape[-1])
-        blocks = (cols + KEPT_BLOCK - 1) // KEPT_BLOCK
-        _need(cols >= 1, "new_checkpoint: columns")
-        like = torch.empty(0, dtype=torch.uint8, device=self.device)
-        return Checkpoint(_empty(like, lead + (KEPT_BLOCK * blocks,), torch.uint8, stream), _empty(like, lead + (blocks,), torch.uint8, stream), cols)
+        shape = torch.Size(shape)
+        _need(len(shape) >= 1 and shape[-1] >= 1, "new_checkpoint: columns")
+        return Checkpoint._made(self._like, shape, stream)
 
     @staticmethod
     def _kept_rows(x, name):
@@ -647,8 +656,10 @@ class Context:
         draws of that call."""
         code, wk, rows, cols, xw, xr = self._kept_rows(x, "x")
         if out is None:
-            out = self.new_checkpoint(x.shape, stream)
-        _need(out.shape == x.shape and out.codes.get_device() == x.get_device(), "out: a checkpoint of x's shape, on its device")
+            _need(cols >= 1, "x: columns")
+            out = Checkpoint._made(x, x.shape, stream)
+        else:
+            _need(out.shape == x.shape and out.codes.get_device() == x.get_device(), "out: a checkpoint of x's shape, on its device")
         _need(call_id is None or 0 <= call_id < 1 << 32, "call_id: 32 bits")
         st = self.lib.qgx_checkpoint(self._h, code, wk, rows, cols, x.data_ptr(), xw, xr, call_id is not None, call_id or 0, out._ref, _handle(stream, x))
         if st:
@@ -658,13 +669,15 @@ class Context:
     def restore(self, kept: Checkpoint, dtype=torch.float32, out=None, stream=None):
         """The kept elements, rounded once to dtype."""
         cols = kept.shape[-1]
-        if out is None:
-            out = _empty(kept.codes, kept.shape, dtype, stream)
-        _need(out.shape == kept.shape and out.dtype in DTYPES and out.get_device() == kept.codes.get_device(), "out: of the kept shape, on its device")
         step = cols
-        if not out.is_contiguous():
-            _need(out.dim() == 2 and out.stride(1) == 1, "out: contiguous, or [rows, cols] with contiguous rows")
-            step = out.stride(0)
+        if out is None:
+            _need(dtype in DTYPES, "dtype: float32, float16 or bfloat16")
+            out = _empty(kept.codes, kept.shape, dtype, stream)
+        else:
+            _need(out.shape == kept.shape and out.dtype in DTYPES and out.get_device() == kept.codes.get_device(), "out: of the kept shape, on its device")
+            if not out.is_contiguous():
+                _need(out.dim() == 2 and out.stride(1) == 1, "out: contiguous, or [rows, cols] with contiguous rows")
+                step = out.stride(0)
         st = self.lib.qgx_restore(self._h, kept._ref, DTYPES[out.dtype], out.data_ptr(), step, _handle(stream, out))
         if st:
             self._check(st)
@@ -695,22 +708,27 @@ class Context:
         return dw
 
     @staticmethod
-    def _places(t, like, name):
+    def _places(t, name):
         """Address and steps of [workers, batch, places, channels], [batch, places, channels] or [places, channels]."""
-        _need(t.shape == like.shape and t.dtype == like.dtype and t.get_device() == like.get_device(), "%s: of x's shape and type, on its device", name)
         step = t.stride()
         n = len(step)
         _need(2 <= n <= 4 and (step[-1] == 1 or t.shape[-1] <= 1), "%s: [workers, batch, places, channels], channels contiguous", name)
         return _Places(t.data_ptr(), step[0] if n == 4 else 0, step[-3] if n > 2 else 0, step[-2])
 
+    @classmethod
+    def _places_like(cls, t, like, name):
+        """The same of a tensor of like's shape and type."""
+        _need(t.shape == like.shape and t.dtype == like.dtype and t.get_device() == like.get_device(), "%s: of x's shape and type, on its device", name)
+        return cls._places(t, name)
+
     @staticmethod
     def _group_shape(t, groups, activation, slope, name):
-        code, sh = DTYPES.get(t.dtype), t.shape
-        _need(code is not None and t.is_cuda, "%s: float32, float16 or bfloat16 on the GPU", name)
-        _need(2 <= len(sh) <= 4, "%s: [workers, batch, places, channels], [batch, places, channels] or [places, channels]", name)
-        _need(activation in ACTIVATIONS, "activation: one of %s", ", ".join(ACTIVATIONS))
+        code, sh, act = DTYPES.get(t.dtype), t.shape, ACTIVATIONS.get(activation)
+        n = len(sh)
+        _need(code is not None and t.is_cuda and 2 <= n <= 4, "%s: [workers, batch, places, channels] of float32, float16 or bfloat16 on the GPU", name)
+        _need(act is not None, "activation: none, silu or leaky")
         _need(0 < groups < 1 << 32 and sh[-1] % groups == 0, "groups: a divisor of the channels")
-        return _GroupShape(code, ACTIVATIONS[activation], slope, groups, sh[0] if len(sh) == 4 else 1, sh[-3] if len(sh) > 2 else 1, sh[-2], sh[-1])
+        return _GroupShape(code, act, slope, groups, sh[0] if n == 4 else 1, sh[-3] if n > 2 else 1, sh[-2], sh[-1])
 
     def _group_scratch(self, shape, backward, like, stream):
         st = self.lib.qgx_group_norm_scratch(self._h, C.addressof(shape), backward, self._need_ref)
@@ -725,11 +743,13 @@ class Context:
         Checkpoint in which x is kept as well, as checkpoint(x, call_id) would."""
         shape = self._group_shape(x, groups, activation, slope, "x")
         channels = x.shape[-1]
-        src = self._places(x, x, "x")
+        src = self._places(x, "x")
         w, b = _parameter(weight, (channels,), "weight"), _parameter(bias, (channels,), "bias")
         if out is None:
             out = _empty_like(x, stream)
-        dst = self._places(out, x, "out")
+            dst = _Places(out.data_ptr(), shape.batch * shape.places * channels, shape.places * channels, channels)
+        else:
+            dst = self._places_like(out, x, "out")
         _need(keep is None or (keep.shape == x.shape and keep.codes.get_device() == x.get_device()), "keep: a checkpoint of x's shape, on its device")
         _need(call_id is None or 0 <= call_id < 1 << 32, "call_id: 32 bits")
         mean = rstd = None
@@ -749,12 +769,12 @@ class Context:
         of V's rows say ([channels] where dy has no worker dimension).  x: the forward pass's input, or a Checkpoint of it."""
         shape = self._group_shape(dy, groups, activation, slope, "dy")
         channels, wk = dy.shape[-1], shape.workers
-        grad = self._places(dy, dy, "dy")
+        grad = self._places(dy, "dy")
         src = None
         if isinstance(x, Checkpoint):
             _need(x.shape == dy.shape and x.codes.get_device() == dy.get_device(), "x: a checkpoint of dy's shape, on its device")
         else:
-            src = self._places(x, dy, "x")
+            src = self._places_like(x, dy, "x")
         w, b = _parameter(weight, (channels,), "weight"), _parameter(bias, (channels,), "bias")
         lead = dy.shape[:-2] + (groups,)
         m, r = _parameter(mean, lead, "mean"), _parameter(rstd, lead, "rstd")
@@ -769,10 +789,10 @@ class Context:
             step = s
         dst = None
         if dx is not None:
-            dst = self._places(dx, dy, "dx")
+            dst = self._places_like(dx, dy, "dx")
         elif need_dx:
             dx = _empty_like(dy, stream)
-            dst = self._places(dx, dy, "dx")
+            dst = _Places(dx.data_ptr(), shape.batch * shape.places * channels, shape.places * channels, channels)
         scratch = self._group_scratch(shape, 1, dy, stream)
         st = self.lib.qgx_group_norm_backward(
             self._h, C.addressof(shape), C.addressof(grad), None if src is None else C.addressof(src), x._ref if src is None else None, w, b, m, r,
@@ -797,11 +817,14 @@ class Context:
         """x [.., batch, tokens, heads, dim] turned by its tokens' positions, int32 [axes, tokens] (the same for all sequences) or [axes, ..,
         tokens] of x's leading dimensions.  back: by the angles' negatives, the backward pass.  out may be x."""
         src = self._heads(x, "x")
-        _need(rotary.pairs is not None and 2 * sum(rotary.pairs) <= x.shape[-1], "rotary: more pairs than a head has")
+        dst = src
         if out is None:
             out = _empty_like(x, stream)
-        _need(out.shape == x.shape and out.dtype == x.dtype and out.get_device() == x.get_device(), "out: of x's shape and type, on its device")
-        dst = self._heads(out, "out")
+            step = src.heads * src.dim
+            dst = _Heads(out.data_ptr(), src.dtype, src.heads, src.dim, src.workers, src.batch, src.tokens, src.batch * src.tokens * step, src.tokens * step, step, src.dim)
+        elif out is not x:
+            _need(out.shape == x.shape and out.dtype == x.dtype and out.get_device() == x.get_device(), "out: of x's shape and type, on its device")
+            dst = self._heads(out, "out")
         ps, pst, axes = positions.shape, positions.stride(), len(rotary.pairs)
         _need(positions.get_device() == x.get_device() and positions.dtype == torch.int32 and (ps == (axes, x.shape[-3]) or ps == (axes,) + x.shape[:-2]) and
               (ps[-1] <= 1 or pst[-1] == 1), "positions: int32 [axes, tokens] or [axes, .., tokens], tokens contiguous, on x's device")
