@@ -190,26 +190,37 @@ __device__ __forceinline__ void activate_back(float (&dy)[W], const float (&h)[W
     }
 }
 
+constexpr int kGroupsMost = 256;                           // groups of a workgroup
+
 // ---- sums over a workgroup ------------------------------------------------------------------------------------------------
 
-// The threads' sums of their channels in LDS, joined over the places: afterwards [runs][slots], slot j W + c the piece j's channel c.
+// The threads' sums of their channels in LDS, M numbers of each, joined over the places: afterwards [M][THREADS * W] with [runs][slots] in each, slot
+// j W + c the piece j's channel c.
 struct Runs { uint32_t runs, slots; };
-template <int THREADS, int W>
-__device__ __forceinline__ Runs column_sums(const float (&x)[W], uint32_t pieces, float* s)
+template <int THREADS, int W, int M>
+__device__ __forceinline__ Runs column_sums(const float (&x)[M][W], uint32_t pieces, float* s)
 {
     const uint32_t slots = pieces * W, steps = THREADS / pieces;
     __syncthreads();                                       // (the memory may have been read for the sums before)
 #pragma unroll
-    for (int h = 0; h < W / 4; ++h)
-        *reinterpret_cast<float4*>(s + threadIdx.x * W + 4 * h) = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int h = 0; h < W / 4; ++h)
+            *reinterpret_cast<float4*>(s + (m * THREADS + threadIdx.x) * W + 4 * h) = make_float4(x[m][4 * h], x[m][4 * h + 1], x[m][4 * h + 2], x[m][4 * h + 3]);
     __syncthreads();
     if (slots > THREADS) return Runs{steps, slots};
     const uint32_t runs = THREADS / slots, run = threadIdx.x / slots, col = threadIdx.x % slots;
-    float sum = 0.0f;
-    if (run < runs)
-        for (uint32_t i = run; i < steps; i += runs) sum += s[i * slots + col];
+    float sum[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        sum[m] = 0.0f;
+        if (run < runs)
+            for (uint32_t i = run; i < steps; i += runs) sum[m] += s[m * THREADS * W + i * slots + col];
+    }
     __syncthreads();
-    if (run < runs) s[threadIdx.x] = sum;                  // run * slots + col
+    if (run < runs)
+#pragma unroll
+        for (int m = 0; m < M; ++m) s[m * THREADS * W + threadIdx.x] = sum[m];          // run * slots + col
     __syncthreads();
     return Runs{runs, slots};
 }
@@ -220,33 +231,38 @@ __device__ __forceinline__ uint32_t slot_of(uint32_t channel, uint32_t pieces, u
     return SHORT || channel < (pieces - 1u) * W ? channel : channel + pieces * W - span;
 }
 
-// Every group's sum of what column_sums left, each times its channel's weight: out[group].  A wave takes a group.
-template <int THREADS, int W, bool SHORT>
-__device__ __forceinline__ void group_sums(Runs r, uint32_t pieces, uint32_t span, uint32_t per, const float* weight, const float* s, float* out)
+// Every group's sums of what column_sums left, each times its channel's weight: out[m][group].  A wave takes a group.
+template <int THREADS, int W, bool SHORT, int M>
+__device__ __forceinline__ void group_sums(Runs r, uint32_t pieces, uint32_t span, uint32_t per, const float* weight, const float* s, float (*out)[kGroupsMost])
 {
     const uint32_t groups = span / per, n = r.runs * per;
     for (uint32_t g = wave_id(); g < groups; g += THREADS / kWave) {
-        float sum = 0.0f;
+        float sum[M];
+#pragma unroll
+        for (int m = 0; m < M; ++m) sum[m] = 0.0f;
         for (uint32_t i = lane_id(); i < n; i += kWave) {
-            const uint32_t c = g * per + i % per;
-            sum = fmaf(s[i / per * r.slots + slot_of<W, SHORT>(c, pieces, span)], weight ? weight[c] : 1.0f, sum);
+            const uint32_t c = g * per + i % per, at = i / per * r.slots + slot_of<W, SHORT>(c, pieces, span);
+            const float w = weight ? weight[c] : 1.0f;
+#pragma unroll
+            for (int m = 0; m < M; ++m) sum[m] = fmaf(s[m * THREADS * W + at], w, sum[m]);
         }
-        sum = lanes_sum<kWave>(sum);
-        if (lane_id() == 0) out[g] = sum;
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            sum[m] = lanes_sum<kWave>(sum[m]);
+            if (lane_id() == 0) out[m][g] = sum[m];
+        }
     }
     __syncthreads();
 }
 
 // ---- forward, whole groups ------------------------------------------------------------------------------------------------
 
-constexpr int kGroupsMost = 256;                           // groups of a workgroup
-
 template <typename T, int THREADS, int N, bool SHORT>
 __global__ __launch_bounds__(THREADS) void k_group_norm(GroupArgs a, uint32_t batch)
 {
     constexpr int W = kPiece<T>;
     __shared__ __align__(16) float s_sums[THREADS * W];
-    __shared__ float s_mean[kGroupsMost], s_rstd[kGroupsMost];
+    __shared__ float s_mean[1][kGroupsMost], s_rstd[1][kGroupsMost];
     const uint32_t unit = unit_of_block(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
     const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = THREADS / pieces;
     const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
@@ -260,25 +276,25 @@ __global__ __launch_bounds__(THREADS) void k_group_norm(GroupArgs a, uint32_t ba
         const uint32_t p = i * steps + step;
         raw[i] = any && p < a.places ? load_place<T, false, SHORT>(places, p, at.n) : no_place<T, false>();
     }
-    float sum[W];
+    float sum[1][W];
 #pragma unroll
-    for (int c = 0; c < W; ++c) sum[c] = 0.0f;
+    for (int c = 0; c < W; ++c) sum[0][c] = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         float v[W];
         values_at(raw[i], places, v);
 #pragma unroll
-        for (int c = 0; c < W; ++c) sum[c] += v[c];
+        for (int c = 0; c < W; ++c) sum[0][c] += v[c];
     }
 #pragma unroll
-    for (int c = 0; c < W; ++c) sum[c] = at.owns(c) ? sum[c] : 0.0f;
-    Runs r = column_sums<THREADS, W>(sum, pieces, s_sums);
-    group_sums<THREADS, W, SHORT>(r, pieces, span, a.per, nullptr, s_sums, s_mean);
+    for (int c = 0; c < W; ++c) sum[0][c] = at.owns(c) ? sum[0][c] : 0.0f;
+    Runs r = column_sums<THREADS, W, 1>(sum, pieces, s_sums);
+    group_sums<THREADS, W, SHORT, 1>(r, pieces, span, a.per, nullptr, s_sums, s_mean);
     float mean[W], rstd[W];
 #pragma unroll
     for (int c = 0; c < W; ++c) {
-        mean[c] = s_mean[min((uint32_t)(at.c + c) - first, span - 1u) / a.per] / n;
-        sum[c] = 0.0f;
+        mean[c] = s_mean[0][min((uint32_t)(at.c + c) - first, span - 1u) / a.per] / n;
+        sum[0][c] = 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -289,24 +305,24 @@ __global__ __launch_bounds__(THREADS) void k_group_norm(GroupArgs a, uint32_t ba
 #pragma unroll
         for (int c = 0; c < W; ++c) {
             const float t = ok ? v[c] - mean[c] : 0.0f;
-            sum[c] = fmaf(t, t, sum[c]);
+            sum[0][c] = fmaf(t, t, sum[0][c]);
         }
     }
 #pragma unroll
-    for (int c = 0; c < W; ++c) sum[c] = at.owns(c) ? sum[c] : 0.0f;
-    r = column_sums<THREADS, W>(sum, pieces, s_sums);
-    group_sums<THREADS, W, SHORT>(r, pieces, span, a.per, nullptr, s_sums, s_rstd);
+    for (int c = 0; c < W; ++c) sum[0][c] = at.owns(c) ? sum[0][c] : 0.0f;
+    r = column_sums<THREADS, W, 1>(sum, pieces, s_sums);
+    group_sums<THREADS, W, SHORT, 1>(r, pieces, span, a.per, nullptr, s_sums, s_rstd);
     const uint32_t own_groups = span / a.per;
     for (uint32_t g = threadIdx.x; g < own_groups; g += THREADS) {
         const size_t to = (size_t)sample * a.groups + first / a.per + g;
-        if (a.mean) a.mean[to] = s_mean[g] / n;
-        if (a.rstd) a.rstd[to] = 1.0f / sqrtf(s_rstd[g] / n + a.eps);
+        if (a.mean) a.mean[to] = s_mean[0][g] / n;
+        if (a.rstd) a.rstd[to] = 1.0f / sqrtf(s_rstd[0][g] / n + a.eps);
     }
     float w[W], b[W];
     channel_parameters<W>(a.w, at, 1.0f, w);
     channel_parameters<W>(a.b, at, 0.0f, b);
 #pragma unroll
-    for (int c = 0; c < W; ++c) rstd[c] = 1.0f / sqrtf(s_rstd[min((uint32_t)(at.c + c) - first, span - 1u) / a.per] / n + a.eps);
+    for (int c = 0; c < W; ++c) rstd[c] = 1.0f / sqrtf(s_rstd[0][min((uint32_t)(at.c + c) - first, span - 1u) / a.per] / n + a.eps);
     T* y = (T*)a.y + sample / batch * a.y_worker + sample % batch * a.y_batch + at.c;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -362,7 +378,7 @@ template <typename T, int THREADS, int N, bool KEPT, bool SHORT>
 __global__ __launch_bounds__(THREADS) void k_group_norm_back(GroupArgs a, uint32_t batch)
 {
     constexpr int W = kPiece<T>;
-    __shared__ __align__(16) float s_sums[THREADS * W];
+    __shared__ __align__(16) float s_sums[2 * THREADS * W];
     __shared__ float s_group[2][kGroupsMost];
     const uint32_t unit = unit_of_block(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
     const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = THREADS / pieces;
@@ -399,21 +415,24 @@ __global__ __launch_bounds__(THREADS) void k_group_norm_back(GroupArgs a, uint32
         }
     }
     const float* weight = a.w ? a.w + first : nullptr;
+    float sum[2][W];
+#pragma unroll
+    for (int c = 0; c < W; ++c) {
+        sum[0][c] = at.owns(c) ? dw[c] : 0.0f;
+        sum[1][c] = at.owns(c) ? db[c] : 0.0f;
+    }
+    const Runs r = column_sums<THREADS, W, 2>(sum, pieces, s_sums);
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        float sum[W];
-#pragma unroll
-        for (int c = 0; c < W; ++c) sum[c] = at.owns(c) ? (which ? db[c] : dw[c]) : 0.0f;
-        const Runs r = column_sums<THREADS, W>(sum, pieces, s_sums);
         float* to = channel_sums_at(a, sample, batch, 0u, which);
         if (to)
             for (uint32_t c = threadIdx.x; c < span; c += THREADS) {
-                float x = 0.0f;
-                for (uint32_t i = 0; i < r.runs; ++i) x += s_sums[i * r.slots + slot_of<W, SHORT>(c, pieces, span)];
-                to[first + c] = x;
+                float t = 0.0f;
+                for (uint32_t i = 0; i < r.runs; ++i) t += s_sums[which * THREADS * W + i * r.slots + slot_of<W, SHORT>(c, pieces, span)];
+                to[first + c] = t;
             }
-        if (a.y) group_sums<THREADS, W, SHORT>(r, pieces, span, a.per, weight, s_sums, s_group[which]);
     }
+    if (a.y) group_sums<THREADS, W, SHORT, 2>(r, pieces, span, a.per, weight, s_sums, s_group);
     if (!a.y) return;
     const float n = (float)a.places * (float)a.per;
     float minus_m1[W], minus_m2[W];
@@ -694,7 +713,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_group_norm_back_one(GroupArgs a,
 // Workgroup (part, column, sample) has `part` places from part * a.part on of `span` channels.
 
 constexpr int kPartThreads = 256;
-constexpr int kPartTurns = 4;                              // places of a thread whose loads are under way together
+constexpr int kPartTurns = 8, kBackTurns = 4;              // places of a thread whose loads are under way together
 
 // Mean and sum of squares about it of every channel over the part's places, [samples][parts][2][channels].
 template <typename T, bool SHORT>
@@ -745,10 +764,10 @@ __global__ __launch_bounds__(kPartThreads) void k_group_channels(GroupArgs a, ui
     // the threads' joined: sum of n mean, then of the squares about the whole's mean
     float* to = a.scratch + ((size_t)sample * a.parts + part) * 2u * a.channels + first;
     const float total = (float)(p1 - p0);
-    float x[W];
+    float x[1][W];
 #pragma unroll
-    for (int c = 0; c < W; ++c) x[c] = at.owns(c) ? n * mean[c] : 0.0f;
-    Runs r = column_sums<kPartThreads, W>(x, pieces, s_sums);
+    for (int c = 0; c < W; ++c) x[0][c] = at.owns(c) ? n * mean[c] : 0.0f;
+    Runs r = column_sums<kPartThreads, W, 1>(x, pieces, s_sums);
     float all[W];
 #pragma unroll
     for (int c = 0; c < W; ++c) {
@@ -759,8 +778,8 @@ __global__ __launch_bounds__(kPartThreads) void k_group_channels(GroupArgs a, ui
         if (step == 0 && at.owns(c)) to[at.c + c - (int)first] = all[c];
     }
 #pragma unroll
-    for (int c = 0; c < W; ++c) x[c] = at.owns(c) ? fmaf((mean[c] - all[c]) * (mean[c] - all[c]), n, m2[c]) : 0.0f;
-    r = column_sums<kPartThreads, W>(x, pieces, s_sums);
+    for (int c = 0; c < W; ++c) x[0][c] = at.owns(c) ? fmaf((mean[c] - all[c]) * (mean[c] - all[c]), n, m2[c]) : 0.0f;
+    r = column_sums<kPartThreads, W, 1>(x, pieces, s_sums);
     if (step == 0)
 #pragma unroll
         for (int c = 0; c < W; ++c)
@@ -854,7 +873,7 @@ template <typename T, bool KEPT, bool SHORT>
 __global__ __launch_bounds__(kPartThreads) void k_group_back_channels(GroupArgs a, uint32_t batch)
 {
     constexpr int W = kPiece<T>;
-    __shared__ __align__(16) float s_sums[kPartThreads * W];
+    __shared__ __align__(16) float s_sums[2 * kPartThreads * W];
     const uint32_t sample = blockIdx.z, part = blockIdx.x, first = blockIdx.y * a.span;
     const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = kPartThreads / pieces;
     const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
@@ -869,17 +888,17 @@ __global__ __launch_bounds__(kPartThreads) void k_group_back_channels(GroupArgs 
 #pragma unroll
     for (int c = 0; c < W; ++c) dw[c] = db[c] = 0.0f;
     if (step < steps)
-        for (uint32_t p = p0 + step; p < p1; p += steps * kPartTurns) {
-            RawPiece<T, KEPT> x[kPartTurns];
-            RawPiece<T, false> dy[kPartTurns];
+        for (uint32_t p = p0 + step; p < p1; p += steps * kBackTurns) {
+            RawPiece<T, KEPT> x[kBackTurns];
+            RawPiece<T, false> dy[kBackTurns];
 #pragma unroll
-            for (int i = 0; i < kPartTurns; ++i) {
+            for (int i = 0; i < kBackTurns; ++i) {
                 const bool ok = p + i * steps < p1;
                 x[i] = ok ? load_place<T, KEPT, SHORT>(places, p + i * steps, at.n) : no_place<T, KEPT>();
                 dy[i] = ok ? load_place<T, false, SHORT>(grads, p + i * steps, at.n) : no_place<T, false>();
             }
 #pragma unroll
-            for (int i = 0; i < kPartTurns; ++i) {
+            for (int i = 0; i < kBackTurns; ++i) {
                 if (p + i * steps >= p1) break;
                 float h[W], dz[W];
                 back_values<T, KEPT>(a, x[i], places, dy[i], grads, mean, rstd, w, b, h, dz);
@@ -891,18 +910,20 @@ __global__ __launch_bounds__(kPartThreads) void k_group_back_channels(GroupArgs 
             }
         }
     float* to = a.scratch + ((size_t)sample * a.parts + part) * 2u * a.channels;
+    float sum[2][W];
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        float sum[W];
+    for (int c = 0; c < W; ++c) {
+        sum[0][c] = at.owns(c) ? dw[c] : 0.0f;
+        sum[1][c] = at.owns(c) ? db[c] : 0.0f;
+    }
+    const Runs r = column_sums<kPartThreads, W, 2>(sum, pieces, s_sums);
 #pragma unroll
-        for (int c = 0; c < W; ++c) sum[c] = at.owns(c) ? (which ? db[c] : dw[c]) : 0.0f;
-        const Runs r = column_sums<kPartThreads, W>(sum, pieces, s_sums);
+    for (int which = 0; which < 2; ++which)
         for (uint32_t c = threadIdx.x; c < span; c += kPartThreads) {
             float x = 0.0f;
-            for (uint32_t i = 0; i < r.runs; ++i) x += s_sums[i * r.slots + slot_of<W, SHORT>(c, pieces, span)];
+            for (uint32_t i = 0; i < r.runs; ++i) x += s_sums[which * kPartThreads * W + i * r.slots + slot_of<W, SHORT>(c, pieces, span)];
             to[which * a.channels + first + c] = x;
         }
-    }
 }
 
 // A group's means of g h and g from its channels' sums.
@@ -952,17 +973,17 @@ __global__ __launch_bounds__(kPartThreads) void k_group_back_apply(GroupArgs a, 
         minus_m1[c] = -a.sums[(size_t)a.samples * a.groups + g];
     }
     T* dx = (T*)a.y + sample / batch * a.y_worker + sample % batch * a.y_batch + at.c;
-    for (uint32_t p = p0 + step; p < p1; p += steps * kPartTurns) {
-        RawPiece<T, KEPT> x[kPartTurns];
-        RawPiece<T, false> dy[kPartTurns];
+    for (uint32_t p = p0 + step; p < p1; p += steps * kBackTurns) {
+        RawPiece<T, KEPT> x[kBackTurns];
+        RawPiece<T, false> dy[kBackTurns];
 #pragma unroll
-        for (int i = 0; i < kPartTurns; ++i) {
+        for (int i = 0; i < kBackTurns; ++i) {
             const bool ok = p + i * steps < p1;
             x[i] = ok ? load_place<T, KEPT, SHORT>(places, p + i * steps, at.n) : no_place<T, KEPT>();
             dy[i] = ok ? load_place<T, false, SHORT>(grads, p + i * steps, at.n) : no_place<T, false>();
         }
 #pragma unroll
-        for (int i = 0; i < kPartTurns; ++i) {
+        for (int i = 0; i < kBackTurns; ++i) {
             if (p + i * steps >= p1) break;
             float h[W], dz[W];
             back_values<T, KEPT>(a, x[i], places, dy[i], grads, mean, rstd, w, b, h, dz);
@@ -1004,7 +1025,8 @@ GroupPlan group_plan(int dtype, uint32_t samples, uint32_t places, uint32_t chan
     p.parts = 1;
     p.part = places;
     if (samples == 0 || places == 0) return p;
-    // groups of a workgroup: those of 64 bytes at least, and of more while there are workgroups enough
+    // groups of a workgroup: those of 128 bytes where that leaves two workgroups for every compute unit, else of 64, and of more while there are enough
+    // (8 x 16 x 1024 x 256 bfloat16, forward and kept / backward: spans of 64 bytes 63 / 62 us, of 128 56 / 58)
     auto pieces_of = [&](uint32_t n) { return ceil_div((uint64_t)n * per, W); };
     auto fits = [&](uint32_t n) {
         const uint32_t pieces = pieces_of(n);
@@ -1015,8 +1037,9 @@ GroupPlan group_plan(int dtype, uint32_t samples, uint32_t places, uint32_t chan
         const uint32_t pieces = pieces_of(n);
         return per % W == 0u && groups % n == 0u && pieces <= 64u && (pieces & (pieces - 1u)) == 0u && per / W <= 8u;
     };
-    uint32_t of = min(groups, max(1u, ceil_div(4u * W, per)));
-    if (!one(of) && one(2u * of) && fits(2u * of) && 2u * of <= groups) of *= 2u;
+    const uint32_t wide = min(groups, ceil_div(8u * W, per));
+    uint32_t of = fits(wide) && (uint64_t)samples * groups >= 2u * n_cu * (uint64_t)wide ? wide : min(groups, ceil_div(4u * W, per));
+    if (!one(of) && 2u * of <= groups && one(2u * of) && fits(2u * of)) of *= 2u;
     while (of < groups && 2u * of <= groups && fits(2u * of) && (one(2u * of) || !one(of)) && (uint64_t)samples * (groups / (2u * of)) >= 4u * n_cu) of *= 2u;
     if (channels >= W && fits(of)) {
         p.whole = true;
@@ -1034,7 +1057,7 @@ GroupPlan group_plan(int dtype, uint32_t samples, uint32_t places, uint32_t chan
         const uint32_t pieces = ceil_div(p.span, W), steps = 256u / pieces;
         // eight workgroups for every compute unit, but four turns for each of them
         const uint32_t want = max(1u, ceil_div(8u * n_cu, (uint64_t)samples * p.spans));
-        p.part = max(ceil_div(places, want), 4u * steps * (uint32_t)kPartTurns);
+        p.part = max(ceil_div(places, want), 4u * steps * (uint32_t)(backward ? kBackTurns : kPartTurns));
         p.parts = ceil_div(places, p.part);
     }
     const bool sums = !p.whole || backward;

@@ -6,7 +6,7 @@
 namespace qgx {
 
 constexpr uint32_t kTurnThreads = 256;
-constexpr uint32_t kTurnAngles = 2048;                     // most sines of a workgroup's tokens
+constexpr uint32_t kTurnAngles = 2048, kTurnTokens = 64;   // most sines, and tokens, of a workgroup
 
 // Sine and cosine of an angle in turns, reduced in binary64 before it becomes binary32.
 __device__ __forceinline__ float2 cos_sin_of(double turns)
@@ -20,64 +20,114 @@ __device__ __forceinline__ float2 cos_sin_of(double turns)
 // The frequencies come with the launch; PAIRS: as many as there is room for (the fewer, the sooner a launch is made).
 template <int PAIRS> struct Frequencies { double turns[PAIRS]; };
 
+// A thread's piece of a head: pairs from the item's first on, or elements that stay as they are.
+template <typename T, bool NEIGHBOURS>
+struct HeadPiece {
+    static constexpr int W = kPiece<T>;
+    uint32_t c;                                            // its first element, in the first half where pairs are apart
+    int left;                                              // elements of it that are there
+    bool turned;
+    float v[W], u[W];
+
+    __device__ __forceinline__ void load(const T* in, uint32_t P)
+    {
+        load_piece(in + c, left, v);
+        if (!NEIGHBOURS && turned) load_piece(in + P + c, left, u);
+    }
+    // cs, sn: of the piece's first pair on, 16-byte aligned (what lies past the last pair may be anything)
+    __device__ __forceinline__ void turn(const float* cs, const float* sn)
+    {
+        if (!turned) return;
+        constexpr int n = NEIGHBOURS ? W / 2 : W;
+        float co[n], si[n];
+        if constexpr (n == 2) {
+            const float2 x = *reinterpret_cast<const float2*>(cs), y = *reinterpret_cast<const float2*>(sn);
+            co[0] = x.x; co[1] = x.y; si[0] = y.x; si[1] = y.y;
+        } else {
+#pragma unroll
+            for (int h = 0; h < n / 4; ++h) {
+                const float4 x = *reinterpret_cast<const float4*>(cs + 4 * h), y = *reinterpret_cast<const float4*>(sn + 4 * h);
+                co[4 * h] = x.x; co[4 * h + 1] = x.y; co[4 * h + 2] = x.z; co[4 * h + 3] = x.w;
+                si[4 * h] = y.x; si[4 * h + 1] = y.y; si[4 * h + 2] = y.z; si[4 * h + 3] = y.w;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < n; ++j) {
+            float& x = NEIGHBOURS ? v[2 * j] : v[j];
+            float& y = NEIGHBOURS ? v[2 * j + 1] : u[j];
+            const float t = fmaf(x, co[j], -(y * si[j]));
+            y = fmaf(x, si[j], y * co[j]);
+            x = t;
+        }
+    }
+    __device__ __forceinline__ void store(T* out, uint32_t P) const
+    {
+        auto put = [&](T* p, const float (&x)[W]) {
+            if (left >= W) stream_piece(p, x);
+            else store_piece(p, left, x);
+        };
+        put(out + c, v);
+        if (!NEIGHBOURS && turned) put(out + P + c, u);
+    }
+};
+
 template <typename T, bool NEIGHBOURS, int PAIRS>
 __global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, Frequencies<PAIRS> f, uint32_t tile_tokens, uint32_t turned, uint32_t items)
 {
     constexpr int W = kPiece<T>;
-    __shared__ float s_cos[kTurnAngles], s_sin[kTurnAngles];
-    const uint32_t P = a.pairs;
+    __shared__ __align__(16) float s_cos[kTurnAngles], s_sin[kTurnAngles];
+    __shared__ uint64_t s_in[kTurnTokens], s_out[kTurnTokens];
+    const uint32_t P = a.pairs, stride = (P + 7u) & ~7u;
     for (uint32_t first = blockIdx.x * tile_tokens; first < a.n_tokens; first += gridDim.x * tile_tokens) {
         const uint32_t count = min(tile_tokens, a.n_tokens - first);
         for (uint32_t i = threadIdx.x; i < count * P; i += kTurnThreads) {
-            const uint32_t token = first + i / P, p = i % P, sequence = token / a.tokens, t = token % a.tokens;
+            const uint32_t local = i / P, token = first + local, p = i % P, sequence = token / a.tokens, t = token % a.tokens;
             uint32_t axis = 0;
 #pragma unroll
             for (uint32_t x = 0; x + 1 < QGX_MAX_AXES; ++x) axis += p >= a.axis_end[x];
-            const int32_t at = a.positions[axis * a.p_axis + sequence / a.batch * a.p_worker + sequence % a.batch * a.p_batch + t];
+            const uint32_t k = sequence / a.batch, n = sequence % a.batch;
+            const int32_t at = a.positions[axis * a.p_axis + k * a.p_worker + n * a.p_batch + t];
             const float2 cs = cos_sin_of((double)at * f.turns[p]);
-            s_cos[i] = cs.x;
-            s_sin[i] = a.back ? -cs.y : cs.y;
+            s_cos[local * stride + p] = cs.x;
+            s_sin[local * stride + p] = a.back ? -cs.y : cs.y;
+            if (p == 0u) {
+                s_in[local] = k * a.i_worker + n * a.i_batch + t * a.i_token;
+                s_out[local] = k * a.o_worker + n * a.o_batch + t * a.o_token;
+            }
         }
         __syncthreads();
-        // an item: a piece of pairs (the first `turned` of a head's), or a piece of what stays as it is
-        for (uint32_t i = threadIdx.x; i < count * a.heads * items; i += kTurnThreads) {
-            const uint32_t row = i / items, item = i % items, local = row / a.heads, head = row % a.heads;
-            const uint32_t token = first + local, sequence = token / a.tokens, t = token % a.tokens, k = sequence / a.batch, n = sequence % a.batch;
-            const T* in = (const T*)a.in + k * a.i_worker + n * a.i_batch + t * a.i_token + head * a.i_head;
-            T* out = (T*)a.out + k * a.o_worker + n * a.o_batch + t * a.o_token + head * a.o_head;
-            if (item >= turned) {
-                const uint32_t c = 2u * P + (item - turned) * W;
-                float v[W];
-                load_piece(in + c, (int)(a.dim - c), v);
-                store_piece(out + c, (int)(a.dim - c), v);
-            } else if constexpr (NEIGHBOURS) {
-                const uint32_t c = item * W, p = local * P + c / 2u;
-                const int left = (int)(2u * P - c);
-                float v[W], w[W];
-                load_piece(in + c, left, v);
+        // The items of a head (pieces of pairs, the first `turned`, then pieces of what stays) to as many threads, heads and tokens in turn, two at
+        // a time: their loads are under way together.
+        const uint32_t heads_at_once = items <= kTurnThreads ? kTurnThreads / items : 1u, rows = count * a.heads;
+        const uint32_t row0 = threadIdx.x / items;
+        for (uint32_t item = threadIdx.x % items; item < items && row0 < heads_at_once; item += items <= kTurnThreads ? items : kTurnThreads) {
+            HeadPiece<T, NEIGHBOURS> x[2];
+            const bool turns = item < turned;
+            const uint32_t c = turns ? item * W : 2u * P + (item - turned) * W, pair = NEIGHBOURS ? c / 2u : c;
+            const int left = turns ? (NEIGHBOURS ? (int)(2u * P - c) : (int)(P - c)) : (int)(a.dim - c);
+            uint32_t local = row0 / a.heads, head = row0 % a.heads;
+            for (uint32_t row = row0; row < rows; row += 2u * heads_at_once) {
+                uint32_t where[2];
+                T* to[2];
 #pragma unroll
-                for (int j = 0; j < W / 2; ++j) {
-                    const uint32_t q = p + (2 * j < left ? j : 0);
-                    const float cs = s_cos[q], sn = s_sin[q];
-                    w[2 * j] = fmaf(v[2 * j], cs, -(v[2 * j + 1] * sn));
-                    w[2 * j + 1] = fmaf(v[2 * j], sn, v[2 * j + 1] * cs);
+                for (int j = 0; j < 2; ++j) {
+                    const bool ok = row + j * heads_at_once < rows;
+                    where[j] = local * stride + pair;
+                    x[j].c = c;
+                    x[j].turned = turns;
+                    x[j].left = ok ? left : 0;
+                    const uint32_t token = min(local, count - 1u);
+                    to[j] = (T*)a.out + s_out[token] + head * a.o_head;
+                    x[j].load((const T*)a.in + s_in[token] + head * a.i_head, P);
+                    if (!ok) where[j] = 0u;
+                    head += heads_at_once;
+                    while (head >= a.heads) { head -= a.heads; ++local; }
                 }
-                store_piece(out + c, left, w);
-            } else {
-                const uint32_t c = item * W, p = local * P + c;
-                const int left = (int)(P - c);
-                float v[W], u[W], w[W], z[W];
-                load_piece(in + c, left, v);
-                load_piece(in + P + c, left, u);
 #pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    const uint32_t q = p + (j < left ? j : 0);
-                    const float cs = s_cos[q], sn = s_sin[q];
-                    w[j] = fmaf(v[j], cs, -(u[j] * sn));
-                    z[j] = fmaf(v[j], sn, u[j] * cs);
+                for (int j = 0; j < 2; ++j) {
+                    x[j].turn(s_cos + where[j], s_sin + where[j]);
+                    x[j].store(to[j], P);
                 }
-                store_piece(out + c, left, w);
-                store_piece(out + P + c, left, z);
             }
         }
         __syncthreads();
@@ -90,8 +140,10 @@ static hipError_t launch_rotary_as(const RotaryArgs& a, const double* turns, uin
     constexpr uint32_t W = kPiece<T>;
     const uint32_t turned = a.neighbours ? (2u * a.pairs + W - 1u) / W : (a.pairs + W - 1u) / W;
     const uint32_t rest = a.dim - 2u * a.pairs, items = turned + (a.in == a.out ? 0u : (rest + W - 1u) / W);
-    const uint32_t most = max(1u, min(kTurnAngles / a.pairs, (1u << 30) / (a.heads * items)));
-    const uint32_t tile = min(most, max(1u, a.n_tokens / (8u * n_cu)));
+    const uint32_t most = min(kTurnTokens, kTurnAngles / ((a.pairs + 7u) & ~7u));
+    // (more workgroups than find room at once, so that the last ones are short: 4 x 16384 tokens of 16 x 128 bfloat16 117 us with 8 to a compute
+    // unit, 107 with 16, 94 with 32, 95 with 64)
+    const uint32_t tile = min(most, max(1u, a.n_tokens / (32u * n_cu)));
     const dim3 grid(min((a.n_tokens + tile - 1u) / tile, 1u << 20));
     Frequencies<PAIRS> f;
     for (uint32_t p = 0; p < (uint32_t)PAIRS; ++p) f.turns[p] = p < a.pairs ? turns[p] : 0.0;
