@@ -263,7 +263,7 @@ __global__ __launch_bounds__(THREADS) void k_group_norm(GroupArgs a, uint32_t ba
     constexpr int W = kPiece<T>;
     __shared__ __align__(16) float s_sums[THREADS * W];
     __shared__ float s_mean[1][kGroupsMost], s_rstd[1][kGroupsMost];
-    const uint32_t unit = unit_of_block(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
+    const uint32_t unit = unit_of_block(blockIdx.x, a.units), sample = unit / a.spans, first = unit % a.spans * a.span;
     const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = THREADS / pieces;
     const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
     const bool any = step < steps;
@@ -367,11 +367,64 @@ __device__ __forceinline__ void statistics_of(const GroupArgs& a, uint32_t sampl
 // Where a workgroup's channels' sums go: in scratch [samples][parts][2][channels], or, where it has all of a worker's places, where they belong.
 __device__ __forceinline__ float* channel_sums_at(const GroupArgs& a, uint32_t sample, uint32_t batch, uint32_t part, int which)
 {
+    if (a.apart) return nullptr;
     if (batch * a.parts == 1u) {
         float* to = which ? a.db : a.dw;
         return to ? to + sample * a.param_stride : nullptr;
     }
     return (which ? a.db : a.dw) ? a.scratch + (((size_t)sample * a.parts + part) * 2u + which) * a.channels : nullptr;
+}
+
+// Small tensors: the parameters' gradients of four pieces' channels by a workgroup of their own, from dy and x once more (from the cache): no scratch and
+// no second launch, which would take longer.  A worker's samples and places are dealt to THREADS / 4 threads for each piece.  s: [2][THREADS][W].
+template <typename T, int THREADS, bool KEPT>
+__device__ __forceinline__ void parameters_apart(const GroupArgs& a, uint32_t batch, uint32_t block, float* s)
+{
+    constexpr int W = kPiece<T>;
+    constexpr uint32_t kRuns = THREADS / 4;
+    const uint32_t columns = (a.channels + 4u * W - 1u) / (4u * W), k = block / columns, first = block % columns * 4u * W;
+    const uint32_t piece = threadIdx.x % 4u, run = threadIdx.x / 4u, span = min(4u * W, a.channels - first), pieces = (span + W - 1u) / W;
+    const ChannelsAt at = channels_at<W, false>(min(piece, pieces - 1u), first, span);
+    float w[W], b[W], sum[2][W];
+    channel_parameters<W>(a.w, at, 1.0f, w);
+    channel_parameters<W>(a.b, at, 0.0f, b);
+#pragma unroll
+    for (int c = 0; c < W; ++c) sum[0][c] = sum[1][c] = 0.0f;
+    const uint32_t rows = batch * a.places;
+#pragma unroll 4
+    for (uint32_t r = run; r < rows; r += kRuns) {
+        const uint32_t sample = k * batch + r / a.places, p = r % a.places;
+        const Places<T, KEPT> places = places_of<T, KEPT>(a, sample, batch, at);
+        const Places<T, false> grads = gradients_of<T>(a, sample, batch, at);
+        const RawPiece<T, KEPT> x = load_place<T, KEPT, false>(places, p, W);
+        const RawPiece<T, false> dy = load_place<T, false, false>(grads, p, W);
+        float mean[W], rstd[W], h[W], dz[W];
+        statistics_of<W>(a, sample, at, mean, rstd);
+        back_values<T, KEPT>(a, x, places, dy, grads, mean, rstd, w, b, h, dz);
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+            sum[0][c] = fmaf(dz[c], h[c], sum[0][c]);
+            sum[1][c] += dz[c];
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int c = 0; c < W; ++c) s[(m * THREADS + threadIdx.x) * W + c] = sum[m][c];
+    __syncthreads();
+    // eight threads to a sum: a run of the threads' each, then those in a tree
+    const uint32_t which = threadIdx.x / (THREADS / 2), each = threadIdx.x % (THREADS / 2), share = each % 8u;
+    float* to = which ? a.db : a.dw;
+    for (uint32_t c = each / 8u; c < 4u * W; c += THREADS / 16) {
+        const uint32_t j = c / W, lane = c % W;
+        float t = 0.0f;
+        for (uint32_t i = share; i < kRuns; i += 8u) t += s[(which * THREADS + i * 4u + j) * W + lane];
+        t = __uint_as_float(xor_lane<1>(__float_as_uint(t))) + t;
+        t = __uint_as_float(xor_lane<2>(__float_as_uint(t))) + t;
+        t += __shfl_xor(t, 4, 64);
+        const int channel = min((int)(j * W), (int)span - W) + (int)lane;              // of the span, where the piece lies
+        if (to && share == 0u && j < pieces && (int)lane >= (int)(j * W) - min((int)(j * W), (int)span - W)) to[k * a.param_stride + first + channel] = t;
+    }
 }
 
 template <typename T, int THREADS, int N, bool KEPT, bool SHORT>
@@ -380,7 +433,9 @@ __global__ __launch_bounds__(THREADS) void k_group_norm_back(GroupArgs a, uint32
     constexpr int W = kPiece<T>;
     __shared__ __align__(16) float s_sums[2 * THREADS * W];
     __shared__ float s_group[2][kGroupsMost];
-    const uint32_t unit = unit_of_block(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
+    if constexpr (THREADS == 256)
+        if (a.apart && blockIdx.x >= a.units) return parameters_apart<T, THREADS, KEPT>(a, batch, blockIdx.x - a.units, s_sums);
+    const uint32_t unit = unit_of_block(blockIdx.x, a.units), sample = unit / a.spans, first = unit % a.spans * a.span;
     const uint32_t span = min(a.span, a.channels - first), pieces = SHORT ? 1u : (span + W - 1u) / W, steps = THREADS / pieces;
     const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
     const bool any = step < steps;
@@ -531,7 +586,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_group_norm_one(GroupArgs a, uint
 {
     constexpr int W = kPiece<T>;
     __shared__ __align__(16) float s_sum[2][kWave * THREADS / kWave];
-    const uint32_t unit = unit_of_block(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
+    const uint32_t unit = unit_of_block(blockIdx.x, a.units), sample = unit / a.spans, first = unit % a.spans * a.span;
     const uint32_t pieces = a.span / W, group_pieces = a.per / W, steps = THREADS / pieces;
     const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
     const ChannelsAt at{(int)(first + j * W), 0, W};
@@ -624,7 +679,9 @@ __global__ __launch_bounds__(THREADS, 4) void k_group_norm_back_one(GroupArgs a,
     constexpr int W = kPiece<T>, kWaves = THREADS / kWave;
     __shared__ __align__(16) float s_sum[2 * kWave * kWaves];
     __shared__ float s_channel[2][kWaves][kWave * W];
-    const uint32_t unit = unit_of_block(blockIdx.x, gridDim.x), sample = unit / a.spans, first = unit % a.spans * a.span;
+    if constexpr (THREADS == 256)
+        if (a.apart && blockIdx.x >= a.units) return parameters_apart<T, THREADS, KEPT>(a, batch, blockIdx.x - a.units, &s_channel[0][0][0]);
+    const uint32_t unit = unit_of_block(blockIdx.x, a.units), sample = unit / a.spans, first = unit % a.spans * a.span;
     const uint32_t pieces = a.span / W, group_pieces = a.per / W, steps = THREADS / pieces;
     const uint32_t j = threadIdx.x % pieces, step = threadIdx.x / pieces;
     const ChannelsAt at{(int)(first + j * W), 0, W};
@@ -671,7 +728,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_group_norm_back_one(GroupArgs a,
         sum[0] = fmaf(dw[c], w[c], sum[0]);
         sum[1] = fmaf(db[c], w[c], sum[1]);
     }
-    if (a.dw || a.db) {
+    if ((a.dw || a.db) && !a.apart) {
         piece_sums(dw, pieces);
         piece_sums(db, pieces);
         if (lane_id() < (int)pieces)
@@ -1018,7 +1075,7 @@ static uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1u
 
 // Whole groups where a span of at least 64 bytes (or of all channels) has its places in a workgroup's registers: 1024 threads with up to 16 pieces of
 // 16 bytes forward, 8 backward (of each of two streams).
-GroupPlan group_plan(int dtype, uint32_t samples, uint32_t places, uint32_t channels, uint32_t groups, bool backward, uint32_t n_cu)
+GroupPlan group_plan(int dtype, uint32_t workers, uint32_t samples, uint32_t places, uint32_t channels, uint32_t groups, bool backward, uint32_t n_cu)
 {
     const uint32_t W = dtype == QGX_F32 ? 4u : 8u, per = channels / groups, most = backward ? 8u : 16u;
     GroupPlan p{};
@@ -1060,7 +1117,10 @@ GroupPlan group_plan(int dtype, uint32_t samples, uint32_t places, uint32_t chan
         p.part = max(ceil_div(places, want), 4u * steps * (uint32_t)(backward ? kBackTurns : kPartTurns));
         p.parts = ceil_div(places, p.part);
     }
-    const bool sums = !p.whole || backward;
+    // Little in all: the parameters' gradients apart.  (4 x 3 x 221 x 90 binary32: kernels 9.6 and 3.9 us and a call of 19 with the sums joined by a launch)
+    p.apart = p.whole && backward && samples > workers && p.threads == 256u && (uint64_t)samples * places * channels <= (1u << 20) &&
+              (uint64_t)(samples / workers) * places <= 4096u;
+    const bool sums = !p.whole || (backward && samples > workers && !p.apart);
     p.at_sums = sums ? ((uint64_t)samples * p.parts * 2u * channels + 3u) / 4u * 4u : 0u;
     const uint64_t floats = p.at_sums + (p.whole ? 0u : 2u * (uint64_t)samples * groups);
     p.scratch = floats * sizeof(float);
@@ -1070,6 +1130,8 @@ GroupPlan group_plan(int dtype, uint32_t samples, uint32_t places, uint32_t chan
 static void deal(GroupArgs& a, const GroupPlan& p)
 {
     a.span = p.span; a.spans = p.spans; a.parts = p.parts; a.part = p.part;
+    a.units = a.samples * p.spans;
+    a.apart = p.apart && (a.dw || a.db);
     a.sums = a.scratch ? a.scratch + p.at_sums : nullptr;
 }
 
@@ -1129,7 +1191,8 @@ hipError_t launch_group_norm(int dtype, const GroupArgs& args, uint32_t workers,
 template <typename T, int THREADS, int N, bool KEPT>
 static hipError_t launch_back_whole_as(const GroupArgs& a, uint32_t batch, const GroupPlan& p, hipStream_t st)
 {
-    const dim3 grid(a.samples * a.spans), block(THREADS);
+    const uint32_t apart = a.apart ? a.samples / batch * ((a.channels + 4u * kPiece<T> - 1u) / (4u * kPiece<T>)) : 0u;
+    const dim3 grid(a.units + apart), block(THREADS);
     if (p.one) hipLaunchKernelGGL((k_group_norm_back_one<T, THREADS, N, KEPT>), grid, block, 0, st, a, batch);
     else hipLaunchKernelGGL((k_group_norm_back<T, THREADS, N, KEPT, false>), grid, block, 0, st, a, batch);
     return hipGetLastError();
@@ -1169,6 +1232,7 @@ hipError_t launch_group_norm_back(int dtype, const GroupArgs& args, uint32_t wor
     GroupArgs a = args;
     if (!a.y && !a.dw && !a.db) return hipSuccess;
     deal(a, plan);
+    if (a.apart && !a.y) a.units = 0u;                     // no groups' workgroups
     const uint32_t batch = a.samples / workers;
     if (batch && a.places) {
         const hipError_t e = dtype == QGX_F32   ? launch_back_of<float>(a, batch, plan, st)
@@ -1176,7 +1240,7 @@ hipError_t launch_group_norm_back(int dtype, const GroupArgs& args, uint32_t wor
                                                 : launch_back_of<__bf16>(a, batch, plan, st);
         if (e != hipSuccess) return e;
     }
-    if ((!a.dw && !a.db) || (plan.whole && batch == 1u)) return hipSuccess;
+    if ((!a.dw && !a.db) || (plan.whole && (batch == 1u || plan.apart))) return hipSuccess;
     // (no samples or places: sums of nothing)
     hipLaunchKernelGGL(k_group_parameters, dim3((a.channels + kWave - 1u) / kWave, workers, 2u), dim3(256), 0, st, a, a.places ? batch : 0u);
     return hipGetLastError();

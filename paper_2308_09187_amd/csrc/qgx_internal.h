@@ -395,18 +395,20 @@ struct GroupArgs {
     // how it is dealt out, filled in by the launch
     uint32_t span, spans;       // whole groups' channels of a workgroup, workgroups across a sample's
     uint32_t parts, part;       // workgroups along a sample's places, places of each
+    uint32_t units, apart;      // workgroups with whole groups; the parameters' gradients have workgroups of their own after them
     float* scratch;             // see GroupPlan
     float* sums;
 };
 struct GroupPlan {
     bool whole;                 // a workgroup has all of its groups' places in its registers
     bool one;                   // and a thread's piece lies in one of them
+    bool apart;                 // the parameters' gradients have workgroups of their own
     uint32_t threads, pieces;   // of that kernel
     uint32_t span, spans, parts, part;
     uint64_t at_sums;           // floats before the groups' sums, after the channels' [samples][parts][2][channels]
     uint64_t scratch;           // bytes
 };
-GroupPlan group_plan(int dtype, uint32_t samples, uint32_t places, uint32_t channels, uint32_t groups, bool backward, uint32_t n_cu);
+GroupPlan group_plan(int dtype, uint32_t workers, uint32_t samples, uint32_t places, uint32_t channels, uint32_t groups, bool backward, uint32_t n_cu);
 bool group_keeps(const GroupPlan& plan, uint32_t channels);     // whether the kernel of this plan keeps x as well
 hipError_t launch_group_norm(int dtype, const GroupArgs& a, uint32_t workers, const GroupPlan& plan, Scalars* sc, hipStream_t st);
 hipError_t launch_group_norm_back(int dtype, const GroupArgs& a, uint32_t workers, const GroupPlan& plan, hipStream_t st);

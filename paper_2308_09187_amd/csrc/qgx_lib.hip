@@ -1382,7 +1382,7 @@ static qgx_status check_group(qgx_ctx* ctx, const char* what, const qgx_group_sh
 
 static GroupPlan plan_of(const qgx_ctx* ctx, const qgx_group_shape* g, bool backward)
 {
-    return group_plan(g->dtype, (uint32_t)(g->workers * g->batch), (uint32_t)g->places, (uint32_t)g->channels, g->groups, backward, ctx->n_simd / 4u);
+    return group_plan(g->dtype, (uint32_t)g->workers, (uint32_t)(g->workers * g->batch), (uint32_t)g->places, (uint32_t)g->channels, g->groups, backward, ctx->n_simd / 4u);
 }
 
 static bool no_places(const qgx_group_shape* g) { return g->workers == 0 || g->batch == 0 || g->places == 0; }

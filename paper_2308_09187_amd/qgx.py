@@ -707,34 +707,73 @@ class Context:
             self._check(st)
         return dw
 
+    # (Checks of the calls below are written out, several to a condition: a call of a function for each costs as much as the launch.)
     @staticmethod
     def _places(t, name):
         """Address and steps of [workers, batch, places, channels], [batch, places, channels] or [places, channels]."""
         step = t.stride()
         n = len(step)
-        _need(2 <= n <= 4 and (step[-1] == 1 or t.shape[-1] <= 1), "%s: [workers, batch, places, channels], channels contiguous", name)
-        return _Places(t.data_ptr(), step[0] if n == 4 else 0, step[-3] if n > 2 else 0, step[-2])
+        if not (2 <= n <= 4 and (step[-1] == 1 or t.shape[-1] <= 1)):
+            raise QgxError(ERR_ARG, "%s: [workers, batch, places, channels], channels contiguous" % name)
+        if n == 4:
+            return _Places(t.data_ptr(), step[0], step[1], step[2])
+        return _Places(t.data_ptr(), 0, step[0] if n == 3 else 0, step[-2])
 
     @classmethod
     def _places_like(cls, t, like, name):
         """The same of a tensor of like's shape and type."""
-        _need(t.shape == like.shape and t.dtype == like.dtype and t.get_device() == like.get_device(), "%s: of x's shape and type, on its device", name)
+        if not (t.shape == like.shape and t.dtype == like.dtype and t.get_device() == like.get_device()):
+            raise QgxError(ERR_ARG, "%s: of x's shape and type, on its device" % name)
         return cls._places(t, name)
+
+    @staticmethod
+    def _places_new(t, shape):
+        """The same of a new tensor."""
+        run = shape.places * shape.channels
+        return _Places(t.data_ptr(), shape.batch * run, run, shape.channels)
 
     @staticmethod
     def _group_shape(t, groups, activation, slope, name):
         code, sh, act = DTYPES.get(t.dtype), t.shape, ACTIVATIONS.get(activation)
         n = len(sh)
-        _need(code is not None and t.is_cuda and 2 <= n <= 4, "%s: [workers, batch, places, channels] of float32, float16 or bfloat16 on the GPU", name)
-        _need(act is not None, "activation: none, silu or leaky")
-        _need(0 < groups < 1 << 32 and sh[-1] % groups == 0, "groups: a divisor of the channels")
-        return _GroupShape(code, act, slope, groups, sh[0] if n == 4 else 1, sh[-3] if n > 2 else 1, sh[-2], sh[-1])
+        if not (code is not None and t.is_cuda and 2 <= n <= 4):
+            raise QgxError(ERR_ARG, "%s: [workers, batch, places, channels] of float32, float16 or bfloat16 on the GPU" % name)
+        if act is None or not 0 < groups < 1 << 32 or sh[-1] % groups:
+            raise QgxError(ERR_ARG, "activation: none, silu or leaky; groups: a divisor of the channels")
+        if n == 4:
+            return _GroupShape(code, act, slope, groups, sh[0], sh[1], sh[2], sh[3])
+        return _GroupShape(code, act, slope, groups, 1, sh[0] if n == 3 else 1, sh[-2], sh[-1])
+
+    @staticmethod
+    def _channel_parameter(t, channels, name):
+        """Address of a contiguous binary32 parameter of the channels, or of a run of one; None stays None."""
+        if t is None:
+            return None
+        if not (t.is_cuda and t.dtype == torch.float32 and t.dim() == 1 and t.shape[0] == channels and (t.stride(0) == 1 or channels == 1)):
+            raise QgxError(ERR_ARG, "%s: contiguous float32 of %d channels on the GPU" % (name, channels))
+        return t.data_ptr()
+
+    @staticmethod
+    def _group_statistic(t, shape, n, name):
+        """Address of a contiguous binary32 [workers, batch, groups], without the dimensions that dy has not."""
+        ok = t is not None and t.is_cuda and t.dtype == torch.float32 and t.dim() == n - 1 and t.is_contiguous()
+        if ok:
+            sh = t.shape
+            ok = sh[-1] == shape.groups and (n < 3 or sh[-2] == shape.batch) and (n < 4 or sh[0] == shape.workers)
+        if not ok:
+            raise QgxError(ERR_ARG, "%s: contiguous float32 [.., groups] on the GPU" % name)
+        return t.data_ptr()
 
     def _group_scratch(self, shape, backward, like, stream):
+        """(tensor or None, address, bytes)"""
         st = self.lib.qgx_group_norm_scratch(self._h, C.addressof(shape), backward, self._need_ref)
         if st:
             self._check(st)
-        return _empty(like, (self._need_bytes.value,), torch.uint8, stream) if self._need_bytes.value else None
+        n = self._need_bytes.value
+        if not n:
+            return None, None, 0
+        t = _empty(like, (n,), torch.uint8, stream)
+        return t, t.data_ptr(), n
 
     def group_norm(self, x, groups, weight=None, bias=None, eps=1e-5, activation="none", slope=0.01, keep=None, call_id=None, out=None, save=True,
                    stream=None):
@@ -742,23 +781,27 @@ class Context:
         "leaky" (slope).  Returns (y, mean, rstd), the last two [.., groups] for the backward pass (save=False: None).  keep: a
         Checkpoint in which x is kept as well, as checkpoint(x, call_id) would."""
         shape = self._group_shape(x, groups, activation, slope, "x")
-        channels = x.shape[-1]
+        channels = shape.channels
         src = self._places(x, "x")
-        w, b = _parameter(weight, (channels,), "weight"), _parameter(bias, (channels,), "bias")
+        w, b = self._channel_parameter(weight, channels, "weight"), self._channel_parameter(bias, channels, "bias")
         if out is None:
             out = _empty_like(x, stream)
-            dst = _Places(out.data_ptr(), shape.batch * shape.places * channels, shape.places * channels, channels)
+            dst = self._places_new(out, shape)
         else:
             dst = self._places_like(out, x, "out")
-        _need(keep is None or (keep.shape == x.shape and keep.codes.get_device() == x.get_device()), "keep: a checkpoint of x's shape, on its device")
-        _need(call_id is None or 0 <= call_id < 1 << 32, "call_id: 32 bits")
-        mean = rstd = None
+        kept, unbiased = None, 0
+        if keep is not None:
+            unbiased = call_id is not None
+            if keep.shape != x.shape or keep.codes.get_device() != x.get_device() or (unbiased and not 0 <= call_id < 1 << 32):
+                raise QgxError(ERR_ARG, "keep: a checkpoint of x's shape, on its device; call_id: 32 bits")
+            kept = keep._ref
+        mean = rstd = m = r = None
         if save:
             mean, rstd = _empty(x, (2,) + x.shape[:-2] + (groups,), torch.float32, stream).unbind(0)
-        scratch = self._group_scratch(shape, 0, x, stream)
-        st = self.lib.qgx_group_norm(self._h, C.addressof(shape), C.addressof(src), w, b, eps, C.addressof(dst), mean.data_ptr() if save else None,
-                                     rstd.data_ptr() if save else None, None if keep is None else keep._ref, call_id is not None, call_id or 0,
-                                     None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel(), _handle(stream, x))
+            m, r = mean.data_ptr(), rstd.data_ptr()
+        scratch, at, size = self._group_scratch(shape, 0, x, stream)
+        st = self.lib.qgx_group_norm(self._h, C.addressof(shape), C.addressof(src), w, b, eps, C.addressof(dst), m, r, kept, unbiased, call_id or 0, at, size,
+                                     _handle(stream, x))
         if st:
             self._check(st)
         return out, mean, rstd
@@ -768,36 +811,40 @@ class Context:
         """Returns dx (None with need_dx=False) and writes the workers' weight and bias gradients to dw and db, float32 [workers, channels], runs
         of V's rows say ([channels] where dy has no worker dimension).  x: the forward pass's input, or a Checkpoint of it."""
         shape = self._group_shape(dy, groups, activation, slope, "dy")
-        channels, wk = dy.shape[-1], shape.workers
-        grad = self._places(dy, "dy")
-        src = None
+        channels, wk, n = shape.channels, shape.workers, dy.dim()
+        grad, dev = self._places(dy, "dy"), dy.get_device()
+        src = kept = None
         if isinstance(x, Checkpoint):
-            _need(x.shape == dy.shape and x.codes.get_device() == dy.get_device(), "x: a checkpoint of dy's shape, on its device")
+            if x.shape != dy.shape or x.codes.get_device() != dev:
+                raise QgxError(ERR_ARG, "x: a checkpoint of dy's shape, on its device")
+            kept = x._ref
         else:
             src = self._places_like(x, dy, "x")
-        w, b = _parameter(weight, (channels,), "weight"), _parameter(bias, (channels,), "bias")
-        lead = dy.shape[:-2] + (groups,)
-        m, r = _parameter(mean, lead, "mean"), _parameter(rstd, lead, "rstd")
-        step = None
-        for t, name in ((dw, "dw"), (db, "db")):
+        w, b = self._channel_parameter(weight, channels, "weight"), self._channel_parameter(bias, channels, "bias")
+        m, r = self._group_statistic(mean, shape, n, "mean"), self._group_statistic(rstd, shape, n, "rstd")
+        step, to = None, [None, None]
+        for i, t in enumerate((dw, db)):
             if t is None:
                 continue
-            _need(t.get_device() == dy.get_device() and t.dtype == torch.float32 and t.shape == (dy.shape[:1] if dy.dim() == 4 else ()) + (channels,) and _dense_last(t),
-                  "%s: float32 [workers, channels] on dy's device", name)
-            s = t.stride(0) if wk > 1 else channels
-            _need(step is None or step == s, "dw and db: one step between workers")
-            step = s
+            sh = t.shape
+            if not (t.dtype == torch.float32 and t.get_device() == dev and len(sh) == (2 if n == 4 else 1) and sh[-1] == channels and (n < 4 or sh[0] == wk) and
+                    (channels <= 1 or t.stride(-1) == 1)):
+                raise QgxError(ERR_ARG, "dw and db: float32 [workers, channels] on dy's device")
+            one = t.stride(0) if wk > 1 else channels
+            if step is not None and step != one:
+                raise QgxError(ERR_ARG, "dw and db: one step between workers")
+            step = one
+            to[i] = t.data_ptr()
         dst = None
         if dx is not None:
             dst = self._places_like(dx, dy, "dx")
         elif need_dx:
             dx = _empty_like(dy, stream)
-            dst = _Places(dx.data_ptr(), shape.batch * shape.places * channels, shape.places * channels, channels)
-        scratch = self._group_scratch(shape, 1, dy, stream)
-        st = self.lib.qgx_group_norm_backward(
-            self._h, C.addressof(shape), C.addressof(grad), None if src is None else C.addressof(src), x._ref if src is None else None, w, b, m, r,
-            None if dst is None else C.addressof(dst), None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
-            channels if step is None else step, None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel(), _handle(stream, dy))
+            dst = self._places_new(dx, shape)
+        scratch, at, size = self._group_scratch(shape, 1, dy, stream)
+        st = self.lib.qgx_group_norm_backward(self._h, C.addressof(shape), C.addressof(grad), None if src is None else C.addressof(src), kept, w, b, m, r,
+                                              None if dst is None else C.addressof(dst), to[0], to[1], channels if step is None else step, at, size,
+                                              _handle(stream, dy))
         if st:
             self._check(st)
         return dx
@@ -806,10 +853,9 @@ class Context:
     def _heads(t, name):
         """[workers, batch, tokens, heads, dim], [batch, tokens, heads, dim] or [tokens, heads, dim], a head's elements contiguous."""
         code, sh, st = DTYPES.get(t.dtype), t.shape, t.stride()
-        _need(code is not None and t.is_cuda, "%s: float32, float16 or bfloat16 on the GPU", name)
         n = len(sh)
-        _need(3 <= n <= 5 and (st[-1] == 1 or sh[-1] <= 1), "%s: [workers, batch, tokens, heads, dim], the last dimension contiguous", name)
-        _need(sh[-2] < 1 << 32 and sh[-1] < 1 << 32, "%s: too many heads or elements", name)
+        if not (code is not None and t.is_cuda and 3 <= n <= 5 and (st[-1] == 1 or sh[-1] <= 1) and sh[-2] < 1 << 32 and sh[-1] < 1 << 32):
+            raise QgxError(ERR_ARG, "%s: [workers, batch, tokens, heads, dim] of float32, float16 or bfloat16 on the GPU, the last dimension contiguous" % name)
         return _Heads(t.data_ptr(), code, sh[-2], sh[-1], sh[0] if n == 5 else 1, sh[-4] if n > 3 else 1, sh[-3], st[0] if n == 5 else 0,
                       st[-4] if n > 3 else 0, st[-3], st[-2])
 
@@ -825,11 +871,12 @@ class Context:
         elif out is not x:
             _need(out.shape == x.shape and out.dtype == x.dtype and out.get_device() == x.get_device(), "out: of x's shape and type, on its device")
             dst = self._heads(out, "out")
-        ps, pst, axes = positions.shape, positions.stride(), len(rotary.pairs)
-        _need(positions.get_device() == x.get_device() and positions.dtype == torch.int32 and (ps == (axes, x.shape[-3]) or ps == (axes,) + x.shape[:-2]) and
-              (ps[-1] <= 1 or pst[-1] == 1), "positions: int32 [axes, tokens] or [axes, .., tokens], tokens contiguous, on x's device")
-        whole = len(ps) > 2
-        st = self.lib.qgx_rotate(self._h, rotary._ref, positions.data_ptr(), pst[0], pst[1] if len(ps) == 4 else 0, pst[-2] if whole else 0,
+        ps, pst, sh = positions.shape, positions.stride(), x.shape
+        n = len(ps)
+        if not (positions.dtype == torch.int32 and positions.get_device() == x.get_device() and n >= 2 and ps[0] == len(rotary.pairs) and ps[-1] == sh[-3] and
+                (n == 2 or ps[1:] == sh[:-2]) and (ps[-1] <= 1 or pst[-1] == 1)):
+            raise QgxError(ERR_ARG, "positions: int32 [axes, tokens] or [axes, .., tokens], tokens contiguous, on x's device")
+        st = self.lib.qgx_rotate(self._h, rotary._ref, positions.data_ptr(), pst[0], pst[1] if n == 4 else 0, pst[-2] if n > 2 else 0,
                                  C.addressof(src), C.addressof(dst), back, _handle(stream, x))
         if st:
             self._check(st)
