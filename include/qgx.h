@@ -503,14 +503,15 @@ qgx_status qgx_weight_gradient(qgx_ctx* ctx, const qgx_kept* x, int dtype, uint6
 /* Group norm with an activation, channels last: x [workers][batch][places][channels] (a place's channels are contiguous), in `groups` runs of
  * channels / groups channels; a group of a sample is all places' channels of a run.
  *   h = (x - mean) * rstd,  z = h * weight[c] + bias[c],  y = act(z),   rstd = 1 / sqrt(variance + eps)
- * mean and variance of the group's elements, the variance about the mean (not E x^2 - mean^2). */
+ * mean and variance of the group's elements, the variance about the mean (not E x^2 - mean^2); the sums of a group's elements and of their squared
+ * distances from the mean have to lie within binary32. */
 typedef enum { QGX_ACT_NONE = 0, QGX_ACT_SILU = 1, QGX_ACT_LEAKY = 2 } qgx_activation;   /* z; z / (1 + e^-z); z, slope * z where z <= 0 */
 typedef struct {
     int32_t dtype;         /* qgx_dtype of x, y, dy and dx */
     int32_t activation;    /* qgx_activation */
     float slope;           /* of QGX_ACT_LEAKY: finite */
     uint32_t groups;       /* divides channels */
-    uint64_t workers, batch, places, channels;   /* workers * batch <= 65535, workers * batch * places < 2^31, channels 1 .. 2^20, places * channels < 2^36 */
+    uint64_t workers, batch, places, channels;   /* workers * batch <= 65535, workers * batch * places < 2^31, channels 1 .. 2^20, places * channels < 2^36; of few places workers * batch * channels < 2^26 */
 } qgx_group_shape;
 typedef struct {
     void* data;            /* DEVICE */
@@ -526,8 +527,9 @@ qgx_status qgx_group_norm_scratch(qgx_ctx* ctx, const qgx_group_shape* shape, in
 qgx_status qgx_group_norm(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_places* x, const float* weight, const float* bias, float eps,
                           const qgx_places* y, float* mean, float* rstd, const qgx_kept* keep, int unbiased, uint32_t call_id,
                           void* scratch, uint64_t scratch_bytes, void* stream);
-/* Its backward pass, from x or, x NULL, from what was kept of it.  dz = dy act'(z), z in binary32 by one subtraction, two products and one
- * addition as above, each rounded (so that a leaky unit's side is reproducible);  g = dz * weight,
+/* Its backward pass, from x or, x NULL, from what was kept of it.  dz = dy act'(z),  g = dz * weight.  Of a leaky unit z is made in
+ * binary32 by one subtraction, two products and one addition as above, each rounded, so that its side of 0 is reproducible (else a kept
+ * element's h may be off by 2^-22 of (255 * its step + |mean|) * rstd);
  *   dx = rstd * (g - mean over the group of g - h * mean over the group of g h)          DEVICE, or NULL; may not be dy or x
  *   dweight_k[c] = sum over worker k's batch and places of dz h,  dbias_k[c] = sum of dz     DEVICE binary32, each or NULL, worker k's at
  *                  + k * param_stride (runs of V's rows), written, not added to; zeros where batch or places is 0

@@ -647,17 +647,17 @@ __global__ __launch_bounds__(THREADS, 4) void k_group_norm_one(GroupArgs a, uint
 }
 
 // h and dz of a piece of one group.  A kept element over its group's spread is one product and one sum of its code, with A = scale rstd and B = (-128 scale - mean)
-// rstd (off by 2^-23 of A's 255 steps); where the side of 0 decides, by the operations the header names.
+// rstd (off by 2^-23 of A's 255 steps); `plain`, where the side of 0 decides or B is beyond binary32: by the operations the header names.
 template <typename T, bool KEPT>
 __device__ __forceinline__ void back_values_one(const GroupArgs& a, const RawPiece<T, KEPT>& x, const Places<T, KEPT>& places, const RawPiece<T, false>& dy,
-                                                const Places<T, false>& grads, float mean, float rstd, const float (&w)[kPiece<T>], const float (&b)[kPiece<T>],
-                                                float (&h)[kPiece<T>], float (&dz)[kPiece<T>])
+                                                const Places<T, false>& grads, float mean, float rstd, bool plain, const float (&w)[kPiece<T>],
+                                                const float (&b)[kPiece<T>], float (&h)[kPiece<T>], float (&dz)[kPiece<T>])
 {
     values_at(dy, grads, dz);
     if constexpr (KEPT) {
         // (one block to a piece: pieces start at multiples of W)
         const float scale = kept_scale(x.powers & 0xFFu);
-        if (a.activation != QGX_ACT_LEAKY) {
+        if (!plain) {
             const float A = scale * rstd, B = fmaf(-128.0f, scale, -mean) * rstd;
 #pragma unroll
             for (int c = 0; c < kPiece<T>; ++c) h[c] = fmaf((float)((x.code[c / 4] >> (8 * (c & 3))) & 0xFFu), A, B);
@@ -695,16 +695,15 @@ __global__ __launch_bounds__(THREADS, 4) void k_group_norm_back_one(GroupArgs a,
         x[i] = load_place<T, KEPT, false>(places, p, W);
         dy[i] = load_place<T, false, false>(grads, p, W);
     }
-    if (a.places != steps * N)                             // (past the last place: zeros, of which nothing is added)
+    // past the last place: the last one's x (another's h might be no number, and so dz) and a dy of zeros, so that nothing is added
+    if (a.places != steps * N)
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            if (i * steps + step >= a.places) {
-                x[i] = no_place<T, KEPT>();
-                dy[i] = no_place<T, false>();
-            }
+            if (i * steps + step >= a.places) dy[i] = no_place<T, false>();
     const size_t g = (size_t)sample * a.groups + (first + j * W) / a.per;
     float w[W], b[W], dw[W], db[W];
     const float one_mean = a.mean_in[g], one_rstd = a.rstd_in[g];
+    const bool plain = a.activation == QGX_ACT_LEAKY || __builtin_amdgcn_ballot_w64(!(fabsf(one_mean) * one_rstd < 1e30f)) != 0ull;   // (nearly constant, far from 0)
     channel_parameters<W>(a.w, at, 1.0f, w);
     channel_parameters<W>(a.b, at, 0.0f, b);
 #pragma unroll
@@ -714,7 +713,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_group_norm_back_one(GroupArgs a,
         float h[W], dz[W];
         forget(x[i]);
         forget(dy[i]);
-        back_values_one<T, KEPT>(a, x[i], places, dy[i], grads, one_mean, one_rstd, w, b, h, dz);
+        back_values_one<T, KEPT>(a, x[i], places, dy[i], grads, one_mean, one_rstd, plain, w, b, h, dz);
 #pragma unroll
         for (int c = 0; c < W; ++c) {
             dw[c] = fmaf(dz[c], h[c], dw[c]);
@@ -759,7 +758,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_group_norm_back_one(GroupArgs a,
         float h[W], dz[W];
         forget(x[i]);
         forget(dy[i]);
-        back_values_one<T, KEPT>(a, x[i], places, dy[i], grads, one_mean, one_rstd, w, b, h, dz);
+        back_values_one<T, KEPT>(a, x[i], places, dy[i], grads, one_mean, one_rstd, plain, w, b, h, dz);
 #pragma unroll
         for (int c = 0; c < W; ++c) dz[c] = one_rstd * fmaf(h[c], minus_m2, fmaf(dz[c], w[c], minus_m1));
         if (p < a.places) stream_piece(dx + p * a.y_place, dz);

@@ -1331,13 +1331,24 @@ static qgx_status check_gradient(qgx_ctx* ctx, const char* what, int dtype, uint
     return QGX_OK;
 }
 
+// The plan, and that its grid (of one dimension, 2^32 threads at most) holds it.
+static qgx_status gradient_plan(qgx_ctx* ctx, const char* what, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, uint64_t out, uint64_t dy_row,
+                                WeightGradPlan& plan)
+{
+    plan = weight_grad_plan(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols, (uint32_t)out, dy_row, ctx->n_simd / 4u);
+    if ((uint64_t)plan.tiles_i * plan.tiles_o * plan.parts * workers >= (1u << 24)) return fail(ctx, QGX_ERR_ARG, "%s: more tiles than a launch has", what);
+    return QGX_OK;
+}
+
 qgx_status qgx_weight_gradient_scratch(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, uint64_t out, uint64_t dy_row, uint64_t* bytes)
 {
-    const qgx_status s = check_gradient(ctx, "qgx_weight_gradient_scratch", dtype, workers, rows, cols, out);
+    qgx_status s = check_gradient(ctx, "qgx_weight_gradient_scratch", dtype, workers, rows, cols, out);
     if (s != QGX_OK) return s;
     if (!bytes) return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient_scratch: null argument");
-    *bytes = weight_grad_plan(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols, (uint32_t)out, dy_row, ctx->n_simd / 4u).scratch;
-    return QGX_OK;
+    WeightGradPlan plan;
+    s = gradient_plan(ctx, "qgx_weight_gradient_scratch", dtype, workers, rows, cols, out, dy_row, plan);
+    if (s == QGX_OK) *bytes = plan.scratch;
+    return s;
 }
 
 qgx_status qgx_weight_gradient(qgx_ctx* ctx, const qgx_kept* x, int dtype, uint64_t workers, uint64_t rows, uint64_t out, const void* dy,
@@ -1354,7 +1365,9 @@ qgx_status qgx_weight_gradient(qgx_ctx* ctx, const qgx_kept* x, int dtype, uint6
     if (!dweight || !aligned_to(dweight, 4u) || !aligned_to(dbias, 4u)) return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient: null or misaligned gradients");
     if ((workers > 1 && (dw_worker < cols * out || (dbias && db_worker < out))) || dw_worker >= (1ull << 60) / workers || db_worker >= (1ull << 60) / workers)
         return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient: the workers' gradients overlap, or a stride out of range");
-    const WeightGradPlan plan = weight_grad_plan(dtype, (uint32_t)workers, (uint32_t)rows, (uint32_t)cols, (uint32_t)out, dy_row, ctx->n_simd / 4u);
+    WeightGradPlan plan;
+    s = gradient_plan(ctx, "qgx_weight_gradient", dtype, workers, rows, cols, out, dy_row, plan);
+    if (s != QGX_OK) return s;
     if (plan.scratch && (!scratch || !aligned16(scratch))) return fail(ctx, QGX_ERR_ARG, "qgx_weight_gradient: null or misaligned scratch");
     if (scratch_bytes < plan.scratch) return fail(ctx, QGX_ERR_CAPACITY, "qgx_weight_gradient: scratch needs %llu bytes", (unsigned long long)plan.scratch);
     WeightGradArgs a{};
@@ -1380,9 +1393,13 @@ static qgx_status check_group(qgx_ctx* ctx, const char* what, const qgx_group_sh
     return QGX_OK;
 }
 
-static GroupPlan plan_of(const qgx_ctx* ctx, const qgx_group_shape* g, bool backward)
+// The plan, and that its grid holds it: 2^32 threads at most.
+static qgx_status plan_of(qgx_ctx* ctx, const char* what, const qgx_group_shape* g, bool backward, GroupPlan& plan)
 {
-    return group_plan(g->dtype, (uint32_t)g->workers, (uint32_t)(g->workers * g->batch), (uint32_t)g->places, (uint32_t)g->channels, g->groups, backward, ctx->n_simd / 4u);
+    const uint64_t samples = g->workers * g->batch;
+    plan = group_plan(g->dtype, (uint32_t)g->workers, (uint32_t)samples, (uint32_t)g->places, (uint32_t)g->channels, g->groups, backward, ctx->n_simd / 4u);
+    if (plan.whole && samples * plan.spans * plan.threads >= (1ull << 32)) return fail(ctx, QGX_ERR_ARG, "%s: more samples and channels than a launch has", what);
+    return QGX_OK;
 }
 
 static bool no_places(const qgx_group_shape* g) { return g->workers == 0 || g->batch == 0 || g->places == 0; }
@@ -1414,7 +1431,6 @@ static GroupArgs group_args(const qgx_group_shape* g)
 
 static qgx_status check_group_scratch(qgx_ctx* ctx, const char* what, const GroupPlan& plan, const void* scratch, uint64_t bytes)
 {
-    if (plan.whole && (uint64_t)plan.spans > (1u << 21)) return fail(ctx, QGX_ERR_ARG, "%s: size out of range", what);
     if (plan.scratch && (!scratch || !aligned16(scratch))) return fail(ctx, QGX_ERR_ARG, "%s: null or misaligned scratch", what);
     if (bytes < plan.scratch) return fail(ctx, QGX_ERR_CAPACITY, "%s: scratch needs %llu bytes", what, (unsigned long long)plan.scratch);
     return QGX_OK;
@@ -1422,11 +1438,13 @@ static qgx_status check_group_scratch(qgx_ctx* ctx, const char* what, const Grou
 
 qgx_status qgx_group_norm_scratch(qgx_ctx* ctx, const qgx_group_shape* shape, int backward, uint64_t* bytes)
 {
-    const qgx_status s = check_group(ctx, "qgx_group_norm_scratch", shape);
+    qgx_status s = check_group(ctx, "qgx_group_norm_scratch", shape);
     if (s != QGX_OK) return s;
     if (!bytes) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm_scratch: null argument");
-    *bytes = no_places(shape) ? 0 : plan_of(ctx, shape, backward != 0).scratch;
-    return QGX_OK;
+    GroupPlan plan{};
+    if (!no_places(shape)) s = plan_of(ctx, "qgx_group_norm_scratch", shape, backward != 0, plan);
+    if (s == QGX_OK) *bytes = plan.scratch;
+    return s;
 }
 
 qgx_status qgx_group_norm(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_places* x, const float* weight, const float* bias, float eps,
@@ -1445,8 +1463,9 @@ qgx_status qgx_group_norm(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_
     if (x->data == y->data && !same_places(shape, x, y)) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: y at x's memory must have its strides");
     if (!aligned_to(weight, 4u) || !aligned_to(bias, 4u) || !aligned_to(mean, 4u) || !aligned_to(rstd, 4u))
         return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: binary32 buffers must be 4-byte aligned");
-    const GroupPlan plan = plan_of(ctx, shape, false);
-    s = check_group_scratch(ctx, "qgx_group_norm", plan, scratch, scratch_bytes);
+    GroupPlan plan;
+    s = plan_of(ctx, "qgx_group_norm", shape, false, plan);
+    if (s == QGX_OK) s = check_group_scratch(ctx, "qgx_group_norm", plan, scratch, scratch_bytes);
     if (s != QGX_OK) return s;
     GroupArgs a = group_args(shape);
     a.x = x->data; a.x_worker = x->s_worker; a.x_batch = x->s_batch; a.x_place = x->s_place;
@@ -1488,8 +1507,8 @@ qgx_status qgx_group_norm_backward(qgx_ctx* ctx, const qgx_group_shape* shape, c
     if (!aligned_to(weight, 4u) || !aligned_to(bias, 4u) || !aligned_to(mean, 4u) || !aligned_to(rstd, 4u) || !aligned_to(dweight, 4u) || !aligned_to(dbias, 4u))
         return fail(ctx, QGX_ERR_ARG, "qgx_group_norm_backward: binary32 buffers must be 4-byte aligned");
     GroupPlan plan{};
-    if (!no_places(shape)) plan = plan_of(ctx, shape, true);
-    s = check_group_scratch(ctx, "qgx_group_norm_backward", plan, scratch, scratch_bytes);
+    if (!no_places(shape)) s = plan_of(ctx, "qgx_group_norm_backward", shape, true, plan);
+    if (s == QGX_OK) s = check_group_scratch(ctx, "qgx_group_norm_backward", plan, scratch, scratch_bytes);
     if (s != QGX_OK) return s;
     GroupArgs a = group_args(shape);
     if (!no_places(shape)) {

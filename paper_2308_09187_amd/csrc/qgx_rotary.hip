@@ -99,7 +99,7 @@ __global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, Frequenci
         // The items of a head (pieces of pairs, the first `turned`, then pieces of what stays) to as many threads, heads and tokens in turn, two at
         // a time: their loads are under way together.
         const uint32_t heads_at_once = items <= kTurnThreads ? kTurnThreads / items : 1u, rows = count * a.heads;
-        const uint32_t row0 = threadIdx.x / items;
+        const uint32_t row0 = threadIdx.x / items, next_token = heads_at_once / a.heads, next_head = heads_at_once % a.heads;
         for (uint32_t item = threadIdx.x % items; item < items && row0 < heads_at_once; item += items <= kTurnThreads ? items : kTurnThreads) {
             HeadPiece<T, NEIGHBOURS> x[2];
             const bool turns = item < turned;
@@ -120,8 +120,9 @@ __global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, Frequenci
                     to[j] = (T*)a.out + s_out[token] + head * a.o_head;
                     x[j].load((const T*)a.in + s_in[token] + head * a.i_head, P);
                     if (!ok) where[j] = 0u;
-                    head += heads_at_once;
-                    while (head >= a.heads) { head -= a.heads; ++local; }
+                    local += next_token;
+                    head += next_head;
+                    if (head >= a.heads) { head -= a.heads; ++local; }
                 }
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {

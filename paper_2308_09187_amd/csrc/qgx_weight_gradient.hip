@@ -40,7 +40,7 @@ __device__ __forceinline__ FourOf<T> load_four(const T* p, int left)
 }
 
 template <typename T>
-__global__ __launch_bounds__(kGradThreads, 2) void k_weight_gradient(WeightGradArgs a)
+__global__ __launch_bounds__(kGradThreads) void k_weight_gradient(WeightGradArgs a)
 {
     constexpr int P = kGradParts<T>, kOcts = kGradRows / 8;
     __shared__ __align__(16) uint4 s_x[2][kOcts][kGradTile];

@@ -745,23 +745,23 @@ class Context:
         return _GroupShape(code, act, slope, groups, 1, sh[0] if n == 3 else 1, sh[-2], sh[-1])
 
     @staticmethod
-    def _channel_parameter(t, channels, name):
-        """Address of a contiguous binary32 parameter of the channels, or of a run of one; None stays None."""
+    def _channel_parameter(t, channels, dev, name):
+        """Address of a contiguous binary32 parameter of the channels on that device, or of a run of one; None stays None."""
         if t is None:
             return None
-        if not (t.is_cuda and t.dtype == torch.float32 and t.dim() == 1 and t.shape[0] == channels and (t.stride(0) == 1 or channels == 1)):
-            raise QgxError(ERR_ARG, "%s: contiguous float32 of %d channels on the GPU" % (name, channels))
+        if not (t.get_device() == dev and t.dtype == torch.float32 and t.dim() == 1 and t.shape[0] == channels and (t.stride(0) == 1 or channels == 1)):
+            raise QgxError(ERR_ARG, "%s: contiguous float32 of %d channels on the device of the others" % (name, channels))
         return t.data_ptr()
 
     @staticmethod
-    def _group_statistic(t, shape, n, name):
+    def _group_statistic(t, shape, n, dev, name):
         """Address of a contiguous binary32 [workers, batch, groups], without the dimensions that dy has not."""
-        ok = t is not None and t.is_cuda and t.dtype == torch.float32 and t.dim() == n - 1 and t.is_contiguous()
+        ok = t is not None and t.get_device() == dev and t.dtype == torch.float32 and t.dim() == n - 1 and t.is_contiguous()
         if ok:
             sh = t.shape
             ok = sh[-1] == shape.groups and (n < 3 or sh[-2] == shape.batch) and (n < 4 or sh[0] == shape.workers)
         if not ok:
-            raise QgxError(ERR_ARG, "%s: contiguous float32 [.., groups] on the GPU" % name)
+            raise QgxError(ERR_ARG, "%s: contiguous float32 [.., groups] on dy's device" % name)
         return t.data_ptr()
 
     def _group_scratch(self, shape, backward, like, stream):
@@ -783,7 +783,8 @@ class Context:
         shape = self._group_shape(x, groups, activation, slope, "x")
         channels = shape.channels
         src = self._places(x, "x")
-        w, b = self._channel_parameter(weight, channels, "weight"), self._channel_parameter(bias, channels, "bias")
+        dev = x.get_device()
+        w, b = self._channel_parameter(weight, channels, dev, "weight"), self._channel_parameter(bias, channels, dev, "bias")
         if out is None:
             out = _empty_like(x, stream)
             dst = self._places_new(out, shape)
@@ -792,7 +793,7 @@ class Context:
         kept, unbiased = None, 0
         if keep is not None:
             unbiased = call_id is not None
-            if keep.shape != x.shape or keep.codes.get_device() != x.get_device() or (unbiased and not 0 <= call_id < 1 << 32):
+            if keep.shape != x.shape or keep.codes.get_device() != dev or (unbiased and not 0 <= call_id < 1 << 32):
                 raise QgxError(ERR_ARG, "keep: a checkpoint of x's shape, on its device; call_id: 32 bits")
             kept = keep._ref
         mean = rstd = m = r = None
@@ -820,8 +821,8 @@ class Context:
             kept = x._ref
         else:
             src = self._places_like(x, dy, "x")
-        w, b = self._channel_parameter(weight, channels, "weight"), self._channel_parameter(bias, channels, "bias")
-        m, r = self._group_statistic(mean, shape, n, "mean"), self._group_statistic(rstd, shape, n, "rstd")
+        w, b = self._channel_parameter(weight, channels, dev, "weight"), self._channel_parameter(bias, channels, dev, "bias")
+        m, r = self._group_statistic(mean, shape, n, dev, "mean"), self._group_statistic(rstd, shape, n, dev, "rstd")
         step, to = None, [None, None]
         for i, t in enumerate((dw, db)):
             if t is None:

@@ -204,6 +204,27 @@ def test_another_stream_repeats_and_nothing_to_do(ctx):
     assert ctx.restore(ctx.checkpoint(torch.zeros(2, 0, 40, device="cuda"))).shape == (2, 0, 40)
 
 
+@pytest.mark.parametrize("call", [None, 3])
+def test_offsets_beyond_32_bits(ctx, call):
+    rows, cols, last = (1 << 20) + 9, 4128, 70
+    x = torch.zeros(rows, cols, device="cuda", dtype=torch.bfloat16)
+    x[-last:] = inputs(11, last, cols, "bf16")
+    kept = ctx.checkpoint(x, call)
+    flat = x[-last:].double().cpu().numpy()
+    if call is None:
+        codes, powers, values = model(flat, "bf16", None)
+        assert np.array_equal(kept.codes[-last:].cpu().numpy(), codes) and np.array_equal(kept.powers[-last:].cpu().numpy(), powers)
+        got = ctx.restore(kept, torch.float32)[-last:]
+        assert np.array_equal(got.double().cpu().numpy(), values)
+    else:                                                  # (to the one or the other side; the row in the draws is that of the whole)
+        got = ctx.restore(kept, torch.float32)[-last:].double().cpu().numpy()
+        step = np.exp2(kept.powers[-last:].double().cpu().numpy() - 127.0).repeat(32, 1)
+        assert (np.abs(got - flat) < np.where(flat == 0, 1e-300, step)).all()
+    assert int(kept.powers[:-last].max()) == 0 and int((kept.codes[:-last] != 128).sum()) == 0
+    del x, kept, got
+    torch.cuda.empty_cache()
+
+
 def test_refusals(ctx):
     from paper_2308_09187_amd import qgx
     x = torch.zeros(4, 40, device="cuda")

@@ -383,6 +383,72 @@ def test_nothing_to_do(ctx):
     ctx.group_norm_backward(x, x.clone(), 2, w, b, m, r, dw=dw[:0], db=db[:0])
 
 
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+@pytest.mark.parametrize("P,C,G", [(50, 64, 4), (50, 45, 5), (9000, 64, 4)])
+@pytest.mark.parametrize("kind", ["none", "silu", "leaky"])
+def test_constant_groups_far_from_zero(ctx, kind, P, C, G, typ):
+    """mean * rstd beyond binary32, x - mean 0: z is the bias, dx = rstd (g - mean g), dw 0.  Also of what was kept (3 2^121 is 96 2^116, kept exactly), and
+    where places do not fill the threads.  The statistics are given: a forward pass's sum of n of these, 3 n 2^121, is beyond binary32 (2^128) from n = 43 on,
+    which the header rules out, so that it has none to offer."""
+    x = torch.full((1, 2, P, C), 3 * 2.0 ** 121, device="cuda").to(TYPES[typ])
+    w, b = params(2, C)
+    mean, rstd = torch.full((1, 2, G), 3 * 2.0 ** 121, device="cuda"), torch.full((1, 2, G), 1e5 ** 0.5, device="cuda")
+    _, d = act(host(b), kind)
+    dy = make(3, x.shape, typ)
+    want = (host(dy) * d).sum((1, 2))
+    bound = (S_of(P, 1) + 20 * U) * (np.abs(host(dy)) * np.abs(d)).sum((1, 2))
+    for source in (x, ctx.checkpoint(x)):
+        dw, db = torch.empty(1, C, device="cuda"), torch.empty(1, C, device="cuda")
+        dx = ctx.group_norm_backward(dy, source, G, w, b, mean, rstd, kind, SLOPE, dw=dw, db=db)
+        assert bool((dw == 0).all()) and bool(torch.isfinite(dx).all())
+        assert (np.abs(host(db) - want) <= bound).all()
+
+
+def test_two_graphs_at_once(ctx):
+    """Two captured steps replayed side by side on two streams: each has its own memory for the parts' sums."""
+    P, C, G = 8000, 64, 8
+    xs, dys = [make(30 + i, (2, 2, P, C), "bf16") for i in range(2)], [make(40 + i, (2, 2, P, C), "bf16") for i in range(2)]
+    w, b = params(50, C)
+    want, got, graphs, streams = [], [], [], [torch.cuda.Stream() for _ in xs]
+
+    def step(i, stream=None):
+        dw, db = torch.empty(2, C, device="cuda"), torch.empty(2, C, device="cuda")
+        y, m, r = ctx.group_norm(xs[i], G, w, b, activation="silu", stream=stream)
+        return y, m, r, ctx.group_norm_backward(dys[i], xs[i], G, w, b, m, r, "silu", dw=dw, db=db, stream=stream), dw, db
+
+    for i in range(2):
+        want.append(step(i))
+    torch.cuda.synchronize()
+    for i, s in enumerate(streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            got.append(step(i, s))
+        graphs.append(g)
+    for _ in range(3):
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for a, c in zip(got, want):
+            assert all(torch.equal(s, t) for s, t in zip(a, c))
+            for t in a:
+                t.zero_()
+
+
+def test_grids_too_large_are_refused(ctx):
+    from ctypes import addressof
+
+    from paper_2308_09187_amd import qgx
+
+    def ask(*a):
+        shape = qgx._GroupShape(*a)
+        return ctx.lib.qgx_group_norm_scratch(ctx._h, addressof(shape), 0, ctx._need_ref)
+
+    assert ask(qgx.DTYPES[torch.float32], 0, 0.0, 1 << 18, 1, 65535, 1, 1 << 20) == qgx.ERR_ARG
+    assert ask(qgx.DTYPES[torch.float32], 0, 0.0, 1 << 8, 1, 65535, 1, 1 << 10) == 0
+
+
 @pytest.mark.parametrize("P", [60, 8000])
 def test_on_another_stream_and_in_a_graph(ctx, P):
     K, N, C, G = 2, 2, 64, 8

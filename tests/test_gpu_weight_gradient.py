@@ -170,6 +170,79 @@ def test_against_differences(ctx):
         assert float(loss) == float(dw[0, i, o])
 
 
+@pytest.mark.parametrize("typ", TYPES)
+def test_rows_far_apart(ctx, typ):
+    """dy's rows 2^24 + 6 elements apart (a step of more than the tiled kernels take), and one column of many."""
+    rows, cols, out = 40, 33, 6
+    x, d = whole_numbers(6, 1, rows, cols, out, typ)
+    dy = torch.empty(rows, (1 << 24) + 6, device="cuda", dtype=TYPES[typ])[:, 5:5 + out]
+    dy.copy_(d[0])
+    dw, db = torch.empty(cols, out, device="cuda"), torch.empty(out, device="cuda")
+    kept = ctx.checkpoint(x[0])
+    ctx.weight_gradient(kept, dy, dw, db)
+    assert torch.equal(dw.double(), product(x[0], d[0])) and torch.equal(db.double(), d[0].double().sum(0))
+    ctx.weight_gradient(kept, dy[:, 2:3], dw[:, :1].contiguous(), db[:1])
+    assert float(db[0]) == float(d[0, :, 2].double().sum())
+    torch.cuda.empty_cache()
+
+
+def test_offsets_beyond_32_bits(ctx):
+    """More than 2^32 codes, and a dy of more than 2^32 elements, of which only the last rows are no zeros."""
+    rows, cols, out, last = (1 << 20) + 77, 4128, 34, 300
+    x, d = whole_numbers(7, 1, last, cols, out, "bf16")
+    kept = ctx.new_checkpoint((rows, cols))
+    kept.codes.fill_(128)
+    kept.powers.zero_()
+    small = ctx.checkpoint(x[0])
+    kept.codes[-last:].copy_(small.codes)
+    kept.powers[-last:].copy_(small.powers)
+    wide = torch.zeros(rows, 4200, device="cuda", dtype=torch.bfloat16)
+    dy = wide[:, 4001:4001 + out]
+    dy[-last:].copy_(d[0])
+    dw, db = torch.empty(cols, out, device="cuda"), torch.empty(out, device="cuda")
+    ctx.weight_gradient(kept, dy, dw, db)
+    assert torch.equal(dw.double(), product(x[0], d[0])) and torch.equal(db.double(), d[0].double().sum(0))
+    del kept, wide, dy
+    torch.cuda.empty_cache()
+
+
+def test_two_calls_at_once(ctx):
+    """Two streams' calls, and two graphs replayed side by side: each has its own memory for the parts' sums."""
+    data = [whole_numbers(8 + i, 2, 3000, 96, 200, "bf16") for i in range(2)]
+    kept = [ctx.checkpoint(x) for x, _ in data]
+    dw = [torch.zeros(2, 96, 200, device="cuda") for _ in data]
+    want = [product(x, dy) for x, dy in data]
+    streams = [torch.cuda.Stream() for _ in data]
+    torch.cuda.synchronize()
+    for i, s in enumerate(streams):
+        ctx.weight_gradient(kept[i], data[i][1], dw[i], stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a.double(), b) for a, b in zip(dw, want))
+    graphs = []
+    for i, s in enumerate(streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            ctx.weight_gradient(kept[i], data[i][1], dw[i], stream=s)
+        graphs.append(g)
+    for _ in range(3):
+        for t in dw:
+            t.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.double(), b) for a, b in zip(dw, want))
+
+
+def test_grids_too_large_are_refused(ctx):
+    from paper_2308_09187_amd import qgx
+    ask = lambda *a: ctx.lib.qgx_weight_gradient_scratch(ctx._h, *a, ctx._need_ref)  # noqa: E731
+    assert ask(2, 65535, 1, 1 << 17, 1 << 13, 1 << 13) == qgx.ERR_ARG
+    assert ask(2, 65535, 1, 1 << 10, 1 << 10, 1 << 10) == 0
+    assert ask(2, 65535, 1, 1 << 17, 1, 1) == qgx.ERR_ARG
+
+
 def test_nothing_to_do(ctx):
     dw, db = torch.full((2, 40, 30), 5.0, device="cuda"), torch.full((2, 30), 5.0, device="cuda")
     ctx.weight_gradient(ctx.checkpoint(torch.zeros(2, 0, 40, device="cuda")), torch.zeros(2, 0, 30, device="cuda"), dw, db)
