@@ -289,6 +289,28 @@ class Rotary:
         return cls(pairs, [base ** (-i / n) for n in pairs for i in range(n)], neighbours)
 
 
+class _GroupCall:
+    """What is the same in every group norm of tensors of one shape, one type and the same steps."""
+
+    def __init__(self, ctx, t, groups, activation, slope, backward, name):
+        code, sh, act = DTYPES.get(t.dtype), t.shape, ACTIVATIONS.get(activation)
+        n = len(sh)
+        _need(code is not None and t.is_cuda and 2 <= n <= 4, "%s: [workers, batch, places, channels] of float32, float16 or bfloat16 on the GPU", name)
+        _need(act is not None and 0 < groups < 1 << 32 and sh[-1] % groups == 0, "activation: none, silu or leaky; groups: a divisor of the channels")
+        self.workers, batch = sh[0] if n == 4 else 1, sh[-3] if n > 2 else 1
+        self.shape = _GroupShape(code, act, slope, groups, self.workers, batch, sh[-2], sh[-1])
+        self.device, self.channels, self.statistics = t.get_device(), sh[-1:], sh[:-2] + (groups,)
+        self.both, self.gradients = (2,) + self.statistics, sh[:1] + sh[-1:] if n == 4 else sh[-1:]
+        self.first = Context._places(t, name)            # t itself, x or dy
+        run = sh[-2] * sh[-1]
+        self.new = _Places(None, batch * run, run, sh[-1])                     # a new tensor of its shape
+        self.shape_ref, self.first_ref, self.new_ref = C.addressof(self.shape), C.addressof(self.first), C.addressof(self.new)
+        st = ctx.lib.qgx_group_norm_scratch(ctx._h, self.shape_ref, backward, ctx._need_ref)
+        if st:
+            ctx._check(st)
+        self.scratch = ctx._need_bytes.value
+
+
 class TensorList:
     """Gradient tensors of the K workers and where they belong in V; made by Context.tensor_list.  Holds the tensors."""
 
@@ -334,6 +356,7 @@ class Context:
         self._h = C.c_void_p()
         self._need_bytes = C.c_uint64()           # where the scratch functions answer
         self._need_ref = C.addressof(self._need_bytes)
+        self._group_calls = {}
         self._like = torch.empty(0, dtype=torch.uint8, device=device)
         self._table, self._n_sym = 0, {}          # the table selected; symbols of each table that was set
         with torch.cuda.device(device):
@@ -726,83 +749,61 @@ class Context:
             raise QgxError(ERR_ARG, "%s: of x's shape and type, on its device" % name)
         return cls._places(t, name)
 
-    @staticmethod
-    def _places_new(t, shape):
-        """The same of a new tensor."""
-        run = shape.places * shape.channels
-        return _Places(t.data_ptr(), shape.batch * run, run, shape.channels)
+    def _group_call(self, t, groups, activation, slope, backward, name):
+        """The call for tensors of t's shape, steps, type and device, worked out once for each."""
+        key = (t.shape, t.stride(), t.dtype, t.get_device(), groups, activation, slope, backward)
+        call = self._group_calls.get(key)
+        if call is None:
+            call = _GroupCall(self, t, groups, activation, slope, backward, name)
+            if len(self._group_calls) >= 256:
+                self._group_calls.clear()
+            self._group_calls[key] = call
+        return call
 
     @staticmethod
-    def _group_shape(t, groups, activation, slope, name):
-        code, sh, act = DTYPES.get(t.dtype), t.shape, ACTIVATIONS.get(activation)
-        n = len(sh)
-        if not (code is not None and t.is_cuda and 2 <= n <= 4):
-            raise QgxError(ERR_ARG, "%s: [workers, batch, places, channels] of float32, float16 or bfloat16 on the GPU" % name)
-        if act is None or not 0 < groups < 1 << 32 or sh[-1] % groups:
-            raise QgxError(ERR_ARG, "activation: none, silu or leaky; groups: a divisor of the channels")
-        if n == 4:
-            return _GroupShape(code, act, slope, groups, sh[0], sh[1], sh[2], sh[3])
-        return _GroupShape(code, act, slope, groups, 1, sh[0] if n == 3 else 1, sh[-2], sh[-1])
-
-    @staticmethod
-    def _channel_parameter(t, channels, dev, name):
-        """Address of a contiguous binary32 parameter of the channels on that device, or of a run of one; None stays None."""
+    def _channel_parameter(t, call, name):
+        """Address of a contiguous binary32 parameter of the channels, or of a run of one; None stays None."""
         if t is None:
             return None
-        if not (t.get_device() == dev and t.dtype == torch.float32 and t.dim() == 1 and t.shape[0] == channels and (t.stride(0) == 1 or channels == 1)):
-            raise QgxError(ERR_ARG, "%s: contiguous float32 of %d channels on the device of the others" % (name, channels))
+        if not (t.shape == call.channels and t.dtype == torch.float32 and t.get_device() == call.device and (t.stride(0) == 1 or call.channels[0] == 1)):
+            raise QgxError(ERR_ARG, "%s: contiguous float32 of %d channels on the device of the others" % (name, call.channels[0]))
         return t.data_ptr()
 
     @staticmethod
-    def _group_statistic(t, shape, n, dev, name):
+    def _group_statistic(t, call, name):
         """Address of a contiguous binary32 [workers, batch, groups], without the dimensions that dy has not."""
-        ok = t is not None and t.get_device() == dev and t.dtype == torch.float32 and t.dim() == n - 1 and t.is_contiguous()
-        if ok:
-            sh = t.shape
-            ok = sh[-1] == shape.groups and (n < 3 or sh[-2] == shape.batch) and (n < 4 or sh[0] == shape.workers)
-        if not ok:
+        if not (t is not None and t.shape == call.statistics and t.dtype == torch.float32 and t.get_device() == call.device and t.is_contiguous()):
             raise QgxError(ERR_ARG, "%s: contiguous float32 [.., groups] on dy's device" % name)
         return t.data_ptr()
-
-    def _group_scratch(self, shape, backward, like, stream):
-        """(tensor or None, address, bytes)"""
-        st = self.lib.qgx_group_norm_scratch(self._h, C.addressof(shape), backward, self._need_ref)
-        if st:
-            self._check(st)
-        n = self._need_bytes.value
-        if not n:
-            return None, None, 0
-        t = _empty(like, (n,), torch.uint8, stream)
-        return t, t.data_ptr(), n
 
     def group_norm(self, x, groups, weight=None, bias=None, eps=1e-5, activation="none", slope=0.01, keep=None, call_id=None, out=None, save=True,
                    stream=None):
         """Group norm of x [workers, batch, places, channels] (or without workers, or without both) and an activation: "none", "silu",
         "leaky" (slope).  Returns (y, mean, rstd), the last two [.., groups] for the backward pass (save=False: None).  keep: a
         Checkpoint in which x is kept as well, as checkpoint(x, call_id) would."""
-        shape = self._group_shape(x, groups, activation, slope, "x")
-        channels = shape.channels
-        src = self._places(x, "x")
-        dev = x.get_device()
-        w, b = self._channel_parameter(weight, channels, dev, "weight"), self._channel_parameter(bias, channels, dev, "bias")
+        call = self._group_call(x, groups, activation, slope, 0, "x")
+        call.first.data = x.data_ptr()
+        w, b = self._channel_parameter(weight, call, "weight"), self._channel_parameter(bias, call, "bias")
         if out is None:
-            out = _empty_like(x, stream)
-            dst = self._places_new(out, shape)
+            out, to = _empty_like(x, stream), call.new_ref
+            call.new.data = out.data_ptr()
         else:
             dst = self._places_like(out, x, "out")
+            to = C.addressof(dst)
         kept, unbiased = None, 0
         if keep is not None:
             unbiased = call_id is not None
-            if keep.shape != x.shape or keep.codes.get_device() != dev or (unbiased and not 0 <= call_id < 1 << 32):
+            if keep.shape != x.shape or keep.codes.get_device() != call.device or (unbiased and not 0 <= call_id < 1 << 32):
                 raise QgxError(ERR_ARG, "keep: a checkpoint of x's shape, on its device; call_id: 32 bits")
             kept = keep._ref
         mean = rstd = m = r = None
         if save:
-            mean, rstd = _empty(x, (2,) + x.shape[:-2] + (groups,), torch.float32, stream).unbind(0)
+            mean, rstd = _empty(x, call.both, torch.float32, stream).unbind(0)
             m, r = mean.data_ptr(), rstd.data_ptr()
-        scratch, at, size = self._group_scratch(shape, 0, x, stream)
-        st = self.lib.qgx_group_norm(self._h, C.addressof(shape), C.addressof(src), w, b, eps, C.addressof(dst), m, r, kept, unbiased, call_id or 0, at, size,
-                                     _handle(stream, x))
+        size = call.scratch
+        scratch = _empty(x, (size,), torch.uint8, stream) if size else None
+        st = self.lib.qgx_group_norm(self._h, call.shape_ref, call.first_ref, w, b, eps, to, m, r, kept, unbiased, call_id or 0,
+                                     scratch.data_ptr() if size else None, size, _handle(stream, x))
         if st:
             self._check(st)
         return out, mean, rstd
@@ -811,41 +812,40 @@ class Context:
                             stream=None):
         """Returns dx (None with need_dx=False) and writes the workers' weight and bias gradients to dw and db, float32 [workers, channels], runs
         of V's rows say ([channels] where dy has no worker dimension).  x: the forward pass's input, or a Checkpoint of it."""
-        shape = self._group_shape(dy, groups, activation, slope, "dy")
-        channels, wk, n = shape.channels, shape.workers, dy.dim()
-        grad, dev = self._places(dy, "dy"), dy.get_device()
-        src = kept = None
+        call = self._group_call(dy, groups, activation, slope, 1, "dy")
+        dev, src, kept = call.device, None, None
+        call.first.data = dy.data_ptr()
         if isinstance(x, Checkpoint):
             if x.shape != dy.shape or x.codes.get_device() != dev:
                 raise QgxError(ERR_ARG, "x: a checkpoint of dy's shape, on its device")
             kept = x._ref
         else:
-            src = self._places_like(x, dy, "x")
-        w, b = self._channel_parameter(weight, channels, dev, "weight"), self._channel_parameter(bias, channels, dev, "bias")
-        m, r = self._group_statistic(mean, shape, n, dev, "mean"), self._group_statistic(rstd, shape, n, dev, "rstd")
+            places = self._places_like(x, dy, "x")
+            src = C.addressof(places)
+        w, b = self._channel_parameter(weight, call, "weight"), self._channel_parameter(bias, call, "bias")
+        m, r = self._group_statistic(mean, call, "mean"), self._group_statistic(rstd, call, "rstd")
         step, to = None, [None, None]
         for i, t in enumerate((dw, db)):
             if t is None:
                 continue
-            sh = t.shape
-            if not (t.dtype == torch.float32 and t.get_device() == dev and len(sh) == (2 if n == 4 else 1) and sh[-1] == channels and (n < 4 or sh[0] == wk) and
-                    (channels <= 1 or t.stride(-1) == 1)):
+            if not (t.shape == call.gradients and t.dtype == torch.float32 and t.get_device() == dev and (t.stride(-1) == 1 or call.channels[0] == 1)):
                 raise QgxError(ERR_ARG, "dw and db: float32 [workers, channels] on dy's device")
-            one = t.stride(0) if wk > 1 else channels
+            one = t.stride(0) if call.workers > 1 else call.channels[0]
             if step is not None and step != one:
                 raise QgxError(ERR_ARG, "dw and db: one step between workers")
             step = one
             to[i] = t.data_ptr()
         dst = None
         if dx is not None:
-            dst = self._places_like(dx, dy, "dx")
+            out = self._places_like(dx, dy, "dx")
+            dst = C.addressof(out)
         elif need_dx:
-            dx = _empty_like(dy, stream)
-            dst = self._places_new(dx, shape)
-        scratch, at, size = self._group_scratch(shape, 1, dy, stream)
-        st = self.lib.qgx_group_norm_backward(self._h, C.addressof(shape), C.addressof(grad), None if src is None else C.addressof(src), kept, w, b, m, r,
-                                              None if dst is None else C.addressof(dst), to[0], to[1], channels if step is None else step, at, size,
-                                              _handle(stream, dy))
+            dx, dst = _empty_like(dy, stream), call.new_ref
+            call.new.data = dx.data_ptr()
+        size = call.scratch
+        scratch = _empty(dy, (size,), torch.uint8, stream) if size else None
+        st = self.lib.qgx_group_norm_backward(self._h, call.shape_ref, call.first_ref, src, kept, w, b, m, r, dst, to[0], to[1],
+                                              call.channels[0] if step is None else step, scratch.data_ptr() if size else None, size, _handle(stream, dy))
         if st:
             self._check(st)
         return dx
