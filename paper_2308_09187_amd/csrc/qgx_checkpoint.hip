@@ -24,47 +24,70 @@ __device__ __forceinline__ Eight<T> load_eight(const T* p, int n)
     return e;
 }
 
-// The row and eight of a thread's turn, from its workgroup's first: a division of 64 bits by the workgroup; by the thread one of a number of at most 22
-// bits, in binary32 and put right by one (whole divisions, three to a turn, were half of the kernel's time).
-struct EightAt { uint32_t row, group; bool any; };
-__device__ __forceinline__ EightAt eight_at(uint64_t first_row, uint32_t first_group, uint32_t turn, uint32_t groups, float per_group, uint32_t rows)
-{
-    const uint32_t at = first_group + turn * kKeepThreads + threadIdx.x;
-    uint32_t q = (uint32_t)((float)at * per_group);
-    int rest = (int)(at - q * groups);
-    if (rest < 0) { --q; rest += (int)groups; }
-    else if (rest >= (int)groups) { ++q; rest -= (int)groups; }
-    const uint64_t row = first_row + q;
-    return EightAt{(uint32_t)min(row, (uint64_t)rows - 1u), (uint32_t)rest, row < rows};
-}
+// A thread's eights, turn by turn, from its workgroup's first: the row after the first, and the eight of it.  A division of 64 bits by the workgroup; by the
+// thread one of numbers of at most 22 bits, in binary32 and put right by one, and from one turn to the next an addition (whole divisions, three to a turn, were
+// half of the kernel's time; one of these to a turn, with 64-bit addresses, a sixth).
+struct EightAt {
+    uint32_t row, group;
+    bool carried;                                          // in the last step: into a row more than the step's own
 
-// WHOLE: rows one step apart throughout, of whole blocks.
+    __device__ __forceinline__ EightAt(uint32_t first_group, uint32_t groups)
+    {
+        const uint32_t at = first_group + threadIdx.x;
+        row = (uint32_t)((float)at * (1.0f / (float)groups));
+        const int rest = (int)(at - row * groups), below = rest >> 31;
+        row += (uint32_t)below;
+        group = (uint32_t)(rest + (below & (int)groups));
+        carry(groups);
+    }
+    __device__ __forceinline__ void next(uint32_t step_rows, uint32_t step_groups, uint32_t groups)
+    {
+        row += step_rows;
+        group += step_groups;
+        carry(groups);
+    }
+    __device__ __forceinline__ void carry(uint32_t groups)
+    {
+        carried = group >= groups;
+        group -= carried ? groups : 0u;
+        row += carried ? 1u : 0u;
+    }
+};
+
+// WHOLE: rows one step apart throughout, of whole blocks, a workgroup's rows less than 2^31 bytes apart.
 template <typename T, bool WHOLE>
 __global__ __launch_bounds__(kKeepThreads) void k_checkpoint(KeepArgs a, KeptDraws d, Scalars* sc)
 {
     constexpr int W = kPiece<T>;
-    const uint32_t groups = a.blocks * 4u;
-    const float per_group = 1.0f / (float)groups;
+    const uint32_t groups = a.blocks * 4u, step_rows = kKeepThreads / groups, step_groups = kKeepThreads % groups;
     const uint32_t call = d.on ? kept_call(d, sc) : 0u;
     const PhiloxKeys keys = philox_keys(d.seed_lo, d.seed_hi);
+    const uint32_t gap = (uint32_t)a.x_row - a.cols, step = 8u * kKeepThreads + step_rows * gap;
     for (uint64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
         const uint64_t first = tile * (kKeepThreads * kKeepTurns), first_row = first / groups;
-        const uint32_t first_group = (uint32_t)(first - first_row * groups);
+        const uint32_t rows = a.n_rows - (uint32_t)first_row;
+        EightAt at((uint32_t)(first - first_row * groups), groups);
         Eight<T> raw[kKeepTurns];
-        EightAt at[kKeepTurns];
+        uint32_t row[kKeepTurns], group[kKeepTurns], offset = at.row * (uint32_t)a.x_row + at.group * 8u;
 #pragma unroll
         for (int i = 0; i < kKeepTurns; ++i) {
-            at[i] = eight_at(first_row, first_group, (uint32_t)i, groups, per_group, a.n_rows);
-            uint64_t row = at[i].row * a.x_row;
-            if (!WHOLE && !a.even) {
-                const uint32_t sample = at[i].row / a.rows, r = at[i].row % a.rows, k = sample / a.batch;
-                row = k * a.x_worker + (sample - k * a.batch) * a.x_batch + r * a.x_row;
+            row[i] = at.row;
+            group[i] = at.group;
+            const bool any = at.row < rows;                // (past the last row: the workgroup's first)
+            if constexpr (WHOLE) {
+                raw[i] = load_eight<T, true>((const T*)a.x + first_row * a.x_row + (any ? offset : 0u), 8);
+            } else {
+                const uint32_t whole = (uint32_t)first_row + (any ? at.row : 0u), sample = whole / a.rows, r = whole % a.rows, k = sample / a.batch;
+                const uint64_t from = k * a.x_worker + (sample - k * a.batch) * a.x_batch + r * a.x_row;
+                raw[i] = load_eight<T, false>((const T*)a.x + from + (size_t)at.group * 8u, any ? (int)a.cols - (int)at.group * 8 : 0);
             }
-            // (past the last row: of the last)
-            raw[i] = load_eight<T, WHOLE>((const T*)a.x + row + (size_t)at[i].group * 8u, at[i].any ? (int)a.cols - (int)at[i].group * 8 : 0);
+            at.next(step_rows, step_groups, groups);
+            offset += step + (at.carried ? gap : 0u);
         }
         uint8_t* codes = a.codes + first * 8u;
         uint8_t* powers = a.powers + first / 4u;
+        uint32_t to = threadIdx.x;
+        asm volatile("" : "+v"(to));                       // (else every thread's address is kept in 64 bits)
 #pragma unroll
         for (int i = 0; i < kKeepTurns; ++i) {
             float v[8];
@@ -78,12 +101,11 @@ __global__ __launch_bounds__(kKeepThreads) void k_checkpoint(KeepArgs a, KeptDra
                 for (int c = 0; c < W; ++c) v[h * W + c] = x[c];
             }
             uint32_t word[2];
-            const uint32_t power = kept_codes<8>(v, quad_max(bits), a.top, d.on != 0u, at[i].group, 0u, at[i].row, call, keys, word);
-            if (!at[i].any) continue;
-            const uint32_t to = i * kKeepThreads + threadIdx.x;
-            *reinterpret_cast<uint2*>(codes + to * 8u) = make_uint2(word[0], word[1]);
+            const uint32_t power = kept_codes<8>(v, quad_max(bits), a.top, d.on != 0u, group[i], 0u, (uint32_t)first_row + row[i], call, keys, word);
+            if (row[i] >= rows) continue;
+            *reinterpret_cast<uint2*>(codes + i * kKeepThreads * 8u + to * 8u) = make_uint2(word[0], word[1]);
             if ((to & 3u) == 0u) {
-                powers[to / 4u] = (uint8_t)power;
+                powers[i * kKeepThreads / 4u + to / 4u] = (uint8_t)power;
                 if (power == kKeptSpoilt) raise_error(sc, QGX_EBIT_NONFINITE);
             }
         }
@@ -93,20 +115,21 @@ __global__ __launch_bounds__(kKeepThreads) void k_checkpoint(KeepArgs a, KeptDra
 template <typename T>
 __global__ __launch_bounds__(kKeepThreads) void k_restore(KeepArgs a)
 {
-    const uint32_t groups = a.blocks * 4u;
-    const float per_group = 1.0f / (float)groups;
+    const uint32_t groups = a.blocks * 4u, step_rows = kKeepThreads / groups, step_groups = kKeepThreads % groups;
     for (uint64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
         const uint64_t first = tile * (kKeepThreads * kKeepTurns), first_row = first / groups;
-        const uint32_t first_group = (uint32_t)(first - first_row * groups);
-        EightAt at[kKeepTurns];
+        const uint32_t rows = a.n_rows - (uint32_t)first_row;
+        EightAt at((uint32_t)(first - first_row * groups), groups);
+        uint32_t row[kKeepTurns], group[kKeepTurns], power[kKeepTurns];
         uint2 word[kKeepTurns];
-        uint32_t power[kKeepTurns];
 #pragma unroll
         for (int i = 0; i < kKeepTurns; ++i) {
-            at[i] = eight_at(first_row, first_group, (uint32_t)i, groups, per_group, a.n_rows);
-            const size_t from = (size_t)at[i].row * groups + at[i].group;
-            word[i] = *reinterpret_cast<const uint2*>(a.codes + from * 8u);
-            power[i] = a.powers[from / 4u];
+            row[i] = at.row;
+            group[i] = at.group;
+            const uint32_t from = at.row < rows ? i * kKeepThreads + threadIdx.x : 0u;           // (rows follow each other without a gap)
+            word[i] = *reinterpret_cast<const uint2*>(a.codes + first * 8u + from * 8u);
+            power[i] = (a.powers + first / 4u)[from / 4u];
+            at.next(step_rows, step_groups, groups);
         }
 #pragma unroll
         for (int i = 0; i < kKeepTurns; ++i) {
@@ -114,8 +137,8 @@ __global__ __launch_bounds__(kKeepThreads) void k_restore(KeepArgs a)
             float v[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) v[c] = kept_value(((c < 4 ? word[i].x : word[i].y) >> (8 * (c & 3))) & 0xFFu, scale);
-            const int n = at[i].any ? (int)a.cols - (int)at[i].group * 8 : 0;
-            T* y = (T*)a.y + at[i].row * a.y_row + (size_t)at[i].group * 8u;
+            const int n = row[i] < rows ? (int)a.cols - (int)group[i] * 8 : 0;
+            T* y = (T*)a.y + first_row * a.y_row + row[i] * a.y_row + (size_t)group[i] * 8u;
             if constexpr (sizeof(T) == 2) {
                 store_piece(y, n, v);
             } else {
@@ -140,7 +163,8 @@ static KeepArgs tiles_of(const KeepArgs& args)
 template <typename T>
 static void launch_checkpoint_of(const KeepArgs& a, const KeptDraws& d, Scalars* sc, dim3 grid, hipStream_t st)
 {
-    if (a.even && a.cols % QGX_KEPT_BLOCK == 0u) hipLaunchKernelGGL((k_checkpoint<T, true>), grid, dim3(kKeepThreads), 0, st, a, d, sc);
+    const uint64_t apart = (kKeepThreads * kKeepTurns / (a.blocks * 4u) + 2u) * a.x_row;         // (x_row < 2^60 / rows: of one row it may be anything)
+    if (a.even && a.cols % QGX_KEPT_BLOCK == 0u && a.x_row < (1u << 28) && apart * sizeof(T) < (1ull << 31)) hipLaunchKernelGGL((k_checkpoint<T, true>), grid, dim3(kKeepThreads), 0, st, a, d, sc);
     else hipLaunchKernelGGL((k_checkpoint<T, false>), grid, dim3(kKeepThreads), 0, st, a, d, sc);
 }
 

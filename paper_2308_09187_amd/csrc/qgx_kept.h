@@ -37,12 +37,27 @@ __device__ __forceinline__ uint32_t kept_code(float u, uint32_t at, uint32_t wor
     return __builtin_amdgcn_cvt_pk_u8_f32(rintf(u) + 128.0f, at, word);
 }
 
-// Rounded away from zero where the draw d, 16 bits, is below 2^16 times the remainder of |u|, as a signed byte: with T = ceil(2^16 |u|), a whole number of 23
-// bits, the magnitude is (T + 65535 - d) >> 16.  u16 = 2^16 u: a product by a power of two; rest = 65535 - d.
-__device__ __forceinline__ uint32_t kept_code(float u16, uint32_t rest)
+// Four codes rounded away from zero where the draw d, 16 bits, is below 2^16 times the remainder of |u|, u16 = 2^16 u.  With T = ceil(2^16 |u|), a whole
+// number of 23 bits, the magnitude's negative is (d - T) >> 16: its byte 2 is b = 256 - magnitude, or 0.  Of a negative element the code is b ^ 0x80, of
+// another (b ^ 0x7F) + 1, which never carries into the next byte, so that four are put right in their word.  (One element after the other took 8 operations
+// each for these 5: 8 x 4096 x 2048 bfloat16 51 us.)
+__device__ __forceinline__ uint32_t kept_less(float u16, uint32_t draw)
 {
-    const uint32_t T = (uint32_t)ceilf(fabsf(u16)), minus = (uint32_t)(__float_as_int(u16) >> 31);
-    return (((T + rest) >> 16) ^ minus) - minus;
+    int minus_T;
+    asm("v_cvt_flr_i32_f32_e64 %0, -|%1|" : "=v"(minus_T) : "v"(u16));
+    return draw + (uint32_t)minus_T;
+}
+
+__device__ __forceinline__ uint32_t kept_word(const float (&u16)[4], uint32_t draws01, uint32_t draws23)
+{
+    const uint32_t b0 = kept_less(u16[0], draws01 & 0xFFFFu), b1 = kept_less(u16[1], draws01 >> 16), b2 = kept_less(u16[2], draws23 & 0xFFFFu),
+                   b3 = kept_less(u16[3], draws23 >> 16);
+    const uint32_t lo = __builtin_amdgcn_perm(b1, b0, 0x0C0C0602u), hi = __builtin_amdgcn_perm(b3, b2, 0x06020C0Cu);
+    // (a selector of 9 or 11: the sign of the first or second word, all over a byte)
+    const uint32_t sign_lo = __builtin_amdgcn_perm(__float_as_uint(u16[1]), __float_as_uint(u16[0]), 0x0C0C0B09u);
+    const uint32_t sign_hi = __builtin_amdgcn_perm(__float_as_uint(u16[3]), __float_as_uint(u16[2]), 0x0B090C0Cu);
+    const uint32_t turn = (sign_lo | sign_hi) ^ 0x7F7F7F7Fu;
+    return ((lo | hi) ^ turn) + (turn & 0x01010101u);
 }
 
 // The codes of W neighbouring columns, as the words that are stored, and the block's power, from the bits of its largest magnitude.  W = 8: the columns of one
@@ -55,23 +70,16 @@ __device__ __forceinline__ uint32_t kept_codes(float (&v)[W], uint32_t bits, uin
     uint32_t over = (254u - power) << 23;                  // 2^-e (of zeros it may be anything)
     float wide = 65536.0f;
     if (__builtin_amdgcn_ballot_w64(kept_is_rare(bits, power, top)) != 0ull) {
-        if (bits >= 0x7F800000u) {
-            power = kKeptSpoilt;
-            over = 0u;
+        // (no branches within: their results would be copied on the way past them too)
+        const bool spoilt = bits >= 0x7F800000u;
+        power = bits ? min(max(power, 1u), top) : 0u;
+        const bool small = draws && power < 16u;           // the elements by 2^16
+        const float most = __uint_as_float(power << 23) * 127.0f, by = small ? 65536.0f : 1.0f;
+        wide = small ? 1.0f : 65536.0f;
+        over = spoilt ? 0u : (254u - power) << 23;
+        power = spoilt ? kKeptSpoilt : power;
 #pragma unroll
-            for (int c = 0; c < W; ++c) v[c] = 0.0f;       // (0 * infinity is no zero)
-        } else if (bits) {
-            power = min(max(power, 1u), top);
-            over = (254u - power) << 23;
-            const float most = __uint_as_float(power << 23) * 127.0f;
-#pragma unroll
-            for (int c = 0; c < W; ++c) v[c] = __builtin_amdgcn_fmed3f(v[c], -most, most);
-            if (power < 16u && draws) {                    // (the elements by 2^16, which are small then)
-#pragma unroll
-                for (int c = 0; c < W; ++c) v[c] *= 65536.0f;
-                wide = 1.0f;
-            }
-        }
+        for (int c = 0; c < W; ++c) v[c] = spoilt ? 0.0f : __builtin_amdgcn_fmed3f(v[c], -most, most) * by;      // (0 * infinity is no zero)
     }
     if (draws) {
         uint32_t w[4];
@@ -80,14 +88,10 @@ __device__ __forceinline__ uint32_t kept_codes(float (&v)[W], uint32_t bits, uin
         const float over16 = __uint_as_float(over) * wide;
 #pragma unroll
         for (int h = 0; h < W / 4; ++h) {
-            uint32_t code[4];
+            float u16[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint32_t rest = ~w[2 * h + c / 2];
-                code[c] = kept_code(v[4 * h + c] * over16, (c & 1) ? rest >> 16 : rest & 0xFFFFu);
-            }
-            const uint32_t lo = __builtin_amdgcn_perm(code[1], code[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(code[3], code[2], 0x04000C0Cu);
-            word[h] = (lo | hi) ^ 0x80808080u;
+            for (int c = 0; c < 4; ++c) u16[c] = v[4 * h + c] * over16;
+            word[h] = kept_word(u16, w[2 * h], w[2 * h + 1]);
         }
     } else {
 #pragma unroll
