@@ -7,6 +7,7 @@ streams.  Loading fails loudly when the library has not been built
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 import os
 
@@ -253,20 +254,47 @@ class Checkpoint:
         for t, n, name in ((codes, KEPT_BLOCK * blocks, "codes"), (powers, blocks, "powers")):
             _need(t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous() and t.dim() >= 1 and t.shape[-1] == n, "%s: contiguous uint8 [.., %d] on the GPU", name, n)
         _need(codes.shape[:-1] == powers.shape[:-1] and codes.get_device() == powers.get_device(), "codes and powers: of the same rows")
-        self._set(codes, powers, codes.shape[:-1] + (cols,))
-
-    def _set(self, codes, powers, shape):
-        self.codes, self.powers, self.shape = codes, powers, shape
-        self._c = _Kept(codes.data_ptr(), powers.data_ptr(), math.prod(shape[:-1]), shape[-1])
+        self.shape, self._device = codes.shape[:-1] + (cols,), codes.get_device()
+        self._memory, self._codes, self._powers = codes, codes, powers
+        self._c = _Kept(codes.data_ptr(), powers.data_ptr(), math.prod(self.shape[:-1]), cols)
         self._ref = C.addressof(self._c)
-        return self
 
     @classmethod
     def _made(cls, like, shape, stream):
-        """Memory for rows of this shape on like's device."""
-        blocks = (shape[-1] + KEPT_BLOCK - 1) // KEPT_BLOCK
-        lead = shape[:-1]
-        return cls.__new__(cls)._set(_empty(like, lead + (KEPT_BLOCK * blocks,), torch.uint8, stream), _empty(like, lead + (blocks,), torch.uint8, stream), shape)
+        """Memory for rows of this shape on like's device: one piece, of which codes and powers become tensors when they are asked for."""
+        rows, split, size = _kept_layout(shape)
+        k = cls.__new__(cls)
+        k.shape, k._device, k._codes = shape, like.get_device(), None
+        k._memory = _empty(like, (size,), torch.uint8, stream)
+        at = k._memory.data_ptr()
+        k._c = _Kept(at, at + split, rows, shape[-1])
+        k._ref = C.addressof(k._c)
+        return k
+
+    def _parts(self):
+        split = _kept_layout(self.shape)[1]
+        lead = self.shape[:-1]
+        blocks = (self.shape[-1] + KEPT_BLOCK - 1) // KEPT_BLOCK
+        self._codes, self._powers = self._memory[:split].view(lead + (KEPT_BLOCK * blocks,)), self._memory[split:].view(lead + (blocks,))
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            self._parts()
+        return self._codes
+
+    @property
+    def powers(self):
+        if self._codes is None:
+            self._parts()
+        return self._powers
+
+
+@functools.lru_cache(maxsize=256)
+def _kept_layout(shape):
+    """Rows, and bytes of their codes and of both."""
+    rows, blocks = math.prod(shape[:-1]), (shape[-1] + KEPT_BLOCK - 1) // KEPT_BLOCK
+    return rows, rows * blocks * KEPT_BLOCK, rows * blocks * (KEPT_BLOCK + 1)
 
 
 class Rotary:
@@ -682,7 +710,7 @@ class Context:
             _need(cols >= 1, "x: columns")
             out = Checkpoint._made(x, x.shape, stream)
         else:
-            _need(out.shape == x.shape and out.codes.get_device() == x.get_device(), "out: a checkpoint of x's shape, on its device")
+            _need(out.shape == x.shape and out._device == x.get_device(), "out: a checkpoint of x's shape, on its device")
         _need(call_id is None or 0 <= call_id < 1 << 32, "call_id: 32 bits")
         st = self.lib.qgx_checkpoint(self._h, code, wk, rows, cols, x.data_ptr(), xw, xr, call_id is not None, call_id or 0, out._ref, _handle(stream, x))
         if st:
@@ -695,9 +723,9 @@ class Context:
         step = cols
         if out is None:
             _need(dtype in DTYPES, "dtype: float32, float16 or bfloat16")
-            out = _empty(kept.codes, kept.shape, dtype, stream)
+            out = _empty(kept._memory, kept.shape, dtype, stream)
         else:
-            _need(out.shape == kept.shape and out.dtype in DTYPES and out.get_device() == kept.codes.get_device(), "out: of the kept shape, on its device")
+            _need(out.shape == kept.shape and out.dtype in DTYPES and out.get_device() == kept._device, "out: of the kept shape, on its device")
             if not out.is_contiguous():
                 _need(out.dim() == 2 and out.stride(1) == 1, "out: contiguous, or [rows, cols] with contiguous rows")
                 step = out.stride(0)
@@ -711,7 +739,7 @@ class Context:
         [workers, cols, out] and db [workers, out], runs of V's rows say, are written.  Returns dw."""
         code, wk, rows, out, gw, gr = self._rows(dy, "dy")
         cols = kept.shape[-1]
-        _need(dy.dim() >= 2 and kept.shape[:-1] == dy.shape[:-1] and kept.codes.get_device() == dy.get_device(), "dy: [.., out] of the kept rows, on their device")
+        _need(dy.dim() >= 2 and kept.shape[:-1] == dy.shape[:-1] and kept._device == dy.get_device(), "dy: [.., out] of the kept rows, on their device")
         lead = dy.shape[:-2]
         _need(dw is not None, "dw: where the gradient goes")
         for t, shape, name in ((dw, lead + (cols, out), "dw"), (db, lead + (out,), "db")):
@@ -793,7 +821,7 @@ class Context:
         kept, unbiased = None, 0
         if keep is not None:
             unbiased = call_id is not None
-            if keep.shape != x.shape or keep.codes.get_device() != call.device or (unbiased and not 0 <= call_id < 1 << 32):
+            if keep.shape != x.shape or keep._device != call.device or (unbiased and not 0 <= call_id < 1 << 32):
                 raise QgxError(ERR_ARG, "keep: a checkpoint of x's shape, on its device; call_id: 32 bits")
             kept = keep._ref
         mean = rstd = m = r = None
@@ -816,7 +844,7 @@ class Context:
         dev, src, kept = call.device, None, None
         call.first.data = dy.data_ptr()
         if isinstance(x, Checkpoint):
-            if x.shape != dy.shape or x.codes.get_device() != dev:
+            if x.shape != dy.shape or x._device != dev:
                 raise QgxError(ERR_ARG, "x: a checkpoint of dy's shape, on its device")
             kept = x._ref
         else:
