@@ -1097,28 +1097,34 @@ GroupPlan group_plan(int dtype, uint32_t workers, uint32_t samples, uint32_t pla
     uint32_t of = fits(wide) && (uint64_t)samples * groups >= 2u * n_cu * (uint64_t)wide ? wide : min(groups, ceil_div(4u * W, per));
     if (!one(of) && 2u * of <= groups && one(2u * of) && fits(2u * of)) of *= 2u;
     while (of < groups && 2u * of <= groups && fits(2u * of) && (one(2u * of) || !one(of)) && (uint64_t)samples * (groups / (2u * of)) >= 4u * n_cu) of *= 2u;
-    if (channels >= W && fits(of)) {
+    const uint32_t pieces = pieces_of(of);
+    uint32_t threads = 1024u;
+    for (uint32_t t = 256u; t < 1024u; t *= 2u)
+        if (pieces <= t && ceil_div(places, t / pieces) <= most) { threads = t; break; }
+    // (few workgroups, each with much to do in threads of several groups: 8 x 2120 x 112 in 16 groups forward 27 us whole, 17 in parts, 7 x 1000 x 144 in 8
+    // groups backward 40 and 21; but 32 x 1024 x 320 in 32 groups forward 24 and 29)
+    const bool few = !one(of) && threads > 256u && (uint64_t)samples * ceil_div(groups, of) < n_cu;
+    if (channels >= W && fits(of) && !few) {
         p.whole = true;
         p.one = one(of);
         p.span = of * per;
         p.spans = ceil_div(groups, of);
-        const uint32_t pieces = pieces_of(of);
-        p.threads = 1024u;
-        for (uint32_t t = 256u; t < 1024u; t *= 2u)
-            if (pieces <= t && ceil_div(places, t / pieces) <= most) { p.threads = t; break; }
-        p.pieces = ceil_div(places, p.threads / pieces);
+        p.threads = threads;
+        p.pieces = ceil_div(places, threads / pieces);
     } else {
         p.span = min(channels, 256u * W);                  // (any channels: borders of groups do not matter here)
         p.spans = ceil_div(channels, p.span);
-        const uint32_t pieces = ceil_div(p.span, W), steps = 256u / pieces;
-        // eight workgroups for every compute unit, but four turns for each of them
-        const uint32_t want = max(1u, ceil_div(8u * n_cu, (uint64_t)samples * p.spans));
-        p.part = max(ceil_div(places, want), 4u * steps * (uint32_t)(backward ? kBackTurns : kPartTurns));
+        const uint32_t steps = 256u / ceil_div(p.span, W);
+        // two or three workgroups for every compute unit, but a turn for each of them (4 x 65536 x 128 bfloat16 forward, 1, 2, 3, 4 of them: 55, 49, 50,
+        // 51 us; 6 x 17332 x 184 binary32 backward 120, 98, 85, 88; 20 x 4301 x 30 forward 19, with four turns at least 30)
+        const uint32_t want = max(1u, ceil_div((backward ? 3u : 2u) * n_cu, (uint64_t)samples * p.spans));
+        p.part = max(ceil_div(places, want), steps * (uint32_t)(backward ? kBackTurns : kPartTurns));
         p.parts = ceil_div(places, p.part);
     }
-    // Little in all: the parameters' gradients apart.  (4 x 3 x 221 x 90 binary32: kernels 9.6 and 3.9 us and a call of 19 with the sums joined by a launch)
+    // Little in all: the parameters' gradients apart.  (4 x 3 x 221 x 90 binary32 8.9 us, with the sums joined by a launch 11.2; 2 x 11 x 154 x 192 19.9 and
+    // 11.8)
     p.apart = p.whole && backward && samples > workers && p.threads == 256u && (uint64_t)samples * places * channels <= (1u << 20) &&
-              (uint64_t)(samples / workers) * places <= 4096u;
+              (uint64_t)(samples / workers) * places <= 1024u;
     const bool sums = !p.whole || (backward && samples > workers && !p.apart);
     p.at_sums = sums ? ((uint64_t)samples * p.parts * 2u * channels + 3u) / 4u * 4u : 0u;
     const uint64_t floats = p.at_sums + (p.whole ? 0u : 2u * (uint64_t)samples * groups);
