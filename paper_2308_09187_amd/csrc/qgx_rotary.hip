@@ -72,25 +72,29 @@ struct HeadPiece {
 };
 
 template <typename T, bool NEIGHBOURS, int PAIRS>
-__global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, Frequencies<PAIRS> f, uint32_t tile_tokens, uint32_t turned, uint32_t items)
+__global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, Frequencies<PAIRS> f, uint32_t tile_tokens, uint32_t turned, uint32_t items, uint32_t moved)
 {
     constexpr int W = kPiece<T>;
+    constexpr uint32_t kPairs = NEIGHBOURS ? W / 2 : W;    // of a piece
     __shared__ __align__(16) float s_cos[kTurnAngles], s_sin[kTurnAngles];
     __shared__ uint64_t s_in[kTurnTokens], s_out[kTurnTokens];
     const uint32_t P = a.pairs, stride = (P + 7u) & ~7u;
     for (uint32_t first = blockIdx.x * tile_tokens; first < a.n_tokens; first += gridDim.x * tile_tokens) {
         const uint32_t count = min(tile_tokens, a.n_tokens - first);
-        for (uint32_t i = threadIdx.x; i < count * P; i += kTurnThreads) {
-            const uint32_t local = i / P, token = first + local, p = i % P, sequence = token / a.tokens, t = token % a.tokens;
+        // (piece by piece: the last one's pairs where it has been moved to)
+        const uint32_t slots = turned * kPairs;
+        for (uint32_t i = threadIdx.x; i < count * slots; i += kTurnThreads) {
+            const uint32_t local = i / slots, token = first + local, slot = i % slots, sequence = token / a.tokens, t = token % a.tokens;
+            const uint32_t p = min(slot < slots - kPairs ? slot : slot - moved, P - 1u);
             uint32_t axis = 0;
 #pragma unroll
             for (uint32_t x = 0; x + 1 < QGX_MAX_AXES; ++x) axis += p >= a.axis_end[x];
             const uint32_t k = sequence / a.batch, n = sequence % a.batch;
             const int32_t at = a.positions[axis * a.p_axis + k * a.p_worker + n * a.p_batch + t];
             const float2 cs = cos_sin_of((double)at * f.turns[p]);
-            s_cos[local * stride + p] = cs.x;
-            s_sin[local * stride + p] = a.back ? -cs.y : cs.y;
-            if (p == 0u) {
+            s_cos[local * stride + slot] = cs.x;
+            s_sin[local * stride + slot] = a.back ? -cs.y : cs.y;
+            if (slot == 0u) {
                 s_in[local] = k * a.i_worker + n * a.i_batch + t * a.i_token;
                 s_out[local] = k * a.o_worker + n * a.o_batch + t * a.o_token;
             }
@@ -103,7 +107,7 @@ __global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, Frequenci
         for (uint32_t item = threadIdx.x % items; item < items && row0 < heads_at_once; item += items <= kTurnThreads ? items : kTurnThreads) {
             HeadPiece<T, NEIGHBOURS> x[2];
             const bool turns = item < turned;
-            const uint32_t c = turns ? item * W : 2u * P + (item - turned) * W, pair = NEIGHBOURS ? c / 2u : c;
+            const uint32_t c = turns ? item * W - (item + 1u == turned ? moved * (W / kPairs) : 0u) : 2u * P + (item - turned) * W, pair = item * kPairs;
             const int left = turns ? (NEIGHBOURS ? (int)(2u * P - c) : (int)(P - c)) : (int)(a.dim - c);
             uint32_t local = row0 / a.heads, head = row0 % a.heads;
             for (uint32_t row = row0; row < rows; row += 2u * heads_at_once) {
@@ -146,10 +150,14 @@ static hipError_t launch_rotary_as(const RotaryArgs& a, const double* turns, uin
     // unit, 107 with 16, 94 with 32, 95 with 64)
     const uint32_t tile = min(most, max(1u, a.n_tokens / (32u * n_cu)));
     const dim3 grid(min((a.n_tokens + tile - 1u) / tile, 1u << 20));
+    // The last piece of pairs moved back by so many, to end where they do: some are turned twice, with equal results, and no piece is in part.  Not in
+    // place, where the second would turn the first's.  (8 x 4481 tokens of 13 x 102 bfloat16 64 us with the last piece element by element, so 50; 12 x 3890 of 11 x 90
+    // neighbours in binary32 75 and 60)
+    const uint32_t pairs_of = a.neighbours ? W / 2u : W, moved = a.in != a.out && a.pairs >= pairs_of ? turned * pairs_of - a.pairs : 0u;
     Frequencies<PAIRS> f;
     for (uint32_t p = 0; p < (uint32_t)PAIRS; ++p) f.turns[p] = p < a.pairs ? turns[p] : 0.0;
-    if (a.neighbours) hipLaunchKernelGGL((k_rotary<T, true, PAIRS>), grid, dim3(kTurnThreads), 0, st, a, f, tile, turned, items);
-    else hipLaunchKernelGGL((k_rotary<T, false, PAIRS>), grid, dim3(kTurnThreads), 0, st, a, f, tile, turned, items);
+    if (a.neighbours) hipLaunchKernelGGL((k_rotary<T, true, PAIRS>), grid, dim3(kTurnThreads), 0, st, a, f, tile, turned, items, moved);
+    else hipLaunchKernelGGL((k_rotary<T, false, PAIRS>), grid, dim3(kTurnThreads), 0, st, a, f, tile, turned, items, moved);
     return hipGetLastError();
 }
 

@@ -117,6 +117,19 @@ def test_in_place_strides_and_odd_addresses(ctx, neighbours, typ):
     assert torch.equal(ctx.rotary(x[:1].expand(3, 9, 5, 23), r, p[:, :1].expand(2, 3, 9)), ctx.rotary(x[:1].contiguous(), r, p[:, :1].contiguous()).expand(3, 9, 5, 23))
 
 
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("neighbours", [False, True])
+@pytest.mark.parametrize("pairs,dim", [((1,), 2), ((2, 1), 9), ((4, 3), 14), ((5, 4), 20), ((8, 9), 34), ((20, 31), 102), ((13, 13, 9), 76), ((100, 111), 423)])
+def test_in_place_is_out_of_place(ctx, pairs, dim, neighbours, typ):
+    """(Pieces in part in the one, moved ones in the other.)"""
+    from paper_2308_09187_amd import qgx
+    r = qgx.Rotary.by_base(pairs, neighbours=neighbours)
+    x = torch.randn(3, 50, 5, dim, device="cuda").to(TYPES[typ])
+    p = torch.randint(-1000, 1000, (len(pairs), 3, 50), dtype=torch.int32, device="cuda")
+    want = ctx.rotary(x, r, p)
+    assert ctx.rotary(x, r, p, out=x) is x and torch.equal(x, want)
+
+
 def test_far_positions_and_their_ends(ctx):
     """Positions of all 31 bits: the angle in binary64, reduced there, is good to 2^31 2^-53 = 2.4e-7 radians, 4 u."""
     from paper_2308_09187_amd import qgx
