@@ -40,7 +40,7 @@ __device__ __forceinline__ uint32_t kept_code(float u, uint32_t at, uint32_t wor
 // Four codes rounded away from zero where the draw d, 16 bits, is below 2^16 times the remainder of |u|, u16 = 2^16 u.  With T = ceil(2^16 |u|), a whole
 // number of 23 bits, the magnitude's negative is (d - T) >> 16: its byte 2 is b = 256 - magnitude, or 0.  Of a negative element the code is b ^ 0x80, of
 // another (b ^ 0x7F) + 1, which never carries into the next byte, so that four are put right in their word.  (One element after the other took 8 operations
-// each for these 5: 8 x 4096 x 2048 bfloat16 51 us.)
+// each for these 5: 8 x 4096 x 2048 bfloat16 51 us, with these and addresses of 32 bits 45.)
 __device__ __forceinline__ uint32_t kept_less(float u16, uint32_t draw)
 {
     int minus_T;
