@@ -339,6 +339,48 @@ class _GroupCall:
         self.scratch = ctx._need_bytes.value
 
 
+def _looks(t):
+    """All that a call's checks see of a tensor: shape, steps, type and device."""
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
+
+
+class _GradientCall:
+    """What is the same in every weight gradient of tensors that look alike."""
+
+    def __init__(self, ctx, kept, dy, dw, db):
+        self.rows = code, wk, rows, out, _, step = ctx._rows(dy, "dy")
+        cols, lead = kept.shape[-1], dy.shape[:-2]
+        _need(dy.dim() >= 2 and kept.shape[:-1] == dy.shape[:-1] and kept._device == dy.get_device(), "dy: [.., out] of the kept rows, on their device")
+        _need(dw is not None, "dw: where the gradient goes")
+        for t, shape, name in ((dw, lead + (cols, out), "dw"), (db, lead + (out,), "db")):
+            _need(t is None or (t.get_device() == dy.get_device() and t.dtype == torch.float32 and t.shape == shape and
+                                (wk == 0 or (t[0] if lead else t).is_contiguous())),
+                  "%s: float32 of shape %s, each worker's contiguous, on dy's device", name, tuple(shape))
+        self.dw_step, self.db_step = dw.stride(0) if lead else 0, db.stride(0) if lead and db is not None else 0
+        ctx._check(ctx.lib.qgx_weight_gradient_scratch(ctx._h, code, wk, rows, cols, out, step, ctx._need_ref))
+        self.scratch = ctx._need_bytes.value
+
+
+class _RotaryCall:
+    """What is the same in every rotation of tensors that look alike.  out None: a new tensor."""
+
+    def __init__(self, x, out, positions, axes):
+        self.src = src = Context._heads(x, "x")
+        if out is None:
+            step = src.heads * src.dim
+            self.dst = _Heads(None, src.dtype, src.heads, src.dim, src.workers, src.batch, src.tokens, src.batch * src.tokens * step, src.tokens * step, step, src.dim)
+        else:
+            _need(out.shape == x.shape and out.dtype == x.dtype and out.get_device() == x.get_device(), "out: of x's shape and type, on its device")
+            self.dst = Context._heads(out, "out")
+        ps, step, sh = positions.shape, positions.stride(), x.shape
+        n = len(ps)
+        _need(positions.dtype == torch.int32 and positions.get_device() == x.get_device() and n >= 2 and ps[0] == axes and ps[-1] == sh[-3] and
+              (n == 2 or ps[1:] == sh[:-2]) and (ps[-1] <= 1 or step[-1] == 1),
+              "positions: int32 [axes, tokens] or [axes, .., tokens], tokens contiguous, on x's device")
+        self.steps = step[0], step[1] if n == 4 else 0, step[-2] if n > 2 else 0
+        self.src_ref, self.dst_ref = C.addressof(self.src), C.addressof(self.dst)
+
+
 class TensorList:
     """Gradient tensors of the K workers and where they belong in V; made by Context.tensor_list.  Holds the tensors."""
 
@@ -384,7 +426,7 @@ class Context:
         self._h = C.c_void_p()
         self._need_bytes = C.c_uint64()           # where the scratch functions answer
         self._need_ref = C.addressof(self._need_bytes)
-        self._group_calls = {}
+        self._calls = {}                          # what calls of the same shapes share, by how their tensors look
         self._like = torch.empty(0, dtype=torch.uint8, device=device)
         self._table, self._n_sym = 0, {}          # the table selected; symbols of each table that was set
         with torch.cuda.device(device):
@@ -683,6 +725,12 @@ class Context:
         return dtable
 
     # -- an image or video model's block --------------------------------------------------------------
+    def _laid_out(self, key, call):
+        if len(self._calls) >= 512:
+            self._calls.clear()
+        self._calls[key] = call
+        return call
+
     def new_checkpoint(self, shape, stream=None):
         """Memory for an activation of this shape, the last dimension its columns (its contents are what checkpoint or group_norm put
         there)."""
@@ -737,23 +785,13 @@ class Context:
     def weight_gradient(self, kept: Checkpoint, dy, dw, db=None, stream=None):
         """Gradients of x W + b from the kept x [workers, rows, cols] and dy [workers, rows, out] (or both without workers): dw float32
         [workers, cols, out] and db [workers, out], runs of V's rows say, are written.  Returns dw."""
-        code, wk, rows, out, gw, gr = self._rows(dy, "dy")
-        cols = kept.shape[-1]
-        _need(dy.dim() >= 2 and kept.shape[:-1] == dy.shape[:-1] and kept._device == dy.get_device(), "dy: [.., out] of the kept rows, on their device")
-        lead = dy.shape[:-2]
-        _need(dw is not None, "dw: where the gradient goes")
-        for t, shape, name in ((dw, lead + (cols, out), "dw"), (db, lead + (out,), "db")):
-            if t is None:
-                continue
-            _need(t.get_device() == dy.get_device() and t.dtype == torch.float32 and t.shape == shape and (wk == 0 or (t[0] if lead else t).is_contiguous()),
-                  "%s: float32 of shape %s, each worker's contiguous, on dy's device", name, tuple(shape))
-        need, scratch = self._need_bytes, None
-        st = self.lib.qgx_weight_gradient_scratch(self._h, code, wk, rows, cols, out, gr, self._need_ref)
-        if not st:
-            if need.value:
-                scratch = _empty(dy, (need.value,), torch.uint8, stream)
-            st = self.lib.qgx_weight_gradient(self._h, kept._ref, code, wk, rows, out, dy.data_ptr(), gw, gr, dw.data_ptr(), dw.stride(0) if lead else 0,
-                                              None if db is None else db.data_ptr(), db.stride(0) if lead and db is not None else 0, None if scratch is None else scratch.data_ptr(), need.value, _handle(stream, dy))
+        key = (kept.shape, kept._device, _looks(dy), _looks(dw), _looks(db))
+        call = self._calls.get(key) or self._laid_out(key, _GradientCall(self, kept, dy, dw, db))
+        code, wk, rows, out, gw, gr = call.rows
+        size = call.scratch
+        scratch = _empty(dy, (size,), torch.uint8, stream) if size else None
+        st = self.lib.qgx_weight_gradient(self._h, kept._ref, code, wk, rows, out, dy.data_ptr(), gw, gr, dw.data_ptr(), call.dw_step,
+                                          None if db is None else db.data_ptr(), call.db_step, scratch.data_ptr() if size else None, size, _handle(stream, dy))
         if st:
             self._check(st)
         return dw
@@ -778,15 +816,9 @@ class Context:
         return cls._places(t, name)
 
     def _group_call(self, t, groups, activation, slope, backward, name):
-        """The call for tensors of t's shape, steps, type and device, worked out once for each."""
+        """The call for tensors of t's shape, steps, type and device."""
         key = (t.shape, t.stride(), t.dtype, t.get_device(), groups, activation, slope, backward)
-        call = self._group_calls.get(key)
-        if call is None:
-            call = _GroupCall(self, t, groups, activation, slope, backward, name)
-            if len(self._group_calls) >= 256:
-                self._group_calls.clear()
-            self._group_calls[key] = call
-        return call
+        return self._calls.get(key) or self._laid_out(key, _GroupCall(self, t, groups, activation, slope, backward, name))
 
     @staticmethod
     def _channel_parameter(t, call, name):
@@ -891,22 +923,14 @@ class Context:
     def rotary(self, x, rotary: Rotary, positions, back=False, out=None, stream=None):
         """x [.., batch, tokens, heads, dim] turned by its tokens' positions, int32 [axes, tokens] (the same for all sequences) or [axes, ..,
         tokens] of x's leading dimensions.  back: by the angles' negatives, the backward pass.  out may be x."""
-        src = self._heads(x, "x")
-        dst = src
-        if out is None:
+        new = out is None
+        if new:
             out = _empty_like(x, stream)
-            step = src.heads * src.dim
-            dst = _Heads(out.data_ptr(), src.dtype, src.heads, src.dim, src.workers, src.batch, src.tokens, src.batch * src.tokens * step, src.tokens * step, step, src.dim)
-        elif out is not x:
-            _need(out.shape == x.shape and out.dtype == x.dtype and out.get_device() == x.get_device(), "out: of x's shape and type, on its device")
-            dst = self._heads(out, "out")
-        ps, pst, sh = positions.shape, positions.stride(), x.shape
-        n = len(ps)
-        if not (positions.dtype == torch.int32 and positions.get_device() == x.get_device() and n >= 2 and ps[0] == len(rotary.pairs) and ps[-1] == sh[-3] and
-                (n == 2 or ps[1:] == sh[:-2]) and (ps[-1] <= 1 or pst[-1] == 1)):
-            raise QgxError(ERR_ARG, "positions: int32 [axes, tokens] or [axes, .., tokens], tokens contiguous, on x's device")
-        st = self.lib.qgx_rotate(self._h, rotary._ref, positions.data_ptr(), pst[0], pst[1] if n == 4 else 0, pst[-2] if n > 2 else 0,
-                                 C.addressof(src), C.addressof(dst), back, _handle(stream, x))
+        key = (_looks(x), _looks(positions), len(rotary.pairs), None if new else _looks(out))
+        call = self._calls.get(key) or self._laid_out(key, _RotaryCall(x, None if new else out, positions, len(rotary.pairs)))
+        call.src.data, call.dst.data = x.data_ptr(), out.data_ptr()
+        axis, worker, batch = call.steps
+        st = self.lib.qgx_rotate(self._h, rotary._ref, positions.data_ptr(), axis, worker, batch, call.src_ref, call.dst_ref, back, _handle(stream, x))
         if st:
             self._check(st)
         return out
