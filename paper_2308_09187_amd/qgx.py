@@ -176,6 +176,14 @@ def _empty(like, shape, dtype, stream):
         return like.new_empty(shape, dtype=dtype)
 
 
+def _more(like, shape, stream):
+    """Memory of like's type on its device (1.2 us)."""
+    if stream is None:
+        return like.new_empty(shape)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape)
+
+
 def _parameter(t, shape, name):
     """Address of a contiguous binary32 parameter, or of a run of one; None stays None."""
     if t is None:
@@ -261,11 +269,11 @@ class Checkpoint:
 
     @classmethod
     def _made(cls, like, shape, stream):
-        """Memory for rows of this shape on like's device: one piece, of which codes and powers become tensors when they are asked for."""
+        """Memory for rows of this shape on the device of like, of bytes: one piece, of which codes and powers become tensors when they are asked for."""
         rows, split, size = _kept_layout(shape)
         k = cls.__new__(cls)
         k.shape, k._device, k._codes = shape, like.get_device(), None
-        k._memory = _empty(like, (size,), torch.uint8, stream)
+        k._memory = _more(like, size, stream)
         at = k._memory.data_ptr()
         k._c = _Kept(at, at + split, rows, shape[-1])
         k._ref = C.addressof(k._c)
@@ -328,6 +336,7 @@ class _GroupCall:
         self.workers, batch = sh[0] if n == 4 else 1, sh[-3] if n > 2 else 1
         self.shape = _GroupShape(code, act, slope, groups, self.workers, batch, sh[-2], sh[-1])
         self.device, self.channels, self.statistics = t.get_device(), sh[-1:], sh[:-2] + (groups,)
+        self.like = t.new_empty(0, dtype=torch.float32)
         self.both, self.gradients = (2,) + self.statistics, sh[:1] + sh[-1:] if n == 4 else sh[-1:]
         self.first = Context._places(t, name)            # t itself, x or dy
         run = sh[-2] * sh[-1]
@@ -756,7 +765,10 @@ class Context:
         code, wk, rows, cols, xw, xr = self._kept_rows(x, "x")
         if out is None:
             _need(cols >= 1, "x: columns")
-            out = Checkpoint._made(x, x.shape, stream)
+            like = self._like
+            if x.get_device() != like.get_device():
+                like = x.new_empty(0, dtype=torch.uint8)
+            out = Checkpoint._made(like, x.shape, stream)
         else:
             _need(out.shape == x.shape and out._device == x.get_device(), "out: a checkpoint of x's shape, on its device")
         _need(call_id is None or 0 <= call_id < 1 << 32, "call_id: 32 bits")
@@ -858,7 +870,7 @@ class Context:
             kept = keep._ref
         mean = rstd = m = r = None
         if save:
-            mean, rstd = _empty(x, call.both, torch.float32, stream).unbind(0)
+            mean, rstd = _more(call.like, call.both, stream).unbind(0)
             m, r = mean.data_ptr(), rstd.data_ptr()
         size = call.scratch
         scratch = _empty(x, (size,), torch.uint8, stream) if size else None
