@@ -983,11 +983,10 @@ __global__ __launch_bounds__(kPartThreads) void k_group_back_channels(GroupArgs 
         }
 }
 
-// A group's means of g h and g from its channels' sums.
-__global__ __launch_bounds__(256) void k_group_back_join(GroupArgs a)
+// A group's means of g h and g from its channels' sums.  s: four numbers of LDS.
+__device__ __forceinline__ void join_group(const GroupArgs& a, uint32_t sample, uint32_t g, float* s)
 {
-    __shared__ float s[4];
-    const uint32_t sample = blockIdx.y, g = blockIdx.x, entries = a.parts * a.per;
+    const uint32_t entries = a.parts * a.per;
     const float* from = a.scratch + (size_t)sample * a.parts * 2u * a.channels + g * a.per;
     float gh = 0.0f, gs = 0.0f;
     for (uint32_t i = threadIdx.x; i < entries; i += 256u) {
@@ -1005,6 +1004,43 @@ __global__ __launch_bounds__(256) void k_group_back_join(GroupArgs a)
         a.sums[to] = gh / all;
         a.sums[groups + to] = gs / all;
     }
+}
+
+// A worker's parameters' gradients: its samples' and parts' sums, of sixteen channels by sixteen runs side by side.  (Of 64 channels by four, 770 of them took
+// 18 us.)  s: [runs][channels].
+constexpr uint32_t kJoinChannels = 16, kJoinRuns = 16;
+__device__ __forceinline__ void join_parameters(const GroupArgs& a, uint32_t batch, uint32_t k, uint32_t which, uint32_t first, float* s)
+{
+    const uint32_t i = threadIdx.x % kJoinChannels, run = threadIdx.x / kJoinChannels, c = first + i, entries = batch * a.parts;
+    float* to = which ? a.db : a.dw;
+    if (!to) return;
+    float sum = 0.0f;
+    if (c < a.channels) {
+        const float* from = a.scratch + ((size_t)k * entries * 2u + which) * a.channels + c;
+#pragma unroll 8
+        for (uint32_t e = run; e < entries; e += kJoinRuns) sum += from[(size_t)e * 2u * a.channels];
+    }
+    s[threadIdx.x] = sum;
+    __syncthreads();
+    if (run == 0 && c < a.channels) {
+#pragma unroll
+        for (uint32_t r = 1; r < kJoinRuns; ++r) sum += s[r * kJoinChannels + i];
+        to[k * a.param_stride + c] = sum;
+    }
+    __syncthreads();
+}
+
+// Both, in one launch: the first `group_blocks` workgroups take the `joins` groups of all samples, the others the parameters of all workers.
+__global__ __launch_bounds__(kJoinChannels * kJoinRuns) void k_group_back_join(GroupArgs a, uint32_t batch, uint64_t joins, uint32_t group_blocks, uint64_t columns)
+{
+    __shared__ float s[kJoinChannels * kJoinRuns];
+    if (blockIdx.x < group_blocks) {
+        for (uint64_t u = blockIdx.x; u < joins; u += group_blocks) join_group(a, (uint32_t)(u / a.groups), (uint32_t)(u % a.groups), s);
+        return;
+    }
+    const uint32_t each = (a.channels + kJoinChannels - 1u) / kJoinChannels;
+    for (uint64_t u = blockIdx.x - group_blocks; u < columns; u += gridDim.x - group_blocks)
+        join_parameters(a, batch, (uint32_t)(u / 2u / each), (uint32_t)(u % 2u), (uint32_t)(u / 2u % each) * kJoinChannels, s);
 }
 
 template <typename T, bool KEPT, bool SHORT>
@@ -1048,31 +1084,6 @@ __global__ __launch_bounds__(kPartThreads) void k_group_back_apply(GroupArgs a, 
             for (int c = 0; c < W; ++c) dz[c] = rstd[c] * fmaf(h[c], minus_m2[c], fmaf(dz[c], w[c], minus_m1[c]));
             store_place(dx + (p + i * steps) * a.y_place, at, dz);
         }
-    }
-}
-
-// A worker's parameters' gradients: its samples' and parts' sums, of sixteen channels by sixteen runs side by side.  (Of 64 channels by four, 770 of them took
-// 18 us.)
-constexpr uint32_t kJoinChannels = 16, kJoinRuns = 16;
-__global__ __launch_bounds__(kJoinChannels * kJoinRuns) void k_group_parameters(GroupArgs a, uint32_t batch)
-{
-    __shared__ float s[kJoinRuns][kJoinChannels];
-    const uint32_t k = blockIdx.y, which = blockIdx.z, i = threadIdx.x % kJoinChannels, run = threadIdx.x / kJoinChannels, c = blockIdx.x * kJoinChannels + i;
-    const uint32_t entries = batch * a.parts;
-    float* to = which ? a.db : a.dw;
-    if (!to) return;
-    float sum = 0.0f;
-    if (c < a.channels) {
-        const float* from = a.scratch + ((size_t)k * entries * 2u + which) * a.channels + c;
-#pragma unroll 8
-        for (uint32_t e = run; e < entries; e += kJoinRuns) sum += from[(size_t)e * 2u * a.channels];
-    }
-    s[run][i] = sum;
-    __syncthreads();
-    if (run == 0 && c < a.channels) {
-#pragma unroll
-        for (uint32_t r = 1; r < kJoinRuns; ++r) sum += s[r][i];
-        to[k * a.param_stride + c] = sum;
     }
 }
 
@@ -1218,6 +1229,15 @@ static hipError_t launch_back_whole(const GroupArgs& a, uint32_t batch, const Gr
     return p.threads == 512u ? launch_back_whole_as<T, 512, 8, KEPT>(a, batch, p, st) : launch_back_whole_as<T, 1024, 8, KEPT>(a, batch, p, st);
 }
 
+// The groups' sums (of parts) and the parameters'.
+static void launch_join(const GroupArgs& a, uint32_t batch, bool parts, hipStream_t st)
+{
+    const uint64_t joins = parts && a.y ? (uint64_t)a.samples * a.groups : 0u;
+    const uint64_t columns = a.dw || a.db ? 2u * (uint64_t)a.workers * ((a.channels + kJoinChannels - 1u) / kJoinChannels) : 0u;
+    const uint32_t most = 1u << 22, group_blocks = (uint32_t)(joins < most ? joins : most), blocks = group_blocks + (uint32_t)(columns < most ? columns : most);
+    if (blocks) hipLaunchKernelGGL(k_group_back_join, dim3(blocks), dim3(kJoinChannels * kJoinRuns), 0, st, a, batch, joins, group_blocks, columns);
+}
+
 template <typename T, bool KEPT, bool SHORT>
 static hipError_t launch_back(const GroupArgs& a, uint32_t batch, const GroupPlan& p, hipStream_t st)
 {
@@ -1225,10 +1245,8 @@ static hipError_t launch_back(const GroupArgs& a, uint32_t batch, const GroupPla
         if (p.whole) return launch_back_whole<T, KEPT>(a, batch, p, st);
     const dim3 grid(a.parts, a.spans, a.samples);
     hipLaunchKernelGGL((k_group_back_channels<T, KEPT, SHORT>), grid, dim3(kPartThreads), 0, st, a, batch);
-    if (a.y) {
-        hipLaunchKernelGGL(k_group_back_join, dim3(a.groups, a.samples), dim3(256), 0, st, a);
-        hipLaunchKernelGGL((k_group_back_apply<T, KEPT, SHORT>), grid, dim3(kPartThreads), 0, st, a, batch);
-    }
+    launch_join(a, batch, true, st);
+    if (a.y) hipLaunchKernelGGL((k_group_back_apply<T, KEPT, SHORT>), grid, dim3(kPartThreads), 0, st, a, batch);
     return hipGetLastError();
 }
 
@@ -1245,6 +1263,7 @@ hipError_t launch_group_norm_back(int dtype, const GroupArgs& args, uint32_t wor
     GroupArgs a = args;
     if (!a.y && !a.dw && !a.db) return hipSuccess;
     deal(a, plan);
+    a.workers = workers;
     if (a.apart && !a.y) a.units = 0u;                     // no groups' workgroups
     const uint32_t batch = a.samples / workers;
     if (batch && a.places) {
@@ -1253,10 +1272,10 @@ hipError_t launch_group_norm_back(int dtype, const GroupArgs& args, uint32_t wor
                                                 : launch_back_of<__bf16>(a, batch, plan, st);
         if (e != hipSuccess) return e;
     }
-    if ((!a.dw && !a.db) || (plan.whole && (batch == 1u || plan.apart))) return hipSuccess;
-    // (no samples or places: sums of nothing)
-    hipLaunchKernelGGL(k_group_parameters, dim3((a.channels + kJoinChannels - 1u) / kJoinChannels, workers, 2u), dim3(kJoinChannels * kJoinRuns), 0, st, a,
-                       a.places ? batch : 0u);
+    // (parts: made in the launch that joins them; no samples or places: sums of nothing)
+    if (!plan.whole && batch && a.places) return hipSuccess;
+    if (plan.whole && (batch == 1u || plan.apart)) return hipSuccess;
+    launch_join(a, a.places ? batch : 0u, false, st);
     return hipGetLastError();
 }
 

@@ -385,7 +385,7 @@ struct GroupArgs {
     float* db;
     uint64_t x_worker, x_batch, x_place, dy_worker, dy_batch, dy_place, y_worker, y_batch, y_place, param_stride;
     uint64_t code_place, power_place;      // from a place's codes and powers to the next's
-    uint32_t samples, batch, places, channels, groups, per;    // samples = workers * batch; per = channels of a group
+    uint32_t samples, workers, places, channels, groups, per;  // samples = workers * batch; per = channels of a group
     int32_t activation;
     float slope, eps;
     uint8_t* keep_codes;        // where x is kept as well, or null
