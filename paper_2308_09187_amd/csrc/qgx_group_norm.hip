@@ -1135,7 +1135,7 @@ GroupPlan group_plan(int dtype, uint32_t workers, uint32_t samples, uint32_t pla
         p.spans = ceil_div(channels, p.span);
         const uint32_t steps = 256u / ceil_div(p.span, W);
         // two or three workgroups for every compute unit, but a turn for each of them (4 x 65536 x 128 bfloat16 forward, 1, 2, 3, 4 of them: 55, 49, 50,
-        // 51 us; 6 x 17332 x 184 binary32 backward 120, 98, 85, 88; 20 x 4301 x 30 forward 19, with four turns at least 30)
+        // 51 us; 6 x 17332 x 184 binary32 backward 120, 98, 85, 88, 77 since; 20 x 4301 x 30 forward 19, with four turns at least 30)
         const uint32_t want = max(1u, ceil_div((backward ? 3u : 2u) * n_cu, (uint64_t)samples * p.spans));
         p.part = max(ceil_div(places, want), steps * (uint32_t)(backward ? kBackTurns : kPartTurns));
         p.parts = ceil_div(places, p.part);
