@@ -20,17 +20,48 @@ __device__ __forceinline__ float2 cos_sin_of(double turns)
 // The frequencies come with the launch; PAIRS: as many as there is room for (the fewer, the sooner a launch is made).
 template <int PAIRS> struct Frequencies { double turns[PAIRS]; };
 
+template <int BYTES> struct Bytes { static constexpr int value = BYTES; };
+typedef uint32_t Word __attribute__((aligned(2)));         // at any element
+
 // A thread's piece of a head: pairs from the item's first on, or elements that stay as they are.
-template <typename T, bool NEIGHBOURS>
+// REST: of 16-bit elements, where there are some behind the pairs, which are copied as they are (through binary32 a signalling NaN would become a quiet one).
+template <typename T, bool NEIGHBOURS, bool REST>
 struct HeadPiece {
     static constexpr int W = kPiece<T>;
     uint32_t c;                                            // its first element, in the first half where pairs are apart
     int left;                                              // elements of it that are there
     bool turned;
     float v[W], u[W];
+    uint32_t word[4];                                      // of elements that stay: a piece, or runs of 8, 4 and 2 bytes
+
+    // Bit by bit of their number, instead of element by element.  (12 x 3890 tokens of 11 x 78 binary16, neighbours, six elements behind the pairs 61 us, so 41; of
+    // binary32, at most three, this is no gain.)
+    template <typename F> __device__ __forceinline__ void runs(F&& copy)
+    {
+        const uint32_t n = (uint32_t)max(left, 0);
+        if (n & 4u) {
+            copy(c, &word[0], Bytes<4>{});
+            copy(c + 2u, &word[1], Bytes<4>{});
+        }
+        if (n & 2u) copy(c + (n & 4u), &word[2], Bytes<4>{});
+        if (n & 1u) copy(c + (n & 6u), &word[3], Bytes<2>{});
+    }
 
     __device__ __forceinline__ void load(const T* in, uint32_t P)
     {
+        if (REST && !turned) {
+            if (left >= W) {
+                const nt_u32x4 x = load_bits(in + c);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) word[i] = x[i];
+                return;
+            }
+            runs([&](uint32_t at, uint32_t* to, auto bytes) {
+                if constexpr (decltype(bytes)::value == 4) *to = *reinterpret_cast<const Word*>(in + at);
+                else *to = *reinterpret_cast<const uint16_t*>(in + at);
+            });
+            return;
+        }
         load_piece(in + c, left, v);
         if (!NEIGHBOURS && turned) load_piece(in + P + c, left, u);
     }
@@ -60,18 +91,29 @@ struct HeadPiece {
             x = t;
         }
     }
-    __device__ __forceinline__ void store(T* out, uint32_t P) const
+    __device__ __forceinline__ void store(T* out, uint32_t P)
     {
         auto put = [&](T* p, const float (&x)[W]) {
             if (left >= W) stream_piece(p, x);
             else store_piece(p, left, x);
         };
+        if (REST && !turned) {
+            if (left >= W) {
+                *reinterpret_cast<Piece<T>*>(out + c) = __builtin_bit_cast(Piece<T>, nt_u32x4{word[0], word[1], word[2], word[3]});
+                return;
+            }
+            runs([&](uint32_t at, uint32_t* from, auto bytes) {
+                if constexpr (decltype(bytes)::value == 4) *reinterpret_cast<Word*>(out + at) = *from;
+                else *reinterpret_cast<uint16_t*>(out + at) = (uint16_t)*from;
+            });
+            return;
+        }
         put(out + c, v);
         if (!NEIGHBOURS && turned) put(out + P + c, u);
     }
 };
 
-template <typename T, bool NEIGHBOURS, int PAIRS>
+template <typename T, bool NEIGHBOURS, int PAIRS, bool REST>
 __global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, Frequencies<PAIRS> f, uint32_t tile_tokens, uint32_t turned, uint32_t items, uint32_t moved)
 {
     constexpr int W = kPiece<T>;
@@ -105,7 +147,7 @@ __global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, Frequenci
         const uint32_t heads_at_once = items <= kTurnThreads ? kTurnThreads / items : 1u, rows = count * a.heads;
         const uint32_t row0 = threadIdx.x / items, next_token = heads_at_once / a.heads, next_head = heads_at_once % a.heads;
         for (uint32_t item = threadIdx.x % items; item < items && row0 < heads_at_once; item += items <= kTurnThreads ? items : kTurnThreads) {
-            HeadPiece<T, NEIGHBOURS> x[2];
+            HeadPiece<T, NEIGHBOURS, REST> x[2];
             const bool turns = item < turned;
             const uint32_t c = turns ? item * W - (item + 1u == turned ? moved * (W / kPairs) : 0u) : 2u * P + (item - turned) * W, pair = item * kPairs;
             const int left = turns ? (NEIGHBOURS ? (int)(2u * P - c) : (int)(P - c)) : (int)(a.dim - c);
@@ -156,8 +198,15 @@ static hipError_t launch_rotary_as(const RotaryArgs& a, const double* turns, uin
     const uint32_t pairs_of = a.neighbours ? W / 2u : W, moved = a.in != a.out && a.pairs >= pairs_of ? turned * pairs_of - a.pairs : 0u;
     Frequencies<PAIRS> f;
     for (uint32_t p = 0; p < (uint32_t)PAIRS; ++p) f.turns[p] = p < a.pairs ? turns[p] : 0.0;
-    if (a.neighbours) hipLaunchKernelGGL((k_rotary<T, true, PAIRS>), grid, dim3(kTurnThreads), 0, st, a, f, tile, turned, items, moved);
-    else hipLaunchKernelGGL((k_rotary<T, false, PAIRS>), grid, dim3(kTurnThreads), 0, st, a, f, tile, turned, items, moved);
+    const dim3 block(kTurnThreads);
+    if constexpr (sizeof(T) == 2)
+        if (items > turned) {
+            if (a.neighbours) hipLaunchKernelGGL((k_rotary<T, true, PAIRS, true>), grid, block, 0, st, a, f, tile, turned, items, moved);
+            else hipLaunchKernelGGL((k_rotary<T, false, PAIRS, true>), grid, block, 0, st, a, f, tile, turned, items, moved);
+            return hipGetLastError();
+        }
+    if (a.neighbours) hipLaunchKernelGGL((k_rotary<T, true, PAIRS, false>), grid, block, 0, st, a, f, tile, turned, items, moved);
+    else hipLaunchKernelGGL((k_rotary<T, false, PAIRS, false>), grid, block, 0, st, a, f, tile, turned, items, moved);
     return hipGetLastError();
 }
 

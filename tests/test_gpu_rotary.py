@@ -119,6 +119,23 @@ def test_in_place_strides_and_odd_addresses(ctx, neighbours, typ):
 
 @pytest.mark.parametrize("typ", TYPES)
 @pytest.mark.parametrize("neighbours", [False, True])
+@pytest.mark.parametrize("rest", range(1, 18))
+def test_elements_behind_the_pairs_stay(ctx, rest, neighbours, typ):
+    """Any number of them, bit for bit (NaN payloads too), at an odd address, and nothing beside them is written."""
+    from paper_2308_09187_amd import qgx
+    r = qgx.Rotary.by_base((3, 2), neighbours=neighbours)
+    bits = torch.int32 if typ == "f32" else torch.int16
+    x = torch.randn(2, 9, 3, 10 + rest + 4, device="cuda").to(TYPES[typ])[..., 1:11 + rest]
+    x[..., 10:].view(bits).random_()
+    out = torch.full((2, 9, 3, 10 + rest + 6), 5.0, device="cuda", dtype=TYPES[typ])
+    p = torch.randint(-50, 50, (2, 9), dtype=torch.int32, device="cuda")
+    y = ctx.rotary(x, r, p, out=out[..., 3:13 + rest])
+    assert torch.equal(y[..., 10:].contiguous().view(bits), x[..., 10:].contiguous().view(bits))
+    assert torch.equal(y[..., :10], ctx.rotary(x[..., :10], r, p)) and bool((out[..., :3] == 5).all()) and bool((out[..., 13 + rest:] == 5).all())
+
+
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("neighbours", [False, True])
 @pytest.mark.parametrize("pairs,dim", [((1,), 2), ((2, 1), 9), ((4, 3), 14), ((5, 4), 20), ((8, 9), 34), ((20, 31), 102), ((13, 13, 9), 76), ((100, 111), 423)])
 def test_in_place_is_out_of_place(ctx, pairs, dim, neighbours, typ):
     """(Pieces in part in the one, moved ones in the other.)"""
