@@ -60,10 +60,10 @@ class Model:
         K, B, P, D, H = *tokens.shape, self.D, self.H
         p = {name: self.run_of(X, name) for name in self.sizes}
         x0 = embedding[tokens]                            # [K, B, P, D], channels last
-        kept0 = ctx.new_checkpoint(x0.shape)
+        kept0 = ctx.new_checkpoint(x0.shape)              # tensor 0 of those that are kept in this call
         x, mean, rstd = ctx.group_norm(x0, self.G, p["norm_w"], p["norm_b"], activation="silu", keep=kept0, call_id=call)
         x = x.view(K, B * P, D)
-        kept = ctx.checkpoint(x, call)
+        kept = ctx.checkpoint(x, call, tensor=1)
 
         def heads(t):                                     # [K, B P, D] -> [K, B, P, H, D / H]
             return t.view(K, B, P, H, D // H)
@@ -78,7 +78,7 @@ class Model:
         scale = 1.0 / math.sqrt(D // H)
         attention = torch.softmax((q @ k.transpose(-1, -2)) * scale, -1)
         mixed = flat(attention @ v)
-        kept_mixed = ctx.checkpoint(mixed, call)
+        kept_mixed = ctx.checkpoint(mixed, call, tensor=2)
         logits = mixed @ p["head"]
         logp = torch.log_softmax(logits, -1)
         seen = targets.view(K, B * P) >= 0

@@ -470,6 +470,7 @@ typedef struct {
     uint8_t* codes;        /* DEVICE, 16-byte aligned */
     uint8_t* powers;       /* DEVICE */
     uint64_t rows, cols;   /* rows of all workers, < 2^31; 1 <= cols <= 2^24 */
+    uint32_t tensor;       /* which of the tensors kept under one call number, < 2^24: its place in the draws */
 } qgx_kept;
 
 /* Keeps workers x rows rows of cols elements (row r of worker k at x + k * x_worker + r * x_row, kept as row k * rows + r of `out`).
@@ -477,9 +478,11 @@ typedef struct {
  * restored to x's type is finite: magnitudes beyond 127 of those are 127 of them).  Rounding of x 2^-e:
  *   unbiased = 0  to the nearest whole number, ties to even
  *   unbiased = 1  away from zero with the probability of the remainder, by a draw of 16 bits: element c of row r of the whole takes 16 bits of
- *                 Philox4x32-10(key = the context's seed, counter = (c / 8, 2, r, call_id)), the low or high half (c odd) of word (c mod 8) / 2,
- *                 and rounds away iff the draw < remainder * 2^16.  So a product with what was kept has the expectation of the product
- *                 with x to 2^-16 of a step, as the method asks of its vectors.  call_id as in qgx_quantize (the two special values too).
+ *                 Philox4x32-10(key = the context's seed, counter = (c / 8, 2 + 256 * out->tensor, r, call_id)), the low or high half (c odd) of word
+ *                 (c mod 8) / 2, and rounds away iff the draw < remainder * 2^16.  So a product with what was kept has the expectation of the
+ *                 product with x to 2^-16 of a step, as the method asks of its vectors, as long as the other factor does not depend on the same
+ *                 draws: tensors kept under one call number (all of a half-step's, by the special values) need numbers of their own, else what
+ *                 flows back through the one is rounded as the other.  call_id as in qgx_quantize (the two special values too).
  * A block with an infinity or a NaN sets QGX_EBIT_NONFINITE. */
 qgx_status qgx_checkpoint(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t rows, uint64_t cols, const void* x, uint64_t x_worker,
                           uint64_t x_row, int unbiased, uint32_t call_id, const qgx_kept* out, void* stream);

@@ -103,7 +103,7 @@ __global__ __launch_bounds__(kKeepThreads) void k_checkpoint(KeepArgs a, KeptDra
                 for (int c = 0; c < W; ++c) v[h * W + c] = x[c];
             }
             uint32_t word[2];
-            const uint32_t power = kept_codes<8>(v, quad_max(bits), a.top, d.on != 0u, group[i], 0u, (uint32_t)first_row + row[i], call, keys, word);
+            const uint32_t power = kept_codes<8>(v, quad_max(bits), a.top, d.on != 0u, group[i], 0u, (uint32_t)first_row + row[i], d.domain, call, keys, word);
             if (row[i] >= rows) continue;
             *reinterpret_cast<uint2*>(codes + i * kKeepThreads * 8u + to * 8u) = make_uint2(word[0], word[1]);
             if ((to & 3u) == 0u) {

@@ -570,7 +570,7 @@ __device__ __forceinline__ void keep_piece(const GroupArgs& a, const RawPiece<T,
     uint32_t bits = quad_max(largest_bits<T>(raw.bits));
     if constexpr (W == 4) bits = max(bits, (uint32_t)__builtin_amdgcn_mov_dpp((int)bits, 0x141, 0xf, 0xf, true));       // row_half_mirror: the other four lanes
     uint32_t word[W / 4];
-    const uint32_t power = kept_codes<W>(v, bits, a.keep_top, a.draws.on != 0u, channel / 8u, channel / 4u & 1u, row, call, keys, word);
+    const uint32_t power = kept_codes<W>(v, bits, a.keep_top, a.draws.on != 0u, channel / 8u, channel / 4u & 1u, row, a.draws.domain, call, keys, word);
     asm volatile("" : : "v"(word[0]));                     // (made before the next piece's is begun)
     if (!ok) return;
     uint8_t* to = a.keep_codes + (size_t)row * a.channels + channel;                    // (whole blocks: rows without a gap)

@@ -353,6 +353,7 @@ hipError_t launch_position_bias_back(int dtype, const BiasArgs& a, const BucketA
 // ---- an image or video model's block (qgx_checkpoint.hip, qgx_group_norm.hip, qgx_weight_gradient.hip, qgx_rotary.hip) ----
 struct KeptDraws {              // what a call that rounds without bias draws from
     uint32_t seed_lo, seed_hi, call_id, call_mode;   // call_mode: 0: call_id as given; 1, 2: 2(t-1), 2(t-1)+1 from the iteration counter on the device
+    uint32_t domain;            // of the counter: 2 + 256 * the tensor's number (0 and 1 are the vectors' and the game's)
     uint32_t on;                // 0: to nearest
 };
 struct KeepArgs {

@@ -63,8 +63,8 @@ __device__ __forceinline__ uint32_t kept_word(const float (&u16)[4], uint32_t dr
 // The codes of W neighbouring columns, as the words that are stored, and the block's power, from the bits of its largest magnitude.  W = 8: the columns of one
 // Philox block; W = 4: its half `half`.
 template <int W>
-__device__ __forceinline__ uint32_t kept_codes(float (&v)[W], uint32_t bits, uint32_t top, bool draws, uint32_t group, uint32_t half, uint32_t row, uint32_t call,
-                                               const PhiloxKeys& keys, uint32_t (&word)[W / 4])
+__device__ __forceinline__ uint32_t kept_codes(float (&v)[W], uint32_t bits, uint32_t top, bool draws, uint32_t group, uint32_t half, uint32_t row, uint32_t domain,
+                                               uint32_t call, const PhiloxKeys& keys, uint32_t (&word)[W / 4])
 {
     uint32_t power = kept_power(bits);
     uint32_t over = (254u - power) << 23;                  // 2^-e (of zeros it may be anything)
@@ -83,7 +83,7 @@ __device__ __forceinline__ uint32_t kept_codes(float (&v)[W], uint32_t bits, uin
     }
     if (draws) {
         uint32_t w[4];
-        philox4x32_10(group, 2u, row, call, keys, w);
+        philox4x32_10(group, domain, row, call, keys, w);
         if (W == 4 && half) { w[0] = w[2]; w[1] = w[3]; }
         const float over16 = __uint_as_float(over) * wide;
 #pragma unroll

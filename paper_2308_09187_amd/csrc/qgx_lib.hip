@@ -1274,6 +1274,7 @@ static qgx_status check_kept(qgx_ctx* ctx, const char* what, const qgx_kept* kep
 {
     if (kept->cols == 0 || kept->cols > (1u << 24) || kept->rows >= (1ull << 31)) return fail(ctx, QGX_ERR_ARG, "%s: kept rows or columns out of range", what);
     if (kept->rows != rows || kept->cols != cols) return fail(ctx, QGX_ERR_ARG, "%s: kept rows of another shape", what);
+    if (kept->tensor >= (1u << 24)) return fail(ctx, QGX_ERR_ARG, "%s: a kept tensor's number must be below 2^24", what);
     if (rows && (!kept->codes || !kept->powers || !aligned16(kept->codes))) return fail(ctx, QGX_ERR_ARG, "%s: null or misaligned codes or powers", what);
     return QGX_OK;
 }
@@ -1281,11 +1282,12 @@ static qgx_status check_kept(qgx_ctx* ctx, const char* what, const qgx_kept* kep
 static uint32_t kept_blocks(uint64_t cols) { return (uint32_t)((cols + QGX_KEPT_BLOCK - 1u) / QGX_KEPT_BLOCK); }
 static uint32_t kept_top(int dtype) { return dtype == QGX_F16 ? kKeptTopF16 : kKeptTop; }
 
-static KeptDraws kept_draws(const qgx_ctx* ctx, int unbiased, uint32_t call_id)
+static KeptDraws kept_draws(const qgx_ctx* ctx, const qgx_kept* out, int unbiased, uint32_t call_id)
 {
     KeptDraws d{};
     d.seed_lo = (uint32_t)ctx->cfg.seed; d.seed_hi = (uint32_t)(ctx->cfg.seed >> 32); d.call_id = call_id;
     d.call_mode = call_id == QGX_CALL_FIRST_HALF ? 1u : call_id == QGX_CALL_SECOND_HALF ? 2u : 0u;
+    d.domain = 2u + 256u * out->tensor;
     d.on = unbiased != 0;
     return d;
 }
@@ -1304,7 +1306,7 @@ qgx_status qgx_checkpoint(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t ro
     KeepArgs a{};
     a.x = x; a.codes = out->codes; a.powers = out->powers; a.x_worker = x_worker; a.x_row = x_row;
     a.rows = (uint32_t)rows; a.batch = 1; a.n_rows = (uint32_t)(workers * rows); a.cols = (uint32_t)cols; a.blocks = kept_blocks(cols); a.top = kept_top(dtype);
-    QGX_HIP(ctx, launch_checkpoint(dtype, a, kept_draws(ctx, unbiased, call_id), ctx->d_sc, (hipStream_t)stream));
+    QGX_HIP(ctx, launch_checkpoint(dtype, a, kept_draws(ctx, out, unbiased, call_id), ctx->d_sc, (hipStream_t)stream));
     return QGX_OK;
 }
 
@@ -1472,13 +1474,13 @@ qgx_status qgx_group_norm(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_
     a.y = y->data; a.y_worker = y->s_worker; a.y_batch = y->s_batch; a.y_place = y->s_place;
     a.w = weight; a.b = bias; a.mean = mean; a.rstd = rstd; a.eps = eps; a.scratch = (float*)scratch;
     if (keep && group_keeps(plan, a.channels)) {
-        a.keep_codes = keep->codes; a.keep_powers = keep->powers; a.keep_top = kept_top(shape->dtype); a.draws = kept_draws(ctx, unbiased, call_id);
+        a.keep_codes = keep->codes; a.keep_powers = keep->powers; a.keep_top = kept_top(shape->dtype); a.draws = kept_draws(ctx, keep, unbiased, call_id);
     } else if (keep) {
         KeepArgs k{};
         k.x = x->data; k.codes = keep->codes; k.powers = keep->powers; k.x_worker = x->s_worker; k.x_batch = x->s_batch; k.x_row = x->s_place;
         k.batch = (uint32_t)shape->batch; k.rows = a.places; k.n_rows = a.samples * a.places; k.cols = a.channels; k.blocks = kept_blocks(a.channels);
         k.top = kept_top(shape->dtype);
-        QGX_HIP(ctx, launch_checkpoint(shape->dtype, k, kept_draws(ctx, unbiased, call_id), ctx->d_sc, (hipStream_t)stream));
+        QGX_HIP(ctx, launch_checkpoint(shape->dtype, k, kept_draws(ctx, keep, unbiased, call_id), ctx->d_sc, (hipStream_t)stream));
     }
     QGX_HIP(ctx, launch_group_norm(shape->dtype, a, (uint32_t)shape->workers, plan, ctx->d_sc, (hipStream_t)stream));
     return QGX_OK;

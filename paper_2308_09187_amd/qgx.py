@@ -88,7 +88,7 @@ class _Scores(C.Structure):
 
 
 class _Kept(C.Structure):
-    _fields_ = [("codes", C.c_void_p), ("powers", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64)]
+    _fields_ = [("codes", C.c_void_p), ("powers", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64), ("tensor", C.c_uint32)]
 
 
 class _GroupShape(C.Structure):
@@ -253,10 +253,10 @@ class Buckets:
 
 class Checkpoint:
     """An activation kept in 8 bits, rows of `cols` elements in blocks of 32: codes uint8 [.., 32 * blocks] and powers uint8
-    [.., blocks], contiguous; an element is (code - 128) * 2^(power - 127).  Made by Context.new_checkpoint or
-    Context.checkpoint, or from such tensors."""
+    [.., blocks], contiguous; an element is (code - 128) * 2^(power - 127).  tensor: which of those kept under one call number, a
+    number of its own for each.  Made by Context.new_checkpoint or Context.checkpoint, or from such tensors."""
 
-    def __init__(self, codes, powers, cols):
+    def __init__(self, codes, powers, cols, tensor=0):
         cols = int(cols)
         blocks = (cols + KEPT_BLOCK - 1) // KEPT_BLOCK
         for t, n, name in ((codes, KEPT_BLOCK * blocks, "codes"), (powers, blocks, "powers")):
@@ -264,18 +264,18 @@ class Checkpoint:
         _need(codes.shape[:-1] == powers.shape[:-1] and codes.get_device() == powers.get_device(), "codes and powers: of the same rows")
         self.shape, self._device = codes.shape[:-1] + (cols,), codes.get_device()
         self._memory, self._codes, self._powers = codes, codes, powers
-        self._c = _Kept(codes.data_ptr(), powers.data_ptr(), math.prod(self.shape[:-1]), cols)
+        self._c = _Kept(codes.data_ptr(), powers.data_ptr(), math.prod(self.shape[:-1]), cols, _tensor_number(tensor))
         self._ref = C.addressof(self._c)
 
     @classmethod
-    def _made(cls, like, shape, stream):
+    def _made(cls, like, shape, stream, tensor):
         """Memory for rows of this shape on the device of like, of bytes: one piece, of which codes and powers become tensors when they are asked for."""
         rows, split, size = _kept_layout(shape)
         k = cls.__new__(cls)
         k.shape, k._device, k._codes = shape, like.get_device(), None
         k._memory = _more(like, size, stream)
         at = k._memory.data_ptr()
-        k._c = _Kept(at, at + split, rows, shape[-1])
+        k._c = _Kept(at, at + split, rows, shape[-1], tensor)
         k._ref = C.addressof(k._c)
         return k
 
@@ -284,6 +284,10 @@ class Checkpoint:
         lead = self.shape[:-1]
         blocks = (self.shape[-1] + KEPT_BLOCK - 1) // KEPT_BLOCK
         self._codes, self._powers = self._memory[:split].view(lead + (KEPT_BLOCK * blocks,)), self._memory[split:].view(lead + (blocks,))
+
+    @property
+    def tensor(self):
+        return self._c.tensor
 
     @property
     def codes(self):
@@ -296,6 +300,11 @@ class Checkpoint:
         if self._codes is None:
             self._parts()
         return self._powers
+
+
+def _tensor_number(n):
+    _need(0 <= n < 1 << 24, "tensor: a number below 2^24")
+    return n
 
 
 @functools.lru_cache(maxsize=256)
@@ -740,12 +749,12 @@ class Context:
         self._calls[key] = call
         return call
 
-    def new_checkpoint(self, shape, stream=None):
+    def new_checkpoint(self, shape, stream=None, tensor=0):
         """Memory for an activation of this shape, the last dimension its columns (its contents are what checkpoint or group_norm put
-        there)."""
+        there).  tensor: its number in the draws, another for each of the activations that are kept under one call number."""
         shape = torch.Size(shape)
         _need(len(shape) >= 1 and shape[-1] >= 1, "new_checkpoint: columns")
-        return Checkpoint._made(self._like, shape, stream)
+        return Checkpoint._made(self._like, shape, stream, _tensor_number(tensor))
 
     @staticmethod
     def _kept_rows(x, name):
@@ -759,18 +768,20 @@ class Context:
             _need(x.dim() == 3, "%s: leading dimensions that come down to two of one step each", name)
         return Context._rows(x, name)
 
-    def checkpoint(self, x, call_id=None, out=None, stream=None):
+    def checkpoint(self, x, call_id=None, out=None, stream=None, tensor=None):
         """Keeps x [.., cols] in 8 bits.  call_id None: rounded to nearest; a number (or CALL_FIRST_HALF, CALL_SECOND_HALF): without bias, by
-        draws of that call."""
+        draws of that call and of the tensor's number (None: out's, or 0).  Tensors kept under one call number need numbers of their own: by the same
+        draws, a gradient that has passed through the one would not be independent of the other."""
         code, wk, rows, cols, xw, xr = self._kept_rows(x, "x")
         if out is None:
             _need(cols >= 1, "x: columns")
             like = self._like
             if x.get_device() != like.get_device():
                 like = x.new_empty(0, dtype=torch.uint8)
-            out = Checkpoint._made(like, x.shape, stream)
+            out = Checkpoint._made(like, x.shape, stream, 0 if tensor is None else _tensor_number(tensor))
         else:
             _need(out.shape == x.shape and out._device == x.get_device(), "out: a checkpoint of x's shape, on its device")
+            _need(tensor is None or tensor == out.tensor, "tensor: out has a number of its own")
         _need(call_id is None or 0 <= call_id < 1 << 32, "call_id: 32 bits")
         st = self.lib.qgx_checkpoint(self._h, code, wk, rows, cols, x.data_ptr(), xw, xr, call_id is not None, call_id or 0, out._ref, _handle(stream, x))
         if st:
@@ -852,7 +863,7 @@ class Context:
                    stream=None):
         """Group norm of x [workers, batch, places, channels] (or without workers, or without both) and an activation: "none", "silu",
         "leaky" (slope).  Returns (y, mean, rstd), the last two [.., groups] for the backward pass (save=False: None).  keep: a
-        Checkpoint in which x is kept as well, as checkpoint(x, call_id) would."""
+        Checkpoint in which x is kept as well, as checkpoint(x, call_id, out=keep) would."""
         call = self._group_call(x, groups, activation, slope, 0, "x")
         call.first.data = x.data_ptr()
         w, b = self._channel_parameter(weight, call, "weight"), self._channel_parameter(bias, call, "bias")
