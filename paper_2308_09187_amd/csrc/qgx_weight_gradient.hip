@@ -104,8 +104,8 @@ __global__ __launch_bounds__(kGradThreads) void k_weight_gradient(WeightGradArgs
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
                     u[r] = __float_as_uint(v[r]);
-                    // what the upper half leaves (of an infinity nothing)
-                    if (p + 1 < P) v[r] = (u[r] & 0x7F800000u) == 0x7F800000u ? 0.0f : v[r] - __uint_as_float(u[r] & 0xFFFF0000u);
+                    // what the upper half leaves: of an infinity nothing, of a NaN a NaN (its upper half may be an infinity's)
+                    if (p + 1 < P) v[r] = (u[r] & 0x7FFFFFFFu) == 0x7F800000u ? 0.0f : v[r] - __uint_as_float(u[r] & 0xFFFF0000u);
                 }
                 s_dy[to][p][oct][grad_slot(quad * 4u + c)] = make_uint4(upper_halves(u[0], u[1]), upper_halves(u[2], u[3]), upper_halves(u[4], u[5]), upper_halves(u[6], u[7]));
             }
@@ -366,8 +366,13 @@ __device__ __forceinline__ void weight_gradient_tile(const WeightGradArgs& a, ty
                 most = fmaxf(most, fabsf(left[r]));
             }
             if constexpr (SUMS) add_eight(left, db[j]);
-            // of an infinity the parts after the first are zeros (a NaN, which may hide here, is a NaN in every part)
+            // of an infinity the parts after the first are zeros; of a NaN they are NaNs, and so is the first beside an infinity, which it would else be taken for
+            // where its payload lies in the lower half
             const bool infinite = most > 3.402823466e38f;
+            if (__builtin_expect(infinite, 0)) {
+#pragma unroll
+                for (int r = 0; r < 8; ++r) left[r] = left[r] != left[r] ? __builtin_nanf("") : left[r];
+            }
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 uint32_t w[8];
