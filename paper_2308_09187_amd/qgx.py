@@ -760,10 +760,10 @@ class Context:
     def _kept_rows(x, name):
         """(type, workers, rows, cols, step between workers, between rows) of [.., cols] whose leading dimensions come down to two."""
         if x.dim() > 3:
-            shape, step = x.shape, x.stride()
-            for cut in range(1, x.dim() - 1):              # [a .., b ..]: each run of dimensions one
-                if all(shape[i] == 1 or step[i - 1] == step[i] * shape[i] or shape[i - 1] == 1 for i in range(1, x.dim() - 1) if i != cut):
-                    x = x.view(math.prod(shape[:cut]), math.prod(shape[cut:-1]), shape[-1])
+            lead = [(n, s) for n, s in zip(x.shape[:-1], x.stride()[:-1]) if n != 1]          # (the step of a single index is nothing's)
+            for cut in range(len(lead) + 1):               # [a .., b ..]: each run of dimensions one
+                if x.numel() == 0 or all(lead[i - 1][1] == lead[i][1] * lead[i][0] for i in range(1, len(lead)) if i != cut):
+                    x = x.view(math.prod(n for n, _ in lead[:cut]), math.prod(n for n, _ in lead[cut:]), x.shape[-1])
                     break
             _need(x.dim() == 3, "%s: leading dimensions that come down to two of one step each", name)
         return Context._rows(x, name)
