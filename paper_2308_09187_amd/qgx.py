@@ -279,6 +279,23 @@ class Checkpoint:
         k._ref = C.addressof(k._c)
         return k
 
+    def view(self, shape):
+        """The same rows with other leading dimensions, for a call that counts them in another way; no memory of its own."""
+        shape = torch.Size(shape)
+        _need(len(shape) >= 1 and shape[-1] == self.shape[-1] and math.prod(shape[:-1]) == math.prod(self.shape[:-1]),
+              "view: as many rows, of %d columns", self.shape[-1])
+        k = Checkpoint.__new__(Checkpoint)
+        k.shape, k._device, k._codes = shape, self._device, None
+        if self._codes is None:
+            k._memory = self._memory
+        else:                                              # (codes and powers may be memory of their own)
+            lead = shape[:-1]
+            k._memory = k._codes = self._codes.view(lead + self._codes.shape[-1:])
+            k._powers = self._powers.view(lead + self._powers.shape[-1:])
+        k._c = _Kept(self._c.codes, self._c.powers, self._c.rows, self._c.cols, self._c.tensor)
+        k._ref = C.addressof(k._c)
+        return k
+
     def _parts(self):
         split = _kept_layout(self.shape)[1]
         lead = self.shape[:-1]
@@ -366,9 +383,14 @@ class _GradientCall:
     """What is the same in every weight gradient of tensors that look alike."""
 
     def __init__(self, ctx, kept, dy, dw, db):
-        self.rows = code, wk, rows, out, _, step = ctx._rows(dy, "dy")
-        cols, lead = kept.shape[-1], dy.shape[:-2]
         _need(dy.dim() >= 2 and kept.shape[:-1] == dy.shape[:-1] and kept._device == dy.get_device(), "dy: [.., out] of the kept rows, on their device")
+        cols, lead = kept.shape[-1], dy.shape[:1] if dy.dim() > 2 else ()
+        if dy.dim() > 3:                                   # a worker's rows one step apart
+            try:
+                dy = dy.view(dy.shape[0], math.prod(dy.shape[1:-1]), dy.shape[-1])
+            except RuntimeError:
+                raise QgxError(ERR_ARG, "dy: dimensions between the first and the last that come down to rows of one step") from None
+        self.rows = code, wk, rows, out, _, step = ctx._rows(dy, "dy")
         _need(dw is not None, "dw: where the gradient goes")
         for t, shape, name in ((dw, lead + (cols, out), "dw"), (db, lead + (out,), "db")):
             _need(t is None or (t.get_device() == dy.get_device() and t.dtype == torch.float32 and t.shape == shape and
@@ -806,8 +828,9 @@ class Context:
         return out
 
     def weight_gradient(self, kept: Checkpoint, dy, dw, db=None, stream=None):
-        """Gradients of x W + b from the kept x [workers, rows, cols] and dy [workers, rows, out] (or both without workers): dw float32
-        [workers, cols, out] and db [workers, out], runs of V's rows say, are written.  Returns dw."""
+        """Gradients of x W + b from the kept x [workers, rows, cols] and dy [workers, rows, out], or [workers, batch, places, ..] of both, or [rows, ..]
+        without workers (Checkpoint.view gives x the dimensions it needs): dw float32 [workers, cols, out] and db [workers, out], runs
+        of V's rows say, are written.  Returns dw."""
         key = (kept.shape, kept._device, _looks(dy), _looks(dw), _looks(db))
         call = self._calls.get(key) or self._laid_out(key, _GradientCall(self, kept, dy, dw, db))
         code, wk, rows, out, gw, gr = call.rows
