@@ -525,7 +525,7 @@ typedef struct {
 qgx_status qgx_group_norm_scratch(qgx_ctx* ctx, const qgx_group_shape* shape, int backward, uint64_t* bytes);
 /*   weight, bias  DEVICE [channels] binary32, each or both NULL (1 and 0)
  *   y             may be x (with its strides)
- *   mean, rstd    DEVICE [workers][batch][groups] binary32, each or both NULL
+ *   mean, rstd    DEVICE [workers][batch][groups] binary32, each or both NULL; NaNs where there are no places
  *   keep          NULL, or where x's rows are kept as well, as qgx_checkpoint does with `unbiased` and `call_id`: row (worker, batch, place) */
 qgx_status qgx_group_norm(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_places* x, const float* weight, const float* bias, float eps,
                           const qgx_places* y, float* mean, float* rstd, const qgx_kept* keep, int unbiased, uint32_t call_id,

@@ -890,6 +890,16 @@ __global__ __launch_bounds__(256) void k_group_join(GroupArgs a)
     }
 }
 
+// Samples without places: 0 / 0 each.
+__global__ __launch_bounds__(256) void k_group_no_places(GroupArgs a)
+{
+    const uint64_t n = (uint64_t)a.samples * a.groups;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256u) {
+        if (a.mean) a.mean[i] = __builtin_nanf("");
+        if (a.rstd) a.rstd[i] = __builtin_nanf("");
+    }
+}
+
 template <typename T, bool SHORT>
 __global__ __launch_bounds__(kPartThreads) void k_group_apply(GroupArgs a, uint32_t batch)
 {
@@ -1200,6 +1210,14 @@ static hipError_t launch_forward_of(GroupArgs& a, uint32_t batch, const GroupPla
 }
 
 bool group_keeps(const GroupPlan& plan, uint32_t channels) { return plan.one && plan.span % QGX_KEPT_BLOCK == 0u && channels % QGX_KEPT_BLOCK == 0u; }
+
+hipError_t launch_group_no_places(const GroupArgs& a, hipStream_t st)
+{
+    const uint64_t n = (uint64_t)a.samples * a.groups;
+    if (n == 0u || (!a.mean && !a.rstd)) return hipSuccess;
+    hipLaunchKernelGGL(k_group_no_places, dim3(ceil_div(n < (1ull << 24) ? n : 1ull << 24, 256u)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
 
 hipError_t launch_group_norm(int dtype, const GroupArgs& args, uint32_t workers, const GroupPlan& plan, Scalars* sc, hipStream_t st)
 {

@@ -411,6 +411,7 @@ struct GroupPlan {
 };
 GroupPlan group_plan(int dtype, uint32_t workers, uint32_t samples, uint32_t places, uint32_t channels, uint32_t groups, bool backward, uint32_t n_cu);
 bool group_keeps(const GroupPlan& plan, uint32_t channels);     // whether the kernel of this plan keeps x as well
+hipError_t launch_group_no_places(const GroupArgs& a, hipStream_t st);      // the statistics of nothing
 hipError_t launch_group_norm(int dtype, const GroupArgs& a, uint32_t workers, const GroupPlan& plan, Scalars* sc, hipStream_t st);
 hipError_t launch_group_norm_back(int dtype, const GroupArgs& a, uint32_t workers, const GroupPlan& plan, hipStream_t st);
 

@@ -1458,18 +1458,24 @@ qgx_status qgx_group_norm(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_
     if (!x || !y) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: null argument");
     if (!(eps >= 0.0f)) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: eps must be >= 0");
     if (keep) s = check_kept(ctx, "qgx_group_norm(keep)", keep, shape->workers * shape->batch * shape->places, shape->channels);
-    if (s != QGX_OK || no_places(shape)) return s;
-    s = check_places(ctx, "qgx_group_norm(x)", shape, x, false);
-    if (s == QGX_OK) s = check_places(ctx, "qgx_group_norm(y)", shape, y, true);
     if (s != QGX_OK) return s;
-    if (x->data == y->data && !same_places(shape, x, y)) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: y at x's memory must have its strides");
+    const bool none = no_places(shape);
+    if (!none) s = check_places(ctx, "qgx_group_norm(x)", shape, x, false);
+    if (!none && s == QGX_OK) s = check_places(ctx, "qgx_group_norm(y)", shape, y, true);
+    if (s != QGX_OK) return s;
+    if (!none && x->data == y->data && !same_places(shape, x, y)) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: y at x's memory must have its strides");
     if (!aligned_to(weight, 4u) || !aligned_to(bias, 4u) || !aligned_to(mean, 4u) || !aligned_to(rstd, 4u))
         return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: binary32 buffers must be 4-byte aligned");
+    GroupArgs a = group_args(shape);
+    if (none) {
+        a.mean = mean; a.rstd = rstd;
+        QGX_HIP(ctx, launch_group_no_places(a, (hipStream_t)stream));
+        return QGX_OK;
+    }
     GroupPlan plan;
     s = plan_of(ctx, "qgx_group_norm", shape, false, plan);
     if (s == QGX_OK) s = check_group_scratch(ctx, "qgx_group_norm", plan, scratch, scratch_bytes);
     if (s != QGX_OK) return s;
-    GroupArgs a = group_args(shape);
     a.x = x->data; a.x_worker = x->s_worker; a.x_batch = x->s_batch; a.x_place = x->s_place;
     a.y = y->data; a.y_worker = y->s_worker; a.y_batch = y->s_batch; a.y_place = y->s_place;
     a.w = weight; a.b = bias; a.mean = mean; a.rstd = rstd; a.eps = eps; a.scratch = (float*)scratch;

@@ -885,7 +885,7 @@ class Context:
     def group_norm(self, x, groups, weight=None, bias=None, eps=1e-5, activation="none", slope=0.01, keep=None, call_id=None, out=None, save=True,
                    stream=None):
         """Group norm of x [workers, batch, places, channels] (or without workers, or without both) and an activation: "none", "silu",
-        "leaky" (slope).  Returns (y, mean, rstd), the last two [.., groups] for the backward pass (save=False: None).  keep: a
+        "leaky" (slope).  Returns (y, mean, rstd), the last two [.., groups] for the backward pass (save=False: None; NaNs of no places).  keep: a
         Checkpoint in which x is kept as well, as checkpoint(x, call_id, out=keep) would."""
         call = self._group_call(x, groups, activation, slope, 0, "x")
         call.first.data = x.data_ptr()
