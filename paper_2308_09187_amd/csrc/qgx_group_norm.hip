@@ -648,7 +648,8 @@ __global__ __launch_bounds__(THREADS, 4) void k_group_norm_one(GroupArgs a, uint
 }
 
 // h and dz of a piece of one group.  A kept element over its group's spread is one product and one sum of its code, with A = scale rstd and B = (-128 scale - mean)
-// rstd (off by 2^-23 of A's 255 steps); `plain`, where the side of 0 decides or B is beyond binary32: by the operations the header names.
+// rstd (off by 2^-23 of A's 255 steps); `plain`, where the side of 0 decides, and where B (and 128 A with it) may be beyond binary32, as of a block that holds
+// another group's far larger values too: by the operations the header names.
 template <typename T, bool KEPT>
 __device__ __forceinline__ void back_values_one(const GroupArgs& a, const RawPiece<T, KEPT>& x, const Places<T, KEPT>& places, const RawPiece<T, false>& dy,
                                                 const Places<T, false>& grads, float mean, float rstd, bool plain, const float (&w)[kPiece<T>],
@@ -658,8 +659,8 @@ __device__ __forceinline__ void back_values_one(const GroupArgs& a, const RawPie
     if constexpr (KEPT) {
         // (one block to a piece: pieces start at multiples of W)
         const float scale = kept_scale(x.powers & 0xFFu);
-        if (!plain) {
-            const float A = scale * rstd, B = fmaf(-128.0f, scale, -mean) * rstd;
+        const float A = scale * rstd, B = fmaf(-128.0f, scale, -mean) * rstd;
+        if (!plain && fabsf(B) < 1e30f) {
 #pragma unroll
             for (int c = 0; c < kPiece<T>; ++c) h[c] = fmaf((float)((x.code[c / 4] >> (8 * (c & 3))) & 0xFFu), A, B);
         } else {

@@ -1,0 +1,54 @@
+"""Group norm backward (qgx_group_norm_backward): groups whose neighbours are no numbers or far larger."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+ROUND = {"f32": U, "bf16": 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2308_09187_amd import qgx as m
+    c = m.Context(1024, 1, 256, seed=78)
+    yield c
+    c.close()
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+@pytest.mark.parametrize("batch", [1, 70])
+def test_small_groups_beside_far_larger_ones(ctx, typ, batch):
+    """Groups that share a block of 32, one of values so large that the block's step times another's rstd is beyond binary32: the small ones were kept as zeros,
+    h = -mean rstd.  One place, groups of one piece.  h is off by 3 u of itself, sums of n terms by n u of their magnitudes, dx by four roundings more."""
+    n = 4 if typ == "f32" else 8
+    C, G = 32, 32 // n
+    g = torch.Generator(device="cuda")
+    g.manual_seed(batch)
+    x = torch.randn(1, batch, 1, C, generator=g, device="cuda") * 1e-3
+    x[..., :n] = 3.3e38 / n
+    x = x.to(TYPES[typ])
+    dy = torch.randn(x.shape, generator=g, device="cuda").to(TYPES[typ])
+    y, mean, rstd = ctx.group_norm(x, G)
+    assert bool(torch.isfinite(y).all()) and bool(torch.isfinite(rstd).all())
+    kept = ctx.checkpoint(x)
+    assert float(ctx.restore(kept)[..., n:].abs().max()) == 0
+    dw, db = torch.empty(1, C, device="cuda"), torch.empty(1, C, device="cuda")
+    dx = ctx.group_norm_backward(dy, kept, G, None, None, mean, rstd, dw=dw, db=db)
+    v, d = (t.double().cpu().numpy().reshape(batch, G, n)[:, 1:] for t in (ctx.restore(kept), dy))
+    mu, r = (t.double().cpu().numpy().reshape(batch, G, 1)[:, 1:] for t in (mean, rstd))
+    h = (v - mu) * r
+    m1, m2 = d.mean(-1, keepdims=True), (d * h).mean(-1, keepdims=True)
+    a1, a2 = np.abs(d).mean(-1, keepdims=True), np.abs(d * h).mean(-1, keepdims=True)
+    want = (d - m1 - h * m2) * r
+    err = (16 + n) * U * r * (np.abs(d) + a1 + np.abs(h) * a2)
+    err = err + ROUND[typ] * (np.abs(want) + err)
+    assert (np.abs(dx.double().cpu().numpy().reshape(batch, G, n)[:, 1:] - want) <= err).all()
+    terms = np.abs(d * h).sum(0).reshape(-1)
+    assert (np.abs(dw.double().cpu().numpy()[0, n:] - (d * h).sum(0).reshape(-1)) <= (batch + 8) * U * terms).all()
+    for kind in ("silu", "leaky"):
+        assert bool(torch.isfinite(ctx.group_norm_backward(dy, kept, G, None, None, mean, rstd, kind)[..., n:]).all())
