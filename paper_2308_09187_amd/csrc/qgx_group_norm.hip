@@ -648,8 +648,9 @@ __global__ __launch_bounds__(THREADS, 4) void k_group_norm_one(GroupArgs a, uint
 }
 
 // h and dz of a piece of one group.  A kept element over its group's spread is one product and one sum of its code, with A = scale rstd and B = (-128 scale - mean)
-// rstd (off by 2^-23 of A's 255 steps); `plain`, where the side of 0 decides, and where B (and 128 A with it) may be beyond binary32, as of a block that holds
-// another group's far larger values too: by the operations the header names.
+// rstd (off by 2^-23 of A's 255 steps); `plain`, where the side of 0 decides, and where B (and 128 A with it) may be beyond binary32, as of a nearly constant group
+// far from 0 or of a block that holds another group's far larger values too: by the operations the header names.  (Thread by thread: what a group gets is no matter of
+// its neighbours.)
 template <typename T, bool KEPT>
 __device__ __forceinline__ void back_values_one(const GroupArgs& a, const RawPiece<T, KEPT>& x, const Places<T, KEPT>& places, const RawPiece<T, false>& dy,
                                                 const Places<T, false>& grads, float mean, float rstd, bool plain, const float (&w)[kPiece<T>],
@@ -705,7 +706,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_group_norm_back_one(GroupArgs a,
     const size_t g = (size_t)sample * a.groups + (first + j * W) / a.per;
     float w[W], b[W], dw[W], db[W];
     const float one_mean = a.mean_in[g], one_rstd = a.rstd_in[g];
-    const bool plain = a.activation == QGX_ACT_LEAKY || __builtin_amdgcn_ballot_w64(!(fabsf(one_mean) * one_rstd < 1e30f)) != 0ull;   // (nearly constant, far from 0)
+    const bool plain = a.activation == QGX_ACT_LEAKY;
     channel_parameters<W>(a.w, at, 1.0f, w);
     channel_parameters<W>(a.b, at, 0.0f, b);
 #pragma unroll

@@ -1,4 +1,6 @@
 """Group norm backward (qgx_group_norm_backward): groups whose neighbours are no numbers or far larger."""
+import math
+
 import numpy as np
 import pytest
 
@@ -52,3 +54,29 @@ def test_small_groups_beside_far_larger_ones(ctx, typ, batch):
     assert (np.abs(dw.double().cpu().numpy()[0, n:] - (d * h).sum(0).reshape(-1)) <= (batch + 8) * U * terms).all()
     for kind in ("silu", "leaky"):
         assert bool(torch.isfinite(ctx.group_norm_backward(dy, kept, G, None, None, mean, rstd, kind)[..., n:]).all())
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, 3 * 2.0 ** 121])
+@pytest.mark.parametrize("kind", ["none", "silu", "leaky"])
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,P,C,G", [(2, 50, 64, 8), (2, 30, 128, 8), (600, 3, 64, 8), (1100, 3, 64, 8), (2, 9000, 64, 8)])
+def test_a_groups_gradient_is_its_own(ctx, batch, P, C, G, typ, kind, bad):
+    """From kept codes and from x: what a group of another block of 32 holds, no numbers or one far value throughout, leaves every bit of the others."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(P)
+    x, dy = (torch.randn(1, batch, P, C, generator=g, device="cuda").to(TYPES[typ]) for _ in range(2))
+    w, b = torch.randn(C, generator=g, device="cuda"), torch.randn(C, generator=g, device="cuda")
+    _, mean, rstd = ctx.group_norm(x, G, w, b, activation=kind)
+    spoilt, m, r = x.clone(), mean.clone(), rstd.clone()
+    spoilt[..., C - C // G:] = bad                         # the last group, in the last block
+    m[..., -1] = bad
+    r[..., -1] = 1e5 ** 0.5 if math.isfinite(bad) else math.nan
+    for keep in (False, True):
+        got = []
+        for source, mu, rs in ((x, mean, rstd), (spoilt, m, r)):
+            dw, db = torch.empty(1, C, device="cuda"), torch.empty(1, C, device="cuda")
+            dx = ctx.group_norm_backward(dy, ctx.checkpoint(source, 2) if keep else source, G, w, b, mu, rs, kind, dw=dw, db=db)
+            got.append([t[..., :C - 32] for t in (dx, dw, db)])
+        assert all(torch.equal(s, t) for s, t in zip(*got))
+        assert bool(torch.isfinite(got[1][0]).all())
+    ctx.poll_error()
