@@ -561,8 +561,8 @@ typedef struct {
 } qgx_heads;
 
 /* positions DEVICE int32: of axis a, worker k, sequence n, token t at positions[a * p_axis + k * p_worker + n * p_batch + t] (a stride of 0: the same
- * for all).  The angle is reduced in binary64 (good to 1e-9 of a turn at any position), sine and cosine are good to 2^-23, products and
- * sums in binary32, one rounding.  back = 1: by -t, the backward pass (the transposed map, which is its inverse).  out may be in (with its
+ * for all).  The angle is reduced in two binary64 numbers (good to 1e-9 of a turn at any position, of frequencies of at most 1e12), sine and cosine
+ * are good to 2^-23, products and sums in binary32, one rounding.  back = 1: by -t, the backward pass (the transposed map, which is its inverse).  out may be in (with its
  * strides); out's shape is in's. */
 qgx_status qgx_rotate(qgx_ctx* ctx, const qgx_rotary* rotary, const int32_t* positions, uint64_t p_axis, uint64_t p_worker, uint64_t p_batch,
                       const qgx_heads* in, const qgx_heads* out, int back, void* stream);

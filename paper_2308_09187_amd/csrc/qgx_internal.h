@@ -443,6 +443,6 @@ struct RotaryArgs {
     uint32_t axis_end[QGX_MAX_AXES];       // pairs up to an axis' last
     int32_t neighbours, back;
 };
-hipError_t launch_rotary(int dtype, const RotaryArgs& a, const double* turns /* HOST [pairs]: frequencies / 2 pi */, uint32_t n_cu, hipStream_t st);
+hipError_t launch_rotary(int dtype, const RotaryArgs& a, const double* frequencies /* HOST [pairs] */, uint32_t n_cu, hipStream_t st);
 
 }  // namespace qgx

@@ -1554,7 +1554,6 @@ qgx_status qgx_rotate(qgx_ctx* ctx, const qgx_rotary* rotary, const int32_t* pos
     if (!ctx || !rotary || !in || !out || !rotary->frequencies) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: null argument");
     if (rotary->axes == 0 || rotary->axes > QGX_MAX_AXES) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: 1 .. %u axes", QGX_MAX_AXES);
     RotaryArgs a{};
-    double turns[QGX_MAX_PAIRS];
     uint64_t pairs = 0;
     for (uint32_t i = 0; i < rotary->axes; ++i) {
         pairs += rotary->pairs[i];
@@ -1563,10 +1562,8 @@ qgx_status qgx_rotate(qgx_ctx* ctx, const qgx_rotary* rotary, const int32_t* pos
     }
     if (pairs == 0 || pairs > QGX_MAX_PAIRS) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: 1 .. %u pairs", QGX_MAX_PAIRS);
     for (uint32_t i = rotary->axes; i < QGX_MAX_AXES; ++i) a.axis_end[i] = (uint32_t)pairs;
-    for (uint32_t p = 0; p < pairs; ++p) {
+    for (uint32_t p = 0; p < pairs; ++p)
         if (!(std::fabs(rotary->frequencies[p]) <= DBL_MAX)) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: frequency %u is not finite", p);
-        turns[p] = rotary->frequencies[p] * 0.15915494309189533577;                   // 1 / (2 pi)
-    }
     qgx_status s = check_heads(ctx, "qgx_rotate(in)", in, false);
     if (s == QGX_OK) s = check_heads(ctx, "qgx_rotate(out)", out, true);
     if (s != QGX_OK) return s;
@@ -1586,7 +1583,7 @@ qgx_status qgx_rotate(qgx_ctx* ctx, const qgx_rotary* rotary, const int32_t* pos
     a.batch = (uint32_t)in->batch; a.tokens = (uint32_t)in->tokens; a.heads = in->heads; a.dim = in->dim; a.pairs = (uint32_t)pairs;
     a.n_tokens = (uint32_t)(in->workers * in->batch * in->tokens);
     a.neighbours = rotary->neighbours != 0; a.back = back != 0;
-    QGX_HIP(ctx, launch_rotary(in->dtype, a, turns, ctx->n_simd / 4u, (hipStream_t)stream));
+    QGX_HIP(ctx, launch_rotary(in->dtype, a, rotary->frequencies, ctx->n_simd / 4u, (hipStream_t)stream));
     return QGX_OK;
 }
 

@@ -8,17 +8,23 @@ namespace qgx {
 constexpr uint32_t kTurnThreads = 256;
 constexpr uint32_t kTurnAngles = 2048, kTurnTokens = 64;   // most sines, and tokens, of a workgroup
 
-// Sine and cosine of an angle in turns, reduced in binary64 before it becomes binary32.
-__device__ __forceinline__ float2 cos_sin_of(double turns)
+// Cosine and sine of position * frequency radians.  The product and its turns are sums of two binary64 numbers each, the second what the rounding of the first left
+// (by fma, exactly), 1 / (2 pi) too; whole turns go before anything becomes binary32.  So the angle's own size costs 2^-103 of it, 1e-10 of a turn at 1e21 turns.  (In one
+// binary64 number it was 5e-8 of a turn at the farthest position of frequency 1.)
+__device__ __forceinline__ float2 cos_sin_of(int32_t position, double frequency)
 {
-    const float r = (float)(turns - rint(turns));
+    constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57;          // 1 / (2 pi)
+    const double at = (double)position, angle = at * frequency, angle_rest = fma(at, frequency, -angle);
+    const double turns = angle * kTurn, rest = fma(angle, kTurn, -turns) + fma(angle, kTurnRest, angle_rest * kTurn);
+    const double left = (turns - rint(turns)) + rest;
+    const float r = (float)(left - rint(left));
     float s, c;
     sincospif(2.0f * r, &s, &c);
     return make_float2(c, s);
 }
 
 // The frequencies come with the launch; PAIRS: as many as there is room for (the fewer, the sooner a launch is made).
-template <int PAIRS> struct Frequencies { double turns[PAIRS]; };
+template <int PAIRS> struct Frequencies { double radians[PAIRS]; };
 
 template <int BYTES> struct Bytes { static constexpr int value = BYTES; };
 typedef uint32_t Word __attribute__((aligned(2)));         // at any element
@@ -133,7 +139,7 @@ __global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, Frequenci
             for (uint32_t x = 0; x + 1 < QGX_MAX_AXES; ++x) axis += p >= a.axis_end[x];
             const uint32_t k = sequence / a.batch, n = sequence % a.batch;
             const int32_t at = a.positions[axis * a.p_axis + k * a.p_worker + n * a.p_batch + t];
-            const float2 cs = cos_sin_of((double)at * f.turns[p]);
+            const float2 cs = cos_sin_of(at, f.radians[p]);
             s_cos[local * stride + slot] = cs.x;
             s_sin[local * stride + slot] = a.back ? -cs.y : cs.y;
             if (slot == 0u) {
@@ -182,7 +188,7 @@ __global__ __launch_bounds__(kTurnThreads) void k_rotary(RotaryArgs a, Frequenci
 }
 
 template <typename T, int PAIRS>
-static hipError_t launch_rotary_as(const RotaryArgs& a, const double* turns, uint32_t n_cu, hipStream_t st)
+static hipError_t launch_rotary_as(const RotaryArgs& a, const double* frequencies, uint32_t n_cu, hipStream_t st)
 {
     constexpr uint32_t W = kPiece<T>;
     const uint32_t turned = a.neighbours ? (2u * a.pairs + W - 1u) / W : (a.pairs + W - 1u) / W;
@@ -197,7 +203,7 @@ static hipError_t launch_rotary_as(const RotaryArgs& a, const double* turns, uin
     // neighbours in binary32 75 and 60)
     const uint32_t pairs_of = a.neighbours ? W / 2u : W, moved = a.in != a.out && a.pairs >= pairs_of ? turned * pairs_of - a.pairs : 0u;
     Frequencies<PAIRS> f;
-    for (uint32_t p = 0; p < (uint32_t)PAIRS; ++p) f.turns[p] = p < a.pairs ? turns[p] : 0.0;
+    for (uint32_t p = 0; p < (uint32_t)PAIRS; ++p) f.radians[p] = p < a.pairs ? frequencies[p] : 0.0;
     const dim3 block(kTurnThreads);
     if constexpr (sizeof(T) == 2)
         if (items > turned) {
@@ -211,17 +217,17 @@ static hipError_t launch_rotary_as(const RotaryArgs& a, const double* turns, uin
 }
 
 template <typename T>
-static hipError_t launch_rotary_of(const RotaryArgs& a, const double* turns, uint32_t n_cu, hipStream_t st)
+static hipError_t launch_rotary_of(const RotaryArgs& a, const double* frequencies, uint32_t n_cu, hipStream_t st)
 {
-    return a.pairs <= 64u ? launch_rotary_as<T, 64>(a, turns, n_cu, st) : launch_rotary_as<T, (int)QGX_MAX_PAIRS>(a, turns, n_cu, st);
+    return a.pairs <= 64u ? launch_rotary_as<T, 64>(a, frequencies, n_cu, st) : launch_rotary_as<T, (int)QGX_MAX_PAIRS>(a, frequencies, n_cu, st);
 }
 
-hipError_t launch_rotary(int dtype, const RotaryArgs& a, const double* turns, uint32_t n_cu, hipStream_t st)
+hipError_t launch_rotary(int dtype, const RotaryArgs& a, const double* frequencies, uint32_t n_cu, hipStream_t st)
 {
     if (a.n_tokens == 0) return hipSuccess;
-    return dtype == QGX_F32   ? launch_rotary_of<float>(a, turns, n_cu, st)
-           : dtype == QGX_F16 ? launch_rotary_of<_Float16>(a, turns, n_cu, st)
-                              : launch_rotary_of<__bf16>(a, turns, n_cu, st);
+    return dtype == QGX_F32   ? launch_rotary_of<float>(a, frequencies, n_cu, st)
+           : dtype == QGX_F16 ? launch_rotary_of<_Float16>(a, frequencies, n_cu, st)
+                              : launch_rotary_of<__bf16>(a, frequencies, n_cu, st);
 }
 
 }  // namespace qgx
