@@ -550,7 +550,7 @@ typedef struct {
     uint32_t axes;                /* 1 .. QGX_MAX_AXES */
     uint32_t pairs[QGX_MAX_AXES]; /* of each axis; P = their sum, 1 .. QGX_MAX_PAIRS */
     int32_t neighbours;           /* 1: pair p is elements 2 p, 2 p + 1; 0: p, p + P */
-    const double* frequencies;    /* HOST [P], radians a position, finite */
+    const double* frequencies;    /* HOST [P], radians a position, finite times every position (below 2^993) */
 } qgx_rotary;
 typedef struct {
     void* data;                   /* DEVICE; a head's dim elements are contiguous */

@@ -1563,7 +1563,7 @@ qgx_status qgx_rotate(qgx_ctx* ctx, const qgx_rotary* rotary, const int32_t* pos
     if (pairs == 0 || pairs > QGX_MAX_PAIRS) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: 1 .. %u pairs", QGX_MAX_PAIRS);
     for (uint32_t i = rotary->axes; i < QGX_MAX_AXES; ++i) a.axis_end[i] = (uint32_t)pairs;
     for (uint32_t p = 0; p < pairs; ++p)
-        if (!(std::fabs(rotary->frequencies[p]) <= DBL_MAX)) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: frequency %u is not finite", p);
+        if (!(std::fabs(rotary->frequencies[p]) <= DBL_MAX / 2147483648.0)) return fail(ctx, QGX_ERR_ARG, "qgx_rotate: frequency %u is not finite at every position", p);
     qgx_status s = check_heads(ctx, "qgx_rotate(in)", in, false);
     if (s == QGX_OK) s = check_heads(ctx, "qgx_rotate(out)", out, true);
     if (s != QGX_OK) return s;

@@ -339,7 +339,8 @@ class Rotary:
     def __init__(self, pairs, frequencies, neighbours=False):
         pairs, frequencies = [int(n) for n in pairs], [float(f) for f in frequencies]
         _need(1 <= len(pairs) <= MAX_AXES and all(n >= 0 for n in pairs) and 1 <= sum(pairs) <= MAX_PAIRS, "Rotary: 1 .. %d axes, 1 .. %d pairs", MAX_AXES, MAX_PAIRS)
-        _need(len(frequencies) == sum(pairs) and all(math.isfinite(f) for f in frequencies), "Rotary: a finite frequency for every pair")
+        _need(len(frequencies) == sum(pairs) and all(math.isfinite(f * 2.0 ** 31) for f in frequencies),
+              "Rotary: a frequency for every pair, finite at every position")
         self.pairs, self.neighbours = pairs, bool(neighbours)
         self.frequencies = (C.c_double * len(frequencies))(*frequencies)
         self._c = _Rotary(len(pairs), (C.c_uint32 * MAX_AXES)(*pairs), int(self.neighbours), self.frequencies)
