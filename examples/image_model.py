@@ -4,8 +4,9 @@
 The task: every place of an image of random tokens has to name the token that lies `shift` rows and columns further on, which one attention layer
 learns through rotary positions with two axes.  The model's parameters are runs of the iterate X [d]; per half-step every worker
   - normalises its images by groups of channels with an activation, keeping the input in 8 bits in the same pass,
-  - keeps what the linear layers take in 8 bits as well, rounded without bias (so that their weight gradients, which are linear in it, have
-    the expectation of the exact ones: an unbiased oracle, as the method asks),
+  - keeps what the linear layers take in 8 bits as well, rounded without bias, each tensor by draws of its own (so that their weight gradients, which are
+    linear in it, have the expectation of the exact ones, as the method asks of its oracle; the norm's, of its own kept input, are not linear in that
+    and are off the exact ones by the order of a step squared in expectation),
   - turns queries and keys by their places' rows and columns,
   - writes all gradients, the matrices' from the matrix cores, straight into its row of V [K][d], where they are clipped to one global norm,
 and the workers' rows are quantised, coded, decoded, averaged and stepped by the two extra-gradient half-steps.

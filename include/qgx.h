@@ -530,7 +530,8 @@ qgx_status qgx_group_norm_scratch(qgx_ctx* ctx, const qgx_group_shape* shape, in
 qgx_status qgx_group_norm(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_places* x, const float* weight, const float* bias, float eps,
                           const qgx_places* y, float* mean, float* rstd, const qgx_kept* keep, int unbiased, uint32_t call_id,
                           void* scratch, uint64_t scratch_bytes, void* stream);
-/* Its backward pass, from x or, x NULL, from what was kept of it.  dz = dy act'(z),  g = dz * weight.  Of a leaky unit z is made in
+/* Its backward pass, from x or, x NULL, from what was kept of it (whose gradients are not linear in it: what was kept without bias gives them the
+ * exact ones' expectation but for a bias of the order of its step squared, within a step of a leaky unit's corner of the order of the step).  dz = dy act'(z),  g = dz * weight.  Of a leaky unit z is made in
  * binary32 by one subtraction, two products and one addition as above, each rounded, so that its side of 0 is reproducible (else a kept
  * element's h may be off by 2^-22 of (255 * its step + |mean|) * rstd);
  *   dx = rstd * (g - mean over the group of g - h * mean over the group of g h)          DEVICE, or NULL; may not be dy or x
