@@ -1,7 +1,7 @@
 // Rows kept in 8 bits, and restored (see qgx_kept.h).  A thread has eight columns, which is what one Philox block rounds, four neighbours a block: its largest
 // magnitude is two exchanges between lanes, and no element leaves its thread.  Rows follow each other without a gap, each filled up to whole blocks.
-// Keeping without bias is bound by vector arithmetic: of some 190 issue slots for eight elements Philox takes 100, rounding 46; restoring by memory.
-// (8 x 4096 x 2048 bfloat16: kept 45 us, the bytes alone 31 at 6.5 TB/s; restored 30, 6.7 TB/s.)
+// Keeping without bias is bound by vector arithmetic: of some 190 issue slots for eight elements Philox takes 104, rounding 46; restoring by memory.
+// (8 x 4096 x 2048 bfloat16: kept 46 us, the bytes alone 31 at 6.5 TB/s; restored 30, 6.7 TB/s.)
 #include "qgx_kept.h"
 
 namespace qgx {

@@ -4,7 +4,7 @@
 // Bound by memory.  A thread has W neighbouring channels (16 bytes) of every so manieth place, so that whatever belongs to a channel stays in
 // its registers; sums are made channel by channel (a thread's places one by one, then the threads' of a channel) and only then
 // joined to groups, whose borders may lie anywhere in a piece.  (8 x 16 x 1024 x 256 bfloat16 in 32 groups: forward with the input kept 51 us, backward from
-// that 57, the bytes alone 26 each at 6.5 TB/s; 4 x 65536 x 128 forward, in parts, 47 of 21.)  Where all places of some groups fit a workgroup's registers it has them whole: one
+// that 56, the bytes alone 26 each at 6.5 TB/s; 4 x 65536 x 128 forward, in parts, 47 of 21.)  Where all places of some groups fit a workgroup's registers it has them whole: one
 // launch, x (and dy) cross memory once.  Else the places are dealt to workgroups that leave their channels' sums in scratch, a launch joins
 // them, and a second pass over x makes y or dx.
 #include "qgx_kept.h"

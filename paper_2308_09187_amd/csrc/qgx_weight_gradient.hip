@@ -5,8 +5,9 @@
 // Both operands lie with the summed index (the rows) outermost, the matrix cores take eight consecutive rows of a column from a lane: a thread
 // loads eight rows of four columns, brings them into that order in its registers (codes are decoded on the way) and leaves each
 // column's eight rows, 16 bytes, in LDS, from where a wave's operands are single loads of 16 bytes.
-// Bound by how steadily the matrix cores are fed.  8 x 4096 x 1024 x 4096 bfloat16: 288 us, 955 TFLOP/s (223 for the library's product of operands laid out
-// for it; 240 without decoding and loads); 4 x 65536 x 256 x 320 binary32, three times the products: 171 us with the join of its parts.
+// Bound by how steadily the matrix cores are fed.  In calls one after the other 8 x 4096 x 1024 x 4096 bfloat16: 288 us, 955 TFLOP/s (223 for the library's product
+// of operands laid out for it; 240 without decoding and loads); 4 x 65536 x 256 x 320 binary32, three times the products: 171 us with the join of its parts.
+// (Under a kernel trace, median and least: 327 and 293; 190 and 158, the join 12.)
 #include "qgx_kept.h"
 #include "qgx_plan.h"
 
