@@ -470,7 +470,7 @@ typedef struct {
     uint8_t* codes;        /* DEVICE, 16-byte aligned */
     uint8_t* powers;       /* DEVICE */
     uint64_t rows, cols;   /* rows of all workers, < 2^31; 1 <= cols <= 2^24 */
-    uint32_t tensor;       /* which of the tensors kept under one call number, < 2^24: its place in the draws */
+    uint32_t tensor;       /* which of the tensors kept under one call number, < 2^24: its place in the draws (read where rows are kept) */
 } qgx_kept;
 
 /* Keeps workers x rows rows of cols elements (row r of worker k at x + k * x_worker + r * x_row, kept as row k * rows + r of `out`).

@@ -1274,9 +1274,15 @@ static qgx_status check_kept(qgx_ctx* ctx, const char* what, const qgx_kept* kep
 {
     if (kept->cols == 0 || kept->cols > (1u << 24) || kept->rows >= (1ull << 31)) return fail(ctx, QGX_ERR_ARG, "%s: kept rows or columns out of range", what);
     if (kept->rows != rows || kept->cols != cols) return fail(ctx, QGX_ERR_ARG, "%s: kept rows of another shape", what);
-    if (kept->tensor >= (1u << 24)) return fail(ctx, QGX_ERR_ARG, "%s: a kept tensor's number must be below 2^24", what);
     if (rows && (!kept->codes || !kept->powers || !aligned16(kept->codes))) return fail(ctx, QGX_ERR_ARG, "%s: null or misaligned codes or powers", what);
     return QGX_OK;
+}
+
+// The same of rows that are to be kept: their tensor's number too.
+static qgx_status check_keep(qgx_ctx* ctx, const char* what, const qgx_kept* kept, uint64_t rows, uint64_t cols)
+{
+    if (kept->tensor >= (1u << 24)) return fail(ctx, QGX_ERR_ARG, "%s: a kept tensor's number must be below 2^24", what);
+    return check_kept(ctx, what, kept, rows, cols);
 }
 
 static uint32_t kept_blocks(uint64_t cols) { return (uint32_t)((cols + QGX_KEPT_BLOCK - 1u) / QGX_KEPT_BLOCK); }
@@ -1298,7 +1304,7 @@ qgx_status qgx_checkpoint(qgx_ctx* ctx, int dtype, uint64_t workers, uint64_t ro
     qgx_status s = check_norm(ctx, "qgx_checkpoint", dtype, workers, rows, cols);
     if (s != QGX_OK) return s;
     if (!out) return fail(ctx, QGX_ERR_ARG, "qgx_checkpoint: null argument");
-    s = check_kept(ctx, "qgx_checkpoint", out, workers * rows, cols);
+    s = check_keep(ctx, "qgx_checkpoint", out, workers * rows, cols);
     if (s != QGX_OK) return s;
     if (workers == 0 || rows == 0) return QGX_OK;
     s = check_rows(ctx, "qgx_checkpoint(x)", x, dtype, workers, rows, cols, x_worker, x_row, false);
@@ -1457,7 +1463,7 @@ qgx_status qgx_group_norm(qgx_ctx* ctx, const qgx_group_shape* shape, const qgx_
     if (s != QGX_OK) return s;
     if (!x || !y) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: null argument");
     if (!(eps >= 0.0f)) return fail(ctx, QGX_ERR_ARG, "qgx_group_norm: eps must be >= 0");
-    if (keep) s = check_kept(ctx, "qgx_group_norm(keep)", keep, shape->workers * shape->batch * shape->places, shape->channels);
+    if (keep) s = check_keep(ctx, "qgx_group_norm(keep)", keep, shape->workers * shape->batch * shape->places, shape->channels);
     if (s != QGX_OK) return s;
     const bool none = no_places(shape);
     if (!none) s = check_places(ctx, "qgx_group_norm(x)", shape, x, false);

@@ -139,3 +139,5 @@ def test_refusals(ctx):
     assert qgx.Checkpoint(k.codes, k.powers, 40, tensor=MOST).tensor == MOST and k.tensor == 0
     k._c.tensor = MOST + 1
     refused(lambda: ctx.checkpoint(x, 1, out=k))
+    refused(lambda: ctx.group_norm(x, 4, keep=k, call_id=1))
+    assert torch.equal(ctx.restore(k), x)                  # (what was kept is read without it)
