@@ -364,16 +364,12 @@ __device__ __forceinline__ void weight_gradient_tile(const WeightGradArgs& a, ty
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
                 left[r] = (float)(j ? raw[r].y : raw[r].x);
-                most = fmaxf(most, fabsf(left[r]));
+                most = __builtin_elementwise_maximum(most, fabsf(left[r]));
             }
             if constexpr (SUMS) add_eight(left, db[j]);
-            // of an infinity the parts after the first are zeros; of a NaN they are NaNs, and so is the first beside an infinity, which it would else be taken for
-            // where its payload lies in the lower half
+            // of an infinity the parts after the first are zeros; of a NaN they are NaNs, and so they may be of an infinity beside it (`most` is a NaN then): the
+            // column is one
             const bool infinite = most > 3.402823466e38f;
-            if (__builtin_expect(infinite, 0)) {
-#pragma unroll
-                for (int r = 0; r < 8; ++r) left[r] = left[r] != left[r] ? __builtin_nanf("") : left[r];
-            }
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 uint32_t w[8];
